@@ -279,6 +279,143 @@ moe_status moe_bwd_dw(const moe_cfg* cfg, const void* x, const float* dlogits,
 moe_status moe_product_timing(int32_t on);
 moe_status moe_product_times(double* ms, int32_t* counts);
 
+/* ----------------------------------------------------------------- router */
+
+/* Routing beyond moe_gate_topk's softmax top-k: softmax or sigmoid scores, a
+ * per-expert bias that takes part in the choice but not in the weights (the
+ * load balance of training without an auxiliary loss), experts in groups of
+ * which the best stay, renormalised and scaled weights, masked experts and
+ * padding tokens; with the gradient at the logits.  The logits are those of
+ * moe_gate_topk or of any other product. */
+typedef enum { MOE_SCORE_SOFTMAX = 0, MOE_SCORE_SIGMOID = 1 } moe_score;
+
+typedef struct {
+  int64_t T;          /* tokens */
+  int32_t E;          /* experts, 1..512 (the dispatch and the expert products take up to 64) */
+  int32_t k;          /* choices per token, 1..min(E, 16) (the dispatch takes up to 8) */
+  int32_t score;      /* moe_score */
+  int32_t renorm;     /* 1: weights divided by the sum of the token's chosen scores */
+  int32_t groups;     /* the experts are this many runs of E / groups; 1 = no groups */
+  int32_t top_groups; /* groups that stay, 1..groups; top_groups * (E / groups) >= k */
+  float scale;        /* the weights' factor, finite and > 0 */
+} moe_route_cfg;
+
+/* The router.
+ *   logits [T][E] float, bias [E] float or NULL (0), 16-byte aligned like every array.
+ *   Scores s = softmax(logits[t]) or sigmoid(logits[t][e]); an expert whose logit is
+ *   -inf or NaN is masked for that token (softmax: it has no share), so is one whose
+ *   bias makes its choice value c_e = s_e + bias_e -inf or NaN.  +inf logits share the
+ *   softmax evenly.
+ *   Groups: a group's value is the sum of its two largest c (of the one there is), and
+ *   the top_groups best groups stay (ties: the lowest group first).
+ *   idx [T][k] int32 = the k largest c among the experts that stay, descending, ties by
+ *   lowest index (without bias and groups: by the logits themselves); -1 where no expert
+ *   is left, which every later call takes for a dropped choice.
+ *   w [T][k] float = scale * s of each choice, divided by the chosen scores' sum if
+ *   renorm; 0 where idx is -1 (and where every chosen score underflows).
+ *   load [E] int32 or NULL: the number of choices of each expert is ADDED to it (a
+ *   caller clears it once and counts over as many calls as its bias update spans).
+ *   The values c are compared as doubles: the choice is that of an evaluation in
+ *   64 bits. */
+moe_status moe_route(const moe_route_cfg* cfg, const float* logits, const float* bias, int32_t* idx, float* w,
+                     int32_t* load, moe_stream_t stream);
+
+/* The router's gradient through the weights (none through the choice, reading as in
+ * moe_bwd_dx): dw [T][k] = dL/dw -> dlogits [T][E] float, every element written.
+ *   logits, idx, w as moe_route took and wrote them (with the same cfg); with G =
+ *   sum_r w_r dw_r over the token's choices:
+ *   softmax, renorm: dlogits[e_r] = w_r (dw_r - G / scale); plain: dlogits[j] =
+ *     [j = e_r] w_r dw_r - p_j G;
+ *   sigmoid, renorm: dlogits[e_r] = w_r (1 - s_r)(dw_r - G / scale); plain:
+ *     dlogits[e_r] = w_r (1 - s_r) dw_r; 0 elsewhere.
+ *   An idx outside 0..E-1 takes no part, whatever its w and dw hold.  A row that
+ *   names an expert twice gets the sum of both. */
+moe_status moe_route_bwd(const moe_route_cfg* cfg, const float* logits, const int32_t* idx, const float* w,
+                         const float* dw, float* dlogits, moe_stream_t stream);
+
+/* moe_bwd_dx for a layer whose idx and w come from moe_route: the same chain, with
+ * moe_route_bwd in the place of the softmax gate's backward.  cfg->renorm is not
+ * used; route's T, E and k equal cfg's.  Also out: dw [T][k] float = <dy[t],
+ * expert_out> of each kept choice (0: dropped), the gradient at w. */
+moe_status moe_bwd_dx_route(const moe_cfg* cfg, const moe_route_cfg* route, const void* Wg, const float* logits,
+                            const int32_t* idx, const float* w, const int32_t* slot, const int32_t* row_begin,
+                            const int32_t* row_end, const void* H, const void* expert_out, const void* W1p,
+                            const void* W2p, const void* dy, void* dO, void* dH, void* dXe, float* dw,
+                            float* dlogits, void* dx, void* ws, size_t ws_bytes, moe_stream_t stream);
+
+/* --------------------------------------------------- experts on 4-bit weights */
+
+/* The experts' FFNs on weights held in 4 bits, for serving: tokens are gathered by
+ * the router's choices inside the products and summed with its weights, without
+ * capacity, send buffers or drops; meant for one token up to a short prompt.
+ * A weight matrix [N][K] (out, in; K a multiple of 32) is
+ *   codes [N][K/2] uint8: input 2j in the low, 2j + 1 in the high half of byte j; a
+ *     code is a sign (8) and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6;
+ *   scales [N][K/32] uint8: byte b stands for 2^(b - 127), for 32 consecutive inputs
+ *     (255: NaN; a value past the largest bfloat16 is infinite). */
+typedef struct {
+  int64_t T;       /* tokens; T * k <= 2^21, T * k * max(d, f) <= 2^33 */
+  int32_t d_model; /* multiple of 32, up to 2^20 */
+  int32_t d_ff;    /* multiple of 32, up to 2^20 */
+  int32_t E;       /* 1..512 */
+  int32_t k;       /* 1..16 */
+  int32_t dtype;   /* moe_dtype of x and y */
+  int32_t act;     /* moe_act */
+} moe_w4_cfg;
+
+/* n_rows rows of K floats or bfloat16 (dtype) -> codes and scales.  The scale is the
+ * smallest power of two 2^s, -100 <= s <= 125, with max|group| <= 7 * 2^s, so every
+ * weight is off by at most half the codes' spacing at its place (nearest code, ties to
+ * the even mantissa; past 7 * 2^125 the largest code); a group with an infinite or NaN weight gets the scale byte 255. */
+moe_status moe_w4_quantize(int64_t n_rows, int32_t K, int32_t dtype, const void* W, uint8_t* codes,
+                           uint8_t* scales, moe_stream_t stream);
+
+/* Bytes of device workspace moe_experts_w4 needs (host only; 0 and a message on an
+ * invalid cfg; never falls as T grows). */
+size_t moe_experts_w4_workspace_bytes(const moe_w4_cfg* cfg);
+
+/* y[t] = sum over r of w[t][r] W2_e act(W1_e x_t), e = idx[t][r]; an idx outside
+ * 0..E-1 takes no part, whatever its w holds; a token without a choice gets 0.
+ *   x, y [T][d] dtype; idx [T][k] int32, w [T][k] float; W1 codes [E][f][d/2] and
+ *   scales [E][f][d/32], W2 codes [E][d][f/2] and scales [E][d][f/32].
+ *   Sums in float over products exact in bfloat16 factors: x is bfloat16, or its
+ *   three bfloat16 parts (MOE_F32); act(W1 x) two (three) such parts, so that only y
+ *   is rounded to its type.  The same call gives the same bits.  Tokens do not mix;
+ *   the order of a token's sums depends on T, d and f only.
+ *   ws: moe_experts_w4_workspace_bytes(cfg) bytes.  Calls that overlap in time need
+ *   separate workspaces. */
+moe_status moe_experts_w4(const moe_w4_cfg* cfg, const void* x, const int32_t* idx, const float* w,
+                          const uint8_t* W1c, const uint8_t* W1s, const uint8_t* W2c, const uint8_t* W2s, void* y,
+                          void* ws, size_t ws_bytes, moe_stream_t stream);
+
+/* ------------------------------------------------- 8-bit activation checkpoint */
+
+/* What the backward reads of the forward's expert buffers, kept in 8 bits between
+ * the two, so that the layers of a model share one set of full-size buffers:
+ * send_buf, H and expert_out, at 1 + 1/16 bytes a value (A = act(H) is rebuilt).
+ *   64 consecutive columns of a row (64j .. 64j + 63) share a float step =
+ *   max|x| / 127; a value is kept as the integer nearest to 127 x / max|x| (ties to
+ *   even) and restored as integer * step, rounded to dtype.  A group under 1e-30
+ *   becomes zeros; a group with an infinite or NaN value becomes NaN.
+ *   Rows [row_begin_e, row_end_e) (row_begin NULL = zeros) of each expert are saved
+ *   and restored; other rows are neither read nor written.
+ * cfg as for moe_expert_ffn_fwd: T, k, G and the flags play no part. */
+/* Bytes of a checkpoint of cfg (host only; 0 and a message on an invalid cfg). */
+size_t moe_ckpt_bytes(const moe_cfg* cfg);
+
+/* Buffers that are NULL are left out of the checkpoint; what was saved before of
+ * them stays. */
+moe_status moe_ckpt_save(const moe_cfg* cfg, const void* send_buf, const void* H, const void* expert_out,
+                         const int32_t* row_begin, const int32_t* row_end, void* ckpt, size_t ckpt_bytes,
+                         moe_stream_t stream);
+
+/* Restores the buffers that are not NULL; A = act(restored H before its rounding),
+ * with or without H.  What is asked for must have been saved, with row ranges that
+ * cover these. */
+moe_status moe_ckpt_load(const moe_cfg* cfg, const void* ckpt, size_t ckpt_bytes, const int32_t* row_begin,
+                         const int32_t* row_end, void* send_buf, void* H, void* A, void* expert_out,
+                         moe_stream_t stream);
+
 /* ------------------------------------------------------------------ block */
 
 /* The pre-LN transformer block whose FFN is the MoE layer, with its

@@ -1,6 +1,7 @@
 // C ABI of the MoE-layer library: host-side validation, then kernel launches.
 // Validation needs no GPU, so every error path can be exercised on a host
 // without one; only a call that passes validation touches the HIP runtime.
+#include <cmath>
 #include <cstddef>
 #include <cstdio>
 #include <cstdarg>
@@ -14,6 +15,8 @@ static_assert(sizeof(moe_cfg) == 56 && offsetof(moe_cfg, ksplit) == 48, "moe_cfg
 static_assert(sizeof(moe_block_cfg) == 96 && offsetof(moe_block_cfg, moe) == 16 &&
                   offsetof(moe_block_cfg, dw_order) == 72,
               "moe_block_cfg layout");
+static_assert(sizeof(moe_route_cfg) == 40 && offsetof(moe_route_cfg, scale) == 32, "moe_route_cfg layout");
+static_assert(sizeof(moe_w4_cfg) == 32 && offsetof(moe_w4_cfg, act) == 28, "moe_w4_cfg layout");
 
 namespace {
 
@@ -356,6 +359,201 @@ moe_status moe_bwd_dw(const moe_cfg* cfg, const void* x, const float* dlogits, c
   hipStream_t s = (hipStream_t)stream;
   lmoe::launch_expert_bwd_dw(*cfg, send_buf, A, dO, dH, row_begin, row_end, dW1, dW2, s);
   lmoe::launch_dwg(*cfg, x, dlogits, dWg, ws, s);
+  return check_launch(fn);
+}
+
+// ----------------------------------------------------------------- router
+namespace {
+
+moe_status check_route(const moe_route_cfg* c, const char* fn) {
+  if (!c) return fail(MOE_EINVAL, "%s: cfg is NULL", fn);
+  if (c->T < 0) return fail(MOE_EINVAL, "%s: T < 0", fn);
+  if (c->T > (int64_t)1 << 31) return fail(MOE_ESHAPE, "%s: T > 2^31 unsupported", fn);
+  if (c->E < 1 || c->E > lmoe::kRouterMaxE)
+    return fail(MOE_ESHAPE, "%s: E=%d outside 1..%d", fn, c->E, lmoe::kRouterMaxE);
+  if (c->k < 1 || c->k > c->E || c->k > lmoe::kRouterMaxK)
+    return fail(MOE_EINVAL, "%s: k=%d outside 1..min(E, %d)", fn, c->k, lmoe::kRouterMaxK);
+  if (c->score != MOE_SCORE_SOFTMAX && c->score != MOE_SCORE_SIGMOID)
+    return fail(MOE_EINVAL, "%s: unknown score %d", fn, c->score);
+  if (c->renorm != 0 && c->renorm != 1) return fail(MOE_EINVAL, "%s: renorm must be 0 or 1", fn);
+  if (c->groups < 1 || c->E % c->groups != 0)
+    return fail(MOE_EINVAL, "%s: groups=%d does not divide E=%d", fn, c->groups, c->E);
+  if (c->top_groups < 1 || c->top_groups > c->groups)
+    return fail(MOE_EINVAL, "%s: top_groups=%d outside 1..groups=%d", fn, c->top_groups, c->groups);
+  if (c->top_groups * (c->E / c->groups) < c->k)
+    return fail(MOE_EINVAL, "%s: %d groups of %d experts hold fewer than k=%d", fn, c->top_groups, c->E / c->groups, c->k);
+  if (!std::isfinite(c->scale) || !(c->scale > 0.f)) return fail(MOE_EINVAL, "%s: scale must be finite and > 0", fn);
+  return MOE_OK;
+}
+
+}  // namespace
+
+moe_status moe_route(const moe_route_cfg* cfg, const float* logits, const float* bias, int32_t* idx, float* w,
+                     int32_t* load, moe_stream_t stream) {
+  const char* fn = "moe_route";
+  CHECK(check_route(cfg, fn));
+  REQUIRE_TPTR(logits); OPTIONAL_PTR(bias); REQUIRE_TPTR(idx); REQUIRE_TPTR(w); OPTIONAL_PTR(load);
+  CHECK(check_device(fn));
+  lmoe::launch_route(*cfg, logits, bias, idx, w, load, (hipStream_t)stream);
+  return check_launch(fn);
+}
+
+moe_status moe_route_bwd(const moe_route_cfg* cfg, const float* logits, const int32_t* idx, const float* w,
+                         const float* dw, float* dlogits, moe_stream_t stream) {
+  const char* fn = "moe_route_bwd";
+  CHECK(check_route(cfg, fn));
+  REQUIRE_TPTR(logits); REQUIRE_TPTR(idx); REQUIRE_TPTR(w); REQUIRE_TPTR(dw); REQUIRE_TPTR(dlogits);
+  if (cfg->T > 0 && (dlogits == logits || dlogits == dw || dlogits == w))
+    return fail(MOE_EINVAL, "%s: dlogits may not alias an input", fn);
+  CHECK(check_device(fn));
+  lmoe::launch_route_bwd(*cfg, logits, idx, w, dw, dlogits, (hipStream_t)stream);
+  return check_launch(fn);
+}
+
+moe_status moe_bwd_dx_route(const moe_cfg* cfg, const moe_route_cfg* route, const void* Wg, const float* logits,
+                            const int32_t* idx, const float* w, const int32_t* slot, const int32_t* row_begin,
+                            const int32_t* row_end, const void* H, const void* expert_out, const void* W1p,
+                            const void* W2p, const void* dy, void* dO, void* dH, void* dXe, float* dw,
+                            float* dlogits, void* dx, void* ws, size_t ws_bytes, moe_stream_t stream) {
+  const char* fn = "moe_bwd_dx_route";
+  CHECK(check_cfg(cfg, fn, true));
+  CHECK(check_route(route, fn));
+  if (route->T != cfg->T || route->E != cfg->E || route->k != cfg->k)
+    return fail(MOE_EINVAL, "%s: cfg and route differ in T, E or k", fn);
+  REQUIRE_PTR(Wg); REQUIRE_TPTR(logits); REQUIRE_TPTR(idx); REQUIRE_TPTR(w); REQUIRE_TPTR(slot);
+  OPTIONAL_PTR(row_begin); REQUIRE_PTR(row_end); REQUIRE_PTR(H); REQUIRE_PTR(expert_out);
+  REQUIRE_PTR(W1p); REQUIRE_PTR(W2p); REQUIRE_TPTR(dy); REQUIRE_PTR(dO); REQUIRE_PTR(dH); REQUIRE_PTR(dXe);
+  REQUIRE_TPTR(dw); REQUIRE_TPTR(dlogits); REQUIRE_TPTR(dx);
+  if (cfg->T > 0 && (dlogits == logits || dlogits == dw || dlogits == w || dw == w))
+    return fail(MOE_EINVAL, "%s: dw and dlogits may not alias each other or an input", fn);
+  const size_t need = lmoe::bwd_dx_ws_bytes(*cfg);
+  if (need > 0) {
+    if (ws == nullptr || ws_bytes < need)
+      return fail(MOE_EWORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need, ws ? ws_bytes : 0);
+    REQUIRE_PTR(ws);
+  }
+  CHECK(check_device(fn));
+  hipStream_t s = (hipStream_t)stream;
+  lmoe::launch_combine_bwd(*cfg, logits, idx, w, slot, expert_out, dy, dO, dlogits, s, dw);
+  lmoe::launch_route_bwd(*route, logits, idx, w, dw, dlogits, s);
+  lmoe::launch_expert_bwd_dx(*cfg, dO, row_begin, row_end, H, W1p, W2p, dH, dXe, ws, s);
+  // Only a plain softmax has a gradient at the experts that were not chosen.
+  moe_cfg c = *cfg;
+  c.renorm = !(route->score == MOE_SCORE_SOFTMAX && route->renorm == 0);
+  lmoe::launch_dispatch_bwd(c, Wg, dlogits, idx, slot, dXe, dx, s);
+  return check_launch(fn);
+}
+
+// --------------------------------------------------- experts on 4-bit weights
+namespace {
+
+moe_status check_w4(const moe_w4_cfg* c, const char* fn) {
+  if (!c) return fail(MOE_EINVAL, "%s: cfg is NULL", fn);
+  if (c->dtype != MOE_F32 && c->dtype != MOE_BF16) return fail(MOE_EDTYPE, "%s: unknown dtype %d", fn, c->dtype);
+  if (c->act < MOE_ACT_IDENTITY || c->act > MOE_ACT_GELU_ERF) return fail(MOE_EINVAL, "%s: unknown act %d", fn, c->act);
+  if (c->T < 0) return fail(MOE_EINVAL, "%s: T < 0", fn);
+  if (c->E < 1 || c->E > lmoe::kRouterMaxE)
+    return fail(MOE_ESHAPE, "%s: E=%d outside 1..%d", fn, c->E, lmoe::kRouterMaxE);
+  if (c->k < 1 || c->k > lmoe::kRouterMaxK)
+    return fail(MOE_EINVAL, "%s: k=%d outside 1..%d", fn, c->k, lmoe::kRouterMaxK);
+  const int32_t most = 1 << 20;
+  if (c->d_model < 32 || c->d_model % 32 != 0 || c->d_model > most)
+    return fail(MOE_ESHAPE, "%s: d_model=%d not a multiple of 32 in 32..%d", fn, c->d_model, most);
+  if (c->d_ff < 32 || c->d_ff % 32 != 0 || c->d_ff > most)
+    return fail(MOE_ESHAPE, "%s: d_ff=%d not a multiple of 32 in 32..%d", fn, c->d_ff, most);
+  if (c->T > (int64_t)1 << 21 || c->T * c->k > (int64_t)1 << 21)
+    return fail(MOE_ESHAPE, "%s: T * k above 2^21", fn);
+  if (c->T * c->k * std::max(c->d_model, c->d_ff) > (int64_t)1 << 33)
+    return fail(MOE_ESHAPE, "%s: T * k * max(d, f) above 2^33", fn);
+  return MOE_OK;
+}
+
+}  // namespace
+
+moe_status moe_w4_quantize(int64_t n_rows, int32_t K, int32_t dtype, const void* W, uint8_t* codes, uint8_t* scales,
+                           moe_stream_t stream) {
+  const char* fn = "moe_w4_quantize";
+  if (dtype != MOE_F32 && dtype != MOE_BF16) return fail(MOE_EDTYPE, "%s: unknown dtype %d", fn, dtype);
+  if (n_rows < 0) return fail(MOE_EINVAL, "%s: n_rows < 0", fn);
+  if (K < 32 || K % 32 != 0) return fail(MOE_ESHAPE, "%s: K=%d not a positive multiple of 32", fn, K);
+  if (n_rows > ((int64_t)1 << 40) / K) return fail(MOE_ESHAPE, "%s: n_rows * K above 2^40", fn);
+  if (n_rows > 0) {
+    REQUIRE_PTR(W); REQUIRE_PTR(codes); REQUIRE_PTR(scales);
+    if (W == codes || W == scales || codes == scales) return fail(MOE_EINVAL, "%s: arrays may not alias", fn);
+  }
+  CHECK(check_device(fn));
+  lmoe::launch_w4_quantize(n_rows, K, dtype, W, codes, scales, (hipStream_t)stream);
+  return check_launch(fn);
+}
+
+size_t moe_experts_w4_workspace_bytes(const moe_w4_cfg* cfg) {
+  if (check_w4(cfg, "moe_experts_w4_workspace_bytes") != MOE_OK) return 0;
+  return lmoe::experts_w4_ws_bytes(*cfg);
+}
+
+moe_status moe_experts_w4(const moe_w4_cfg* cfg, const void* x, const int32_t* idx, const float* w,
+                          const uint8_t* W1c, const uint8_t* W1s, const uint8_t* W2c, const uint8_t* W2s, void* y,
+                          void* ws, size_t ws_bytes, moe_stream_t stream) {
+  const char* fn = "moe_experts_w4";
+  CHECK(check_w4(cfg, fn));
+  REQUIRE_TPTR(x); REQUIRE_TPTR(idx); REQUIRE_TPTR(w);
+  REQUIRE_PTR(W1c); REQUIRE_PTR(W1s); REQUIRE_PTR(W2c); REQUIRE_PTR(W2s); REQUIRE_TPTR(y);
+  if (cfg->T > 0) {
+    const size_t need = lmoe::experts_w4_ws_bytes(*cfg);
+    if (ws == nullptr || ws_bytes < need)
+      return fail(MOE_EWORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need, ws ? ws_bytes : 0);
+    REQUIRE_PTR(ws);
+  }
+  CHECK(check_device(fn));
+  lmoe::launch_experts_w4(*cfg, x, idx, w, W1c, W1s, W2c, W2s, y, ws, (hipStream_t)stream);
+  return check_launch(fn);
+}
+
+// ------------------------------------------------- 8-bit activation checkpoint
+namespace {
+
+moe_status check_ckpt(const moe_cfg* c, const int32_t* row_begin, const int32_t* row_end, const void* ckpt, size_t bytes,
+                      const char* fn) {
+  CHECK(check_cfg(c, fn, true));
+  OPTIONAL_PTR(row_begin); REQUIRE_PTR(row_end); REQUIRE_PTR(ckpt);
+  const size_t need = lmoe::ckpt_bytes(*c);
+  if (bytes < need) return fail(MOE_EWORKSPACE, "%s: checkpoint of %zu bytes needed, %zu given", fn, need, bytes);
+  return MOE_OK;
+}
+
+}  // namespace
+
+size_t moe_ckpt_bytes(const moe_cfg* cfg) {
+  if (check_cfg(cfg, "moe_ckpt_bytes", true) != MOE_OK) return 0;
+  return lmoe::ckpt_bytes(*cfg);
+}
+
+moe_status moe_ckpt_save(const moe_cfg* cfg, const void* send_buf, const void* H, const void* expert_out,
+                         const int32_t* row_begin, const int32_t* row_end, void* ckpt, size_t ckpt_bytes,
+                         moe_stream_t stream) {
+  const char* fn = "moe_ckpt_save";
+  CHECK(check_ckpt(cfg, row_begin, row_end, ckpt, ckpt_bytes, fn));
+  OPTIONAL_PTR(send_buf); OPTIONAL_PTR(H); OPTIONAL_PTR(expert_out);
+  if (ckpt == send_buf || ckpt == H || ckpt == expert_out) return fail(MOE_EINVAL, "%s: ckpt may not alias a buffer", fn);
+  CHECK(check_device(fn));
+  lmoe::launch_ckpt_save(*cfg, send_buf, H, expert_out, row_begin, row_end, ckpt, (hipStream_t)stream);
+  return check_launch(fn);
+}
+
+moe_status moe_ckpt_load(const moe_cfg* cfg, const void* ckpt, size_t ckpt_bytes, const int32_t* row_begin,
+                         const int32_t* row_end, void* send_buf, void* H, void* A, void* expert_out,
+                         moe_stream_t stream) {
+  const char* fn = "moe_ckpt_load";
+  CHECK(check_ckpt(cfg, row_begin, row_end, ckpt, ckpt_bytes, fn));
+  OPTIONAL_PTR(send_buf); OPTIONAL_PTR(H); OPTIONAL_PTR(A); OPTIONAL_PTR(expert_out);
+  const void* out[4] = {send_buf, H, A, expert_out};
+  for (int i = 0; i < 4; ++i)
+    for (int j = 0; j < i; ++j)
+      if (out[i] != nullptr && out[i] == out[j]) return fail(MOE_EINVAL, "%s: two outputs are one buffer", fn);
+  for (int i = 0; i < 4; ++i)
+    if (out[i] == ckpt) return fail(MOE_EINVAL, "%s: ckpt may not alias a buffer", fn);
+  CHECK(check_device(fn));
+  lmoe::launch_ckpt_load(*cfg, ckpt, row_begin, row_end, send_buf, H, A, expert_out, (hipStream_t)stream);
   return check_launch(fn);
 }
 

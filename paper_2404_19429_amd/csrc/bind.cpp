@@ -25,10 +25,21 @@ struct Abi {   // addresses in the loaded library, given by init()
   decltype(&moe_bwd_dx) bwd_dx;
   decltype(&moe_bwd_dw) bwd_dw;
   decltype(&moe_block_chunked) block_chunked;
+  decltype(&moe_route) route;
+  decltype(&moe_route_bwd) route_bwd;
+  decltype(&moe_bwd_dx_route) bwd_dx_route;
+  decltype(&moe_w4_quantize) w4_quantize;
+  decltype(&moe_experts_w4_workspace_bytes) experts_w4_workspace_bytes;
+  decltype(&moe_experts_w4) experts_w4;
+  decltype(&moe_ckpt_bytes) ckpt_bytes;
+  decltype(&moe_ckpt_save) ckpt_save;
+  decltype(&moe_ckpt_load) ckpt_load;
 } g_abi;
 PyObject* g_stream;      // the module's function from a stream argument to a raw stream
 PyObject* g_cfg_type;    // the ctypes structures
 PyObject* g_block_type;
+PyObject* g_route_type;
+PyObject* g_w4_type;
 
 struct Error {};   // a Python exception is set
 
@@ -91,12 +102,23 @@ void* ptr(PyObject* o, const char* name, at::ScalarType type, Num numel, bool nu
 }
 int64_t numel_or_0(PyObject* o) { return o == Py_None ? 0 : THPVariable_Unpack(o).numel(); }
 
+// The Python type of a ctypes structure.
+template <typename T> PyObject* struct_type();
+template <> PyObject* struct_type<moe_cfg>() { return g_cfg_type; }
+template <> PyObject* struct_type<moe_block_cfg>() { return g_block_type; }
+template <> PyObject* struct_type<moe_route_cfg>() { return g_route_type; }
+template <> PyObject* struct_type<moe_w4_cfg>() { return g_w4_type; }
+
 // A ctypes structure's bytes.
 template <typename T>
 struct Struct {
   Py_buffer buf;
   explicit Struct(PyObject* o) {
-    PyObject* type = std::is_same<T, moe_cfg>::value ? g_cfg_type : g_block_type;
+    PyObject* type = struct_type<T>();
+    if (!type) {
+      PyErr_SetString(PyExc_RuntimeError, "the binding was initialised without this structure");
+      throw Error();
+    }
     const int is = PyObject_IsInstance(o, type);
     if (is == 0) PyErr_Format(PyExc_TypeError, "cfg must be a %s", ((PyTypeObject*)type)->tp_name);
     if (is != 1 || PyObject_GetBuffer(o, &buf, PyBUF_SIMPLE) != 0) throw Error();
@@ -456,9 +478,148 @@ ENTRY(block_chunked) {
   });
 }
 
-// init({C ABI name: address}, stream function, moe_cfg type, moe_block_cfg type)
+ENTRY(route) {   // cfg, logits, bias, idx, w, load, stream
+  return entry(n, 7, [&] {
+    Struct<moe_route_cfg> c(a[0]);
+    const Num T = c->T, E = c->E, k = c->k;
+    const float* logits = (const float*)ptr(a[1], "logits", kF32, T * E);
+    const float* bias = (const float*)ptr(a[2], "bias", kF32, E, true);
+    int32_t* idx = (int32_t*)ptr(a[3], "idx", kI32, T * k);
+    float* w = (float*)ptr(a[4], "w", kF32, T * k);
+    int32_t* load = (int32_t*)ptr(a[5], "load", kI32, E, true);
+    void* s = stream_arg(a[6]);
+    return status([&] { return g_abi.route(c, logits, bias, idx, w, load, s); });
+  });
+}
+
+ENTRY(route_bwd) {   // cfg, logits, idx, w, dw, dlogits, stream
+  return entry(n, 7, [&] {
+    Struct<moe_route_cfg> c(a[0]);
+    const Num T = c->T, E = c->E, k = c->k;
+    const float* logits = (const float*)ptr(a[1], "logits", kF32, T * E);
+    const int32_t* idx = (const int32_t*)ptr(a[2], "idx", kI32, T * k);
+    const float* w = (const float*)ptr(a[3], "w", kF32, T * k);
+    const float* dw = (const float*)ptr(a[4], "dw", kF32, T * k);
+    float* dl = (float*)ptr(a[5], "dlogits", kF32, T * E);
+    void* s = stream_arg(a[6]);
+    return status([&] { return g_abi.route_bwd(c, logits, idx, w, dw, dl, s); });
+  });
+}
+
+// cfg, route, Wg, logits, idx, w, slot, row_begin, row_end, H, expert_out, W1p, W2p, dy, dO, dH, dXe, dw, dlogits,
+// dx, ws, stream
+ENTRY(bwd_dx_route) {
+  return entry(n, 22, [&] {
+    Struct<moe_cfg> c(a[0]);
+    Struct<moe_route_cfg> r(a[1]);
+    const auto dt = dtype_of(c);
+    const Num T = c->T, d = c->d_model, f = c->d_ff, E = c->E, k = c->k;
+    const Num nd = expert_numel(c, d), nf = expert_numel(c, f);
+    const size_t need = g_abi.workspace_bytes(c, MOE_CALL_BWD_DX);
+    const void* Wg = ptr(a[2], "Wg", dt, E * d);
+    const float* logits = (const float*)ptr(a[3], "logits", kF32, T * E);
+    const int32_t* idx = (const int32_t*)ptr(a[4], "idx", kI32, T * k);
+    const float* w = (const float*)ptr(a[5], "w", kF32, T * k);
+    const int32_t* slot = (const int32_t*)ptr(a[6], "slot", kI32, T * k);
+    const int32_t* rb = (const int32_t*)ptr(a[7], "row_begin", kI32, E, true);
+    const int32_t* re = (const int32_t*)ptr(a[8], "row_end", kI32, E);
+    const void* H = ptr(a[9], "H", dt, nf);
+    const void* O = ptr(a[10], "expert_out", dt, nd);
+    const void* W1p = ptr(a[11], "W1p", dt, E * f * d);
+    const void* W2p = ptr(a[12], "W2p", dt, E * d * f);
+    const void* dy = ptr(a[13], "dy", dt, T * d);
+    void* dO = ptr(a[14], "dO", dt, nd);
+    void* dH = ptr(a[15], "dH", dt, nf);
+    void* dXe = ptr(a[16], "dXe", dt, nd);
+    float* dw = (float*)ptr(a[17], "dw", kF32, T * k);
+    float* dl = (float*)ptr(a[18], "dlogits", kF32, T * E);
+    void* dx = ptr(a[19], "dx", dt, T * d);
+    void* ws = ptr(a[20], "ws", at::kByte, need, need == 0);
+    const size_t wsn = numel_or_0(a[20]);
+    void* s = stream_arg(a[21]);
+    return status([&] {
+      return g_abi.bwd_dx_route(c, r, Wg, logits, idx, w, slot, rb, re, H, O, W1p, W2p, dy, dO, dH, dXe, dw, dl, dx, ws,
+                                wsn, s);
+    });
+  });
+}
+
+ENTRY(w4_quantize) {   // n_rows, K, dtype, W, codes, scales, stream
+  return entry(n, 7, [&] {
+    const Num rows = big(a[0]), K = big(a[1]), dtype = big(a[2]);
+    if (rows > INT64_MAX || rows < INT64_MIN || K > INT32_MAX || K < INT32_MIN || dtype > INT32_MAX || dtype < INT32_MIN) {
+      PyErr_SetString(PyExc_ValueError, "n_rows, K or dtype out of range");
+      throw Error();
+    }
+    const void* W = ptr(a[3], "W", dtype == MOE_BF16 ? kBf16 : kF32, rows * K);
+    uint8_t* codes = (uint8_t*)ptr(a[4], "codes", at::kByte, rows * (K / 2));
+    uint8_t* scales = (uint8_t*)ptr(a[5], "scales", at::kByte, rows * (K / 32));
+    void* s = stream_arg(a[6]);
+    return status([&] { return g_abi.w4_quantize((int64_t)rows, (int32_t)K, (int32_t)dtype, W, codes, scales, s); });
+  });
+}
+
+ENTRY(experts_w4) {   // cfg, x, idx, w, W1c, W1s, W2c, W2s, y, ws, stream
+  return entry(n, 11, [&] {
+    Struct<moe_w4_cfg> c(a[0]);
+    const auto dt = c->dtype == MOE_BF16 ? kBf16 : kF32;
+    const Num T = c->T, d = c->d_model, f = c->d_ff, E = c->E, k = c->k;
+    const size_t need = T == 0 ? 0 : g_abi.experts_w4_workspace_bytes(c);
+    const void* x = ptr(a[1], "x", dt, T * d);
+    const int32_t* idx = (const int32_t*)ptr(a[2], "idx", kI32, T * k);
+    const float* w = (const float*)ptr(a[3], "w", kF32, T * k);
+    const uint8_t* W1c = (const uint8_t*)ptr(a[4], "W1c", at::kByte, E * f * (d / 2));
+    const uint8_t* W1s = (const uint8_t*)ptr(a[5], "W1s", at::kByte, E * f * (d / 32));
+    const uint8_t* W2c = (const uint8_t*)ptr(a[6], "W2c", at::kByte, E * d * (f / 2));
+    const uint8_t* W2s = (const uint8_t*)ptr(a[7], "W2s", at::kByte, E * d * (f / 32));
+    void* y = ptr(a[8], "y", dt, T * d);
+    void* ws = ptr(a[9], "ws", at::kByte, need, need == 0);
+    const size_t wsn = numel_or_0(a[9]);
+    void* s = stream_arg(a[10]);
+    return status([&] { return g_abi.experts_w4(c, x, idx, w, W1c, W1s, W2c, W2s, y, ws, wsn, s); });
+  });
+}
+
+ENTRY(ckpt_save) {   // cfg, send_buf, H, expert_out, row_begin, row_end, ckpt, stream
+  return entry(n, 8, [&] {
+    Struct<moe_cfg> c(a[0]);
+    const auto dt = dtype_of(c);
+    const Num nd = expert_numel(c, c->d_model), nf = expert_numel(c, c->d_ff), E = c->E;
+    const size_t need = g_abi.ckpt_bytes(c);
+    const void* send = ptr(a[1], "send_buf", dt, nd, true);
+    const void* H = ptr(a[2], "H", dt, nf, true);
+    const void* O = ptr(a[3], "expert_out", dt, nd, true);
+    const int32_t* rb = (const int32_t*)ptr(a[4], "row_begin", kI32, E, true);
+    const int32_t* re = (const int32_t*)ptr(a[5], "row_end", kI32, E);
+    void* ck = ptr(a[6], "ckpt", at::kByte, need);
+    const size_t ckn = numel_or_0(a[6]);
+    void* s = stream_arg(a[7]);
+    return status([&] { return g_abi.ckpt_save(c, send, H, O, rb, re, ck, ckn, s); });
+  });
+}
+
+ENTRY(ckpt_load) {   // cfg, ckpt, row_begin, row_end, send_buf, H, A, expert_out, stream
+  return entry(n, 9, [&] {
+    Struct<moe_cfg> c(a[0]);
+    const auto dt = dtype_of(c);
+    const Num nd = expert_numel(c, c->d_model), nf = expert_numel(c, c->d_ff), E = c->E;
+    const size_t need = g_abi.ckpt_bytes(c);
+    const void* ck = ptr(a[1], "ckpt", at::kByte, need);
+    const size_t ckn = numel_or_0(a[1]);
+    const int32_t* rb = (const int32_t*)ptr(a[2], "row_begin", kI32, E, true);
+    const int32_t* re = (const int32_t*)ptr(a[3], "row_end", kI32, E);
+    void* send = ptr(a[4], "send_buf", dt, nd, true);
+    void* H = ptr(a[5], "H", dt, nf, true);
+    void* A = ptr(a[6], "A", dt, nf, true);
+    void* O = ptr(a[7], "expert_out", dt, nd, true);
+    void* s = stream_arg(a[8]);
+    return status([&] { return g_abi.ckpt_load(c, ck, ckn, rb, re, send, H, A, O, s); });
+  });
+}
+
+// init({C ABI name: address}, stream function, moe_cfg type, moe_block_cfg type[, moe_route_cfg type, moe_w4_cfg type])
 ENTRY(init) {
-  if (n != 4) return PyErr_Format(PyExc_TypeError, "init takes 4 arguments");
+  if (n != 4 && n != 6) return PyErr_Format(PyExc_TypeError, "init takes 4 or 6 arguments");
   PyObject* d = a[0];
   auto set = [&](auto& fn, const char* name) {
     Item it(d, name);
@@ -482,11 +643,20 @@ ENTRY(init) {
     set(g_abi.bwd_dx, "moe_bwd_dx");
     set(g_abi.bwd_dw, "moe_bwd_dw");
     set(g_abi.block_chunked, "moe_block_chunked");
+    set(g_abi.route, "moe_route");
+    set(g_abi.route_bwd, "moe_route_bwd");
+    set(g_abi.bwd_dx_route, "moe_bwd_dx_route");
+    set(g_abi.w4_quantize, "moe_w4_quantize");
+    set(g_abi.experts_w4_workspace_bytes, "moe_experts_w4_workspace_bytes");
+    set(g_abi.experts_w4, "moe_experts_w4");
+    set(g_abi.ckpt_bytes, "moe_ckpt_bytes");
+    set(g_abi.ckpt_save, "moe_ckpt_save");
+    set(g_abi.ckpt_load, "moe_ckpt_load");
   } catch (const Error&) {
     return nullptr;
   }
-  PyObject** slots[] = {&g_stream, &g_cfg_type, &g_block_type};
-  for (int i = 0; i < 3; ++i) {
+  PyObject** slots[] = {&g_stream, &g_cfg_type, &g_block_type, &g_route_type, &g_w4_type};
+  for (int i = 0; i < n - 1; ++i) {
     Py_INCREF(a[i + 1]);
     Py_XSETREF(*slots[i], a[i + 1]);
   }
@@ -505,6 +675,13 @@ PyMethodDef kMethods[] = {METHOD(init),
                           METHOD(bwd_dx),
                           METHOD(bwd_dw),
                           METHOD(block_chunked),
+                          METHOD(route),
+                          METHOD(route_bwd),
+                          METHOD(bwd_dx_route),
+                          METHOD(w4_quantize),
+                          METHOD(experts_w4),
+                          METHOD(ckpt_save),
+                          METHOD(ckpt_load),
                           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_bind", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 

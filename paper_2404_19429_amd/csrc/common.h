@@ -130,6 +130,11 @@ __device__ __forceinline__ float act_bwd(float h, int act) {
   }
 }
 
+// The same with a ReLU that keeps NaN, for results that go to a caller without a loss to show it.
+__device__ __forceinline__ float act_fwd_nan(float h, int act) {
+  return act == MOE_ACT_RELU ? (h < 0.f ? 0.f : h) : act_fwd(h, act);
+}
+
 // Compile-time activation for the bf16 GEMM epilogues, whose outputs are
 // rounded to bf16: GELU-tanh is evaluated as h * s, s = sigmoid(2u), the same
 // function as 0.5 h (1 + tanh u), u = sqrt(2/pi) (h + 0.044715 h^3), with the

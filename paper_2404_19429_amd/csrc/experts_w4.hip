@@ -1,0 +1,366 @@
+// The experts' FFNs on 4-bit weights for a few tokens, and the weights' quantiser.
+//
+// y_t = sum_r w_tr W2_e act(W1_e x_t).  With n = T k choices, two products over the
+// chosen experts (act(W1 x) of every choice goes through the workspace) and a sum over
+// a token's choices.  The weights are read once and bound the time; 16 output rows x
+// 128 inputs of them are one 16-byte load a lane, which v_cvt_scalef32_pk_bf16_fp4
+// turns into bfloat16 exactly, scale included (eight codes in four instructions), for
+// v_mfma_f32_16x16x32_bf16 against up to 16 tokens.
+//
+// Lane (i = lane & 15, q = lane >> 4) holds row i, inputs 32 q .. 32 q + 31 of a chunk
+// of 128: one scale group.  MFMA j takes its inputs 8 j .. 8 j + 7 from weights and
+// tokens alike, so the product's k-index stands for the same input in both operands,
+// which is all a dot product needs, and the codes can stay row-major.
+#include "internal.h"
+
+namespace lmoe {
+
+constexpr int kW4Waves = 4;        // waves of a block: they share its rows and split K
+constexpr int kW4Small = 64;       // up to so many choices a block finds its expert's tokens by itself
+constexpr int kW4Tile = 64;        // tokens of one block, at most
+constexpr int kW4ListThreads = 1024;
+
+typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
+
+// -------------------------------------------------------------------- choices
+// More than kW4Small choices: their numbers sorted by expert (the order inside an
+// expert is left to the atomics: rows do not mix, so it changes no value) and the
+// table of token tiles {expert, first, count}.
+struct W4Tile {
+  int32_t e, first, count, pad;
+};
+__global__ __launch_bounds__(kW4ListThreads) void w4_list_kernel(const int32_t* __restrict__ idx, int n, int E,
+                                                                 int32_t* __restrict__ list,
+                                                                 W4Tile* __restrict__ tiles,
+                                                                 int32_t* __restrict__ ntiles) {
+  __shared__ int32_t cnt[kRouterMaxE], at[kRouterMaxE], sum[2][kRouterMaxE];
+  const int tid = threadIdx.x;
+  for (int e = tid; e < kRouterMaxE; e += kW4ListThreads) cnt[e] = 0;
+  __syncthreads();
+  for (int i = tid; i < n; i += kW4ListThreads) {
+    const int e = idx[i];
+    if (e >= 0 && e < E) atomicAdd(&cnt[e], 1);
+  }
+  __syncthreads();
+  // exclusive sums of the counts and of the tiles
+  if (tid < kRouterMaxE) {
+    sum[0][tid] = cnt[tid];
+    sum[1][tid] = (cnt[tid] + kW4Tile - 1) / kW4Tile;
+  }
+  __syncthreads();
+  for (int o = 1; o < kRouterMaxE; o <<= 1) {
+    int a = 0, b = 0;
+    if (tid < kRouterMaxE && tid >= o) {
+      a = sum[0][tid - o];
+      b = sum[1][tid - o];
+    }
+    __syncthreads();
+    if (tid < kRouterMaxE) {
+      sum[0][tid] += a;
+      sum[1][tid] += b;
+    }
+    __syncthreads();
+  }
+  if (tid < kRouterMaxE) {
+    const int c = cnt[tid], nt = (c + kW4Tile - 1) / kW4Tile;
+    const int first = sum[0][tid] - c, t0 = sum[1][tid] - nt;
+    at[tid] = first;
+    for (int j = 0; j < nt; ++j) tiles[t0 + j] = W4Tile{tid, first + j * kW4Tile, min(kW4Tile, c - j * kW4Tile), 0};
+    if (tid == kRouterMaxE - 1) *ntiles = sum[1][tid];
+  }
+  __syncthreads();
+  for (int i = tid; i < n; i += kW4ListThreads) {
+    const int e = idx[i];
+    if (e >= 0 && e < E) list[atomicAdd(&at[e], 1)] = i;
+  }
+}
+
+// ------------------------------------------------------------------- products
+struct W4Args {
+  const uint8_t *codes, *scales;   // [E][N][K/2], [E][N][K/32]
+  const void* in;                  // rows of K: x by token, or the parts of act(W1 x) by choice
+  void* out;                       // FIRST: the parts [parts][n][N] bf16; else float [n][N]
+  const int32_t *idx, *list;
+  const W4Tile* tiles;
+  const int32_t* ntiles;
+  int32_t N, K, n, k, E, act;
+};
+
+// Eight codes to bfloat16.
+__device__ __forceinline__ bf16x8 w4_frag(uint32_t c, float s) {
+  u32x4 r;
+  r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0));
+  r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1));
+  r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2));
+  r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3));
+  return __builtin_bit_cast(bf16x8, r);
+}
+
+// A float's leading eight significand bits (truncated: never past the largest
+// bfloat16), and what is left of it; of an infinity nothing is left.
+__device__ __forceinline__ float part_of(float& v) {
+  const float h = __uint_as_float(__float_as_uint(v) & 0xffff0000u);
+  v = h == v ? 0.f : v - h;
+  return h;
+}
+
+// Eight inputs of a token as NS bfloat16 parts that sum to them.
+template <typename T, int NS, bool FIRST>
+__device__ __forceinline__ void w4_inputs(const W4Args& a, int64_t off, bool ok, bf16x8 (&b)[NS]) {
+  const u32x4 zero = {0u, 0u, 0u, 0u};
+  if constexpr (FIRST && sizeof(T) == 4) {
+    float v[8];
+    const float* p = (const float*)a.in + off;
+    Vec<float>::load(p, v);
+    Vec<float>::load(p + 4, v + 4);
+    u32x4 r[NS];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        const float lo = part_of(v[2 * i]), hi = part_of(v[2 * i + 1]);
+        r[s][i] = ok ? (__float_as_uint(lo) >> 16) | __float_as_uint(hi) : 0u;
+      }
+#pragma unroll
+    for (int s = 0; s < NS; ++s) b[s] = __builtin_bit_cast(bf16x8, r[s]);
+  } else {
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      const u32x4 r = *reinterpret_cast<const u32x4*>((const uint16_t*)a.in + (int64_t)s * a.n * a.K + off);
+      b[s] = __builtin_bit_cast(bf16x8, ok ? r : zero);
+    }
+  }
+}
+
+template <typename T, bool FIRST, int NS, int NO, int RT, int TN>
+__device__ __forceinline__ void w4_tile(const W4Args& a, int e, int cnt, const int32_t* list, f32x4 (*red)[64]) {
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  const int i16 = lane & 15, q = lane >> 4;
+  const int row0 = blockIdx.x * 16 * RT;
+  const int nch = (a.K + 127) / 128;
+  f32x4 acc[RT][TN];
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int t = 0; t < TN; ++t) acc[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  int64_t in_off[TN];
+#pragma unroll
+  for (int t = 0; t < TN; ++t) {
+    const int c = list[min(t * 16 + i16, cnt - 1)];   // columns past the count repeat the last
+    in_off[t] = (int64_t)(FIRST ? c / a.k : c) * a.K;
+  }
+  const int64_t wrow = (int64_t)e * a.N + row0 + i16;
+  for (int c = wv; c < nch; c += kW4Waves) {
+    const int col = c * 128 + q * 32;
+    const bool ok = col < a.K;          // K is a multiple of 32
+    const int cc = ok ? col : 0;
+    u32x4 code[RT];
+    float sc[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      const int64_t row = wrow + r * 16;
+      code[r] = *reinterpret_cast<const u32x4*>(a.codes + row * (a.K / 2) + cc / 2);
+      sc[r] = __uint_as_float((uint32_t)a.scales[row * (a.K / 32) + cc / 32] << 23);
+      if (!ok) code[r] = u32x4{0u, 0u, 0u, 0u}, sc[r] = 1.f;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      bf16x8 w[RT];
+#pragma unroll
+      for (int r = 0; r < RT; ++r) w[r] = w4_frag(code[r][j], sc[r]);
+#pragma unroll
+      for (int t = 0; t < TN; ++t) {
+        bf16x8 b[NS];
+        w4_inputs<T, NS, FIRST>(a, in_off[t] + cc + 8 * j, ok, b);
+#pragma unroll
+        for (int s = NS - 1; s >= 0; --s)
+#pragma unroll
+          for (int r = 0; r < RT; ++r) acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[r], b[s], acc[r][t], 0, 0, 0);
+      }
+    }
+  }
+  // The waves' sums meet in LDS and are added in wave order, every wave its tiles.
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int t = 0; t < TN; ++t) red[(wv * RT + r) * TN + t][lane] = acc[r][t];
+  __syncthreads();
+#pragma unroll
+  for (int u0 = 0; u0 < RT * TN; u0 += kW4Waves) {
+    const int u = u0 + wv;
+    if (u >= RT * TN) break;
+    const int r = u / TN, t = u % TN;
+    f32x4 s = red[u][lane];
+#pragma unroll
+    for (int w = 1; w < kW4Waves; ++w) s += red[w * RT * TN + u][lane];
+    const int col = t * 16 + i16;
+    if (col < cnt) {
+      const int64_t off = (int64_t)list[col] * a.N + row0 + r * 16 + 4 * q;
+      if constexpr (FIRST) {
+        float h[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h[i] = act_fwd_nan(s[i], a.act);
+#pragma unroll
+        for (int p = 0; p < NO; ++p) {
+          float v[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] = p + 1 < NO || NO == 3 ? part_of(h[i]) : h[i];   // two parts: the second rounds
+          *reinterpret_cast<u32x2*>((uint16_t*)a.out + (int64_t)p * a.n * a.N + off) =
+              u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+        }
+      } else {
+        *reinterpret_cast<f32x4*>((float*)a.out + off) = s;
+      }
+    }
+  }
+}
+
+template <typename T, bool FIRST, int NS, int NO, int RT>
+__global__ __launch_bounds__(64 * kW4Waves) void w4_product_kernel(W4Args a) {
+  __shared__ f32x4 red[kW4Waves * RT * 4][64];
+  __shared__ int32_t list[kW4Tile];
+  const int lane = threadIdx.x & 63;
+  int e, cnt;
+  if (a.tiles) {
+    if ((int)blockIdx.y >= *a.ntiles) return;
+    const W4Tile t = a.tiles[blockIdx.y];
+    e = t.e;
+    cnt = t.count;
+    if ((int)threadIdx.x < cnt) list[threadIdx.x] = a.list[t.first + threadIdx.x];
+  } else {
+    // Choice blockIdx.y, if it is the first of its expert, stands for all of them.
+    const int my = lane < a.n ? a.idx[lane] : -1;
+    e = __shfl(my, (int)blockIdx.y, kWave);
+    if (e < 0 || e >= a.E) return;
+    const uint64_t same = __ballot(my == e);
+    if (__builtin_ctzll(same) != (int)blockIdx.y) return;
+    cnt = __popcll(same);
+    if (threadIdx.x < 64 && my == e) list[__popcll(same & ((1ull << lane) - 1))] = lane;
+  }
+  __syncthreads();
+  if (cnt <= 16) w4_tile<T, FIRST, NS, NO, RT, 1>(a, e, cnt, list, red);
+  else if (cnt <= 32) w4_tile<T, FIRST, NS, NO, RT, 2>(a, e, cnt, list, red);
+  else w4_tile<T, FIRST, NS, NO, RT, 4>(a, e, cnt, list, red);
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void w4_combine_kernel(const float* __restrict__ O, const int32_t* __restrict__ idx,
+                                                         const float* __restrict__ w, T* __restrict__ y, int64_t T_tokens,
+                                                         int d, int E, int k) {
+  const int64_t g = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+  const int nc = d / 4;
+  const int64_t t = g / nc;
+  if (t >= T_tokens) return;
+  const int c = (int)(g - t * nc) * 4;
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+  for (int r = 0; r < k; ++r) {
+    const int e = idx[t * k + r];
+    if (e < 0 || e >= E) continue;
+    const float wr = w[t * k + r];
+    const f32x4 o = *reinterpret_cast<const f32x4*>(O + (t * k + r) * d + c);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] = fmaf(wr, o[i], s[i]);
+  }
+  if constexpr (sizeof(T) == 2)
+    *reinterpret_cast<u32x2*>(y + t * d + c) = u32x2{pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3])};
+  else
+    *reinterpret_cast<f32x4*>(y + t * d + c) = s;
+}
+
+// Workspace: list, tiles, tile count | parts | O.
+struct W4Ws {
+  size_t list, tiles, ntiles, parts, O, total;
+  int max_tiles;
+};
+static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
+static W4Ws w4_ws(const moe_w4_cfg& c) {
+  W4Ws w;
+  const int64_t n = c.T * c.k;
+  const int ns = c.dtype == MOE_BF16 ? 2 : 3;
+  w.max_tiles = (int)(std::min<int64_t>(n, c.E) + n / kW4Tile);
+  w.list = 0;
+  w.tiles = up256(4 * (size_t)n);
+  w.ntiles = w.tiles + sizeof(W4Tile) * (size_t)w.max_tiles;
+  w.parts = up256(w.ntiles + 4);
+  w.O = up256(w.parts + (size_t)ns * n * c.d_ff * 2);
+  w.total = up256(w.O + (size_t)n * c.d_model * 4);
+  return w;
+}
+size_t experts_w4_ws_bytes(const moe_w4_cfg& c) { return w4_ws(c).total; }
+
+template <typename T, int NX, int NA>
+static void launch_w4_t(const moe_w4_cfg& c, const void* x, const int32_t* idx, const float* w, const uint8_t* W1c,
+                        const uint8_t* W1s, const uint8_t* W2c, const uint8_t* W2s, void* y, void* ws, hipStream_t s) {
+  const W4Ws L = w4_ws(c);
+  const int n = (int)(c.T * c.k);
+  char* base = (char*)ws;
+  int32_t* list = (int32_t*)(base + L.list);
+  W4Tile* tiles = (W4Tile*)(base + L.tiles);
+  int32_t* ntiles = (int32_t*)(base + L.ntiles);
+  const bool small = n <= kW4Small;
+  if (!small)
+    hipLaunchKernelGGL(w4_list_kernel, dim3(1), dim3(kW4ListThreads), 0, s, idx, n, c.E, list, tiles, ntiles);
+  const unsigned gy = (unsigned)(small ? n : L.max_tiles);
+  W4Args a{W1c, W1s, x, base + L.parts, idx, list, small ? nullptr : tiles, ntiles, c.d_ff, c.d_model, n, c.k, c.E, c.act};
+  hipLaunchKernelGGL((w4_product_kernel<T, true, NX, NA, 1>), dim3(c.d_ff / 16, gy), dim3(64 * kW4Waves), 0, s, a);
+  W4Args b{W2c, W2s, base + L.parts, base + L.O, idx, list, small ? nullptr : tiles, ntiles, c.d_model, c.d_ff, n, c.k,
+           c.E, c.act};
+  hipLaunchKernelGGL((w4_product_kernel<T, false, NA, NA, 1>), dim3(c.d_model / 16, gy), dim3(64 * kW4Waves), 0, s, b);
+  const int64_t g = c.T * (c.d_model / 4);
+  hipLaunchKernelGGL(w4_combine_kernel<T>, dim3((unsigned)((g + 255) / 256)), dim3(256), 0, s,
+                     (const float*)(base + L.O), idx, w, (T*)y, c.T, c.d_model, c.E, c.k);
+}
+
+void launch_experts_w4(const moe_w4_cfg& c, const void* x, const int32_t* idx, const float* w, const uint8_t* W1c,
+                       const uint8_t* W1s, const uint8_t* W2c, const uint8_t* W2s, void* y, void* ws, hipStream_t s) {
+  if (c.T == 0) return;
+  if (c.dtype == MOE_BF16) launch_w4_t<uint16_t, 1, 2>(c, x, idx, w, W1c, W1s, W2c, W2s, y, ws, s);
+  else launch_w4_t<float, 3, 3>(c, x, idx, w, W1c, W1s, W2c, W2s, y, ws, s);
+}
+
+// ------------------------------------------------------------------ quantiser
+// One thread per group of 32 weights (run once per weight load).
+template <typename T>
+__global__ __launch_bounds__(256) void w4_quantize_kernel(const T* __restrict__ W, uint8_t* __restrict__ codes,
+                                                          uint8_t* __restrict__ scales, int64_t groups) {
+  for (int64_t g = (int64_t)blockIdx.x * 256 + threadIdx.x; g < groups; g += (int64_t)gridDim.x * 256) {
+    float v[32];
+#pragma unroll
+    for (int i = 0; i < 32; i += Vec<T>::N) Vec<T>::load(W + g * 32 + i, v + i);
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+    const bool bad = m >= 0x7f800000u;
+    // amax = f 2^e with f in [1/2, 1): 7 * 2^s = 7/8 * 2^(s + 3)
+    int e = 0;
+    const float f = bad || m == 0 ? 0.f : frexpf(__uint_as_float(m), &e);
+    int s = m == 0 || bad ? -100 : f <= 0.875f ? e - 3 : e - 2;
+    s = min(max(s, -100), 125);
+    const float inv = ldexpf(1.f, -s);
+    u32x4 out = {0u, 0u, 0u, 0u};
+    if (!bad) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        const float a = fabsf(v[i]) * inv;
+        // nearest of 0 0.5 1 1.5 2 3 4 6; half way the code with the even mantissa
+        const uint32_t c = (a > 0.25f) + (a >= 0.75f) + (a > 1.25f) + (a >= 1.75f) + (a > 2.5f) + (a >= 3.5f) + (a > 5.f);
+        out[i >> 3] |= (c | (__float_as_uint(v[i]) >> 31 << 3)) << (4 * (i & 7));
+      }
+    }
+    *reinterpret_cast<u32x4*>(codes + g * 16) = out;
+    scales[g] = bad ? 255 : (uint8_t)(s + 127);
+  }
+}
+
+void launch_w4_quantize(int64_t rows, int K, int dtype, const void* W, uint8_t* codes, uint8_t* scales,
+                        hipStream_t s) {
+  const int64_t groups = rows * (K / 32);
+  if (groups == 0) return;
+  const dim3 grid((unsigned)std::min<int64_t>((groups + 255) / 256, 1 << 16));
+  if (dtype == MOE_BF16)
+    hipLaunchKernelGGL(w4_quantize_kernel<uint16_t>, grid, dim3(256), 0, s, (const uint16_t*)W, codes, scales, groups);
+  else
+    hipLaunchKernelGGL(w4_quantize_kernel<float>, grid, dim3(256), 0, s, (const float*)W, codes, scales, groups);
+}
+
+}  // namespace lmoe

@@ -78,11 +78,32 @@ void launch_combine(const moe_cfg& c, const void* O, const int32_t* idx, const i
                     void* y, hipStream_t s, const void* resid = nullptr);
 size_t bwd_dx_ws_bytes(const moe_cfg& c);
 void launch_combine_bwd(const moe_cfg& c, const float* logits, const int32_t* idx, const float* w,
-                        const int32_t* slot, const void* O, const void* dy, void* dO, float* dlogits, hipStream_t s);
+                        const int32_t* slot, const void* O, const void* dy, void* dO, float* dlogits, hipStream_t s,
+                        float* dw = nullptr);   // dw: the gradient at w instead of dlogits
 void launch_dispatch_bwd(const moe_cfg& c, const void* Wg, const float* dlogits, const int32_t* idx,
                          const int32_t* slot, const void* dXe, void* dx, hipStream_t s);
 size_t bwd_dw_ws_bytes(const moe_cfg& c);
 void launch_dwg(const moe_cfg& c, const void* x, const float* dlogits, float* dWg, void* ws, hipStream_t s);
+
+// router.hip
+constexpr int kRouterMaxE = 512, kRouterMaxK = 16;
+void launch_route(const moe_route_cfg& c, const float* logits, const float* bias, int32_t* idx, float* w,
+                  int32_t* load, hipStream_t s);
+void launch_route_bwd(const moe_route_cfg& c, const float* logits, const int32_t* idx, const float* w,
+                      const float* dw, float* dlogits, hipStream_t s);
+
+// experts_w4.hip
+void launch_w4_quantize(int64_t rows, int K, int dtype, const void* W, uint8_t* codes, uint8_t* scales, hipStream_t s);
+size_t experts_w4_ws_bytes(const moe_w4_cfg& c);
+void launch_experts_w4(const moe_w4_cfg& c, const void* x, const int32_t* idx, const float* w, const uint8_t* W1c,
+                       const uint8_t* W1s, const uint8_t* W2c, const uint8_t* W2s, void* y, void* ws, hipStream_t s);
+
+// ckpt.hip
+size_t ckpt_bytes(const moe_cfg& c);
+void launch_ckpt_save(const moe_cfg& c, const void* send, const void* H, const void* O, const int32_t* rb,
+                      const int32_t* re, void* ckpt, hipStream_t s);
+void launch_ckpt_load(const moe_cfg& c, const void* ckpt, const int32_t* rb, const int32_t* re, void* send, void* H,
+                      void* A, void* O, hipStream_t s);
 
 // Expert weights into the layout the expert GEMMs read (blocked for bf16, a copy for float).
 void launch_pack_weights(const moe_cfg& c, const void* W1, const void* W2, void* W1p, void* W2p, hipStream_t s);

@@ -826,7 +826,8 @@ void launch_combine(const moe_cfg& c, const void* O, const int32_t* idx, const i
 }
 
 // ------------------------------------------------------ combine + gate backward
-// One wavefront per token: dO[e][s] = w dy, g_r = <dy, O[e][s]>, then dlogits.
+// One wavefront per token: dO[e][s] = w dy, g_r = <dy, O[e][s]>, then dlogits; or, with
+// dw non-null, g itself (the gradient at the weights, whose router has its own backward).
 template <typename T, int KT>
 __global__ __launch_bounds__(256) void combine_bwd_kernel(const float* __restrict__ logits,
                                                           const int32_t* __restrict__ idx,
@@ -834,7 +835,8 @@ __global__ __launch_bounds__(256) void combine_bwd_kernel(const float* __restric
                                                           const int32_t* __restrict__ slot,
                                                           const T* __restrict__ O, const T* __restrict__ dy,
                                                           T* __restrict__ dO, float* __restrict__ dlogits,
-                                                          int64_t T_tokens, int d, int E, int kr, int C, int renorm) {
+                                                          float* __restrict__ dw, int64_t T_tokens, int d, int E,
+                                                          int kr, int C, int renorm) {
   constexpr int V = Vec<T>::N;
   constexpr int KK = KT > 0 ? KT : kMaxK;
   const int k = KT > 0 ? KT : kr;
@@ -892,6 +894,12 @@ __global__ __launch_bounds__(256) void combine_bwd_kernel(const float* __restric
     gp[r] = wave_sum(gp[r]);
     gsum = fmaf(wr[r], gp[r], gsum);
   }
+  if (dw) {
+#pragma unroll
+    for (int r = 0; r < KK; ++r)
+      if (r < k && lane == r) dw[t * k + r] = gp[r];
+    return;
+  }
   // dlogits: lane j handles expert j (E <= 64).
   const int j = lane;
   float dl = 0.f;
@@ -918,13 +926,13 @@ size_t bwd_dx_ws_bytes(const moe_cfg& c) { return expert_sk_ws_bytes(c); }
 
 void launch_combine_bwd(const moe_cfg& c, const float* logits, const int32_t* idx, const float* w,
                         const int32_t* slot, const void* O, const void* dy, void* dO, float* dlogits,
-                        hipStream_t s) {
+                        hipStream_t s, float* dw) {
   if (c.T == 0) return;
   const unsigned blocks = (unsigned)((c.T + 3) / 4);
   auto go = [&](auto kern, auto tag) {
     using T = decltype(tag);
     hipLaunchKernelGGL(kern, dim3(blocks), dim3(256), 0, s, logits, idx, w, slot, (const T*)O, (const T*)dy,
-                       (T*)dO, dlogits, c.T, c.d_model, c.E, c.k, c.C, c.renorm);
+                       (T*)dO, dlogits, dw, c.T, c.d_model, c.E, c.k, c.C, c.renorm);
   };
   if (c.dtype == MOE_BF16) {
     if (c.k == 1) go(combine_bwd_kernel<uint16_t, 1>, uint16_t{});

@@ -24,6 +24,7 @@ LIB_PATH = os.environ.get("LANCET_MOE_LIB") or os.path.join(_HERE, "liblancet_mo
 MOE_OK, MOE_EINVAL, MOE_ESHAPE, MOE_EALIGN, MOE_EDTYPE, MOE_EDEVICE, MOE_ELAUNCH, MOE_EWORKSPACE = 0, -1, -2, -3, -4, -5, -6, -7
 MOE_F32, MOE_BF16 = 0, 1
 ACTS = {"identity": 0, "relu": 1, "gelu_tanh": 2, "gelu_erf": 3}
+SCORES = {"softmax": 0, "sigmoid": 1}
 MOE_CALL_DISPATCH, MOE_CALL_BWD_DX, MOE_CALL_BWD_DW, MOE_CALL_FFN_FWD, MOE_CALL_DISPATCH_BPR = 0, 1, 2, 3, 4
 
 #: Every symbol include/lancet_moe.h declares.
@@ -31,7 +32,8 @@ EXPORTS = ["moe_capacity", "moe_workspace_bytes", "moe_last_error", "moe_gate_to
            "moe_dispatch_noalloc", "moe_dispatch_bpr", "moe_pack_weights", "moe_expert_ffn_fwd", "moe_combine", "moe_bwd_dx", "moe_bwd_dw",
            "moe_block_workspace_bytes", "moe_block_chunked", "moe_block_op_times", "moe_block_dw_schedule",
            "moe_dw_schedule", "moe_pipeline_plan", "moe_pipeline_range_cost", "moe_product_timing",
-           "moe_product_times"]
+           "moe_product_times", "moe_route", "moe_route_bwd", "moe_bwd_dx_route", "moe_w4_quantize",
+           "moe_experts_w4_workspace_bytes", "moe_experts_w4", "moe_ckpt_bytes", "moe_ckpt_save", "moe_ckpt_load"]
 #: The expert products moe_product_times reports, in its order.
 PRODUCTS = ["fwd1", "fwd2", "dA", "dXe", "dW2", "dW1"]
 MOE_BLOCK_FWD, MOE_BLOCK_BWD, MOE_BLOCK_TIMED = 1, 2, 4
@@ -57,6 +59,17 @@ class moe_cfg(ctypes.Structure):
 class moe_block_cfg(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int32), ("S", ctypes.c_int32), ("heads", ctypes.c_int32), ("moe", moe_cfg),
                 ("dw_order", ctypes.c_int32 * 6)]
+
+
+class moe_route_cfg(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64), ("E", ctypes.c_int32), ("k", ctypes.c_int32), ("score", ctypes.c_int32),
+                ("renorm", ctypes.c_int32), ("groups", ctypes.c_int32), ("top_groups", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
+
+
+class moe_w4_cfg(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64), ("d_model", ctypes.c_int32), ("d_ff", ctypes.c_int32), ("E", ctypes.c_int32),
+                ("k", ctypes.c_int32), ("dtype", ctypes.c_int32), ("act", ctypes.c_int32)]
 
 
 BLOCK_WEIGHTS = ["ln1_g", "ln1_b", "Wqkv", "Wo", "ln2_g", "ln2_b", "Wg", "W1", "W2"]
@@ -104,6 +117,15 @@ def _load():
         "moe_block_dw_schedule": (I32, [P, ctypes.c_double, P, P, P]),
         "moe_pipeline_plan": (I32, [I32, I32, P, P, P, I32, P, P, P, P, P]),
         "moe_pipeline_range_cost": (I32, [I32, I32, P, P, P, I32, I32, I32, P]),
+        "moe_route": (I32, [ctypes.POINTER(moe_route_cfg)] + [P] * 6),
+        "moe_route_bwd": (I32, [ctypes.POINTER(moe_route_cfg)] + [P] * 6),
+        "moe_bwd_dx_route": (I32, [CFG, ctypes.POINTER(moe_route_cfg)] + [P] * 19 + [SZ, P]),
+        "moe_w4_quantize": (I32, [I64, I32, I32, P, P, P, P]),
+        "moe_experts_w4_workspace_bytes": (SZ, [ctypes.POINTER(moe_w4_cfg)]),
+        "moe_experts_w4": (I32, [ctypes.POINTER(moe_w4_cfg)] + [P] * 9 + [SZ, P]),
+        "moe_ckpt_bytes": (SZ, [CFG]),
+        "moe_ckpt_save": (I32, [CFG] + [P] * 6 + [SZ, P]),
+        "moe_ckpt_load": (I32, [CFG, P, SZ] + [P] * 7),
         "moe_block_workspace_bytes": (SZ, [ctypes.POINTER(moe_block_cfg), I32]),
         "moe_block_chunked": (I32, [ctypes.POINTER(moe_block_cfg), ctypes.POINTER(moe_block_weights),
                                     ctypes.POINTER(moe_block_grads), P, P, P, P, ctypes.POINTER(moe_block_acts),
@@ -124,7 +146,7 @@ def _load_bind():
     except ImportError as e:
         raise ImportError("the native binding is not built; run `python -m paper_2404_19429_amd.build`") from e
     _bind.init({n: ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in EXPORTS}, lambda s: _stream(s),
-               moe_cfg, moe_block_cfg)
+               moe_cfg, moe_block_cfg, moe_route_cfg, moe_w4_cfg)
     return _bind
 
 
@@ -267,6 +289,72 @@ def moe_bwd_dw(cfg, x, dlogits, row_begin, row_end, send_buf, A, dO, dH, dW1, dW
     _check(_bind.bwd_dw(cfg, x, dlogits, row_begin, row_end, send_buf, A, dO, dH, dW1, dW2, dWg, ws, stream))
 
 
+# ------------------------------------------------------------------------ router
+def make_route_cfg(T, E, k, score="softmax", renorm=1, groups=1, top_groups=1, scale=1.0) -> moe_route_cfg:
+    return moe_route_cfg(int(T), int(E), int(k), SCORES[score] if isinstance(score, str) else int(score), int(renorm),
+                         int(groups), int(top_groups), float(scale))
+
+
+def moe_route(cfg, logits, bias, idx, w, load=None, stream=None):
+    """load: the choices of each expert are added to it."""
+    _check(_bind.route(cfg, logits, bias, idx, w, load, stream))
+
+
+def moe_route_bwd(cfg, logits, idx, w, dw, dlogits, stream=None):
+    _check(_bind.route_bwd(cfg, logits, idx, w, dw, dlogits, stream))
+
+
+def moe_bwd_dx_route(cfg, route, Wg, logits, idx, w, slot, row_begin, row_end, H, expert_out, W1p, W2p, dy, dO, dH, dXe,
+                     dw, dlogits, dx, ws=None, stream=None):
+    _check(_bind.bwd_dx_route(cfg, route, Wg, logits, idx, w, slot, row_begin, row_end, H, expert_out, W1p, W2p, dy, dO,
+                              dH, dXe, dw, dlogits, dx, ws, stream))
+
+
+# --------------------------------------------------------- experts on 4-bit weights
+def make_w4_cfg(T, d_model, d_ff, E, k, dtype="bf16", act="gelu_tanh") -> moe_w4_cfg:
+    dt = {"bf16": MOE_BF16, "f32": MOE_F32}[dtype] if isinstance(dtype, str) else int(dtype)
+    return moe_w4_cfg(int(T), int(d_model), int(d_ff), int(E), int(k), dt, ACTS[act] if isinstance(act, str) else int(act))
+
+
+def moe_w4_quantize(W, codes, scales, stream=None):
+    """W [..., K] (bf16 or f32) -> codes [..., K/2] and scales [..., K/32] (uint8)."""
+    if not isinstance(W, torch.Tensor) or W.dim() < 1:
+        raise ValueError("W must be a device tensor of at least one dimension")
+    K = W.shape[-1]
+    _check(_bind.w4_quantize(W.numel() // K if K else 0, K, MOE_BF16 if W.dtype == torch.bfloat16 else MOE_F32, W, codes,
+                             scales, stream))
+
+
+def alloc_w4(*shape, device="cuda"):
+    """Empty codes and scales of a weight of `shape` [..., K]."""
+    K = shape[-1]
+    if K % 32:
+        raise ValueError(f"{K} inputs are not a multiple of 32")
+    return (torch.empty(*shape[:-1], K // 2, dtype=torch.uint8, device=device),
+            torch.empty(*shape[:-1], K // 32, dtype=torch.uint8, device=device))
+
+
+def moe_experts_w4_workspace_bytes(cfg: moe_w4_cfg) -> int:
+    return int(_lib.moe_experts_w4_workspace_bytes(ctypes.byref(cfg)))
+
+
+def moe_experts_w4(cfg, x, idx, w, W1c, W1s, W2c, W2s, y, ws, stream=None):
+    _check(_bind.experts_w4(cfg, x, idx, w, W1c, W1s, W2c, W2s, y, ws, stream))
+
+
+# ------------------------------------------------------- 8-bit activation checkpoint
+def moe_ckpt_bytes(cfg: moe_cfg) -> int:
+    return int(_lib.moe_ckpt_bytes(ctypes.byref(cfg)))
+
+
+def moe_ckpt_save(cfg, send_buf, H, expert_out, row_begin, row_end, ckpt, stream=None):
+    _check(_bind.ckpt_save(cfg, send_buf, H, expert_out, row_begin, row_end, ckpt, stream))
+
+
+def moe_ckpt_load(cfg, ckpt, row_begin, row_end, send_buf, H, A, expert_out, stream=None):
+    _check(_bind.ckpt_load(cfg, ckpt, row_begin, row_end, send_buf, H, A, expert_out, stream))
+
+
 # ------------------------------------------------------------- layer step driver
 @dataclass
 class LayerBuffers:
@@ -299,6 +387,7 @@ class LayerBuffers:
     ws_dw: torch.Tensor
     order: torch.Tensor       # batch-prioritized routing: the visiting order
     ws_bpr: torch.Tensor
+    dw: torch.Tensor          # layers with a router: the gradient at w
 
 
 def alloc_layer(cfg: moe_cfg, device="cuda") -> LayerBuffers:
@@ -318,15 +407,26 @@ def alloc_layer(cfg: moe_cfg, device="cuda") -> LayerBuffers:
         ws_dw=e(max(16, moe_workspace_bytes(cfg, MOE_CALL_BWD_DW)), dtype=torch.uint8),
         order=e(max(1, T), dtype=torch.int32),
         ws_bpr=e(max(16, moe_workspace_bytes(cfg, MOE_CALL_DISPATCH_BPR)), dtype=torch.uint8),
+        dw=e(T, k, dtype=torch.float32),
     )
 
 
-def layer_forward(b: LayerBuffers, x, Wg, bias, W1, W2, stream=None, routing="token"):
-    """weight packing -> gate -> dispatch -> experts -> combine, all on one stream.
+@dataclass
+class Router:
+    """How a layer's choices and weights come from the gate's logits (moe_route), in the place of the gate's own."""
+    cfg: moe_route_cfg
+    bias: Optional[torch.Tensor] = None    # [E] float, in the choice only
+    load: Optional[torch.Tensor] = None    # [E] int32, the choices of each expert are added to it
+
+
+def layer_forward(b: LayerBuffers, x, Wg, bias, W1, W2, stream=None, routing="token", router: Optional[Router] = None):
+    """weight packing -> gate [-> router] -> dispatch -> experts -> combine, all on one stream.
     routing "bpr": batch-prioritized capacity order (no carry-in; b.carry must be zero)."""
     c = b.cfg
     moe_pack_weights(c, W1, W2, b.W1p, b.W2p, stream)
     moe_gate_topk(c, x, Wg, bias, b.logits, b.idx, b.w, stream)
+    if router is not None:
+        moe_route(router.cfg, b.logits, router.bias, b.idx, b.w, router.load, stream)
     if routing == "bpr":
         moe_dispatch_bpr(c, x, b.logits, b.idx, b.fill, b.slot, b.send_buf, b.order, b.ws_bpr, stream)
     else:
@@ -335,12 +435,32 @@ def layer_forward(b: LayerBuffers, x, Wg, bias, W1, W2, stream=None, routing="to
     moe_combine(c, b.O, b.idx, b.slot, b.w, b.y, stream)
 
 
-def layer_backward(b: LayerBuffers, x, Wg, dy, stream=None, dw_stream=None):
+def alloc_ckpt(cfg: moe_cfg, device="cuda") -> torch.Tensor:
+    """An empty checkpoint of one layer's saved activations."""
+    return torch.empty(max(16, moe_ckpt_bytes(cfg)), dtype=torch.uint8, device=device)
+
+
+def layer_save(b: LayerBuffers, ckpt, stream=None):
+    """After layer_forward: what its backward reads of the expert buffers, in 8 bits (another layer may then
+    use them; the token-sized results, the weights and carry and fill stay the layer's own)."""
+    moe_ckpt_save(b.cfg, b.send_buf, b.H, b.O, b.carry, b.fill, ckpt, stream)
+
+
+def layer_restore(b: LayerBuffers, ckpt, stream=None):
+    """Before layer_backward: the expert buffers as layer_save kept them, A from H."""
+    moe_ckpt_load(b.cfg, ckpt, b.carry, b.fill, b.send_buf, b.H, b.A, b.O, stream)
+
+
+def layer_backward(b: LayerBuffers, x, Wg, dy, stream=None, dw_stream=None, router: Optional[Router] = None):
     """dX chain on `stream` (with the weights packed by layer_forward); the dW
     products on `dw_stream` (default: same stream), ordered after the dX chain by an event."""
     c = b.cfg
-    moe_bwd_dx(c, Wg, b.logits, b.idx, b.w, b.slot, b.carry, b.fill, b.H, b.O, b.W1p, b.W2p, dy, b.dO, b.dH, b.dXe,
-               b.dlogits, b.dx, b.ws_dx, stream)
+    if router is not None:
+        moe_bwd_dx_route(c, router.cfg, Wg, b.logits, b.idx, b.w, b.slot, b.carry, b.fill, b.H, b.O, b.W1p, b.W2p, dy,
+                         b.dO, b.dH, b.dXe, b.dw, b.dlogits, b.dx, b.ws_dx, stream)
+    else:
+        moe_bwd_dx(c, Wg, b.logits, b.idx, b.w, b.slot, b.carry, b.fill, b.H, b.O, b.W1p, b.W2p, dy, b.dO, b.dH, b.dXe,
+                   b.dlogits, b.dx, b.ws_dx, stream)
     if dw_stream is not None:
         ev = torch.cuda.Event()
         ev.record(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.current_stream())
