@@ -1,55 +1,101 @@
 // The router: scores, choice with balance bias and groups, weights, loads; and its
 // gradient at the logits.
 //
-// Forward, one wavefront per token: lane l holds experts l, l + 64, ...  The choice
-// value c = s + b is compared in double, so that the choice is the one of any other
-// evaluation in 64 bits (two values of a token closer than 1e-15 aside).
+// The choice is defined on the values c = s + b compared as doubles (so that it is the
+// one of any other evaluation in 64 bits, two values of a token closer than 1e-15 aside).
+// Doubles for every expert would bound the kernel, so tokens are routed in float first:
+// a team of 4 or 16 lanes holds a token's row, and every step that compares two values
+// also sees whether they are too close for float to tell (kRouteEps, above the sum of
+// the errors).  Such a token (a few in a thousand of ordinary logits; all of them where
+// logits tie) goes the exact way, one wavefront for the token in double.
+#include <utility>
+
 #include "internal.h"
 
 namespace lmoe {
 
-constexpr int kRouteWavesPerBlock = 4;
+struct RouteArgs {
+  const float *logits, *bias;
+  int32_t* idx;
+  float* w;
+  int32_t* load;
+  int64_t T;
+  int32_t E, k, score, renorm, groups, top_groups;
+  float scale;
+  int64_t first;   // the launch's first token
+};
 
+template <int CTRL>
+__device__ __forceinline__ float dpp_f(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+template <int CTRL>
+__device__ __forceinline__ double dpp_f64(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, 0xf, 0xf, true);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, 0xf, 0xf, true);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double readlane_f64(double v, int l) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)u, l), hi = __builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), l);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+
+// ------------------------------------------------------------------- exact way
+// Within rows of 16 lanes by rotations, then the four rows' results: a fifth of the
+// latency of six exchanges through LDS, and a rare token's latency is the kernel's tail.
+template <typename F>
+__device__ __forceinline__ double wave_reduce_f64(double v, F f) {
+  v = f(v, dpp_f64<0x128>(v));
+  v = f(v, dpp_f64<0x124>(v));
+  v = f(v, dpp_f64<0x122>(v));
+  v = f(v, dpp_f64<0x121>(v));
+  return f(f(readlane_f64(v, 0), readlane_f64(v, 16)), f(readlane_f64(v, 32), readlane_f64(v, 48)));
+}
 __device__ __forceinline__ double wave_max_f64(double v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = fmax(v, __shfl_xor(v, o, kWave));
-  return v;
+  return wave_reduce_f64(v, [](double a, double b) __attribute__((always_inline)) { return fmax(a, b); });
 }
 __device__ __forceinline__ double wave_sum_f64(double v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
-  return v;
+  return wave_reduce_f64(v, [](double a, double b) __attribute__((always_inline)) { return a + b; });
 }
 
-// 1 / (1 + e^-l); l = -inf gives 0.
-__device__ __forceinline__ double sigmoid_f64(double l) { return 1.0 / (1.0 + exp(-l)); }
+// LDS written by a lane of the wave, read by another.
+__device__ __forceinline__ void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 
+// A wave's: MG groups at most (0: there are none).
+template <int NE, int MG>
+struct RouteLds {
+  double key[64 * NE], gval[MG];
+  uint8_t keep[MG];
+};
 template <int NE>
-__global__ __launch_bounds__(64 * kRouteWavesPerBlock) void route_kernel(
-    const float* __restrict__ logits, const float* __restrict__ bias, int32_t* __restrict__ idx,
-    float* __restrict__ w, int32_t* __restrict__ load, int64_t T, int E, int k, int score, int renorm, int groups,
-    int top_groups, float scale) {
-  __shared__ double keys[kRouteWavesPerBlock][64 * NE];
-  __shared__ double gval[kRouteWavesPerBlock][64 * NE];
-  __shared__ uint8_t gkeep[kRouteWavesPerBlock][64 * NE];
-  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-  const int64_t t = (int64_t)blockIdx.x * kRouteWavesPerBlock + wv;
-  const bool on = t < T;
+struct RouteLds<NE, 0> {};
+
+// Token t by the whole wave: lane l holds experts l, l + 64, ...  hist: the block's loads.
+template <int NE, int MG>
+__device__ __forceinline__ void route_exact(const RouteArgs& a, int64_t t, RouteLds<NE, MG>& lds, int32_t* hist) {
+  const int lane = threadIdx.x & 63;
+  const int E = a.E;
   double l[NE], s[NE], key[NE];
 #pragma unroll
   for (int i = 0; i < NE; ++i) {
     const int e = i * 64 + lane;
-    const float f = on && e < E ? logits[t * E + e] : -INFINITY;
+    const float f = e < E ? a.logits[t * E + e] : -INFINITY;
     l[i] = f > -INFINITY ? (double)f : -INFINITY;
   }
-  if (score == MOE_SCORE_SOFTMAX) {
+  if (a.score == MOE_SCORE_SOFTMAX) {
     double m = l[0], z = 0.0;
 #pragma unroll
     for (int i = 1; i < NE; ++i) m = fmax(m, l[i]);
     m = wave_max_f64(m);
 #pragma unroll
     for (int i = 0; i < NE; ++i) {
-      s[i] = l[i] == -INFINITY ? 0.0 : l[i] == m ? 1.0 : exp(l[i] - m);
+      s[i] = l[i] == -INFINITY ? 0.0 : l[i] == m ? 1.0 : exp(l[i] - m);   // (+inf logits: an even share)
       z += s[i];
     }
     z = wave_sum_f64(z);
@@ -57,49 +103,49 @@ __global__ __launch_bounds__(64 * kRouteWavesPerBlock) void route_kernel(
     for (int i = 0; i < NE; ++i) s[i] = z > 0.0 ? s[i] / z : 0.0;
   } else {
 #pragma unroll
-    for (int i = 0; i < NE; ++i) s[i] = sigmoid_f64(l[i]);
+    for (int i = 0; i < NE; ++i) s[i] = 1.0 / (1.0 + exp(-l[i]));
   }
 #pragma unroll
   for (int i = 0; i < NE; ++i) {
     const int e = i * 64 + lane;
-    double c = l[i];
-    if (bias || groups > 1) {
-      c = s[i] + (bias && e < E ? (double)bias[e] : 0.0);
-      if (!(c > -INFINITY) || l[i] == -INFINITY) c = -INFINITY;
+    key[i] = l[i];
+    if (a.bias || a.groups > 1) {
+      const double c = s[i] + (a.bias && e < E ? (double)a.bias[e] : 0.0);
+      key[i] = c > -INFINITY && l[i] > -INFINITY ? c : -INFINITY;
     }
-    key[i] = c;
-    keys[wv][e] = c;
   }
-  if (groups > 1) {
-    __syncthreads();
-    const int n = E / groups;
-    for (int g = lane; g < groups; g += 64) {
-      double a = -INFINITY, b = -INFINITY;
+  if constexpr (MG > 0) if (a.groups > 1) {
+    const int n = E / a.groups;
+    wave_lds_fence();
+#pragma unroll
+    for (int i = 0; i < NE; ++i) lds.key[i * 64 + lane] = key[i];
+    wave_lds_fence();
+    for (int g = lane; g < a.groups; g += 64) {
+      double x = -INFINITY, y = -INFINITY;
       for (int j = 0; j < n; ++j) {
-        const double c = keys[wv][g * n + j];
-        b = fmax(b, fmin(a, c));
-        a = fmax(a, c);
+        const double c = lds.key[g * n + j];
+        y = fmax(y, fmin(x, c));
+        x = fmax(x, c);
       }
-      gval[wv][g] = a == -INFINITY ? a : b == -INFINITY ? a : a + b;
+      lds.gval[g] = y == -INFINITY ? x : x + y;
     }
-    __syncthreads();
-    for (int g = lane; g < groups; g += 64) {
+    wave_lds_fence();
+    for (int g = lane; g < a.groups; g += 64) {
+      const double v = lds.gval[g];
       int rank = 0;
-      for (int h = 0; h < groups; ++h)
-        rank += gval[wv][h] > gval[wv][g] || (gval[wv][h] == gval[wv][g] && h < g);
-      gkeep[wv][g] = rank < top_groups;
+      for (int h = 0; h < a.groups; ++h) rank += lds.gval[h] > v || (lds.gval[h] == v && h < g);
+      lds.keep[g] = rank < a.top_groups;
     }
-    __syncthreads();
+    wave_lds_fence();
 #pragma unroll
     for (int i = 0; i < NE; ++i) {
       const int e = i * 64 + lane;
-      if (e < E && !gkeep[wv][e / n]) key[i] = -INFINITY;
+      if (e < E && !lds.keep[e / n]) key[i] = -INFINITY;
     }
   }
-  if (!on) return;
   double mine = 0.0, sum = 0.0;
   int mine_e = -1;
-  for (int r = 0; r < k; ++r) {
+  for (int r = 0; r < a.k; ++r) {
     double best = -INFINITY;
     int be = 1 << 30;
 #pragma unroll
@@ -110,9 +156,9 @@ __global__ __launch_bounds__(64 * kRouteWavesPerBlock) void route_kernel(
       }
     const double m = wave_max_f64(best);
     if (m == -INFINITY) break;
-    int e = best == m ? be : 1 << 30;
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) e = min(e, __shfl_xor(e, o, kWave));
+    int e = 1 << 30;
+    for (uint64_t at = __ballot(best == m); at; at &= at - 1)   // (several lanes: a tie)
+      e = min(e, __builtin_amdgcn_readlane(be, __builtin_ctzll(at)));
     double se = 0.0;
 #pragma unroll
     for (int i = 0; i < NE; ++i)
@@ -120,44 +166,393 @@ __global__ __launch_bounds__(64 * kRouteWavesPerBlock) void route_kernel(
         key[i] = -INFINITY;
         se = s[i];
       }
-    se = __shfl(se, e & 63, kWave);
+    se = readlane_f64(se, e & 63);
     sum += se;
     if (lane == r) {
       mine = se;
       mine_e = e;
     }
   }
-  if (lane < k) {
-    idx[t * k + lane] = mine_e;
-    double v = scale * mine;
-    if (renorm) v = sum > 0.0 ? v / sum : 0.0;
-    w[t * k + lane] = (float)v;
-    if (load && mine_e >= 0) atomicAdd(load + mine_e, 1);
+  if (lane < a.k) {
+    double v = a.scale * mine;
+    if (a.renorm) v = sum > 0.0 ? v / sum : 0.0;
+    a.idx[t * a.k + lane] = mine_e;
+    a.w[t * a.k + lane] = (float)v;
+    if (a.load && mine_e >= 0) atomicAdd(hist + mine_e, 1);
   }
+}
+
+// -------------------------------------------------------------------- float way
+constexpr float kRouteMasked = -3e38f;    // a masked expert's value; every other is clamped to +-1e30
+constexpr float kRouteNone = -2e38f;      // below: masked
+constexpr float kRouteFar = 1e30f;
+// Two values are told apart if they differ by more than kRouteEps max(1, |value|): each
+// is off by at most 2^-19 of its size for the element number in its low bits, and by
+// 1.2e-6 for the score (v_exp_f32 and v_rcp_f32 of 1 ulp each, the rounded argument of
+// the exponential, the sum of the softmax, + b): 2 * (1.9e-6 + 1.2e-6) < 8e-6.
+constexpr float kRouteEps = 8e-6f;
+constexpr int kRouteGroupsFast = 16;      // one lane of a team for each group
+constexpr int kRouteWaves = 8;            // per block
+
+template <int CTRL>
+__device__ __forceinline__ int dpp_i(int v) {
+  return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, true);
+}
+// Exchanges within 4 lanes (quad_perm) or 16 (row_ror): every lane ends with the result.
+template <int LPT>
+__device__ __forceinline__ int team_max(int v) {
+  if constexpr (LPT == 4) {
+    v = max(v, dpp_i<0xB1>(v));
+    v = max(v, dpp_i<0x4E>(v));
+  } else {
+    v = max(v, dpp_i<0x128>(v));
+    v = max(v, dpp_i<0x124>(v));
+    v = max(v, dpp_i<0x122>(v));
+    v = max(v, dpp_i<0x121>(v));
+  }
+  return v;
+}
+template <int LPT>
+__device__ __forceinline__ float team_sum(float v) {
+  if constexpr (LPT == 4) {
+    v += dpp_f<0xB1>(v);
+    v += dpp_f<0x4E>(v);
+  } else {
+    v += dpp_f<0x128>(v);
+    v += dpp_f<0x124>(v);
+    v += dpp_f<0x122>(v);
+    v += dpp_f<0x121>(v);
+  }
+  return v;
+}
+// The value of the team's lane before this one (of its last lane for the first).
+template <int LPT>
+__device__ __forceinline__ int team_before(int v) {
+  if constexpr (LPT == 4) return dpp_i<0x93>(v);   // quad_perm 3 0 1 2
+  else return dpp_i<0x121>(v);
+}
+
+// A float's place in the order, as a signed integer, and back.  Integers sort without the
+// canonicalising copies that a float maximum of unknown bits takes.
+__device__ __forceinline__ int order_key(float f) {
+  const int i = __float_as_int(f);
+  return i ^ (int)((uint32_t)(i >> 31) >> 1);
+}
+__device__ __forceinline__ float from_order_key(int i) { return __int_as_float(i ^ (int)((uint32_t)(i >> 31) >> 1)); }
+
+// Batcher's odd-even merge sort: the comparisons of N values.
+template <int N>
+struct SortNet {
+  int n = 0;
+  uint8_t a[N * 6] = {}, b[N * 6] = {};
+  constexpr SortNet() {
+    for (int p = 1; p < N; p *= 2)
+      for (int q = p; q >= 1; q /= 2)
+        for (int j = q % p; j <= N - 1 - q; j += 2 * q)
+          for (int i = 0; i < q; ++i)
+            if (i + j + q < N && (i + j) / (2 * p) == (i + j + q) / (2 * p)) {
+              a[n] = (uint8_t)(i + j);
+              b[n++] = (uint8_t)(i + j + q);
+            }
+  }
+};
+// f(0), f(1), .. f(N - 1), the number a constant of each.
+template <typename F, int... I>
+__device__ __forceinline__ void each_of(F f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void each_of(F f) {
+  each_of(f, std::make_integer_sequence<int, N>{});
+}
+template <int N>
+__device__ __forceinline__ void sort_desc(int (&v)[N]) {
+  each_of<SortNet<N>().n>([&](auto i) __attribute__((always_inline)) {
+    constexpr SortNet<N> net;
+    constexpr int a = net.a[decltype(i)::value], b = net.b[decltype(i)::value];
+    const int hi = max(v[a], v[b]);
+    v[b] = min(v[a], v[b]);
+    v[a] = hi;
+  });
+}
+
+// Values e .. e + 3 of a row of E >= 4, those past its end `none`.  One load from inside
+// the row (of any alignment); where E is no multiple of four the last is shifted.
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+__device__ __forceinline__ void load_chunk(const float* row, int e, int E, float none, float* v) {
+  const int at = min(e, E - 4), past = e - at;
+  const f32x4 x = *reinterpret_cast<const f32x4_any*>(row + at);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = past > 0 ? none : x[i];
+  if (E & 3) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      v[i] = past == 1 ? x[i + 1] : v[i];
+      if (i < 2) v[i] = past == 2 ? x[i + 2] : v[i];
+      if (i < 1) v[i] = past == 3 ? x[i + 3] : v[i];
+    }
+  }
+}
+
+// LPT lanes per token, NCH chunks of four experts per lane (chunk c of lane j: experts
+// 4 (j + LPT c) ..), up to KT choices.
+template <int LPT, int NCH, int KT, bool GROUPS>
+__global__ __launch_bounds__(64 * kRouteWaves) void route_kernel(RouteArgs a) {
+  constexpr int NV = 4 * NCH, TPW = kWave / LPT, NE = (LPT * NV + 63) / 64;
+  constexpr int NL = NV < KT + 1 ? NV : KT + 1;     // entries of a lane's sorted list that can matter
+  constexpr int NM = KT / LPT + 1;                  // rounds (the choices and the next best) a lane keeps
+  const int masked = order_key(kRouteMasked), none = order_key(kRouteNone);
+  __shared__ RouteLds<NE, GROUPS ? kRouteGroupsFast : 0> lds[kRouteWaves];
+  __shared__ int16_t chosen[kRouteWaves][TPW][KT];
+  __shared__ int32_t hist[64 * NE];
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  const int j = lane % LPT, team = lane / LPT;
+  const int E = a.E, k = a.k;
+  if (a.load) {
+    for (int e = threadIdx.x; e < 64 * NE; e += blockDim.x) hist[e] = 0;
+    __syncthreads();
+  }
+  const bool use_c = a.bias || GROUPS;                                   // the choice is by c, else by the logits
+  const bool soft = a.score == MOE_SCORE_SOFTMAX;
+  const bool use_z = soft && (use_c || !a.renorm);
+
+  const int64_t tb = a.first + ((int64_t)blockIdx.x * kRouteWaves + wv) * TPW;   // the wave's tokens
+  uint64_t redo = 0;
+  if (tb < a.T) {
+    const int64_t t = tb + team;
+    const bool on = t < a.T;
+    const float* row = a.logits + (on ? t : a.T - 1) * E;
+    float v[NV];
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) load_chunk(row, 4 * (j + LPT * c), E, -INFINITY, v + 4 * c);
+    float m = kRouteMasked;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      v[i] = v[i] > -INFINITY ? fmaxf(v[i], -kRouteFar) : kRouteMasked;   // (a NaN compares false)
+      m = fmaxf(m, v[i]);
+    }
+    if (soft || !use_c) m = from_order_key(team_max<LPT>(order_key(m)));
+    bool amb = m > kRouteFar;   // (among them +inf)
+    float z = 1.f;
+    if (use_z) {
+      z = 0.f;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) z += __builtin_amdgcn_exp2f((v[i] - m) * 1.44269504f);
+      z = team_sum<LPT>(z);
+    }
+    if (use_c) {
+      const float rz = __builtin_amdgcn_rcpf(z);
+#pragma unroll
+      for (int c = 0; c < NCH; ++c) {
+        float b[4] = {0.f, 0.f, 0.f, 0.f};
+        if (a.bias) load_chunk(a.bias, 4 * (j + LPT * c), E, 0.f, b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float l = v[4 * c + i];
+          const float s = soft ? __builtin_amdgcn_exp2f((l - m) * 1.44269504f) * rz
+                               : __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(l * -1.44269504f));
+          const float x = s + b[i];
+          v[4 * c + i] = l > kRouteNone && x > -INFINITY ? fminf(fmaxf(x, -kRouteFar), kRouteFar) : kRouteMasked;
+        }
+      }
+    }
+    if constexpr (GROUPS) {
+      static_assert(sizeof(float2) * TPW * LPT * NCH <= sizeof(lds[0].key), "the chunks' two largest share the exact way's memory");
+      float2* mine = (float2*)lds[wv].key + team * (LPT * NCH);
+      wave_lds_fence();
+#pragma unroll
+      for (int c = 0; c < NCH; ++c) {
+        const float h0 = fmaxf(v[4 * c], v[4 * c + 1]), l0 = fminf(v[4 * c], v[4 * c + 1]);
+        const float h1 = fmaxf(v[4 * c + 2], v[4 * c + 3]), l1 = fminf(v[4 * c + 2], v[4 * c + 3]);
+        mine[j + LPT * c] = make_float2(fmaxf(h0, h1), fmaxf(fminf(h0, h1), fmaxf(l0, l1)));
+      }
+      wave_lds_fence();
+      const int n4 = E / a.groups / 4;      // chunks of a group
+      const float rn4 = 1.f / (float)n4;
+      float x = kRouteMasked, y = kRouteMasked;
+      if (j < a.groups) {
+#pragma unroll 4
+        for (int q = 0; q < n4; ++q) {
+          const float2 f = mine[j * n4 + q];
+          y = fmaxf(fmaxf(y, f.y), fminf(x, f.x));
+          x = fmaxf(x, f.x);
+        }
+      }
+      const float gv = x > kRouteNone ? (y > kRouteNone ? x + y : x) : kRouteMasked;
+      const float eps = 2.f * kRouteEps * fmaxf(1.f, fmaxf(fabsf(x), fabsf(y)));
+      const float lo = gv - eps, hi = gv + eps;
+      int above = 0, near = 0;   // groups surely better; groups that may be
+      each_of<15>([&](auto i) __attribute__((always_inline)) {
+        const float o = dpp_f<0x121 + decltype(i)::value>(gv);
+        above += o > hi;
+        near += o > lo;
+      });
+      const bool keep = above < a.top_groups;
+      amb |= gv > kRouteNone && keep && near >= a.top_groups;
+      const uint32_t kept = (uint32_t)(__ballot(keep && j < a.groups) >> (lane & 48));
+#pragma unroll
+      for (int c = 0; c < NCH; ++c) {
+        // (whole numbers below 128 and a reciprocal within 2^-24: the half keeps the quotient exact)
+        const int g = (int)(((float)(j + LPT * c) + 0.5f) * rn4);
+        const bool out = !((kept >> (g & 15)) & 1);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[4 * c + i] = out ? kRouteMasked : v[4 * c + i];
+      }
+    }
+    // The element's number in the low bits: the values of a lane are distinct, and sort with it.
+    int key[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) key[i] = (order_key(v[i]) & ~(NV - 1)) | i;
+    sort_desc(key);
+    // Round r finds the team's r-th largest among the heads of the lanes' lists (KT + 1
+    // rounds whatever k is: leaving early costs more in branches than the rounds).
+    int kept_key[NM];
+#pragma unroll
+    for (int q = 0; q < NM; ++q) kept_key[q] = masked;
+    bool tie = false;
+    each_of<KT + 1>([&](auto rc) __attribute__((always_inline)) {
+      constexpr int r = decltype(rc)::value;
+      const int M = team_max<LPT>(key[0]);
+      kept_key[r / LPT] = j == r % LPT ? M : kept_key[r / LPT];
+      if constexpr (r < KT) {
+        const bool win = key[0] == M;
+        // two heads alike (their numbers too): the values tie in float
+        tie |= r < k && __popcll(__ballot(win && M > none)) * LPT != __popcll(__ballot(M > none));
+        if (win) chosen[wv][team][r] = (int16_t)(4 * (j + LPT * ((key[0] & (NV - 1)) >> 2)) + (key[0] & 3));
+#pragma unroll
+        for (int q = 0; q + 1 < NL; ++q) key[q] = win ? key[q + 1] : key[q];
+        key[NL - 1] = win ? masked : key[NL - 1];
+      }
+    });
+    amb |= tie;
+    wave_lds_fence();
+    // Neighbours in the order too close to tell, the next best after the last choice too.
+#pragma unroll
+    for (int q = 0; q < NM; ++q) {
+      const int r = q * LPT + j;
+      const int before = q == 0 ? team_before<LPT>(kept_key[0])
+                                : j == 0 ? team_before<LPT>(kept_key[q > 0 ? q - 1 : 0]) : team_before<LPT>(kept_key[q]);
+      const float x = from_order_key(kept_key[q]), p = from_order_key(before);
+      amb |= r >= 1 && r <= k && x > kRouteNone && p - x <= kRouteEps * fmaxf(1.f, fabsf(p));
+    }
+    float s[NM], sum = 0.f;
+    int e[NM];
+#pragma unroll
+    for (int q = 0; q < NM; ++q) {
+      const int r = q * LPT + j;
+      s[q] = 0.f;
+      e[q] = -1;
+      if (r < k && kept_key[q] > none) {
+        e[q] = chosen[wv][team][r];
+        const float l = row[e[q]];
+        s[q] = soft ? expf(l - m) : 1.f / (1.f + expf(-l));
+        amb |= (soft ? l - m : l) < -80.f && (a.renorm || !soft);   // next to float's smallest numbers
+      }
+      sum += s[q];
+    }
+    wave_lds_fence();
+    float f = a.scale;
+    if (a.renorm) {
+      sum = team_sum<LPT>(sum);
+      f = sum > 0.f ? a.scale / sum : 0.f;
+    } else if (soft) {
+      f = a.scale / z;
+    }
+    redo = __ballot(amb && on);
+    const uint64_t lanes = (LPT == 16 ? 0xffffull : 0xfull) << (lane & ~(LPT - 1));
+    if (on && !(redo & lanes)) {
+#pragma unroll
+      for (int q = 0; q < NM; ++q) {
+        const int r = q * LPT + j;
+        if (r < k) {
+          a.idx[t * k + r] = e[q];
+          a.w[t * k + r] = s[q] * f;
+          if (a.load && e[q] >= 0) atomicAdd(&hist[e[q]], 1);
+        }
+      }
+    }
+  }
+  while (redo) {
+    const int l = __builtin_ctzll(redo) / LPT;
+    redo &= ~((LPT == 16 ? 0xffffull : 0xfull) << (l * LPT));
+    route_exact(a, tb + l, lds[wv], hist);
+  }
+  if (a.load) {
+    __syncthreads();
+    for (int e = threadIdx.x; e < E; e += blockDim.x)
+      if (hist[e]) atomicAdd(a.load + e, hist[e]);
+  }
+}
+
+// Every token the exact way: groups that are no whole chunks, or many.
+template <int NE>
+__global__ __launch_bounds__(256) void route_exact_kernel(RouteArgs a) {
+  __shared__ RouteLds<NE, 64 * NE> lds[4];
+  __shared__ int32_t hist[64 * NE];
+  for (int e = threadIdx.x; e < 64 * NE; e += blockDim.x) hist[e] = 0;
+  __syncthreads();
+  const int wv = threadIdx.x >> 6;
+  for (int64_t t = (int64_t)blockIdx.x * 4 + wv; t < a.T; t += (int64_t)gridDim.x * 4) route_exact<NE>(a, t, lds[wv], hist);
+  if (a.load) {
+    __syncthreads();
+    for (int e = threadIdx.x; e < a.E; e += blockDim.x)
+      if (hist[e]) atomicAdd(a.load + e, hist[e]);
+  }
+}
+
+template <int LPT, int NCH, bool GROUPS>
+static void launch_route_n(const RouteArgs& a, hipStream_t s) {
+  const int64_t tokens = (int64_t)kRouteWaves * (kWave / LPT);   // of a block
+  const int64_t most = tokens << 22;                             // of a launch (its thread count is 32 bits)
+  auto go = [&](auto kern) {
+    RouteArgs b = a;
+    for (b.first = 0; b.first < a.T; b.first += most) {
+      const int64_t n = std::min(a.T - b.first, most);
+      hipLaunchKernelGGL(kern, dim3((unsigned)((n + tokens - 1) / tokens)), dim3(64 * kRouteWaves), 0, s, b);
+    }
+  };
+  if (a.k <= 2) go(route_kernel<LPT, NCH, 2, GROUPS>);
+  else if (a.k <= 4) go(route_kernel<LPT, NCH, 4, GROUPS>);
+  else if (a.k <= 8) go(route_kernel<LPT, NCH, 8, GROUPS>);
+  else go(route_kernel<LPT, NCH, 16, GROUPS>);
 }
 
 void launch_route(const moe_route_cfg& c, const float* logits, const float* bias, int32_t* idx, float* w,
                   int32_t* load, hipStream_t s) {
   if (c.T == 0) return;
-  const unsigned blocks = (unsigned)((c.T + kRouteWavesPerBlock - 1) / kRouteWavesPerBlock);
-  auto go = [&](auto kern) {
-    hipLaunchKernelGGL(kern, dim3(blocks), dim3(64 * kRouteWavesPerBlock), 0, s, logits, bias, idx, w, load, c.T, c.E,
-                       c.k, c.score, c.renorm, c.groups, c.top_groups, c.scale);
-  };
-  if (c.E <= 64) go(route_kernel<1>);
-  else if (c.E <= 128) go(route_kernel<2>);
-  else if (c.E <= 256) go(route_kernel<4>);
-  else go(route_kernel<8>);
+  const RouteArgs a{logits, bias, idx, w, load, c.T, c.E, c.k, c.score, c.renorm, c.groups, c.top_groups, c.scale, 0};
+  // E < 4 has no whole load; groups that are no whole chunks or more than a team's lanes
+  // have no place in it.
+  if (c.E < 4 || (c.groups > 1 && (c.groups > kRouteGroupsFast || (c.E / c.groups) % 4 != 0))) {
+    const unsigned blocks = (unsigned)std::min<int64_t>((c.T + 3) / 4, 8 * num_cus());
+    auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(blocks), dim3(256), 0, s, a); };
+    if (c.E <= 64) go(route_exact_kernel<1>);
+    else if (c.E <= 128) go(route_exact_kernel<2>);
+    else if (c.E <= 256) go(route_exact_kernel<4>);
+    else go(route_exact_kernel<8>);
+  } else if (c.groups > 1) {
+    if (c.E <= 64) launch_route_n<16, 1, true>(a, s);
+    else if (c.E <= 128) launch_route_n<16, 2, true>(a, s);
+    else if (c.E <= 256) launch_route_n<16, 4, true>(a, s);
+    else launch_route_n<16, 8, true>(a, s);
+  } else {
+    if (c.E <= 16) launch_route_n<4, 1, false>(a, s);
+    else if (c.E <= 64) launch_route_n<4, 4, false>(a, s);
+    else if (c.E <= 128) launch_route_n<16, 2, false>(a, s);
+    else if (c.E <= 256) launch_route_n<16, 4, false>(a, s);
+    else launch_route_n<16, 8, false>(a, s);
+  }
 }
 
 // ------------------------------------------------------------------- gradient
+constexpr int kRouteBwdWaves = 4;
 template <int NE>
-__global__ __launch_bounds__(64 * kRouteWavesPerBlock) void route_bwd_kernel(
+__global__ __launch_bounds__(64 * kRouteBwdWaves) void route_bwd_kernel(
     const float* __restrict__ logits, const int32_t* __restrict__ idx, const float* __restrict__ w,
     const float* __restrict__ dw, float* __restrict__ dlogits, int64_t T, int E, int k, int score, int renorm,
     float scale) {
   const int lane = threadIdx.x & 63;
-  const int64_t t = (int64_t)blockIdx.x * kRouteWavesPerBlock + (threadIdx.x >> 6);
+  const int64_t t = (int64_t)blockIdx.x * kRouteBwdWaves + (threadIdx.x >> 6);
   if (t >= T) return;
   int er = lane < k ? idx[t * k + lane] : -1;
   if (er < 0 || er >= E) er = -1;
@@ -203,9 +598,9 @@ __global__ __launch_bounds__(64 * kRouteWavesPerBlock) void route_bwd_kernel(
 void launch_route_bwd(const moe_route_cfg& c, const float* logits, const int32_t* idx, const float* w,
                       const float* dw, float* dlogits, hipStream_t s) {
   if (c.T == 0) return;
-  const unsigned blocks = (unsigned)((c.T + kRouteWavesPerBlock - 1) / kRouteWavesPerBlock);
+  const unsigned blocks = (unsigned)((c.T + kRouteBwdWaves - 1) / kRouteBwdWaves);
   auto go = [&](auto kern) {
-    hipLaunchKernelGGL(kern, dim3(blocks), dim3(64 * kRouteWavesPerBlock), 0, s, logits, idx, w, dw, dlogits, c.T, c.E,
+    hipLaunchKernelGGL(kern, dim3(blocks), dim3(64 * kRouteBwdWaves), 0, s, logits, idx, w, dw, dlogits, c.T, c.E,
                        c.k, c.score, c.renorm, c.scale);
   };
   if (c.E <= 64) go(route_bwd_kernel<1>);
