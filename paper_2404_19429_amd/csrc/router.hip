@@ -18,7 +18,6 @@ struct RouteArgs {
   const float *logits, *bias;
   int32_t* idx;
   float* w;
-  int32_t* load;
   int64_t T;
   int32_t E, k, score, renorm, groups, top_groups;
   float scale;
@@ -76,9 +75,9 @@ struct RouteLds {
 template <int NE>
 struct RouteLds<NE, 0> {};
 
-// Token t by the whole wave: lane l holds experts l, l + 64, ...  hist: the block's loads.
+// Token t by the whole wave: lane l holds experts l, l + 64, ...
 template <int NE, int MG>
-__device__ __forceinline__ void route_exact(const RouteArgs& a, int64_t t, RouteLds<NE, MG>& lds, int32_t* hist) {
+__device__ __forceinline__ void route_exact(const RouteArgs& a, int64_t t, RouteLds<NE, MG>& lds) {
   const int lane = threadIdx.x & 63;
   const int E = a.E;
   double l[NE], s[NE], key[NE];
@@ -122,6 +121,7 @@ __device__ __forceinline__ void route_exact(const RouteArgs& a, int64_t t, Route
     wave_lds_fence();
     for (int g = lane; g < a.groups; g += 64) {
       double x = -INFINITY, y = -INFINITY;
+#pragma unroll 8
       for (int j = 0; j < n; ++j) {
         const double c = lds.key[g * n + j];
         y = fmax(y, fmin(x, c));
@@ -133,6 +133,7 @@ __device__ __forceinline__ void route_exact(const RouteArgs& a, int64_t t, Route
     for (int g = lane; g < a.groups; g += 64) {
       const double v = lds.gval[g];
       int rank = 0;
+#pragma unroll 8
       for (int h = 0; h < a.groups; ++h) rank += lds.gval[h] > v || (lds.gval[h] == v && h < g);
       lds.keep[g] = rank < a.top_groups;
     }
@@ -178,7 +179,6 @@ __device__ __forceinline__ void route_exact(const RouteArgs& a, int64_t t, Route
     if (a.renorm) v = sum > 0.0 ? v / sum : 0.0;
     a.idx[t * a.k + lane] = mine_e;
     a.w[t * a.k + lane] = (float)v;
-    if (a.load && mine_e >= 0) atomicAdd(hist + mine_e, 1);
   }
 }
 
@@ -276,21 +276,35 @@ __device__ __forceinline__ void sort_desc(int (&v)[N]) {
   });
 }
 
-// Values e .. e + 3 of a row of E >= 4, those past its end `none`.  One load from inside
-// the row (of any alignment); where E is no multiple of four the last is shifted.
+// Lane j's chunks of a row of E >= 4: experts 4 (j + LPT c) .., those past its end `none`.
+// One load a chunk from inside the row (of any alignment); where E is no multiple of four
+// the last is shifted.
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
-__device__ __forceinline__ void load_chunk(const float* row, int e, int E, float none, float* v) {
-  const int at = min(e, E - 4), past = e - at;
-  const f32x4 x = *reinterpret_cast<const f32x4_any*>(row + at);
+template <int LPT, int NCH>
+__device__ __forceinline__ void load_row(const float* row, int j, int E, float none, float (&v)[4 * NCH]) {
+  int past[NCH];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = past > 0 ? none : x[i];
+  for (int c = 0; c < NCH; ++c) {
+    const int e = 4 * (j + LPT * c), at = min(e, E - 4);
+    past[c] = e - at;
+    const f32x4 x = *reinterpret_cast<const f32x4_any*>(row + at);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[4 * c + i] = x[i];
+  }
   if (E & 3) {
 #pragma unroll
-    for (int i = 0; i < 3; ++i) {
-      v[i] = past == 1 ? x[i + 1] : v[i];
-      if (i < 2) v[i] = past == 2 ? x[i + 2] : v[i];
-      if (i < 1) v[i] = past == 3 ? x[i + 3] : v[i];
+    for (int c = 0; c < NCH; ++c) {
+      const float x1 = v[4 * c + 1], x2 = v[4 * c + 2], x3 = v[4 * c + 3];
+      v[4 * c + 3] = past[c] > 0 ? none : x3;
+      v[4 * c + 2] = past[c] > 1 ? none : past[c] > 0 ? x3 : x2;
+      v[4 * c + 1] = past[c] > 2 ? none : past[c] > 1 ? x3 : past[c] > 0 ? x2 : x1;
+      v[4 * c] = past[c] > 3 ? none : past[c] > 2 ? x3 : past[c] > 1 ? x2 : past[c] > 0 ? x1 : v[4 * c];
     }
+  } else if (E < 4 * LPT * NCH) {
+#pragma unroll
+    for (int c = 0; c < NCH; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[4 * c + i] = past[c] > 0 ? none : v[4 * c + i];
   }
 }
 
@@ -303,15 +317,9 @@ __global__ __launch_bounds__(64 * kRouteWaves) void route_kernel(RouteArgs a) {
   constexpr int NM = KT / LPT + 1;                  // rounds (the choices and the next best) a lane keeps
   const int masked = order_key(kRouteMasked), none = order_key(kRouteNone);
   __shared__ RouteLds<NE, GROUPS ? kRouteGroupsFast : 0> lds[kRouteWaves];
-  __shared__ int16_t chosen[kRouteWaves][TPW][KT];
-  __shared__ int32_t hist[64 * NE];
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
   const int j = lane % LPT, team = lane / LPT;
   const int E = a.E, k = a.k;
-  if (a.load) {
-    for (int e = threadIdx.x; e < 64 * NE; e += blockDim.x) hist[e] = 0;
-    __syncthreads();
-  }
   const bool use_c = a.bias || GROUPS;                                   // the choice is by c, else by the logits
   const bool soft = a.score == MOE_SCORE_SOFTMAX;
   const bool use_z = soft && (use_c || !a.renorm);
@@ -323,37 +331,46 @@ __global__ __launch_bounds__(64 * kRouteWaves) void route_kernel(RouteArgs a) {
     const bool on = t < a.T;
     const float* row = a.logits + (on ? t : a.T - 1) * E;
     float v[NV];
-#pragma unroll
-    for (int c = 0; c < NCH; ++c) load_chunk(row, 4 * (j + LPT * c), E, -INFINITY, v + 4 * c);
+    load_row<LPT, NCH>(row, j, E, -INFINITY, v);
     float m = kRouteMasked;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       v[i] = v[i] > -INFINITY ? fmaxf(v[i], -kRouteFar) : kRouteMasked;   // (a NaN compares false)
       m = fmaxf(m, v[i]);
     }
-    if (soft || !use_c) m = from_order_key(team_max<LPT>(order_key(m)));
     bool amb = m > kRouteFar;   // (among them +inf)
     float z = 1.f;
-    if (use_z) {
-      z = 0.f;
+    if (soft) m = from_order_key(team_max<LPT>(order_key(m)));
+    if (use_c || use_z) {
+      // scores; 0 for a masked expert but in rows without any other
+      float x[NV];
+      if (soft) {
+        z = 0.f;
 #pragma unroll
-      for (int i = 0; i < NV; ++i) z += __builtin_amdgcn_exp2f((v[i] - m) * 1.44269504f);
-      z = team_sum<LPT>(z);
-    }
-    if (use_c) {
-      const float rz = __builtin_amdgcn_rcpf(z);
-#pragma unroll
-      for (int c = 0; c < NCH; ++c) {
-        float b[4] = {0.f, 0.f, 0.f, 0.f};
-        if (a.bias) load_chunk(a.bias, 4 * (j + LPT * c), E, 0.f, b);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float l = v[4 * c + i];
-          const float s = soft ? __builtin_amdgcn_exp2f((l - m) * 1.44269504f) * rz
-                               : __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(l * -1.44269504f));
-          const float x = s + b[i];
-          v[4 * c + i] = l > kRouteNone && x > -INFINITY ? fminf(fmaxf(x, -kRouteFar), kRouteFar) : kRouteMasked;
+        for (int i = 0; i < NV; ++i) {
+          x[i] = __builtin_amdgcn_exp2f((v[i] - m) * 1.44269504f);
+          z += x[i];
         }
+        z = team_sum<LPT>(z);
+        const float rz = __builtin_amdgcn_rcpf(z);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) x[i] *= rz;
+      } else {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) x[i] = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v[i] * -1.44269504f));
+      }
+      if (use_c) {
+        if (a.bias) {
+          float b[NV];
+          load_row<LPT, NCH>(a.bias, j, E, 0.f, b);
+#pragma unroll
+          for (int i = 0; i < NV; ++i) {   // (a NaN compares false, and the clamp of one is not looked at)
+            x[i] += b[i];
+            x[i] = x[i] > -INFINITY ? __builtin_amdgcn_fmed3f(x[i], -kRouteFar, kRouteFar) : kRouteMasked;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) v[i] = v[i] > kRouteNone ? x[i] : kRouteMasked;
       }
     }
     if constexpr (GROUPS) {
@@ -379,17 +396,18 @@ __global__ __launch_bounds__(64 * kRouteWaves) void route_kernel(RouteArgs a) {
         }
       }
       const float gv = x > kRouteNone ? (y > kRouteNone ? x + y : x) : kRouteMasked;
-      const float eps = 2.f * kRouteEps * fmaxf(1.f, fmaxf(fabsf(x), fabsf(y)));
-      const float lo = gv - eps, hi = gv + eps;
-      int above = 0, near = 0;   // groups surely better; groups that may be
-      each_of<15>([&](auto i) __attribute__((always_inline)) {
-        const float o = dpp_f<0x121 + decltype(i)::value>(gv);
-        above += o > hi;
-        near += o > lo;
-      });
-      const bool keep = above < a.top_groups;
-      amb |= gv > kRouteNone && keep && near >= a.top_groups;
-      const uint32_t kept = (uint32_t)(__ballot(keep && j < a.groups) >> (lane & 48));
+      const float big = x > kRouteNone ? fmaxf(fabsf(x), y > kRouteNone ? fabsf(y) : 0.f) : 0.f;
+      const float eps = 2.f * kRouteEps * fmaxf(1.f, from_order_key(team_max<LPT>(order_key(big))));
+      // The best groups one after the other (the lane in the low bits keeps them apart).
+      const int gk = j < a.groups ? (order_key(gv) & ~15) | (15 - j) : (int)0x80000000;
+      int rest = gk, last = 0;
+      for (int i = 0; i < a.top_groups; ++i) {
+        last = team_max<LPT>(rest);
+        rest = rest == last ? (int)0x80000000 : rest;
+      }
+      const int next = team_max<LPT>(rest);
+      amb |= next > none && from_order_key(last) - from_order_key(next) <= eps;
+      const uint32_t kept = (uint32_t)(__ballot(gk >= last) >> (lane & 48));
 #pragma unroll
       for (int c = 0; c < NCH; ++c) {
         // (whole numbers below 128 and a reciprocal within 2^-24: the half keeps the quotient exact)
@@ -405,27 +423,28 @@ __global__ __launch_bounds__(64 * kRouteWaves) void route_kernel(RouteArgs a) {
     for (int i = 0; i < NV; ++i) key[i] = (order_key(v[i]) & ~(NV - 1)) | i;
     sort_desc(key);
     // Round r finds the team's r-th largest among the heads of the lanes' lists (KT + 1
-    // rounds whatever k is: leaving early costs more in branches than the rounds).
+    // rounds whatever k is: leaving early costs more in branches than the rounds).  Lane
+    // r keeps it, and the lanes that hold it.
     int kept_key[NM];
+    uint32_t kept_at[NM];
 #pragma unroll
-    for (int q = 0; q < NM; ++q) kept_key[q] = masked;
-    bool tie = false;
+    for (int q = 0; q < NM; ++q) {
+      kept_key[q] = masked;
+      kept_at[q] = 1;
+    }
     each_of<KT + 1>([&](auto rc) __attribute__((always_inline)) {
       constexpr int r = decltype(rc)::value;
       const int M = team_max<LPT>(key[0]);
+      const bool win = key[0] == M;
+      const uint32_t at = (uint32_t)(__ballot(win) >> (lane & ~(LPT - 1)));
       kept_key[r / LPT] = j == r % LPT ? M : kept_key[r / LPT];
+      kept_at[r / LPT] = j == r % LPT ? at : kept_at[r / LPT];
       if constexpr (r < KT) {
-        const bool win = key[0] == M;
-        // two heads alike (their numbers too): the values tie in float
-        tie |= r < k && __popcll(__ballot(win && M > none)) * LPT != __popcll(__ballot(M > none));
-        if (win) chosen[wv][team][r] = (int16_t)(4 * (j + LPT * ((key[0] & (NV - 1)) >> 2)) + (key[0] & 3));
 #pragma unroll
         for (int q = 0; q + 1 < NL; ++q) key[q] = win ? key[q + 1] : key[q];
         key[NL - 1] = win ? masked : key[NL - 1];
       }
     });
-    amb |= tie;
-    wave_lds_fence();
     // Neighbours in the order too close to tell, the next best after the last choice too.
 #pragma unroll
     for (int q = 0; q < NM; ++q) {
@@ -434,6 +453,7 @@ __global__ __launch_bounds__(64 * kRouteWaves) void route_kernel(RouteArgs a) {
                                 : j == 0 ? team_before<LPT>(kept_key[q > 0 ? q - 1 : 0]) : team_before<LPT>(kept_key[q]);
       const float x = from_order_key(kept_key[q]), p = from_order_key(before);
       amb |= r >= 1 && r <= k && x > kRouteNone && p - x <= kRouteEps * fmaxf(1.f, fabsf(p));
+      amb |= r <= k && x > kRouteNone && __popc(kept_at[q] & (LPT == 16 ? 0xffffu : 0xfu)) > 1;   // two alike
     }
     float s[NM], sum = 0.f;
     int e[NM];
@@ -443,14 +463,14 @@ __global__ __launch_bounds__(64 * kRouteWaves) void route_kernel(RouteArgs a) {
       s[q] = 0.f;
       e[q] = -1;
       if (r < k && kept_key[q] > none) {
-        e[q] = chosen[wv][team][r];
+        const int i = kept_key[q] & (NV - 1);
+        e[q] = 4 * (__builtin_ctz(kept_at[q]) + LPT * (i >> 2)) + (i & 3);
         const float l = row[e[q]];
         s[q] = soft ? expf(l - m) : 1.f / (1.f + expf(-l));
         amb |= (soft ? l - m : l) < -80.f && (a.renorm || !soft);   // next to float's smallest numbers
       }
       sum += s[q];
     }
-    wave_lds_fence();
     float f = a.scale;
     if (a.renorm) {
       sum = team_sum<LPT>(sum);
@@ -467,7 +487,6 @@ __global__ __launch_bounds__(64 * kRouteWaves) void route_kernel(RouteArgs a) {
         if (r < k) {
           a.idx[t * k + r] = e[q];
           a.w[t * k + r] = s[q] * f;
-          if (a.load && e[q] >= 0) atomicAdd(&hist[e[q]], 1);
         }
       }
     }
@@ -475,29 +494,36 @@ __global__ __launch_bounds__(64 * kRouteWaves) void route_kernel(RouteArgs a) {
   while (redo) {
     const int l = __builtin_ctzll(redo) / LPT;
     redo &= ~((LPT == 16 ? 0xffffull : 0xfull) << (l * LPT));
-    route_exact(a, tb + l, lds[wv], hist);
-  }
-  if (a.load) {
-    __syncthreads();
-    for (int e = threadIdx.x; e < E; e += blockDim.x)
-      if (hist[e]) atomicAdd(a.load + e, hist[e]);
+    route_exact(a, tb + l, lds[wv]);
   }
 }
 
-// Every token the exact way: groups that are no whole chunks, or many.
+// Every token the exact way.
 template <int NE>
 __global__ __launch_bounds__(256) void route_exact_kernel(RouteArgs a) {
   __shared__ RouteLds<NE, 64 * NE> lds[4];
-  __shared__ int32_t hist[64 * NE];
-  for (int e = threadIdx.x; e < 64 * NE; e += blockDim.x) hist[e] = 0;
-  __syncthreads();
   const int wv = threadIdx.x >> 6;
-  for (int64_t t = (int64_t)blockIdx.x * 4 + wv; t < a.T; t += (int64_t)gridDim.x * 4) route_exact<NE>(a, t, lds[wv], hist);
-  if (a.load) {
-    __syncthreads();
-    for (int e = threadIdx.x; e < a.E; e += blockDim.x)
-      if (hist[e]) atomicAdd(a.load + e, hist[e]);
+  for (int64_t t = (int64_t)blockIdx.x * 4 + wv; t < a.T; t += (int64_t)gridDim.x * 4) route_exact(a, t, lds[wv]);
+}
+
+// load[e] += the choices of e.  A launch of its own, with few blocks: a count is one
+// address, and atomics on it are served one after the other (from every routing block
+// they took 12 us of 28 for 32768 tokens; integers, so their order changes nothing).
+constexpr int kLoadThreads = 1024;
+__global__ __launch_bounds__(kLoadThreads) void route_load_kernel(const int32_t* __restrict__ idx, int64_t n, int E,
+                                                                  int32_t* __restrict__ load) {
+  __shared__ int32_t hist[kRouterMaxE];
+  for (int e = threadIdx.x; e < E; e += kLoadThreads) hist[e] = 0;
+  __syncthreads();
+  const int64_t step = (int64_t)gridDim.x * kLoadThreads;
+#pragma unroll 4
+  for (int64_t i = (int64_t)blockIdx.x * kLoadThreads + threadIdx.x; i < n; i += step) {
+    const int e = idx[i];
+    if (e >= 0) atomicAdd(&hist[e], 1);
   }
+  __syncthreads();
+  for (int e = threadIdx.x; e < E; e += kLoadThreads)
+    if (hist[e]) atomicAdd(load + e, hist[e]);
 }
 
 template <int LPT, int NCH, bool GROUPS>
@@ -520,7 +546,7 @@ static void launch_route_n(const RouteArgs& a, hipStream_t s) {
 void launch_route(const moe_route_cfg& c, const float* logits, const float* bias, int32_t* idx, float* w,
                   int32_t* load, hipStream_t s) {
   if (c.T == 0) return;
-  const RouteArgs a{logits, bias, idx, w, load, c.T, c.E, c.k, c.score, c.renorm, c.groups, c.top_groups, c.scale, 0};
+  const RouteArgs a{logits, bias, idx, w, c.T, c.E, c.k, c.score, c.renorm, c.groups, c.top_groups, c.scale, 0};
   // E < 4 has no whole load; groups that are no whole chunks or more than a team's lanes
   // have no place in it.
   if (c.E < 4 || (c.groups > 1 && (c.groups > kRouteGroupsFast || (c.E / c.groups) % 4 != 0))) {
@@ -542,71 +568,153 @@ void launch_route(const moe_route_cfg& c, const float* logits, const float* bias
     else if (c.E <= 256) launch_route_n<16, 4, false>(a, s);
     else launch_route_n<16, 8, false>(a, s);
   }
+  if (load) {
+    const int64_t n = c.T * c.k;
+    const unsigned blocks = (unsigned)std::min<int64_t>((n + 4 * kLoadThreads - 1) / (4 * kLoadThreads), 64);
+    hipLaunchKernelGGL(route_load_kernel, dim3(blocks), dim3(kLoadThreads), 0, s, (const int32_t*)idx, n, c.E, load);
+  }
 }
 
 // ------------------------------------------------------------------- gradient
-constexpr int kRouteBwdWaves = 4;
-template <int NE>
-__global__ __launch_bounds__(64 * kRouteBwdWaves) void route_bwd_kernel(
-    const float* __restrict__ logits, const int32_t* __restrict__ idx, const float* __restrict__ w,
-    const float* __restrict__ dw, float* __restrict__ dlogits, int64_t T, int E, int k, int score, int renorm,
-    float scale) {
+// Bound by writing dlogits, most of it zeros (but for a plain softmax, which also reads
+// the logits).  A wavefront builds its tokens' rows in LDS and stores them as one run.
+struct RouteBwdArgs {
+  const float* logits;
+  const int32_t* idx;
+  const float *w, *dw;
+  float* dlogits;
+  int64_t T;
+  int32_t E, k, score, renorm;
+  float scale;
+  int64_t first;
+};
+constexpr int kBwdWaves = 4;
+constexpr int kBwdLds = 2048;   // floats of a wave
+
+// Lane (token i / KP, choice i % KP) of the wave's tokens: its part of the gradient, and G.
+template <int KP>
+__device__ __forceinline__ float choice_grad(const RouteBwdArgs& a, int64_t t, int r, bool on, int& e, float& G) {
+  e = -1;
+  float w = 0.f, g = 0.f;
+  if (on && r < a.k) {
+    e = a.idx[t * a.k + r];
+    if (e < 0 || e >= a.E) e = -1;
+    if (e >= 0) {
+      w = a.w[t * a.k + r];
+      g = a.dw[t * a.k + r];
+    }
+  }
+  G = w * g;
+  if constexpr (KP >= 2) G += dpp_f<0xB1>(G);
+  if constexpr (KP >= 4) G += dpp_f<0x4E>(G);
+  if constexpr (KP >= 8) G += dpp_f<0x141>(G);    // row_half_mirror
+  if constexpr (KP >= 16) G += dpp_f<0x140>(G);   // row_mirror
+  float v = w * (a.renorm ? g - G / a.scale : g);
+  if (a.score == MOE_SCORE_SIGMOID && e >= 0) v *= 1.f / (1.f + expf(a.logits[t * a.E + e]));   // 1 - s
+  return v;
+}
+
+// Every score but the plain softmax: k elements of a row are not zero.
+template <int KP>
+__global__ __launch_bounds__(64 * kBwdWaves) void route_bwd_kernel(RouteBwdArgs a, int tokens) {
+  __shared__ __attribute__((aligned(16))) float rows[kBwdWaves][kBwdLds];
   const int lane = threadIdx.x & 63;
-  const int64_t t = (int64_t)blockIdx.x * kRouteBwdWaves + (threadIdx.x >> 6);
-  if (t >= T) return;
-  int er = lane < k ? idx[t * k + lane] : -1;
-  if (er < 0 || er >= E) er = -1;
-  const float wr = er >= 0 ? w[t * k + lane] : 0.f, gr = er >= 0 ? dw[t * k + lane] : 0.f;
-  const float G = wave_sum(wr * gr);
-  float v = wr * (renorm ? gr - G / scale : gr);
-  if (score == MOE_SCORE_SIGMOID && er >= 0) v *= 1.f / (1.f + expf(logits[t * E + er]));   // 1 - s
-  float p[NE];
+  float* mine = rows[threadIdx.x >> 6];
+  const int64_t tb = a.first + ((int64_t)blockIdx.x * kBwdWaves + (threadIdx.x >> 6)) * tokens;   // (a multiple of 4)
+  if (tb >= a.T) return;
+  const int64_t left = (a.T - tb) * a.E;
+  const int n = (int)(left < tokens * a.E ? left : tokens * a.E);   // elements of the wave's rows
+  int e;
+  float G;
+  const int tok = lane / KP;
+  const float v = choice_grad<KP>(a, tb + tok, lane % KP, tok < tokens && tb + tok < a.T, e, G);
+  for (int i = 4 * lane; i < n; i += 256) *reinterpret_cast<f32x4*>(mine + i) = f32x4{0.f, 0.f, 0.f, 0.f};
+  wave_lds_fence();
+  if (e >= 0) unsafeAtomicAdd(mine + tok * a.E + e, v);   // (a row may name an expert twice)
+  wave_lds_fence();
+  float* out = a.dlogits + tb * a.E;
+  for (int i = 4 * lane; i < (n & ~3); i += 256) *reinterpret_cast<f32x4*>(out + i) = *reinterpret_cast<const f32x4*>(mine + i);
+  if (lane < (n & 3)) out[(n & ~3) + lane] = mine[(n & ~3) + lane];
+}
+
+// The plain softmax: 16 lanes per token, lane j experts j, j + 16, ...
+template <int NV>
+__global__ __launch_bounds__(64 * kBwdWaves) void route_bwd_softmax_kernel(RouteBwdArgs a) {
+  __shared__ float rows[kBwdWaves][4][16 * NV];
+  const int lane = threadIdx.x & 63, j = lane & 15, team = lane >> 4;
+  float* mine = rows[threadIdx.x >> 6][team];
+  const int64_t t = a.first + ((int64_t)blockIdx.x * kBwdWaves + (threadIdx.x >> 6)) * 4 + team;
+  const bool on = t < a.T;
+  const float* row = a.logits + (on ? t : a.T - 1) * a.E;
+  float l[NV], m = kRouteMasked, z = 0.f;
 #pragma unroll
-  for (int i = 0; i < NE; ++i) p[i] = 0.f;
-  if (score == MOE_SCORE_SOFTMAX && !renorm) {
-    float l[NE], m = -INFINITY, z = 0.f;
-#pragma unroll
-    for (int i = 0; i < NE; ++i) {
-      const int e = i * 64 + lane;
-      l[i] = e < E ? logits[t * E + e] : -INFINITY;
-      if (!(l[i] > -INFINITY)) l[i] = -INFINITY;
-      m = fmaxf(m, l[i]);
-    }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, kWave));
-#pragma unroll
-    for (int i = 0; i < NE; ++i) {
-      p[i] = l[i] == -INFINITY ? 0.f : l[i] == m ? 1.f : expf(l[i] - m);
-      z += p[i];
-    }
-    z = wave_sum(z);
-#pragma unroll
-    for (int i = 0; i < NE; ++i) p[i] = z > 0.f ? -G * (p[i] / z) : 0.f;
+  for (int i = 0; i < NV; ++i) {
+    const int x = j + 16 * i;
+    l[i] = x < a.E ? row[x] : -INFINITY;
   }
-  for (int r = 0; r < k; ++r) {
-    const int e = __shfl(er, r, kWave);
-    const float a = __shfl(v, r, kWave);
+  int e;
+  float G;
+  const float v = choice_grad<16>(a, t, j, on, e, G);
 #pragma unroll
-    for (int i = 0; i < NE; ++i)
-      if (i * 64 + lane == e) p[i] += a;
+  for (int i = 0; i < NV; ++i) {
+    l[i] = l[i] > -INFINITY ? fmaxf(l[i], kRouteNone) : kRouteMasked;   // masked: apart from every other
+    m = fmaxf(m, l[i]);
+    mine[j + 16 * i] = 0.f;
   }
+  m = from_order_key(team_max<16>(order_key(m)));
+  float p[NV];
 #pragma unroll
-  for (int i = 0; i < NE; ++i)
-    if (i * 64 + lane < E) dlogits[t * E + i * 64 + lane] = p[i];
+  for (int i = 0; i < NV; ++i) {
+    p[i] = l[i] < kRouteNone ? 0.f : l[i] == m ? 1.f : expf(l[i] - m);   // (+inf logits: an even share)
+    z += p[i];
+  }
+  z = team_sum<16>(z);
+  const float f = z > 0.f ? -G / z : 0.f;
+  wave_lds_fence();
+  if (e >= 0) unsafeAtomicAdd(mine + e, v);
+  wave_lds_fence();
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int x = j + 16 * i;
+    if (on && x < a.E) a.dlogits[t * a.E + x] = mine[x] + f * p[i];
+  }
 }
 
 void launch_route_bwd(const moe_route_cfg& c, const float* logits, const int32_t* idx, const float* w,
                       const float* dw, float* dlogits, hipStream_t s) {
   if (c.T == 0) return;
-  const unsigned blocks = (unsigned)((c.T + kRouteBwdWaves - 1) / kRouteBwdWaves);
-  auto go = [&](auto kern) {
-    hipLaunchKernelGGL(kern, dim3(blocks), dim3(64 * kRouteBwdWaves), 0, s, logits, idx, w, dw, dlogits, c.T, c.E,
-                       c.k, c.score, c.renorm, c.scale);
+  const RouteBwdArgs a{logits, idx, w, dw, dlogits, c.T, c.E, c.k, c.score, c.renorm, c.scale, 0};
+  auto slices = [&](int tokens, auto launch) {   // tokens of a wave; a launch's thread count is 32 bits
+    const int64_t per = (int64_t)kBwdWaves * tokens, most = per << 23;
+    RouteBwdArgs b = a;
+    for (b.first = 0; b.first < c.T; b.first += most)
+      launch(b, dim3((unsigned)((std::min(c.T - b.first, most) + per - 1) / per)));
   };
-  if (c.E <= 64) go(route_bwd_kernel<1>);
-  else if (c.E <= 128) go(route_bwd_kernel<2>);
-  else if (c.E <= 256) go(route_bwd_kernel<4>);
-  else go(route_bwd_kernel<8>);
+  if (c.score == MOE_SCORE_SOFTMAX && !c.renorm) {
+    auto go = [&](auto kern) {
+      slices(4, [&](const RouteBwdArgs& b, dim3 grid) { hipLaunchKernelGGL(kern, grid, dim3(64 * kBwdWaves), 0, s, b); });
+    };
+    if (c.E <= 16) go(route_bwd_softmax_kernel<1>);
+    else if (c.E <= 64) go(route_bwd_softmax_kernel<4>);
+    else if (c.E <= 128) go(route_bwd_softmax_kernel<8>);
+    else if (c.E <= 256) go(route_bwd_softmax_kernel<16>);
+    else go(route_bwd_softmax_kernel<32>);
+    return;
+  }
+  // As many tokens a wave as its choices have lanes and its rows have room in LDS.
+  int kp = 1, tokens = 4;
+  while (kp < c.k) kp *= 2;
+  while (tokens * 2 * kp <= kWave && tokens * 2 * c.E <= kBwdLds) tokens *= 2;
+  auto go = [&](auto kern) {
+    slices(tokens, [&](const RouteBwdArgs& b, dim3 grid) {
+      hipLaunchKernelGGL(kern, grid, dim3(64 * kBwdWaves), 0, s, b, tokens);
+    });
+  };
+  if (kp == 1) go(route_bwd_kernel<1>);
+  else if (kp == 2) go(route_bwd_kernel<2>);
+  else if (kp == 4) go(route_bwd_kernel<4>);
+  else if (kp == 8) go(route_bwd_kernel<8>);
+  else go(route_bwd_kernel<16>);
 }
 
 }  // namespace lmoe
