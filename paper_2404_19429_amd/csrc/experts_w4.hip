@@ -15,15 +15,14 @@
 
 namespace lmoe {
 
-constexpr int kW4Waves = 4;        // waves of a block: they share its rows and split K
-constexpr int kW4Small = 64;       // up to so many choices a block finds its expert's tokens by itself
-constexpr int kW4Tile = 64;        // tokens of one block, at most
+constexpr int kW4Scan = 1024;      // up to so many choices a block finds its expert's tokens by itself
+constexpr int kW4Tile = 32;        // tokens of one block, at most
 constexpr int kW4ListThreads = 1024;
 
 typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
 
 // -------------------------------------------------------------------- choices
-// More than kW4Small choices: their numbers sorted by expert (the order inside an
+// More than kW4Scan choices: their numbers sorted by expert (the order inside an
 // expert is left to the atomics: rows do not mix, so it changes no value) and the
 // table of token tiles {expert, first, count}.
 struct W4Tile {
@@ -81,9 +80,10 @@ struct W4Args {
   const void* in;                  // rows of K: x by token, or the parts of act(W1 x) by choice
   void* out;                       // FIRST: the parts [parts][n][N] bf16; else float [n][N]
   const int32_t *idx, *list;
-  const W4Tile* tiles;
+  const W4Tile* tiles;             // null: the blocks find their tokens
   const int32_t* ntiles;
   int32_t N, K, n, k, E, act;
+  int32_t by_choice;               // blockIdx.y is a choice, not an expert (fewer choices than experts)
 };
 
 // Eight codes to bfloat16.
@@ -104,35 +104,58 @@ __device__ __forceinline__ float part_of(float& v) {
   return h;
 }
 
-// Eight inputs of a token as NS bfloat16 parts that sum to them.
-template <typename T, int NS, bool FIRST>
-__device__ __forceinline__ void w4_inputs(const W4Args& a, int64_t off, bool ok, bf16x8 (&b)[NS]) {
-  const u32x4 zero = {0u, 0u, 0u, 0u};
-  if constexpr (FIRST && sizeof(T) == 4) {
-    float v[8];
-    const float* p = (const float*)a.in + off;
-    Vec<float>::load(p, v);
-    Vec<float>::load(p + 4, v + 4);
-    u32x4 r[NS];
+// The 16-byte pieces that eight inputs of a token come from, and their NS bfloat16 parts.
+template <typename T, int NS, bool FIRST> struct W4In {
+  static constexpr int NP = FIRST && sizeof(T) == 4 ? 2 : NS;
+  u32x4 raw[NP];
+  __device__ __forceinline__ void load(const W4Args& a, int64_t off) {
+    if constexpr (FIRST && sizeof(T) == 4) {
+      const u32x4* p = reinterpret_cast<const u32x4*>((const float*)a.in + off);
+      raw[0] = p[0];
+      raw[1] = p[1];
+    } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int s = 0; s < NS; ++s) {
-        const float lo = part_of(v[2 * i]), hi = part_of(v[2 * i + 1]);
-        r[s][i] = ok ? (__float_as_uint(lo) >> 16) | __float_as_uint(hi) : 0u;
-      }
-#pragma unroll
-    for (int s = 0; s < NS; ++s) b[s] = __builtin_bit_cast(bf16x8, r[s]);
-  } else {
-#pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      const u32x4 r = *reinterpret_cast<const u32x4*>((const uint16_t*)a.in + (int64_t)s * a.n * a.K + off);
-      b[s] = __builtin_bit_cast(bf16x8, ok ? r : zero);
+      for (int s = 0; s < NS; ++s)
+        raw[s] = *reinterpret_cast<const u32x4*>((const uint16_t*)a.in + (int64_t)s * a.n * a.K + off);
     }
   }
-}
+  __device__ __forceinline__ void parts(bf16x8 (&b)[NS]) const {
+    if constexpr (FIRST && sizeof(T) == 4) {
+      u32x4 r[NS];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float lo = __uint_as_float(raw[i >> 1][(2 * i) & 3]), hi = __uint_as_float(raw[i >> 1][(2 * i + 1) & 3]);
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+          const float l = part_of(lo), h = part_of(hi);
+          r[s][i] = (__float_as_uint(l) >> 16) | __float_as_uint(h);
+        }
+      }
+#pragma unroll
+      for (int s = 0; s < NS; ++s) b[s] = __builtin_bit_cast(bf16x8, r[s]);
+    } else {
+#pragma unroll
+      for (int s = 0; s < NS; ++s) b[s] = __builtin_bit_cast(bf16x8, raw[s]);
+    }
+  }
+};
 
-template <typename T, bool FIRST, int NS, int NO, int RT, int TN>
+// The weights of 16 RT rows x 128 inputs.
+template <int RT> struct W4Chunk {
+  u32x4 code[RT];
+  uint32_t sc[RT];
+  __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, int64_t row, int K, int col) {
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      code[r] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(codes + (row + r * 16) * (K / 2) + col / 2));
+      sc[r] = scales[(row + r * 16) * (K / 32) + col / 32];
+    }
+  }
+};
+
+// Tokens list[0 .. cnt) of one expert against the block's 16 RT rows; the block's WV
+// waves split K into interleaved chunks of 128.
+template <typename T, bool FIRST, int NS, int NO, int RT, int WV, int TN>
 __device__ __forceinline__ void w4_tile(const W4Args& a, int e, int cnt, const int32_t* list, f32x4 (*red)[64]) {
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
   const int i16 = lane & 15, q = lane >> 4;
@@ -150,34 +173,44 @@ __device__ __forceinline__ void w4_tile(const W4Args& a, int e, int cnt, const i
     in_off[t] = (int64_t)(FIRST ? c / a.k : c) * a.K;
   }
   const int64_t wrow = (int64_t)e * a.N + row0 + i16;
-  for (int c = wv; c < nch; c += kW4Waves) {
+  // A lane past K (a multiple of 32) reads the chunk's first group, and its weights become zeros.
+  auto column = [&](int c) __attribute__((always_inline)) {
     const int col = c * 128 + q * 32;
-    const bool ok = col < a.K;          // K is a multiple of 32
-    const int cc = ok ? col : 0;
-    u32x4 code[RT];
-    float sc[RT];
+    return col < a.K ? col : c * 128;
+  };
+  W4Chunk<RT> w;
+  if (wv < nch) w.load(a.codes, a.scales, wrow, a.K, column(wv));
+#pragma unroll 2
+  for (int c = wv; c < nch; c += WV) {
+    const int col = column(c);
+    const bool ok = c * 128 + q * 32 < a.K;
+    W4In<T, NS, FIRST> in[TN][4];
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-      const int64_t row = wrow + r * 16;
-      code[r] = *reinterpret_cast<const u32x4*>(a.codes + row * (a.K / 2) + cc / 2);
-      sc[r] = __uint_as_float((uint32_t)a.scales[row * (a.K / 32) + cc / 32] << 23);
-      if (!ok) code[r] = u32x4{0u, 0u, 0u, 0u}, sc[r] = 1.f;
-    }
+    for (int t = 0; t < TN; ++t)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) in[t][j].load(a, in_off[t] + col + 8 * j);
+    W4Chunk<RT> next = w;
+    if (c + WV < nch) next.load(a.codes, a.scales, wrow, a.K, column(c + WV));
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      bf16x8 w[RT];
+      bf16x8 f[RT];
 #pragma unroll
-      for (int r = 0; r < RT; ++r) w[r] = w4_frag(code[r][j], sc[r]);
+      for (int r = 0; r < RT; ++r)
+        f[r] = w4_frag(ok ? w.code[r][j] : 0u, __uint_as_float((ok ? w.sc[r] : 127u) << 23));
 #pragma unroll
       for (int t = 0; t < TN; ++t) {
         bf16x8 b[NS];
-        w4_inputs<T, NS, FIRST>(a, in_off[t] + cc + 8 * j, ok, b);
+        in[t][j].parts(b);
 #pragma unroll
-        for (int s = NS - 1; s >= 0; --s)
+        for (int s = NS - 1; s >= 0; --s) {
+          // (the repeated group may hold an infinity)
+          const bf16x8 bs = __builtin_bit_cast(bf16x8, ok ? __builtin_bit_cast(u32x4, b[s]) : u32x4{0u, 0u, 0u, 0u});
 #pragma unroll
-          for (int r = 0; r < RT; ++r) acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[r], b[s], acc[r][t], 0, 0, 0);
+          for (int r = 0; r < RT; ++r) acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[r], bs, acc[r][t], 0, 0, 0);
+        }
       }
     }
+    w = next;
   }
   // The waves' sums meet in LDS and are added in wave order, every wave its tiles.
 #pragma unroll
@@ -186,13 +219,13 @@ __device__ __forceinline__ void w4_tile(const W4Args& a, int e, int cnt, const i
     for (int t = 0; t < TN; ++t) red[(wv * RT + r) * TN + t][lane] = acc[r][t];
   __syncthreads();
 #pragma unroll
-  for (int u0 = 0; u0 < RT * TN; u0 += kW4Waves) {
+  for (int u0 = 0; u0 < RT * TN; u0 += WV) {
     const int u = u0 + wv;
     if (u >= RT * TN) break;
     const int r = u / TN, t = u % TN;
     f32x4 s = red[u][lane];
 #pragma unroll
-    for (int w = 1; w < kW4Waves; ++w) s += red[w * RT * TN + u][lane];
+    for (int x = 1; x < WV; ++x) s += red[x * RT * TN + u][lane];
     const int col = t * 16 + i16;
     if (col < cnt) {
       const int64_t off = (int64_t)list[col] * a.N + row0 + r * 16 + 4 * q;
@@ -215,11 +248,11 @@ __device__ __forceinline__ void w4_tile(const W4Args& a, int e, int cnt, const i
   }
 }
 
-template <typename T, bool FIRST, int NS, int NO, int RT>
-__global__ __launch_bounds__(64 * kW4Waves) void w4_product_kernel(W4Args a) {
-  __shared__ f32x4 red[kW4Waves * RT * 4][64];
-  __shared__ int32_t list[kW4Tile];
-  const int lane = threadIdx.x & 63;
+template <typename T, bool FIRST, int NS, int NO, int RT, int WV>
+__global__ __launch_bounds__(64 * WV) void w4_product_kernel(W4Args a) {
+  __shared__ f32x4 red[WV * RT * 2][64];
+  __shared__ int32_t list[kW4Scan];
+  __shared__ int32_t found, earlier;
   int e, cnt;
   if (a.tiles) {
     if ((int)blockIdx.y >= *a.ntiles) return;
@@ -227,20 +260,29 @@ __global__ __launch_bounds__(64 * kW4Waves) void w4_product_kernel(W4Args a) {
     e = t.e;
     cnt = t.count;
     if ((int)threadIdx.x < cnt) list[threadIdx.x] = a.list[t.first + threadIdx.x];
+    __syncthreads();
   } else {
-    // Choice blockIdx.y, if it is the first of its expert, stands for all of them.
-    const int my = lane < a.n ? a.idx[lane] : -1;
-    e = __shfl(my, (int)blockIdx.y, kWave);
+    // The expert's choices, in any order (rows do not mix).  By choice: the first choice
+    // of an expert stands for all of them.
+    e = a.by_choice ? a.idx[blockIdx.y] : (int)blockIdx.y;
     if (e < 0 || e >= a.E) return;
-    const uint64_t same = __ballot(my == e);
-    if (__builtin_ctzll(same) != (int)blockIdx.y) return;
-    cnt = __popcll(same);
-    if (threadIdx.x < 64 && my == e) list[__popcll(same & ((1ull << lane) - 1))] = lane;
+    if (threadIdx.x == 0) found = earlier = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < a.n; i += 64 * WV)
+      if (a.idx[i] == e) {
+        list[atomicAdd(&found, 1)] = i;
+        if (a.by_choice && i < (int)blockIdx.y) earlier = 1;
+      }
+    __syncthreads();
+    cnt = found;
+    if (cnt == 0 || earlier) return;
   }
-  __syncthreads();
-  if (cnt <= 16) w4_tile<T, FIRST, NS, NO, RT, 1>(a, e, cnt, list, red);
-  else if (cnt <= 32) w4_tile<T, FIRST, NS, NO, RT, 2>(a, e, cnt, list, red);
-  else w4_tile<T, FIRST, NS, NO, RT, 4>(a, e, cnt, list, red);
+  for (int c0 = 0; c0 < cnt; c0 += kW4Tile) {
+    if (c0) __syncthreads();   // the sums of the tile before have been read
+    const int n = min(kW4Tile, cnt - c0);
+    if (n <= 16) w4_tile<T, FIRST, NS, NO, RT, WV, 1>(a, e, n, list + c0, red);
+    else w4_tile<T, FIRST, NS, NO, RT, WV, 2>(a, e, n, list + c0, red);
+  }
 }
 
 template <typename T>
@@ -253,13 +295,23 @@ __global__ __launch_bounds__(256) void w4_combine_kernel(const float* __restrict
   if (t >= T_tokens) return;
   const int c = (int)(g - t * nc) * 4;
   f32x4 s = {0.f, 0.f, 0.f, 0.f};
-  for (int r = 0; r < k; ++r) {
-    const int e = idx[t * k + r];
-    if (e < 0 || e >= E) continue;
-    const float wr = w[t * k + r];
-    const f32x4 o = *reinterpret_cast<const f32x4*>(O + (t * k + r) * d + c);
+  // Four choices at a time, every load of them ahead of the sums.
+  for (int r0 = 0; r0 < k; r0 += 4) {
+    int e[4];
+    float wr[4];
+    f32x4 o[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s[i] = fmaf(wr, o[i], s[i]);
+    for (int r = 0; r < 4; ++r) {
+      const int64_t i = t * k + min(r0 + r, k - 1);
+      e[r] = idx[i];
+      wr[r] = w[i];
+      o[r] = *reinterpret_cast<const f32x4*>(O + i * d + c);
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (r0 + r < k && e[r] >= 0 && e[r] < E)   // (of another choice O and w may hold anything)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[i] = fmaf(wr[r], o[r][i], s[i]);
   }
   if constexpr (sizeof(T) == 2)
     *reinterpret_cast<u32x2*>(y + t * d + c) = u32x2{pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3])};
@@ -288,6 +340,21 @@ static W4Ws w4_ws(const moe_w4_cfg& c) {
 }
 size_t experts_w4_ws_bytes(const moe_w4_cfg& c) { return w4_ws(c).total; }
 
+// A product over gy experts or tiles.  More rows a block read its tokens' inputs less
+// often and keep more weights in flight, as long as two blocks a CU are left.
+template <typename T, bool FIRST, int NS, int NO>
+static void launch_w4_product(const W4Args& a, int gy, hipStream_t s) {
+  const int64_t tiles = (int64_t)(a.N / 16) * gy;
+  const int rt = a.N % 64 == 0 && tiles >= 4 * 2 * num_cus() ? 4 : tiles >= 2 * 2 * num_cus() ? 2 : 1;
+  auto go = [&](auto kern, int wv) {
+    hipLaunchKernelGGL(kern, dim3(a.N / (16 * rt), gy), dim3(64 * wv), 0, s, a);
+  };
+  const bool deep = a.K >= 8 * 128;
+  if (rt == 4) deep ? go(w4_product_kernel<T, FIRST, NS, NO, 4, 8>, 8) : go(w4_product_kernel<T, FIRST, NS, NO, 4, 4>, 4);
+  else if (rt == 2) deep ? go(w4_product_kernel<T, FIRST, NS, NO, 2, 8>, 8) : go(w4_product_kernel<T, FIRST, NS, NO, 2, 4>, 4);
+  else deep ? go(w4_product_kernel<T, FIRST, NS, NO, 1, 8>, 8) : go(w4_product_kernel<T, FIRST, NS, NO, 1, 4>, 4);
+}
+
 template <typename T, int NX, int NA>
 static void launch_w4_t(const moe_w4_cfg& c, const void* x, const int32_t* idx, const float* w, const uint8_t* W1c,
                         const uint8_t* W1s, const uint8_t* W2c, const uint8_t* W2s, void* y, void* ws, hipStream_t s) {
@@ -297,15 +364,18 @@ static void launch_w4_t(const moe_w4_cfg& c, const void* x, const int32_t* idx, 
   int32_t* list = (int32_t*)(base + L.list);
   W4Tile* tiles = (W4Tile*)(base + L.tiles);
   int32_t* ntiles = (int32_t*)(base + L.ntiles);
-  const bool small = n <= kW4Small;
-  if (!small)
+  const bool scan = n <= kW4Scan;
+  const int by_choice = scan && n < c.E;
+  if (!scan)
     hipLaunchKernelGGL(w4_list_kernel, dim3(1), dim3(kW4ListThreads), 0, s, idx, n, c.E, list, tiles, ntiles);
-  const unsigned gy = (unsigned)(small ? n : L.max_tiles);
-  W4Args a{W1c, W1s, x, base + L.parts, idx, list, small ? nullptr : tiles, ntiles, c.d_ff, c.d_model, n, c.k, c.E, c.act};
-  hipLaunchKernelGGL((w4_product_kernel<T, true, NX, NA, 1>), dim3(c.d_ff / 16, gy), dim3(64 * kW4Waves), 0, s, a);
-  W4Args b{W2c, W2s, base + L.parts, base + L.O, idx, list, small ? nullptr : tiles, ntiles, c.d_model, c.d_ff, n, c.k,
-           c.E, c.act};
-  hipLaunchKernelGGL((w4_product_kernel<T, false, NA, NA, 1>), dim3(c.d_model / 16, gy), dim3(64 * kW4Waves), 0, s, b);
+  else
+    tiles = nullptr;
+  const int gy = !scan ? L.max_tiles : by_choice ? n : c.E;
+  const W4Args a{W1c, W1s, x, base + L.parts, idx, list, tiles, ntiles, c.d_ff, c.d_model, n, c.k, c.E, c.act, by_choice};
+  launch_w4_product<T, true, NX, NA>(a, gy, s);
+  const W4Args b{W2c, W2s, base + L.parts, base + L.O, idx, list, tiles, ntiles, c.d_model, c.d_ff, n, c.k, c.E, c.act,
+                 by_choice};
+  launch_w4_product<T, false, NA, NA>(b, gy, s);
   const int64_t g = c.T * (c.d_model / 4);
   hipLaunchKernelGGL(w4_combine_kernel<T>, dim3((unsigned)((g + 255) / 256)), dim3(256), 0, s,
                      (const float*)(base + L.O), idx, w, (T*)y, c.T, c.d_model, c.E, c.k);

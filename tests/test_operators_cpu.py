@@ -5,6 +5,7 @@ import math
 
 import numpy as np
 import pytest
+import torch
 
 from oracle import operators_oracle as O
 
@@ -98,6 +99,10 @@ def test_struct_layouts():
 
 
 # ----------------------------------------------------------------------- refusals
+# These calls pass addresses that are none: on a machine with a device a valid one would run.
+no_device = pytest.mark.skipif(torch.cuda.device_count() > 0, reason="passes addresses that are not memory")
+
+
 def rcfg(**kw):
     base = dict(T=64, E=16, k=2)
     base.update(kw)
@@ -108,6 +113,7 @@ def route(c, logits=P(0), bias=None, idx=P(1), w=P(2), load=None):
     return lib.moe_route(ctypes.byref(c) if c is not None else None, logits, bias, idx, w, load, None)
 
 
+@no_device
 @pytest.mark.parametrize("kw,status", [
     (dict(T=-1), L.MOE_EINVAL), (dict(T=2 ** 31 + 1), L.MOE_ESHAPE), (dict(E=0), L.MOE_ESHAPE),
     (dict(E=513), L.MOE_ESHAPE), (dict(k=0), L.MOE_EINVAL), (dict(k=17), L.MOE_EINVAL), (dict(E=4, k=5), L.MOE_EINVAL),
@@ -122,6 +128,7 @@ def test_route_cfg_refused(kw, status):
     assert lib.moe_route_bwd(ctypes.byref(c), P(0), P(1), P(2), P(3), P(4), None) == status
 
 
+@no_device
 def test_route_pointers():
     c = rcfg()
     assert route(None) == L.MOE_EINVAL
@@ -144,6 +151,7 @@ def bwd_dx_route(c, r, ws=None, **over):
     return lib.moe_bwd_dx_route(ctypes.byref(c), ctypes.byref(r), *p, P(30), need if ws is None else ws, None)
 
 
+@no_device
 def test_bwd_dx_route_refused():
     c = L.make_cfg(64, 128, 256, 16, 2, 20)
     assert bwd_dx_route(c, rcfg()) == L.MOE_EDEVICE
@@ -169,6 +177,7 @@ def experts(c, ws=None, **over):
     return lib.moe_experts_w4(ctypes.byref(c), *p, over.get("ws_ptr", P(20)), need, None)
 
 
+@no_device
 @pytest.mark.parametrize("kw,status", [
     (dict(T=-1), L.MOE_EINVAL), (dict(d_model=48), L.MOE_ESHAPE), (dict(d_model=0), L.MOE_ESHAPE),
     (dict(d_ff=100), L.MOE_ESHAPE), (dict(d_ff=2 ** 20 + 32), L.MOE_ESHAPE), (dict(E=0), L.MOE_ESHAPE),
@@ -181,6 +190,7 @@ def test_experts_cfg_refused(kw, status):
     assert L.moe_experts_w4_workspace_bytes(c) == 0
 
 
+@no_device
 def test_experts_pointers_and_workspace():
     c = wcfg()
     need = L.moe_experts_w4_workspace_bytes(c)
@@ -198,6 +208,7 @@ def test_experts_workspace_of_a_longer_batch_serves_a_shorter_one(k, E, dtype):
     assert all(a <= b for a, b in zip(need, need[1:])) and need[1] > 0
 
 
+@no_device
 def test_quantize_refused():
     q = lib.moe_w4_quantize
     assert q(4, 64, 1, P(0), P(1), P(2), None) == L.MOE_EDEVICE
@@ -215,6 +226,7 @@ def ccfg(**kw):
     return L.make_cfg(**base)
 
 
+@no_device
 def test_ckpt_refused():
     c = ccfg()
     need = L.moe_ckpt_bytes(c)
@@ -234,7 +246,6 @@ def test_ckpt_refused():
 
 
 def test_binding_refuses_host_short_and_mistyped_tensors():
-    import torch
     from torch._subclasses.fake_tensor import FakeTensorMode
     with FakeTensorMode():
         e = lambda n, dt: torch.empty(n, dtype=dt, device="cuda")   # noqa: E731
