@@ -7,16 +7,22 @@
 // turns into bfloat16 exactly, scale included (eight codes in four instructions), for
 // v_mfma_f32_16x16x32_bf16 against up to 16 tokens.
 //
-// Lane (i = lane & 15, q = lane >> 4) holds row i, inputs 32 q .. 32 q + 31 of a chunk
-// of 128: one scale group.  MFMA j takes its inputs 8 j .. 8 j + 7 from weights and
-// tokens alike, so the product's k-index stands for the same input in both operands,
-// which is all a dot product needs, and the codes can stay row-major.
+// A matrix instruction wants lane (i = lane & 15, q = lane >> 4) to hold row i, and 16
+// rows are 16 cache lines: loads straight into that order are bound by the L1's line
+// look-ups (64 per load; measured, 48 tokens against 16 experts of 1024 x 4096: 19 + 26
+// us where 36 + 36 MB take 14).  So a wave loads 8 rows x 256 inputs at a time, whole
+// 128-byte lines, and turns them in LDS.  Of a row's 256 inputs lane q gets 32 q ..
+// 32 q + 31 of each half, one scale group; MFMA j of a half takes inputs 8 j .. 8 j + 7
+// of these from weights and tokens alike, so the product's k-index stands for the same
+// input in both operands, which is all a dot product needs.
+#include <type_traits>
+
 #include "internal.h"
 
 namespace lmoe {
 
 constexpr int kW4Scan = 1024;      // up to so many choices a block finds its expert's tokens by itself
-constexpr int kW4Tile = 32;        // tokens of one block, at most
+constexpr int kW4Tile = 16;        // tokens of one pass over the weights: a matrix instruction's columns
 constexpr int kW4ListThreads = 1024;
 
 typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
@@ -140,183 +146,247 @@ template <typename T, int NS, bool FIRST> struct W4In {
   }
 };
 
-// The weights of 16 RT rows x 128 inputs.
-template <int RT> struct W4Chunk {
-  u32x4 code[RT];
-  uint32_t sc[RT];
-  __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, int64_t row, int K, int col) {
+// The weights of 16 RT rows x 256 inputs (a step), on their way: lane l has 16-byte piece
+// l % 8 of row l / 8 of every eight rows, and the scales of row l (l < 16 RT).
+constexpr int kStep = 256;
+template <int RT, bool FULL> struct W4Step {
+  u32x4 code[2 * RT];
+  u32x2 sc;
+  // codes, scales: at the first of the rows; col: the step's first input.
+  __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, int K, int col) {
+    const int lane = threadIdx.x & 63;
+    const int at = col + (lane & 7) * 32;
+    const bool ok = FULL || at < K;   // (K is a multiple of 32)
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-      code[r] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(codes + (row + r * 16) * (K / 2) + col / 2));
-      sc[r] = scales[(row + r * 16) * (K / 32) + col / 32];
+    for (int g = 0; g < 2 * RT; ++g) {
+      const u32x4 v = __builtin_nontemporal_load(
+          reinterpret_cast<const u32x4*>(codes + (int64_t)(8 * g + (lane >> 3)) * (K / 2) + (ok ? at : col) / 2));
+      code[g] = ok ? v : u32x4{0u, 0u, 0u, 0u};
+    }
+    const uint8_t* p = scales + (int64_t)(lane & (16 * RT - 1)) * (K / 32) + col / 32;
+    if constexpr (FULL) {
+      sc = *reinterpret_cast<const u32x2*>(p);
+    } else {
+      sc = u32x2{0x7f7f7f7fu, 0x7f7f7f7fu};
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (col + 32 * i < K) sc[i >> 2] = (sc[i >> 2] & ~(0xffu << (8 * (i & 3)))) | (uint32_t)p[i] << (8 * (i & 3));
     }
   }
 };
+template <int RT> struct W4Lds {   // a wave's step, turned
+  u32x4 code[RT][16][8];           // [row][piece ^ row % 8]: neither side meets a bank conflict
+  u32x2 sc[RT][16];
+};
 
-// Tokens list[0 .. cnt) of one expert against the block's 16 RT rows; the block's WV
-// waves split K into interleaved chunks of 128.
-template <typename T, bool FIRST, int NS, int NO, int RT, int WV, int TN>
-__device__ __forceinline__ void w4_tile(const W4Args& a, int e, int cnt, const int32_t* list, f32x4 (*red)[64]) {
+// (one activation's code for four values, not four switches: it is most of the kernel's)
+__device__ __forceinline__ void w4_act(float (&h)[4], int act) {
+  auto all = [&](auto kind) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = act_fwd_nan(h[i], decltype(kind)::value);
+  };
+  if (act == MOE_ACT_RELU) all(std::integral_constant<int, MOE_ACT_RELU>{});
+  else if (act == MOE_ACT_GELU_TANH) all(std::integral_constant<int, MOE_ACT_GELU_TANH>{});
+  else if (act == MOE_ACT_GELU_ERF) all(std::integral_constant<int, MOE_ACT_GELU_ERF>{});
+}
+
+__device__ __forceinline__ void w4_wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// Tokens list[0 .. cnt) of one expert, 16 at most, against the block's 16 RT rows; the
+// block's WV waves split K into interleaved steps (w: the wave's first, on its way).
+template <typename T, bool FIRST, int NS, int NO, int RT, int WV, bool FULL>
+__device__ __forceinline__ void w4_tile(const W4Args& a, int cnt, const int32_t* list, const uint8_t* codes,
+                                        const uint8_t* scales, W4Step<RT, FULL>& w, W4Lds<RT>* lds) {
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
   const int i16 = lane & 15, q = lane >> 4;
   const int row0 = blockIdx.x * 16 * RT;
-  const int nch = (a.K + 127) / 128;
-  f32x4 acc[RT][TN];
+  W4Lds<RT>& mine = lds[wv];
+  f32x4 acc[RT];
 #pragma unroll
-  for (int r = 0; r < RT; ++r)
+  for (int r = 0; r < RT; ++r) acc[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int choice = list[min(i16, cnt - 1)];   // columns past the count repeat the last
+  const int64_t in_off = (int64_t)(FIRST ? choice / a.k : choice) * a.K;
+  for (int col = wv * kStep; col < a.K; col += WV * kStep) {
+    w4_wave_fence();
 #pragma unroll
-    for (int t = 0; t < TN; ++t) acc[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  int64_t in_off[TN];
+    for (int g = 0; g < 2 * RT; ++g) mine.code[g >> 1][8 * (g & 1) + (lane >> 3)][(lane & 7) ^ (lane >> 3)] = w.code[g];
+    if (lane < 16 * RT) mine.sc[lane >> 4][lane & 15] = w.sc;
+    w4_wave_fence();
+    // The inputs are asked for ahead of the next weights: loads return in order, and a
+    // wait for inputs behind them would be a wait for memory.
+    W4In<T, NS, FIRST> in[2][4];
 #pragma unroll
-  for (int t = 0; t < TN; ++t) {
-    const int c = list[min(t * 16 + i16, cnt - 1)];   // columns past the count repeat the last
-    in_off[t] = (int64_t)(FIRST ? c / a.k : c) * a.K;
-  }
-  const int64_t wrow = (int64_t)e * a.N + row0 + i16;
-  // A lane past K (a multiple of 32) reads the chunk's first group, and its weights become zeros.
-  auto column = [&](int c) __attribute__((always_inline)) {
-    const int col = c * 128 + q * 32;
-    return col < a.K ? col : c * 128;
-  };
-  W4Chunk<RT> w;
-  if (wv < nch) w.load(a.codes, a.scales, wrow, a.K, column(wv));
-#pragma unroll 2
-  for (int c = wv; c < nch; c += WV) {
-    const int col = column(c);
-    const bool ok = c * 128 + q * 32 < a.K;
-    W4In<T, NS, FIRST> in[TN][4];
+    for (int h = 0; h < 2; ++h) {
+      const int at = col + 128 * h + 32 * q;
 #pragma unroll
-    for (int t = 0; t < TN; ++t)
+      for (int j = 0; j < 4; ++j) in[h][j].load(a, in_off + (FULL || at < a.K ? at : col) + 8 * j);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (col + WV * kStep < a.K) w.load(codes, scales, a.K, col + WV * kStep);
+    __builtin_amdgcn_sched_barrier(0);
+    u32x2 sc[RT];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) in[t][j].load(a, in_off[t] + col + 8 * j);
-    W4Chunk<RT> next = w;
-    if (c + WV < nch) next.load(a.codes, a.scales, wrow, a.K, column(c + WV));
+    for (int r = 0; r < RT; ++r) sc[r] = mine.sc[r][i16];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      bf16x8 f[RT];
+    for (int h = 0; h < 2; ++h) {
+      const bool ok = FULL || col + 128 * h + 32 * q < a.K;
+      u32x4 code[RT];
+      float s[RT];
 #pragma unroll
-      for (int r = 0; r < RT; ++r)
-        f[r] = w4_frag(ok ? w.code[r][j] : 0u, __uint_as_float((ok ? w.sc[r] : 127u) << 23));
+      for (int r = 0; r < RT; ++r) {
+        code[r] = mine.code[r][i16][(4 * h + q) ^ (i16 & 7)];
+        s[r] = __uint_as_float(((sc[r][h] >> (8 * q)) & 0xffu) << 23);
+      }
 #pragma unroll
-      for (int t = 0; t < TN; ++t) {
+      for (int j = 0; j < 4; ++j) {
         bf16x8 b[NS];
-        in[t][j].parts(b);
+        in[h][j].parts(b);
+        if (!FULL)   // (weights past K are zeros, but the inputs read in their place may be infinite)
 #pragma unroll
-        for (int s = NS - 1; s >= 0; --s) {
-          // (the repeated group may hold an infinity)
-          const bf16x8 bs = __builtin_bit_cast(bf16x8, ok ? __builtin_bit_cast(u32x4, b[s]) : u32x4{0u, 0u, 0u, 0u});
+          for (int x = 0; x < NS; ++x)
+            b[x] = __builtin_bit_cast(bf16x8, ok ? __builtin_bit_cast(u32x4, b[x]) : u32x4{0u, 0u, 0u, 0u});
 #pragma unroll
-          for (int r = 0; r < RT; ++r) acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[r], bs, acc[r][t], 0, 0, 0);
+        for (int r = 0; r < RT; ++r) {
+          const bf16x8 f = w4_frag(code[r][j], s[r]);
+#pragma unroll
+          for (int x = NS - 1; x >= 0; --x) acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, b[x], acc[r], 0, 0, 0);
         }
       }
     }
-    w = next;
   }
-  // The waves' sums meet in LDS and are added in wave order, every wave its tiles.
-#pragma unroll
-  for (int r = 0; r < RT; ++r)
-#pragma unroll
-    for (int t = 0; t < TN; ++t) red[(wv * RT + r) * TN + t][lane] = acc[r][t];
+  // The waves' sums meet in LDS and are added in wave order, every wave its rows.
+  f32x4 (*red)[64] = reinterpret_cast<f32x4(*)[64]>(lds);
+  static_assert(sizeof(f32x4) * 64 * RT <= sizeof(W4Lds<RT>), "");
   __syncthreads();
 #pragma unroll
-  for (int u0 = 0; u0 < RT * TN; u0 += WV) {
-    const int u = u0 + wv;
-    if (u >= RT * TN) break;
-    const int r = u / TN, t = u % TN;
-    f32x4 s = red[u][lane];
+  for (int r = 0; r < RT; ++r) red[wv * RT + r][lane] = acc[r];
+  __syncthreads();
+  if (wv < RT && i16 < cnt) {
+    f32x4 s = red[wv][lane];
 #pragma unroll
-    for (int x = 1; x < WV; ++x) s += red[x * RT * TN + u][lane];
-    const int col = t * 16 + i16;
-    if (col < cnt) {
-      const int64_t off = (int64_t)list[col] * a.N + row0 + r * 16 + 4 * q;
-      if constexpr (FIRST) {
-        float h[4];
+    for (int x = 1; x < WV; ++x) s += red[x * RT + wv][lane];
+    const int64_t off = (int64_t)choice * a.N + row0 + wv * 16 + 4 * q;
+    if constexpr (FIRST) {
+      float h[4] = {s[0], s[1], s[2], s[3]};
+      w4_act(h, a.act);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) h[i] = act_fwd_nan(s[i], a.act);
+      for (int p = 0; p < NO; ++p) {
+        float v[4];
 #pragma unroll
-        for (int p = 0; p < NO; ++p) {
-          float v[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) v[i] = p + 1 < NO || NO == 3 ? part_of(h[i]) : h[i];   // two parts: the second rounds
-          *reinterpret_cast<u32x2*>((uint16_t*)a.out + (int64_t)p * a.n * a.N + off) =
-              u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-        }
-      } else {
-        *reinterpret_cast<f32x4*>((float*)a.out + off) = s;
+        for (int i = 0; i < 4; ++i) v[i] = p + 1 < NO || NO == 3 ? part_of(h[i]) : h[i];   // two parts: the second rounds
+        *reinterpret_cast<u32x2*>((uint16_t*)a.out + (int64_t)p * a.n * a.N + off) =
+            u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
       }
+    } else {
+      *reinterpret_cast<f32x4*>((float*)a.out + off) = s;
     }
   }
 }
 
-template <typename T, bool FIRST, int NS, int NO, int RT, int WV>
-__global__ __launch_bounds__(64 * WV) void w4_product_kernel(W4Args a) {
-  __shared__ f32x4 red[WV * RT * 2][64];
-  __shared__ int32_t list[kW4Scan];
-  __shared__ int32_t found, earlier;
+template <typename T, bool FIRST, int NS, int NO, int RT, int WV, bool FULL>
+__global__ __launch_bounds__(64 * WV, 3) void w4_product_kernel(W4Args a) {
+  static_assert(RT <= WV, "every 16 rows of the block have a wave that adds them");
+  __shared__ W4Lds<RT> lds[WV];
+  __shared__ int32_t found, lists[kW4Scan];
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  const int32_t* list = lists;
   int e, cnt;
+  W4Step<RT, FULL> w;
+  const uint8_t *codes, *scales;
+  auto weights = [&]() __attribute__((always_inline)) {   // the wave's first step
+    const int64_t row = (int64_t)e * a.N + blockIdx.x * 16 * RT;
+    codes = a.codes + row * (a.K / 2);
+    scales = a.scales + row * (a.K / 32);
+    if (wv * kStep < a.K) w.load(codes, scales, a.K, wv * kStep);
+  };
   if (a.tiles) {
     if ((int)blockIdx.y >= *a.ntiles) return;
     const W4Tile t = a.tiles[blockIdx.y];
     e = t.e;
     cnt = t.count;
-    if ((int)threadIdx.x < cnt) list[threadIdx.x] = a.list[t.first + threadIdx.x];
+    weights();
+    if ((int)threadIdx.x < cnt) lists[threadIdx.x] = a.list[t.first + threadIdx.x];
     __syncthreads();
+  } else if (a.n <= kWave) {
+    // Every wave by itself: choice blockIdx.y, if it is the first of its expert, or expert
+    // blockIdx.y.
+    const int my = lane < a.n ? a.idx[lane] : -1;
+    e = a.by_choice ? __builtin_amdgcn_readlane(my, (int)blockIdx.y) : (int)blockIdx.y;
+    if (e < 0 || e >= a.E) return;
+    const uint64_t same = __ballot(my == e);
+    if (same == 0 || (a.by_choice && __builtin_ctzll(same) != (int)blockIdx.y)) return;
+    weights();
+    cnt = __popcll(same);
+    int32_t* mine = lists + wv * kWave;
+    if (my == e) mine[__popcll(same & ((1ull << lane) - 1))] = lane;
+    list = mine;
+    w4_wave_fence();
   } else {
     // The expert's choices, in any order (rows do not mix).  By choice: the first choice
-    // of an expert stands for all of them.
+    // of an expert stands for all of them.  Where nearly every expert has a choice its
+    // weights are fetched ahead of the answer.
     e = a.by_choice ? a.idx[blockIdx.y] : (int)blockIdx.y;
     if (e < 0 || e >= a.E) return;
-    if (threadIdx.x == 0) found = earlier = 0;
+    const bool ahead = a.n >= 3 * a.E;
+    if (ahead) weights();
+    if (threadIdx.x == 0) found = 0;
     __syncthreads();
+    bool earlier = false;
     for (int i = threadIdx.x; i < a.n; i += 64 * WV)
       if (a.idx[i] == e) {
-        list[atomicAdd(&found, 1)] = i;
-        if (a.by_choice && i < (int)blockIdx.y) earlier = 1;
+        lists[atomicAdd(&found, 1)] = i;
+        earlier |= a.by_choice && i < (int)blockIdx.y;
       }
-    __syncthreads();
+    if (__syncthreads_or(earlier)) return;
     cnt = found;
-    if (cnt == 0 || earlier) return;
+    if (cnt == 0) return;
+    if (!ahead) weights();
   }
   for (int c0 = 0; c0 < cnt; c0 += kW4Tile) {
-    if (c0) __syncthreads();   // the sums of the tile before have been read
-    const int n = min(kW4Tile, cnt - c0);
-    if (n <= 16) w4_tile<T, FIRST, NS, NO, RT, WV, 1>(a, e, n, list + c0, red);
-    else w4_tile<T, FIRST, NS, NO, RT, WV, 2>(a, e, n, list + c0, red);
+    if (c0) {
+      weights();
+      __syncthreads();   // the sums of the tile before have been read
+    }
+    w4_tile<T, FIRST, NS, NO, RT, WV, FULL>(a, min(kW4Tile, cnt - c0), list + c0, codes, scales, w, lds);
   }
 }
 
+// Thread: four columns of a token (blockIdx.y; further ones past the grid's limit).
 template <typename T>
 __global__ __launch_bounds__(256) void w4_combine_kernel(const float* __restrict__ O, const int32_t* __restrict__ idx,
                                                          const float* __restrict__ w, T* __restrict__ y, int64_t T_tokens,
                                                          int d, int E, int k) {
-  const int64_t g = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-  const int nc = d / 4;
-  const int64_t t = g / nc;
-  if (t >= T_tokens) return;
-  const int c = (int)(g - t * nc) * 4;
-  f32x4 s = {0.f, 0.f, 0.f, 0.f};
-  // Four choices at a time, every load of them ahead of the sums.
-  for (int r0 = 0; r0 < k; r0 += 4) {
-    int e[4];
-    float wr[4];
-    f32x4 o[4];
+  const int c = (blockIdx.x * 256 + threadIdx.x) * 4;
+  if (c >= d) return;
+  for (int64_t t = blockIdx.y; t < T_tokens; t += gridDim.y) {
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    // Four choices at a time, every load of them ahead of the sums.
+    for (int r0 = 0; r0 < k; r0 += 4) {
+      int e[4];
+      float wr[4];
+      f32x4 o[4];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int64_t i = t * k + min(r0 + r, k - 1);
-      e[r] = idx[i];
-      wr[r] = w[i];
-      o[r] = *reinterpret_cast<const f32x4*>(O + i * d + c);
+      for (int r = 0; r < 4; ++r) {
+        const int64_t i = t * k + min(r0 + r, k - 1);
+        e[r] = idx[i];
+        wr[r] = w[i];
+        o[r] = *reinterpret_cast<const f32x4*>(O + i * d + c);
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (r0 + r < k && e[r] >= 0 && e[r] < E)   // (of another choice O and w may hold anything)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[i] = fmaf(wr[r], o[r][i], s[i]);
     }
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-      if (r0 + r < k && e[r] >= 0 && e[r] < E)   // (of another choice O and w may hold anything)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[i] = fmaf(wr[r], o[r][i], s[i]);
+    if constexpr (sizeof(T) == 2)
+      *reinterpret_cast<u32x2*>(y + t * d + c) = u32x2{pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3])};
+    else
+      *reinterpret_cast<f32x4*>(y + t * d + c) = s;
   }
-  if constexpr (sizeof(T) == 2)
-    *reinterpret_cast<u32x2*>(y + t * d + c) = u32x2{pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3])};
-  else
-    *reinterpret_cast<f32x4*>(y + t * d + c) = s;
 }
 
 // Workspace: list, tiles, tile count | parts | O.
@@ -342,17 +412,21 @@ size_t experts_w4_ws_bytes(const moe_w4_cfg& c) { return w4_ws(c).total; }
 
 // A product over gy experts or tiles.  More rows a block read its tokens' inputs less
 // often and keep more weights in flight, as long as two blocks a CU are left.
-template <typename T, bool FIRST, int NS, int NO>
-static void launch_w4_product(const W4Args& a, int gy, hipStream_t s) {
+template <typename T, bool FIRST, int NS, int NO, bool FULL>
+static void launch_w4_rows(const W4Args& a, int gy, hipStream_t s) {
   const int64_t tiles = (int64_t)(a.N / 16) * gy;
-  const int rt = a.N % 64 == 0 && tiles >= 4 * 2 * num_cus() ? 4 : tiles >= 2 * 2 * num_cus() ? 2 : 1;
+  const int rt = tiles >= 2 * 2 * num_cus() ? 2 : 1;
   auto go = [&](auto kern, int wv) {
     hipLaunchKernelGGL(kern, dim3(a.N / (16 * rt), gy), dim3(64 * wv), 0, s, a);
   };
-  const bool deep = a.K >= 8 * 128;
-  if (rt == 4) deep ? go(w4_product_kernel<T, FIRST, NS, NO, 4, 8>, 8) : go(w4_product_kernel<T, FIRST, NS, NO, 4, 4>, 4);
-  else if (rt == 2) deep ? go(w4_product_kernel<T, FIRST, NS, NO, 2, 8>, 8) : go(w4_product_kernel<T, FIRST, NS, NO, 2, 4>, 4);
-  else deep ? go(w4_product_kernel<T, FIRST, NS, NO, 1, 8>, 8) : go(w4_product_kernel<T, FIRST, NS, NO, 1, 4>, 4);
+  const bool deep = a.K > 4 * kStep;   // more than a step for each of four waves
+  if (rt == 2) deep ? go(w4_product_kernel<T, FIRST, NS, NO, 2, 8, FULL>, 8) : go(w4_product_kernel<T, FIRST, NS, NO, 2, 4, FULL>, 4);
+  else deep ? go(w4_product_kernel<T, FIRST, NS, NO, 1, 8, FULL>, 8) : go(w4_product_kernel<T, FIRST, NS, NO, 1, 4, FULL>, 4);
+}
+template <typename T, bool FIRST, int NS, int NO>
+static void launch_w4_product(const W4Args& a, int gy, hipStream_t s) {
+  if (a.K % kStep == 0) launch_w4_rows<T, FIRST, NS, NO, true>(a, gy, s);
+  else launch_w4_rows<T, FIRST, NS, NO, false>(a, gy, s);
 }
 
 template <typename T, int NX, int NA>
@@ -376,8 +450,8 @@ static void launch_w4_t(const moe_w4_cfg& c, const void* x, const int32_t* idx, 
   const W4Args b{W2c, W2s, base + L.parts, base + L.O, idx, list, tiles, ntiles, c.d_model, c.d_ff, n, c.k, c.E, c.act,
                  by_choice};
   launch_w4_product<T, false, NA, NA>(b, gy, s);
-  const int64_t g = c.T * (c.d_model / 4);
-  hipLaunchKernelGGL(w4_combine_kernel<T>, dim3((unsigned)((g + 255) / 256)), dim3(256), 0, s,
+  hipLaunchKernelGGL(w4_combine_kernel<T>, dim3((c.d_model + 1023) / 1024, (unsigned)std::min<int64_t>(c.T, 32768)),
+                     dim3(256), 0, s,
                      (const float*)(base + L.O), idx, w, (T*)y, c.T, c.d_model, c.E, c.k);
 }
 
