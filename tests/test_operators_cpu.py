@@ -92,6 +92,30 @@ def test_ckpt_oracle_hand_worked():
     assert np.isnan(y[1, :64]).all() and y[1, 70] == 5.0 and (y[1, 64:70] == 0).all()
 
 
+def test_bf16_codes_rounding_rule_holds_for_every_pair():
+    """The kernel's rule for bfloat16 (a float product, rounded to 19 bits, then to an integer) against
+    exact integers: every pair of significands, exponents 0 .. 9 apart."""
+    A = np.arange(128, 256)
+    for s in range(10):
+        X = np.arange(128, 256)
+        if s == 0:
+            x, a = np.meshgrid(X, A, indexing="ij")
+            x, a = x[x <= a], a[x <= a]
+        else:
+            x, a = (v.reshape(-1) for v in np.meshgrid(X, A, indexing="ij"))
+        for scale in (1.0, 2.0 ** -40, 2.0 ** 60):
+            amax = (a * scale).astype(np.float32)
+            v = (x * 2.0 ** -s * scale).astype(np.float32)
+            q = v * (np.float32(127) / amax)
+            q = ((q.view(np.uint32) + np.uint32(8)) & ~np.uint32(15)).view(np.float32)
+            got = np.rint(q).astype(np.int64)
+            num, den = 2 * 127 * x, a * 2 ** s            # twice the quotient
+            lo = num // (2 * den)
+            rest = num - 2 * den * lo                      # against den: below, at or above the half
+            want = lo + ((rest > den) | ((rest == den) & (lo % 2 == 1)))
+            assert np.array_equal(got, want), s
+
+
 # ------------------------------------------------------------------ struct layout
 def test_struct_layouts():
     assert ctypes.sizeof(L.moe_route_cfg) == 40 and L.moe_route_cfg.scale.offset == 32
