@@ -145,11 +145,11 @@ def act(h, name):
     return 0.5 * h * (1 + np.tanh(math.sqrt(2 / math.pi) * (h + 0.044715 * h ** 3)))
 
 
-def experts(x, idx, w, W1, W2, act_name):
+def experts(x, idx, w, W1, W2, act_name, part=2.0 ** -16):
     """y (W1 [E][f][d], W2 [E][d][f] decoded), and a bound on a float32 evaluation's error:
     sums of K terms are off by (K + 4) half steps of the sum of magnitudes (the order is
     free), the activation by 16 half steps of |h| and, with slope up to 1.13, by what h is;
-    act(h) goes on as bfloat16 parts good to 2^-16."""
+    act(h) goes on as bfloat16 parts good to `part` (one part: 2^-8, half a step)."""
     T, d = x.shape
     E, f = W1.shape[:2]
     y, err = np.zeros((T, d)), np.zeros((T, d))
@@ -161,7 +161,7 @@ def experts(x, idx, w, W1, W2, act_name):
             h = W1[e] @ x[t]
             eh = (d + 4) * U32 * (np.abs(W1[e]) @ np.abs(x[t]))
             a = act(h, act_name)
-            ea = 1.13 * eh + 16 * U32 * np.abs(h) + 2.0 ** -16 * np.abs(a)
+            ea = 1.13 * eh + 16 * U32 * np.abs(h) + part * np.abs(a)
             y[t] += w[t, r] * (W2[e] @ a)
             err[t] += abs(w[t, r]) * (np.abs(W2[e]) @ ea + (f + 8 + idx.shape[1]) * U32 * (np.abs(W2[e]) @ np.abs(a)))
     return y, err

@@ -359,7 +359,7 @@ __global__ __launch_bounds__(64 * WV, 3) void w4_product_kernel(W4Args a) {
 template <typename T>
 __global__ __launch_bounds__(256) void w4_combine_kernel(const float* __restrict__ O, const int32_t* __restrict__ idx,
                                                          const float* __restrict__ w, T* __restrict__ y, int64_t T_tokens,
-                                                         int d, int E, int k) {
+                                                         int d, int E, int k, int splits) {
   const int c = (blockIdx.x * 256 + threadIdx.x) * 4;
   if (c >= d) return;
   for (int64_t t = blockIdx.y; t < T_tokens; t += gridDim.y) {
@@ -375,6 +375,7 @@ __global__ __launch_bounds__(256) void w4_combine_kernel(const float* __restrict
         e[r] = idx[i];
         wr[r] = w[i];
         o[r] = *reinterpret_cast<const f32x4*>(O + i * d + c);
+        for (int z = 1; z < splits; ++z) o[r] += *reinterpret_cast<const f32x4*>(O + (z * T_tokens * k + i) * d + c);
       }
 #pragma unroll
       for (int r = 0; r < 4; ++r)
@@ -389,23 +390,261 @@ __global__ __launch_bounds__(256) void w4_combine_kernel(const float* __restrict
   }
 }
 
-// Workspace: list, tiles, tile count | parts | O.
+// ------------------------------------------------------------------ many tokens
+// bfloat16 with two dozen tokens an expert and more: the products are matrix products
+// again.  The tokens' rows are laid out by expert, padded to 16, in the order in which the
+// matrix instructions take them (x by w4_pack_kernel, act(W1 x) by the first product), so
+// both sides of a 128-row x 128-token block go through LDS in whole lines: the codes of 256
+// inputs, the tokens' values of 64, each with the next on its way.  Four waves, 64 x 64 each.
+// act(W1 x) is rounded once to bfloat16 here, as moe_expert_ffn_fwd does: a second part
+// would double the second product, which is no longer hidden behind the weights.
+constexpr int kGemmRows = 128, kGemmToks = 128;
+struct W4Group {   // where an expert's rows are
+  int32_t e, row, rows, pad;   // first padded row of a token tile, its rows (a multiple of 16)
+};
+
+// choice_of[row] (-1: padding), the token tiles and their number; an expert's tiles are
+// alike in size.
+__global__ __launch_bounds__(kW4ListThreads) void w4_group_kernel(const int32_t* __restrict__ idx, int n, int E,
+                                                                  int32_t* __restrict__ choice_of,
+                                                                  W4Group* __restrict__ tiles,
+                                                                  int32_t* __restrict__ ntiles, int max_rows) {
+  __shared__ int32_t cnt[kRouterMaxE], at[kRouterMaxE], sum[2][kRouterMaxE];
+  const int tid = threadIdx.x;
+  for (int e = tid; e < kRouterMaxE; e += kW4ListThreads) cnt[e] = 0;
+  for (int i = tid; i < max_rows; i += kW4ListThreads) choice_of[i] = -1;
+  __syncthreads();
+  for (int i = tid; i < n; i += kW4ListThreads) {
+    const int e = idx[i];
+    if (e >= 0 && e < E) atomicAdd(&cnt[e], 1);
+  }
+  __syncthreads();
+  if (tid < kRouterMaxE) {
+    sum[0][tid] = (cnt[tid] + 15) / 16;
+    sum[1][tid] = (cnt[tid] + kGemmToks - 1) / kGemmToks;
+  }
+  __syncthreads();
+  for (int o = 1; o < kRouterMaxE; o <<= 1) {
+    int a = 0, b = 0;
+    if (tid < kRouterMaxE && tid >= o) {
+      a = sum[0][tid - o];
+      b = sum[1][tid - o];
+    }
+    __syncthreads();
+    if (tid < kRouterMaxE) {
+      sum[0][tid] += a;
+      sum[1][tid] += b;
+    }
+    __syncthreads();
+  }
+  if (tid < kRouterMaxE) {
+    const int t16 = (cnt[tid] + 15) / 16, nt = (cnt[tid] + kGemmToks - 1) / kGemmToks;
+    const int first = 16 * (sum[0][tid] - t16), t0 = sum[1][tid] - nt;
+    at[tid] = first;
+    const int each = nt ? (t16 + nt - 1) / nt : 0;   // 16-row tiles of a token tile
+    for (int j = 0; j < nt; ++j) tiles[t0 + j] = W4Group{tid, first + 16 * j * each, 16 * max(0, min(each, t16 - j * each)), 0};
+    if (tid == kRouterMaxE - 1) *ntiles = sum[1][tid];
+  }
+  __syncthreads();
+  for (int i = tid; i < n; i += kW4ListThreads) {
+    const int e = idx[i];
+    if (e >= 0 && e < E) choice_of[atomicAdd(&at[e], 1)] = i;
+  }
+}
+
+// Element (row, input) of the laid-out tokens [row / 16][input / 128][j][lane][8].
+__host__ __device__ __forceinline__ int64_t w4_tok_off(int64_t row, int in, int K) {
+  return (((row >> 4) * (K >> 7) + (in >> 7)) * 4 + ((in & 31) >> 3)) * 512 + (((in >> 5) & 3) * 16 + (row & 15)) * 8 + (in & 7);
+}
+
+// One thread per 8 values, in the output's order.
+__global__ __launch_bounds__(256) void w4_pack_kernel(const uint16_t* __restrict__ x, const int32_t* __restrict__ choice_of,
+                                                      uint16_t* __restrict__ out, int K, int k, int64_t pieces) {
+  for (int64_t p = (int64_t)blockIdx.x * 256 + threadIdx.x; p < pieces; p += (int64_t)gridDim.x * 256) {
+    const int lane = (int)(p & 63), j = (int)(p >> 6) & 3;
+    const int64_t chunk = p >> 8;
+    const int nc = K >> 7;
+    const int64_t t16 = chunk / nc;
+    const int c = (int)(chunk - t16 * nc);
+    const int choice = choice_of[t16 * 16 + (lane & 15)];
+    u32x4 v = {0u, 0u, 0u, 0u};
+    if (choice >= 0) v = *reinterpret_cast<const u32x4*>(x + (int64_t)(choice / k) * K + c * 128 + (lane >> 4) * 32 + 8 * j);
+    *reinterpret_cast<u32x4*>(out + p * 8) = v;
+  }
+}
+
+struct W4GemmArgs {
+  const uint8_t *codes, *scales;
+  const uint16_t* in;    // laid-out tokens of K values
+  void* out;             // FIRST: laid-out tokens of N values; else float [splits][n][N]
+  const int32_t* choice_of;
+  const W4Group* tiles;
+  const int32_t* ntiles;
+  int32_t N, K, n, act, steps;   // steps of 256 inputs of one split
+};
+
+template <bool FIRST>
+__global__ __launch_bounds__(256, 2) void w4_gemm_kernel(W4GemmArgs a) {
+  __shared__ u32x4 wcode[2][kGemmRows][8];     // [row][piece ^ row % 8]
+  __shared__ uint32_t wsc[2][2][kGemmRows];    // [half][row]: four groups' bytes
+  __shared__ u32x4 tok[2][8][2][64];           // [16-token tile][j][lane]
+  if ((int)blockIdx.y >= *a.ntiles) return;
+  const W4Group g = a.tiles[blockIdx.y];
+  if (g.rows == 0) return;
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  const int i16 = lane & 15, q = lane >> 4;
+  const int rg = wv & 1, tg = wv >> 1;
+  const int row0 = blockIdx.x * kGemmRows;
+  const int nt16 = g.rows >> 4;                                  // 16-token tiles of the block
+  const int mine = min(4, max(0, nt16 - 4 * tg));                // of the wave
+  const int k0 = blockIdx.z * a.steps * kStep;
+  const int k1 = min(a.K, k0 + a.steps * kStep);
+  if (k0 >= k1) return;   // (the launch leaves no split empty)
+  const uint8_t* codes = a.codes + ((int64_t)g.e * a.N + row0) * (a.K / 2);
+  const uint8_t* scales = a.scales + ((int64_t)g.e * a.N + row0) * (a.K / 32);
+  const uint16_t* toks = a.in + (int64_t)(g.row >> 4) * a.K * 16;
+
+  u32x4 wreg[4];
+  uint32_t sreg[2];
+  auto load_w = [&](int col) __attribute__((always_inline)) {
+    const int at = col + (lane & 7) * 32;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int64_t row = 32 * wv + 8 * i + (lane >> 3);
+      wreg[i] = u32x4{0u, 0u, 0u, 0u};
+      if (at < k1) wreg[i] = *reinterpret_cast<const u32x4*>(codes + row * (a.K / 2) + at / 2);
+    }
+    if (tid < kGemmRows) {   // (K is a multiple of 128: whole halves)
+      const uint8_t* p = scales + (int64_t)tid * (a.K / 32) + col / 32;
+      sreg[0] = *reinterpret_cast<const uint32_t*>(p);
+      sreg[1] = col + 128 < k1 ? *reinterpret_cast<const uint32_t*>(p + 4) : 0u;
+    }
+  };
+  auto store_w = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) wcode[b][32 * wv + 8 * i + (lane >> 3)][(lane & 7) ^ (lane >> 3)] = wreg[i];
+    if (tid < kGemmRows) {
+      wsc[b][0][tid] = sreg[0];
+      wsc[b][1][tid] = sreg[1];
+    }
+  };
+  // Values of 64 inputs: those of pair jp (j = 2 jp, 2 jp + 1) of the 128 from `col` on.
+  u32x4 treg[4];
+  auto load_t = [&](int col, int jp) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int f = wv * 4 + i, t = f >> 1, j = 2 * jp + (f & 1);   // fragments 4 wv .. of 16
+      treg[i] = u32x4{0u, 0u, 0u, 0u};
+      if (t < nt16)
+        treg[i] = *reinterpret_cast<const u32x4*>(toks + (((int64_t)t * (a.K >> 7) + (col >> 7)) * 4 + j) * 512 + lane * 8);
+    }
+  };
+  auto store_t = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) tok[b][(wv * 4 + i) >> 1][i & 1][lane] = treg[i];
+  };
+
+  f32x4 acc[4][4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int t = 0; t < 4; ++t) acc[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  load_w(k0);
+  load_t(k0, 0);
+  store_w(0);
+  store_t(0);
+  __syncthreads();
+  int wb = 0;
+  for (int col = k0; col < k1; col += kStep, wb ^= 1) {
+    const bool more = col + kStep < k1;
+    if (more) load_w(col + kStep);
+    const int halves = col + 128 < k1 ? 2 : 1;
+    for (int h = 0; h < halves; ++h) {
+      u32x4 code[4];
+      float sc[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int row = 64 * rg + 16 * r + i16;
+        code[r] = wcode[wb][row][(4 * h + q) ^ (i16 & 7)];
+        sc[r] = __uint_as_float(((wsc[wb][h][row] >> (8 * q)) & 0xffu) << 23);
+      }
+#pragma unroll
+      for (int jp = 0; jp < 2; ++jp) {
+        // the next 64 inputs; none after the last
+        const bool last = jp == 1 && h + 1 == halves;
+        const int ncol = jp == 0 ? col + 128 * h : last ? col + kStep : col + 128;
+        const bool next = !last || more;
+        if (next) load_t(ncol, jp ^ 1);
+#pragma unroll
+        for (int jj = 0; jj < 2; ++jj) {
+          bf16x8 b[4];
+#pragma unroll
+          for (int t = 0; t < 4; ++t) b[t] = __builtin_bit_cast(bf16x8, tok[jp][4 * tg + t][jj][lane]);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const bf16x8 f = w4_frag(code[r][2 * jp + jj], sc[r]);
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+              if (t < mine) acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, b[t], acc[r][t], 0, 0, 0);
+          }
+        }
+        if (next) store_t(jp ^ 1);
+        if (last && more) store_w(wb ^ 1);
+        __syncthreads();
+      }
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    if (t >= mine) break;
+    const int64_t row = g.row + 64 * tg + 16 * t + i16;
+    const int choice = FIRST ? 0 : a.choice_of[row];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int f = row0 + 64 * rg + 16 * r + 4 * q;
+      if constexpr (FIRST) {   // (padding rows: act(0) = 0)
+        float h[4] = {acc[r][t][0], acc[r][t][1], acc[r][t][2], acc[r][t][3]};
+        w4_act(h, a.act);
+        *reinterpret_cast<u32x2*>((uint16_t*)a.out + w4_tok_off(row, f, a.N)) =
+            u32x2{pack_bf16x2(h[0], h[1]), pack_bf16x2(h[2], h[3])};
+      } else {
+        if (choice >= 0)
+          *reinterpret_cast<f32x4*>((float*)a.out + ((int64_t)blockIdx.z * a.n + choice) * a.N + f) = acc[r][t];
+      }
+    }
+  }
+}
+
+// The laid-out form serves: bfloat16, whole 128s, and tokens enough.
+constexpr int kGemmFrom = 24;   // choices an expert, on average
+constexpr int kGemmSplits = 4;
+static bool w4_gemm(const moe_w4_cfg& c) {
+  return c.dtype == MOE_BF16 && c.d_model % 128 == 0 && c.d_ff % 128 == 0 && c.T * c.k >= (int64_t)kGemmFrom * c.E;
+}
+
+// Workspace: list (or choices by row), tiles, tile count | parts (or laid-out act(W1 x)) |
+// O | laid-out x.
 struct W4Ws {
-  size_t list, tiles, ntiles, parts, O, total;
+  size_t list, tiles, ntiles, parts, O, x, total;
   int max_tiles;
+  int64_t rows;   // laid-out rows at most
 };
 static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 static W4Ws w4_ws(const moe_w4_cfg& c) {
   W4Ws w;
   const int64_t n = c.T * c.k;
-  const int ns = c.dtype == MOE_BF16 ? 2 : 3;
-  w.max_tiles = (int)(std::min<int64_t>(n, c.E) + n / kW4Tile);
+  const bool bf = c.dtype == MOE_BF16;
+  w.rows = n + 15 * std::min<int64_t>(n, c.E);
+  w.rows = (w.rows + 15) / 16 * 16;
+  w.max_tiles = (int)(std::min<int64_t>(n, c.E) + n / kW4Tile);   // (of 16 tokens; of 128 there are fewer)
   w.list = 0;
-  w.tiles = up256(4 * (size_t)n);
+  w.tiles = up256(4 * (size_t)w.rows);
   w.ntiles = w.tiles + sizeof(W4Tile) * (size_t)w.max_tiles;
   w.parts = up256(w.ntiles + 4);
-  w.O = up256(w.parts + (size_t)ns * n * c.d_ff * 2);
-  w.total = up256(w.O + (size_t)n * c.d_model * 4);
+  w.O = up256(w.parts + std::max((size_t)(bf ? 2 : 3) * n, bf ? (size_t)w.rows : 0) * c.d_ff * 2);
+  w.x = up256(w.O + (size_t)(bf ? kGemmSplits : 1) * n * c.d_model * 4);
+  w.total = up256(w.x + (bf ? (size_t)w.rows * c.d_model * 2 : 0));
   return w;
 }
 size_t experts_w4_ws_bytes(const moe_w4_cfg& c) { return w4_ws(c).total; }
@@ -427,6 +666,36 @@ template <typename T, bool FIRST, int NS, int NO>
 static void launch_w4_product(const W4Args& a, int gy, hipStream_t s) {
   if (a.K % kStep == 0) launch_w4_rows<T, FIRST, NS, NO, true>(a, gy, s);
   else launch_w4_rows<T, FIRST, NS, NO, false>(a, gy, s);
+}
+
+static void launch_w4_gemm(const moe_w4_cfg& c, const void* x, const int32_t* idx, const float* w, const uint8_t* W1c,
+                           const uint8_t* W1s, const uint8_t* W2c, const uint8_t* W2s, void* y, void* ws, hipStream_t s) {
+  const W4Ws L = w4_ws(c);
+  const int n = (int)(c.T * c.k), d = c.d_model, f = c.d_ff;
+  char* base = (char*)ws;
+  int32_t* choice_of = (int32_t*)(base + L.list);
+  W4Group* tiles = (W4Group*)(base + L.tiles);
+  int32_t* ntiles = (int32_t*)(base + L.ntiles);
+  static_assert(sizeof(W4Group) == sizeof(W4Tile), "one table's room");
+  hipLaunchKernelGGL(w4_group_kernel, dim3(1), dim3(kW4ListThreads), 0, s, idx, n, c.E, choice_of, tiles, ntiles,
+                     (int)L.rows);
+  const int64_t pieces = L.rows * (d / 8);
+  hipLaunchKernelGGL(w4_pack_kernel, dim3((unsigned)std::min<int64_t>((pieces + 255) / 256, 1 << 20)), dim3(256), 0, s,
+                     (const uint16_t*)x, (const int32_t*)choice_of, (uint16_t*)(base + L.x), d, c.k, pieces);
+  const int gy = std::min<int64_t>(n, c.E) + n / kGemmToks;
+  const W4GemmArgs a{W1c, W1s, (const uint16_t*)(base + L.x), base + L.parts, choice_of, tiles, ntiles, f, d, n, c.act,
+                     (d + kStep - 1) / kStep};
+  hipLaunchKernelGGL(w4_gemm_kernel<true>, dim3(f / kGemmRows, gy), dim3(256), 0, s, a);
+  // K is split where the blocks would not fill the CUs twice; whole steps, no split empty.
+  const int steps = (f + kStep - 1) / kStep;
+  const int64_t blocks = (int64_t)(d / kGemmRows) * (std::min<int64_t>(n, c.E) + n / kGemmToks) * 2 / 3;   // (of the bound, about)
+  int splits = (int)std::min<int64_t>(std::min(kGemmSplits, steps), std::max<int64_t>(1, 2 * num_cus() / std::max<int64_t>(1, blocks)));
+  const int per = (steps + splits - 1) / splits;
+  splits = (steps + per - 1) / per;
+  const W4GemmArgs b{W2c, W2s, (const uint16_t*)(base + L.parts), base + L.O, choice_of, tiles, ntiles, d, f, n, c.act, per};
+  hipLaunchKernelGGL(w4_gemm_kernel<false>, dim3(d / kGemmRows, gy, splits), dim3(256), 0, s, b);
+  hipLaunchKernelGGL(w4_combine_kernel<uint16_t>, dim3((d + 1023) / 1024, (unsigned)std::min<int64_t>(c.T, 32768)), dim3(256), 0,
+                     s, (const float*)(base + L.O), idx, w, (uint16_t*)y, c.T, d, c.E, c.k, splits);
 }
 
 template <typename T, int NX, int NA>
@@ -452,13 +721,14 @@ static void launch_w4_t(const moe_w4_cfg& c, const void* x, const int32_t* idx, 
   launch_w4_product<T, false, NA, NA>(b, gy, s);
   hipLaunchKernelGGL(w4_combine_kernel<T>, dim3((c.d_model + 1023) / 1024, (unsigned)std::min<int64_t>(c.T, 32768)),
                      dim3(256), 0, s,
-                     (const float*)(base + L.O), idx, w, (T*)y, c.T, c.d_model, c.E, c.k);
+                     (const float*)(base + L.O), idx, w, (T*)y, c.T, c.d_model, c.E, c.k, 1);
 }
 
 void launch_experts_w4(const moe_w4_cfg& c, const void* x, const int32_t* idx, const float* w, const uint8_t* W1c,
                        const uint8_t* W1s, const uint8_t* W2c, const uint8_t* W2s, void* y, void* ws, hipStream_t s) {
   if (c.T == 0) return;
-  if (c.dtype == MOE_BF16) launch_w4_t<uint16_t, 1, 2>(c, x, idx, w, W1c, W1s, W2c, W2s, y, ws, s);
+  if (w4_gemm(c)) launch_w4_gemm(c, x, idx, w, W1c, W1s, W2c, W2s, y, ws, s);
+  else if (c.dtype == MOE_BF16) launch_w4_t<uint16_t, 1, 2>(c, x, idx, w, W1c, W1s, W2c, W2s, y, ws, s);
   else launch_w4_t<float, 3, 3>(c, x, idx, w, W1c, W1s, W2c, W2s, y, ws, s);
 }
 

@@ -44,8 +44,8 @@ def inputs(T, d, f, E, k, dtype, seed, skew=None):
     return x, idx.reshape(T, k), w, W
 
 
-def check(y, x, idx, w, W, act, dtype):
-    ref, err = O.experts(x.double().numpy(), idx, w.astype(np.float64), O.w4_decode(W[0], W[1]), O.w4_decode(W[2], W[3]), act)
+def check(y, x, idx, w, W, act, dtype, part=2.0 ** -16):
+    ref, err = O.experts(x.double().numpy(), idx, w.astype(np.float64), O.w4_decode(W[0], W[1]), O.w4_decode(W[2], W[3]), act, part)
     got = y.double().cpu().numpy()
     tol = err + (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) * (np.abs(ref) + err)   # y's own rounding
     assert np.isfinite(got).all()
@@ -74,6 +74,47 @@ def test_activations(T, act, dtype):
     x, idx, w, W = inputs(T, 192, 320, 6, 2, dtype, 5)
     y = run(x.cuda(), dev(idx), dev(w), [dev(v) for v in W], 6, 320, 2, dtype, act)
     check(y, x, idx, w, W, act, dtype)
+
+
+# From 24 tokens an expert on, bfloat16 with whole 128s: the laid-out products, where act(W1 x)
+# is rounded once (half a step of bfloat16).
+MANY = [  # T, d, f, E, k
+    (24, 128, 128, 1, 1), (48, 128, 256, 2, 1), (47, 128, 128, 1, 1), (128, 256, 128, 1, 1), (129, 384, 128, 1, 1),
+    (300, 128, 640, 3, 2), (257, 640, 128, 4, 2), (600, 128, 128, 16, 1), (512, 256, 384, 2, 2), (33, 128, 1152, 1, 1),
+    (100, 128, 2048, 2, 2)]
+
+
+@pytest.mark.parametrize("T,d,f,E,k", MANY)
+def test_many_tokens(T, d, f, E, k):
+    x, idx, w, W = inputs(T, d, f, E, k, "bf16", T + d + f)
+    y = run(x.cuda(), dev(idx), dev(w), [dev(v) for v in W], E, f, k, "bf16", "gelu_tanh")
+    check(y, x, idx, w, W, "gelu_tanh", "bf16", 2.0 ** -8)
+
+
+@pytest.mark.parametrize("act", ["identity", "relu", "gelu_erf"])
+def test_many_tokens_uneven(act):
+    T, d, f, E, k = 320, 128, 256, 6, 3
+    x, idx, w, W = inputs(T, d, f, E, k, "bf16", 9, np.array([0.5, 0.0, 0.3, 0.15, 0.04, 0.01]))
+    idx[::7, 1] = -1
+    idx[300:] = E
+    w[(idx < 0) | (idx >= E)] = np.nan
+    x[300:] = float("inf")
+    y = run(x.cuda(), dev(idx), dev(w), [dev(v) for v in W], E, f, k, "bf16", act)
+    x[300:] = 0
+    check(y, x, idx, np.nan_to_num(w), W, act, "bf16", 2.0 ** -8)
+    again = run(x.cuda(), dev(idx), dev(w), [dev(v) for v in W], E, f, k, "bf16", act)
+    assert torch.equal(y[:300], again[:300]) and (y[300:] == 0).all()
+
+
+def test_many_tokens_infinities_stay_with_their_token():
+    T, d, f, E, k = 60, 128, 128, 2, 1
+    x, idx, w, W = inputs(T, d, f, E, k, "bf16", 1)
+    ref = run(x.cuda(), dev(idx), dev(w), [dev(v) for v in W], E, f, k, "bf16", "relu")
+    bad = x.clone()
+    bad[3, 5], bad[8, 127] = float("inf"), float("nan")
+    y = run(bad.cuda(), dev(idx), dev(w), [dev(v) for v in W], E, f, k, "bf16", "relu")
+    rest = [t for t in range(T) if t not in (3, 8)]
+    assert torch.equal(y[rest], ref[rest]) and torch.isnan(y[8]).all() and not torch.isfinite(y[3]).any()
 
 
 @pytest.mark.parametrize("T", [10, 90, 400])
