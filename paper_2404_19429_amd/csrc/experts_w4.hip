@@ -394,11 +394,11 @@ __global__ __launch_bounds__(256) void w4_combine_kernel(const float* __restrict
 // bfloat16 with two dozen tokens an expert and more: the products are matrix products
 // again.  The tokens' rows are laid out by expert, padded to 16, in the order in which the
 // matrix instructions take them (x by w4_pack_kernel, act(W1 x) by the first product), so
-// both sides of a 128-row x 128-token block go through LDS in whole lines: the codes of 256
-// inputs, the tokens' values of 64, each with the next on its way.  Four waves, 64 x 64 each.
+// both sides of a 128-row x 160-token block go through LDS in whole lines: the codes of 256
+// inputs, the tokens' values of 64, each with the next on its way.  Four waves, 64 rows by half the tokens each.
 // act(W1 x) is rounded once to bfloat16 here, as moe_expert_ffn_fwd does: a second part
 // would double the second product, which is no longer hidden behind the weights.
-constexpr int kGemmRows = 128, kGemmToks = 128;
+constexpr int kGemmRows = 128, kGemmToks = 160, kGemmT = kGemmToks / 32;   // kGemmT: 16-token tiles of a wave
 struct W4Group {   // where an expert's rows are
   int32_t e, row, rows, pad;   // first padded row of a token tile, its rows (a multiple of 16)
 };
@@ -483,20 +483,38 @@ struct W4GemmArgs {
   int32_t N, K, n, act, steps;   // steps of 256 inputs of one split
 };
 
+// The activation of values that are then rounded to bfloat16.  (erf's code once, not at
+// each of a lane's twenty places: unrolled it is most of the kernel.)
+__device__ __noinline__ f32x4 w4_act_erf(f32x4 v) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = act_fwd_t<MOE_ACT_GELU_ERF>(v[i]);
+  return v;
+}
+__device__ __forceinline__ f32x4 w4_act_rounded(f32x4 v, int act) {
+  if (act == MOE_ACT_GELU_ERF) return w4_act_erf(v);
+  f32x4 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float t = act_fwd_t<MOE_ACT_GELU_TANH>(v[i]);
+    r[i] = act == MOE_ACT_GELU_TANH ? t : act == MOE_ACT_RELU && v[i] < 0.f ? 0.f : v[i];
+  }
+  return r;
+}
+
 template <bool FIRST>
 __global__ __launch_bounds__(256, 2) void w4_gemm_kernel(W4GemmArgs a) {
   __shared__ u32x4 wcode[2][kGemmRows][8];     // [row][piece ^ row % 8]
   __shared__ uint32_t wsc[2][2][kGemmRows];    // [half][row]: four groups' bytes
-  __shared__ u32x4 tok[2][8][2][64];           // [16-token tile][j][lane]
+  __shared__ u32x4 tok[2][2 * kGemmT][2][64];  // [16-token tile][j][lane]
   if ((int)blockIdx.y >= *a.ntiles) return;
   const W4Group g = a.tiles[blockIdx.y];
   if (g.rows == 0) return;
-  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int i16 = lane & 15, q = lane >> 4;
   const int rg = wv & 1, tg = wv >> 1;
   const int row0 = blockIdx.x * kGemmRows;
   const int nt16 = g.rows >> 4;                                  // 16-token tiles of the block
-  const int mine = min(4, max(0, nt16 - 4 * tg));                // of the wave
+  const int t0 = tg * ((nt16 + 1) / 2), mine = tg ? nt16 - t0 : (nt16 + 1) / 2;   // of the wave
   const int k0 = blockIdx.z * a.steps * kStep;
   const int k1 = min(a.K, k0 + a.steps * kStep);
   if (k0 >= k1) return;   // (the launch leaves no split empty)
@@ -504,6 +522,8 @@ __global__ __launch_bounds__(256, 2) void w4_gemm_kernel(W4GemmArgs a) {
   const uint8_t* scales = a.scales + ((int64_t)g.e * a.N + row0) * (a.K / 32);
   const uint16_t* toks = a.in + (int64_t)(g.row >> 4) * a.K * 16;
 
+  // (K is a multiple of 128.  A half step past k1 is not looked at, nor are tiles past
+  // nt16: their loads are of something inside the arrays, and wait for no branch.)
   u32x4 wreg[4];
   uint32_t sreg[2];
   auto load_w = [&](int col) __attribute__((always_inline)) {
@@ -511,14 +531,11 @@ __global__ __launch_bounds__(256, 2) void w4_gemm_kernel(W4GemmArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int64_t row = 32 * wv + 8 * i + (lane >> 3);
-      wreg[i] = u32x4{0u, 0u, 0u, 0u};
-      if (at < k1) wreg[i] = *reinterpret_cast<const u32x4*>(codes + row * (a.K / 2) + at / 2);
+      wreg[i] = *reinterpret_cast<const u32x4*>(codes + row * (a.K / 2) + (at < k1 ? at : col) / 2);
     }
-    if (tid < kGemmRows) {   // (K is a multiple of 128: whole halves)
-      const uint8_t* p = scales + (int64_t)tid * (a.K / 32) + col / 32;
-      sreg[0] = *reinterpret_cast<const uint32_t*>(p);
-      sreg[1] = col + 128 < k1 ? *reinterpret_cast<const uint32_t*>(p + 4) : 0u;
-    }
+    const uint8_t* p = scales + (int64_t)(tid & (kGemmRows - 1)) * (a.K / 32);
+    sreg[0] = *reinterpret_cast<const uint32_t*>(p + col / 32);
+    sreg[1] = *reinterpret_cast<const uint32_t*>(p + (col + 128 < k1 ? col + 128 : col) / 32);
   };
   auto store_w = [&](int b) __attribute__((always_inline)) {
 #pragma unroll
@@ -529,26 +546,24 @@ __global__ __launch_bounds__(256, 2) void w4_gemm_kernel(W4GemmArgs a) {
     }
   };
   // Values of 64 inputs: those of pair jp (j = 2 jp, 2 jp + 1) of the 128 from `col` on.
-  u32x4 treg[4];
+  u32x4 treg[kGemmT];
   auto load_t = [&](int col, int jp) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int f = wv * 4 + i, t = f >> 1, j = 2 * jp + (f & 1);   // fragments 4 wv .. of 16
-      treg[i] = u32x4{0u, 0u, 0u, 0u};
-      if (t < nt16)
-        treg[i] = *reinterpret_cast<const u32x4*>(toks + (((int64_t)t * (a.K >> 7) + (col >> 7)) * 4 + j) * 512 + lane * 8);
+    for (int i = 0; i < kGemmT; ++i) {
+      const int f = wv + 4 * i, t = min(f >> 1, nt16 - 1), j = 2 * jp + (f & 1);   // every fourth fragment
+      treg[i] = *reinterpret_cast<const u32x4*>(toks + (((int64_t)t * (a.K >> 7) + (col >> 7)) * 4 + j) * 512 + lane * 8);
     }
   };
   auto store_t = [&](int b) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) tok[b][(wv * 4 + i) >> 1][i & 1][lane] = treg[i];
+    for (int i = 0; i < kGemmT; ++i) tok[b][(wv + 4 * i) >> 1][wv & 1][lane] = treg[i];
   };
 
-  f32x4 acc[4][4];
+  f32x4 acc[4][kGemmT];
 #pragma unroll
   for (int r = 0; r < 4; ++r)
 #pragma unroll
-    for (int t = 0; t < 4; ++t) acc[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < kGemmT; ++t) acc[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 
   load_w(k0);
   load_t(k0, 0);
@@ -557,55 +572,75 @@ __global__ __launch_bounds__(256, 2) void w4_gemm_kernel(W4GemmArgs a) {
   __syncthreads();
   int wb = 0;
   for (int col = k0; col < k1; col += kStep, wb ^= 1) {
-    const bool more = col + kStep < k1;
-    if (more) load_w(col + kStep);
-    const int halves = col + 128 < k1 ? 2 : 1;
-    for (int h = 0; h < halves; ++h) {
-      u32x4 code[4];
-      float sc[4];
+    // (After the last step the loads ask for what is there already: a branch around a load
+    // has its results copied, and so waited for, right behind it.)
+    const bool two = col + 128 < k1;
+    const int after = col + kStep < k1 ? col + kStep : col;
+    u32x4 code[4];
+    float sc[4];
+    // 64 inputs: half h, pair jp.  (Straight code, no loop over the four: ahead of a loop
+    // the compiler waits for the weights that are still on their way.)
+    auto sub = [&](auto hc, auto jc) __attribute__((always_inline)) {
+      constexpr int h = decltype(hc)::value, jp = decltype(jc)::value;
+      if constexpr (jp == 0) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int row = 64 * rg + 16 * r + i16;
-        code[r] = wcode[wb][row][(4 * h + q) ^ (i16 & 7)];
-        sc[r] = __uint_as_float(((wsc[wb][h][row] >> (8 * q)) & 0xffu) << 23);
-      }
-#pragma unroll
-      for (int jp = 0; jp < 2; ++jp) {
-        // the next 64 inputs; none after the last
-        const bool last = jp == 1 && h + 1 == halves;
-        const int ncol = jp == 0 ? col + 128 * h : last ? col + kStep : col + 128;
-        const bool next = !last || more;
-        if (next) load_t(ncol, jp ^ 1);
-#pragma unroll
-        for (int jj = 0; jj < 2; ++jj) {
-          bf16x8 b[4];
-#pragma unroll
-          for (int t = 0; t < 4; ++t) b[t] = __builtin_bit_cast(bf16x8, tok[jp][4 * tg + t][jj][lane]);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const bf16x8 f = w4_frag(code[r][2 * jp + jj], sc[r]);
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-              if (t < mine) acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, b[t], acc[r][t], 0, 0, 0);
-          }
+        for (int r = 0; r < 4; ++r) {
+          const int row = 64 * rg + 16 * r + i16;
+          code[r] = wcode[wb][row][(4 * h + q) ^ (i16 & 7)];
+          sc[r] = __uint_as_float(((wsc[wb][h][row] >> (8 * q)) & 0xffu) << 23);
         }
-        if (next) store_t(jp ^ 1);
-        if (last && more) store_w(wb ^ 1);
-        __syncthreads();
       }
+      const bool last = jp == 1 && (h == 1 || !two);
+      load_t(jp == 0 ? col + 128 * h : last ? after : col + 128, jp ^ 1);
+      // loads return in order: the next weights behind these, not ahead of them
+      if constexpr (h == 0 && jp == 0) load_w(after);
+      __builtin_amdgcn_sched_barrier(0);
+      // Both j's reads ahead of the products, which wait for the first j's only.  (An empty
+      // asm uses the values where they are waited for: left alone the compiler moves each
+      // read into the branch of its products, and every product waits for LDS.)
+      u32x4 b[2][kGemmT];
+#pragma unroll
+      for (int jj = 0; jj < 2; ++jj)
+#pragma unroll
+        for (int t = 0; t < kGemmT; ++t) b[jj][t] = tok[jp][t0 + t][jj][lane];
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int jj = 0; jj < 2; ++jj) {
+        bf16x8 f[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) f[r] = w4_frag(code[r][2 * jp + jj], sc[r]);
+#pragma unroll
+        for (int t = 0; t < kGemmT; ++t) asm volatile("" : "+v"(b[jj][t]));
+#pragma unroll
+        for (int t = 0; t < kGemmT; ++t)
+          if (t < mine)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[r], __builtin_bit_cast(bf16x8, b[jj][t]), acc[r][t], 0, 0, 0);
+      }
+      store_t(jp ^ 1);
+      if (last) store_w(wb ^ 1);
+      __syncthreads();
+    };
+    constexpr std::integral_constant<int, 0> c0;
+    constexpr std::integral_constant<int, 1> c1;
+    sub(c0, c0);
+    sub(c0, c1);
+    if (two) {
+      sub(c1, c0);
+      sub(c1, c1);
     }
   }
 #pragma unroll
-  for (int t = 0; t < 4; ++t) {
+  for (int t = 0; t < kGemmT; ++t) {
     if (t >= mine) break;
-    const int64_t row = g.row + 64 * tg + 16 * t + i16;
+    const int64_t row = g.row + 16 * (t0 + t) + i16;
     const int choice = FIRST ? 0 : a.choice_of[row];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int f = row0 + 64 * rg + 16 * r + 4 * q;
       if constexpr (FIRST) {   // (padding rows: act(0) = 0)
-        float h[4] = {acc[r][t][0], acc[r][t][1], acc[r][t][2], acc[r][t][3]};
-        w4_act(h, a.act);
+        const f32x4 h = w4_act_rounded(acc[r][t], a.act);
         *reinterpret_cast<u32x2*>((uint16_t*)a.out + w4_tok_off(row, f, a.N)) =
             u32x2{pack_bf16x2(h[0], h[1]), pack_bf16x2(h[2], h[3])};
       } else {
