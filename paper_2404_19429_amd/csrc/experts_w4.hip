@@ -24,6 +24,7 @@ namespace lmoe {
 constexpr int kW4Scan = 1024;      // up to so many choices a block finds its expert's tokens by itself
 constexpr int kW4Tile = 16;        // tokens of one pass over the weights: a matrix instruction's columns
 constexpr int kW4ListThreads = 1024;
+constexpr int kW4Splits = 4;       // of the second product's K, at most
 
 typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
 
@@ -84,12 +85,13 @@ __global__ __launch_bounds__(kW4ListThreads) void w4_list_kernel(const int32_t* 
 struct W4Args {
   const uint8_t *codes, *scales;   // [E][N][K/2], [E][N][K/32]
   const void* in;                  // rows of K: x by token, or the parts of act(W1 x) by choice
-  void* out;                       // FIRST: the parts [parts][n][N] bf16; else float [n][N]
+  void* out;                       // FIRST: the parts [parts][n][N] bf16; else float [splits][n][N]
   const int32_t *idx, *list;
   const W4Tile* tiles;             // null: the blocks find their tokens
   const int32_t* ntiles;
   int32_t N, K, n, k, E, act;
   int32_t by_choice;               // blockIdx.y is a choice, not an expert (fewer choices than experts)
+  int32_t steps;                   // steps of 256 inputs of one split (blocks of 128 rows)
 };
 
 // Eight codes to bfloat16.
@@ -196,6 +198,26 @@ __device__ __forceinline__ void w4_wave_fence() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
+// Rows row .. row + 3 of a choice's product: act of it in parts, or itself.
+template <bool FIRST, int NO>
+__device__ __forceinline__ void w4_out(const W4Args& a, int choice, int row, f32x4 s) {
+  const int64_t off = (int64_t)choice * a.N + row;
+  if constexpr (FIRST) {
+    float h[4] = {s[0], s[1], s[2], s[3]};
+    w4_act(h, a.act);
+#pragma unroll
+    for (int p = 0; p < NO; ++p) {
+      float v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = p + 1 < NO || NO == 3 ? part_of(h[i]) : h[i];   // two parts: the second rounds
+      *reinterpret_cast<u32x2*>((uint16_t*)a.out + (int64_t)p * a.n * a.N + off) =
+          u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+    }
+  } else {
+    *reinterpret_cast<f32x4*>((float*)a.out + (int64_t)blockIdx.z * a.n * a.N + off) = s;
+  }
+}
+
 // Tokens list[0 .. cnt) of one expert, 16 at most, against the block's 16 RT rows; the
 // block's WV waves split K into interleaved steps (w: the wave's first, on its way).
 template <typename T, bool FIRST, int NS, int NO, int RT, int WV, bool FULL>
@@ -269,22 +291,64 @@ __device__ __forceinline__ void w4_tile(const W4Args& a, int cnt, const int32_t*
     f32x4 s = red[wv][lane];
 #pragma unroll
     for (int x = 1; x < WV; ++x) s += red[x * RT + wv][lane];
-    const int64_t off = (int64_t)choice * a.N + row0 + wv * 16 + 4 * q;
-    if constexpr (FIRST) {
-      float h[4] = {s[0], s[1], s[2], s[3]};
-      w4_act(h, a.act);
-#pragma unroll
-      for (int p = 0; p < NO; ++p) {
-        float v[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = p + 1 < NO || NO == 3 ? part_of(h[i]) : h[i];   // two parts: the second rounds
-        *reinterpret_cast<u32x2*>((uint16_t*)a.out + (int64_t)p * a.n * a.N + off) =
-            u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-      }
-    } else {
-      *reinterpret_cast<f32x4*>((float*)a.out + off) = s;
-    }
+    w4_out<FIRST, NO>(a, choice, row0 + wv * 16 + 4 * q, s);
   }
+}
+
+// The block's expert and its tokens: list and their number (0: none, or another block has
+// them).  first() runs as soon as the expert is known.  WV waves; every one ends with the same
+// answer.
+struct W4Found {
+  int e, cnt;
+  const int32_t* list;
+};
+template <int WV, typename F>
+__device__ __forceinline__ W4Found w4_find(const W4Args& a, int32_t (&lists)[kW4Scan], int32_t& found, F first) {
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  W4Found r{-1, 0, lists};
+  if (a.tiles) {
+    if ((int)blockIdx.y >= *a.ntiles) return r;
+    const W4Tile t = a.tiles[blockIdx.y];
+    r.e = t.e;
+    first(r.e);
+    if ((int)threadIdx.x < t.count) lists[threadIdx.x] = a.list[t.first + threadIdx.x];
+    __syncthreads();
+    r.cnt = t.count;
+  } else if (a.n <= kWave) {
+    // Every wave by itself: choice blockIdx.y, if it is the first of its expert, or expert
+    // blockIdx.y.
+    const int my = lane < a.n ? a.idx[lane] : -1;
+    r.e = a.by_choice ? __builtin_amdgcn_readlane(my, (int)blockIdx.y) : (int)blockIdx.y;
+    if (r.e < 0 || r.e >= a.E) return r;
+    const uint64_t same = __ballot(my == r.e);
+    if (same == 0 || (a.by_choice && __builtin_ctzll(same) != (int)blockIdx.y)) return r;
+    first(r.e);
+    int32_t* mine = lists + wv * kWave;
+    if (my == r.e) mine[__popcll(same & ((1ull << lane) - 1))] = lane;
+    r.list = mine;
+    w4_wave_fence();
+    r.cnt = __popcll(same);
+  } else {
+    // The expert's choices, in any order (rows do not mix).  By choice: the first choice
+    // of an expert stands for all of them.  Where nearly every expert has a choice its
+    // weights are fetched ahead of the answer.
+    r.e = a.by_choice ? a.idx[blockIdx.y] : (int)blockIdx.y;
+    if (r.e < 0 || r.e >= a.E) return r;
+    const bool ahead = a.n >= 3 * a.E;
+    if (ahead) first(r.e);
+    if (threadIdx.x == 0) found = 0;
+    __syncthreads();
+    bool earlier = false;
+    for (int i = threadIdx.x; i < a.n; i += 64 * WV)
+      if (a.idx[i] == r.e) {
+        lists[atomicAdd(&found, 1)] = i;
+        earlier |= a.by_choice && i < (int)blockIdx.y;
+      }
+    if (__syncthreads_or(earlier) || found == 0) return r;
+    if (!ahead) first(r.e);
+    r.cnt = found;
+  }
+  return r;
 }
 
 template <typename T, bool FIRST, int NS, int NO, int RT, int WV, bool FULL>
@@ -292,66 +356,155 @@ __global__ __launch_bounds__(64 * WV, 3) void w4_product_kernel(W4Args a) {
   static_assert(RT <= WV, "every 16 rows of the block have a wave that adds them");
   __shared__ W4Lds<RT> lds[WV];
   __shared__ int32_t found, lists[kW4Scan];
-  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-  const int32_t* list = lists;
-  int e, cnt;
+  const int wv = threadIdx.x >> 6;
   W4Step<RT, FULL> w;
-  const uint8_t *codes, *scales;
-  auto weights = [&]() __attribute__((always_inline)) {   // the wave's first step
+  const uint8_t *codes = nullptr, *scales = nullptr;
+  auto weights = [&](int e) __attribute__((always_inline)) {   // the wave's first step
     const int64_t row = (int64_t)e * a.N + blockIdx.x * 16 * RT;
     codes = a.codes + row * (a.K / 2);
     scales = a.scales + row * (a.K / 32);
     if (wv * kStep < a.K) w.load(codes, scales, a.K, wv * kStep);
   };
-  if (a.tiles) {
-    if ((int)blockIdx.y >= *a.ntiles) return;
-    const W4Tile t = a.tiles[blockIdx.y];
-    e = t.e;
-    cnt = t.count;
-    weights();
-    if ((int)threadIdx.x < cnt) lists[threadIdx.x] = a.list[t.first + threadIdx.x];
-    __syncthreads();
-  } else if (a.n <= kWave) {
-    // Every wave by itself: choice blockIdx.y, if it is the first of its expert, or expert
-    // blockIdx.y.
-    const int my = lane < a.n ? a.idx[lane] : -1;
-    e = a.by_choice ? __builtin_amdgcn_readlane(my, (int)blockIdx.y) : (int)blockIdx.y;
-    if (e < 0 || e >= a.E) return;
-    const uint64_t same = __ballot(my == e);
-    if (same == 0 || (a.by_choice && __builtin_ctzll(same) != (int)blockIdx.y)) return;
-    weights();
-    cnt = __popcll(same);
-    int32_t* mine = lists + wv * kWave;
-    if (my == e) mine[__popcll(same & ((1ull << lane) - 1))] = lane;
-    list = mine;
-    w4_wave_fence();
-  } else {
-    // The expert's choices, in any order (rows do not mix).  By choice: the first choice
-    // of an expert stands for all of them.  Where nearly every expert has a choice its
-    // weights are fetched ahead of the answer.
-    e = a.by_choice ? a.idx[blockIdx.y] : (int)blockIdx.y;
-    if (e < 0 || e >= a.E) return;
-    const bool ahead = a.n >= 3 * a.E;
-    if (ahead) weights();
-    if (threadIdx.x == 0) found = 0;
-    __syncthreads();
-    bool earlier = false;
-    for (int i = threadIdx.x; i < a.n; i += 64 * WV)
-      if (a.idx[i] == e) {
-        lists[atomicAdd(&found, 1)] = i;
-        earlier |= a.by_choice && i < (int)blockIdx.y;
-      }
-    if (__syncthreads_or(earlier)) return;
-    cnt = found;
-    if (cnt == 0) return;
-    if (!ahead) weights();
-  }
-  for (int c0 = 0; c0 < cnt; c0 += kW4Tile) {
+  const W4Found f = w4_find<WV>(a, lists, found, weights);
+  for (int c0 = 0; c0 < f.cnt; c0 += kW4Tile) {
     if (c0) {
-      weights();
+      weights(f.e);
       __syncthreads();   // the sums of the tile before have been read
     }
-    w4_tile<T, FIRST, NS, NO, RT, WV, FULL>(a, min(kW4Tile, cnt - c0), list + c0, codes, scales, w, lds);
+    w4_tile<T, FIRST, NS, NO, RT, WV, FULL>(a, min(kW4Tile, f.cnt - c0), f.list + c0, codes, scales, w, lds);
+  }
+}
+
+// ------------------------------------------------------------- blocks of 128 rows
+// Where there are blocks enough, four waves take 32 rows each over the whole K (of
+// blockIdx.z's split), and the tokens' inputs go through LDS once for all of them: with K
+// split over the waves every 16 or 32 rows fetched them anew, four times the weights' bytes.
+constexpr int kRowsBlock = 128;
+template <typename T, bool FIRST, int NS, int NO, bool FULL>
+__global__ __launch_bounds__(256, 2) void w4_rows_kernel(W4Args a) {
+  __shared__ u32x4 wcode[2][kRowsBlock][8];        // [row][piece ^ row % 8]
+  __shared__ u32x2 wsc[2][kRowsBlock];
+  __shared__ u32x4 tok[2][NS][16][32];             // [part][token][piece ^ token % 8]
+  __shared__ int32_t found, lists[kW4Scan];
+  const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int i16 = lane & 15, q = lane >> 4;
+  const int row0 = blockIdx.x * kRowsBlock;
+  const bool on = row0 + 32 * wv < a.N;            // (N is a multiple of 32)
+  const int k0 = blockIdx.z * a.steps * kStep;
+  const int k1 = min(a.K, k0 + a.steps * kStep);
+  const uint8_t *codes = nullptr, *scales = nullptr;
+  u32x4 wreg[4];
+  u32x2 sreg;
+  auto load_w = [&](int col) __attribute__((always_inline)) {
+    const int at = col + (lane & 7) * 32;
+    const bool ok = FULL || at < k1;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const u32x4 v = __builtin_nontemporal_load(
+          reinterpret_cast<const u32x4*>(codes + (int64_t)(8 * i + (lane >> 3)) * (a.K / 2) + (ok ? at : col) / 2));
+      wreg[i] = ok ? v : u32x4{0u, 0u, 0u, 0u};
+    }
+    const uint8_t* p = scales + (int64_t)(lane & 31) * (a.K / 32) + col / 32;
+    if constexpr (FULL) {
+      sreg = *reinterpret_cast<const u32x2*>(p);
+    } else {
+      sreg = u32x2{0x7f7f7f7fu, 0x7f7f7f7fu};
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (col + 32 * i < k1) sreg[i >> 2] = (sreg[i >> 2] & ~(0xffu << (8 * (i & 3)))) | (uint32_t)p[i] << (8 * (i & 3));
+    }
+  };
+  auto first = [&](int e) __attribute__((always_inline)) {   // the wave's rows
+    const int64_t row = (int64_t)e * a.N + (on ? row0 + 32 * wv : 0);
+    codes = a.codes + row * (a.K / 2);
+    scales = a.scales + row * (a.K / 32);
+    load_w(k0);
+  };
+  const W4Found fnd = w4_find<4>(a, lists, found, first);
+  for (int c0 = 0; c0 < fnd.cnt; c0 += kW4Tile) {
+    const int cnt = min(kW4Tile, fnd.cnt - c0);
+    const int32_t* list = fnd.list + c0;
+    if (c0) load_w(k0);
+    // Thread: inputs 8 (tid % 32) .. of tokens tid / 32 and 8 + tid / 32.
+    int64_t src[2];
+    bool has[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int t = 8 * i + (tid >> 5);
+      has[i] = t < cnt;
+      const int choice = list[has[i] ? t : 0];
+      src[i] = (int64_t)(FIRST ? choice / a.k : choice) * a.K;
+    }
+    W4In<T, NS, FIRST> in[2];
+    auto load_t = [&](int col) __attribute__((always_inline)) {
+      const int at = col + 8 * (tid & 31);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (has[i]) in[i].load(a, src[i] + (FULL || at < k1 ? at : col));
+    };
+    auto store = [&](int b, int col) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) wcode[b][32 * wv + 8 * i + (lane >> 3)][(lane & 7) ^ (lane >> 3)] = wreg[i];
+      if (lane < 32) wsc[b][32 * wv + lane] = sreg;
+      const bool ok = FULL || col + 8 * (tid & 31) < k1;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (has[i]) {
+          bf16x8 p[NS];
+          in[i].parts(p);
+          const int t = 8 * i + (tid >> 5);
+#pragma unroll
+          for (int x = 0; x < NS; ++x)   // (weights past K are zeros, but the inputs read in their place may be infinite)
+            tok[b][x][t][(tid & 31) ^ (t & 7)] = ok ? __builtin_bit_cast(u32x4, p[x]) : u32x4{0u, 0u, 0u, 0u};
+        }
+    };
+    f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+    load_t(k0);
+    if (c0) __syncthreads();   // the tile before has been read
+    store(0, k0);
+    __syncthreads();
+    int b = 0;
+    for (int col = k0; col < k1; col += kStep, b ^= 1) {
+      // (After the last step the loads ask for what is there already: a branch around a load
+      // has its results copied, and so waited for, right behind it.)
+      const int after = col + kStep < k1 ? col + kStep : col;
+      load_t(after);
+      load_w(after);
+      __builtin_amdgcn_sched_barrier(0);
+      u32x2 sc[2];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) sc[r] = wsc[b][32 * wv + 16 * r + i16];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (!FULL && col + 128 * h >= k1) break;
+        u32x4 code[2];
+        float s[2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          code[r] = wcode[b][32 * wv + 16 * r + i16][(4 * h + q) ^ (i16 & 7)];
+          s[r] = __uint_as_float(((sc[r][h] >> (8 * q)) & 0xffu) << 23);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          bf16x8 t[NS];
+#pragma unroll
+          for (int x = 0; x < NS; ++x) t[x] = __builtin_bit_cast(bf16x8, tok[b][x][i16][(16 * h + 4 * q + j) ^ (i16 & 7)]);
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const bf16x8 f = w4_frag(code[r][j], s[r]);
+#pragma unroll
+            for (int x = NS - 1; x >= 0; --x) acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, t[x], acc[r], 0, 0, 0);
+          }
+        }
+      }
+      store(b ^ 1, after);
+      __syncthreads();
+    }
+    if (on && i16 < cnt) {
+      const int choice = list[i16];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) w4_out<FIRST, NO>(a, choice, row0 + 32 * wv + 16 * r + 4 * q, acc[r]);
+    }
   }
 }
 
@@ -653,7 +806,6 @@ __global__ __launch_bounds__(256, 2) void w4_gemm_kernel(W4GemmArgs a) {
 
 // The laid-out form serves: bfloat16, whole 128s, and tokens enough.
 constexpr int kGemmFrom = 24;   // choices an expert, on average
-constexpr int kGemmSplits = 4;
 static bool w4_gemm(const moe_w4_cfg& c) {
   return c.dtype == MOE_BF16 && c.d_model % 128 == 0 && c.d_ff % 128 == 0 && c.T * c.k >= (int64_t)kGemmFrom * c.E;
 }
@@ -678,29 +830,41 @@ static W4Ws w4_ws(const moe_w4_cfg& c) {
   w.ntiles = w.tiles + sizeof(W4Tile) * (size_t)w.max_tiles;
   w.parts = up256(w.ntiles + 4);
   w.O = up256(w.parts + std::max((size_t)(bf ? 2 : 3) * n, bf ? (size_t)w.rows : 0) * c.d_ff * 2);
-  w.x = up256(w.O + (size_t)(bf ? kGemmSplits : 1) * n * c.d_model * 4);
+  w.x = up256(w.O + (size_t)kW4Splits * n * c.d_model * 4);
   w.total = up256(w.x + (bf ? (size_t)w.rows * c.d_model * 2 : 0));
   return w;
 }
 size_t experts_w4_ws_bytes(const moe_w4_cfg& c) { return w4_ws(c).total; }
 
-// A product over gy experts or tiles.  More rows a block read its tokens' inputs less
-// often and keep more weights in flight, as long as two blocks a CU are left.
+// A product over gy experts or tiles; the splits it was done in.  Blocks of 128 rows where
+// they reach every CU (the second product's K split to get there); else 16 or 32 rows, as
+// long as two blocks a CU are left, and K split over the waves.
 template <typename T, bool FIRST, int NS, int NO, bool FULL>
-static void launch_w4_rows(const W4Args& a, int gy, hipStream_t s) {
-  const int64_t tiles = (int64_t)(a.N / 16) * gy;
-  const int rt = tiles >= 2 * 2 * num_cus() ? 2 : 1;
+static int launch_w4_rows(W4Args a, int gy, hipStream_t s) {
+  const int cus = num_cus();
+  const int64_t blocks = (int64_t)((a.N + kRowsBlock - 1) / kRowsBlock) * gy;
+  const int steps = (a.K + kStep - 1) / kStep;
+  int splits = FIRST ? 1 : (int)std::min<int64_t>(std::min(kW4Splits, steps), std::max<int64_t>(1, 2 * cus / blocks));
+  a.steps = (steps + splits - 1) / splits;
+  splits = (steps + a.steps - 1) / a.steps;   // whole steps, no split empty
+  if (blocks * splits >= cus) {
+    hipLaunchKernelGGL((w4_rows_kernel<T, FIRST, NS, NO, FULL>), dim3((a.N + kRowsBlock - 1) / kRowsBlock, gy, splits),
+                       dim3(256), 0, s, a);
+    return splits;
+  }
+  const int rt = (int64_t)(a.N / 16) * gy >= 2 * 2 * cus ? 2 : 1;
   auto go = [&](auto kern, int wv) {
     hipLaunchKernelGGL(kern, dim3(a.N / (16 * rt), gy), dim3(64 * wv), 0, s, a);
   };
   const bool deep = a.K > 4 * kStep;   // more than a step for each of four waves
   if (rt == 2) deep ? go(w4_product_kernel<T, FIRST, NS, NO, 2, 8, FULL>, 8) : go(w4_product_kernel<T, FIRST, NS, NO, 2, 4, FULL>, 4);
   else deep ? go(w4_product_kernel<T, FIRST, NS, NO, 1, 8, FULL>, 8) : go(w4_product_kernel<T, FIRST, NS, NO, 1, 4, FULL>, 4);
+  return 1;
 }
 template <typename T, bool FIRST, int NS, int NO>
-static void launch_w4_product(const W4Args& a, int gy, hipStream_t s) {
-  if (a.K % kStep == 0) launch_w4_rows<T, FIRST, NS, NO, true>(a, gy, s);
-  else launch_w4_rows<T, FIRST, NS, NO, false>(a, gy, s);
+static int launch_w4_product(const W4Args& a, int gy, hipStream_t s) {
+  return a.K % kStep == 0 ? launch_w4_rows<T, FIRST, NS, NO, true>(a, gy, s)
+                          : launch_w4_rows<T, FIRST, NS, NO, false>(a, gy, s);
 }
 
 static void launch_w4_gemm(const moe_w4_cfg& c, const void* x, const int32_t* idx, const float* w, const uint8_t* W1c,
@@ -723,8 +887,8 @@ static void launch_w4_gemm(const moe_w4_cfg& c, const void* x, const int32_t* id
   hipLaunchKernelGGL(w4_gemm_kernel<true>, dim3(f / kGemmRows, gy), dim3(256), 0, s, a);
   // K is split where the blocks would not fill the CUs twice; whole steps, no split empty.
   const int steps = (f + kStep - 1) / kStep;
-  const int64_t blocks = (int64_t)(d / kGemmRows) * (std::min<int64_t>(n, c.E) + n / kGemmToks) * 2 / 3;   // (of the bound, about)
-  int splits = (int)std::min<int64_t>(std::min(kGemmSplits, steps), std::max<int64_t>(1, 2 * num_cus() / std::max<int64_t>(1, blocks)));
+  const int64_t blocks = (int64_t)(d / kGemmRows) * c.E * ((n / c.E + kGemmToks - 1) / kGemmToks);   // for an even load
+  int splits = (int)std::min<int64_t>(std::min(kW4Splits, steps), std::max<int64_t>(1, 2 * num_cus() / std::max<int64_t>(1, blocks)));
   const int per = (steps + splits - 1) / splits;
   splits = (steps + per - 1) / per;
   const W4GemmArgs b{W2c, W2s, (const uint16_t*)(base + L.parts), base + L.O, choice_of, tiles, ntiles, d, f, n, c.act, per};
@@ -749,14 +913,15 @@ static void launch_w4_t(const moe_w4_cfg& c, const void* x, const int32_t* idx, 
   else
     tiles = nullptr;
   const int gy = !scan ? L.max_tiles : by_choice ? n : c.E;
-  const W4Args a{W1c, W1s, x, base + L.parts, idx, list, tiles, ntiles, c.d_ff, c.d_model, n, c.k, c.E, c.act, by_choice};
+  const W4Args a{W1c, W1s, x, base + L.parts, idx, list, tiles, ntiles, c.d_ff, c.d_model, n, c.k, c.E, c.act,
+                 by_choice, 0};
   launch_w4_product<T, true, NX, NA>(a, gy, s);
   const W4Args b{W2c, W2s, base + L.parts, base + L.O, idx, list, tiles, ntiles, c.d_model, c.d_ff, n, c.k, c.E, c.act,
-                 by_choice};
-  launch_w4_product<T, false, NA, NA>(b, gy, s);
+                 by_choice, 0};
+  const int splits = launch_w4_product<T, false, NA, NA>(b, gy, s);
   hipLaunchKernelGGL(w4_combine_kernel<T>, dim3((c.d_model + 1023) / 1024, (unsigned)std::min<int64_t>(c.T, 32768)),
                      dim3(256), 0, s,
-                     (const float*)(base + L.O), idx, w, (T*)y, c.T, c.d_model, c.E, c.k, 1);
+                     (const float*)(base + L.O), idx, w, (T*)y, c.T, c.d_model, c.E, c.k, splits);
 }
 
 void launch_experts_w4(const moe_w4_cfg& c, const void* x, const int32_t* idx, const float* w, const uint8_t* W1c,

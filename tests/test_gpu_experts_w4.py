@@ -67,6 +67,23 @@ def test_against_oracle(T, d, f, E, k, dtype):
     check(y, x, idx, w, W, "gelu_tanh", dtype)
 
 
+# Blocks of 128 rows in either product or both: tokens found by expert and by choice, in one
+# wave, in a block and in the list; whole and part steps of 256 inputs, rows that end inside a
+# block, K in one and several splits, more than 16 tokens an expert.
+ROWS = [  # T, d, f, E, k
+    (80, 256, 1024, 48, 2), (40, 160, 1056, 48, 2), (11, 384, 512, 160, 6), (7, 768, 1024, 64, 8), (150, 96, 4128, 8, 2),
+    (90, 4128, 96, 8, 2), (600, 96, 160, 64, 2), (3, 2080, 1312, 16, 16), (24, 1024, 2048, 16, 2)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,d,f,E,k", ROWS)
+def test_blocks_of_rows(T, d, f, E, k, dtype):
+    x, idx, w, W = inputs(T, d, f, E, k, dtype, T + d + E)
+    idx[T // 2, 0] = -1
+    y = run(x.cuda(), dev(idx), dev(w), [dev(v) for v in W], E, f, k, dtype, "gelu_tanh")
+    check(y, x, idx, w, W, "gelu_tanh", dtype)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("act", ["identity", "relu", "gelu_erf"])
 @pytest.mark.parametrize("T", [3, 70])
