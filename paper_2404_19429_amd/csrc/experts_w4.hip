@@ -295,18 +295,21 @@ __device__ __forceinline__ void w4_tile(const W4Args& a, int cnt, const int32_t*
   }
 }
 
-// The block's expert and its tokens: list and their number (0: none, or another block has
-// them).  first() runs as soon as the expert is known.  WV waves; every one ends with the same
-// answer.
+// How a block finds its expert and tokens (blockIdx.y): by the list's tiles; every wave by
+// itself in up to 64 choices (a choice, if it is the first of its expert, or an expert); or the
+// block in up to kW4Scan: by expert, or by choice.
+enum { kFindTiles, kFindWave, kFindExpert, kFindChoice };
+// list and their number (0: none, or another block has them).  first() runs as soon as the
+// expert is known.  WV waves; every one ends with the same answer.
 struct W4Found {
   int e, cnt;
   const int32_t* list;
 };
-template <int WV, typename F>
+template <int HOW, int WV, typename F>
 __device__ __forceinline__ W4Found w4_find(const W4Args& a, int32_t (&lists)[kW4Scan], int32_t& found, F first) {
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
   W4Found r{-1, 0, lists};
-  if (a.tiles) {
+  if constexpr (HOW == kFindTiles) {
     if ((int)blockIdx.y >= *a.ntiles) return r;
     const W4Tile t = a.tiles[blockIdx.y];
     r.e = t.e;
@@ -314,9 +317,7 @@ __device__ __forceinline__ W4Found w4_find(const W4Args& a, int32_t (&lists)[kW4
     if ((int)threadIdx.x < t.count) lists[threadIdx.x] = a.list[t.first + threadIdx.x];
     __syncthreads();
     r.cnt = t.count;
-  } else if (a.n <= kWave) {
-    // Every wave by itself: choice blockIdx.y, if it is the first of its expert, or expert
-    // blockIdx.y.
+  } else if constexpr (HOW == kFindWave) {
     const int my = lane < a.n ? a.idx[lane] : -1;
     r.e = a.by_choice ? __builtin_amdgcn_readlane(my, (int)blockIdx.y) : (int)blockIdx.y;
     if (r.e < 0 || r.e >= a.E) return r;
@@ -329,29 +330,41 @@ __device__ __forceinline__ W4Found w4_find(const W4Args& a, int32_t (&lists)[kW4
     w4_wave_fence();
     r.cnt = __popcll(same);
   } else {
-    // The expert's choices, in any order (rows do not mix).  By choice: the first choice
-    // of an expert stands for all of them.  Where nearly every expert has a choice its
-    // weights are fetched ahead of the answer.
-    r.e = a.by_choice ? a.idx[blockIdx.y] : (int)blockIdx.y;
-    if (r.e < 0 || r.e >= a.E) return r;
-    const bool ahead = a.n >= 3 * a.E;
-    if (ahead) first(r.e);
+    // The expert's choices, in any order (rows do not mix).  By expert most have some, and
+    // the weights are asked for right behind the choices, not behind the answer.
+    constexpr int NI = kW4Scan / (64 * WV);
+    int at[NI];
+#pragma unroll
+    for (int i = 0; i < NI; ++i) at[i] = a.idx[min((int)threadIdx.x + 64 * WV * i, a.n - 1)];
+    r.e = HOW == kFindChoice ? a.idx[blockIdx.y] : (int)blockIdx.y;
+    if (HOW == kFindChoice && (r.e < 0 || r.e >= a.E)) return r;
+    if constexpr (HOW == kFindExpert) {
+      __builtin_amdgcn_sched_barrier(0);
+      first(r.e);
+    }
     if (threadIdx.x == 0) found = 0;
     __syncthreads();
     bool earlier = false;
-    for (int i = threadIdx.x; i < a.n; i += 64 * WV)
-      if (a.idx[i] == r.e) {
-        lists[atomicAdd(&found, 1)] = i;
-        earlier |= a.by_choice && i < (int)blockIdx.y;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int c = threadIdx.x + 64 * WV * i;
+      if (c < a.n && at[i] == r.e) {
+        lists[atomicAdd(&found, 1)] = c;
+        earlier |= c < (int)blockIdx.y;
       }
-    if (__syncthreads_or(earlier) || found == 0) return r;
-    if (!ahead) first(r.e);
+    }
+    if constexpr (HOW == kFindChoice) {   // the first choice of an expert stands for all of them
+      if (__syncthreads_or(earlier)) return r;
+      first(r.e);
+    } else {
+      __syncthreads();
+    }
     r.cnt = found;
   }
   return r;
 }
 
-template <typename T, bool FIRST, int NS, int NO, int RT, int WV, bool FULL>
+template <typename T, bool FIRST, int NS, int NO, int RT, int WV, bool FULL, int HOW>
 __global__ __launch_bounds__(64 * WV, 3) void w4_product_kernel(W4Args a) {
   static_assert(RT <= WV, "every 16 rows of the block have a wave that adds them");
   __shared__ W4Lds<RT> lds[WV];
@@ -365,7 +378,7 @@ __global__ __launch_bounds__(64 * WV, 3) void w4_product_kernel(W4Args a) {
     scales = a.scales + row * (a.K / 32);
     if (wv * kStep < a.K) w.load(codes, scales, a.K, wv * kStep);
   };
-  const W4Found f = w4_find<WV>(a, lists, found, weights);
+  const W4Found f = w4_find<HOW, WV>(a, lists, found, weights);
   for (int c0 = 0; c0 < f.cnt; c0 += kW4Tile) {
     if (c0) {
       weights(f.e);
@@ -380,7 +393,7 @@ __global__ __launch_bounds__(64 * WV, 3) void w4_product_kernel(W4Args a) {
 // blockIdx.z's split), and the tokens' inputs go through LDS once for all of them: with K
 // split over the waves every 16 or 32 rows fetched them anew, four times the weights' bytes.
 constexpr int kRowsBlock = 128;
-template <typename T, bool FIRST, int NS, int NO, bool FULL>
+template <typename T, bool FIRST, int NS, int NO, bool FULL, int HOW>
 __global__ __launch_bounds__(256, 2) void w4_rows_kernel(W4Args a) {
   __shared__ u32x4 wcode[2][kRowsBlock][8];        // [row][piece ^ row % 8]
   __shared__ u32x2 wsc[2][kRowsBlock];
@@ -420,7 +433,7 @@ __global__ __launch_bounds__(256, 2) void w4_rows_kernel(W4Args a) {
     scales = a.scales + row * (a.K / 32);
     load_w(k0);
   };
-  const W4Found fnd = w4_find<4>(a, lists, found, first);
+  const W4Found fnd = w4_find<HOW, 4>(a, lists, found, first);
   for (int c0 = 0; c0 < fnd.cnt; c0 += kW4Tile) {
     const int cnt = min(kW4Tile, fnd.cnt - c0);
     const int32_t* list = fnd.list + c0;
@@ -837,8 +850,8 @@ static W4Ws w4_ws(const moe_w4_cfg& c) {
 size_t experts_w4_ws_bytes(const moe_w4_cfg& c) { return w4_ws(c).total; }
 
 // A product over gy experts or tiles; the splits it was done in.  Blocks of 128 rows where
-// they reach every CU (the second product's K split to get there); else 16 or 32 rows, as
-// long as two blocks a CU are left, and K split over the waves.
+// there are three for two CUs (the second product's K split to get there); else 16 rows, and K
+// split over the waves.
 template <typename T, bool FIRST, int NS, int NO, bool FULL>
 static int launch_w4_rows(W4Args a, int gy, hipStream_t s) {
   const int cus = num_cus();
@@ -847,18 +860,28 @@ static int launch_w4_rows(W4Args a, int gy, hipStream_t s) {
   int splits = FIRST ? 1 : (int)std::min<int64_t>(std::min(kW4Splits, steps), std::max<int64_t>(1, 2 * cus / blocks));
   a.steps = (steps + splits - 1) / splits;
   splits = (steps + a.steps - 1) / a.steps;   // whole steps, no split empty
-  if (blocks * splits >= cus) {
-    hipLaunchKernelGGL((w4_rows_kernel<T, FIRST, NS, NO, FULL>), dim3((a.N + kRowsBlock - 1) / kRowsBlock, gy, splits),
-                       dim3(256), 0, s, a);
+  auto how = [&](auto go) {
+    if (a.tiles) go(std::integral_constant<int, kFindTiles>{});
+    else if (a.n <= kWave) go(std::integral_constant<int, kFindWave>{});
+    else if (a.by_choice) go(std::integral_constant<int, kFindChoice>{});
+    else go(std::integral_constant<int, kFindExpert>{});
+  };
+  if (2 * blocks * splits >= 3 * cus) {
+    how([&](auto h) {
+      hipLaunchKernelGGL((w4_rows_kernel<T, FIRST, NS, NO, FULL, decltype(h)::value>),
+                         dim3((a.N + kRowsBlock - 1) / kRowsBlock, gy, splits), dim3(256), 0, s, a);
+    });
     return splits;
   }
-  const int rt = (int64_t)(a.N / 16) * gy >= 2 * 2 * cus ? 2 : 1;
-  auto go = [&](auto kern, int wv) {
-    hipLaunchKernelGGL(kern, dim3(a.N / (16 * rt), gy), dim3(64 * wv), 0, s, a);
-  };
-  const bool deep = a.K > 4 * kStep;   // more than a step for each of four waves
-  if (rt == 2) deep ? go(w4_product_kernel<T, FIRST, NS, NO, 2, 8, FULL>, 8) : go(w4_product_kernel<T, FIRST, NS, NO, 2, 4, FULL>, 4);
-  else deep ? go(w4_product_kernel<T, FIRST, NS, NO, 1, 8, FULL>, 8) : go(w4_product_kernel<T, FIRST, NS, NO, 1, 4, FULL>, 4);
+  // (Here too little is left to do for 32 rows a block, or four waves, to be worth code of
+  // their own: 16 rows, eight waves where there are steps for them.)
+  const bool deep = a.K > 4 * kStep;
+  how([&](auto h) {
+    constexpr int H = decltype(h)::value;
+    auto go = [&](auto kern, int wv) { hipLaunchKernelGGL(kern, dim3(a.N / 16, gy), dim3(64 * wv), 0, s, a); };
+    if (deep) go(w4_product_kernel<T, FIRST, NS, NO, 1, 8, FULL, H>, 8);
+    else go(w4_product_kernel<T, FIRST, NS, NO, 1, 4, FULL, H>, 4);
+  });
   return 1;
 }
 template <typename T, bool FIRST, int NS, int NO>
