@@ -391,33 +391,36 @@ __global__ __launch_bounds__(64 * WV, 3) void w4_product_kernel(W4Args a) {
 // ------------------------------------------------------------- blocks of 128 rows
 // Where there are blocks enough, four waves take 32 rows each over the whole K (of
 // blockIdx.z's split), and the tokens' inputs go through LDS once for all of them: with K
-// split over the waves every 16 or 32 rows fetched them anew, four times the weights' bytes.
-constexpr int kRowsBlock = 128;
+// split over the waves every 16 or 32 rows fetched them anew, four times the weights' bytes.  (Blocks of 64 rows, twice as many: 48
+// tokens, 16 experts of 1024 x 4096, 12.3 -> 12.0 us for the first product and 14.1 -> 17.0
+// for the second, whose inputs are two parts.  Three steps on their way instead of one: 14.2
+// and 18.3; the registers, and the loads after the last step, cost more than they hide.)
 template <typename T, bool FIRST, int NS, int NO, bool FULL, int HOW>
 __global__ __launch_bounds__(256, 2) void w4_rows_kernel(W4Args a) {
-  __shared__ u32x4 wcode[2][kRowsBlock][8];        // [row][piece ^ row % 8]
-  __shared__ u32x2 wsc[2][kRowsBlock];
+  constexpr int RT = 2, WR = 16 * RT, BR = 4 * WR;   // rows of a wave, of the block
+  __shared__ u32x4 wcode[2][BR][8];        // [row][piece ^ row % 8]
+  __shared__ u32x2 wsc[2][BR];
   __shared__ u32x4 tok[2][NS][16][32];             // [part][token][piece ^ token % 8]
   __shared__ int32_t found, lists[kW4Scan];
   const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int i16 = lane & 15, q = lane >> 4;
-  const int row0 = blockIdx.x * kRowsBlock;
-  const bool on = row0 + 32 * wv < a.N;            // (N is a multiple of 32)
+  const int row0 = blockIdx.x * BR;
+  const bool on = row0 + WR * wv < a.N;            // (N is a multiple of 32)
   const int k0 = blockIdx.z * a.steps * kStep;
   const int k1 = min(a.K, k0 + a.steps * kStep);
   const uint8_t *codes = nullptr, *scales = nullptr;
-  u32x4 wreg[4];
+  u32x4 wreg[2 * RT];
   u32x2 sreg;
   auto load_w = [&](int col) __attribute__((always_inline)) {
     const int at = col + (lane & 7) * 32;
     const bool ok = FULL || at < k1;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 2 * RT; ++i) {
       const u32x4 v = __builtin_nontemporal_load(
           reinterpret_cast<const u32x4*>(codes + (int64_t)(8 * i + (lane >> 3)) * (a.K / 2) + (ok ? at : col) / 2));
       wreg[i] = ok ? v : u32x4{0u, 0u, 0u, 0u};
     }
-    const uint8_t* p = scales + (int64_t)(lane & 31) * (a.K / 32) + col / 32;
+    const uint8_t* p = scales + (int64_t)(lane & (WR - 1)) * (a.K / 32) + col / 32;
     if constexpr (FULL) {
       sreg = *reinterpret_cast<const u32x2*>(p);
     } else {
@@ -428,7 +431,7 @@ __global__ __launch_bounds__(256, 2) void w4_rows_kernel(W4Args a) {
     }
   };
   auto first = [&](int e) __attribute__((always_inline)) {   // the wave's rows
-    const int64_t row = (int64_t)e * a.N + (on ? row0 + 32 * wv : 0);
+    const int64_t row = (int64_t)e * a.N + (on ? row0 + WR * wv : 0);
     codes = a.codes + row * (a.K / 2);
     scales = a.scales + row * (a.K / 32);
     load_w(k0);
@@ -457,8 +460,8 @@ __global__ __launch_bounds__(256, 2) void w4_rows_kernel(W4Args a) {
     };
     auto store = [&](int b, int col) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) wcode[b][32 * wv + 8 * i + (lane >> 3)][(lane & 7) ^ (lane >> 3)] = wreg[i];
-      if (lane < 32) wsc[b][32 * wv + lane] = sreg;
+      for (int i = 0; i < 2 * RT; ++i) wcode[b][WR * wv + 8 * i + (lane >> 3)][(lane & 7) ^ (lane >> 3)] = wreg[i];
+      if (lane < WR) wsc[b][WR * wv + lane] = sreg;
       const bool ok = FULL || col + 8 * (tid & 31) < k1;
 #pragma unroll
       for (int i = 0; i < 2; ++i)
@@ -471,7 +474,9 @@ __global__ __launch_bounds__(256, 2) void w4_rows_kernel(W4Args a) {
             tok[b][x][t][(tid & 31) ^ (t & 7)] = ok ? __builtin_bit_cast(u32x4, p[x]) : u32x4{0u, 0u, 0u, 0u};
         }
     };
-    f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+    f32x4 acc[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) acc[r] = f32x4{0.f, 0.f, 0.f, 0.f};
     load_t(k0);
     if (c0) __syncthreads();   // the tile before has been read
     store(0, k0);
@@ -484,17 +489,17 @@ __global__ __launch_bounds__(256, 2) void w4_rows_kernel(W4Args a) {
       load_t(after);
       load_w(after);
       __builtin_amdgcn_sched_barrier(0);
-      u32x2 sc[2];
+      u32x2 sc[RT];
 #pragma unroll
-      for (int r = 0; r < 2; ++r) sc[r] = wsc[b][32 * wv + 16 * r + i16];
+      for (int r = 0; r < RT; ++r) sc[r] = wsc[b][WR * wv + 16 * r + i16];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         if (!FULL && col + 128 * h >= k1) break;
-        u32x4 code[2];
-        float s[2];
+        u32x4 code[RT];
+        float s[RT];
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          code[r] = wcode[b][32 * wv + 16 * r + i16][(4 * h + q) ^ (i16 & 7)];
+        for (int r = 0; r < RT; ++r) {
+          code[r] = wcode[b][WR * wv + 16 * r + i16][(4 * h + q) ^ (i16 & 7)];
           s[r] = __uint_as_float(((sc[r][h] >> (8 * q)) & 0xffu) << 23);
         }
 #pragma unroll
@@ -503,7 +508,7 @@ __global__ __launch_bounds__(256, 2) void w4_rows_kernel(W4Args a) {
 #pragma unroll
           for (int x = 0; x < NS; ++x) t[x] = __builtin_bit_cast(bf16x8, tok[b][x][i16][(16 * h + 4 * q + j) ^ (i16 & 7)]);
 #pragma unroll
-          for (int r = 0; r < 2; ++r) {
+          for (int r = 0; r < RT; ++r) {
             const bf16x8 f = w4_frag(code[r][j], s[r]);
 #pragma unroll
             for (int x = NS - 1; x >= 0; --x) acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, t[x], acc[r], 0, 0, 0);
@@ -516,7 +521,7 @@ __global__ __launch_bounds__(256, 2) void w4_rows_kernel(W4Args a) {
     if (on && i16 < cnt) {
       const int choice = list[i16];
 #pragma unroll
-      for (int r = 0; r < 2; ++r) w4_out<FIRST, NO>(a, choice, row0 + 32 * wv + 16 * r + 4 * q, acc[r]);
+      for (int r = 0; r < RT; ++r) w4_out<FIRST, NO>(a, choice, row0 + WR * wv + 16 * r + 4 * q, acc[r]);
     }
   }
 }
@@ -850,12 +855,14 @@ static W4Ws w4_ws(const moe_w4_cfg& c) {
 size_t experts_w4_ws_bytes(const moe_w4_cfg& c) { return w4_ws(c).total; }
 
 // A product over gy experts or tiles; the splits it was done in.  Blocks of 128 rows where
-// there are three for two CUs (the second product's K split to get there); else 16 rows, and K
-// split over the waves.
+// there are three for two CUs (the second product's K split to get there); else 16 or 32 rows,
+// two blocks a CU if there are that many, and K split over the waves.  5 float tokens, 15
+// choices, d 736, f 1888: first product 11.1 us with 32 rows and 16.2 with 16; second (270
+// blocks of 128) 13.6 with 16 and 16.3 with 128.
 template <typename T, bool FIRST, int NS, int NO, bool FULL>
 static int launch_w4_rows(W4Args a, int gy, hipStream_t s) {
   const int cus = num_cus();
-  const int64_t blocks = (int64_t)((a.N + kRowsBlock - 1) / kRowsBlock) * gy;
+  const int64_t blocks = (int64_t)((a.N + 127) / 128) * gy;
   const int steps = (a.K + kStep - 1) / kStep;
   int splits = FIRST ? 1 : (int)std::min<int64_t>(std::min(kW4Splits, steps), std::max<int64_t>(1, 2 * cus / blocks));
   a.steps = (steps + splits - 1) / splits;
@@ -868,19 +875,18 @@ static int launch_w4_rows(W4Args a, int gy, hipStream_t s) {
   };
   if (2 * blocks * splits >= 3 * cus) {
     how([&](auto h) {
-      hipLaunchKernelGGL((w4_rows_kernel<T, FIRST, NS, NO, FULL, decltype(h)::value>),
-                         dim3((a.N + kRowsBlock - 1) / kRowsBlock, gy, splits), dim3(256), 0, s, a);
+      hipLaunchKernelGGL((w4_rows_kernel<T, FIRST, NS, NO, FULL, decltype(h)::value>), dim3((a.N + 127) / 128, gy, splits),
+                         dim3(256), 0, s, a);
     });
     return splits;
   }
-  // (Here too little is left to do for 32 rows a block, or four waves, to be worth code of
-  // their own: 16 rows, eight waves where there are steps for them.)
-  const bool deep = a.K > 4 * kStep;
+  const bool deep = a.K > 4 * kStep;   // more than a step for each of four waves
+  const int rt = (int64_t)(a.N / 16) * gy >= 4 * cus ? 2 : 1;
   how([&](auto h) {
     constexpr int H = decltype(h)::value;
-    auto go = [&](auto kern, int wv) { hipLaunchKernelGGL(kern, dim3(a.N / 16, gy), dim3(64 * wv), 0, s, a); };
-    if (deep) go(w4_product_kernel<T, FIRST, NS, NO, 1, 8, FULL, H>, 8);
-    else go(w4_product_kernel<T, FIRST, NS, NO, 1, 4, FULL, H>, 4);
+    auto go = [&](auto kern, int wv) { hipLaunchKernelGGL(kern, dim3(a.N / (16 * rt), gy), dim3(64 * wv), 0, s, a); };
+    if (rt == 2) deep ? go(w4_product_kernel<T, FIRST, NS, NO, 2, 8, FULL, H>, 8) : go(w4_product_kernel<T, FIRST, NS, NO, 2, 4, FULL, H>, 4);
+    else deep ? go(w4_product_kernel<T, FIRST, NS, NO, 1, 8, FULL, H>, 8) : go(w4_product_kernel<T, FIRST, NS, NO, 1, 4, FULL, H>, 4);
   });
   return 1;
 }
