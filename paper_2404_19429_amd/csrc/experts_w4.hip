@@ -150,10 +150,37 @@ template <typename T, int NS, bool FIRST> struct W4In {
 
 // The weights of 16 RT rows x 256 inputs (a step), on their way: lane l has 16-byte piece
 // l % 8 of row l / 8 of every eight rows, and the scales of row l (l < 16 RT).
+// Where K is no multiple of a step the scales' rows have any alignment: lane l then has
+// byte l % 8 of row l / 8 of every eight rows (past K the row's last).
 constexpr int kStep = 256;
+template <int RT, bool FULL> struct W4Scales {
+  u32x2 v;
+  __device__ __forceinline__ void load(const uint8_t* scales, int K, int col) {
+    const int lane = threadIdx.x & 63;
+    v = *reinterpret_cast<const u32x2*>(scales + (int64_t)(lane & (16 * RT - 1)) * (K / 32) + col / 32);
+  }
+  __device__ __forceinline__ void store(u32x2* rows) const {
+    const int lane = threadIdx.x & 63;
+    if (lane < 16 * RT) rows[lane] = v;
+  }
+};
+template <int RT> struct W4Scales<RT, false> {
+  uint8_t v[2 * RT];
+  __device__ __forceinline__ void load(const uint8_t* scales, int K, int col) {
+    const int lane = threadIdx.x & 63;
+    const uint8_t* p = scales + (int64_t)(lane >> 3) * (K / 32) + min(col / 32 + (lane & 7), K / 32 - 1);
+#pragma unroll
+    for (int i = 0; i < 2 * RT; ++i) v[i] = p[(int64_t)8 * i * (K / 32)];
+  }
+  __device__ __forceinline__ void store(u32x2* rows) const {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < 2 * RT; ++i) ((uint8_t*)rows)[64 * i + lane] = v[i];
+  }
+};
 template <int RT, bool FULL> struct W4Step {
   u32x4 code[2 * RT];
-  u32x2 sc;
+  W4Scales<RT, FULL> sc;
   // codes, scales: at the first of the rows; col: the step's first input.
   __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, int K, int col) {
     const int lane = threadIdx.x & 63;
@@ -165,15 +192,7 @@ template <int RT, bool FULL> struct W4Step {
           reinterpret_cast<const u32x4*>(codes + (int64_t)(8 * g + (lane >> 3)) * (K / 2) + (ok ? at : col) / 2));
       code[g] = ok ? v : u32x4{0u, 0u, 0u, 0u};
     }
-    const uint8_t* p = scales + (int64_t)(lane & (16 * RT - 1)) * (K / 32) + col / 32;
-    if constexpr (FULL) {
-      sc = *reinterpret_cast<const u32x2*>(p);
-    } else {
-      sc = u32x2{0x7f7f7f7fu, 0x7f7f7f7fu};
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (col + 32 * i < K) sc[i >> 2] = (sc[i >> 2] & ~(0xffu << (8 * (i & 3)))) | (uint32_t)p[i] << (8 * (i & 3));
-    }
+    sc.load(scales, K, col);
   }
 };
 template <int RT> struct W4Lds {   // a wave's step, turned
@@ -236,7 +255,7 @@ __device__ __forceinline__ void w4_tile(const W4Args& a, int cnt, const int32_t*
     w4_wave_fence();
 #pragma unroll
     for (int g = 0; g < 2 * RT; ++g) mine.code[g >> 1][8 * (g & 1) + (lane >> 3)][(lane & 7) ^ (lane >> 3)] = w.code[g];
-    if (lane < 16 * RT) mine.sc[lane >> 4][lane & 15] = w.sc;
+    w.sc.store(&mine.sc[0][0]);
     w4_wave_fence();
     // The inputs are asked for ahead of the next weights: loads return in order, and a
     // wait for inputs behind them would be a wait for memory.
@@ -410,7 +429,7 @@ __global__ __launch_bounds__(256, 2) void w4_rows_kernel(W4Args a) {
   const int k1 = min(a.K, k0 + a.steps * kStep);
   const uint8_t *codes = nullptr, *scales = nullptr;
   u32x4 wreg[2 * RT];
-  u32x2 sreg;
+  W4Scales<RT, FULL> sreg;
   auto load_w = [&](int col) __attribute__((always_inline)) {
     const int at = col + (lane & 7) * 32;
     const bool ok = FULL || at < k1;
@@ -420,15 +439,7 @@ __global__ __launch_bounds__(256, 2) void w4_rows_kernel(W4Args a) {
           reinterpret_cast<const u32x4*>(codes + (int64_t)(8 * i + (lane >> 3)) * (a.K / 2) + (ok ? at : col) / 2));
       wreg[i] = ok ? v : u32x4{0u, 0u, 0u, 0u};
     }
-    const uint8_t* p = scales + (int64_t)(lane & (WR - 1)) * (a.K / 32) + col / 32;
-    if constexpr (FULL) {
-      sreg = *reinterpret_cast<const u32x2*>(p);
-    } else {
-      sreg = u32x2{0x7f7f7f7fu, 0x7f7f7f7fu};
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (col + 32 * i < k1) sreg[i >> 2] = (sreg[i >> 2] & ~(0xffu << (8 * (i & 3)))) | (uint32_t)p[i] << (8 * (i & 3));
-    }
+    sreg.load(scales, a.K, col);
   };
   auto first = [&](int e) __attribute__((always_inline)) {   // the wave's rows
     const int64_t row = (int64_t)e * a.N + (on ? row0 + WR * wv : 0);
@@ -461,7 +472,7 @@ __global__ __launch_bounds__(256, 2) void w4_rows_kernel(W4Args a) {
     auto store = [&](int b, int col) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < 2 * RT; ++i) wcode[b][WR * wv + 8 * i + (lane >> 3)][(lane & 7) ^ (lane >> 3)] = wreg[i];
-      if (lane < WR) wsc[b][WR * wv + lane] = sreg;
+      sreg.store(&wsc[b][WR * wv]);
       const bool ok = FULL || col + 8 * (tid & 31) < k1;
 #pragma unroll
       for (int i = 0; i < 2; ++i)
