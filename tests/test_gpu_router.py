@@ -114,6 +114,22 @@ def test_scores_one_step_apart():
         check(l, 4, np.full(E, 0.3, np.float32), score=score, groups=4, top_groups=2)
 
 
+@pytest.mark.parametrize("E", [4, 5, 16, 60, 64, 128, 200, 512])
+def test_single_live_expert_and_zeros(E):
+    """One expert left (its logit 0, its value 0 and just beside it), wherever it stands."""
+    l = np.full((E, E), -np.inf, np.float32)
+    l[np.arange(E), np.arange(E)] = 0.0
+    for score in ("softmax", "sigmoid"):
+        check(l, min(E, 3), score=score)
+        check(l, min(E, 3), np.full(E, -1.0 if score == "softmax" else -0.5, np.float32), score=score)   # values exactly 0
+        if E % 4 == 0:
+            check(l, 1, np.full(E, -0.5, np.float32), score=score, groups=E // 4 if E // 4 <= 16 else 4, top_groups=1)
+    l = np.zeros((3, E), np.float32)
+    l[1] = np.float32(1e-42) * np.arange(E)
+    l[2] = -l[1]
+    check(l, min(E, 4))
+
+
 def test_load_is_added_and_counts_every_choice():
     l = make_logits(4099, 48, 5)
     c = L.make_route_cfg(4099, 48, 4)
