@@ -316,7 +316,7 @@ typedef struct {
  *   load [E] int32 or NULL: the number of choices of each expert is ADDED to it (a
  *   caller clears it once and counts over as many calls as its bias update spans).
  *   The values c are compared as doubles: the choice is that of an evaluation in
- *   64 bits. */
+ *   64 bits.  No output may alias another array. */
 moe_status moe_route(const moe_route_cfg* cfg, const float* logits, const float* bias, int32_t* idx, float* w,
                      int32_t* load, moe_stream_t stream);
 
@@ -347,7 +347,7 @@ moe_status moe_bwd_dx_route(const moe_cfg* cfg, const moe_route_cfg* route, cons
 
 /* The experts' FFNs on weights held in 4 bits, for serving: tokens are gathered by
  * the router's choices inside the products and summed with its weights, without
- * capacity, send buffers or drops; meant for one token up to a short prompt.
+ * capacity, send buffers or drops, from one token up to a prompt's many.
  * A weight matrix [N][K] (out, in; K a multiple of 32) is
  *   codes [N][K/2] uint8: input 2j in the low, 2j + 1 in the high half of byte j; a
  *     code is a sign (8) and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6;
@@ -366,7 +366,8 @@ typedef struct {
 /* n_rows rows of K floats or bfloat16 (dtype) -> codes and scales.  The scale is the
  * smallest power of two 2^s, -100 <= s <= 125, with max|group| <= 7 * 2^s, so every
  * weight is off by at most half the codes' spacing at its place (nearest code, ties to
- * the even mantissa; past 7 * 2^125 the largest code); a group with an infinite or NaN weight gets the scale byte 255. */
+ * the even mantissa; past 7 * 2^125 the largest code); a group with an infinite or
+ * NaN weight gets the scale byte 255. */
 moe_status moe_w4_quantize(int64_t n_rows, int32_t K, int32_t dtype, const void* W, uint8_t* codes,
                            uint8_t* scales, moe_stream_t stream);
 
@@ -380,8 +381,10 @@ size_t moe_experts_w4_workspace_bytes(const moe_w4_cfg* cfg);
  *   scales [E][f][d/32], W2 codes [E][d][f/2] and scales [E][d][f/32].
  *   Sums in float over products exact in bfloat16 factors: x is bfloat16, or its
  *   three bfloat16 parts (MOE_F32); act(W1 x) two (three) such parts, so that only y
- *   is rounded to its type.  The same call gives the same bits.  Tokens do not mix;
- *   the order of a token's sums depends on T, d and f only.
+ *   is rounded to its type.  Many tokens (MOE_BF16, d_model and d_ff multiples of 128,
+ *   T * k >= 24 E): act(W1 x) is rounded once, to bfloat16, as by moe_expert_ffn_fwd.
+ *   The same call gives the same bits.  Tokens do not mix; the order of a token's sums
+ *   depends on cfg only.
  *   ws: moe_experts_w4_workspace_bytes(cfg) bytes.  Calls that overlap in time need
  *   separate workspaces. */
 moe_status moe_experts_w4(const moe_w4_cfg* cfg, const void* x, const int32_t* idx, const float* w,

@@ -393,6 +393,12 @@ moe_status moe_route(const moe_route_cfg* cfg, const float* logits, const float*
   const char* fn = "moe_route";
   CHECK(check_route(cfg, fn));
   REQUIRE_TPTR(logits); OPTIONAL_PTR(bias); REQUIRE_TPTR(idx); REQUIRE_TPTR(w); OPTIONAL_PTR(load);
+  const void* out[3] = {idx, w, load};
+  for (int i = 0; i < 3 && cfg->T > 0; ++i) {
+    bool twice = out[i] != nullptr && (out[i] == logits || out[i] == bias);
+    for (int j = 0; j < i; ++j) twice = twice || (out[i] != nullptr && out[i] == out[j]);
+    if (twice) return fail(MOE_EINVAL, "%s: an output may not alias another array", fn);
+  }
   CHECK(check_device(fn));
   lmoe::launch_route(*cfg, logits, bias, idx, w, load, (hipStream_t)stream);
   return check_launch(fn);

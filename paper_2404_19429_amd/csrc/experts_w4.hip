@@ -25,6 +25,7 @@ constexpr int kW4Scan = 1024;      // up to so many choices a block finds its ex
 constexpr int kW4Tile = 16;        // tokens of one pass over the weights: a matrix instruction's columns
 constexpr int kW4ListThreads = 1024;
 constexpr int kW4Splits = 4;       // of the second product's K, at most
+constexpr int kMaxGridY = 65535;
 
 typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
 
@@ -92,6 +93,7 @@ struct W4Args {
   int32_t N, K, n, k, E, act;
   int32_t by_choice;               // blockIdx.y is a choice, not an expert (fewer choices than experts)
   int32_t steps;                   // steps of 256 inputs of one split (blocks of 128 rows)
+  int32_t tile0;                   // the tile of blockIdx.y 0
 };
 
 // Eight codes to bfloat16.
@@ -329,8 +331,9 @@ __device__ __forceinline__ W4Found w4_find(const W4Args& a, int32_t (&lists)[kW4
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
   W4Found r{-1, 0, lists};
   if constexpr (HOW == kFindTiles) {
-    if ((int)blockIdx.y >= *a.ntiles) return r;
-    const W4Tile t = a.tiles[blockIdx.y];
+    const int tile = a.tile0 + blockIdx.y;
+    if (tile >= *a.ntiles) return r;
+    const W4Tile t = a.tiles[tile];
     r.e = t.e;
     first(r.e);
     if ((int)threadIdx.x < t.count) lists[threadIdx.x] = a.list[t.first + threadIdx.x];
@@ -415,7 +418,7 @@ __global__ __launch_bounds__(64 * WV, 3) void w4_product_kernel(W4Args a) {
 // for the second, whose inputs are two parts.  Three steps on their way instead of one: 14.2
 // and 18.3; the registers, and the loads after the last step, cost more than they hide.)
 template <typename T, bool FIRST, int NS, int NO, bool FULL, int HOW>
-__global__ __launch_bounds__(256, 2) void w4_rows_kernel(W4Args a) {
+__global__ __launch_bounds__(256, NS == 3 ? 1 : 2) void w4_rows_kernel(W4Args a) {
   constexpr int RT = 2, WR = 16 * RT, BR = 4 * WR;   // rows of a wave, of the block
   __shared__ u32x4 wcode[2][BR][8];        // [row][piece ^ row % 8]
   __shared__ u32x2 wsc[2][BR];
@@ -833,7 +836,11 @@ __global__ __launch_bounds__(256, 2) void w4_gemm_kernel(W4GemmArgs a) {
   }
 }
 
-// The laid-out form serves: bfloat16, whole 128s, and tokens enough.
+// The laid-out form serves: bfloat16, whole 128s, and tokens enough.  Its time hardly
+// grows with the tokens, the other form's does with every 16 of an expert; whole call, us,
+// other form against this one, by choices an expert: 16 experts of 1024 x 4096, 16: 48.5
+// and 54.0, 24: 54.9 and 55.0, 32: 70.2 and 56.6; 64 experts of 2048 x 1408, 18: 109.7 and
+// 114.5, 24: 118.8 and 117.5, 36: 158.4 and 124.4.
 constexpr int kGemmFrom = 24;   // choices an expert, on average
 static bool w4_gemm(const moe_w4_cfg& c) {
   return c.dtype == MOE_BF16 && c.d_model % 128 == 0 && c.d_ff % 128 == 0 && c.T * c.k >= (int64_t)kGemmFrom * c.E;
@@ -885,10 +892,11 @@ static int launch_w4_rows(W4Args a, int gy, hipStream_t s) {
     else go(std::integral_constant<int, kFindExpert>{});
   };
   if (2 * blocks * splits >= 3 * cus) {
-    how([&](auto h) {
-      hipLaunchKernelGGL((w4_rows_kernel<T, FIRST, NS, NO, FULL, decltype(h)::value>), dim3((a.N + 127) / 128, gy, splits),
-                         dim3(256), 0, s, a);
-    });
+    for (; a.tile0 < gy; a.tile0 += kMaxGridY)   // (only a list's tiles pass the grid's limit)
+      how([&](auto h) {
+        hipLaunchKernelGGL((w4_rows_kernel<T, FIRST, NS, NO, FULL, decltype(h)::value>),
+                           dim3((a.N + 127) / 128, std::min(kMaxGridY, gy - a.tile0), splits), dim3(256), 0, s, a);
+      });
     return splits;
   }
   const bool deep = a.K > 4 * kStep;   // more than a step for each of four waves
@@ -954,10 +962,10 @@ static void launch_w4_t(const moe_w4_cfg& c, const void* x, const int32_t* idx, 
     tiles = nullptr;
   const int gy = !scan ? L.max_tiles : by_choice ? n : c.E;
   const W4Args a{W1c, W1s, x, base + L.parts, idx, list, tiles, ntiles, c.d_ff, c.d_model, n, c.k, c.E, c.act,
-                 by_choice, 0};
+                 by_choice, 0, 0};
   launch_w4_product<T, true, NX, NA>(a, gy, s);
   const W4Args b{W2c, W2s, base + L.parts, base + L.O, idx, list, tiles, ntiles, c.d_model, c.d_ff, n, c.k, c.E, c.act,
-                 by_choice, 0};
+                 by_choice, 0, 0};
   const int splits = launch_w4_product<T, false, NA, NA>(b, gy, s);
   hipLaunchKernelGGL(w4_combine_kernel<T>, dim3((c.d_model + 1023) / 1024, (unsigned)std::min<int64_t>(c.T, 32768)),
                      dim3(256), 0, s,

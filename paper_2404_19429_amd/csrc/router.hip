@@ -5,7 +5,7 @@
 // one of any other evaluation in 64 bits, two values of a token closer than 1e-15 aside).
 // Doubles for every expert would bound the kernel, so tokens are routed in float first:
 // a team of 4 or 16 lanes holds a token's row, and every step that compares two values
-// also sees whether they are too close for float to tell (kRouteEps, above the sum of
+// also sees whether they are too close for float to tell (route_eps, above the sum of
 // the errors).  Such a token (a few in a thousand of ordinary logits; all of them where
 // logits tie) goes the exact way, one wavefront for the token in double.
 #include <utility>
@@ -186,11 +186,16 @@ __device__ __forceinline__ void route_exact(const RouteArgs& a, int64_t t, Route
 constexpr float kRouteMasked = -3e38f;    // a masked expert's value; every other is clamped to +-1e30
 constexpr float kRouteNone = -2e38f;      // below: masked
 constexpr float kRouteFar = 1e30f;
-// Two values are told apart if they differ by more than kRouteEps max(1, |value|): each
-// is off by at most 2^-19 of its size for the element number in its low bits, and by
-// 1.2e-6 for the score (v_exp_f32 and v_rcp_f32 of 1 ulp each, the rounded argument of
-// the exponential, the sum of the softmax, + b): 2 * (1.9e-6 + 1.2e-6) < 8e-6.
-constexpr float kRouteEps = 8e-6f;
+// Two values of a row held NV a lane are told apart if they differ by more than
+// route_eps(NV) max(1, |value|): the element numbers in their low bits move each by at most
+// (NV - 1) 2^-23 of its size; the sum of a softmax (NV - 1 additions of a lane, 4 of the
+// team) moves their difference, 1 at most, by (NV + 3) 2^-24; and 1e-6 is for the scores by
+// themselves (2 * 4.1e-7: v_exp_f32 and v_rcp_f32 of 1 ulp each, the rounded argument of the
+// exponential, the product, + b).
+constexpr float route_eps(int nv) { return (float)(5 * nv - 1) * 0x1p-24f + 1e-6f; }
+// Two groups, sums of two values: 15 2^-22 each for the lane's number in the low bits,
+// 2^-23 for the sum, and as above for four scores in 32 a lane: 1.12e-5.
+constexpr float kRouteGroupEps = 1.25e-5f;
 constexpr int kRouteGroupsFast = 16;      // one lane of a team for each group
 constexpr int kRouteWaves = 8;            // per block
 
@@ -397,7 +402,7 @@ __global__ __launch_bounds__(64 * kRouteWaves) void route_kernel(RouteArgs a) {
       }
       const float gv = x > kRouteNone ? (y > kRouteNone ? x + y : x) : kRouteMasked;
       const float big = x > kRouteNone ? fmaxf(fabsf(x), y > kRouteNone ? fabsf(y) : 0.f) : 0.f;
-      const float eps = 2.f * kRouteEps * fmaxf(1.f, from_order_key(team_max<LPT>(order_key(big))));
+      const float eps = kRouteGroupEps * fmaxf(1.f, from_order_key(team_max<LPT>(order_key(big))));
       // The best groups one after the other (the lane in the low bits keeps them apart).
       const int gk = j < a.groups ? (order_key(gv) & ~15) | (15 - j) : (int)0x80000000;
       int rest = gk, last = 0;
@@ -452,7 +457,7 @@ __global__ __launch_bounds__(64 * kRouteWaves) void route_kernel(RouteArgs a) {
       const int before = q == 0 ? team_before<LPT>(kept_key[0])
                                 : j == 0 ? team_before<LPT>(kept_key[q > 0 ? q - 1 : 0]) : team_before<LPT>(kept_key[q]);
       const float x = from_order_key(kept_key[q]), p = from_order_key(before);
-      amb |= r >= 1 && r <= k && x > kRouteNone && p - x <= kRouteEps * fmaxf(1.f, fabsf(p));
+      amb |= r >= 1 && r <= k && x > kRouteNone && p - x <= route_eps(NV) * fmaxf(1.f, fabsf(p));
       amb |= r <= k && x > kRouteNone && __popc(kept_at[q] & (LPT == 16 ? 0xffffu : 0xfu)) > 1;   // two alike
     }
     float s[NM], sum = 0.f;

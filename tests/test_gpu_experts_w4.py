@@ -223,6 +223,41 @@ def test_same_bits_again_and_in_a_used_workspace():
     assert torch.equal(run(*a, ws=ws, stream=s), first)
 
 
+def test_two_calls_at_once():
+    """Two streams, a workspace each, the same weights; results as one after the other."""
+    for T, d, f, E, k in ((6, 256, 512, 8, 2), (90, 128, 160, 7, 3), (200, 256, 384, 4, 2)):
+        x, idx, w, W = inputs(T, d, f, E, k, "bf16", T)
+        Wd = [dev(v) for v in W]
+        sets = [(x.cuda(), dev(idx), dev(w)), (x.flip(0).contiguous().cuda(), dev(idx[::-1]), dev(w[::-1]))]
+        want = [run(a, i, v, Wd, E, f, k, "bf16", "relu") for a, i, v in sets]
+        c = L.make_w4_cfg(T, d, f, E, k, "bf16", "relu")
+        ws = [torch.empty(L.moe_experts_w4_workspace_bytes(c), dtype=torch.uint8, device="cuda") for _ in sets]
+        ys = [[torch.empty_like(v) for _ in range(8)] for v in want]
+        streams = [torch.cuda.Stream() for _ in sets]
+        torch.cuda.synchronize()
+        for j in range(8):
+            for (a, i, v), y, u, s in zip(sets, ys, ws, streams):
+                L.moe_experts_w4(c, a, i, v, *Wd, y[j], u, stream=s)
+        torch.cuda.synchronize()
+        assert all(torch.equal(y, r) for r, l in zip(want, ys) for y in l), T
+
+
+@pytest.mark.parametrize("T,k", [(2 ** 21, 1), (2 ** 17, 16)])
+def test_most_choices(T, k):
+    """T * k = 2^21 in tiles of 16: more blocks down than a grid may have.  Token t is row t % 8 of x."""
+    d = f = 32
+    E = 2
+    x, idx, w, W = inputs(8, d, f, E, k, "f32", 3, np.array([0.6, 0.4]))
+    idx[5] = -1
+    ref, err = O.experts(x.double().numpy(), idx, w.astype(np.float64), O.w4_decode(W[0], W[1]), O.w4_decode(W[2], W[3]), "relu", 2.0 ** -16)
+    n = T // 8
+    y = run(x.cuda().repeat(n, 1), dev(idx).repeat(n, 1), dev(w).repeat(n, 1), [dev(v) for v in W], E, f, k, "f32", "relu")
+    y = y.view(n, 8, d)
+    assert torch.equal(y, y[:1].expand_as(y))
+    tol = err + 2.0 ** -24 * (np.abs(ref) + err)
+    assert (np.abs(y[0].double().cpu().numpy() - ref) <= tol).all()
+
+
 def test_empty_batch():
     W = [dev(v) for v in (*weights(2, 64, 32, np.random.default_rng(0)), *weights(2, 32, 64, np.random.default_rng(1)))]
     x = torch.empty(0, 32, dtype=torch.bfloat16, device="cuda")

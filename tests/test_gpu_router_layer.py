@@ -89,6 +89,29 @@ def test_training_step_with_router_and_checkpoint(route, dtype):
         assert_close(n, getattr(b, n).double().cpu().numpy(), v, TOL[dtype])
 
 
+@pytest.mark.parametrize("routing", ["token", "bpr"])
+@pytest.mark.parametrize("route", [dict(score="sigmoid"), dict(score="softmax", renorm=0), dict(score="softmax")])
+def test_choices_left_open_take_no_part(route, routing):
+    """Two live experts (the others' bias is -inf) for three choices: the third is -1 throughout the layer."""
+    cfg, b, t, r = build("bf16", 90, 128, 128, 8, 3, 17, cf=(3, 1), **route)
+    r.bias.fill_(float("-inf"))
+    r.bias[[2, 7]] = 0.0
+    L.layer_forward(b, t["x"], t["Wg"], None, t["W1"], t["W2"], routing=routing, router=r)
+    torch.cuda.synchronize()
+    idx, slot = b.idx.cpu().numpy(), b.slot.cpu().numpy()
+    assert (np.sort(idx, 1) == [-1, 2, 7]).all() and (idx[:, 2] == -1).all()
+    assert (slot[:, 2] < 0).all() and (slot[:, :2] >= 0).all() and (b.w[:, 2] == 0).all()
+    O_, w = ebuf(b, "O").astype(np.float64), b.w.double().cpu().numpy()
+    y = sum(w[:, r_, None] * O_[idx[:, r_], slot[:, r_]] for r_ in (0, 1))
+    assert_close("y", b.y.double().cpu().numpy(), y, TOL["bf16"])
+    L.layer_backward(b, t["x"], t["Wg"], t["dy"], router=r)
+    torch.cuda.synchronize()
+    ref = reference(cfg, b, t, (route["score"], route.get("renorm", 1), 1.0))
+    assert (b.dw[:, 2] == 0).all()
+    for n, v in ref.items():
+        assert_close(n, getattr(b, n).double().cpu().numpy(), v, TOL["bf16"])
+
+
 def test_softmax_router_is_the_gate():
     """Without bias and groups the router is moe_gate_topk, and its backward moe_bwd_dx's."""
     for renorm in (0, 1):

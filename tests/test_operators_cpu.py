@@ -159,6 +159,8 @@ def test_route_pointers():
     assert route(c) == L.MOE_EDEVICE and route(c, bias=P(5), load=P(6)) == L.MOE_EDEVICE   # valid; no GPU here
     assert route(c, logits=None) == L.MOE_EINVAL and "logits is NULL" in L.moe_last_error()
     assert route(c, idx=P(1) + 4) == L.MOE_EALIGN and route(c, load=8) == L.MOE_EALIGN
+    for kw in (dict(w=P(0)), dict(idx=P(0)), dict(idx=P(2)), dict(bias=P(5), w=P(5)), dict(load=P(1)), dict(bias=P(5), load=P(5))):
+        assert route(c, **kw) == L.MOE_EINVAL and "alias" in L.moe_last_error(), kw
     z = rcfg(T=0)
     assert route(z, logits=None, idx=None, w=None) == L.MOE_EDEVICE
     assert lib.moe_route_bwd(ctypes.byref(c), P(0), P(1), P(2), P(3), P(0), None) == L.MOE_EINVAL
