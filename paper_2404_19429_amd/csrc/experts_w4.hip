@@ -1,4 +1,4 @@
-// The experts' FFNs on 4-bit weights for a few tokens, and the weights' quantiser.
+// The experts' FFNs on 4-bit weights, from one token on, and the weights' quantiser.
 //
 // y_t = sum_r w_tr W2_e act(W1_e x_t).  With n = T k choices, two products over the
 // chosen experts (act(W1 x) of every choice goes through the workspace) and a sum over
@@ -10,7 +10,7 @@
 // A matrix instruction wants lane (i = lane & 15, q = lane >> 4) to hold row i, and 16
 // rows are 16 cache lines: loads straight into that order are bound by the L1's line
 // look-ups (64 per load; measured, 48 tokens against 16 experts of 1024 x 4096: 19 + 26
-// us where 36 + 36 MB take 14).  So a wave loads 8 rows x 256 inputs at a time, whole
+// us where 36 + 36 MB take 14, and the two products take 12.3 + 13.6 now).  So a wave loads 8 rows x 256 inputs at a time, whole
 // 128-byte lines, and turns them in LDS.  Of a row's 256 inputs lane q gets 32 q ..
 // 32 q + 31 of each half, one scale group; MFMA j of a half takes inputs 8 j .. 8 j + 7
 // of these from weights and tokens alike, so the product's k-index stands for the same
@@ -21,11 +21,16 @@
 
 namespace lmoe {
 
-constexpr int kW4Scan = 1024;      // up to so many choices a block finds its expert's tokens by itself
+// Up to so many choices a block finds its expert's tokens by itself, past that a launch sorts
+// them (whole calls, us, by itself and sorted: 64 experts of 1024 x 2048, 400 choices 48.5 and
+// 52.8, 640 62.7 and 66.9, 1000 78.6 and 76.0; 16 of 736 x 512, 720 29.3 and 28.6, 1000 37.6
+// and 29.5: the tiles of an expert with many tokens are then blocks of their own).
+constexpr int kW4Scan = 640;
 constexpr int kW4Tile = 16;        // tokens of one pass over the weights: a matrix instruction's columns
 constexpr int kW4ListThreads = 1024;
 constexpr int kW4Splits = 4;       // of the second product's K, at most
 constexpr int kMaxGridY = 65535;
+constexpr int kW4Waves = 8, kW4PerSimd = 3;   // of a block that splits K over waves, at most; of a SIMD, by registers
 
 typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
 
@@ -107,10 +112,12 @@ __device__ __forceinline__ bf16x8 w4_frag(uint32_t c, float s) {
 }
 
 // A float's leading eight significand bits (truncated: never past the largest
-// bfloat16), and what is left of it; of an infinity nothing is left.
+// bfloat16), and what is left of it; of an infinity nothing is left (what is left of a
+// finite value or NaN is none).
+template <bool FINITE = false>
 __device__ __forceinline__ float part_of(float& v) {
   const float h = __uint_as_float(__float_as_uint(v) & 0xffff0000u);
-  v = h == v ? 0.f : v - h;
+  v = !FINITE && h == v ? 0.f : v - h;
   return h;
 }
 
@@ -137,7 +144,7 @@ template <typename T, int NS, bool FIRST> struct W4In {
         float lo = __uint_as_float(raw[i >> 1][(2 * i) & 3]), hi = __uint_as_float(raw[i >> 1][(2 * i + 1) & 3]);
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
-          const float l = part_of(lo), h = part_of(hi);
+          const float l = s == 0 ? part_of(lo) : part_of<true>(lo), h = s == 0 ? part_of(hi) : part_of<true>(hi);
           r[s][i] = (__float_as_uint(l) >> 16) | __float_as_uint(h);
         }
       }
@@ -240,9 +247,9 @@ __device__ __forceinline__ void w4_out(const W4Args& a, int choice, int row, f32
 }
 
 // Tokens list[0 .. cnt) of one expert, 16 at most, against the block's 16 RT rows; the
-// block's WV waves split K into interleaved steps (w: the wave's first, on its way).
-template <typename T, bool FIRST, int NS, int NO, int RT, int WV, bool FULL>
-__device__ __forceinline__ void w4_tile(const W4Args& a, int cnt, const int32_t* list, const uint8_t* codes,
+// block's waves split K into interleaved steps (w: the wave's first, on its way).
+template <typename T, bool FIRST, int NS, int NO, int RT, bool FULL>
+__device__ __forceinline__ void w4_tile(const W4Args& a, int waves, int cnt, const int32_t* list, const uint8_t* codes,
                                         const uint8_t* scales, W4Step<RT, FULL>& w, W4Lds<RT>* lds) {
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
   const int i16 = lane & 15, q = lane >> 4;
@@ -253,7 +260,7 @@ __device__ __forceinline__ void w4_tile(const W4Args& a, int cnt, const int32_t*
   for (int r = 0; r < RT; ++r) acc[r] = f32x4{0.f, 0.f, 0.f, 0.f};
   const int choice = list[min(i16, cnt - 1)];   // columns past the count repeat the last
   const int64_t in_off = (int64_t)(FIRST ? choice / a.k : choice) * a.K;
-  for (int col = wv * kStep; col < a.K; col += WV * kStep) {
+  for (int col = wv * kStep; col < a.K; col += waves * kStep) {
     w4_wave_fence();
 #pragma unroll
     for (int g = 0; g < 2 * RT; ++g) mine.code[g >> 1][8 * (g & 1) + (lane >> 3)][(lane & 7) ^ (lane >> 3)] = w.code[g];
@@ -269,7 +276,7 @@ __device__ __forceinline__ void w4_tile(const W4Args& a, int cnt, const int32_t*
       for (int j = 0; j < 4; ++j) in[h][j].load(a, in_off + (FULL || at < a.K ? at : col) + 8 * j);
     }
     __builtin_amdgcn_sched_barrier(0);
-    if (col + WV * kStep < a.K) w.load(codes, scales, a.K, col + WV * kStep);
+    if (col + waves * kStep < a.K) w.load(codes, scales, a.K, col + waves * kStep);
     __builtin_amdgcn_sched_barrier(0);
     u32x2 sc[RT];
 #pragma unroll
@@ -309,9 +316,12 @@ __device__ __forceinline__ void w4_tile(const W4Args& a, int cnt, const int32_t*
   for (int r = 0; r < RT; ++r) red[wv * RT + r][lane] = acc[r];
   __syncthreads();
   if (wv < RT && i16 < cnt) {
-    f32x4 s = red[wv][lane];
+    f32x4 v[kW4Waves];
 #pragma unroll
-    for (int x = 1; x < WV; ++x) s += red[x * RT + wv][lane];
+    for (int x = 0; x < kW4Waves; ++x) v[x] = red[min(x, waves - 1) * RT + wv][lane];
+    f32x4 s = v[0];
+#pragma unroll
+    for (int x = 1; x < kW4Waves; ++x) s = x < waves ? s + v[x] : s;
     w4_out<FIRST, NO>(a, choice, row0 + wv * 16 + 4 * q, s);
   }
 }
@@ -321,13 +331,13 @@ __device__ __forceinline__ void w4_tile(const W4Args& a, int cnt, const int32_t*
 // block in up to kW4Scan: by expert, or by choice.
 enum { kFindTiles, kFindWave, kFindExpert, kFindChoice };
 // list and their number (0: none, or another block has them).  first() runs as soon as the
-// expert is known.  WV waves; every one ends with the same answer.
+// expert is known.  Four or eight waves; every one ends with the same answer.
 struct W4Found {
   int e, cnt;
   const int32_t* list;
 };
-template <int HOW, int WV, typename F>
-__device__ __forceinline__ W4Found w4_find(const W4Args& a, int32_t (&lists)[kW4Scan], int32_t& found, F first) {
+template <int HOW, typename F>
+__device__ __forceinline__ W4Found w4_find(const W4Args& a, int waves, int32_t (&lists)[kW4Scan], int32_t& found, F first) {
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
   W4Found r{-1, 0, lists};
   if constexpr (HOW == kFindTiles) {
@@ -354,10 +364,10 @@ __device__ __forceinline__ W4Found w4_find(const W4Args& a, int32_t (&lists)[kW4
   } else {
     // The expert's choices, in any order (rows do not mix).  By expert most have some, and
     // the weights are asked for right behind the choices, not behind the answer.
-    constexpr int NI = kW4Scan / (64 * WV);
+    constexpr int NI = (kW4Scan + 255) / 256;
     int at[NI];
 #pragma unroll
-    for (int i = 0; i < NI; ++i) at[i] = a.idx[min((int)threadIdx.x + 64 * WV * i, a.n - 1)];
+    for (int i = 0; i < NI; ++i) at[i] = a.idx[min((int)threadIdx.x + 64 * waves * i, a.n - 1)];
     r.e = HOW == kFindChoice ? a.idx[blockIdx.y] : (int)blockIdx.y;
     if (HOW == kFindChoice && (r.e < 0 || r.e >= a.E)) return r;
     if constexpr (HOW == kFindExpert) {
@@ -369,7 +379,7 @@ __device__ __forceinline__ W4Found w4_find(const W4Args& a, int32_t (&lists)[kW4
     bool earlier = false;
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-      const int c = threadIdx.x + 64 * WV * i;
+      const int c = threadIdx.x + 64 * waves * i;
       if (c < a.n && at[i] == r.e) {
         lists[atomicAdd(&found, 1)] = c;
         earlier |= c < (int)blockIdx.y;
@@ -386,12 +396,12 @@ __device__ __forceinline__ W4Found w4_find(const W4Args& a, int32_t (&lists)[kW4
   return r;
 }
 
-template <typename T, bool FIRST, int NS, int NO, int RT, int WV, bool FULL, int HOW>
-__global__ __launch_bounds__(64 * WV, 3) void w4_product_kernel(W4Args a) {
-  static_assert(RT <= WV, "every 16 rows of the block have a wave that adds them");
-  __shared__ W4Lds<RT> lds[WV];
+template <typename T, bool FIRST, int NS, int NO, int RT, bool FULL, int HOW>
+__global__ __launch_bounds__(64 * kW4Waves, kW4PerSimd) void w4_product_kernel(W4Args a) {
+  extern __shared__ __attribute__((aligned(16))) char w4_lds[];
+  W4Lds<RT>* lds = reinterpret_cast<W4Lds<RT>*>(w4_lds);   // one a wave
   __shared__ int32_t found, lists[kW4Scan];
-  const int wv = threadIdx.x >> 6;
+  const int wv = threadIdx.x >> 6, waves = blockDim.x >> 6;
   W4Step<RT, FULL> w;
   const uint8_t *codes = nullptr, *scales = nullptr;
   auto weights = [&](int e) __attribute__((always_inline)) {   // the wave's first step
@@ -400,13 +410,13 @@ __global__ __launch_bounds__(64 * WV, 3) void w4_product_kernel(W4Args a) {
     scales = a.scales + row * (a.K / 32);
     if (wv * kStep < a.K) w.load(codes, scales, a.K, wv * kStep);
   };
-  const W4Found f = w4_find<HOW, WV>(a, lists, found, weights);
+  const W4Found f = w4_find<HOW>(a, waves, lists, found, weights);
   for (int c0 = 0; c0 < f.cnt; c0 += kW4Tile) {
     if (c0) {
       weights(f.e);
       __syncthreads();   // the sums of the tile before have been read
     }
-    w4_tile<T, FIRST, NS, NO, RT, WV, FULL>(a, min(kW4Tile, f.cnt - c0), f.list + c0, codes, scales, w, lds);
+    w4_tile<T, FIRST, NS, NO, RT, FULL>(a, waves, min(kW4Tile, f.cnt - c0), f.list + c0, codes, scales, w, lds);
   }
 }
 
@@ -450,7 +460,7 @@ __global__ __launch_bounds__(256, NS == 3 ? 1 : 2) void w4_rows_kernel(W4Args a)
     scales = a.scales + row * (a.K / 32);
     load_w(k0);
   };
-  const W4Found fnd = w4_find<HOW, 4>(a, lists, found, first);
+  const W4Found fnd = w4_find<HOW>(a, 4, lists, found, first);
   for (int c0 = 0; c0 < fnd.cnt; c0 += kW4Tile) {
     const int cnt = min(kW4Tile, fnd.cnt - c0);
     const int32_t* list = fnd.list + c0;
@@ -540,39 +550,61 @@ __global__ __launch_bounds__(256, NS == 3 ? 1 : 2) void w4_rows_kernel(W4Args a)
   }
 }
 
-// Thread: four columns of a token (blockIdx.y; further ones past the grid's limit).
-template <typename T>
+// Thread: four columns of a token (blockIdx.y; further ones past the grid's limit).  NR
+// choices at a time, every load of them and of their SP splits ahead of the sums: with few
+// tokens the kernel is the latency of its loads.
+template <typename T, int SP, int NR>
 __global__ __launch_bounds__(256) void w4_combine_kernel(const float* __restrict__ O, const int32_t* __restrict__ idx,
                                                          const float* __restrict__ w, T* __restrict__ y, int64_t T_tokens,
-                                                         int d, int E, int k, int splits) {
+                                                         int d, int E, int k) {
   const int c = (blockIdx.x * 256 + threadIdx.x) * 4;
   if (c >= d) return;
   for (int64_t t = blockIdx.y; t < T_tokens; t += gridDim.y) {
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
-    // Four choices at a time, every load of them ahead of the sums.
-    for (int r0 = 0; r0 < k; r0 += 4) {
-      int e[4];
-      float wr[4];
-      f32x4 o[4];
+    for (int r0 = 0; r0 < k; r0 += NR) {
+      int e[NR];
+      float wr[NR];
+      f32x4 o[NR][SP];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
+      for (int r = 0; r < NR; ++r) {
         const int64_t i = t * k + min(r0 + r, k - 1);
         e[r] = idx[i];
         wr[r] = w[i];
-        o[r] = *reinterpret_cast<const f32x4*>(O + i * d + c);
-        for (int z = 1; z < splits; ++z) o[r] += *reinterpret_cast<const f32x4*>(O + (z * T_tokens * k + i) * d + c);
-      }
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
+        for (int z = 0; z < SP; ++z) o[r][z] = *reinterpret_cast<const f32x4*>(O + (z * T_tokens * k + i) * d + c);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int r = 0; r < NR; ++r) {
+#pragma unroll
+        for (int z = 1; z < SP; ++z) o[r][0] += o[r][z];
         if (r0 + r < k && e[r] >= 0 && e[r] < E)   // (of another choice O and w may hold anything)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s[i] = fmaf(wr[r], o[r][i], s[i]);
+          for (int i = 0; i < 4; ++i) s[i] = fmaf(wr[r], o[r][0][i], s[i]);
+      }
     }
     if constexpr (sizeof(T) == 2)
       *reinterpret_cast<u32x2*>(y + t * d + c) = u32x2{pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3])};
     else
       *reinterpret_cast<f32x4*>(y + t * d + c) = s;
   }
+}
+template <typename T>
+static void launch_w4_combine(const moe_w4_cfg& c, const float* O, const int32_t* idx, const float* w, void* y, int splits,
+                              hipStream_t s) {
+  const dim3 grid((c.d_model + 1023) / 1024, (unsigned)std::min<int64_t>(c.T, 32768));
+  auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, O, idx, w, (T*)y, c.T, c.d_model, c.E, c.k); };
+  auto choices = [&](auto sp) {
+    constexpr int SP = decltype(sp)::value;
+    if (c.k <= 2) go(w4_combine_kernel<T, SP, 2>);
+    else if (c.k <= 4) go(w4_combine_kernel<T, SP, 4>);
+    else go(w4_combine_kernel<T, SP, 8>);
+  };
+  static_assert(kW4Splits == 4, "a case for each");
+  if (splits == 1) choices(std::integral_constant<int, 1>{});
+  else if (splits == 2) choices(std::integral_constant<int, 2>{});
+  else if (splits == 3) choices(std::integral_constant<int, 3>{});
+  else choices(std::integral_constant<int, 4>{});
 }
 
 // ------------------------------------------------------------------ many tokens
@@ -873,10 +905,12 @@ static W4Ws w4_ws(const moe_w4_cfg& c) {
 size_t experts_w4_ws_bytes(const moe_w4_cfg& c) { return w4_ws(c).total; }
 
 // A product over gy experts or tiles; the splits it was done in.  Blocks of 128 rows where
-// there are three for two CUs (the second product's K split to get there); else 16 or 32 rows,
-// two blocks a CU if there are that many, and K split over the waves.  5 float tokens, 15
-// choices, d 736, f 1888: first product 11.1 us with 32 rows and 16.2 with 16; second (270
-// blocks of 128) 13.6 with 16 and 16.3 with 128.
+// there are three for two CUs (the second product's K split to get there): 48 tokens, 16
+// experts of 1024 x 4096, 512 blocks, 12.3 and 13.6 us; one token, top-2 of them, 64 blocks,
+// 8.3 and 7.0 us where 16 rows take 4.9 and 6.0.  Else 16 or 32 rows, 32 where there are two
+// blocks a CU of them: 5 float tokens, 15 choices, d 736, f 1888, first product (885 blocks of
+// 32) 10.1 us, with 16 rows 14.4, with 128 11.7; second (690 blocks of 16) 9.4, with 32 rows
+// 11.9, with 128 11.4.
 template <typename T, bool FIRST, int NS, int NO, bool FULL>
 static int launch_w4_rows(W4Args a, int gy, hipStream_t s) {
   const int cus = num_cus();
@@ -899,14 +933,25 @@ static int launch_w4_rows(W4Args a, int gy, hipStream_t s) {
       });
     return splits;
   }
-  const bool deep = a.K > 4 * kStep;   // more than a step for each of four waves
   const int rt = (int64_t)(a.N / 16) * gy >= 4 * cus ? 2 : 1;
-  how([&](auto h) {
-    constexpr int H = decltype(h)::value;
-    auto go = [&](auto kern, int wv) { hipLaunchKernelGGL(kern, dim3(a.N / (16 * rt), gy), dim3(64 * wv), 0, s, a); };
-    if (rt == 2) deep ? go(w4_product_kernel<T, FIRST, NS, NO, 2, 8, FULL, H>, 8) : go(w4_product_kernel<T, FIRST, NS, NO, 2, 4, FULL, H>, 4);
-    else deep ? go(w4_product_kernel<T, FIRST, NS, NO, 1, 8, FULL, H>, 8) : go(w4_product_kernel<T, FIRST, NS, NO, 1, 4, FULL, H>, 4);
-  });
+  // Eight waves split K finer than four, but more of such blocks wait for a place: rounds of
+  // blocks times a wave's steps and the latencies ahead of the first, as long as three.
+  // (Second product of the one token: 6.0 us with eight, 6.7 with four; of the 5 float
+  // tokens 11.9 and 9.4, their first 14.3 and 10.1.)
+  auto cost = [&](int wv) {
+    const int64_t places = (int64_t)cus * (4 * kW4PerSimd / wv);
+    return ((int64_t)(a.N / (16 * rt)) * gy + places - 1) / places * (3 + (steps + wv - 1) / wv);
+  };
+  const int waves = cost(kW4Waves) < cost(4) ? kW4Waves : 4;
+  for (; a.tile0 < gy; a.tile0 += kMaxGridY)
+    how([&](auto h) {
+      constexpr int H = decltype(h)::value;
+      auto go = [&](auto kern, size_t lds) {
+        hipLaunchKernelGGL(kern, dim3(a.N / (16 * rt), std::min(kMaxGridY, gy - a.tile0)), dim3(64 * waves), waves * lds, s, a);
+      };
+      if (rt == 2) go(w4_product_kernel<T, FIRST, NS, NO, 2, FULL, H>, sizeof(W4Lds<2>));
+      else go(w4_product_kernel<T, FIRST, NS, NO, 1, FULL, H>, sizeof(W4Lds<1>));
+    });
   return 1;
 }
 template <typename T, bool FIRST, int NS, int NO>
@@ -941,8 +986,7 @@ static void launch_w4_gemm(const moe_w4_cfg& c, const void* x, const int32_t* id
   splits = (steps + per - 1) / per;
   const W4GemmArgs b{W2c, W2s, (const uint16_t*)(base + L.parts), base + L.O, choice_of, tiles, ntiles, d, f, n, c.act, per};
   hipLaunchKernelGGL(w4_gemm_kernel<false>, dim3(d / kGemmRows, gy, splits), dim3(256), 0, s, b);
-  hipLaunchKernelGGL(w4_combine_kernel<uint16_t>, dim3((d + 1023) / 1024, (unsigned)std::min<int64_t>(c.T, 32768)), dim3(256), 0,
-                     s, (const float*)(base + L.O), idx, w, (uint16_t*)y, c.T, d, c.E, c.k, splits);
+  launch_w4_combine<uint16_t>(c, (const float*)(base + L.O), idx, w, y, splits, s);
 }
 
 template <typename T, int NX, int NA>
@@ -967,9 +1011,7 @@ static void launch_w4_t(const moe_w4_cfg& c, const void* x, const int32_t* idx, 
   const W4Args b{W2c, W2s, base + L.parts, base + L.O, idx, list, tiles, ntiles, c.d_model, c.d_ff, n, c.k, c.E, c.act,
                  by_choice, 0, 0};
   const int splits = launch_w4_product<T, false, NA, NA>(b, gy, s);
-  hipLaunchKernelGGL(w4_combine_kernel<T>, dim3((c.d_model + 1023) / 1024, (unsigned)std::min<int64_t>(c.T, 32768)),
-                     dim3(256), 0, s,
-                     (const float*)(base + L.O), idx, w, (T*)y, c.T, c.d_model, c.E, c.k, splits);
+  launch_w4_combine<T>(c, (const float*)(base + L.O), idx, w, y, splits, s);
 }
 
 void launch_experts_w4(const moe_w4_cfg& c, const void* x, const int32_t* idx, const float* w, const uint8_t* W1c,

@@ -454,8 +454,9 @@ __global__ __launch_bounds__(64 * kRouteWaves) void route_kernel(RouteArgs a) {
 #pragma unroll
     for (int q = 0; q < NM; ++q) {
       const int r = q * LPT + j;
-      const int before = q == 0 ? team_before<LPT>(kept_key[0])
-                                : j == 0 ? team_before<LPT>(kept_key[q > 0 ? q - 1 : 0]) : team_before<LPT>(kept_key[q]);
+      // (both exchanges by every lane: in the arms of a condition their sources would be idle)
+      const int here = team_before<LPT>(kept_key[q]), there = team_before<LPT>(kept_key[q > 0 ? q - 1 : 0]);
+      const int before = j == 0 ? there : here;
       const float x = from_order_key(kept_key[q]), p = from_order_key(before);
       amb |= r >= 1 && r <= k && x > kRouteNone && p - x <= route_eps(NV) * fmaxf(1.f, fabsf(p));
       amb |= r <= k && x > kRouteNone && __popc(kept_at[q] & (LPT == 16 ? 0xffffu : 0xfu)) > 1;   // two alike
@@ -553,7 +554,8 @@ void launch_route(const moe_route_cfg& c, const float* logits, const float* bias
   if (c.T == 0) return;
   const RouteArgs a{logits, bias, idx, w, c.T, c.E, c.k, c.score, c.renorm, c.groups, c.top_groups, c.scale, 0};
   // E < 4 has no whole load; groups that are no whole chunks or more than a team's lanes
-  // have no place in it.
+  // have no place in it.  (All in double: E 64, k 8, 64 tokens 4.5 us where it takes 3.1,
+  // 65536 71 where it takes 9.4.)
   if (c.E < 4 || (c.groups > 1 && (c.groups > kRouteGroupsFast || (c.E / c.groups) % 4 != 0))) {
     const unsigned blocks = (unsigned)std::min<int64_t>((c.T + 3) / 4, 8 * num_cus());
     auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(blocks), dim3(256), 0, s, a); };
@@ -567,8 +569,14 @@ void launch_route(const moe_route_cfg& c, const float* logits, const float* bias
     else if (c.E <= 256) launch_route_n<16, 4, true>(a, s);
     else launch_route_n<16, 8, true>(a, s);
   } else {
+    // Teams of 4 take fewer instructions a token, teams of 16 have shorter chains.  Up to 16
+    // experts 4 lanes hold a row in a load each (top-2, us, 4 and 16 lanes: 64 tokens 2.4 and
+    // 2.7, 65536 3.4 and 6.7); up to 64 it is 16 lanes until a CU's waves are many (E 64, k 8:
+    // 8192 tokens 6.5 and 5.0, 24000 6.8 and 6.5, 32768 7.2 and 7.6, 65536 9.4 and 10.7); above
+    // it is 16 (E 128, k 8: 64 tokens 4.1 and 3.3, 65536 16.1 and 13.8).
     if (c.E <= 16) launch_route_n<4, 1, false>(a, s);
-    else if (c.E <= 64) launch_route_n<4, 4, false>(a, s);
+    else if (c.E <= 64 && c.T > 96 * num_cus()) launch_route_n<4, 4, false>(a, s);
+    else if (c.E <= 64) launch_route_n<16, 1, false>(a, s);
     else if (c.E <= 128) launch_route_n<16, 2, false>(a, s);
     else if (c.E <= 256) launch_route_n<16, 4, false>(a, s);
     else launch_route_n<16, 8, false>(a, s);

@@ -130,6 +130,15 @@ def test_single_live_expert_and_zeros(E):
     check(l, min(E, 4))
 
 
+@pytest.mark.parametrize("T", [24576, 24577, 32771])
+@pytest.mark.parametrize("E,k", [(64, 8), (37, 5)])
+def test_many_tokens_of_up_to_64_experts(T, E, k):
+    l = np.random.default_rng(T + E).standard_normal((T, E)).astype(np.float32)
+    l[::1000, ::2] = -np.inf
+    check(l, k, score="softmax")
+    check(l, k, np.linspace(-0.1, 0.1, E).astype(np.float32), score="sigmoid")
+
+
 def test_load_is_added_and_counts_every_choice():
     l = make_logits(4099, 48, 5)
     c = L.make_route_cfg(4099, 48, 4)
