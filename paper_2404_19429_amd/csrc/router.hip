@@ -7,7 +7,10 @@
 // a team of 4 or 16 lanes holds a token's row, and every step that compares two values
 // also sees whether they are too close for float to tell (route_eps, above the sum of
 // the errors).  Such a token (a few in a thousand of ordinary logits; all of them where
-// logits tie) goes the exact way, one wavefront for the token in double.
+// logits tie) goes the exact way, one wavefront for the token in double, in the same launch.
+// Bound by the comparisons, not by the 4 E bytes a token: 32768 tokens, 256 experts in 8
+// groups, k 8, 22.8 us (8.7 for the bytes; 16 without the exact way, whose registers leave
+// five waves a SIMD); all in double 270.  8192 tokens, 64 experts, k 2: 3.4 us.
 #include <utility>
 
 #include "internal.h"
@@ -197,7 +200,7 @@ constexpr float route_eps(int nv) { return (float)(5 * nv - 1) * 0x1p-24f + 1e-6
 // 2^-23 for the sum, and as above for four scores in 32 a lane: 1.12e-5.
 constexpr float kRouteGroupEps = 1.25e-5f;
 constexpr int kRouteGroupsFast = 16;      // one lane of a team for each group
-constexpr int kRouteWaves = 8;            // per block
+constexpr int kRouteWaves = 4;            // per block (eight: 32768 tokens, 256 experts 23.6 us, four 22.8)
 
 template <int CTRL>
 __device__ __forceinline__ int dpp_i(int v) {
@@ -590,7 +593,8 @@ void launch_route(const moe_route_cfg& c, const float* logits, const float* bias
 
 // ------------------------------------------------------------------- gradient
 // Bound by writing dlogits, most of it zeros (but for a plain softmax, which also reads
-// the logits).  A wavefront builds its tokens' rows in LDS and stores them as one run.
+// the logits).  A wavefront builds its tokens' rows in LDS and stores them as one run
+// (32768 tokens, 256 experts, k 8: 8.3 us; k shuffles a token and scattered stores 16.8).
 struct RouteBwdArgs {
   const float* logits;
   const int32_t* idx;
