@@ -608,11 +608,14 @@ static void launch_w4_combine(const moe_w4_cfg& c, const float* O, const int32_t
 }
 
 // ------------------------------------------------------------------ many tokens
-// bfloat16 with two dozen tokens an expert and more: the products are matrix products
+// bfloat16, two dozen tokens an expert and more: the products are matrix products
 // again.  The tokens' rows are laid out by expert, padded to 16, in the order in which the
 // matrix instructions take them (x by w4_pack_kernel, act(W1 x) by the first product), so
 // both sides of a 128-row x 160-token block go through LDS in whole lines: the codes of 256
 // inputs, the tokens' values of 64, each with the next on its way.  Four waves, 64 rows by half the tokens each.
+// The tokens' rows are padded to whole 128s with zeros; rows and inputs past the matrix are
+// read inside it (WHOLE: there are none), such codes taken as zeros and such rows written as
+// zeros, which the second product meets as its inputs' padding.
 // act(W1 x) is rounded once to bfloat16 here, as moe_expert_ffn_fwd does: a second part
 // would double the second product, which is no longer hidden behind the weights.
 constexpr int kGemmRows = 128, kGemmToks = 160, kGemmT = kGemmToks / 32;   // kGemmT: 16-token tiles of a wave
@@ -669,7 +672,9 @@ __global__ __launch_bounds__(kW4ListThreads) void w4_group_kernel(const int32_t*
   }
 }
 
-// Element (row, input) of the laid-out tokens [row / 16][input / 128][j][lane][8].
+static int w4_pad(int x) { return (x + 127) / 128 * 128; }
+
+// Element (row, input) of the laid-out tokens [row / 16][input / 128][j][lane][8]; K: padded.
 __host__ __device__ __forceinline__ int64_t w4_tok_off(int64_t row, int in, int K) {
   return (((row >> 4) * (K >> 7) + (in >> 7)) * 4 + ((in & 31) >> 3)) * 512 + (((in >> 5) & 3) * 16 + (row & 15)) * 8 + (in & 7);
 }
@@ -680,20 +685,21 @@ __global__ __launch_bounds__(256) void w4_pack_kernel(const uint16_t* __restrict
   for (int64_t p = (int64_t)blockIdx.x * 256 + threadIdx.x; p < pieces; p += (int64_t)gridDim.x * 256) {
     const int lane = (int)(p & 63), j = (int)(p >> 6) & 3;
     const int64_t chunk = p >> 8;
-    const int nc = K >> 7;
+    const int nc = (K + 127) >> 7;
     const int64_t t16 = chunk / nc;
     const int c = (int)(chunk - t16 * nc);
     const int choice = choice_of[t16 * 16 + (lane & 15)];
+    const int in = c * 128 + (lane >> 4) * 32 + 8 * j;
     u32x4 v = {0u, 0u, 0u, 0u};
-    if (choice >= 0) v = *reinterpret_cast<const u32x4*>(x + (int64_t)(choice / k) * K + c * 128 + (lane >> 4) * 32 + 8 * j);
+    if (choice >= 0 && in < K) v = *reinterpret_cast<const u32x4*>(x + (int64_t)(choice / k) * K + in);
     *reinterpret_cast<u32x4*>(out + p * 8) = v;
   }
 }
 
 struct W4GemmArgs {
   const uint8_t *codes, *scales;
-  const uint16_t* in;    // laid-out tokens of K values
-  void* out;             // FIRST: laid-out tokens of N values; else float [splits][n][N]
+  const uint16_t* in;    // laid-out tokens of K values (padded to 128)
+  void* out;             // FIRST: laid-out tokens of N values (padded to 128); else float [splits][n][N]
   const int32_t* choice_of;
   const W4Group* tiles;
   const int32_t* ntiles;
@@ -718,7 +724,7 @@ __device__ __forceinline__ f32x4 w4_act_rounded(f32x4 v, int act) {
   return r;
 }
 
-template <bool FIRST>
+template <bool FIRST, bool WHOLE>
 __global__ __launch_bounds__(256, 2) void w4_gemm_kernel(W4GemmArgs a) {
   __shared__ u32x4 wcode[2][kGemmRows][8];     // [row][piece ^ row % 8]
   __shared__ uint32_t wsc[2][2][kGemmRows];    // [half][row]: four groups' bytes
@@ -733,31 +739,46 @@ __global__ __launch_bounds__(256, 2) void w4_gemm_kernel(W4GemmArgs a) {
   const int nt16 = g.rows >> 4;                                  // 16-token tiles of the block
   const int t0 = tg * ((nt16 + 1) / 2), mine = tg ? nt16 - t0 : (nt16 + 1) / 2;   // of the wave
   const int k0 = blockIdx.z * a.steps * kStep;
-  const int k1 = min(a.K, k0 + a.steps * kStep);
+  const int Kp = WHOLE ? a.K : (a.K + 127) & ~127, Np = WHOLE ? a.N : (a.N + 127) & ~127;
+  const int k1 = min(Kp, k0 + a.steps * kStep);
   if (k0 >= k1) return;   // (the launch leaves no split empty)
   const uint8_t* codes = a.codes + ((int64_t)g.e * a.N + row0) * (a.K / 2);
   const uint8_t* scales = a.scales + ((int64_t)g.e * a.N + row0) * (a.K / 32);
-  const uint16_t* toks = a.in + (int64_t)(g.row >> 4) * a.K * 16;
+  const uint16_t* toks = a.in + (int64_t)(g.row >> 4) * Kp * 16;
 
-  // (K is a multiple of 128.  A half step past k1 is not looked at, nor are tiles past
+  // (k1 is a multiple of 128.  A half step past k1 is not looked at, nor are tiles past
   // nt16: their loads are of something inside the arrays, and wait for no branch.)
   u32x4 wreg[4];
   uint32_t sreg[2];
+  const int last_row = a.N - 1 - row0, groups = a.K / 32;
   auto load_w = [&](int col) __attribute__((always_inline)) {
-    const int at = col + (lane & 7) * 32;
+    const int at = col + (lane & 7) * 32, in = at < k1 ? at : col;
+    const bool ok = WHOLE || in < a.K;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int64_t row = 32 * wv + 8 * i + (lane >> 3);
-      wreg[i] = *reinterpret_cast<const u32x4*>(codes + row * (a.K / 2) + (at < k1 ? at : col) / 2);
+      const int row = 32 * wv + 8 * i + (lane >> 3);
+      const u32x4 v = *reinterpret_cast<const u32x4*>(codes + (int64_t)(WHOLE ? row : min(row, last_row)) * (a.K / 2) +
+                                                      (ok ? in : 0) / 2);
+      wreg[i] = ok ? v : u32x4{0u, 0u, 0u, 0u};
     }
-    const uint8_t* p = scales + (int64_t)(tid & (kGemmRows - 1)) * (a.K / 32);
-    sreg[0] = *reinterpret_cast<const uint32_t*>(p + col / 32);
-    sreg[1] = *reinterpret_cast<const uint32_t*>(p + (col + 128 < k1 ? col + 128 : col) / 32);
+    if constexpr (WHOLE) {
+      const uint8_t* p = scales + (int64_t)(tid & (kGemmRows - 1)) * groups;
+      sreg[0] = *reinterpret_cast<const uint32_t*>(p + col / 32);
+      sreg[1] = *reinterpret_cast<const uint32_t*>(p + (col + 128 < k1 ? col + 128 : col) / 32);
+    } else {   // rows of any alignment: a half step of one row a thread (past K the row's last)
+      const uint8_t* p = scales + (int64_t)min(tid & (kGemmRows - 1), last_row) * groups;
+      const int g0 = (col + 128 * (tid / kGemmRows)) / 32;
+      sreg[0] = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sreg[0] |= (uint32_t)p[min(g0 + i, groups - 1)] << (8 * i);
+    }
   };
   auto store_w = [&](int b) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) wcode[b][32 * wv + 8 * i + (lane >> 3)][(lane & 7) ^ (lane >> 3)] = wreg[i];
-    if (tid < kGemmRows) {
+    if constexpr (!WHOLE) {
+      wsc[b][tid / kGemmRows][tid & (kGemmRows - 1)] = sreg[0];
+    } else if (tid < kGemmRows) {
       wsc[b][0][tid] = sreg[0];
       wsc[b][1][tid] = sreg[1];
     }
@@ -768,7 +789,7 @@ __global__ __launch_bounds__(256, 2) void w4_gemm_kernel(W4GemmArgs a) {
 #pragma unroll
     for (int i = 0; i < kGemmT; ++i) {
       const int f = wv + 4 * i, t = min(f >> 1, nt16 - 1), j = 2 * jp + (f & 1);   // every fourth fragment
-      treg[i] = *reinterpret_cast<const u32x4*>(toks + (((int64_t)t * (a.K >> 7) + (col >> 7)) * 4 + j) * 512 + lane * 8);
+      treg[i] = *reinterpret_cast<const u32x4*>(toks + (((int64_t)t * (Kp >> 7) + (col >> 7)) * 4 + j) * 512 + lane * 8);
     }
   };
   auto store_t = [&](int b) __attribute__((always_inline)) {
@@ -858,24 +879,25 @@ __global__ __launch_bounds__(256, 2) void w4_gemm_kernel(W4GemmArgs a) {
       const int f = row0 + 64 * rg + 16 * r + 4 * q;
       if constexpr (FIRST) {   // (padding rows: act(0) = 0)
         const f32x4 h = w4_act_rounded(acc[r][t], a.act);
-        *reinterpret_cast<u32x2*>((uint16_t*)a.out + w4_tok_off(row, f, a.N)) =
-            u32x2{pack_bf16x2(h[0], h[1]), pack_bf16x2(h[2], h[3])};
+        const bool in = WHOLE || f < a.N;
+        *reinterpret_cast<u32x2*>((uint16_t*)a.out + w4_tok_off(row, f, Np)) =
+            u32x2{in ? pack_bf16x2(h[0], h[1]) : 0u, in ? pack_bf16x2(h[2], h[3]) : 0u};
       } else {
-        if (choice >= 0)
+        if (choice >= 0 && (WHOLE || f < a.N))
           *reinterpret_cast<f32x4*>((float*)a.out + ((int64_t)blockIdx.z * a.n + choice) * a.N + f) = acc[r][t];
       }
     }
   }
 }
 
-// The laid-out form serves: bfloat16, whole 128s, and tokens enough.  Its time hardly
+// The laid-out form serves: bfloat16 and tokens enough.  Its time hardly
 // grows with the tokens, the other form's does with every 16 of an expert; whole call, us,
 // other form against this one, by choices an expert: 16 experts of 1024 x 4096, 16: 48.5
 // and 54.0, 24: 54.9 and 55.0, 32: 70.2 and 56.6; 64 experts of 2048 x 1408, 18: 109.7 and
 // 114.5, 24: 118.8 and 117.5, 36: 158.4 and 124.4.
 constexpr int kGemmFrom = 24;   // choices an expert, on average
 static bool w4_gemm(const moe_w4_cfg& c) {
-  return c.dtype == MOE_BF16 && c.d_model % 128 == 0 && c.d_ff % 128 == 0 && c.T * c.k >= (int64_t)kGemmFrom * c.E;
+  return c.dtype == MOE_BF16 && c.T * c.k >= (int64_t)kGemmFrom * c.E;
 }
 
 // Workspace: list (or choices by row), tiles, tile count | parts (or laid-out act(W1 x)) |
@@ -897,9 +919,9 @@ static W4Ws w4_ws(const moe_w4_cfg& c) {
   w.tiles = up256(4 * (size_t)w.rows);
   w.ntiles = w.tiles + sizeof(W4Tile) * (size_t)w.max_tiles;
   w.parts = up256(w.ntiles + 4);
-  w.O = up256(w.parts + std::max((size_t)(bf ? 2 : 3) * n, bf ? (size_t)w.rows : 0) * c.d_ff * 2);
+  w.O = up256(w.parts + std::max((size_t)(bf ? 2 : 3) * n * c.d_ff, bf ? (size_t)w.rows * w4_pad(c.d_ff) : 0) * 2);
   w.x = up256(w.O + (size_t)kW4Splits * n * c.d_model * 4);
-  w.total = up256(w.x + (bf ? (size_t)w.rows * c.d_model * 2 : 0));
+  w.total = up256(w.x + (bf ? (size_t)w.rows * w4_pad(c.d_model) * 2 : 0));
   return w;
 }
 size_t experts_w4_ws_bytes(const moe_w4_cfg& c) { return w4_ws(c).total; }
@@ -971,21 +993,26 @@ static void launch_w4_gemm(const moe_w4_cfg& c, const void* x, const int32_t* id
   static_assert(sizeof(W4Group) == sizeof(W4Tile), "one table's room");
   hipLaunchKernelGGL(w4_group_kernel, dim3(1), dim3(kW4ListThreads), 0, s, idx, n, c.E, choice_of, tiles, ntiles,
                      (int)L.rows);
-  const int64_t pieces = L.rows * (d / 8);
+  const int64_t pieces = L.rows * (w4_pad(d) / 8);
   hipLaunchKernelGGL(w4_pack_kernel, dim3((unsigned)std::min<int64_t>((pieces + 255) / 256, 1 << 20)), dim3(256), 0, s,
                      (const uint16_t*)x, (const int32_t*)choice_of, (uint16_t*)(base + L.x), d, c.k, pieces);
   const int gy = std::min<int64_t>(n, c.E) + n / kGemmToks;
   const W4GemmArgs a{W1c, W1s, (const uint16_t*)(base + L.x), base + L.parts, choice_of, tiles, ntiles, f, d, n, c.act,
                      (d + kStep - 1) / kStep};
-  hipLaunchKernelGGL(w4_gemm_kernel<true>, dim3(f / kGemmRows, gy), dim3(256), 0, s, a);
+  const bool whole = d % kGemmRows == 0 && f % kGemmRows == 0;
+  static_assert(kGemmRows == 128, "the padding of a layout's rows");
+  auto go = [&](auto kern, int N, int splits, const W4GemmArgs& g) {
+    hipLaunchKernelGGL(kern, dim3(w4_pad(N) / kGemmRows, gy, splits), dim3(256), 0, s, g);
+  };
+  whole ? go(w4_gemm_kernel<true, true>, f, 1, a) : go(w4_gemm_kernel<true, false>, f, 1, a);
   // K is split where the blocks would not fill the CUs twice; whole steps, no split empty.
   const int steps = (f + kStep - 1) / kStep;
-  const int64_t blocks = (int64_t)(d / kGemmRows) * c.E * ((n / c.E + kGemmToks - 1) / kGemmToks);   // for an even load
+  const int64_t blocks = (int64_t)(w4_pad(d) / kGemmRows) * c.E * ((n / c.E + kGemmToks - 1) / kGemmToks);   // for an even load
   int splits = (int)std::min<int64_t>(std::min(kW4Splits, steps), std::max<int64_t>(1, 2 * num_cus() / std::max<int64_t>(1, blocks)));
   const int per = (steps + splits - 1) / splits;
   splits = (steps + per - 1) / per;
   const W4GemmArgs b{W2c, W2s, (const uint16_t*)(base + L.parts), base + L.O, choice_of, tiles, ntiles, d, f, n, c.act, per};
-  hipLaunchKernelGGL(w4_gemm_kernel<false>, dim3(d / kGemmRows, gy, splits), dim3(256), 0, s, b);
+  whole ? go(w4_gemm_kernel<false, true>, d, splits, b) : go(w4_gemm_kernel<false, false>, d, splits, b);
   launch_w4_combine<uint16_t>(c, (const float*)(base + L.O), idx, w, y, splits, s);
 }
 
