@@ -381,8 +381,9 @@ size_t moe_experts_w4_workspace_bytes(const moe_w4_cfg* cfg);
  *   scales [E][f][d/32], W2 codes [E][d][f/2] and scales [E][d][f/32].
  *   Sums in float over products exact in bfloat16 factors: x is bfloat16, or its
  *   three bfloat16 parts (MOE_F32); act(W1 x) two (three) such parts, so that only y
- *   is rounded to its type.  Many tokens (MOE_BF16, T * k >= 24 E): act(W1 x) is
- *   rounded once, to bfloat16, as by moe_expert_ffn_fwd.
+ *   is rounded to its type.  Many tokens (MOE_BF16, T * k >= 24 E, and T * k * d * f >=
+ *   3 * 2^27 with f >= 1024, 2^30 with less): act(W1 x) is rounded once, to bfloat16, as
+ *   by moe_expert_ffn_fwd.
  *   The same call gives the same bits.  Tokens do not mix; the order of a token's sums
  *   depends on cfg only.
  *   ws: moe_experts_w4_workspace_bytes(cfg) bytes.  Calls that overlap in time need

@@ -153,17 +153,17 @@ def experts(x, idx, w, W1, W2, act_name, part=2.0 ** -16):
     T, d = x.shape
     E, f = W1.shape[:2]
     y, err = np.zeros((T, d)), np.zeros((T, d))
-    for t in range(T):
-        for r in range(idx.shape[1]):
-            e = idx[t, r]
-            if not 0 <= e < E:
-                continue
-            h = W1[e] @ x[t]
-            eh = (d + 4) * U32 * (np.abs(W1[e]) @ np.abs(x[t]))
-            a = act(h, act_name)
-            ea = 1.13 * eh + 16 * U32 * np.abs(h) + part * np.abs(a)
-            y[t] += w[t, r] * (W2[e] @ a)
-            err[t] += abs(w[t, r]) * (np.abs(W2[e]) @ ea + (f + 8 + idx.shape[1]) * U32 * (np.abs(W2[e]) @ np.abs(a)))
+    for e in range(E):
+        t, r = np.nonzero(idx == e)
+        if t.size == 0:
+            continue
+        h = x[t] @ W1[e].T
+        eh = (d + 4) * U32 * (np.abs(x[t]) @ np.abs(W1[e]).T)
+        a = act(h, act_name)
+        ea = 1.13 * eh + 16 * U32 * np.abs(h) + part * np.abs(a)
+        abs2 = np.abs(W2[e]).T
+        np.add.at(y, t, w[t, r][:, None] * (a @ W2[e].T))
+        np.add.at(err, t, np.abs(w[t, r])[:, None] * (ea @ abs2 + (f + 8 + idx.shape[1]) * U32 * (np.abs(a) @ abs2)))
     return y, err
 
 

@@ -890,14 +890,19 @@ __global__ __launch_bounds__(256, 2) void w4_gemm_kernel(W4GemmArgs a) {
   }
 }
 
-// The laid-out form serves: bfloat16 and tokens enough.  Its time hardly
-// grows with the tokens, the other form's does with every 16 of an expert; whole call, us,
-// other form against this one, by choices an expert: 16 experts of 1024 x 4096, 16: 48.5
-// and 54.0, 24: 54.9 and 55.0, 32: 70.2 and 56.6; 64 experts of 2048 x 1408, 18: 109.7 and
-// 114.5, 24: 118.8 and 117.5, 36: 158.4 and 124.4.
+// The laid-out form serves: bfloat16, tokens and work enough.  Its time hardly grows with the
+// tokens, the other form's does with every 16 of an expert; but it has two launches more,
+// and of few blocks' long chains if there are few rows.  Whole call, us, other form against
+// this one.  By choices an expert: 16 experts of 1024 x 4096, 16: 48.5 and 54.0, 24: 54.9 and
+// 55.0, 32: 70.2 and 56.6; 64 experts of 2048 x 1408, 18: 109.7 and 114.5, 24: 118.8 and 117.5,
+// 36: 158.4 and 124.4.  By choices x d x f in 10^9: f 1056, 0.27: 29 and 34, 0.45: 49 and 40,
+// 0.57: 43 and 42, 0.67: 68 and 45; f 1024, 0.54: 44 and 40; f 512, 0.54: 34 and 41,
+// 0.63: 43 and 53, 0.77: 40 and 46; f 256, 0.54: 33 and 59.
 constexpr int kGemmFrom = 24;   // choices an expert, on average
 static bool w4_gemm(const moe_w4_cfg& c) {
-  return c.dtype == MOE_BF16 && c.T * c.k >= (int64_t)kGemmFrom * c.E;
+  const int64_t n = c.T * c.k;
+  return c.dtype == MOE_BF16 && n >= (int64_t)kGemmFrom * c.E &&
+         n * c.d_model * c.d_ff >= (c.d_ff >= 1024 ? (int64_t)3 << 27 : (int64_t)1 << 30);
 }
 
 // Workspace: list (or choices by row), tiles, tile count | parts (or laid-out act(W1 x)) |

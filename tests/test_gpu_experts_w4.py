@@ -44,9 +44,13 @@ def inputs(T, d, f, E, k, dtype, seed, skew=None):
     return x, idx.reshape(T, k), w, W
 
 
+def laid_out(n, d, f, E, dtype):
+    return dtype == "bf16" and n >= 24 * E and n * d * f >= (3 << 27 if f >= 1024 else 1 << 30)
+
+
 def check(y, x, idx, w, W, act, dtype):
-    # act(W1 x) keeps 16 significant bits, or (bf16, 24 choices an expert) is rounded once to bfloat16
-    part = 2.0 ** -8 if dtype == "bf16" and idx.size >= 24 * W[0].shape[0] else 2.0 ** -16
+    # act(W1 x) keeps 16 significant bits, or (many tokens) is rounded once to bfloat16
+    part = 2.0 ** -8 if laid_out(idx.size, x.shape[1], W[0].shape[1], W[0].shape[0], dtype) else 2.0 ** -16
     ref, err = O.experts(x.double().numpy(), idx, w.astype(np.float64), O.w4_decode(W[0], W[1]), O.w4_decode(W[2], W[3]), act, part)
     got = y.double().cpu().numpy()
     tol = err + (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) * (np.abs(ref) + err)   # y's own rounding
@@ -95,8 +99,6 @@ def test_activations(T, act, dtype):
     check(y, x, idx, w, W, act, dtype)
 
 
-# From 24 tokens an expert on, bfloat16 with whole 128s: the laid-out products, where act(W1 x)
-# is rounded once (half a step of bfloat16).
 MANY = [  # T, d, f, E, k
     (24, 128, 128, 1, 1), (48, 128, 256, 2, 1), (47, 128, 128, 1, 1), (128, 256, 128, 1, 1), (129, 384, 128, 1, 1),
     (300, 128, 640, 3, 2), (257, 640, 128, 4, 2), (600, 128, 128, 16, 1), (512, 256, 384, 2, 2), (33, 128, 1152, 1, 1),
@@ -113,23 +115,41 @@ def test_many_tokens(T, d, f, E, k):
     check(y, x, idx, w, W, "gelu_tanh", "bf16")
 
 
+# The laid-out products, where act(W1 x) is rounded once (half a step of bfloat16).
+LAID = [(3200, 128, 1024, 3, 1), (1500, 128, 1152, 2, 2), (450, 1024, 1024, 1, 1), (127, 1536, 1024, 2, 3),
+        (2050, 512, 640, 8, 2), (400, 2048, 1024, 16, 1), (24, 2048, 8320, 1, 1), (161, 1280, 2048, 1, 1),
+        # inputs, rows or both past whole 128s
+        (1030, 288, 1184, 2, 2), (420, 1056, 1056, 2, 1), (1024, 416, 2080, 7, 1), (200, 160, 6400, 1, 2),
+        (2048, 512, 544, 8, 2), (64, 1056, 6016, 2, 1), (4100, 96, 1056, 2, 1), (13000, 32, 1024, 5, 1), (700, 1152, 2144, 24, 1)]
+
+
+@pytest.mark.parametrize("T,d,f,E,k", LAID)
+def test_many_tokens_laid_out(T, d, f, E, k):
+    assert laid_out(T * k, d, f, E, "bf16")
+    x, idx, w, W = inputs(T, d, f, E, k, "bf16", T + d + f)
+    y = run(x.cuda(), dev(idx), dev(w), [dev(v) for v in W], E, f, k, "bf16", "gelu_tanh")
+    check(y, x, idx, w, W, "gelu_tanh", "bf16")
+
+
+@pytest.mark.parametrize("T,d,f", [(320, 128, 256), (1100, 128, 1024), (800, 160, 1184)])
 @pytest.mark.parametrize("act", ["identity", "relu", "gelu_erf"])
-def test_many_tokens_uneven(act):
-    T, d, f, E, k = 320, 128, 256, 6, 3
+def test_many_tokens_uneven(act, T, d, f):
+    E, k = 6, 3
     x, idx, w, W = inputs(T, d, f, E, k, "bf16", 9, np.array([0.5, 0.0, 0.3, 0.15, 0.04, 0.01]))
     idx[::7, 1] = -1
-    idx[300:] = E
+    idx[T - 20:] = E
     w[(idx < 0) | (idx >= E)] = np.nan
-    x[300:] = float("inf")
+    x[T - 20:] = float("inf")
     y = run(x.cuda(), dev(idx), dev(w), [dev(v) for v in W], E, f, k, "bf16", act)
-    x[300:] = 0
+    x[T - 20:] = 0
     check(y, x, idx, np.nan_to_num(w), W, act, "bf16")
     again = run(x.cuda(), dev(idx), dev(w), [dev(v) for v in W], E, f, k, "bf16", act)
-    assert torch.equal(y[:300], again[:300]) and (y[300:] == 0).all()
+    assert torch.equal(y, again) and (y[T - 20:] == 0).all()
 
 
-def test_many_tokens_infinities_stay_with_their_token():
-    T, d, f, E, k = 60, 128, 128, 2, 1
+@pytest.mark.parametrize("T,d,f", [(60, 128, 128), (3200, 128, 1024), (420, 1056, 1056)])
+def test_many_tokens_infinities_stay_with_their_token(T, d, f):
+    E, k = 2, 1
     x, idx, w, W = inputs(T, d, f, E, k, "bf16", 1)
     ref = run(x.cuda(), dev(idx), dev(w), [dev(v) for v in W], E, f, k, "bf16", "relu")
     bad = x.clone()
@@ -139,10 +159,10 @@ def test_many_tokens_infinities_stay_with_their_token():
     assert torch.equal(y[rest], ref[rest]) and torch.isnan(y[8]).all() and not torch.isfinite(y[3]).any()
 
 
-@pytest.mark.parametrize("d,f", [(160, 96), (96, 160), (416, 128)])
+@pytest.mark.parametrize("d,f", [(160, 96), (160, 1056), (416, 1024), (96, 1184)])
 def test_many_tokens_far_scales_at_the_rows_ends(d, f):
     """The last scale of a row NaN, or with codes of 0 the largest: no other row or token sees it."""
-    T, E, k = 80, 2, 1
+    T, E, k = 80 if f < 1024 else (3 << 27) // (d * f) + 1, 2, 1
     x, idx, w, W = inputs(T, d, f, E, k, "bf16", d)
     W[2][:, 5, -16:] = 0
     W[3][:, 5, -1] = 254
