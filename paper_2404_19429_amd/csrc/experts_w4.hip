@@ -10,8 +10,8 @@
 // A matrix instruction wants lane (i = lane & 15, q = lane >> 4) to hold row i, and 16
 // rows are 16 cache lines: loads straight into that order are bound by the L1's line
 // look-ups (64 per load; measured, 48 tokens against 16 experts of 1024 x 4096: 19 + 26
-// us where 36 + 36 MB take 14, and the two products take 12.3 + 13.6 now).  So a wave loads 8 rows x 256 inputs at a time, whole
-// 128-byte lines, and turns them in LDS.  Of a row's 256 inputs lane q gets 32 q ..
+// us where 36 + 36 MB take 14, and the two products take 12.5 + 13.7 now).  So a wave loads
+// 8 rows x 256 inputs at a time, whole 128-byte lines, and turns them in LDS.  Of a row's 256 inputs lane q gets 32 q ..
 // 32 q + 31 of each half, one scale group; MFMA j of a half takes inputs 8 j .. 8 j + 7
 // of these from weights and tokens alike, so the product's k-index stands for the same
 // input in both operands, which is all a dot product needs.
@@ -423,10 +423,12 @@ __global__ __launch_bounds__(64 * kW4Waves, kW4PerSimd) void w4_product_kernel(W
 // ------------------------------------------------------------- blocks of 128 rows
 // Where there are blocks enough, four waves take 32 rows each over the whole K (of
 // blockIdx.z's split), and the tokens' inputs go through LDS once for all of them: with K
-// split over the waves every 16 or 32 rows fetched them anew, four times the weights' bytes.  (Blocks of 64 rows, twice as many: 48
-// tokens, 16 experts of 1024 x 4096, 12.3 -> 12.0 us for the first product and 14.1 -> 17.0
-// for the second, whose inputs are two parts.  Three steps on their way instead of one: 14.2
-// and 18.3; the registers, and the loads after the last step, cost more than they hide.)
+// split over the waves every 16 or 32 rows fetched them anew, four times the weights' bytes.
+// Bound by the latency of a block's steps: 48 tokens, 16 experts of 1024 x 4096, 12.5 and
+// 13.7 us for 36 MB each, and still 10-11 with everything in cache.  (Blocks of 64 rows,
+// twice as many: 12.0 for the first product, 17.0 for the second, whose inputs are two parts.
+// Three steps on their way instead of one: 14.2 and 18.3; the registers, and the loads after
+// the last step, cost more than they hide.)
 template <typename T, bool FIRST, int NS, int NO, bool FULL, int HOW>
 __global__ __launch_bounds__(256, NS == 3 ? 1 : 2) void w4_rows_kernel(W4Args a) {
   constexpr int RT = 2, WR = 16 * RT, BR = 4 * WR;   // rows of a wave, of the block
@@ -552,7 +554,8 @@ __global__ __launch_bounds__(256, NS == 3 ? 1 : 2) void w4_rows_kernel(W4Args a)
 
 // Thread: four columns of a token (blockIdx.y; further ones past the grid's limit).  NR
 // choices at a time, every load of them and of their SP splits ahead of the sums: with few
-// tokens the kernel is the latency of its loads.
+// tokens the kernel is the latency of its loads (512 tokens, top-2, four splits: 6.8 us;
+// four choices at a time and the splits one by one 7.9).
 template <typename T, int SP, int NR>
 __global__ __launch_bounds__(256) void w4_combine_kernel(const float* __restrict__ O, const int32_t* __restrict__ idx,
                                                          const float* __restrict__ w, T* __restrict__ y, int64_t T_tokens,
@@ -612,7 +615,10 @@ static void launch_w4_combine(const moe_w4_cfg& c, const float* O, const int32_t
 // again.  The tokens' rows are laid out by expert, padded to 16, in the order in which the
 // matrix instructions take them (x by w4_pack_kernel, act(W1 x) by the first product), so
 // both sides of a 128-row x 160-token block go through LDS in whole lines: the codes of 256
-// inputs, the tokens' values of 64, each with the next on its way.  Four waves, 64 rows by half the tokens each.
+// inputs, the tokens' values of 64, each with the next on its way.  Four waves, 64 rows by
+// half the tokens each.  512 tokens, top-2 of 8 experts of 2048 x 8192: 51 and 52 us for 34
+// GFLOP each, bound by what stands beside the matrix instructions (a code conversion for
+// every four of them, both sides' LDS reads) with one round of two blocks a CU.
 // The tokens' rows are padded to whole 128s with zeros; rows and inputs past the matrix are
 // read inside it (WHOLE: there are none), such codes taken as zeros and such rows written as
 // zeros, which the second product meets as its inputs' padding.
@@ -970,15 +976,14 @@ static int launch_w4_rows(W4Args a, int gy, hipStream_t s) {
     return ((int64_t)(a.N / (16 * rt)) * gy + places - 1) / places * (3 + (steps + wv - 1) / wv);
   };
   const int waves = cost(kW4Waves) < cost(4) ? kW4Waves : 4;
-  for (; a.tile0 < gy; a.tile0 += kMaxGridY)
-    how([&](auto h) {
-      constexpr int H = decltype(h)::value;
-      auto go = [&](auto kern, size_t lds) {
-        hipLaunchKernelGGL(kern, dim3(a.N / (16 * rt), std::min(kMaxGridY, gy - a.tile0)), dim3(64 * waves), waves * lds, s, a);
-      };
-      if (rt == 2) go(w4_product_kernel<T, FIRST, NS, NO, 2, FULL, H>, sizeof(W4Lds<2>));
-      else go(w4_product_kernel<T, FIRST, NS, NO, 1, FULL, H>, sizeof(W4Lds<1>));
-    });
+  how([&](auto h) {   // (gy is within a grid's limit: more tiles are blocks of 128 rows)
+    constexpr int H = decltype(h)::value;
+    auto go = [&](auto kern, size_t lds) {
+      hipLaunchKernelGGL(kern, dim3(a.N / (16 * rt), gy), dim3(64 * waves), waves * lds, s, a);
+    };
+    if (rt == 2) go(w4_product_kernel<T, FIRST, NS, NO, 2, FULL, H>, sizeof(W4Lds<2>));
+    else go(w4_product_kernel<T, FIRST, NS, NO, 1, FULL, H>, sizeof(W4Lds<1>));
+  });
   return 1;
 }
 template <typename T, bool FIRST, int NS, int NO>
