@@ -11,8 +11,8 @@
 // rows are 16 cache lines: loads straight into that order are bound by the L1's line
 // look-ups (64 per load; measured, 48 tokens against 16 experts of 1024 x 4096: 19 + 26
 // us where 36 + 36 MB take 14, and the two products take 12.5 + 13.7 now).  So a wave loads
-// 8 rows x 256 inputs at a time, whole 128-byte lines, and turns them in LDS.  Of a row's 256 inputs lane q gets 32 q ..
-// 32 q + 31 of each half, one scale group; MFMA j of a half takes inputs 8 j .. 8 j + 7
+// 8 rows x 256 inputs at a time, whole 128-byte lines, and turns them in LDS.  Of a row's
+// 256 inputs lane q gets 32 q .. 32 q + 31 of each half, one scale group; MFMA j of a half takes inputs 8 j .. 8 j + 7
 // of these from weights and tokens alike, so the product's k-index stands for the same
 // input in both operands, which is all a dot product needs.
 #include <type_traits>
@@ -328,7 +328,10 @@ __device__ __forceinline__ void w4_tile(const W4Args& a, int waves, int cnt, con
 
 // How a block finds its expert and tokens (blockIdx.y): by the list's tiles; every wave by
 // itself in up to 64 choices (a choice, if it is the first of its expert, or an expert); or the
-// block in up to kW4Scan: by expert, or by choice.
+// block in up to kW4Scan: by expert, or by choice.  (Whole calls, us.  By wave and by block:
+// one token, top-2 of 16 experts of 1024 x 4096 13.0 and 13.9, 32 tokens 29.4 and 29.1.  By
+// choice and by expert: the one token 13.0 and 19.8; top-6 of 160 experts of 1536 x 768, 11
+// tokens 32.2 and 36.9, 20 tokens 46.2 both.)
 enum { kFindTiles, kFindWave, kFindExpert, kFindChoice };
 // list and their number (0: none, or another block has them).  first() runs as soon as the
 // expert is known.  Four or eight waves; every one ends with the same answer.
