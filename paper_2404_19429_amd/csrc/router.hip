@@ -348,7 +348,10 @@ __global__ __launch_bounds__(64 * kRouteWaves) void route_kernel(RouteArgs a) {
     }
     bool amb = m > kRouteFar;   // (among them +inf)
     float z = 1.f;
-    if (soft) m = from_order_key(team_max<LPT>(order_key(m)));
+    if (soft) {
+      m = from_order_key(team_max<LPT>(order_key(m)));
+      amb |= m <= -kRouteFar && m > kRouteNone;   // no live logit above the clamp: the shares are those of the logits themselves
+    }
     if (use_c || use_z) {
       // scores; 0 for a masked expert but in rows without any other
       float x[NV];

@@ -1,0 +1,36 @@
+"""The router at the ends of float's range, against the float64 oracle."""
+import numpy as np
+import pytest
+
+from tests.test_gpu_router import check
+
+pytestmark = pytest.mark.gpu
+L = pytest.importorskip("paper_2404_19429_amd.lancet_moe", reason="library not built")
+
+LOW = np.finfo(np.float32).min
+
+
+def low_rows(E):
+    """Rows whose live logits are all finite and at or below -1e30."""
+    l = np.full((6, E), -np.inf, np.float32)
+    l[0, E // 2] = LOW                                        # one expert left
+    l[1, ::2] = -1e31
+    l[2] = -1e31 * np.arange(1, E + 1, dtype=np.float32)      # apart: the first takes everything
+    l[3] = LOW
+    l[4, 1], l[4, E - 1] = -2e38, -3e38
+    l[5, 0], l[5, E - 1] = np.nan, -1e30
+    return l
+
+
+@pytest.mark.parametrize("renorm", [0, 1])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("E,k", [(4, 2), (16, 2), (64, 8), (200, 6), (512, 16)])
+def test_live_logits_below_1e30(E, k, score, renorm):
+    l = low_rows(E)
+    kw = dict(score=score, renorm=renorm, scale=2.5)
+    bias = 0.1 * np.random.default_rng(E).standard_normal(E).astype(np.float32)
+    check(l, k, **kw)
+    check(l, k, bias, **kw)
+    check(l, k, np.linspace(-1, 0, E).astype(np.float32), **kw)
+    if E % 16 == 0:
+        check(l, k, bias, groups=4, top_groups=2, **kw)
