@@ -408,7 +408,9 @@ __global__ __launch_bounds__(64 * kRouteWaves) void route_kernel(RouteArgs a) {
       }
       const float gv = x > kRouteNone ? (y > kRouteNone ? x + y : x) : kRouteMasked;
       const float big = x > kRouteNone ? fmaxf(fabsf(x), y > kRouteNone ? fabsf(y) : 0.f) : 0.f;
-      const float eps = kRouteGroupEps * fmaxf(1.f, from_order_key(team_max<LPT>(order_key(big))));
+      const float most = from_order_key(team_max<LPT>(order_key(big)));
+      amb |= most >= kRouteFar;   // a clamped value keeps its place in the order, but not in a sum
+      const float eps = kRouteGroupEps * fmaxf(1.f, most);
       // The best groups one after the other (the lane in the low bits keeps them apart).
       const int gk = j < a.groups ? (order_key(gv) & ~15) | (15 - j) : (int)0x80000000;
       int rest = gk, last = 0;

@@ -34,3 +34,25 @@ def test_live_logits_below_1e30(E, k, score, renorm):
     check(l, k, np.linspace(-1, 0, E).astype(np.float32), **kw)
     if E % 16 == 0:
         check(l, k, bias, groups=4, top_groups=2, **kw)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("E", [16, 64, 256])
+def test_groups_of_far_biases(E, score):
+    """Group values are sums: of two biases past 1e30 as of any others."""
+    rng = np.random.default_rng(E)
+    n = E // 4
+    l = rng.standard_normal((32, E)).astype(np.float32)
+    bias = 0.1 * rng.standard_normal(E).astype(np.float32)
+    bias[0], bias[n], bias[n + 1] = 5e30, 2e30, 5e29          # 5e30 against 2.5e30
+    for top in (1, 2):
+        check(l, 2, bias, score=score, groups=4, top_groups=top)
+    bias[[0, n]] = np.inf                                     # infinite sums tie: the lowest group
+    bias[2], bias[n + 1] = -1.0, 5e29
+    check(l, 2, bias, score=score, groups=4, top_groups=1)
+    low = np.full(E, LOW, np.float32)                         # every group's second value is far below
+    low[::n] = 0.0
+    low[n], low[n + 1] = -2e30, -2e30                         # two of them are above one of the lowest
+    for k in (1, 2):
+        check(l, k, low, score=score, groups=4, top_groups=1)
+        check(l, k, low, score=score, groups=4, top_groups=3)
