@@ -489,6 +489,7 @@ __global__ __launch_bounds__(64 * kRouteWaves) void route_kernel(RouteArgs a) {
     if (a.renorm) {
       sum = team_sum<LPT>(sum);
       f = sum > 0.f ? a.scale / sum : 0.f;
+      amb |= f == INFINITY;   // a weight is at most the scale, whatever its factors are
     } else if (soft) {
       f = a.scale / z;
     }

@@ -56,3 +56,17 @@ def test_groups_of_far_biases(E, score):
     for k in (1, 2):
         check(l, k, low, score=score, groups=4, top_groups=1)
         check(l, k, low, score=score, groups=4, top_groups=3)
+
+
+@pytest.mark.parametrize("E,k", [(16, 2), (64, 8), (256, 8)])
+def test_largest_scales_over_small_scores(E, k):
+    """scale * s / sum is at most scale, whatever the sum is next to it."""
+    l = np.full((8, E), -75.0, np.float32) - np.arange(8, dtype=np.float32)[:, None] / 4
+    l += np.linspace(-1, 1, E).astype(np.float32)
+    check(l, k, score="sigmoid", scale=1e7)
+    check(l, k, score="sigmoid", scale=1e38)
+    l[:, 0] = 0.0                                             # a softmax whose largest is not chosen
+    bias = np.linspace(1, 2, E).astype(np.float32)
+    bias[0] = -9.0
+    check(l, k, bias, score="softmax", scale=1e7)
+    check(l, k, bias, score="softmax", scale=1e38)
