@@ -481,7 +481,10 @@ __global__ __launch_bounds__(64 * kRouteWaves) void route_kernel(RouteArgs a) {
         e[q] = 4 * (__builtin_ctz(kept_at[q]) + LPT * (i >> 2)) + (i & 3);
         const float l = row[e[q]];
         s[q] = soft ? expf(l - m) : 1.f / (1.f + expf(-l));
-        amb |= (soft ? l - m : l) < -80.f && (a.renorm || !soft);   // next to float's smallest numbers
+        // Next to float's smallest numbers.  (A plain softmax's weight is its share times the scale:
+        // below e^-210 that is none whatever the scale is.)
+        const float x = soft ? l - m : l;
+        amb |= x < -80.f && (a.renorm || !soft || x > -210.f);
       }
       sum += s[q];
     }

@@ -70,3 +70,13 @@ def test_largest_scales_over_small_scores(E, k):
     bias[0] = -9.0
     check(l, k, bias, score="softmax", scale=1e7)
     check(l, k, bias, score="softmax", scale=1e38)
+
+
+def test_large_scales_of_shares_that_underflow():
+    """scale * s where s is below float's smallest numbers and the product is not."""
+    E = 32
+    l = np.zeros((40, E), np.float32)
+    l[:, 1:] = -70.0 - 2.5 * np.arange(40, dtype=np.float32)[:, None] - np.arange(E - 1, dtype=np.float32) / 8
+    for scale in (1.0, 1e10, 1e38):
+        check(l, 4, score="softmax", renorm=0, scale=scale)
+        check(l, 4, score="sigmoid", renorm=0, scale=scale)
