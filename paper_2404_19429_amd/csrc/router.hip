@@ -672,7 +672,7 @@ __global__ __launch_bounds__(64 * kBwdWaves) void route_bwd_softmax_kernel(Route
   const int64_t t = a.first + ((int64_t)blockIdx.x * kBwdWaves + (threadIdx.x >> 6)) * 4 + team;
   const bool on = t < a.T;
   const float* row = a.logits + (on ? t : a.T - 1) * a.E;
-  float l[NV], m = kRouteMasked, z = 0.f;
+  float l[NV], m = -INFINITY, z = 0.f;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int x = j + 16 * i;
@@ -683,7 +683,7 @@ __global__ __launch_bounds__(64 * kBwdWaves) void route_bwd_softmax_kernel(Route
   const float v = choice_grad<16>(a, t, j, on, e, G);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    l[i] = l[i] > -INFINITY ? fmaxf(l[i], kRouteNone) : kRouteMasked;   // masked: apart from every other
+    l[i] = l[i] > -INFINITY ? l[i] : -INFINITY;   // (a NaN compares false)
     m = fmaxf(m, l[i]);
     mine[j + 16 * i] = 0.f;
   }
@@ -691,7 +691,7 @@ __global__ __launch_bounds__(64 * kBwdWaves) void route_bwd_softmax_kernel(Route
   float p[NV];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    p[i] = l[i] < kRouteNone ? 0.f : l[i] == m ? 1.f : expf(l[i] - m);   // (+inf logits: an even share)
+    p[i] = l[i] == -INFINITY ? 0.f : l[i] == m ? 1.f : expf(l[i] - m);   // (+inf logits: an even share)
     z += p[i];
   }
   z = team_sum<16>(z);

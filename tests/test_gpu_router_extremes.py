@@ -2,7 +2,8 @@
 import numpy as np
 import pytest
 
-from tests.test_gpu_router import check
+from oracle import operators_oracle as O
+from tests.test_gpu_router import check, check_bwd
 
 pytestmark = pytest.mark.gpu
 L = pytest.importorskip("paper_2404_19429_amd.lancet_moe", reason="library not built")
@@ -80,3 +81,17 @@ def test_large_scales_of_shares_that_underflow():
     for scale in (1.0, 1e10, 1e38):
         check(l, 4, score="softmax", renorm=0, scale=scale)
         check(l, 4, score="sigmoid", renorm=0, scale=scale)
+
+
+@pytest.mark.parametrize("E", [4, 16, 40, 100, 200, 512])
+def test_gradient_of_logits_below_2e38(E):
+    """Shares of a plain softmax whose logits differ far below zero, or are all there."""
+    l = low_rows(E)
+    l[5, 1:E - 1] = -2.5e38
+    k = 2
+    idx = O.route(l, None, k, "softmax", 0)[0]
+    idx[5] = [E - 1, 1]                                       # a choice with no share at all
+    dw = np.random.default_rng(E).standard_normal((6, k))
+    for score in ("softmax", "sigmoid"):
+        for renorm in (0, 1):
+            check_bwd(l, idx, dw, score, renorm, 1.5)
