@@ -617,7 +617,8 @@ struct RouteBwdArgs {
 constexpr int kBwdWaves = 4;
 constexpr int kBwdLds = 2048;   // floats of a wave
 
-// Lane (token i / KP, choice i % KP) of the wave's tokens: its part of the gradient, and G.
+// Lane (token i / KP, choice i % KP) of the wave's tokens: its part of the gradient, and G
+// (renorm: G / scale, from shares, which no scale takes past float's range).
 template <int KP>
 __device__ __forceinline__ float choice_grad(const RouteBwdArgs& a, int64_t t, int r, bool on, int& e, float& G) {
   e = -1;
@@ -630,12 +631,12 @@ __device__ __forceinline__ float choice_grad(const RouteBwdArgs& a, int64_t t, i
       g = a.dw[t * a.k + r];
     }
   }
-  G = w * g;
+  G = (a.renorm ? w / a.scale : w) * g;
   if constexpr (KP >= 2) G += dpp_f<0xB1>(G);
   if constexpr (KP >= 4) G += dpp_f<0x4E>(G);
   if constexpr (KP >= 8) G += dpp_f<0x141>(G);    // row_half_mirror
   if constexpr (KP >= 16) G += dpp_f<0x140>(G);   // row_mirror
-  float v = w * (a.renorm ? g - G / a.scale : g);
+  float v = w * (a.renorm ? g - G : g);
   if (a.score == MOE_SCORE_SIGMOID && e >= 0) v *= 1.f / (1.f + expf(a.logits[t * a.E + e]));   // 1 - s
   return v;
 }

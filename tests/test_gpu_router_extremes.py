@@ -95,3 +95,12 @@ def test_gradient_of_logits_below_2e38(E):
     for score in ("softmax", "sigmoid"):
         for renorm in (0, 1):
             check_bwd(l, idx, dw, score, renorm, 1.5)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("E,k", [(16, 2), (64, 8), (512, 16)])
+def test_gradient_of_the_largest_scale(E, k, score):
+    """Renormalised weights of up to 1e38: their mean gradient is an ordinary number."""
+    rng = np.random.default_rng(E)
+    l = rng.standard_normal((20, E)).astype(np.float32)
+    check_bwd(l, O.route(l, None, k, score, 1)[0], 10 + rng.random((20, k)), score, 1, 1e38)
