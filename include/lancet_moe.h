@@ -329,14 +329,15 @@ moe_status moe_route(const moe_route_cfg* cfg, const float* logits, const float*
  *   sigmoid, renorm: dlogits[e_r] = w_r (1 - s_r)(dw_r - G / scale); plain:
  *     dlogits[e_r] = w_r (1 - s_r) dw_r; 0 elsewhere.
  *   An idx outside 0..E-1 takes no part, whatever its w and dw hold.  A row that
- *   names an expert twice gets the sum of both. */
+ *   names an expert twice gets the sum of both.  dlogits may alias no input. */
 moe_status moe_route_bwd(const moe_route_cfg* cfg, const float* logits, const int32_t* idx, const float* w,
                          const float* dw, float* dlogits, moe_stream_t stream);
 
 /* moe_bwd_dx for a layer whose idx and w come from moe_route: the same chain, with
  * moe_route_bwd in the place of the softmax gate's backward.  cfg->renorm is not
  * used; route's T, E and k equal cfg's.  Also out: dw [T][k] float = <dy[t],
- * expert_out> of each kept choice (0: dropped), the gradient at w. */
+ * expert_out> of each kept choice (0: dropped), the gradient at w.  dw and dlogits may
+ * alias neither each other nor another array. */
 moe_status moe_bwd_dx_route(const moe_cfg* cfg, const moe_route_cfg* route, const void* Wg, const float* logits,
                             const int32_t* idx, const float* w, const int32_t* slot, const int32_t* row_begin,
                             const int32_t* row_end, const void* H, const void* expert_out, const void* W1p,

@@ -409,7 +409,7 @@ moe_status moe_route_bwd(const moe_route_cfg* cfg, const float* logits, const in
   const char* fn = "moe_route_bwd";
   CHECK(check_route(cfg, fn));
   REQUIRE_TPTR(logits); REQUIRE_TPTR(idx); REQUIRE_TPTR(w); REQUIRE_TPTR(dw); REQUIRE_TPTR(dlogits);
-  if (cfg->T > 0 && (dlogits == logits || dlogits == dw || dlogits == w))
+  if (cfg->T > 0 && (dlogits == logits || dlogits == dw || dlogits == w || (const void*)dlogits == (const void*)idx))
     return fail(MOE_EINVAL, "%s: dlogits may not alias an input", fn);
   CHECK(check_device(fn));
   lmoe::launch_route_bwd(*cfg, logits, idx, w, dw, dlogits, (hipStream_t)stream);
@@ -430,8 +430,11 @@ moe_status moe_bwd_dx_route(const moe_cfg* cfg, const moe_route_cfg* route, cons
   OPTIONAL_PTR(row_begin); REQUIRE_PTR(row_end); REQUIRE_PTR(H); REQUIRE_PTR(expert_out);
   REQUIRE_PTR(W1p); REQUIRE_PTR(W2p); REQUIRE_TPTR(dy); REQUIRE_PTR(dO); REQUIRE_PTR(dH); REQUIRE_PTR(dXe);
   REQUIRE_TPTR(dw); REQUIRE_TPTR(dlogits); REQUIRE_TPTR(dx);
-  if (cfg->T > 0 && (dlogits == logits || dlogits == dw || dlogits == w || dw == w))
-    return fail(MOE_EINVAL, "%s: dw and dlogits may not alias each other or an input", fn);
+  // (dw is written before the logits, idx and w are read again)
+  const void* others[] = {Wg, logits, idx, w, slot, row_begin, row_end, H, expert_out, W1p, W2p, dy, dO, dH, dXe, dx};
+  bool twice = dw == dlogits;
+  for (const void* p : others) twice = twice || p == (const void*)dw || p == (const void*)dlogits;
+  if (cfg->T > 0 && twice) return fail(MOE_EINVAL, "%s: dw and dlogits may not alias each other or another array", fn);
   const size_t need = lmoe::bwd_dx_ws_bytes(*cfg);
   if (need > 0) {
     if (ws == nullptr || ws_bytes < need)
