@@ -175,11 +175,12 @@ moe_status moe_dispatch_noalloc(const moe_cfg* cfg, const void* x, const int32_t
  * importance, the sum of their top-k gating scores, before they are assigned
  * to experts, so the least important tokens are dropped first).
  *   importance[t] = sum over r of softmax(logits[t])[idx[t][r]] (softmax over
- *   all E experts, not renormalised), evaluated in double and rounded once to
- *   float.  The tokens are visited by importance descending, equal importance
- *   in token order, each token's choices in rank order; an assignment takes
- *   the next free row of its expert below C, else it is dropped.  An expert's
- *   rows therefore hold its kept tokens by descending importance.
+ *   all E experts, not renormalised; a -inf or NaN logit has no share, +inf
+ *   logits share evenly), evaluated in double and rounded once to float.  The
+ *   tokens are visited by importance descending, equal importance in token
+ *   order, each token's choices in rank order; an assignment takes the next
+ *   free row of its expert below C, else it is dropped.  An expert's rows
+ *   therefore hold its kept tokens by descending importance.
  *   In: x [T][d] dtype, logits [T][E] float (moe_gate_topk), idx [T][k] int32.
  *   Out: fill [E] int32 = rows taken (min(C, demand_e)); slot [T][k] int32
  *   (token order; -1 = dropped); send_buf as in moe_dispatch, rows 0..fill_e-1;
@@ -332,6 +333,14 @@ moe_status moe_route(const moe_route_cfg* cfg, const float* logits, const float*
  *   names an expert twice gets the sum of both.  dlogits may alias no input. */
 moe_status moe_route_bwd(const moe_route_cfg* cfg, const float* logits, const int32_t* idx, const float* w,
                          const float* dw, float* dlogits, moe_stream_t stream);
+
+/* moe_dispatch_bpr for a layer whose idx come from moe_route: importance[t] = the sum
+ * over the token's choices of the router's scores s (route->score; the balance bias,
+ * renorm and scale play no part), so the tokens that the router scores least are
+ * dropped first; a token without a choice comes last.  route's T, E and k equal cfg's. */
+moe_status moe_dispatch_bpr_route(const moe_cfg* cfg, const moe_route_cfg* route, const void* x, const float* logits,
+                                  const int32_t* idx, int32_t* fill, int32_t* slot, void* send_buf, int32_t* order,
+                                  void* ws, size_t ws_bytes, moe_stream_t stream);
 
 /* moe_bwd_dx for a layer whose idx and w come from moe_route: the same chain, with
  * moe_route_bwd in the place of the softmax gate's backward.  cfg->renorm is not

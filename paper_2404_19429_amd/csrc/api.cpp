@@ -190,10 +190,10 @@ moe_status moe_dispatch_noalloc(const moe_cfg* cfg, const void* x, const int32_t
   return check_launch(fn);
 }
 
-moe_status moe_dispatch_bpr(const moe_cfg* cfg, const void* x, const float* logits, const int32_t* idx,
-                            int32_t* fill, int32_t* slot, void* send_buf, int32_t* order, void* ws, size_t ws_bytes,
-                            moe_stream_t stream) {
-  const char* fn = "moe_dispatch_bpr";
+namespace {
+
+moe_status check_bpr(const moe_cfg* cfg, const void* x, const float* logits, const int32_t* idx, int32_t* fill,
+                     int32_t* slot, void* send_buf, int32_t* order, void* ws, size_t ws_bytes, const char* fn) {
   CHECK(check_cfg(cfg, fn, false));
   REQUIRE_TPTR(x); REQUIRE_TPTR(logits); REQUIRE_TPTR(idx); REQUIRE_PTR(fill);
   REQUIRE_TPTR(slot); REQUIRE_PTR(send_buf); OPTIONAL_PTR(order);
@@ -203,6 +203,16 @@ moe_status moe_dispatch_bpr(const moe_cfg* cfg, const void* x, const float* logi
       return fail(MOE_EWORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need, ws ? ws_bytes : 0);
     REQUIRE_PTR(ws);
   }
+  return MOE_OK;
+}
+
+}  // namespace
+
+moe_status moe_dispatch_bpr(const moe_cfg* cfg, const void* x, const float* logits, const int32_t* idx,
+                            int32_t* fill, int32_t* slot, void* send_buf, int32_t* order, void* ws, size_t ws_bytes,
+                            moe_stream_t stream) {
+  const char* fn = "moe_dispatch_bpr";
+  CHECK(check_bpr(cfg, x, logits, idx, fill, slot, send_buf, order, ws, ws_bytes, fn));
   CHECK(check_device(fn));
   lmoe::launch_dispatch_bpr(*cfg, x, logits, idx, fill, slot, send_buf, order, ws, (hipStream_t)stream);
   return check_launch(fn);
@@ -386,6 +396,15 @@ moe_status check_route(const moe_route_cfg* c, const char* fn) {
   return MOE_OK;
 }
 
+// The router of a layer.
+moe_status check_route_of(const moe_route_cfg* route, const moe_cfg* cfg, const char* fn) {
+  CHECK(check_cfg(cfg, fn, false));
+  CHECK(check_route(route, fn));
+  if (route->T != cfg->T || route->E != cfg->E || route->k != cfg->k)
+    return fail(MOE_EINVAL, "%s: cfg and route differ in T, E or k", fn);
+  return MOE_OK;
+}
+
 }  // namespace
 
 moe_status moe_route(const moe_route_cfg* cfg, const float* logits, const float* bias, int32_t* idx, float* w,
@@ -416,6 +435,17 @@ moe_status moe_route_bwd(const moe_route_cfg* cfg, const float* logits, const in
   return check_launch(fn);
 }
 
+moe_status moe_dispatch_bpr_route(const moe_cfg* cfg, const moe_route_cfg* route, const void* x, const float* logits,
+                                  const int32_t* idx, int32_t* fill, int32_t* slot, void* send_buf, int32_t* order,
+                                  void* ws, size_t ws_bytes, moe_stream_t stream) {
+  const char* fn = "moe_dispatch_bpr_route";
+  CHECK(check_route_of(route, cfg, fn));
+  CHECK(check_bpr(cfg, x, logits, idx, fill, slot, send_buf, order, ws, ws_bytes, fn));
+  CHECK(check_device(fn));
+  lmoe::launch_dispatch_bpr(*cfg, x, logits, idx, fill, slot, send_buf, order, ws, (hipStream_t)stream, route->score);
+  return check_launch(fn);
+}
+
 moe_status moe_bwd_dx_route(const moe_cfg* cfg, const moe_route_cfg* route, const void* Wg, const float* logits,
                             const int32_t* idx, const float* w, const int32_t* slot, const int32_t* row_begin,
                             const int32_t* row_end, const void* H, const void* expert_out, const void* W1p,
@@ -423,9 +453,7 @@ moe_status moe_bwd_dx_route(const moe_cfg* cfg, const moe_route_cfg* route, cons
                             float* dlogits, void* dx, void* ws, size_t ws_bytes, moe_stream_t stream) {
   const char* fn = "moe_bwd_dx_route";
   CHECK(check_cfg(cfg, fn, true));
-  CHECK(check_route(route, fn));
-  if (route->T != cfg->T || route->E != cfg->E || route->k != cfg->k)
-    return fail(MOE_EINVAL, "%s: cfg and route differ in T, E or k", fn);
+  CHECK(check_route_of(route, cfg, fn));
   REQUIRE_PTR(Wg); REQUIRE_TPTR(logits); REQUIRE_TPTR(idx); REQUIRE_TPTR(w); REQUIRE_TPTR(slot);
   OPTIONAL_PTR(row_begin); REQUIRE_PTR(row_end); REQUIRE_PTR(H); REQUIRE_PTR(expert_out);
   REQUIRE_PTR(W1p); REQUIRE_PTR(W2p); REQUIRE_TPTR(dy); REQUIRE_PTR(dO); REQUIRE_PTR(dH); REQUIRE_PTR(dXe);

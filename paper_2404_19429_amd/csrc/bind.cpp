@@ -27,6 +27,7 @@ struct Abi {   // addresses in the loaded library, given by init()
   decltype(&moe_block_chunked) block_chunked;
   decltype(&moe_route) route;
   decltype(&moe_route_bwd) route_bwd;
+  decltype(&moe_dispatch_bpr_route) dispatch_bpr_route;
   decltype(&moe_bwd_dx_route) bwd_dx_route;
   decltype(&moe_w4_quantize) w4_quantize;
   decltype(&moe_experts_w4_workspace_bytes) experts_w4_workspace_bytes;
@@ -233,23 +234,35 @@ PyObject* dispatch_any(PyObject* const* a, bool ws_arg) {
 ENTRY(dispatch) { return entry(n, 9, [&] { return dispatch_any(a, true); }); }
 ENTRY(dispatch_noalloc) { return entry(n, 8, [&] { return dispatch_any(a, false); }); }
 
+// cfg, x, logits, idx, fill, slot, send_buf, order, ws, stream
+template <typename F>
+PyObject* dispatch_bpr_any(const moe_cfg* c, PyObject* const* a, F&& call) {
+  const auto dt = dtype_of(c);
+  const Num T = c->T, d = c->d_model, E = c->E, k = c->k;
+  const size_t need = g_abi.workspace_bytes(c, MOE_CALL_DISPATCH_BPR);
+  const void* x = ptr(a[0], "x", dt, T * d);
+  const float* logits = (const float*)ptr(a[1], "logits", kF32, T * E);
+  const int32_t* idx = (const int32_t*)ptr(a[2], "idx", kI32, T * k);
+  int32_t* fill = (int32_t*)ptr(a[3], "fill", kI32, E);
+  int32_t* slot = (int32_t*)ptr(a[4], "slot", kI32, T * k);
+  void* send = ptr(a[5], "send_buf", dt, expert_numel(c, d));
+  int32_t* order = (int32_t*)ptr(a[6], "order", kI32, T, true);
+  void* ws = ptr(a[7], "ws", at::kByte, need, need == 0);
+  const size_t wsn = numel_or_0(a[7]);
+  void* s = stream_arg(a[8]);
+  return status([&] { return call(x, logits, idx, fill, slot, send, order, ws, wsn, s); });
+}
 ENTRY(dispatch_bpr) {   // cfg, x, logits, idx, fill, slot, send_buf, order, ws, stream
   return entry(n, 10, [&] {
     Struct<moe_cfg> c(a[0]);
-    const auto dt = dtype_of(c);
-    const Num T = c->T, d = c->d_model, E = c->E, k = c->k;
-    const size_t need = g_abi.workspace_bytes(c, MOE_CALL_DISPATCH_BPR);
-    const void* x = ptr(a[1], "x", dt, T * d);
-    const float* logits = (const float*)ptr(a[2], "logits", kF32, T * E);
-    const int32_t* idx = (const int32_t*)ptr(a[3], "idx", kI32, T * k);
-    int32_t* fill = (int32_t*)ptr(a[4], "fill", kI32, E);
-    int32_t* slot = (int32_t*)ptr(a[5], "slot", kI32, T * k);
-    void* send = ptr(a[6], "send_buf", dt, expert_numel(c, d));
-    int32_t* order = (int32_t*)ptr(a[7], "order", kI32, T, true);
-    void* ws = ptr(a[8], "ws", at::kByte, need, need == 0);
-    const size_t wsn = numel_or_0(a[8]);
-    void* s = stream_arg(a[9]);
-    return status([&] { return g_abi.dispatch_bpr(c, x, logits, idx, fill, slot, send, order, ws, wsn, s); });
+    return dispatch_bpr_any(c, a + 1, [&](auto... v) { return g_abi.dispatch_bpr(c, v...); });
+  });
+}
+ENTRY(dispatch_bpr_route) {   // cfg, route, and as dispatch_bpr
+  return entry(n, 11, [&] {
+    Struct<moe_cfg> c(a[0]);
+    Struct<moe_route_cfg> r(a[1]);
+    return dispatch_bpr_any(c, a + 2, [&](auto... v) { return g_abi.dispatch_bpr_route(c, r, v...); });
   });
 }
 
@@ -645,6 +658,7 @@ ENTRY(init) {
     set(g_abi.block_chunked, "moe_block_chunked");
     set(g_abi.route, "moe_route");
     set(g_abi.route_bwd, "moe_route_bwd");
+    set(g_abi.dispatch_bpr_route, "moe_dispatch_bpr_route");
     set(g_abi.bwd_dx_route, "moe_bwd_dx_route");
     set(g_abi.w4_quantize, "moe_w4_quantize");
     set(g_abi.experts_w4_workspace_bytes, "moe_experts_w4_workspace_bytes");
@@ -677,6 +691,7 @@ PyMethodDef kMethods[] = {METHOD(init),
                           METHOD(block_chunked),
                           METHOD(route),
                           METHOD(route_bwd),
+                          METHOD(dispatch_bpr_route),
                           METHOD(bwd_dx_route),
                           METHOD(w4_quantize),
                           METHOD(experts_w4),

@@ -73,7 +73,8 @@ constexpr size_t kNoAllocScratchBytes = (size_t)1 << 20;
 hipError_t noalloc_scratch(void** out);
 size_t dispatch_bpr_ws_bytes(const moe_cfg& c);
 void launch_dispatch_bpr(const moe_cfg& c, const void* x, const float* logits, const int32_t* idx, int32_t* fill,
-                         int32_t* slot, void* send_buf, int32_t* order, void* ws, hipStream_t s);
+                         int32_t* slot, void* send_buf, int32_t* order, void* ws, hipStream_t s,
+                         int score = MOE_SCORE_SOFTMAX);   // whose importance: moe_score
 void launch_combine(const moe_cfg& c, const void* O, const int32_t* idx, const int32_t* slot, const float* w,
                     void* y, hipStream_t s, const void* resid = nullptr);
 size_t bwd_dx_ws_bytes(const moe_cfg& c);

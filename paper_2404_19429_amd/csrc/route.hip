@@ -415,38 +415,47 @@ hipError_t noalloc_scratch(void** out) {
 
 // ------------------------------------------------------ batch-prioritized routing
 // The tokens are visited by importance (the sum of the selected experts'
-// softmax probabilities) descending, equal importance in token order; the
+// softmax probabilities, or of a router's scores) descending, equal importance in token order; the
 // capacity rule then runs over that walk exactly as over token order.
 
-// elem[t] = (key << 32) | t, key = ~bits of the float importance (ascending
-// key = descending importance; importance >= 0), so the 64-bit elements are
+// elem[t] = (key << 32) | t, key = ~bits of an eighth of the float importance
+// (ascending key = descending importance; importance >= 0), so the 64-bit elements are
 // distinct and their ascending order is the visiting order: importance
 // descending, then token ascending.  One wave per token, lane e for
-// expert e: the softmax over all E experts in double, then the selected
-// experts' probabilities summed in rank order, rounded once to float; the
-// ordering decision is taken on the float values.
+// expert e: the scores in double, then the selected experts' summed in rank
+// order, rounded once to float; the ordering decision is taken on the float
+// values.  A logit of -inf or NaN has no score, +inf logits share the softmax
+// evenly.  The sort takes numbers of at most 1: k <= 8 scores of up to 1 (sigmoids,
+// or an expert named twice) reach 8, and an eighth keeps their order.
 __global__ __launch_bounds__(256) void bpr_key_kernel(const float* __restrict__ logits, const int32_t* __restrict__ idx,
-                                                      uint64_t* __restrict__ elem, int64_t T_tokens, int E, int k) {
+                                                      uint64_t* __restrict__ elem, int64_t T_tokens, int E, int k,
+                                                      int score) {
   const int lane = threadIdx.x & 63;
   const int64_t t = (int64_t)blockIdx.x * (blockDim.x / kWave) + (threadIdx.x >> 6);
   if (t >= T_tokens) return;
-  const bool has = lane < E;
-  const float l = has ? logits[t * E + lane] : -INFINITY;
-  float mf = l;
+  float l = lane < E ? logits[t * E + lane] : -INFINITY;
+  l = l > -INFINITY ? l : -INFINITY;   // (a NaN compares false)
+  double p;
+  if (score == MOE_SCORE_SOFTMAX) {
+    float mf = l;
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) mf = fmaxf(mf, __shfl_xor(mf, o, kWave));
-  const double ex = has ? exp((double)l - (double)mf) : 0.0;
-  double z = ex;
+    for (int o = 32; o > 0; o >>= 1) mf = fmaxf(mf, __shfl_xor(mf, o, kWave));
+    const double ex = l == -INFINITY ? 0.0 : l == mf ? 1.0 : exp((double)l - (double)mf);
+    double z = ex;
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) z += __shfl_xor(z, o, kWave);
-  const double p = ex / z;
+    for (int o = 32; o > 0; o >>= 1) z += __shfl_xor(z, o, kWave);
+    p = z > 0.0 ? ex / z : 0.0;
+  } else {
+    p = 1.0 / (1.0 + exp(-(double)l));
+  }
   double imp = 0.0;
   for (int r = 0; r < k; ++r) {
     const int e = idx[t * k + r];
     const double pe = __shfl(p, (e >= 0 && e < E) ? e : 0, kWave);
     if (e >= 0 && e < E) imp += pe;
   }
-  if (lane == 0) elem[t] = ((uint64_t)~__float_as_uint((float)imp) << 32) | (uint64_t)t;
+  static_assert(kMaxK <= 8, "an eighth of k scores is at most 1");
+  if (lane == 0) elem[t] = ((uint64_t)~__float_as_uint(0.125f * (float)imp) << 32) | (uint64_t)t;
 }
 
 constexpr int kDigitBits = 8;
@@ -718,7 +727,7 @@ size_t dispatch_bpr_ws_bytes(const moe_cfg& c) {
 }
 
 void launch_dispatch_bpr(const moe_cfg& c, const void* x, const float* logits, const int32_t* idx, int32_t* fill,
-                         int32_t* slot, void* send_buf, int32_t* order, void* ws, hipStream_t s) {
+                         int32_t* slot, void* send_buf, int32_t* order, void* ws, hipStream_t s, int score) {
   const size_t a = (dispatch_ws_bytes(c) + 255) / 256 * 256;
   const size_t eb = ((size_t)c.T * sizeof(uint64_t) + 255) / 256 * 256;
   char* w = (char*)ws + a;
@@ -729,7 +738,7 @@ void launch_dispatch_bpr(const moe_cfg& c, const void* x, const float* logits, c
   uint64_t* spl = (uint64_t*)(w + 2 * eb + tb);
   if (c.T > 0) {
     hipLaunchKernelGGL(bpr_key_kernel, dim3((unsigned)((c.T + 3) / 4)), dim3(256), 0, s, logits, idx, e0, c.T, c.E,
-                       c.k);
+                       c.k, score);
     auto sort = [&](auto tag) {
       using ST = decltype(tag);
       static std::atomic<uint64_t> lds_ok{0};

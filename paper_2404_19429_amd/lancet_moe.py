@@ -32,7 +32,7 @@ EXPORTS = ["moe_capacity", "moe_workspace_bytes", "moe_last_error", "moe_gate_to
            "moe_dispatch_noalloc", "moe_dispatch_bpr", "moe_pack_weights", "moe_expert_ffn_fwd", "moe_combine", "moe_bwd_dx", "moe_bwd_dw",
            "moe_block_workspace_bytes", "moe_block_chunked", "moe_block_op_times", "moe_block_dw_schedule",
            "moe_dw_schedule", "moe_pipeline_plan", "moe_pipeline_range_cost", "moe_product_timing",
-           "moe_product_times", "moe_route", "moe_route_bwd", "moe_bwd_dx_route", "moe_w4_quantize",
+           "moe_product_times", "moe_route", "moe_route_bwd", "moe_dispatch_bpr_route", "moe_bwd_dx_route", "moe_w4_quantize",
            "moe_experts_w4_workspace_bytes", "moe_experts_w4", "moe_ckpt_bytes", "moe_ckpt_save", "moe_ckpt_load"]
 #: The expert products moe_product_times reports, in its order.
 PRODUCTS = ["fwd1", "fwd2", "dA", "dXe", "dW2", "dW1"]
@@ -119,6 +119,7 @@ def _load():
         "moe_pipeline_range_cost": (I32, [I32, I32, P, P, P, I32, I32, I32, P]),
         "moe_route": (I32, [ctypes.POINTER(moe_route_cfg)] + [P] * 6),
         "moe_route_bwd": (I32, [ctypes.POINTER(moe_route_cfg)] + [P] * 6),
+        "moe_dispatch_bpr_route": (I32, [CFG, ctypes.POINTER(moe_route_cfg)] + [P] * 8 + [SZ, P]),
         "moe_bwd_dx_route": (I32, [CFG, ctypes.POINTER(moe_route_cfg)] + [P] * 19 + [SZ, P]),
         "moe_w4_quantize": (I32, [I64, I32, I32, P, P, P, P]),
         "moe_experts_w4_workspace_bytes": (SZ, [ctypes.POINTER(moe_w4_cfg)]),
@@ -304,6 +305,10 @@ def moe_route_bwd(cfg, logits, idx, w, dw, dlogits, stream=None):
     _check(_bind.route_bwd(cfg, logits, idx, w, dw, dlogits, stream))
 
 
+def moe_dispatch_bpr_route(cfg, route, x, logits, idx, fill, slot, send_buf, order, ws, stream=None):
+    _check(_bind.dispatch_bpr_route(cfg, route, x, logits, idx, fill, slot, send_buf, order, ws, stream))
+
+
 def moe_bwd_dx_route(cfg, route, Wg, logits, idx, w, slot, row_begin, row_end, H, expert_out, W1p, W2p, dy, dO, dH, dXe,
                      dw, dlogits, dx, ws=None, stream=None):
     _check(_bind.bwd_dx_route(cfg, route, Wg, logits, idx, w, slot, row_begin, row_end, H, expert_out, W1p, W2p, dy, dO,
@@ -421,13 +426,16 @@ class Router:
 
 def layer_forward(b: LayerBuffers, x, Wg, bias, W1, W2, stream=None, routing="token", router: Optional[Router] = None):
     """weight packing -> gate [-> router] -> dispatch -> experts -> combine, all on one stream.
-    routing "bpr": batch-prioritized capacity order (no carry-in; b.carry must be zero)."""
+    routing "bpr": batch-prioritized capacity order, by the router's scores if there is one (no carry-in;
+    b.carry must be zero)."""
     c = b.cfg
     moe_pack_weights(c, W1, W2, b.W1p, b.W2p, stream)
     moe_gate_topk(c, x, Wg, bias, b.logits, b.idx, b.w, stream)
     if router is not None:
         moe_route(router.cfg, b.logits, router.bias, b.idx, b.w, router.load, stream)
-    if routing == "bpr":
+    if routing == "bpr" and router is not None:
+        moe_dispatch_bpr_route(c, router.cfg, x, b.logits, b.idx, b.fill, b.slot, b.send_buf, b.order, b.ws_bpr, stream)
+    elif routing == "bpr":
         moe_dispatch_bpr(c, x, b.logits, b.idx, b.fill, b.slot, b.send_buf, b.order, b.ws_bpr, stream)
     else:
         moe_dispatch(c, x, b.idx, b.carry, b.fill, b.slot, b.send_buf, b.ws_dispatch, stream)

@@ -26,3 +26,24 @@ def test_route_bwd_output_aliases_no_input():
     for i in range(4):
         assert lib.moe_route_bwd(ctypes.byref(c), P(0), P(1), P(2), P(3), P(i), None) == L.MOE_EINVAL
         assert "alias" in L.moe_last_error()
+
+
+def bpr_route(c, r, n=None, **over):
+    names = ["x", "logits", "idx", "fill", "slot", "send", "order", "ws"]
+    p = [over.get(m, P(i)) for i, m in enumerate(names)]
+    need = L.moe_workspace_bytes(c, L.MOE_CALL_DISPATCH_BPR) if n is None else n
+    return lib.moe_dispatch_bpr_route(ctypes.byref(c), None if r is None else ctypes.byref(r), *p, need, None)
+
+
+@no_device
+def test_dispatch_bpr_route_refused():
+    c = L.make_cfg(64, 128, 256, 16, 2, 20)
+    assert bpr_route(c, rcfg()) == L.MOE_EDEVICE and bpr_route(c, rcfg(), order=None) == L.MOE_EDEVICE   # valid
+    assert bpr_route(c, None) == L.MOE_EINVAL
+    for kw in (dict(T=65), dict(E=32), dict(k=3)):
+        assert bpr_route(c, rcfg(**kw)) == L.MOE_EINVAL and "differ" in L.moe_last_error()
+    assert bpr_route(c, rcfg(score=2)) == L.MOE_EINVAL and bpr_route(L.make_cfg(64, 12, 256, 16, 2, 20), rcfg()) == L.MOE_ESHAPE
+    assert bpr_route(c, rcfg(), n=64) == L.MOE_EWORKSPACE and bpr_route(c, rcfg(), ws=None) == L.MOE_EWORKSPACE
+    assert bpr_route(c, rcfg(), logits=None) == L.MOE_EINVAL and bpr_route(c, rcfg(), order=8) == L.MOE_EALIGN
+    z = L.make_cfg(0, 128, 256, 16, 2, 20)
+    assert bpr_route(z, rcfg(T=0), x=None, logits=None, idx=None, slot=None) == L.MOE_EDEVICE
