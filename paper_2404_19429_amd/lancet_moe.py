@@ -429,6 +429,8 @@ def layer_forward(b: LayerBuffers, x, Wg, bias, W1, W2, stream=None, routing="to
     routing "bpr": batch-prioritized capacity order, by the router's scores if there is one (no carry-in;
     b.carry must be zero)."""
     c = b.cfg
+    if router is not None and (router.cfg.T, router.cfg.E, router.cfg.k) != (c.T, c.E, c.k):
+        raise ValueError("the router's T, E and k are not the layer's")
     moe_pack_weights(c, W1, W2, b.W1p, b.W2p, stream)
     moe_gate_topk(c, x, Wg, bias, b.logits, b.idx, b.w, stream)
     if router is not None:

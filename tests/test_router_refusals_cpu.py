@@ -47,3 +47,12 @@ def test_dispatch_bpr_route_refused():
     assert bpr_route(c, rcfg(), logits=None) == L.MOE_EINVAL and bpr_route(c, rcfg(), order=8) == L.MOE_EALIGN
     z = L.make_cfg(0, 128, 256, 16, 2, 20)
     assert bpr_route(z, rcfg(T=0), x=None, logits=None, idx=None, slot=None) == L.MOE_EDEVICE
+
+
+def test_layer_forward_refuses_a_router_of_another_layer():
+    """Before anything is launched: tokens past a shorter router's would keep the gate's own choices."""
+    import types
+    b = types.SimpleNamespace(cfg=L.make_cfg(64, 128, 256, 16, 2, 20))
+    for kw in (dict(T=63), dict(T=65), dict(E=32), dict(k=1)):
+        with pytest.raises(ValueError, match="router"):
+            L.layer_forward(b, None, None, None, None, None, router=L.Router(rcfg(**kw)))
