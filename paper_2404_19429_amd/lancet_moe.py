@@ -392,7 +392,7 @@ class LayerBuffers:
     ws_dw: torch.Tensor
     order: torch.Tensor       # batch-prioritized routing: the visiting order
     ws_bpr: torch.Tensor
-    dw: torch.Tensor          # layers with a router: the gradient at w
+    dw: Optional[torch.Tensor] = None   # layers with a router: the gradient at w
 
 
 def alloc_layer(cfg: moe_cfg, device="cuda") -> LayerBuffers:

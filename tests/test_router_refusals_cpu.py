@@ -56,3 +56,11 @@ def test_layer_forward_refuses_a_router_of_another_layer():
     for kw in (dict(T=63), dict(T=65), dict(E=32), dict(k=1)):
         with pytest.raises(ValueError, match="router"):
             L.layer_forward(b, None, None, None, None, None, router=L.Router(rcfg(**kw)))
+
+
+def test_layer_buffers_of_a_layer_without_a_router():
+    """The gradient at w is a router's: a layer without one is built without it."""
+    import dataclasses
+    names = [f.name for f in dataclasses.fields(L.LayerBuffers)]
+    b = L.LayerBuffers(**{n: None for n in names if n != "dw"})
+    assert b.dw is None
