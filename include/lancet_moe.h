@@ -408,9 +408,10 @@ moe_status moe_experts_w4(const moe_w4_cfg* cfg, const void* x, const int32_t* i
  * the two, so that the layers of a model share one set of full-size buffers:
  * send_buf, H and expert_out, at 1 + 1/16 bytes a value (A = act(H) is rebuilt).
  *   64 consecutive columns of a row (64j .. 64j + 63) share a float step =
- *   max|x| / 127; a value is kept as the integer nearest to 127 x / max|x| (ties to
- *   even) and restored as integer * step, rounded to dtype.  A group under 1e-30
- *   becomes zeros; a group with an infinite or NaN value becomes NaN.
+ *   max|x| / 127 (of the largest float the step below, 127 of which are finite); a
+ *   value is kept as the integer nearest to 127 x / max|x| (ties to even) and restored
+ *   as integer * step, rounded to dtype.  A group under 1e-30 becomes zeros; a group
+ *   with an infinite or NaN value becomes NaN.
  *   Rows [row_begin_e, row_end_e) (row_begin NULL = zeros) of each expert are saved
  *   and restored; other rows are neither read nor written.
  * cfg as for moe_expert_ffn_fwd: T, k, G and the flags play no part. */

@@ -155,7 +155,8 @@ __global__ __launch_bounds__(256) void ckpt_save_kernel(CkptArgs a) {
       const float amax = __uint_as_float(m);
       const bool bad = m >= 0x7f800000u, tiny = amax < 1e-30f;
       const float inv = bad || tiny ? 0.f : 127.f / amax;
-      const float step = bad ? __uint_as_float(0x7fc00000u) : tiny ? 0.f : amax / 127.f;
+      // (of the largest float the quotient rounds up to a step of which 127 are infinite)
+      const float step = bad ? __uint_as_float(0x7fc00000u) : tiny ? 0.f : fminf(amax / 127.f, 0x1.020406p+121f);
       float q[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) q[i] = bad ? 0.f : v[i] * inv;
