@@ -928,7 +928,8 @@ static W4Ws w4_ws(const moe_w4_cfg& c) {
   const bool bf = c.dtype == MOE_BF16;
   w.rows = n + 15 * std::min<int64_t>(n, c.E);
   w.rows = (w.rows + 15) / 16 * 16;
-  w.max_tiles = (int)(std::min<int64_t>(n, c.E) + n / kW4Tile);   // (of 16 tokens; of 128 there are fewer)
+  static_assert(kGemmToks >= kW4Tile, "the laid-out products have no more tiles than the others");
+  w.max_tiles = (int)(std::min<int64_t>(n, c.E) + n / kW4Tile);
   w.list = 0;
   w.tiles = up256(4 * (size_t)w.rows);
   w.ntiles = w.tiles + sizeof(W4Tile) * (size_t)w.max_tiles;
