@@ -316,6 +316,15 @@ __device__ __forceinline__ void load_row(const float* row, int j, int E, float n
   }
 }
 
+// exp(l - m): e^d (1 + what the rounding of d = l - m has lost), which is up to half of 2^-17
+// for the scores of e^-64 and below, 64 half steps of the result.
+__device__ __forceinline__ float exp_diff(float l, float m) {
+  const float d = l - m, b = l - d;
+  const float lost = (l - (d + b)) - (m - b);
+  const float s = expf(d);
+  return fmaf(s, lost, s);
+}
+
 // LPT lanes per token, NCH chunks of four experts per lane (chunk c of lane j: experts
 // 4 (j + LPT c) ..), up to KT choices.
 template <int LPT, int NCH, int KT, bool GROUPS>
@@ -480,7 +489,7 @@ __global__ __launch_bounds__(64 * kRouteWaves) void route_kernel(RouteArgs a) {
         const int i = kept_key[q] & (NV - 1);
         e[q] = 4 * (__builtin_ctz(kept_at[q]) + LPT * (i >> 2)) + (i & 3);
         const float l = row[e[q]];
-        s[q] = soft ? expf(l - m) : 1.f / (1.f + expf(-l));
+        s[q] = soft ? exp_diff(l, m) : 1.f / (1.f + expf(-l));
         // Next to float's smallest numbers.  (A plain softmax's weight is its share times the scale:
         // below e^-210 that is none whatever the scale is.)
         const float x = soft ? l - m : l;

@@ -104,3 +104,15 @@ def test_gradient_of_the_largest_scale(E, k, score):
     rng = np.random.default_rng(E)
     l = rng.standard_normal((20, E)).astype(np.float32)
     check_bwd(l, O.route(l, None, k, score, 1)[0], 10 + rng.random((20, k)), score, 1, 1e38)
+
+
+@pytest.mark.parametrize("renorm", [0, 1])
+@pytest.mark.parametrize("E,k", [(16, 2), (64, 8), (256, 8)])
+def test_weights_far_below_the_largest_logit(E, k, renorm):
+    """Shares of e^-70: the difference to the largest logit is no float, and its rounding not the weight's."""
+    rng = np.random.default_rng(E)
+    l = (-35 + rng.standard_normal((200, E))).astype(np.float32)
+    l[:, 0] = 35 + rng.random(200)                            # the largest, which the bias keeps out
+    bias = np.linspace(1, 2, E).astype(np.float32)
+    bias[0] = -9.0
+    check(l, k, bias, score="softmax", renorm=renorm)
