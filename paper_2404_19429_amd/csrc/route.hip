@@ -427,32 +427,34 @@ hipError_t noalloc_scratch(void** out) {
 // values.  A logit of -inf or NaN has no score, +inf logits share the softmax
 // evenly.  The sort takes numbers of at most 1: k <= 8 scores of up to 1 (sigmoids,
 // or an expert named twice) reach 8, and an eighth keeps their order.
+template <int SCORE>
 __global__ __launch_bounds__(256) void bpr_key_kernel(const float* __restrict__ logits, const int32_t* __restrict__ idx,
-                                                      uint64_t* __restrict__ elem, int64_t T_tokens, int E, int k,
-                                                      int score) {
+                                                      uint64_t* __restrict__ elem, int64_t T_tokens, int E, int k) {
   const int lane = threadIdx.x & 63;
   const int64_t t = (int64_t)blockIdx.x * (blockDim.x / kWave) + (threadIdx.x >> 6);
   if (t >= T_tokens) return;
   float l = lane < E ? logits[t * E + lane] : -INFINITY;
-  l = l > -INFINITY ? l : -INFINITY;   // (a NaN compares false)
+  const int choice = lane < k ? idx[t * k + lane] : -1;   // lane r: the r-th, on its way with the logits
+  l = l > -INFINITY ? l : -INFINITY;                      // (a NaN compares false)
   double p;
-  if (score == MOE_SCORE_SOFTMAX) {
+  if constexpr (SCORE == MOE_SCORE_SOFTMAX) {
     float mf = l;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) mf = fmaxf(mf, __shfl_xor(mf, o, kWave));
-    const double ex = l == -INFINITY ? 0.0 : l == mf ? 1.0 : exp((double)l - (double)mf);
+    if (mf == INFINITY) l = l == INFINITY ? 0.f : -INFINITY;
+    mf = fabsf(mf) < INFINITY ? mf : 0.f;
+    const double ex = exp((double)l - (double)mf);
     double z = ex;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) z += __shfl_xor(z, o, kWave);
-    p = z > 0.0 ? ex / z : 0.0;
+    p = ex / fmax(z, 1.0);   // (z is 1 at least, or there is no share)
   } else {
     p = 1.0 / (1.0 + exp(-(double)l));
   }
   double imp = 0.0;
   for (int r = 0; r < k; ++r) {
-    const int e = idx[t * k + r];
-    const double pe = __shfl(p, (e >= 0 && e < E) ? e : 0, kWave);
-    if (e >= 0 && e < E) imp += pe;
+    const int e = __builtin_amdgcn_readlane(choice, r);
+    if (e >= 0 && e < E) imp += __shfl(p, e, kWave);
   }
   static_assert(kMaxK <= 8, "an eighth of k scores is at most 1");
   if (lane == 0) elem[t] = ((uint64_t)~__float_as_uint(0.125f * (float)imp) << 32) | (uint64_t)t;
@@ -737,8 +739,11 @@ void launch_dispatch_bpr(const moe_cfg& c, const void* x, const float* logits, c
   int32_t* perm = order ? order : (int32_t*)(w + 2 * eb);
   uint64_t* spl = (uint64_t*)(w + 2 * eb + tb);
   if (c.T > 0) {
-    hipLaunchKernelGGL(bpr_key_kernel, dim3((unsigned)((c.T + 3) / 4)), dim3(256), 0, s, logits, idx, e0, c.T, c.E,
-                       c.k, score);
+    auto keys = [&](auto kern) {
+      hipLaunchKernelGGL(kern, dim3((unsigned)((c.T + 3) / 4)), dim3(256), 0, s, logits, idx, e0, c.T, c.E, c.k);
+    };
+    if (score == MOE_SCORE_SOFTMAX) keys(bpr_key_kernel<MOE_SCORE_SOFTMAX>);
+    else keys(bpr_key_kernel<MOE_SCORE_SIGMOID>);
     auto sort = [&](auto tag) {
       using ST = decltype(tag);
       static std::atomic<uint64_t> lds_ok{0};
