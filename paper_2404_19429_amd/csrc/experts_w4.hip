@@ -30,7 +30,9 @@ constexpr int kW4Tile = 16;        // tokens of one pass over the weights: a mat
 constexpr int kW4ListThreads = 1024;
 constexpr int kW4Splits = 4;       // of the second product's K, at most
 constexpr int kMaxGridY = 65535;
-constexpr int kW4Waves = 8, kW4PerSimd = 3;   // of a block that splits K over waves, at most; of a SIMD, by registers
+// Waves of a block that splits K over waves, at most; and of a SIMD, by registers: 168, which
+// the three parts of float inputs with 32 rows spill out of (20-100 bytes a lane), the rest not.
+constexpr int kW4Waves = 8, kW4PerSimd = 3;
 
 typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
 

@@ -9,8 +9,8 @@
 // the errors).  Such a token (a few in a thousand of ordinary logits; all of them where
 // logits tie) goes the exact way, one wavefront for the token in double, in the same launch.
 // Bound by the comparisons, not by the 4 E bytes a token: 32768 tokens, 256 experts in 8
-// groups, k 8, 22.8 us (8.7 for the bytes; 16 without the exact way, whose registers leave
-// five waves a SIMD); all in double 270.  8192 tokens, 64 experts, k 2: 3.4 us.
+// groups, k 8, 23.2-24.3 us (8.7 for the bytes; 16 without the exact way, whose registers leave
+// five waves a SIMD); all in double 270.  8192 tokens, 64 experts, k 2: 3.3 us.
 #include <utility>
 
 #include "internal.h"
@@ -610,9 +610,9 @@ void launch_route(const moe_route_cfg& c, const float* logits, const float* bias
 }
 
 // ------------------------------------------------------------------- gradient
-// Bound by writing dlogits, most of it zeros (but for a plain softmax, which also reads
-// the logits).  A wavefront builds its tokens' rows in LDS and stores them as one run
-// (32768 tokens, 256 experts, k 8: 8.3 us; k shuffles a token and scattered stores 16.8).
+// Bound by writing dlogits, most of it zeros (a plain softmax also reads the logits, a sigmoid
+// those of the choices, with 8 of 256 most lines of a row).  A wavefront builds its tokens' rows in LDS and stores them as one run
+// (32768 tokens, 256 experts, k 8: 8.8 us; k shuffles a token and scattered stores 16.8).
 struct RouteBwdArgs {
   const float* logits;
   const int32_t* idx;
