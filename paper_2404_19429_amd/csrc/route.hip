@@ -840,17 +840,16 @@ void launch_combine(const moe_cfg& c, const void* O, const int32_t* idx, const i
 }
 
 // ------------------------------------------------------ combine + gate backward
-// One wavefront per token: dO[e][s] = w dy, g_r = <dy, O[e][s]>, then dlogits; or, with
-// dw non-null, g itself (the gradient at the weights, whose router has its own backward).
-template <typename T, int KT>
+// One wavefront per token: dO[e][s] = w dy, g_r = <dy, O[e][s]>, then dlogits; or, DW,
+// dw = g itself (the gradient at the weights, whose router has its own backward).
+template <typename T, int KT, bool DW>
 __global__ __launch_bounds__(256) void combine_bwd_kernel(const float* __restrict__ logits,
                                                           const int32_t* __restrict__ idx,
                                                           const float* __restrict__ w,
                                                           const int32_t* __restrict__ slot,
                                                           const T* __restrict__ O, const T* __restrict__ dy,
-                                                          T* __restrict__ dO, float* __restrict__ dlogits,
-                                                          float* __restrict__ dw, int64_t T_tokens, int d, int E,
-                                                          int kr, int C, int renorm) {
+                                                          T* __restrict__ dO, float* __restrict__ out,
+                                                          int64_t T_tokens, int d, int E, int kr, int C, int renorm) {
   constexpr int V = Vec<T>::N;
   constexpr int KK = KT > 0 ? KT : kMaxK;
   const int k = KT > 0 ? KT : kr;
@@ -891,14 +890,14 @@ __global__ __launch_bounds__(256) void combine_bwd_kernel(const float* __restric
 #pragma unroll
       for (int r = 0; r < KK; ++r) {
         if (sr[r] < 0) continue;
-        float o[V], out[V];
+        float o[V], go[V];
         Vec<T>::load(&ov[h][r], o);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
           gp[r] = fmaf(g[i], o[i], gp[r]);
-          out[i] = wr[r] * g[i];
+          go[i] = wr[r] * g[i];
         }
-        Vec<T>::store(dO + eoff<T>(er[r], sr[r], c * V, d, C), out);
+        Vec<T>::store(dO + eoff<T>(er[r], sr[r], c * V, d, C), go);
       }
     }
   }
@@ -908,10 +907,10 @@ __global__ __launch_bounds__(256) void combine_bwd_kernel(const float* __restric
     gp[r] = wave_sum(gp[r]);
     gsum = fmaf(wr[r], gp[r], gsum);
   }
-  if (dw) {
+  if constexpr (DW) {
 #pragma unroll
     for (int r = 0; r < KK; ++r)
-      if (r < k && lane == r) dw[t * k + r] = gp[r];
+      if (r < k && lane == r) out[t * k + r] = gp[r];
     return;
   }
   // dlogits: lane j handles expert j (E <= 64).
@@ -933,7 +932,7 @@ __global__ __launch_bounds__(256) void combine_bwd_kernel(const float* __restric
     for (int r = 0; r < KK; ++r)
       if (r < k && er[r] == j) dl += gp[r] * wr[r];
   }
-  if (j < E) dlogits[t * E + j] = dl;
+  if (j < E) out[t * E + j] = dl;
 }
 
 size_t bwd_dx_ws_bytes(const moe_cfg& c) { return expert_sk_ws_bytes(c); }
@@ -943,20 +942,24 @@ void launch_combine_bwd(const moe_cfg& c, const float* logits, const int32_t* id
                         hipStream_t s, float* dw) {
   if (c.T == 0) return;
   const unsigned blocks = (unsigned)((c.T + 3) / 4);
-  auto go = [&](auto kern, auto tag) {
+  auto go = [&](auto kern, auto tag, float* out) {
     using T = decltype(tag);
     hipLaunchKernelGGL(kern, dim3(blocks), dim3(256), 0, s, logits, idx, w, slot, (const T*)O, (const T*)dy,
-                       (T*)dO, dlogits, dw, c.T, c.d_model, c.E, c.k, c.C, c.renorm);
+                       (T*)dO, out, c.T, c.d_model, c.E, c.k, c.C, c.renorm);
   };
-  if (c.dtype == MOE_BF16) {
-    if (c.k == 1) go(combine_bwd_kernel<uint16_t, 1>, uint16_t{});
-    else if (c.k == 2) go(combine_bwd_kernel<uint16_t, 2>, uint16_t{});
-    else go(combine_bwd_kernel<uint16_t, 0>, uint16_t{});
-  } else {
-    if (c.k == 1) go(combine_bwd_kernel<float, 1>, float{});
-    else if (c.k == 2) go(combine_bwd_kernel<float, 2>, float{});
-    else go(combine_bwd_kernel<float, 0>, float{});
-  }
+  auto pick = [&](auto kt) {
+    constexpr int KT = decltype(kt)::value;
+    if (c.dtype == MOE_BF16) {
+      if (dw) go(combine_bwd_kernel<uint16_t, KT, true>, uint16_t{}, dw);
+      else go(combine_bwd_kernel<uint16_t, KT, false>, uint16_t{}, dlogits);
+    } else {
+      if (dw) go(combine_bwd_kernel<float, KT, true>, float{}, dw);
+      else go(combine_bwd_kernel<float, KT, false>, float{}, dlogits);
+    }
+  };
+  if (c.k == 1) pick(std::integral_constant<int, 1>{});
+  else if (c.k == 2) pick(std::integral_constant<int, 2>{});
+  else pick(std::integral_constant<int, 0>{});
 }
 
 // ----------------------------------------------------------- dispatch backward
