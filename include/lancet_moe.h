@@ -431,6 +431,116 @@ moe_status moe_ckpt_load(const moe_cfg* cfg, const void* ckpt, size_t ckpt_bytes
                          const int32_t* row_end, void* send_buf, void* H, void* A, void* expert_out,
                          moe_stream_t stream);
 
+/* ------------------------------------------- rows sorted by expert, no capacity */
+
+/* The layer without a capacity: every choice gets a row, the rows of an expert lie
+ * together in one buffer that the experts share, and nothing is dropped.  The gate
+ * (or moe_route) gives the choices, moe_sorted_dispatch the rows, moe_sorted_ffn_fwd
+ * the experts' outputs, moe_sorted_combine the sums by token; the backward mirrors
+ * it: moe_sorted_combine_bwd, moe_sorted_bwd_dx, moe_sorted_dispatch_bwd, and
+ * moe_sorted_bwd_dw on any stream after moe_sorted_bwd_dx.
+ *   A sorted buffer holds R = moe_sorted_rows(cfg) rows of X elements: those that the
+ * products read (rows, H, A, dO, dH) in the blocks of the expert buffers above for
+ * MOE_BF16, expert_out and dXe row-major; for MOE_F32 all row-major.  Expert e owns
+ * rows [row_begin_e, row_end_e), row_begin_e a multiple of 16 for MOE_BF16.  Rows that
+ * hold no choice are unspecified: never read and never written.
+ *   An idx outside 0..E-1 takes no part, whatever its w holds; a row of idx may name
+ * an expert twice.  No output may alias another array of its call. */
+typedef struct {
+  int64_t T;       /* tokens; T * k <= 2^30 */
+  int32_t d_model; /* MOE_BF16: a multiple of 64; MOE_F32: of 8; up to 2^20 */
+  int32_t d_ff;    /* likewise */
+  int32_t E;       /* 1..512 */
+  int32_t k;       /* 1..16 */
+  int32_t dtype;   /* moe_dtype */
+  int32_t act;     /* moe_act */
+  int32_t wpacked; /* as in moe_cfg: 1 = moe_sorted_bwd_dw writes dW1, dW2 in the packed layout */
+} moe_sorted_cfg;
+
+/* R: T * k rows, for MOE_BF16 with up to 15 more an expert, in whole blocks of 16
+ * (host only; -1 and a message on an invalid cfg). */
+int64_t moe_sorted_rows(const moe_sorted_cfg* cfg);
+
+/* Bytes of device workspace of a call (host only; 0 if none, 0 and a message on an
+ * invalid cfg): MOE_CALL_DISPATCH moe_sorted_dispatch, MOE_CALL_FFN_FWD
+ * moe_sorted_ffn_fwd, MOE_CALL_BWD_DX moe_sorted_bwd_dx, MOE_CALL_BWD_DW
+ * moe_sorted_bwd_dw with dWg.  Calls that overlap in time need separate workspaces. */
+size_t moe_sorted_workspace_bytes(const moe_sorted_cfg* cfg, int32_t call);
+
+/* x [T][d], idx [T][k] int32 -> row_begin, row_end [E] int32; slot [T][k] int32, the
+ * row of each choice (-1: idx outside 0..E-1); src [R] int32, the choice t * k + r that
+ * each row holds (-1: none); rows [R][d], rows[slot[t][r]] = x[t].  Within an expert
+ * the rows are in (t, r) order. */
+moe_status moe_sorted_dispatch(const moe_sorted_cfg* cfg, const void* x, const int32_t* idx, int32_t* row_begin,
+                               int32_t* row_end, int32_t* slot, int32_t* src, void* rows, void* ws, size_t ws_bytes,
+                               moe_stream_t stream);
+
+/* H = rows W1_e^T, A = act(H), expert_out = A W2_e^T on each expert's rows.  W1p
+ * [E][f][d], W2p [E][d][f] as moe_pack_weights writes them.  bf16: a matrix's and a
+ * buffer's bytes stay under 2 GiB; as with moe_cfg.ksplit = 1 the last bits depend on
+ * the row counts. */
+moe_status moe_sorted_ffn_fwd(const moe_sorted_cfg* cfg, const void* rows, const int32_t* row_begin,
+                              const int32_t* row_end, const void* W1p, const void* W2p, void* H, void* A,
+                              void* expert_out, void* ws, size_t ws_bytes, moe_stream_t stream);
+
+/* y[t] = sum over r with slot[t][r] >= 0 of w[t][r] expert_out[slot[t][r]], in float, in
+ * choice order. */
+moe_status moe_sorted_combine(const moe_sorted_cfg* cfg, const void* expert_out, const int32_t* slot, const float* w,
+                              void* y, moe_stream_t stream);
+
+/* dO[slot[t][r]] = w[t][r] dy[t]; dw [T][k] float = <dy[t], expert_out[slot[t][r]]>, 0
+ * where slot is -1 (the gradient at w: moe_route_bwd takes it on to the logits). */
+moe_status moe_sorted_combine_bwd(const moe_sorted_cfg* cfg, const void* expert_out, const int32_t* slot,
+                                  const int32_t* src, const float* w, const void* dy, void* dO, float* dw,
+                                  moe_stream_t stream);
+
+/* dH = (dO W2_e) * act'(H), dXe = dH W1_e on each expert's rows. */
+moe_status moe_sorted_bwd_dx(const moe_sorted_cfg* cfg, const int32_t* row_begin, const int32_t* row_end, const void* H,
+                             const void* W1p, const void* W2p, const void* dO, void* dH, void* dXe, void* ws,
+                             size_t ws_bytes, moe_stream_t stream);
+
+/* dx[t] = sum over r with slot[t][r] >= 0 of dXe[slot[t][r]]; with Wg [E][d] dtype and
+ * dlogits [T][E] float (both or neither) plus sum over j of dlogits[t][j] Wg_j, the
+ * gate's part (a dlogits of 0 takes no part). */
+moe_status moe_sorted_dispatch_bwd(const moe_sorted_cfg* cfg, const int32_t* slot, const void* dXe, const void* Wg,
+                                   const float* dlogits, void* dx, moe_stream_t stream);
+
+/* dW2_e = dO_e^T A_e [d][f], dW1_e = dH_e^T rows_e [f][d] over each expert's rows
+ * (exact zeros for an expert without one); with x [T][d], dlogits [T][E] float and dWg
+ * [E][d] float (all or none; E <= 64) also dWg = dlogits^T x, for which ws is needed. */
+moe_status moe_sorted_bwd_dw(const moe_sorted_cfg* cfg, const int32_t* row_begin, const int32_t* row_end,
+                             const void* rows, const void* A, const void* dO, const void* dH, void* dW1, void* dW2,
+                             const void* x, const float* dlogits, float* dWg, void* ws, size_t ws_bytes,
+                             moe_stream_t stream);
+
+/* -------------------------------------------------------------- token lookup */
+
+typedef struct {
+  int64_t T;       /* tokens, up to 2^30; T * d_model <= 2^40 */
+  int32_t V;       /* rows of the table, 1..2^30; V * d_model <= 2^40 */
+  int32_t d_model; /* a multiple of 8 */
+  int32_t dtype;   /* moe_dtype */
+  float scale;     /* finite */
+  int32_t accum;   /* moe_embed_bwd: 0 writes every row of dW; 1 adds to the rows of the ids that occur
+                      and leaves the others (a table tied to the output matrix, or micro-batches) */
+} moe_embed_cfg;
+
+/* y[t] = scale W[ids[t]]: ids [T] int32, W [V][d], y [T][d] dtype; 0 where the id is
+ * outside 0..V-1 (padding). */
+moe_status moe_embed(const moe_embed_cfg* cfg, const int32_t* ids, const void* W, void* y, moe_stream_t stream);
+
+/* Bytes of device workspace moe_embed_bwd needs (host only; 0 if none, 0 and a message
+ * on an invalid cfg). */
+size_t moe_embed_bwd_workspace_bytes(const moe_embed_cfg* cfg);
+
+/* dW[v] (accum: +)= scale * sum of dy[t] over the tokens with ids[t] = v: dy [T][d], dW
+ * [V][d] dtype.  Summed in float in an order that depends on ids only, rounded once;
+ * the same call gives the same bits.  dy of a token whose id is outside the table is
+ * not read.  dW may alias no input.  Calls that overlap in time need separate
+ * workspaces. */
+moe_status moe_embed_bwd(const moe_embed_cfg* cfg, const int32_t* ids, const void* dy, void* dW, void* ws,
+                         size_t ws_bytes, moe_stream_t stream);
+
 /* ------------------------------------------------------------------ block */
 
 /* The pre-LN transformer block whose FFN is the MoE layer, with its

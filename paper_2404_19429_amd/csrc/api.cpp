@@ -6,6 +6,7 @@
 #include <cstdio>
 #include <cstdarg>
 #include <cstring>
+#include <initializer_list>
 #include <string>
 
 #include "internal.h"
@@ -17,6 +18,8 @@ static_assert(sizeof(moe_block_cfg) == 96 && offsetof(moe_block_cfg, moe) == 16 
               "moe_block_cfg layout");
 static_assert(sizeof(moe_route_cfg) == 40 && offsetof(moe_route_cfg, scale) == 32, "moe_route_cfg layout");
 static_assert(sizeof(moe_w4_cfg) == 32 && offsetof(moe_w4_cfg, act) == 28, "moe_w4_cfg layout");
+static_assert(sizeof(moe_sorted_cfg) == 40 && offsetof(moe_sorted_cfg, wpacked) == 32, "moe_sorted_cfg layout");
+static_assert(sizeof(moe_embed_cfg) == 32 && offsetof(moe_embed_cfg, accum) == 24, "moe_embed_cfg layout");
 
 namespace {
 
@@ -591,6 +594,237 @@ moe_status moe_ckpt_load(const moe_cfg* cfg, const void* ckpt, size_t ckpt_bytes
     if (out[i] == ckpt) return fail(MOE_EINVAL, "%s: ckpt may not alias a buffer", fn);
   CHECK(check_device(fn));
   lmoe::launch_ckpt_load(*cfg, ckpt, row_begin, row_end, send_buf, H, A, expert_out, (hipStream_t)stream);
+  return check_launch(fn);
+}
+
+// ------------------------------------------- rows sorted by expert, no capacity
+namespace {
+
+// Whether an output is another array of the call, or two outputs are one.
+bool alias(std::initializer_list<const void*> outs, std::initializer_list<const void*> ins) {
+  for (const void* const* o = outs.begin(); o != outs.end(); ++o) {
+    if (*o == nullptr) continue;
+    for (const void* const* q = outs.begin(); q != o; ++q)
+      if (*q == *o) return true;
+    for (const void* i : ins)
+      if (i == *o) return true;
+  }
+  return false;
+}
+#define REFUSE_ALIAS(...)                                                                              \
+  do {                                                                                                 \
+    if (alias(__VA_ARGS__)) return fail(MOE_EINVAL, "%s: an output may not alias another array", fn);  \
+  } while (0)
+#define REQUIRE_WS(need)                                                                               \
+  do {                                                                                                 \
+    const size_t _n = (need);                                                                          \
+    if (_n > 0) {                                                                                      \
+      if (ws == nullptr || ws_bytes < _n)                                                              \
+        return fail(MOE_EWORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, _n, ws ? ws_bytes : 0); \
+      REQUIRE_PTR(ws);                                                                                 \
+    }                                                                                                  \
+  } while (0)
+
+moe_status check_sorted(const moe_sorted_cfg* c, const char* fn, bool products) {
+  if (!c) return fail(MOE_EINVAL, "%s: cfg is NULL", fn);
+  if (c->dtype != MOE_F32 && c->dtype != MOE_BF16) return fail(MOE_EDTYPE, "%s: unknown dtype %d", fn, c->dtype);
+  if (c->act < MOE_ACT_IDENTITY || c->act > MOE_ACT_GELU_ERF) return fail(MOE_EINVAL, "%s: unknown act %d", fn, c->act);
+  if (c->wpacked != 0 && c->wpacked != 1) return fail(MOE_EINVAL, "%s: wpacked must be 0 or 1", fn);
+  if (c->T < 0) return fail(MOE_EINVAL, "%s: T < 0", fn);
+  if (c->E < 1 || c->E > lmoe::kRouterMaxE)
+    return fail(MOE_ESHAPE, "%s: E=%d outside 1..%d", fn, c->E, lmoe::kRouterMaxE);
+  if (c->k < 1 || c->k > lmoe::kRouterMaxK)
+    return fail(MOE_EINVAL, "%s: k=%d outside 1..%d", fn, c->k, lmoe::kRouterMaxK);
+  const int32_t most = 1 << 20, unit = c->dtype == MOE_BF16 ? 64 : 8;
+  if (c->d_model < unit || c->d_model % unit != 0 || c->d_model > most)
+    return fail(MOE_ESHAPE, "%s: d_model=%d not a multiple of %d in %d..%d", fn, c->d_model, unit, unit, most);
+  if (c->d_ff < unit || c->d_ff % unit != 0 || c->d_ff > most)
+    return fail(MOE_ESHAPE, "%s: d_ff=%d not a multiple of %d in %d..%d", fn, c->d_ff, unit, unit, most);
+  if (c->T > (int64_t)1 << 30 || c->T * c->k > (int64_t)1 << 30) return fail(MOE_ESHAPE, "%s: T * k above 2^30", fn);
+  const int64_t x = std::max(c->d_model, c->d_ff);
+  if ((c->T * c->k + 15 * c->E) * x > (int64_t)1 << 40) return fail(MOE_ESHAPE, "%s: T * k * max(d, f) too large", fn);
+  // The bf16 products address one operand with 32-bit byte offsets.
+  if (products && c->dtype == MOE_BF16 &&
+      ((lmoe::sorted_rows(*c) + 15) * x * 2 >= (int64_t)1 << 31 || (int64_t)c->d_model * c->d_ff * 2 >= (int64_t)1 << 31))
+    return fail(MOE_ESHAPE, "%s: a bf16 buffer of rows and one expert's matrix must stay under 2 GiB", fn);
+  return MOE_OK;
+}
+
+// The layer's sizes as the gate's weight gradient takes them.
+moe_cfg gate_cfg(const moe_sorted_cfg& c) {
+  moe_cfg m{};
+  m.T = c.T;
+  m.d_model = c.d_model;
+  m.d_ff = c.d_ff;
+  m.E = c.E;
+  m.k = std::min(c.k, c.E);
+  m.C = m.G = 1;
+  m.dtype = c.dtype;
+  return m;
+}
+
+}  // namespace
+
+int64_t moe_sorted_rows(const moe_sorted_cfg* cfg) {
+  if (check_sorted(cfg, "moe_sorted_rows", false) != MOE_OK) return -1;
+  return lmoe::sorted_rows(*cfg);
+}
+
+size_t moe_sorted_workspace_bytes(const moe_sorted_cfg* cfg, int32_t call) {
+  const char* fn = "moe_sorted_workspace_bytes";
+  if (check_sorted(cfg, fn, false) != MOE_OK) return 0;
+  switch (call) {
+    case MOE_CALL_DISPATCH: return lmoe::sorted_dispatch_ws_bytes(*cfg);
+    case MOE_CALL_FFN_FWD:
+    case MOE_CALL_BWD_DX: return lmoe::sorted_ffn_ws_bytes(*cfg);
+    case MOE_CALL_BWD_DW: return cfg->E <= lmoe::kMaxE ? lmoe::bwd_dw_ws_bytes(gate_cfg(*cfg)) : 0;
+    default: fail(MOE_EINVAL, "%s: no workspace for call %d", fn, call); return 0;
+  }
+}
+
+moe_status moe_sorted_dispatch(const moe_sorted_cfg* cfg, const void* x, const int32_t* idx, int32_t* row_begin,
+                               int32_t* row_end, int32_t* slot, int32_t* src, void* rows, void* ws, size_t ws_bytes,
+                               moe_stream_t stream) {
+  const char* fn = "moe_sorted_dispatch";
+  CHECK(check_sorted(cfg, fn, false));
+  REQUIRE_TPTR(x); REQUIRE_TPTR(idx); REQUIRE_PTR(row_begin); REQUIRE_PTR(row_end);
+  REQUIRE_TPTR(slot); REQUIRE_TPTR(src); REQUIRE_TPTR(rows);
+  REFUSE_ALIAS({row_begin, row_end, slot, src, rows}, {x, idx});
+  REQUIRE_WS(lmoe::sorted_dispatch_ws_bytes(*cfg));
+  CHECK(check_device(fn));
+  lmoe::launch_sorted_dispatch(*cfg, x, idx, row_begin, row_end, slot, src, rows, ws, (hipStream_t)stream);
+  return check_launch(fn);
+}
+
+moe_status moe_sorted_ffn_fwd(const moe_sorted_cfg* cfg, const void* rows, const int32_t* row_begin,
+                              const int32_t* row_end, const void* W1p, const void* W2p, void* H, void* A,
+                              void* expert_out, void* ws, size_t ws_bytes, moe_stream_t stream) {
+  const char* fn = "moe_sorted_ffn_fwd";
+  CHECK(check_sorted(cfg, fn, true));
+  REQUIRE_TPTR(rows); REQUIRE_PTR(row_begin); REQUIRE_PTR(row_end); REQUIRE_PTR(W1p); REQUIRE_PTR(W2p);
+  REQUIRE_TPTR(H); REQUIRE_TPTR(A); REQUIRE_TPTR(expert_out);
+  REFUSE_ALIAS({H, A, expert_out}, {rows, row_begin, row_end, W1p, W2p});
+  REQUIRE_WS(lmoe::sorted_ffn_ws_bytes(*cfg));
+  CHECK(check_device(fn));
+  lmoe::launch_sorted_fwd(*cfg, rows, row_begin, row_end, W1p, W2p, H, A, expert_out, ws, (hipStream_t)stream);
+  return check_launch(fn);
+}
+
+moe_status moe_sorted_combine(const moe_sorted_cfg* cfg, const void* expert_out, const int32_t* slot, const float* w,
+                              void* y, moe_stream_t stream) {
+  const char* fn = "moe_sorted_combine";
+  CHECK(check_sorted(cfg, fn, false));
+  REQUIRE_TPTR(expert_out); REQUIRE_TPTR(slot); REQUIRE_TPTR(w); REQUIRE_TPTR(y);
+  REFUSE_ALIAS({y}, {expert_out, slot, w});
+  CHECK(check_device(fn));
+  lmoe::launch_sorted_combine(*cfg, expert_out, slot, w, y, (hipStream_t)stream);
+  return check_launch(fn);
+}
+
+moe_status moe_sorted_combine_bwd(const moe_sorted_cfg* cfg, const void* expert_out, const int32_t* slot,
+                                  const int32_t* src, const float* w, const void* dy, void* dO, float* dw,
+                                  moe_stream_t stream) {
+  const char* fn = "moe_sorted_combine_bwd";
+  CHECK(check_sorted(cfg, fn, false));
+  REQUIRE_TPTR(expert_out); REQUIRE_TPTR(slot); REQUIRE_TPTR(src); REQUIRE_TPTR(w); REQUIRE_TPTR(dy);
+  REQUIRE_TPTR(dO); REQUIRE_TPTR(dw);
+  REFUSE_ALIAS({dO, dw}, {expert_out, slot, src, w, dy});
+  CHECK(check_device(fn));
+  lmoe::launch_sorted_combine_bwd(*cfg, expert_out, slot, src, w, dy, dO, dw, (hipStream_t)stream);
+  return check_launch(fn);
+}
+
+moe_status moe_sorted_bwd_dx(const moe_sorted_cfg* cfg, const int32_t* row_begin, const int32_t* row_end, const void* H,
+                             const void* W1p, const void* W2p, const void* dO, void* dH, void* dXe, void* ws,
+                             size_t ws_bytes, moe_stream_t stream) {
+  const char* fn = "moe_sorted_bwd_dx";
+  CHECK(check_sorted(cfg, fn, true));
+  REQUIRE_PTR(row_begin); REQUIRE_PTR(row_end); REQUIRE_TPTR(H); REQUIRE_PTR(W1p); REQUIRE_PTR(W2p);
+  REQUIRE_TPTR(dO); REQUIRE_TPTR(dH); REQUIRE_TPTR(dXe);
+  REFUSE_ALIAS({dH, dXe}, {row_begin, row_end, H, W1p, W2p, dO});
+  REQUIRE_WS(lmoe::sorted_ffn_ws_bytes(*cfg));
+  CHECK(check_device(fn));
+  lmoe::launch_sorted_bwd_dx(*cfg, row_begin, row_end, H, W1p, W2p, dO, dH, dXe, ws, (hipStream_t)stream);
+  return check_launch(fn);
+}
+
+moe_status moe_sorted_dispatch_bwd(const moe_sorted_cfg* cfg, const int32_t* slot, const void* dXe, const void* Wg,
+                                   const float* dlogits, void* dx, moe_stream_t stream) {
+  const char* fn = "moe_sorted_dispatch_bwd";
+  CHECK(check_sorted(cfg, fn, false));
+  REQUIRE_TPTR(slot); REQUIRE_TPTR(dXe); OPTIONAL_PTR(Wg); OPTIONAL_PTR(dlogits); REQUIRE_TPTR(dx);
+  if (cfg->T > 0 && (Wg == nullptr) != (dlogits == nullptr))
+    return fail(MOE_EINVAL, "%s: Wg and dlogits go together", fn);
+  REFUSE_ALIAS({dx}, {slot, dXe, Wg, dlogits});
+  CHECK(check_device(fn));
+  lmoe::launch_sorted_dispatch_bwd(*cfg, slot, dXe, Wg, dlogits, dx, (hipStream_t)stream);
+  return check_launch(fn);
+}
+
+moe_status moe_sorted_bwd_dw(const moe_sorted_cfg* cfg, const int32_t* row_begin, const int32_t* row_end,
+                             const void* rows, const void* A, const void* dO, const void* dH, void* dW1, void* dW2,
+                             const void* x, const float* dlogits, float* dWg, void* ws, size_t ws_bytes,
+                             moe_stream_t stream) {
+  const char* fn = "moe_sorted_bwd_dw";
+  CHECK(check_sorted(cfg, fn, true));
+  REQUIRE_PTR(row_begin); REQUIRE_PTR(row_end); REQUIRE_TPTR(rows); REQUIRE_TPTR(A); REQUIRE_TPTR(dO); REQUIRE_TPTR(dH);
+  REQUIRE_PTR(dW1); REQUIRE_PTR(dW2);
+  OPTIONAL_PTR(x); OPTIONAL_PTR(dlogits); OPTIONAL_PTR(dWg);
+  if (dWg == nullptr ? x != nullptr || dlogits != nullptr : cfg->T > 0 && (x == nullptr || dlogits == nullptr))
+    return fail(MOE_EINVAL, "%s: x, dlogits and dWg go together", fn);
+  REFUSE_ALIAS({dW1, dW2, dWg}, {row_begin, row_end, rows, A, dO, dH, x, dlogits});
+  if (dWg != nullptr) {
+    if (cfg->E > lmoe::kMaxE) return fail(MOE_ESHAPE, "%s: dWg is for up to %d experts, E=%d", fn, lmoe::kMaxE, cfg->E);
+    REQUIRE_WS(lmoe::bwd_dw_ws_bytes(gate_cfg(*cfg)));
+  }
+  CHECK(check_device(fn));
+  lmoe::launch_sorted_bwd_dw(*cfg, row_begin, row_end, rows, A, dO, dH, dW1, dW2, (hipStream_t)stream);
+  if (dWg != nullptr) lmoe::launch_dwg(gate_cfg(*cfg), x, dlogits, dWg, ws, (hipStream_t)stream);
+  return check_launch(fn);
+}
+
+// -------------------------------------------------------------- token lookup
+namespace {
+
+moe_status check_embed(const moe_embed_cfg* c, const char* fn) {
+  if (!c) return fail(MOE_EINVAL, "%s: cfg is NULL", fn);
+  if (c->dtype != MOE_F32 && c->dtype != MOE_BF16) return fail(MOE_EDTYPE, "%s: unknown dtype %d", fn, c->dtype);
+  if (c->T < 0) return fail(MOE_EINVAL, "%s: T < 0", fn);
+  if (c->V < 1 || c->V > 1 << 30) return fail(MOE_ESHAPE, "%s: V=%d outside 1..2^30", fn, c->V);
+  if (c->d_model < 8 || c->d_model % 8 != 0) return fail(MOE_ESHAPE, "%s: d_model=%d not a positive multiple of 8", fn, c->d_model);
+  if (c->T > (int64_t)1 << 30 || c->T * c->d_model > (int64_t)1 << 40 || (int64_t)c->V * c->d_model > (int64_t)1 << 40)
+    return fail(MOE_ESHAPE, "%s: T above 2^30, or T * d_model or V * d_model above 2^40", fn);
+  if (!std::isfinite(c->scale)) return fail(MOE_EINVAL, "%s: scale is not finite", fn);
+  if (c->accum != 0 && c->accum != 1) return fail(MOE_EINVAL, "%s: accum must be 0 or 1", fn);
+  return MOE_OK;
+}
+
+}  // namespace
+
+moe_status moe_embed(const moe_embed_cfg* cfg, const int32_t* ids, const void* W, void* y, moe_stream_t stream) {
+  const char* fn = "moe_embed";
+  CHECK(check_embed(cfg, fn));
+  REQUIRE_TPTR(ids); REQUIRE_PTR(W); REQUIRE_TPTR(y);
+  REFUSE_ALIAS({y}, {ids, W});
+  CHECK(check_device(fn));
+  lmoe::launch_embed(*cfg, ids, W, y, (hipStream_t)stream);
+  return check_launch(fn);
+}
+
+size_t moe_embed_bwd_workspace_bytes(const moe_embed_cfg* cfg) {
+  if (check_embed(cfg, "moe_embed_bwd_workspace_bytes") != MOE_OK) return 0;
+  return lmoe::embed_bwd_ws_bytes(*cfg);
+}
+
+moe_status moe_embed_bwd(const moe_embed_cfg* cfg, const int32_t* ids, const void* dy, void* dW, void* ws,
+                         size_t ws_bytes, moe_stream_t stream) {
+  const char* fn = "moe_embed_bwd";
+  CHECK(check_embed(cfg, fn));
+  REQUIRE_TPTR(ids); REQUIRE_TPTR(dy); REQUIRE_PTR(dW);
+  REFUSE_ALIAS({dW, ws}, {ids, dy});
+  REQUIRE_WS(lmoe::embed_bwd_ws_bytes(*cfg));
+  CHECK(check_device(fn));
+  lmoe::launch_embed_bwd(*cfg, ids, dy, dW, ws, (hipStream_t)stream);
   return check_launch(fn);
 }
 

@@ -35,12 +35,26 @@ struct Abi {   // addresses in the loaded library, given by init()
   decltype(&moe_ckpt_bytes) ckpt_bytes;
   decltype(&moe_ckpt_save) ckpt_save;
   decltype(&moe_ckpt_load) ckpt_load;
+  decltype(&moe_sorted_rows) sorted_rows;
+  decltype(&moe_sorted_workspace_bytes) sorted_workspace_bytes;
+  decltype(&moe_sorted_dispatch) sorted_dispatch;
+  decltype(&moe_sorted_ffn_fwd) sorted_ffn_fwd;
+  decltype(&moe_sorted_combine) sorted_combine;
+  decltype(&moe_sorted_combine_bwd) sorted_combine_bwd;
+  decltype(&moe_sorted_bwd_dx) sorted_bwd_dx;
+  decltype(&moe_sorted_dispatch_bwd) sorted_dispatch_bwd;
+  decltype(&moe_sorted_bwd_dw) sorted_bwd_dw;
+  decltype(&moe_embed) embed;
+  decltype(&moe_embed_bwd_workspace_bytes) embed_bwd_workspace_bytes;
+  decltype(&moe_embed_bwd) embed_bwd;
 } g_abi;
 PyObject* g_stream;      // the module's function from a stream argument to a raw stream
 PyObject* g_cfg_type;    // the ctypes structures
 PyObject* g_block_type;
 PyObject* g_route_type;
 PyObject* g_w4_type;
+PyObject* g_sorted_type;
+PyObject* g_embed_type;
 
 struct Error {};   // a Python exception is set
 
@@ -109,6 +123,8 @@ template <> PyObject* struct_type<moe_cfg>() { return g_cfg_type; }
 template <> PyObject* struct_type<moe_block_cfg>() { return g_block_type; }
 template <> PyObject* struct_type<moe_route_cfg>() { return g_route_type; }
 template <> PyObject* struct_type<moe_w4_cfg>() { return g_w4_type; }
+template <> PyObject* struct_type<moe_sorted_cfg>() { return g_sorted_type; }
+template <> PyObject* struct_type<moe_embed_cfg>() { return g_embed_type; }
 
 // A ctypes structure's bytes.
 template <typename T>
@@ -630,9 +646,180 @@ ENTRY(ckpt_load) {   // cfg, ckpt, row_begin, row_end, send_buf, H, A, expert_ou
   });
 }
 
-// init({C ABI name: address}, stream function, moe_cfg type, moe_block_cfg type[, moe_route_cfg type, moe_w4_cfg type])
+at::ScalarType dtype_of(const moe_sorted_cfg* c) { return c->dtype == MOE_BF16 ? kBf16 : kF32; }
+at::ScalarType dtype_of(const moe_embed_cfg* c) { return c->dtype == MOE_BF16 ? kBf16 : kF32; }
+// Rows of the sorted buffers (0 of a cfg that the call refuses).
+Num sorted_rows(const moe_sorted_cfg* c) {
+  const int64_t r = g_abi.sorted_rows(c);
+  return r < 0 ? 0 : r;
+}
+
+ENTRY(sorted_dispatch) {   // cfg, x, idx, row_begin, row_end, slot, src, rows, ws, stream
+  return entry(n, 10, [&] {
+    Struct<moe_sorted_cfg> c(a[0]);
+    const auto dt = dtype_of(c);
+    const Num T = c->T, d = c->d_model, E = c->E, k = c->k, R = sorted_rows(c);
+    const size_t need = g_abi.sorted_workspace_bytes(c, MOE_CALL_DISPATCH);
+    const void* x = ptr(a[1], "x", dt, T * d);
+    const int32_t* idx = (const int32_t*)ptr(a[2], "idx", kI32, T * k);
+    int32_t* rb = (int32_t*)ptr(a[3], "row_begin", kI32, E);
+    int32_t* re = (int32_t*)ptr(a[4], "row_end", kI32, E);
+    int32_t* slot = (int32_t*)ptr(a[5], "slot", kI32, T * k);
+    int32_t* src = (int32_t*)ptr(a[6], "src", kI32, R);
+    void* rows = ptr(a[7], "rows", dt, R * d);
+    void* ws = ptr(a[8], "ws", at::kByte, need, need == 0);
+    const size_t wsn = numel_or_0(a[8]);
+    void* s = stream_arg(a[9]);
+    return status([&] { return g_abi.sorted_dispatch(c, x, idx, rb, re, slot, src, rows, ws, wsn, s); });
+  });
+}
+
+ENTRY(sorted_ffn_fwd) {   // cfg, rows, row_begin, row_end, W1p, W2p, H, A, expert_out, ws, stream
+  return entry(n, 11, [&] {
+    Struct<moe_sorted_cfg> c(a[0]);
+    const auto dt = dtype_of(c);
+    const Num d = c->d_model, f = c->d_ff, E = c->E, R = sorted_rows(c);
+    const size_t need = g_abi.sorted_workspace_bytes(c, MOE_CALL_FFN_FWD);
+    const void* rows = ptr(a[1], "rows", dt, R * d);
+    const int32_t* rb = (const int32_t*)ptr(a[2], "row_begin", kI32, E);
+    const int32_t* re = (const int32_t*)ptr(a[3], "row_end", kI32, E);
+    const void* W1p = ptr(a[4], "W1p", dt, E * f * d);
+    const void* W2p = ptr(a[5], "W2p", dt, E * d * f);
+    void* H = ptr(a[6], "H", dt, R * f);
+    void* A = ptr(a[7], "A", dt, R * f);
+    void* O = ptr(a[8], "expert_out", dt, R * d);
+    void* ws = ptr(a[9], "ws", at::kByte, need, need == 0);
+    const size_t wsn = numel_or_0(a[9]);
+    void* s = stream_arg(a[10]);
+    return status([&] { return g_abi.sorted_ffn_fwd(c, rows, rb, re, W1p, W2p, H, A, O, ws, wsn, s); });
+  });
+}
+
+ENTRY(sorted_combine) {   // cfg, expert_out, slot, w, y, stream
+  return entry(n, 6, [&] {
+    Struct<moe_sorted_cfg> c(a[0]);
+    const auto dt = dtype_of(c);
+    const Num T = c->T, d = c->d_model, k = c->k, R = sorted_rows(c);
+    const void* O = ptr(a[1], "expert_out", dt, R * d);
+    const int32_t* slot = (const int32_t*)ptr(a[2], "slot", kI32, T * k);
+    const float* w = (const float*)ptr(a[3], "w", kF32, T * k);
+    void* y = ptr(a[4], "y", dt, T * d);
+    void* s = stream_arg(a[5]);
+    return status([&] { return g_abi.sorted_combine(c, O, slot, w, y, s); });
+  });
+}
+
+ENTRY(sorted_combine_bwd) {   // cfg, expert_out, slot, src, w, dy, dO, dw, stream
+  return entry(n, 9, [&] {
+    Struct<moe_sorted_cfg> c(a[0]);
+    const auto dt = dtype_of(c);
+    const Num T = c->T, d = c->d_model, k = c->k, R = sorted_rows(c);
+    const void* O = ptr(a[1], "expert_out", dt, R * d);
+    const int32_t* slot = (const int32_t*)ptr(a[2], "slot", kI32, T * k);
+    const int32_t* src = (const int32_t*)ptr(a[3], "src", kI32, R);
+    const float* w = (const float*)ptr(a[4], "w", kF32, T * k);
+    const void* dy = ptr(a[5], "dy", dt, T * d);
+    void* dO = ptr(a[6], "dO", dt, R * d);
+    float* dw = (float*)ptr(a[7], "dw", kF32, T * k);
+    void* s = stream_arg(a[8]);
+    return status([&] { return g_abi.sorted_combine_bwd(c, O, slot, src, w, dy, dO, dw, s); });
+  });
+}
+
+ENTRY(sorted_bwd_dx) {   // cfg, row_begin, row_end, H, W1p, W2p, dO, dH, dXe, ws, stream
+  return entry(n, 11, [&] {
+    Struct<moe_sorted_cfg> c(a[0]);
+    const auto dt = dtype_of(c);
+    const Num d = c->d_model, f = c->d_ff, E = c->E, R = sorted_rows(c);
+    const size_t need = g_abi.sorted_workspace_bytes(c, MOE_CALL_BWD_DX);
+    const int32_t* rb = (const int32_t*)ptr(a[1], "row_begin", kI32, E);
+    const int32_t* re = (const int32_t*)ptr(a[2], "row_end", kI32, E);
+    const void* H = ptr(a[3], "H", dt, R * f);
+    const void* W1p = ptr(a[4], "W1p", dt, E * f * d);
+    const void* W2p = ptr(a[5], "W2p", dt, E * d * f);
+    const void* dO = ptr(a[6], "dO", dt, R * d);
+    void* dH = ptr(a[7], "dH", dt, R * f);
+    void* dXe = ptr(a[8], "dXe", dt, R * d);
+    void* ws = ptr(a[9], "ws", at::kByte, need, need == 0);
+    const size_t wsn = numel_or_0(a[9]);
+    void* s = stream_arg(a[10]);
+    return status([&] { return g_abi.sorted_bwd_dx(c, rb, re, H, W1p, W2p, dO, dH, dXe, ws, wsn, s); });
+  });
+}
+
+ENTRY(sorted_dispatch_bwd) {   // cfg, slot, dXe, Wg, dlogits, dx, stream
+  return entry(n, 7, [&] {
+    Struct<moe_sorted_cfg> c(a[0]);
+    const auto dt = dtype_of(c);
+    const Num T = c->T, d = c->d_model, E = c->E, k = c->k, R = sorted_rows(c);
+    const int32_t* slot = (const int32_t*)ptr(a[1], "slot", kI32, T * k);
+    const void* dXe = ptr(a[2], "dXe", dt, R * d);
+    const void* Wg = ptr(a[3], "Wg", dt, E * d, true);
+    const float* dl = (const float*)ptr(a[4], "dlogits", kF32, T * E, true);
+    void* dx = ptr(a[5], "dx", dt, T * d);
+    void* s = stream_arg(a[6]);
+    return status([&] { return g_abi.sorted_dispatch_bwd(c, slot, dXe, Wg, dl, dx, s); });
+  });
+}
+
+ENTRY(sorted_bwd_dw) {   // cfg, row_begin, row_end, rows, A, dO, dH, dW1, dW2, x, dlogits, dWg, ws, stream
+  return entry(n, 14, [&] {
+    Struct<moe_sorted_cfg> c(a[0]);
+    const auto dt = dtype_of(c);
+    const Num T = c->T, d = c->d_model, f = c->d_ff, E = c->E, R = sorted_rows(c);
+    const bool gate = a[11] != Py_None;
+    const size_t need = gate ? g_abi.sorted_workspace_bytes(c, MOE_CALL_BWD_DW) : 0;
+    const int32_t* rb = (const int32_t*)ptr(a[1], "row_begin", kI32, E);
+    const int32_t* re = (const int32_t*)ptr(a[2], "row_end", kI32, E);
+    const void* rows = ptr(a[3], "rows", dt, R * d);
+    const void* A = ptr(a[4], "A", dt, R * f);
+    const void* dO = ptr(a[5], "dO", dt, R * d);
+    const void* dH = ptr(a[6], "dH", dt, R * f);
+    void* dW1 = ptr(a[7], "dW1", dt, E * f * d);
+    void* dW2 = ptr(a[8], "dW2", dt, E * d * f);
+    const void* x = ptr(a[9], "x", dt, T * d, true);
+    const float* dl = (const float*)ptr(a[10], "dlogits", kF32, T * E, true);
+    float* dWg = (float*)ptr(a[11], "dWg", kF32, E * d, true);
+    void* ws = ptr(a[12], "ws", at::kByte, need, need == 0);
+    const size_t wsn = numel_or_0(a[12]);
+    void* s = stream_arg(a[13]);
+    return status([&] { return g_abi.sorted_bwd_dw(c, rb, re, rows, A, dO, dH, dW1, dW2, x, dl, dWg, ws, wsn, s); });
+  });
+}
+
+ENTRY(embed) {   // cfg, ids, W, y, stream
+  return entry(n, 5, [&] {
+    Struct<moe_embed_cfg> c(a[0]);
+    const auto dt = dtype_of(c);
+    const Num T = c->T, V = c->V, d = c->d_model;
+    const int32_t* ids = (const int32_t*)ptr(a[1], "ids", kI32, T);
+    const void* W = ptr(a[2], "W", dt, V * d);
+    void* y = ptr(a[3], "y", dt, T * d);
+    void* s = stream_arg(a[4]);
+    return status([&] { return g_abi.embed(c, ids, W, y, s); });
+  });
+}
+
+ENTRY(embed_bwd) {   // cfg, ids, dy, dW, ws, stream
+  return entry(n, 6, [&] {
+    Struct<moe_embed_cfg> c(a[0]);
+    const auto dt = dtype_of(c);
+    const Num T = c->T, V = c->V, d = c->d_model;
+    const size_t need = g_abi.embed_bwd_workspace_bytes(c);
+    const int32_t* ids = (const int32_t*)ptr(a[1], "ids", kI32, T);
+    const void* dy = ptr(a[2], "dy", dt, T * d);
+    void* dW = ptr(a[3], "dW", dt, V * d);
+    void* ws = ptr(a[4], "ws", at::kByte, need, need == 0);
+    const size_t wsn = numel_or_0(a[4]);
+    void* s = stream_arg(a[5]);
+    return status([&] { return g_abi.embed_bwd(c, ids, dy, dW, ws, wsn, s); });
+  });
+}
+
+// init({C ABI name: address}, stream function, moe_cfg type, moe_block_cfg type[, moe_route_cfg type, moe_w4_cfg type
+// [, moe_sorted_cfg type, moe_embed_cfg type]])
 ENTRY(init) {
-  if (n != 4 && n != 6) return PyErr_Format(PyExc_TypeError, "init takes 4 or 6 arguments");
+  if (n != 4 && n != 6 && n != 8) return PyErr_Format(PyExc_TypeError, "init takes 4, 6 or 8 arguments");
   PyObject* d = a[0];
   auto set = [&](auto& fn, const char* name) {
     Item it(d, name);
@@ -666,10 +853,24 @@ ENTRY(init) {
     set(g_abi.ckpt_bytes, "moe_ckpt_bytes");
     set(g_abi.ckpt_save, "moe_ckpt_save");
     set(g_abi.ckpt_load, "moe_ckpt_load");
+    if (n > 6) {
+      set(g_abi.sorted_rows, "moe_sorted_rows");
+      set(g_abi.sorted_workspace_bytes, "moe_sorted_workspace_bytes");
+      set(g_abi.sorted_dispatch, "moe_sorted_dispatch");
+      set(g_abi.sorted_ffn_fwd, "moe_sorted_ffn_fwd");
+      set(g_abi.sorted_combine, "moe_sorted_combine");
+      set(g_abi.sorted_combine_bwd, "moe_sorted_combine_bwd");
+      set(g_abi.sorted_bwd_dx, "moe_sorted_bwd_dx");
+      set(g_abi.sorted_dispatch_bwd, "moe_sorted_dispatch_bwd");
+      set(g_abi.sorted_bwd_dw, "moe_sorted_bwd_dw");
+      set(g_abi.embed, "moe_embed");
+      set(g_abi.embed_bwd_workspace_bytes, "moe_embed_bwd_workspace_bytes");
+      set(g_abi.embed_bwd, "moe_embed_bwd");
+    }
   } catch (const Error&) {
     return nullptr;
   }
-  PyObject** slots[] = {&g_stream, &g_cfg_type, &g_block_type, &g_route_type, &g_w4_type};
+  PyObject** slots[] = {&g_stream, &g_cfg_type, &g_block_type, &g_route_type, &g_w4_type, &g_sorted_type, &g_embed_type};
   for (int i = 0; i < n - 1; ++i) {
     Py_INCREF(a[i + 1]);
     Py_XSETREF(*slots[i], a[i + 1]);
@@ -697,6 +898,15 @@ PyMethodDef kMethods[] = {METHOD(init),
                           METHOD(experts_w4),
                           METHOD(ckpt_save),
                           METHOD(ckpt_load),
+                          METHOD(sorted_dispatch),
+                          METHOD(sorted_ffn_fwd),
+                          METHOD(sorted_combine),
+                          METHOD(sorted_combine_bwd),
+                          METHOD(sorted_bwd_dx),
+                          METHOD(sorted_dispatch_bwd),
+                          METHOD(sorted_bwd_dw),
+                          METHOD(embed),
+                          METHOD(embed_bwd),
                           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_bind", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 

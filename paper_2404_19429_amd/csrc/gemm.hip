@@ -217,10 +217,12 @@ __global__ __launch_bounds__(256) void gemm_f32_kernel(GemmParams p, int tm, int
 }
 
 template <int WT, bool B_K, bool RAGGED_K, int EPI>
-static void launch_f32(const GemmParams& p, int groups, int64_t rows, int cols, hipStream_t s) {
-  // (ragged-M: with up to 15 alignment rows, as wide_tile_prefix counts them)
+static void launch_f32(const GemmParams& p, int groups, int64_t rows, int cols, hipStream_t s, int64_t all_rows = 0) {
+  // (ragged-M: with up to 15 alignment rows, as wide_tile_prefix counts them; all_rows: the groups' rows together
+  // are at most so many)
   const int tm = (int)((rows + (RAGGED_K ? 0 : 15) + 32 * WT - 1) / (32 * WT)), tn = (cols + 32 * WT - 1) / (32 * WT);
-  const int64_t blocks = RAGGED_K ? ((int64_t)groups * tm + 7) / 8 * 8 * tn : ((int64_t)groups * tm * tn + 7) / 8 * 8;
+  const int64_t mt = all_rows > 0 ? (all_rows + 15 * groups) / (32 * WT) + groups : (int64_t)groups * tm;
+  const int64_t blocks = RAGGED_K ? ((int64_t)groups * tm + 7) / 8 * 8 * tn : (mt * tn + 7) / 8 * 8;
   hipLaunchKernelGGL((gemm_f32_kernel<WT, B_K, RAGGED_K, EPI>), dim3((unsigned)blocks), dim3(256), 0, s, p, tm, tn,
                      groups);
 }
@@ -346,9 +348,11 @@ static TileK tile_k(const WideCall& w, int cus) {
 }
 static void run_wide_any(const WideCall& w, hipStream_t s) {
   if (w.rows <= 0 || w.cols <= 0 || w.groups <= 0) return;
-  if (w.kind < WK_DW) return kTilesM[tile_m(w, num_cus())].run(w, s);
-  const TileK t = tile_k(w, num_cus());
   WideCall q = w;
+  if (q.p.eA == 0) q.p.eA = q.p.sA;
+  if (q.p.eB == 0) q.p.eB = q.p.sB;
+  if (w.kind < WK_DW) return kTilesM[tile_m(w, num_cus())].run(q, s);
+  const TileK t = tile_k(w, num_cus());
   q.p.only = t == kTileKByRows ? 1 : 0;
   if (t != kTileK128) run_wide_256x256(q, s);
   q.p.only = t == kTileKByRows ? 2 : 0;
@@ -540,6 +544,104 @@ void launch_expert_bwd_dw(const moe_cfg& c, const void* X, const void* A, const 
   tb = ptimer_begin(kProdDW1, s);
   run_expert<false, true, EPI_STORE>(c, blk ? WK_DW_BLK : WK_DW, p1, f, (int)d, s, false, beside);
   ptimer_end(tb, s);
+}
+
+// ------------------------------------------------- experts over sorted rows
+// The same products over one buffer of rows that the experts share (moe_sorted_*):
+// groups without a stride, each on its range of rows, which in bf16 starts at a
+// 16-row block; up to kMaxE experts a launch.
+namespace {
+struct Part {   // experts [e0, e0 + n) of a call
+  int e0, n;
+};
+template <typename F>
+void each_part(const moe_sorted_cfg& c, F&& f) {
+  for (int e = 0; e < c.E; e += kMaxE) f(Part{e, std::min(kMaxE, c.E - e)});
+}
+
+// One product: C rows or, ragged-K, C_e = A_e^T B_e.  X elements a row of A; wide operands as for run_expert.
+template <bool B_K, bool RAGGED_K, int EPI>
+void run_sorted(const moe_sorted_cfg& c, const Part& part, int prod, WideKind kind, GemmParams p, int64_t rows, int cols,
+                void* ws, hipStream_t s) {
+  const int64_t R = sorted_rows(c);
+  p.cap = (int)R;
+  p.act = c.act;
+  p.part = (float*)ws;
+  p.ksplit = 1;
+  p.rb += part.e0;
+  p.re += part.e0;
+  const double expect = (double)c.T * c.k / c.E;
+  const WideCall w{kind, c.act, part.n, rows, cols, expect, std::sqrt(expect * (1. - (double)c.k / c.E)), p};
+  const bool tb = ptimer_begin(prod, s);
+  if (c.dtype == MOE_BF16) {
+    run_wide_any(w, s);
+  } else {
+    WideCall q = w;
+    if (!RAGGED_K) q.rows = R / part.n + 32;   // (the bound on the grid that f32_tile looks at)
+    const int64_t all = RAGGED_K ? 0 : R;
+    if (f32_tile(q, num_cus()) == 32) launch_f32<1, B_K, RAGGED_K, EPI>(p, part.n, rows, cols, s, all);
+    else launch_f32<2, B_K, RAGGED_K, EPI>(p, part.n, rows, cols, s, all);
+  }
+  ptimer_end(tb, s);
+}
+// Element e of the experts' matrices of n elements each.
+const void* mat(const moe_sorted_cfg& c, const void* W, int64_t e, int64_t n) {
+  return (const char*)W + e * n * (c.dtype == MOE_BF16 ? 2 : 4);
+}
+}  // namespace
+
+size_t sorted_ffn_ws_bytes(const moe_sorted_cfg& c) {
+  return c.dtype == MOE_BF16 ? (size_t)kSkPartElems * sizeof(float) : 0;
+}
+
+void launch_sorted_fwd(const moe_sorted_cfg& c, const void* X, const int32_t* rb, const int32_t* re, const void* W1,
+                       const void* W2, void* H, void* A, void* O, void* ws, hipStream_t s) {
+  const int64_t d = c.d_model, f = c.d_ff, R = sorted_rows(c);
+  if (R == 0) return;
+  each_part(c, [&](const Part& q) {
+    GemmParams p{X, d, 0, mat(c, W1, q.e0, f * d), d, f * d, H, f, 0, A, nullptr, rb, re, 0, (int)f, (int)d};
+    p.eA = R * d;
+    run_sorted<true, false, EPI_FWD1>(c, q, kProdFwd1, WK_FWD1, p, R, (int)f, ws, s);
+  });
+  each_part(c, [&](const Part& q) {
+    GemmParams p{A, f, 0, mat(c, W2, q.e0, d * f), f, d * f, O, d, 0, nullptr, nullptr, rb, re, 0, (int)d, (int)f};
+    p.eA = R * f;
+    run_sorted<true, false, EPI_STORE>(c, q, kProdFwd2, WK_NK, p, R, (int)d, ws, s);
+  });
+}
+
+void launch_sorted_bwd_dx(const moe_sorted_cfg& c, const int32_t* rb, const int32_t* re, const void* H, const void* W1,
+                          const void* W2, const void* dO, void* dH, void* dXe, void* ws, hipStream_t s) {
+  const int64_t d = c.d_model, f = c.d_ff, R = sorted_rows(c);
+  if (R == 0) return;
+  each_part(c, [&](const Part& q) {
+    GemmParams p{dO, d, 0, mat(c, W2, q.e0, d * f), f, d * f, dH, f, 0, nullptr, H, rb, re, 0, (int)f, (int)d};
+    p.eA = R * d;
+    run_sorted<false, false, EPI_DACT>(c, q, kProdDA, WK_DACT, p, R, (int)f, ws, s);
+  });
+  each_part(c, [&](const Part& q) {
+    GemmParams p{dH, f, 0, mat(c, W1, q.e0, f * d), d, f * d, dXe, d, 0, nullptr, nullptr, rb, re, 0, (int)d, (int)f};
+    p.eA = R * f;
+    run_sorted<false, false, EPI_STORE>(c, q, kProdDXe, WK_KN, p, R, (int)d, ws, s);
+  });
+}
+
+void launch_sorted_bwd_dw(const moe_sorted_cfg& c, const int32_t* rb, const int32_t* re, const void* X, const void* A,
+                          const void* dO, const void* dH, void* dW1, void* dW2, hipStream_t s) {
+  const int64_t d = c.d_model, f = c.d_ff, R = sorted_rows(c);
+  const WideKind kind = c.wpacked && c.dtype == MOE_BF16 ? WK_DW_BLK : WK_DW;
+  each_part(c, [&](const Part& q) {
+    GemmParams p{dO, d, 0, A, f, 0, (void*)mat(c, dW2, q.e0, d * f), f, d * f, nullptr, nullptr, rb, re, (int)d, (int)f};
+    p.eA = R * d;
+    p.eB = R * f;
+    run_sorted<false, true, EPI_STORE>(c, q, kProdDW2, kind, p, d, (int)f, nullptr, s);
+  });
+  each_part(c, [&](const Part& q) {
+    GemmParams p{dH, f, 0, X, d, 0, (void*)mat(c, dW1, q.e0, f * d), d, f * d, nullptr, nullptr, rb, re, (int)f, (int)d};
+    p.eA = R * f;
+    p.eB = R * d;
+    run_sorted<false, true, EPI_STORE>(c, q, kProdDW1, kind, p, f, (int)d, nullptr, s);
+  });
 }
 
 // Sum of the S float partials of a K-split weight gradient, in group order,

@@ -34,6 +34,8 @@ struct GemmParams {
   int ksplit;       // wide plain-store ragged-M products: 1 = a short last round may be K-split
   int kchunk;       // rb == re == NULL and kchunk > 0: group g's rows are [g kchunk, (g + 1) kchunk)
   int only;         // ragged-K: 1 = run only if the groups are even, 2 = only if they are skewed, 0 = always
+  int64_t eA, eB;   // elements that a group's operand spans from its start (run_wide_any: sA, sB where 0; groups
+                    // that share one buffer have a stride of 0 and its extent)
 };
 
 // Row range of group g, clamped to the buffer so bad ranges cannot reach outside it.
@@ -698,14 +700,14 @@ gemm_wide_kernel(GemmParams p, int tilesM, int tilesN, int groups) {
     const WGeo G = geo(t);
     const uint16_t* Ab = (const uint16_t*)p.A + (RMO ? 0 : G.g * p.sA);
     const uint16_t* Bb = (const uint16_t*)p.B + (RMO ? 0 : G.g * p.sB);
-    const int64_t extA = RMO ? (int64_t)p.cap * p.lda : p.sA, extB = RMO ? (int64_t)p.cap * p.ldb : p.sB;
+    const int64_t extA = RMO ? (int64_t)p.cap * p.lda : p.eA, extB = RMO ? (int64_t)p.cap * p.ldb : p.eB;
     // (rows of the stage past the tile's BMT are not loaded: their places get zeros, which no wave reads)
     const int rlim = min((int)pad16(p.cap), G.lo_al + G.m0 + BMT);
-    if constexpr (AK) opA.plan(Ab, p.sA, p.lda, G.lo_al + G.m0, rlim, 0, 0, 0, wid, lane);
+    if constexpr (AK) opA.plan(Ab, extA, p.lda, G.lo_al + G.m0, rlim, 0, 0, 0, wid, lane);
     else opA.plan(Ab, extA, p.lda, G.m0, p.M, G.lo_al, G.lo, G.hi, wid, lane);
-    if constexpr (BKK) opB.plan(Bb, p.sB, p.ldb, G.n0, p.N, 0, 0, 0, wid, lane);
+    if constexpr (BKK) opB.plan(Bb, extB, p.ldb, G.n0, p.N, 0, 0, 0, wid, lane);
     else if constexpr (RAGGED_K) opB.plan(Bb, extB, p.ldb, G.n0, p.N, G.lo_al, G.lo, G.hi, wid, lane);
-    else opB.plan(Bb, p.sB, p.ldb, G.n0, p.N, 0, 0, p.K, wid, lane);
+    else opB.plan(Bb, extB, p.ldb, G.n0, p.N, 0, 0, p.K, wid, lane);
     if (lkend == 0) lkend = G.nk;
   };
   auto enter = [&]() __attribute__((always_inline)) {   // load cursor onto segment le

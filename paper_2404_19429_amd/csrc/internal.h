@@ -99,6 +99,31 @@ size_t experts_w4_ws_bytes(const moe_w4_cfg& c);
 void launch_experts_w4(const moe_w4_cfg& c, const void* x, const int32_t* idx, const float* w, const uint8_t* W1c,
                        const uint8_t* W1s, const uint8_t* W2c, const uint8_t* W2s, void* y, void* ws, hipStream_t s);
 
+// sorted.hip: tokens sorted by expert and back.
+int64_t sorted_rows(const moe_sorted_cfg& c);
+size_t sorted_dispatch_ws_bytes(const moe_sorted_cfg& c);
+void launch_sorted_dispatch(const moe_sorted_cfg& c, const void* x, const int32_t* idx, int32_t* row_begin,
+                            int32_t* row_end, int32_t* slot, int32_t* src, void* rows, void* ws, hipStream_t s);
+void launch_sorted_combine(const moe_sorted_cfg& c, const void* O, const int32_t* slot, const float* w, void* y,
+                           hipStream_t s);
+void launch_sorted_combine_bwd(const moe_sorted_cfg& c, const void* O, const int32_t* slot, const int32_t* src,
+                               const float* w, const void* dy, void* dO, float* dw, hipStream_t s);
+void launch_sorted_dispatch_bwd(const moe_sorted_cfg& c, const int32_t* slot, const void* dXe, const void* Wg,
+                                const float* dlogits, void* dx, hipStream_t s);
+// gemm.hip: the experts' products over the sorted rows; sorted_ffn_ws_bytes for the forward and dx.
+size_t sorted_ffn_ws_bytes(const moe_sorted_cfg& c);
+void launch_sorted_fwd(const moe_sorted_cfg& c, const void* X, const int32_t* rb, const int32_t* re, const void* W1,
+                       const void* W2, void* H, void* A, void* O, void* ws, hipStream_t s);
+void launch_sorted_bwd_dx(const moe_sorted_cfg& c, const int32_t* rb, const int32_t* re, const void* H, const void* W1,
+                          const void* W2, const void* dO, void* dH, void* dXe, void* ws, hipStream_t s);
+void launch_sorted_bwd_dw(const moe_sorted_cfg& c, const int32_t* rb, const int32_t* re, const void* X, const void* A,
+                          const void* dO, const void* dH, void* dW1, void* dW2, hipStream_t s);
+
+// embed.hip
+void launch_embed(const moe_embed_cfg& c, const int32_t* ids, const void* W, void* y, hipStream_t s);
+size_t embed_bwd_ws_bytes(const moe_embed_cfg& c);
+void launch_embed_bwd(const moe_embed_cfg& c, const int32_t* ids, const void* dy, void* dW, void* ws, hipStream_t s);
+
 // ckpt.hip
 size_t ckpt_bytes(const moe_cfg& c);
 void launch_ckpt_save(const moe_cfg& c, const void* send, const void* H, const void* O, const int32_t* rb,

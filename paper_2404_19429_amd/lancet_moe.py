@@ -33,7 +33,10 @@ EXPORTS = ["moe_capacity", "moe_workspace_bytes", "moe_last_error", "moe_gate_to
            "moe_block_workspace_bytes", "moe_block_chunked", "moe_block_op_times", "moe_block_dw_schedule",
            "moe_dw_schedule", "moe_pipeline_plan", "moe_pipeline_range_cost", "moe_product_timing",
            "moe_product_times", "moe_route", "moe_route_bwd", "moe_dispatch_bpr_route", "moe_bwd_dx_route", "moe_w4_quantize",
-           "moe_experts_w4_workspace_bytes", "moe_experts_w4", "moe_ckpt_bytes", "moe_ckpt_save", "moe_ckpt_load"]
+           "moe_experts_w4_workspace_bytes", "moe_experts_w4", "moe_ckpt_bytes", "moe_ckpt_save", "moe_ckpt_load",
+           "moe_sorted_rows", "moe_sorted_workspace_bytes", "moe_sorted_dispatch", "moe_sorted_ffn_fwd", "moe_sorted_combine",
+           "moe_sorted_combine_bwd", "moe_sorted_bwd_dx", "moe_sorted_dispatch_bwd", "moe_sorted_bwd_dw", "moe_embed",
+           "moe_embed_bwd_workspace_bytes", "moe_embed_bwd"]
 #: The expert products moe_product_times reports, in its order.
 PRODUCTS = ["fwd1", "fwd2", "dA", "dXe", "dW2", "dW1"]
 MOE_BLOCK_FWD, MOE_BLOCK_BWD, MOE_BLOCK_TIMED = 1, 2, 4
@@ -72,6 +75,16 @@ class moe_w4_cfg(ctypes.Structure):
                 ("k", ctypes.c_int32), ("dtype", ctypes.c_int32), ("act", ctypes.c_int32)]
 
 
+class moe_sorted_cfg(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64), ("d_model", ctypes.c_int32), ("d_ff", ctypes.c_int32), ("E", ctypes.c_int32),
+                ("k", ctypes.c_int32), ("dtype", ctypes.c_int32), ("act", ctypes.c_int32), ("wpacked", ctypes.c_int32)]
+
+
+class moe_embed_cfg(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64), ("V", ctypes.c_int32), ("d_model", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("accum", ctypes.c_int32)]
+
+
 BLOCK_WEIGHTS = ["ln1_g", "ln1_b", "Wqkv", "Wo", "ln2_g", "ln2_b", "Wg", "W1", "W2"]
 BLOCK_GRADS = ["dln1_g", "dln1_b", "dWqkv", "dWo", "dln2_g", "dln2_b", "dWg", "dW1", "dW2"]
 BLOCK_ACTS_FWD = ["a", "ln1_mean", "ln1_rstd", "qkv", "attn", "lse", "h", "ln2_mean", "ln2_rstd", "m", "logits",
@@ -96,7 +109,7 @@ def _load():
         raise ImportError(f"{LIB_PATH} is not built; run `python -m paper_2404_19429_amd.build`")
     lib = ctypes.CDLL(LIB_PATH)
     P, I32, I64, SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
-    CFG = ctypes.POINTER(moe_cfg)
+    CFG, SORTED, EMBED = (ctypes.POINTER(t) for t in (moe_cfg, moe_sorted_cfg, moe_embed_cfg))
     sig = {
         "moe_capacity": (I32, [I64, I32, I32, I32, I32]),
         "moe_workspace_bytes": (SZ, [CFG, I32]),
@@ -127,6 +140,18 @@ def _load():
         "moe_ckpt_bytes": (SZ, [CFG]),
         "moe_ckpt_save": (I32, [CFG] + [P] * 6 + [SZ, P]),
         "moe_ckpt_load": (I32, [CFG, P, SZ] + [P] * 7),
+        "moe_sorted_rows": (I64, [SORTED]),
+        "moe_sorted_workspace_bytes": (SZ, [SORTED, I32]),
+        "moe_sorted_dispatch": (I32, [SORTED] + [P] * 8 + [SZ, P]),
+        "moe_sorted_ffn_fwd": (I32, [SORTED] + [P] * 9 + [SZ, P]),
+        "moe_sorted_combine": (I32, [SORTED] + [P] * 5),
+        "moe_sorted_combine_bwd": (I32, [SORTED] + [P] * 8),
+        "moe_sorted_bwd_dx": (I32, [SORTED] + [P] * 9 + [SZ, P]),
+        "moe_sorted_dispatch_bwd": (I32, [SORTED] + [P] * 6),
+        "moe_sorted_bwd_dw": (I32, [SORTED] + [P] * 12 + [SZ, P]),
+        "moe_embed": (I32, [EMBED] + [P] * 4),
+        "moe_embed_bwd_workspace_bytes": (SZ, [EMBED]),
+        "moe_embed_bwd": (I32, [EMBED] + [P] * 4 + [SZ, P]),
         "moe_block_workspace_bytes": (SZ, [ctypes.POINTER(moe_block_cfg), I32]),
         "moe_block_chunked": (I32, [ctypes.POINTER(moe_block_cfg), ctypes.POINTER(moe_block_weights),
                                     ctypes.POINTER(moe_block_grads), P, P, P, P, ctypes.POINTER(moe_block_acts),
@@ -147,7 +172,7 @@ def _load_bind():
     except ImportError as e:
         raise ImportError("the native binding is not built; run `python -m paper_2404_19429_amd.build`") from e
     _bind.init({n: ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in EXPORTS}, lambda s: _stream(s),
-               moe_cfg, moe_block_cfg, moe_route_cfg, moe_w4_cfg)
+               moe_cfg, moe_block_cfg, moe_route_cfg, moe_w4_cfg, moe_sorted_cfg, moe_embed_cfg)
     return _bind
 
 
@@ -360,6 +385,71 @@ def moe_ckpt_load(cfg, ckpt, row_begin, row_end, send_buf, H, A, expert_out, str
     _check(_bind.ckpt_load(cfg, ckpt, row_begin, row_end, send_buf, H, A, expert_out, stream))
 
 
+# ------------------------------------------------ rows sorted by expert, no capacity
+def _dtype(dtype) -> int:
+    return {"bf16": MOE_BF16, "f32": MOE_F32}[dtype] if isinstance(dtype, str) else int(dtype)
+
+
+def make_sorted_cfg(T, d_model, d_ff, E, k, dtype="bf16", act="gelu_tanh", wpacked=0) -> moe_sorted_cfg:
+    return moe_sorted_cfg(int(T), int(d_model), int(d_ff), int(E), int(k), _dtype(dtype),
+                          ACTS[act] if isinstance(act, str) else int(act), int(wpacked))
+
+
+def moe_sorted_rows(cfg: moe_sorted_cfg) -> int:
+    return int(_lib.moe_sorted_rows(ctypes.byref(cfg)))
+
+
+def moe_sorted_workspace_bytes(cfg: moe_sorted_cfg, call: int) -> int:
+    return int(_lib.moe_sorted_workspace_bytes(ctypes.byref(cfg), call))
+
+
+def moe_sorted_dispatch(cfg, x, idx, row_begin, row_end, slot, src, rows, ws, stream=None):
+    _check(_bind.sorted_dispatch(cfg, x, idx, row_begin, row_end, slot, src, rows, ws, stream))
+
+
+def moe_sorted_ffn_fwd(cfg, rows, row_begin, row_end, W1p, W2p, H, A, expert_out, ws=None, stream=None):
+    _check(_bind.sorted_ffn_fwd(cfg, rows, row_begin, row_end, W1p, W2p, H, A, expert_out, ws, stream))
+
+
+def moe_sorted_combine(cfg, expert_out, slot, w, y, stream=None):
+    _check(_bind.sorted_combine(cfg, expert_out, slot, w, y, stream))
+
+
+def moe_sorted_combine_bwd(cfg, expert_out, slot, src, w, dy, dO, dw, stream=None):
+    _check(_bind.sorted_combine_bwd(cfg, expert_out, slot, src, w, dy, dO, dw, stream))
+
+
+def moe_sorted_bwd_dx(cfg, row_begin, row_end, H, W1p, W2p, dO, dH, dXe, ws=None, stream=None):
+    _check(_bind.sorted_bwd_dx(cfg, row_begin, row_end, H, W1p, W2p, dO, dH, dXe, ws, stream))
+
+
+def moe_sorted_dispatch_bwd(cfg, slot, dXe, dx, Wg=None, dlogits=None, stream=None):
+    _check(_bind.sorted_dispatch_bwd(cfg, slot, dXe, Wg, dlogits, dx, stream))
+
+
+def moe_sorted_bwd_dw(cfg, row_begin, row_end, rows, A, dO, dH, dW1, dW2, ws=None, x=None, dlogits=None, dWg=None,
+                      stream=None):
+    """x, dlogits and dWg together: the gate's weight gradient too (ws is for that)."""
+    _check(_bind.sorted_bwd_dw(cfg, row_begin, row_end, rows, A, dO, dH, dW1, dW2, x, dlogits, dWg, ws, stream))
+
+
+# ------------------------------------------------------------------ token lookup
+def make_embed_cfg(T, V, d_model, dtype="bf16", scale=1.0, accum=0) -> moe_embed_cfg:
+    return moe_embed_cfg(int(T), int(V), int(d_model), _dtype(dtype), float(scale), int(accum))
+
+
+def moe_embed(cfg, ids, W, y, stream=None):
+    _check(_bind.embed(cfg, ids, W, y, stream))
+
+
+def moe_embed_bwd_workspace_bytes(cfg: moe_embed_cfg) -> int:
+    return int(_lib.moe_embed_bwd_workspace_bytes(ctypes.byref(cfg)))
+
+
+def moe_embed_bwd(cfg, ids, dy, dW, ws, stream=None):
+    _check(_bind.embed_bwd(cfg, ids, dy, dW, ws, stream))
+
+
 # ------------------------------------------------------------- layer step driver
 @dataclass
 class LayerBuffers:
@@ -477,6 +567,89 @@ def layer_backward(b: LayerBuffers, x, Wg, dy, stream=None, dw_stream=None, rout
         dw_stream.wait_event(ev)
     moe_bwd_dw(c, x, b.dlogits, b.carry, b.fill, b.send_buf, b.A, b.dO, b.dH, b.dW1, b.dW2, b.dWg, b.ws_dw,
                dw_stream if dw_stream is not None else stream)
+
+
+# ------------------------------------------------- layer step without a capacity
+@dataclass
+class SortedBuffers:
+    """Device tensors of one MoE layer step over sorted rows (allocated once, reused every step)."""
+    cfg: moe_sorted_cfg
+    gate: moe_cfg             # the gate's sizes (its C plays no part)
+    logits: torch.Tensor
+    idx: torch.Tensor
+    w: torch.Tensor
+    row_begin: torch.Tensor
+    row_end: torch.Tensor
+    slot: torch.Tensor
+    src: torch.Tensor
+    rows: torch.Tensor
+    H: torch.Tensor
+    A: torch.Tensor
+    O: torch.Tensor
+    y: torch.Tensor
+    dO: torch.Tensor
+    dH: torch.Tensor
+    dXe: torch.Tensor
+    dw: torch.Tensor
+    dlogits: torch.Tensor
+    dx: torch.Tensor
+    dW1: torch.Tensor
+    dW2: torch.Tensor
+    dWg: torch.Tensor
+    W1p: torch.Tensor
+    W2p: torch.Tensor
+    ws: torch.Tensor          # of the calls on the layer's stream
+    ws_dw: torch.Tensor       # of the weight gradients
+
+
+def alloc_sorted(cfg: moe_sorted_cfg, renorm=1, device="cuda") -> SortedBuffers:
+    """E <= 64 and k <= 8, as the gate takes them."""
+    T, d, f, E, k, R = cfg.T, cfg.d_model, cfg.d_ff, cfg.E, cfg.k, moe_sorted_rows(cfg)
+    if R < 0:
+        raise MoeError(MOE_ESHAPE, moe_last_error())
+    gate = make_cfg(T, d, f, E, k, 1, 1, cfg.dtype, cfg.act, renorm, cfg.wpacked)
+    dt, f32, i32 = torch_dtype(gate), torch.float32, torch.int32
+    e = lambda *s, dtype=dt: torch.empty(*s, dtype=dtype, device=device)
+    ws = lambda *calls: e(max(16, *(moe_sorted_workspace_bytes(cfg, c) for c in calls)), dtype=torch.uint8)
+    return SortedBuffers(
+        cfg=cfg, gate=gate, logits=e(T, E, dtype=f32), idx=e(T, k, dtype=i32), w=e(T, k, dtype=f32),
+        row_begin=e(E, dtype=i32), row_end=e(E, dtype=i32), slot=e(T, k, dtype=i32), src=e(R, dtype=i32),
+        rows=e(R, d), H=e(R, f), A=e(R, f), O=e(R, d), y=e(T, d), dO=e(R, d), dH=e(R, f), dXe=e(R, d),
+        dw=e(T, k, dtype=f32), dlogits=e(T, E, dtype=f32), dx=e(T, d), dW1=e(E, f, d), dW2=e(E, d, f),
+        dWg=e(E, d, dtype=f32), W1p=e(E, f, d), W2p=e(E, d, f),
+        ws=ws(MOE_CALL_DISPATCH, MOE_CALL_FFN_FWD, MOE_CALL_BWD_DX), ws_dw=ws(MOE_CALL_BWD_DW))
+
+
+def sorted_layer_forward(b: SortedBuffers, x, Wg, bias, W1, W2, stream=None, router: Optional[Router] = None):
+    """layer_forward without a capacity: weight packing -> gate [-> router] -> rows by expert -> experts -> combine.
+    No token is dropped, and no buffer is padded to the busiest expert."""
+    c = b.cfg
+    if router is not None and (router.cfg.T, router.cfg.E, router.cfg.k) != (c.T, c.E, c.k):
+        raise ValueError("the router's T, E and k are not the layer's")
+    moe_pack_weights(b.gate, W1, W2, b.W1p, b.W2p, stream)
+    moe_gate_topk(b.gate, x, Wg, bias, b.logits, b.idx, b.w, stream)
+    if router is not None:
+        moe_route(router.cfg, b.logits, router.bias, b.idx, b.w, router.load, stream)
+    moe_sorted_dispatch(c, x, b.idx, b.row_begin, b.row_end, b.slot, b.src, b.rows, b.ws, stream)
+    moe_sorted_ffn_fwd(c, b.rows, b.row_begin, b.row_end, b.W1p, b.W2p, b.H, b.A, b.O, b.ws, stream)
+    moe_sorted_combine(c, b.O, b.slot, b.w, b.y, stream)
+
+
+def sorted_layer_backward(b: SortedBuffers, x, Wg, dy, stream=None, dw_stream=None, router: Optional[Router] = None):
+    """The dX chain on `stream` (with the weights packed by sorted_layer_forward); the weight gradients on
+    `dw_stream` (default: the same), ordered after it by an event."""
+    c = b.cfg
+    route = router.cfg if router is not None else make_route_cfg(c.T, c.E, c.k, "softmax", b.gate.renorm)
+    moe_sorted_combine_bwd(c, b.O, b.slot, b.src, b.w, dy, b.dO, b.dw, stream)
+    moe_route_bwd(route, b.logits, b.idx, b.w, b.dw, b.dlogits, stream)
+    moe_sorted_bwd_dx(c, b.row_begin, b.row_end, b.H, b.W1p, b.W2p, b.dO, b.dH, b.dXe, b.ws, stream)
+    moe_sorted_dispatch_bwd(c, b.slot, b.dXe, b.dx, Wg, b.dlogits, stream)
+    if dw_stream is not None:
+        ev = torch.cuda.Event()
+        ev.record(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.current_stream())
+        dw_stream.wait_event(ev)
+    moe_sorted_bwd_dw(c, b.row_begin, b.row_end, b.rows, b.A, b.dO, b.dH, b.dW1, b.dW2, b.ws_dw, x, b.dlogits, b.dWg,
+                      dw_stream if dw_stream is not None else stream)
 
 
 # ------------------------------------------------------------------------ block
