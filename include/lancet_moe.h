@@ -541,6 +541,39 @@ size_t moe_embed_bwd_workspace_bytes(const moe_embed_cfg* cfg);
 moe_status moe_embed_bwd(const moe_embed_cfg* cfg, const int32_t* ids, const void* dy, void* dW, void* ws,
                          size_t ws_bytes, moe_stream_t stream);
 
+/* -------------------------------------------- cross entropy over a vocabulary */
+
+/* The loss of a language model from its last activations x and its output matrix W,
+ * in pieces of the vocabulary; the logits x W^T are never kept. */
+typedef struct {
+  int64_t T;       /* tokens; T * d_model < 2^29 */
+  int32_t V;       /* rows of W, 1..2^30; V * d_model <= 2^40 */
+  int32_t d_model; /* MOE_BF16: a multiple of 64; MOE_F32: of 8; up to 2^20 */
+  int32_t dtype;   /* moe_dtype of x, W, dx and dW */
+} moe_xent_cfg;
+
+/* Bytes of device workspace moe_xent (backward = 0) or moe_xent_bwd (1) needs (host
+ * only; 0 if none, 0 and a message on an invalid cfg).  Calls that overlap in time
+ * need separate workspaces. */
+size_t moe_xent_workspace_bytes(const moe_xent_cfg* cfg, int32_t backward);
+
+/* x [T][d], W [V][d] dtype, target [T] int32 -> lse [T] float = log sum over v of
+ * exp(<x_t, W_v>) of every token, loss [T] float = lse[t] - <x_t, W_target>, 0 where the
+ * target is outside 0..V-1 (padding, tokens that do not count).  Products and sums in
+ * float, logits not rounded in between. */
+moe_status moe_xent(const moe_xent_cfg* cfg, const void* x, const void* W, const int32_t* target, float* loss,
+                    float* lse, void* ws, size_t ws_bytes, moe_stream_t stream);
+
+/* dloss [T] float = dL/dloss[t] (a mean's 1 / n, say) and lse of moe_xent ->
+ *   dx [T][d] dtype = sum over v of dl[t][v] W_v, dW [V][d] dtype = sum over t of
+ *   dl[t][v] x_t, dl[t][v] = dloss[t] (exp(<x_t, W_v> - lse[t]) - [v = target[t]]); the
+ *   rows of tokens whose target is outside 0..V-1 are 0 in dx and take no part in dW,
+ *   whatever their x, lse and dloss hold.  dx or dW may be NULL (not wanted).  dl is
+ *   rounded to dtype, sums are float.  The same call gives the same bits. */
+moe_status moe_xent_bwd(const moe_xent_cfg* cfg, const void* x, const void* W, const int32_t* target,
+                        const float* lse, const float* dloss, void* dx, void* dW, void* ws, size_t ws_bytes,
+                        moe_stream_t stream);
+
 /* ------------------------------------------------------------------ block */
 
 /* The pre-LN transformer block whose FFN is the MoE layer, with its

@@ -15,6 +15,7 @@ import numpy as np
 import torch
 
 U32, UBF = 2.0 ** -24, 2.0 ** -8
+TINY = 2.0 ** -126   # float's smallest normal number: what is smaller may count as 0
 
 
 def half_step(dtype):
@@ -165,6 +166,48 @@ def embed_bwd(ids, dy, V, scale, old=None):
         dW, size = dW + old.double(), size + old.double().abs()
     t = half_step(dy.dtype) * dW.abs() + (n.unsqueeze(1) + 3) * U32 * size
     return dW, torch.where(n.unsqueeze(1) > 0, t, 0.0)   # (an id that does not occur: exactly 0, or what was there)
+
+
+def xent(x, W, target, dloss=None):
+    """{name: (value, bound)} of loss and lse and, with dloss, of dx and dW.
+
+    Bounds: a logit is a float sum of d products.  The sum of V exponentials is positive
+    terms added in at most 16 + V / 64 steps (sixteen of a lane, the runs' sums in turn),
+    each with a rounding or, where the largest logit so far grew, three (the exponential
+    of the difference, 2 of them, and its product).  An exponential of a difference D is
+    off by 2 |D| + 3 roundings.  A probability, a dl or a product below float's normal
+    numbers may be 0: off by as much as TINY each.
+    """
+    u, (T, d), V = half_step(x.dtype), x.shape, W.shape[0]
+    ok = (target >= 0) & (target < V)
+    at = torch.where(ok, target, 0).long().unsqueeze(1)
+    x, W = x.double(), W.double()
+    l = x @ W.t()
+    tl = (d + 2) * U32 * (x.abs() @ W.abs().t())
+    m = l.amax(1, keepdim=True)
+    e = torch.exp(l - m)
+    s = e.sum(1, keepdim=True)
+    lse = m + torch.log(s)
+    te = (e * (tl + (2 * (l - m).abs() + 3) * U32)).sum(1, keepdim=True) / s     # of the sum's terms, relative
+    tz = te + 3 * (16 + V / 64) * U32 + 4 * U32 * (1 + lse.abs())
+    lt = l.gather(1, at)
+    out = {"lse": (lse.squeeze(1), tz.squeeze(1)),
+           "loss": (torch.where(ok, (lse - lt).squeeze(1), 0.0),
+                    torch.where(ok, (tz + tl.gather(1, at) + U32 * (lse - lt).abs()).squeeze(1), 0.0))}
+    if dloss is None:
+        return out
+    g = torch.where(ok, dloss.double(), 0.0).unsqueeze(1)
+    p = torch.exp(l - lse)
+    one = torch.zeros_like(p).scatter_(1, at, 1.0)
+    dl = g * (p - one)
+    t = g.abs() * (p * (tl + tz + (2 * (l - lse).abs() + 4) * U32) + 2 * U32 * (p - one).abs())
+    t = t + u * (dl.abs() + t) + (1 + g.abs()) * TINY
+    xz = torch.where(ok.unsqueeze(1), x, 0.0)
+    for name, a, b, n in (("dx", (dl, t), W, V), ("dW", (dl.t(), t.t()), xz, T)):
+        v = a[0] @ b
+        tv = a[1] @ b.abs() + (n + 2) * U32 * ((a[0].abs() + a[1]) @ b.abs()) + n * TINY
+        out[name] = (v, tv + u * (v.abs() + tv))
+    return out
 
 
 def off(got, want):

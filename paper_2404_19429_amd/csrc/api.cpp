@@ -19,6 +19,7 @@ static_assert(sizeof(moe_block_cfg) == 96 && offsetof(moe_block_cfg, moe) == 16 
 static_assert(sizeof(moe_route_cfg) == 40 && offsetof(moe_route_cfg, scale) == 32, "moe_route_cfg layout");
 static_assert(sizeof(moe_w4_cfg) == 32 && offsetof(moe_w4_cfg, act) == 28, "moe_w4_cfg layout");
 static_assert(sizeof(moe_sorted_cfg) == 40 && offsetof(moe_sorted_cfg, wpacked) == 32, "moe_sorted_cfg layout");
+static_assert(sizeof(moe_xent_cfg) == 24 && offsetof(moe_xent_cfg, dtype) == 16, "moe_xent_cfg layout");
 static_assert(sizeof(moe_embed_cfg) == 32 && offsetof(moe_embed_cfg, accum) == 24, "moe_embed_cfg layout");
 
 namespace {
@@ -825,6 +826,58 @@ moe_status moe_embed_bwd(const moe_embed_cfg* cfg, const int32_t* ids, const voi
   REQUIRE_WS(lmoe::embed_bwd_ws_bytes(*cfg));
   CHECK(check_device(fn));
   lmoe::launch_embed_bwd(*cfg, ids, dy, dW, ws, (hipStream_t)stream);
+  return check_launch(fn);
+}
+
+// -------------------------------------------- cross entropy over a vocabulary
+namespace {
+
+moe_status check_xent(const moe_xent_cfg* c, const char* fn) {
+  if (!c) return fail(MOE_EINVAL, "%s: cfg is NULL", fn);
+  if (c->dtype != MOE_F32 && c->dtype != MOE_BF16) return fail(MOE_EDTYPE, "%s: unknown dtype %d", fn, c->dtype);
+  if (c->T < 0) return fail(MOE_EINVAL, "%s: T < 0", fn);
+  if (c->V < 1 || c->V > 1 << 30) return fail(MOE_ESHAPE, "%s: V=%d outside 1..2^30", fn, c->V);
+  const int32_t most = 1 << 20, unit = c->dtype == MOE_BF16 ? 64 : 8;
+  if (c->d_model < unit || c->d_model % unit != 0 || c->d_model > most)
+    return fail(MOE_ESHAPE, "%s: d_model=%d not a multiple of %d in %d..%d", fn, c->d_model, unit, unit, most);
+  // The products address x, dx and its float sums with 32-bit byte offsets.
+  if (c->T > (int64_t)1 << 29 || (c->T + 15) * c->d_model >= (int64_t)1 << 29)
+    return fail(MOE_ESHAPE, "%s: T * d_model must stay under 2^29", fn);
+  if ((int64_t)c->V * c->d_model > (int64_t)1 << 40) return fail(MOE_ESHAPE, "%s: V * d_model above 2^40", fn);
+  return MOE_OK;
+}
+
+}  // namespace
+
+size_t moe_xent_workspace_bytes(const moe_xent_cfg* cfg, int32_t backward) {
+  if (check_xent(cfg, "moe_xent_workspace_bytes") != MOE_OK) return 0;
+  return lmoe::xent_ws_bytes(*cfg, backward != 0);
+}
+
+moe_status moe_xent(const moe_xent_cfg* cfg, const void* x, const void* W, const int32_t* target, float* loss,
+                    float* lse, void* ws, size_t ws_bytes, moe_stream_t stream) {
+  const char* fn = "moe_xent";
+  CHECK(check_xent(cfg, fn));
+  REQUIRE_TPTR(x); REQUIRE_PTR(W); REQUIRE_TPTR(target); REQUIRE_TPTR(loss); REQUIRE_TPTR(lse);
+  REFUSE_ALIAS({loss, lse, ws}, {x, W, target});
+  REQUIRE_WS(lmoe::xent_ws_bytes(*cfg, false));
+  CHECK(check_device(fn));
+  lmoe::launch_xent(*cfg, x, W, target, loss, lse, ws, (hipStream_t)stream);
+  return check_launch(fn);
+}
+
+moe_status moe_xent_bwd(const moe_xent_cfg* cfg, const void* x, const void* W, const int32_t* target,
+                        const float* lse, const float* dloss, void* dx, void* dW, void* ws, size_t ws_bytes,
+                        moe_stream_t stream) {
+  const char* fn = "moe_xent_bwd";
+  CHECK(check_xent(cfg, fn));
+  REQUIRE_TPTR(x); REQUIRE_PTR(W); REQUIRE_TPTR(target); REQUIRE_TPTR(lse); REQUIRE_TPTR(dloss);
+  OPTIONAL_PTR(dx); OPTIONAL_PTR(dW);
+  if (cfg->T > 0 && dx == nullptr && dW == nullptr) return fail(MOE_EINVAL, "%s: neither dx nor dW is wanted", fn);
+  REFUSE_ALIAS({dx, dW, ws}, {x, W, target, lse, dloss});
+  REQUIRE_WS(lmoe::xent_ws_bytes(*cfg, true));
+  CHECK(check_device(fn));
+  lmoe::launch_xent_bwd(*cfg, x, W, target, lse, dloss, dx, dW, ws, (hipStream_t)stream);
   return check_launch(fn);
 }
 

@@ -47,6 +47,9 @@ struct Abi {   // addresses in the loaded library, given by init()
   decltype(&moe_embed) embed;
   decltype(&moe_embed_bwd_workspace_bytes) embed_bwd_workspace_bytes;
   decltype(&moe_embed_bwd) embed_bwd;
+  decltype(&moe_xent_workspace_bytes) xent_workspace_bytes;
+  decltype(&moe_xent) xent;
+  decltype(&moe_xent_bwd) xent_bwd;
 } g_abi;
 PyObject* g_stream;      // the module's function from a stream argument to a raw stream
 PyObject* g_cfg_type;    // the ctypes structures
@@ -55,6 +58,7 @@ PyObject* g_route_type;
 PyObject* g_w4_type;
 PyObject* g_sorted_type;
 PyObject* g_embed_type;
+PyObject* g_xent_type;
 
 struct Error {};   // a Python exception is set
 
@@ -125,6 +129,7 @@ template <> PyObject* struct_type<moe_route_cfg>() { return g_route_type; }
 template <> PyObject* struct_type<moe_w4_cfg>() { return g_w4_type; }
 template <> PyObject* struct_type<moe_sorted_cfg>() { return g_sorted_type; }
 template <> PyObject* struct_type<moe_embed_cfg>() { return g_embed_type; }
+template <> PyObject* struct_type<moe_xent_cfg>() { return g_xent_type; }
 
 // A ctypes structure's bytes.
 template <typename T>
@@ -816,10 +821,48 @@ ENTRY(embed_bwd) {   // cfg, ids, dy, dW, ws, stream
   });
 }
 
+ENTRY(xent) {   // cfg, x, W, target, loss, lse, ws, stream
+  return entry(n, 8, [&] {
+    Struct<moe_xent_cfg> c(a[0]);
+    const auto dt = c->dtype == MOE_BF16 ? kBf16 : kF32;
+    const Num T = c->T, V = c->V, d = c->d_model;
+    const size_t need = g_abi.xent_workspace_bytes(c, 0);
+    const void* x = ptr(a[1], "x", dt, T * d);
+    const void* W = ptr(a[2], "W", dt, V * d);
+    const int32_t* target = (const int32_t*)ptr(a[3], "target", kI32, T);
+    float* loss = (float*)ptr(a[4], "loss", kF32, T);
+    float* lse = (float*)ptr(a[5], "lse", kF32, T);
+    void* ws = ptr(a[6], "ws", at::kByte, need, need == 0);
+    const size_t wsn = numel_or_0(a[6]);
+    void* s = stream_arg(a[7]);
+    return status([&] { return g_abi.xent(c, x, W, target, loss, lse, ws, wsn, s); });
+  });
+}
+
+ENTRY(xent_bwd) {   // cfg, x, W, target, lse, dloss, dx, dW, ws, stream
+  return entry(n, 10, [&] {
+    Struct<moe_xent_cfg> c(a[0]);
+    const auto dt = c->dtype == MOE_BF16 ? kBf16 : kF32;
+    const Num T = c->T, V = c->V, d = c->d_model;
+    const size_t need = g_abi.xent_workspace_bytes(c, 1);
+    const void* x = ptr(a[1], "x", dt, T * d);
+    const void* W = ptr(a[2], "W", dt, V * d);
+    const int32_t* target = (const int32_t*)ptr(a[3], "target", kI32, T);
+    const float* lse = (const float*)ptr(a[4], "lse", kF32, T);
+    const float* dloss = (const float*)ptr(a[5], "dloss", kF32, T);
+    void* dx = ptr(a[6], "dx", dt, T * d, true);
+    void* dW = ptr(a[7], "dW", dt, V * d, true);
+    void* ws = ptr(a[8], "ws", at::kByte, need, need == 0);
+    const size_t wsn = numel_or_0(a[8]);
+    void* s = stream_arg(a[9]);
+    return status([&] { return g_abi.xent_bwd(c, x, W, target, lse, dloss, dx, dW, ws, wsn, s); });
+  });
+}
+
 // init({C ABI name: address}, stream function, moe_cfg type, moe_block_cfg type[, moe_route_cfg type, moe_w4_cfg type
-// [, moe_sorted_cfg type, moe_embed_cfg type]])
+// [, moe_sorted_cfg type, moe_embed_cfg type, moe_xent_cfg type]])
 ENTRY(init) {
-  if (n != 4 && n != 6 && n != 8) return PyErr_Format(PyExc_TypeError, "init takes 4, 6 or 8 arguments");
+  if (n != 4 && n != 6 && n != 9) return PyErr_Format(PyExc_TypeError, "init takes 4, 6 or 9 arguments");
   PyObject* d = a[0];
   auto set = [&](auto& fn, const char* name) {
     Item it(d, name);
@@ -866,11 +909,14 @@ ENTRY(init) {
       set(g_abi.embed, "moe_embed");
       set(g_abi.embed_bwd_workspace_bytes, "moe_embed_bwd_workspace_bytes");
       set(g_abi.embed_bwd, "moe_embed_bwd");
+      set(g_abi.xent_workspace_bytes, "moe_xent_workspace_bytes");
+      set(g_abi.xent, "moe_xent");
+      set(g_abi.xent_bwd, "moe_xent_bwd");
     }
   } catch (const Error&) {
     return nullptr;
   }
-  PyObject** slots[] = {&g_stream, &g_cfg_type, &g_block_type, &g_route_type, &g_w4_type, &g_sorted_type, &g_embed_type};
+  PyObject** slots[] = {&g_stream, &g_cfg_type, &g_block_type, &g_route_type, &g_w4_type, &g_sorted_type, &g_embed_type, &g_xent_type};
   for (int i = 0; i < n - 1; ++i) {
     Py_INCREF(a[i + 1]);
     Py_XSETREF(*slots[i], a[i + 1]);
@@ -907,6 +953,8 @@ PyMethodDef kMethods[] = {METHOD(init),
                           METHOD(sorted_bwd_dw),
                           METHOD(embed),
                           METHOD(embed_bwd),
+                          METHOD(xent),
+                          METHOD(xent_bwd),
                           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_bind", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 

@@ -109,6 +109,9 @@ __device__ __forceinline__ void f32_store(const GemmParams& p, int64_t off, cons
 #pragma unroll
     for (int u = 0; u < 4; ++u) o[u] = v[u] * act_bwd(h[u], p.act);
   }
+  if constexpr (EPI == EPI_ADD) {
+    if (p.Aux) o += *reinterpret_cast<const f32x4*>((const float*)p.Aux + off);   // (Aux may be C)
+  }
   *reinterpret_cast<f32x4*>((float*)p.C + off) = o;
   if constexpr (EPI == EPI_FWD1) {
 #pragma unroll
@@ -151,6 +154,8 @@ __global__ __launch_bounds__(256) void gemm_f32_kernel(GemmParams p, int tm, int
     span = __builtin_amdgcn_readlane(P.span, g);
   }
   const int Mlim = RAGGED_K ? p.M : span, Klim = RAGGED_K ? span : p.K;
+  // The cross entropy: the gradient at the logits has padding columns (zeros) that W has no rows for.
+  const int Alim = RAGGED_K ? (Mlim + 3) & ~3 : Mlim, Blim = EPI == EPI_DL ? p.x.cols : p.N, KlimB = EPI == EPI_ADD ? p.M : Klim;
   if (m0 >= Mlim) return;
   const float* Ab = (const float*)p.A + g * p.sA + (int64_t)lo * p.lda;
   const float* Bb = (const float*)p.B + g * p.sB + (RAGGED_K ? (int64_t)lo * p.ldb : 0);
@@ -163,16 +168,16 @@ __global__ __launch_bounds__(256) void gemm_f32_kernel(GemmParams p, int tm, int
   f32x4 va[TA::NLD], vb[TB::NLD];
   TA ta;
   TB tb;
-  ta.plan(Ab, p.lda, m0, Mlim);
-  tb.plan(Bb, p.ldb, n0, p.N);
+  ta.plan(Ab, p.lda, m0, Alim);
+  tb.plan(Bb, p.ldb, n0, Blim);
   if (Klim > 0) {
     ta.load(va, p.lda, 0, Klim);
-    tb.load(vb, p.ldb, 0, Klim);
+    tb.load(vb, p.ldb, 0, KlimB);
   }
   int buf = 0;
   for (int k0 = 0; k0 < Klim; k0 += BK, buf ^= 1) {
     TA::store(va, As[buf], k0, Klim);
-    TB::store(vb, Bs[buf], k0, Klim);
+    TB::store(vb, Bs[buf], k0, KlimB);
     __syncthreads();   // this stage is in LDS; every wave is past the stage before (the other buffer)
     // The next stage's loads, in flight under this stage's MFMAs (past the last
     // stage: one that is not stored).  The opaque start keeps the compiler from
@@ -180,7 +185,7 @@ __global__ __launch_bounds__(256) void gemm_f32_kernel(GemmParams p, int tm, int
     int kn = k0 + BK;
     asm volatile("" : "+s"(kn));
     ta.load(va, p.lda, kn, Klim);
-    tb.load(vb, p.ldb, kn, Klim);
+    tb.load(vb, p.ldb, kn, KlimB);
     __builtin_amdgcn_sched_barrier(0);
     constexpr int KB = BK / 16;
     f32x4 fa[KB][WT], fb[KB][WT];
@@ -201,6 +206,21 @@ __global__ __launch_bounds__(256) void gemm_f32_kernel(GemmParams p, int tm, int
 #pragma unroll
           for (int j = 0; j < WT; ++j)
             acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fb[kb][j][s], fa[kb][i][s], acc[i][j], 0, 0, 0);
+  }
+  if constexpr (EPI == EPI_LSE) {
+    xent_lse_rows<WT, WT>(p.x, acc, m0 + wm, n0 + wn, Mlim, p.x.block0 + n0 / BM * 2 + (wid & 1), lane);
+    return;
+  }
+  if constexpr (EPI == EPI_DL) {
+#pragma unroll
+    for (int i = 0; i < WT; ++i) {
+      const XentRow r = xent_row(p.x, m0 + wm + 16 * i + (lane & 15), Mlim);
+#pragma unroll
+      for (int j = 0; j < WT; ++j)
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          acc[i][j][u] = xent_dl(p.x, r, acc[i][j][u], n0 + wn + 16 * j + 4 * (lane >> 4) + u);
+    }
   }
   const int64_t cbase = (int64_t)g * p.sC + (RAGGED_K ? 0 : (int64_t)lo * p.ldc);
 #pragma unroll
@@ -255,12 +275,14 @@ struct TileCost {
   int bm, bn, per_cu;   // per_cu: blocks of this shape on a CU, so a round is per_cu tiles per CU
   double full, part, store;
   void (*run)(const WideCall&, hipStream_t);
+  int wtn;              // columns of a wave's tile
 };
-static const TileCost kTilesM[] = {{256, 256, 1, 650., 650., 8000., run_wide_256x256},
-                                   {192, 256, 1, 560., 560., 7000., run_wide_192x256},
-                                   {128, 128, 2, 520., 330., 4500., run_wide_128x128},
-                                   {64, 128, 2, 390., 230., 3000., run_wide_64x128},
-                                   {64, 64, 2, 300., 190., 2000., run_wide_64x64}};
+static const TileCost kTilesM[] = {{256, 256, 1, 650., 650., 8000., run_wide_256x256, 64},
+                                   {192, 256, 1, 560., 560., 7000., run_wide_192x256, 64},
+                                   {128, 128, 2, 520., 330., 4500., run_wide_128x128, 64},
+                                   {64, 128, 2, 390., 230., 3000., run_wide_64x128, 64},
+                                   {64, 64, 2, 300., 190., 2000., run_wide_64x64, 32}};
+constexpr int kTileCount = sizeof kTilesM / sizeof kTilesM[0];
 static double tile_cost(const TileCost& t, const WideCall& w, int cus) {
   // M-tiles of a group: a mean over the routed rows' spread.
   const double tm = 0.25 * std::ceil(std::max(1., w.expect - w.spread) / t.bm) + 0.5 * std::ceil(w.expect / t.bm) +
@@ -268,7 +290,7 @@ static double tile_cost(const TileCost& t, const WideCall& w, int cus) {
   const double tiles = std::ceil(w.groups * tm * std::ceil((double)w.cols / t.bn));
   const double slots = (double)t.per_cu * cus;
   const double rounds = std::floor(tiles / slots), rem = tiles - rounds * slots;
-  const double steps = w.p.K / 32., store = w.kind == WK_FWD1 || w.kind == WK_DACT ? t.store : t.store / 2;
+  const double steps = w.p.K / 32., store = w.kind == WK_NK || w.kind == WK_NK_RES || w.kind == WK_KN || w.kind == WK_KN_RM ? t.store / 2 : t.store;
   double last = rem <= 0 ? 0. : steps * (rem <= cus ? t.part : t.full) + store;
   // A K-split last round: its share of a round, and the partial tiles' write and sum.
   if (t.bm == 256 && w.p.ksplit && (w.kind == WK_NK || w.kind == WK_KN) && rounds > 0 && rem > 0 && 4 * rem <= slots)
@@ -276,9 +298,9 @@ static double tile_cost(const TileCost& t, const WideCall& w, int cus) {
   return rounds * (steps * t.full + store) + last;
 }
 // The tile of a ragged-M product (index into kTilesM).
-static int tile_m(const WideCall& w, int cus) {
+static int tile_m(const WideCall& w, int cus, int tiles = kTileCount) {
   int best = 0;
-  for (int i = 1; i < (int)(sizeof kTilesM / sizeof kTilesM[0]); ++i)
+  for (int i = 1; i < tiles; ++i)
     if (tile_cost(kTilesM[i], w, cus) < tile_cost(kTilesM[best], w, cus)) best = i;
   return best;
 }
@@ -642,6 +664,94 @@ void launch_sorted_bwd_dw(const moe_sorted_cfg& c, const int32_t* rb, const int3
     p.eB = R * d;
     run_sorted<false, true, EPI_STORE>(c, q, kProdDW1, kind, p, f, (int)d, nullptr, s);
   });
+}
+
+// --------------------------------------------------------------- cross entropy
+// Logits over a piece of the vocabulary (see XentParams), and the products of the
+// gradient at them.  bf16: the wide kernel, W (and in the forward x) as the caller has
+// it, row-major, x in the backward and dl blocked; float: the float kernel, row-major.
+static GemmParams xent_params(int64_t T, int N, int K, const void* A, int64_t lda, int64_t eA, const void* B, int64_t ldb,
+                              int64_t eB, void* C, int64_t ldc) {
+  GemmParams p{A, lda, eA, B, ldb, eB, C, ldc, 0, nullptr, nullptr, nullptr, nullptr, 0, N, K, 0, (int)T};
+  return p;
+}
+static WideCall xent_call(WideKind kind, int64_t T, int cols, const GemmParams& p) {
+  return WideCall{kind, MOE_ACT_IDENTITY, 1, T, cols, (double)T, 0., p};
+}
+// Many tokens: no tile whose waves have narrow runs of columns (the partial sums are one for each).
+constexpr int64_t kXentNarrow = 1024;
+int xent_run_columns(int dtype, int64_t T) { return dtype == MOE_BF16 ? (T <= kXentNarrow ? 32 : 64) : (T <= kXentNarrow ? 16 : 32); }
+
+int launch_xent_lse(int dtype, int64_t T, int d, const void* x, const void* W, const XentParams& xp, hipStream_t s) {
+  GemmParams p = xent_params(T, xp.cols, d, x, d, T * d, W, d, (int64_t)xp.cols * d, nullptr, 0);
+  p.x = xp;
+  WideCall w = xent_call(WK_LSE, T, xp.cols, p);
+  if (dtype == MOE_BF16) {
+    w.p.eA = p.sA;
+    w.p.eB = p.sB;
+    const TileCost& t = kTilesM[tile_m(w, num_cus(), T <= kXentNarrow ? kTileCount : kTileCount - 1)];
+    t.run(w, s);
+    return (xp.cols + t.bn - 1) / t.bn * (t.bn / t.wtn);
+  }
+  if (T <= kXentNarrow && f32_tile(w, num_cus()) == 32) {
+    launch_f32<1, true, false, EPI_LSE>(p, 1, T, xp.cols, s);
+    return (xp.cols + 31) / 32 * 2;
+  }
+  launch_f32<2, true, false, EPI_LSE>(p, 1, T, xp.cols, s);
+  return (xp.cols + 63) / 64 * 2;
+}
+
+// dl [T][ld] (bf16: blocked, pad16(T) rows), ld >= xp.cols a multiple of 64 (float: 8); x: bf16 blocked.
+void launch_xent_dl(int dtype, int64_t T, int d, const void* x, const void* W, const XentParams& xp, void* dl, int ld,
+                    hipStream_t s) {
+  GemmParams p = xent_params(T, ld, d, x, d, pad16(T) * d, W, d, (int64_t)xp.cols * d, dl, ld);
+  p.x = xp;
+  const WideCall w = xent_call(WK_DL, T, ld, p);
+  if (dtype == MOE_BF16) return run_wide_any(w, s);
+  if (f32_tile(w, num_cus()) == 32) launch_f32<1, true, false, EPI_DL>(p, 1, T, ld, s);
+  else launch_f32<2, true, false, EPI_DL>(p, 1, T, ld, s);
+}
+
+// dx over one piece: acc_in (NULL = 0) + dl W -> acc_out (float), or rounded to dx (bf16).
+void launch_xent_dx(int dtype, int64_t T, int d, int cols, const void* dl, int ld, const void* W, const float* acc_in,
+                    float* acc_out, void* dx, hipStream_t s) {
+  GemmParams p = xent_params(T, d, ld, dl, ld, pad16(T) * ld, W, d, (int64_t)cols * d, acc_out, d);
+  p.Aux = acc_in;
+  p.C2 = dx;
+  p.M = cols;
+  const WideCall w = xent_call(WK_ADD, T, d, p);
+  if (dtype == MOE_BF16) return run_wide_any(w, s);
+  if (f32_tile(w, num_cus()) == 32) launch_f32<1, false, false, EPI_ADD>(p, 1, T, d, s);
+  else launch_f32<2, false, false, EPI_ADD>(p, 1, T, d, s);
+}
+
+// dx where the vocabulary is one piece (bf16): no float sums to keep, and where the
+// result has few tiles, their long sums over the vocabulary are split over the CUs
+// (part: sorted_ffn_ws_bytes-sized).
+size_t xent_part_bytes() { return (size_t)kSkPartElems * sizeof(float); }
+void launch_xent_dx_whole(int64_t T, int d, int cols, const void* dl, int ld, const void* W, void* dx, void* part,
+                          hipStream_t s) {
+  GemmParams p = xent_params(T, d, ld, dl, ld, pad16(T) * ld, W, d, (int64_t)cols * d, dx, d);
+  p.part = (float*)part;
+  const int64_t large = (T + 255) / 256 * ((d + 255) / 256);
+  WideCall w = xent_call(WK_KN_RM, T, d, p);
+  if (4 * large <= num_cus()) {
+    w.p.ksplit = 2;
+    w.p.eA = p.sA;
+    w.p.eB = p.sB;
+    return run_wide_256x256(w, s);
+  }
+  run_wide_any(w, s);
+}
+
+// dW [cols][d] = dl^T x; x as dl (bf16: blocked).
+void launch_xent_dw(int dtype, int64_t T, int d, int cols, const void* dl, int ld, const void* x, void* dW, hipStream_t s) {
+  GemmParams p{dl, ld, pad16(T) * ld, x, d, pad16(T) * d, dW, d, 0, nullptr, nullptr, nullptr, nullptr, cols, d, 0, 0, (int)T};
+  WideCall q = xent_call(WK_DW, cols, d, p);
+  q.expect = (double)T;
+  if (dtype == MOE_BF16) return run_wide_any(q, s);
+  if (f32_tile(q, num_cus()) == 32) launch_f32<1, false, true, EPI_STORE>(p, 1, cols, d, s);
+  else launch_f32<2, false, true, EPI_STORE>(p, 1, cols, d, s);
 }
 
 // Sum of the S float partials of a K-split weight gradient, in group order,

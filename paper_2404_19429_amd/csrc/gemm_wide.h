@@ -14,7 +14,26 @@ namespace lmoe {
 // operands row-major [K][*] (not blocked), K split into groups of kchunk rows
 // (group g: rows [g kchunk, (g + 1) kchunk)), each group's float partial C at
 // C + g sC; gemm_wgrad_reduce_kernel adds the partials in group order.
-enum { EPI_STORE = 0, EPI_FWD1 = 1, EPI_DACT = 2, EPI_RES = 3, EPI_WGF32 = 4 };
+// EPI_LSE, EPI_DL: logits that are not kept (see XentParams).  EPI_ADD: a float sum
+// over calls -- the product plus Aux (float, NULL = 0) goes to C (float) or, with
+// C2, rounded to C2.
+enum { EPI_STORE = 0, EPI_FWD1 = 1, EPI_DACT = 2, EPI_RES = 3, EPI_WGF32 = 4, EPI_LSE = 5, EPI_DL = 6, EPI_ADD = 7 };
+
+// The cross entropy's products x W^T over a piece of the vocabulary, columns
+// col0 .. col0 + cols - 1 of it.  EPI_LSE: of each row, and of each wave's run of
+// columns, the largest logit and the sum of exp(logit - largest), at
+// part[block * stride + row]; and the target's logit.  EPI_DL: the gradient at
+// the logits, g (exp(logit - lse) - [column = target]), 0 in the padding columns
+// and in the rows whose target is outside 0 .. V - 1.
+struct XentParams {
+  const int32_t* target;
+  float2* part;
+  float* tl;           // the target's logit (rows whose target is in the piece)
+  const float* lse;
+  const float* g;
+  int64_t stride;
+  int V, col0, cols, block0;
+};
 
 struct GemmParams {
   const void* A;
@@ -31,11 +50,13 @@ struct GemmParams {
   int act;
   int cap;          // rows per expert block (C): row ranges are clamped to [0, cap]; re == NULL means [0, cap)
   float* part;      // wide ragged-M products: partial tiles of the K-split (stream-K) schedule
-  int ksplit;       // wide plain-store ragged-M products: 1 = a short last round may be K-split
+  int ksplit;       // wide plain-store ragged-M products: 1 = a short last round may be K-split; 2: so may the only
+                    // one, on every CU (few tiles, a long K)
   int kchunk;       // rb == re == NULL and kchunk > 0: group g's rows are [g kchunk, (g + 1) kchunk)
   int only;         // ragged-K: 1 = run only if the groups are even, 2 = only if they are skewed, 0 = always
   int64_t eA, eB;   // elements that a group's operand spans from its start (run_wide_any: sA, sB where 0; groups
                     // that share one buffer have a stride of 0 and its extent)
+  XentParams x;
 };
 
 // Row range of group g, clamped to the buffer so bad ranges cannot reach outside it.
@@ -46,6 +67,67 @@ __device__ __forceinline__ void group_rows(const GemmParams& p, int g, int& lo, 
   b = b < a ? a : (b > p.cap ? p.cap : b);
   lo = a;
   span = b - a;
+}
+
+constexpr float kLog2e = 1.44269504088896f;
+// One wave's fragments of logits: acc[i][j] holds row row0 + 16 i + lane % 16, columns col0 + 16 j + 4 (lane / 16) .. + 3.
+// A row's columns lie in the four lanes that share lane % 16, which meet by two exchanges.  Rows: up to `rows`.
+template <int FM, int FN>
+__device__ __forceinline__ void xent_lse_rows(const XentParams& x, const f32x4 (&acc)[FM][FN], int row0, int col0, int rows,
+                                              int block, int lane) {
+  const int rl = lane & 15, c0 = col0 + 4 * (lane >> 4);
+#pragma unroll
+  for (int i = 0; i < FM; ++i) {
+    const int row = row0 + 16 * i + rl;
+    const bool live = row < rows;
+    const int id = live ? x.target[row] : -1;
+    const int t = id >= 0 && id < x.V ? id - x.col0 : -1;   // (of another piece: meets no column here)
+    float m = -INFINITY, tv = 0.f;
+    bool hit = false;
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int c = c0 + 16 * j + u;
+        const float v = c < x.cols ? acc[i][j][u] : -INFINITY;
+        m = fmaxf(m, v);
+        const bool is = c == t && c < x.cols;
+        tv = is ? v : tv;
+        hit |= is;
+      }
+    m = fmaxf(m, __shfl_xor(m, 16, kWave));
+    m = fmaxf(m, __shfl_xor(m, 32, kWave));
+    const float b = m > -INFINITY ? m : 0.f;   // (a run of -inf: a sum of 0)
+    float s = 0.f;
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int c = c0 + 16 * j + u;
+        const float v = c < x.cols ? acc[i][j][u] : -INFINITY;
+        s += __builtin_amdgcn_exp2f((v - b) * kLog2e);
+      }
+    s += __shfl_xor(s, 16, kWave);
+    s += __shfl_xor(s, 32, kWave);
+    if (live && lane < 16) x.part[(int64_t)block * x.stride + row] = make_float2(m, s);
+    if (live && hit) x.tl[row] = tv;
+  }
+}
+// What a row's gradient needs, and the gradient at one logit of it.
+struct XentRow {
+  float lse, g;
+  int t;      // the target's column in the piece
+  bool live;
+};
+__device__ __forceinline__ XentRow xent_row(const XentParams& x, int row, int rows) {
+  const int r = min(row, rows - 1);
+  const int t = x.target[r];
+  const bool live = t >= 0 && t < x.V;
+  return XentRow{x.lse[r], x.g[r], live ? t - x.col0 : -1, live};
+}
+__device__ __forceinline__ float xent_dl(const XentParams& x, const XentRow& r, float v, int c) {
+  const float p = __builtin_amdgcn_exp2f((v - r.lse) * kLog2e) - (c == r.t ? 1.f : 0.f);
+  return r.live && c < x.cols ? r.g * p : 0.f;
 }
 
 // ----------------------------------------------------------------- bf16 MFMA
@@ -224,9 +306,10 @@ __device__ __forceinline__ void acc_pin_mem(f32x4 (&a)[N]) {
 // columns past `lim` and, with KCHK, K rows outside [klo, khi) read zeros.
 constexpr int kBufCfg = 0x00020000;   // buffer descriptor word 3: raw 32-bit data, gfx9 family
 constexpr uint32_t kOob = 0x80000000u;
-// RM (MN-contiguous only): the operand is row-major [K][ld] instead of blocked;
-// a lane loads the same 16-byte chunk (K row, 8 columns) that it would take
-// from the blocked layout, so the stage's LDS layout is the same.
+// RM: the operand is row-major ([K][ld]; K-contiguous: [ROWS][ld]) instead of
+// blocked; a lane loads the same 16-byte chunk (row, 8 columns) that it would take
+// from the blocked layout, so the stage's LDS layout is the same.  A row-major
+// MN-contiguous operand may end before K does (a descriptor past its end is empty).
 template <bool KC, bool KCHK, int NW, int ROWS, bool RM = false>
 struct WOp {
   static constexpr int kWNI = ROWS / 16 / NW;   // loads per wave per stage (1 KB blocks)
@@ -246,11 +329,12 @@ struct WOp {
     klo = lo;
     khi = hi;
     if constexpr (KC) {
-      stride = 1024;
+      stride = RM ? 64 : 1024;
 #pragma unroll
       for (int i = 0; i < kWNI; ++i) {
         const int rb = (row0 >> 4) + i * NW + wid;
-        const uint32_t off = (uint32_t)(rb * (int)(ld >> 5) * 512 + (lane & 15) * 32 + (lane >> 4) * 8) * 2u;
+        const uint32_t off = RM ? (uint32_t)((int64_t)(16 * rb + (lane & 15)) * ld + (lane >> 4) * 8) * 2u
+                                : (uint32_t)(rb * (int)(ld >> 5) * 512 + (lane & 15) * 32 + (lane >> 4) * 8) * 2u;
         voff[i] = (16 * rb + (lane & 15) < lim) ? off : (off | kOob);
         kr[i] = 0;
       }
@@ -272,10 +356,12 @@ struct WOp {
       }
     }
   }
+  // Bytes of the operand from `adv` on.
+  __device__ __forceinline__ int left(uint32_t adv) const { return RM && !KC && adv > bytes ? 0 : (int)(bytes - adv); }
   // Load i (0 .. kWNI-1) of K-step kk into its place in the stage.
   __device__ __forceinline__ void issue(int i, int kk, uint16_t* stage, int wid) const {
     const uint32_t adv = (uint32_t)kk * stride;
-    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)(base + adv), (short)0, (int)(bytes - adv), kBufCfg);
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)(base + adv), (short)0, left(adv), kBufCfg);
     uint32_t vo = voff[i];
     if constexpr (KCHK) {
       const int k = kr[i] + 32 * kk;
@@ -288,7 +374,7 @@ struct WOp {
   // the stage (a stage no later step reads).
   __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(int kk, bool live) const {
     const uint32_t adv = (uint32_t)kk * stride;
-    return __builtin_amdgcn_make_buffer_rsrc((void*)(base + adv), (short)0, live ? (int)(bytes - adv) : 0, kBufCfg);
+    return __builtin_amdgcn_make_buffer_rsrc((void*)(base + adv), (short)0, live ? left(adv) : 0, kBufCfg);
   }
   __device__ __forceinline__ void issue_r(int i, __amdgpu_buffer_rsrc_t r, int kk, uint16_t* stage, int wid) const {
     uint32_t vo = voff[i];
@@ -463,16 +549,22 @@ __device__ __forceinline__ WRange wide_range(const WPrefix& P, int xcd) {
 // EPI-specific store (plain, (H, act(H)), or dA * act'(H) with H read back).
 // acc[i][j] holds output row 16 i + l % 16, columns 16 j + 4 (l / 16) .. +3 of
 // the wave tile at (G.m0 + wm WTM, G.n0 + wn WTN).
-template <int FM, int FN, int WTM, int WTN, bool RAGGED_K, int EPI, int ACT, bool CBLK>
+template <int FM, int FN, int WTM, int WTN, int BN, bool RAGGED_K, int EPI, int ACT, bool CBLK>
 __device__ __forceinline__ void wide_epilogue(const GemmParams& p, const WGeo& G, f32x4 (&acc)[FM][FN], int wm,
                                               int wn, int lane, int i_lo = 0, int i_hi = FM) {
+  if constexpr (EPI == EPI_LSE) {
+    constexpr int WGN = BN / WTN;
+    xent_lse_rows<FM, FN>(p.x, acc, G.m0 + wm * WTM, G.n0 + wn * WTN, G.Mlim, p.x.block0 + G.n0 / BN * WGN + wn, lane);
+    return;
+  }
   // Buffer stores and loads over the group's output: a lane outside the
   // product carries an out-of-range offset (store dropped, load zero), so
   // the epilogue is branch-free and dA * act'(H) issues all of a half's H
   // loads together.  Group offsets fit 31 bits (validated on the host).
   const int64_t cofs = (int64_t)G.g * p.sC + (RAGGED_K || CBLK ? 0 : (int64_t)G.lo_al * p.ldc);
-  constexpr int ESZ = EPI == EPI_WGF32 ? 4 : 2;   // bytes per output element
-  void* const cbase = EPI == EPI_WGF32 ? (void*)((float*)p.C + cofs) : (void*)((uint16_t*)p.C + cofs);
+  constexpr bool F32 = EPI == EPI_WGF32 || EPI == EPI_ADD;
+  constexpr int ESZ = F32 ? 4 : 2;   // bytes per output element
+  void* const cbase = F32 ? (void*)((float*)p.C + cofs) : (void*)((uint16_t*)p.C + cofs);
   const __amdgpu_buffer_rsrc_t rC = __builtin_amdgcn_make_buffer_rsrc(cbase, (short)0, 0x7fffffff, kBufCfg);
   __amdgpu_buffer_rsrc_t rC2 = rC, rAux = rC;
   if constexpr (EPI == EPI_FWD1)
@@ -499,6 +591,40 @@ __device__ __forceinline__ void wide_epilogue(const GemmParams& p, const WGeo& G
                                                (int)voff(row_ok(i) && col < p.N, row_of(i), col), 0, 0);
       }
     return;
+  }
+  if constexpr (EPI == EPI_ADD) {
+    if (p.Aux) {
+      const __amdgpu_buffer_rsrc_t rA = __builtin_amdgcn_make_buffer_rsrc((float*)p.Aux + cofs, (short)0, 0x7fffffff, kBufCfg);
+      constexpr int HA = 2;   // fragment rows whose loads are in flight together
+#pragma unroll
+      for (int i0 = 0; i0 < FM; i0 += HA) {
+        u32x4 a[HA][FN];
+#pragma unroll
+        for (int i = 0; i < HA; ++i)
+#pragma unroll
+          for (int j = 0; j < FN; ++j) {
+            const int col = G.n0 + wn * WTN + 16 * j + 4 * q;
+            a[i][j] = __builtin_amdgcn_raw_buffer_load_b128(
+                rA, (int)voff(row_ok(i0 + i) && col < p.N, row_of(i0 + i), col), 0, 0);
+          }
+#pragma unroll
+        for (int i = 0; i < HA; ++i)
+#pragma unroll
+          for (int j = 0; j < FN; ++j) acc[i0 + i][j] += __builtin_bit_cast(f32x4, a[i][j]);
+      }
+    }
+    if (p.C2 == nullptr) {
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+          const int col = G.n0 + wn * WTN + 16 * j + 4 * q;
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[i][j]), rC,
+                                                 (int)voff(row_ok(i) && col < p.N, row_of(i), col), 0, 0);
+        }
+      return;
+    }
+    rC2 = __builtin_amdgcn_make_buffer_rsrc((uint16_t*)p.C2 + cofs, (short)0, 0x7fffffff, kBufCfg);
   }
   // bf16 outputs move as 16 bytes per lane: of a pair of fragments (32 columns)
   // a lane holds columns 4 q .. +3 of each 16; swapping the odd 16-lane groups of
@@ -533,6 +659,11 @@ __device__ __forceinline__ void wide_epilogue(const GemmParams& p, const WGeo& G
               rAux, (int)voff(row_ok(HR * h + ii) && col < p.N, row_of(HR * h + ii), col), 0, 0);
         }
     }
+    XentRow xr[HR];
+    if constexpr (EPI == EPI_DL) {
+#pragma unroll
+      for (int ii = 0; ii < HR; ++ii) xr[ii] = xent_row(p.x, row_of(HR * h + ii), G.Mlim);
+    }
 #pragma unroll
     for (int ii = 0; ii < HR; ++ii) {
       const int i = HR * h + ii;
@@ -566,13 +697,22 @@ __device__ __forceinline__ void wide_epilogue(const GemmParams& p, const WGeo& G
             for (int u = 0; u < 4; ++u) v[e][u] = EPI == EPI_DACT ? v[e][u] * act_bwd_t<ACT>(f[u]) : v[e][u] + f[u];
           }
         }
-        store(pack4_bf16(v[0]), pack4_bf16(v[1]), rC, vo);
+        if constexpr (EPI == EPI_DL) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+              v[e][u] = xent_dl(p.x, xr[ii], v[e][u], G.n0 + wn * WTN + 16 * (2 * jp + e) + 4 * q + u);
+        }
+        if constexpr (EPI == EPI_ADD) store(pack4_bf16(v[0]), pack4_bf16(v[1]), rC2, vo < 0 ? vo : vo / 2);
+        else store(pack4_bf16(v[0]), pack4_bf16(v[1]), rC, vo);
       }
     }
   }
 }
 
-template <class TC, bool B_K, bool RAGGED_K, int EPI, int ACT, bool CBLK>
+// ARM, BRM: a ragged-M product's A (K-contiguous), B operand is row-major.
+template <class TC, bool B_K, bool RAGGED_K, int EPI, int ACT, bool CBLK, bool ARM = false, bool BRM = false>
 __global__ __attribute__((amdgpu_flat_work_group_size(TC::NW * 64, TC::NW * 64), amdgpu_waves_per_eu(TC::WPE, TC::WPE))) void
 gemm_wide_kernel(GemmParams p, int tilesM, int tilesN, int groups) {
   constexpr int BK = TC::BK, SUB = TC::SUB, HALF = TC::HALF;
@@ -693,8 +833,9 @@ gemm_wide_kernel(GemmParams p, int tilesM, int tilesN, int groups) {
   // a K range of them), so the extent is the whole operand.
   constexpr bool RMO = EPI == EPI_WGF32;
   static_assert(!RMO || RAGGED_K, "row-major operands: ragged-K products only");
-  WOp<AK, RAGGED_K, NW, BM, RMO> opA;
-  WOp<BKK, RAGGED_K, NW, BN, RMO> opB;
+  static_assert(!RAGGED_K || (!ARM && !BRM), "row-major operands of ragged-K products: EPI_WGF32");
+  WOp<AK, RAGGED_K, NW, BM, RMO || ARM> opA;
+  WOp<BKK, RAGGED_K, NW, BN, RMO || BRM> opB;
   int le = 0, lt = 0, lk = 0, lkend = 0, ls = 0;
   auto plan = [&](int t) __attribute__((always_inline)) {
     const WGeo G = geo(t);
@@ -702,7 +843,7 @@ gemm_wide_kernel(GemmParams p, int tilesM, int tilesN, int groups) {
     const uint16_t* Bb = (const uint16_t*)p.B + (RMO ? 0 : G.g * p.sB);
     const int64_t extA = RMO ? (int64_t)p.cap * p.lda : p.eA, extB = RMO ? (int64_t)p.cap * p.ldb : p.eB;
     // (rows of the stage past the tile's BMT are not loaded: their places get zeros, which no wave reads)
-    const int rlim = min((int)pad16(p.cap), G.lo_al + G.m0 + BMT);
+    const int rlim = min(ARM ? p.cap : (int)pad16(p.cap), G.lo_al + G.m0 + BMT);
     if constexpr (AK) opA.plan(Ab, extA, p.lda, G.lo_al + G.m0, rlim, 0, 0, 0, wid, lane);
     else opA.plan(Ab, extA, p.lda, G.m0, p.M, G.lo_al, G.lo, G.hi, wid, lane);
     if constexpr (BKK) opB.plan(Bb, extB, p.ldb, G.n0, p.N, 0, 0, 0, wid, lane);
@@ -753,7 +894,7 @@ gemm_wide_kernel(GemmParams p, int tilesM, int tilesN, int groups) {
     asm volatile("s_nop 15\n s_nop 15" ::: "memory");
 #pragma unroll
     for (int i = 0; i < FM; ++i) acc_pin(acc[i]);
-    wide_epilogue<FM, FN, WTM, WTN, RAGGED_K, EPI, ACT, CBLK>(p, G, acc, wm, wn, lane);
+    wide_epilogue<FM, FN, WTM, WTN, BN, RAGGED_K, EPI, ACT, CBLK>(p, G, acc, wm, wn, lane);
   };
 
   int cs = 0;                // compute steps done (over all of the block's tiles)
@@ -1083,7 +1224,7 @@ __global__ __launch_bounds__(TC::NW * 64) void gemm_wide_fixup_kernel(GemmParams
     if (I == i) {
 #pragma unroll
       for (int j = 0; j < FN; ++j) acc[I][j] = sum[j];
-      wide_epilogue<FM, FN, WTM, WTN, false, EPI, ACT, CBLK>(p, G, acc, wm, wn, lane, I, I + 1);
+      wide_epilogue<FM, FN, WTM, WTN, BN, false, EPI, ACT, CBLK>(p, G, acc, wm, wn, lane, I, I + 1);
     }
   });
 }
@@ -1097,6 +1238,10 @@ enum WideKind {
   WK_NK_RES,    // the same with a residual added
   WK_DACT,      // B [K][N], dA * act'(H) epilogue, blocked output
   WK_KN,        // B [K][N], plain store, row-major output
+  WK_LSE,       // x W^T of the cross entropy, x and W row-major: EPI_LSE
+  WK_DL,        // the same with x blocked: EPI_DL, blocked output
+  WK_KN_RM,     // WK_KN with a row-major B
+  WK_ADD,       // the same added over calls: EPI_ADD
   WK_DW,        // (this kind and the later ones) ragged-K, row-major output
   WK_DW_BLK,    // ragged-K, blocked output
   WK_WGF32      // ragged-K over row-major operands, float partials
@@ -1115,18 +1260,18 @@ struct WideCall {
 
 constexpr int64_t kSkPartElems = (int64_t)256 * 256 * 256;   // floats of the K-split's partial tiles (one per block)
 
-template <class TC, bool B_K, bool RAGGED_K, int EPI, int ACT, bool CBLK>
+template <class TC, bool B_K, bool RAGGED_K, int EPI, int ACT, bool CBLK, bool ARM = false, bool BRM = false>
 static void launch_wide(const WideCall& w, hipStream_t s) {
   constexpr size_t shmem = TC::lds_bytes(B_K);
   constexpr bool SPLIT = TC::KSPLIT && !RAGGED_K && EPI == EPI_STORE;
   const GemmParams& p = w.p;
-  auto kern = gemm_wide_kernel<TC, B_K, RAGGED_K, EPI, ACT, CBLK>;
+  auto kern = gemm_wide_kernel<TC, B_K, RAGGED_K, EPI, ACT, CBLK, ARM, BRM>;
   static std::atomic<uint64_t> lds_ok{0};
   allow_dyn_lds((const void*)kern, (int)shmem, lds_ok);
   const int tm = (int)((w.rows + (RAGGED_K ? 0 : 15) + TC::BMT - 1) / TC::BMT), tn = (w.cols + TC::BN - 1) / TC::BN;
   int64_t blocks = (int64_t)num_cus() * TC::per_cu(B_K);
   if (SPLIT) blocks = std::min<int64_t>(blocks, kSkPartElems / (TC::BMT * TC::BN));   // partial tiles in the workspace
-  blocks = std::min(blocks, (int64_t)tm * tn * w.groups);
+  if (!(SPLIT && p.ksplit == 2)) blocks = std::min(blocks, (int64_t)tm * tn * w.groups);
   blocks = (blocks + 7) / 8 * 8;
   hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(TC::NW * 64), shmem, s, p, tm, tn, w.groups);
   if constexpr (SPLIT) {
@@ -1157,6 +1302,10 @@ static void run_wide_m(const WideCall& w, hipStream_t s) {
     case WK_NK_RES: return launch_wide<TC, true, false, EPI_RES, ID, false>(w, s);
     case WK_DACT: return launch_wide_act<TC, false, EPI_DACT>(w, s);
     case WK_KN: return launch_wide<TC, false, false, EPI_STORE, ID, false>(w, s);
+    case WK_LSE: return launch_wide<TC, true, false, EPI_LSE, ID, false, true, true>(w, s);
+    case WK_DL: return launch_wide<TC, true, false, EPI_DL, ID, true, false, true>(w, s);
+    case WK_KN_RM: return launch_wide<TC, false, false, EPI_STORE, ID, false, false, true>(w, s);
+    case WK_ADD: return launch_wide<TC, false, false, EPI_ADD, ID, false, false, true>(w, s);
     default: return;
   }
 }

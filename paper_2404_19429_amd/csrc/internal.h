@@ -124,6 +124,13 @@ void launch_embed(const moe_embed_cfg& c, const int32_t* ids, const void* W, voi
 size_t embed_bwd_ws_bytes(const moe_embed_cfg& c);
 void launch_embed_bwd(const moe_embed_cfg& c, const int32_t* ids, const void* dy, void* dW, void* ws, hipStream_t s);
 
+// xent.hip: cross entropy over a vocabulary (its products: gemm.hip).
+size_t xent_ws_bytes(const moe_xent_cfg& c, bool backward);
+void launch_xent(const moe_xent_cfg& c, const void* x, const void* W, const int32_t* target, float* loss, float* lse,
+                 void* ws, hipStream_t s);
+void launch_xent_bwd(const moe_xent_cfg& c, const void* x, const void* W, const int32_t* target, const float* lse,
+                     const float* dloss, void* dx, void* dW, void* ws, hipStream_t s);
+
 // ckpt.hip
 size_t ckpt_bytes(const moe_cfg& c);
 void launch_ckpt_save(const moe_cfg& c, const void* send, const void* H, const void* O, const int32_t* rb,

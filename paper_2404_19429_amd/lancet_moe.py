@@ -36,7 +36,7 @@ EXPORTS = ["moe_capacity", "moe_workspace_bytes", "moe_last_error", "moe_gate_to
            "moe_experts_w4_workspace_bytes", "moe_experts_w4", "moe_ckpt_bytes", "moe_ckpt_save", "moe_ckpt_load",
            "moe_sorted_rows", "moe_sorted_workspace_bytes", "moe_sorted_dispatch", "moe_sorted_ffn_fwd", "moe_sorted_combine",
            "moe_sorted_combine_bwd", "moe_sorted_bwd_dx", "moe_sorted_dispatch_bwd", "moe_sorted_bwd_dw", "moe_embed",
-           "moe_embed_bwd_workspace_bytes", "moe_embed_bwd"]
+           "moe_embed_bwd_workspace_bytes", "moe_embed_bwd", "moe_xent_workspace_bytes", "moe_xent", "moe_xent_bwd"]
 #: The expert products moe_product_times reports, in its order.
 PRODUCTS = ["fwd1", "fwd2", "dA", "dXe", "dW2", "dW1"]
 MOE_BLOCK_FWD, MOE_BLOCK_BWD, MOE_BLOCK_TIMED = 1, 2, 4
@@ -85,6 +85,10 @@ class moe_embed_cfg(ctypes.Structure):
                 ("scale", ctypes.c_float), ("accum", ctypes.c_int32)]
 
 
+class moe_xent_cfg(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64), ("V", ctypes.c_int32), ("d_model", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
 BLOCK_WEIGHTS = ["ln1_g", "ln1_b", "Wqkv", "Wo", "ln2_g", "ln2_b", "Wg", "W1", "W2"]
 BLOCK_GRADS = ["dln1_g", "dln1_b", "dWqkv", "dWo", "dln2_g", "dln2_b", "dWg", "dW1", "dW2"]
 BLOCK_ACTS_FWD = ["a", "ln1_mean", "ln1_rstd", "qkv", "attn", "lse", "h", "ln2_mean", "ln2_rstd", "m", "logits",
@@ -109,7 +113,7 @@ def _load():
         raise ImportError(f"{LIB_PATH} is not built; run `python -m paper_2404_19429_amd.build`")
     lib = ctypes.CDLL(LIB_PATH)
     P, I32, I64, SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
-    CFG, SORTED, EMBED = (ctypes.POINTER(t) for t in (moe_cfg, moe_sorted_cfg, moe_embed_cfg))
+    CFG, SORTED, EMBED, XENT = (ctypes.POINTER(t) for t in (moe_cfg, moe_sorted_cfg, moe_embed_cfg, moe_xent_cfg))
     sig = {
         "moe_capacity": (I32, [I64, I32, I32, I32, I32]),
         "moe_workspace_bytes": (SZ, [CFG, I32]),
@@ -152,6 +156,9 @@ def _load():
         "moe_embed": (I32, [EMBED] + [P] * 4),
         "moe_embed_bwd_workspace_bytes": (SZ, [EMBED]),
         "moe_embed_bwd": (I32, [EMBED] + [P] * 4 + [SZ, P]),
+        "moe_xent_workspace_bytes": (SZ, [XENT, I32]),
+        "moe_xent": (I32, [XENT] + [P] * 6 + [SZ, P]),
+        "moe_xent_bwd": (I32, [XENT] + [P] * 8 + [SZ, P]),
         "moe_block_workspace_bytes": (SZ, [ctypes.POINTER(moe_block_cfg), I32]),
         "moe_block_chunked": (I32, [ctypes.POINTER(moe_block_cfg), ctypes.POINTER(moe_block_weights),
                                     ctypes.POINTER(moe_block_grads), P, P, P, P, ctypes.POINTER(moe_block_acts),
@@ -172,7 +179,7 @@ def _load_bind():
     except ImportError as e:
         raise ImportError("the native binding is not built; run `python -m paper_2404_19429_amd.build`") from e
     _bind.init({n: ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in EXPORTS}, lambda s: _stream(s),
-               moe_cfg, moe_block_cfg, moe_route_cfg, moe_w4_cfg, moe_sorted_cfg, moe_embed_cfg)
+               moe_cfg, moe_block_cfg, moe_route_cfg, moe_w4_cfg, moe_sorted_cfg, moe_embed_cfg, moe_xent_cfg)
     return _bind
 
 
@@ -448,6 +455,24 @@ def moe_embed_bwd_workspace_bytes(cfg: moe_embed_cfg) -> int:
 
 def moe_embed_bwd(cfg, ids, dy, dW, ws, stream=None):
     _check(_bind.embed_bwd(cfg, ids, dy, dW, ws, stream))
+
+
+# -------------------------------------------------- cross entropy over a vocabulary
+def make_xent_cfg(T, V, d_model, dtype="bf16") -> moe_xent_cfg:
+    return moe_xent_cfg(int(T), int(V), int(d_model), _dtype(dtype))
+
+
+def moe_xent_workspace_bytes(cfg: moe_xent_cfg, backward=False) -> int:
+    return int(_lib.moe_xent_workspace_bytes(ctypes.byref(cfg), 1 if backward else 0))
+
+
+def moe_xent(cfg, x, W, target, loss, lse, ws, stream=None):
+    _check(_bind.xent(cfg, x, W, target, loss, lse, ws, stream))
+
+
+def moe_xent_bwd(cfg, x, W, target, lse, dloss, dx, dW, ws, stream=None):
+    """dx or dW None: not wanted."""
+    _check(_bind.xent_bwd(cfg, x, W, target, lse, dloss, dx, dW, ws, stream))
 
 
 # ------------------------------------------------------------- layer step driver

@@ -1,0 +1,174 @@
+"""Cross entropy over a vocabulary on the GPU against its plain 64-bit form."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+L = pytest.importorskip("paper_2404_19429_amd.lancet_moe", reason="library not built")
+from oracle import training_oracle as O  # noqa: E402
+
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def _make(T, V, d, dtype, seed, padded=False, std=1.0):
+    torch.manual_seed(seed)
+    x = (torch.randn(T, d, device="cuda") * std).to(DT[dtype])
+    W = (torch.randn(V, d, device="cuda") * 0.05).to(DT[dtype])
+    target = torch.randint(0, V, (T,), device="cuda", dtype=torch.int32)
+    dloss = torch.rand(T, device="cuda") - 0.3
+    if padded:
+        target[T - T // 3:] = -1
+        target[0], target[T // 2] = V, torch.iinfo(torch.int32).min
+    return x, W, target, dloss
+
+
+def _run(x, W, target, dloss, dtype, want_dx=True, want_dW=True, fill=7.0):
+    T, V, d = x.shape[0], W.shape[0], W.shape[1]
+    cfg = L.make_xent_cfg(T, V, d, dtype)
+    ws = [torch.full((max(16, L.moe_xent_workspace_bytes(cfg, b)),), 0xff, dtype=torch.uint8, device="cuda") for b in (False, True)]
+    loss, lse = (torch.full((T,), fill, device="cuda") for _ in range(2))
+    L.moe_xent(cfg, x, W, target, loss, lse, ws[0])
+    dx = torch.full_like(x, fill) if want_dx else None
+    dW = torch.full_like(W, fill) if want_dW else None
+    L.moe_xent_bwd(cfg, x, W, target, lse, dloss, dx, dW, ws[1])
+    return {"loss": loss, "lse": lse, "dx": dx, "dW": dW}
+
+
+CASES = [(1, 1, 64), (1, 2, 128), (1, 50257, 64), (3, 63, 64), (17, 64, 320), (64, 65, 64), (65, 257, 192), (100, 20011, 128),
+         (257, 1000, 64), (1000, 5003, 128), (1025, 777, 64), (2100, 12345, 64), (4096, 512, 256), (300, 3, 1024)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,V,d", CASES)
+def test_loss_and_gradients(T, V, d, dtype):
+    if dtype == "f32":
+        d -= 8 * (V % 7)
+    x, W, target, dloss = _make(T, V, d, dtype, T + V)
+    got, want = _run(x, W, target, dloss, dtype), O.xent(x, W, target, dloss)
+    for n in ("loss", "lse", "dx", "dW"):
+        assert O.off(got[n], want[n]) <= 1, n
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,V,d", [(9, 100, 64), (300, 1003, 128), (1500, 640, 64)])
+def test_tokens_without_a_target_take_no_part(T, V, d, dtype):
+    x, W, target, dloss = _make(T, V, d, dtype, T, padded=True)
+    dead = (target < 0) | (target >= V)
+    want = O.xent(x, W, target, dloss)
+    x[dead], dloss[dead] = float("nan"), float("nan")     # whatever padding holds
+    x[torch.nonzero(dead)[0], 0] = float("inf")
+    got = _run(x, W, target, dloss, dtype)
+    for n in ("loss", "dx", "dW"):
+        assert O.off(got[n], want[n]) <= 1, n
+    assert not got["loss"][dead].any() and not got["dx"][dead].any()
+    assert O.off(got["lse"][~dead], tuple(v[~dead] for v in want["lse"])) <= 1
+    # no token at all counts
+    none = _run(x, W, torch.full_like(target, -1), dloss, dtype)
+    assert not none["loss"].any() and not none["dx"].any() and not none["dW"].any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_pieces_of_the_vocabulary(dtype):
+    """So many tokens that the gradient's pieces are smaller than the vocabulary."""
+    T, V, d = 40000, 5003, 64
+    x, W, target, dloss = _make(T, V, d, dtype, 1, padded=True)
+    got, want = _run(x, W, target, dloss, dtype), O.xent(x, W, target, dloss)
+    for n in ("loss", "lse", "dx", "dW"):
+        assert O.off(got[n], want[n]) <= 1, n
+    one = _run(x, W, target, dloss, dtype, want_dW=False)
+    assert torch.equal(one["dx"], got["dx"])
+    two = _run(x, W, target, dloss, dtype, want_dx=False)
+    assert torch.equal(two["dW"], got["dW"])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_large_logits(dtype):
+    """Logits of several hundred: the sums stay in range, a sure token has a loss near 0."""
+    x, W, target, dloss = _make(200, 3000, 128, dtype, 4, std=400.0)
+    target[::2] = (x.double() @ W.double().t()).argmax(1)[::2].int()
+    got, want = _run(x, W, target, dloss, dtype), O.xent(x, W, target, dloss)
+    for n in ("loss", "lse", "dx", "dW"):
+        assert bool(torch.isfinite(got[n].float()).all())
+        assert O.off(got[n], want[n]) <= 1, n
+
+
+def test_rows_do_not_mix():
+    """A row with NaN has a NaN loss; the others keep their bits."""
+    x, W, target, dloss = _make(300, 1000, 128, "bf16", 5)
+    clean = _run(x, W, target, dloss, "bf16")
+    x[7, 3] = float("nan")
+    got = _run(x, W, target, dloss, "bf16")
+    keep = torch.arange(300, device="cuda") != 7
+    assert bool(got["loss"][7].isnan()) and bool(got["dx"][7].isnan().all())
+    for n in ("loss", "lse", "dx"):
+        assert torch.equal(got[n][keep], clean[n][keep]), n
+
+
+def test_gradient_against_differences():
+    x, W, target, dloss = _make(20, 50, 64, "f32", 6)
+    cfg = L.make_xent_cfg(20, 50, 64, "f32")
+    ws = torch.empty(L.moe_xent_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
+    loss, lse = torch.empty(20, device="cuda"), torch.empty(20, device="cuda")
+
+    def f():
+        L.moe_xent(cfg, x, W, target, loss, lse, ws)
+        return float((loss.double() * dloss.double()).sum())
+    got = _run(x, W, target, dloss, "f32")
+    for m, key in ((x, "dx"), (W, "dW")):
+        for i in ((0, 0), (7, 33), (19, 63)):
+            was, h = float(m[i]), 0.05
+            m[i] = was + h
+            up, hi = f(), float(m[i])
+            m[i] = was - h
+            slope = (up - f()) / (hi - float(m[i]))
+            m[i] = was
+            # third derivatives of a log-sum-exp are at most |W|^3 (|x|^3): h^2 / 6 of that; float losses over 2 h
+            size = float((W if key == "dx" else x).abs().max())
+            assert abs(slope - float(got[key][i])) <= h * h / 6 * 20 * size ** 3 + 20 * 16 * O.U32 * 10 / h
+
+
+def test_no_tokens():
+    for dtype in ("bf16", "f32"):
+        cfg = L.make_xent_cfg(0, 100, 64, dtype)
+        none, f0 = torch.empty(0, dtype=torch.int32, device="cuda"), torch.empty(0, device="cuda")
+        W, dW = (torch.ones(100, 64, device="cuda").to(DT[dtype]) for _ in range(2))
+        x = torch.empty(0, 64, device="cuda", dtype=DT[dtype])
+        L.moe_xent(cfg, x, W, none, f0, f0, None)
+        L.moe_xent_bwd(cfg, x, W, none, f0, f0, x, dW, None)
+        assert not dW.any()
+
+
+def test_same_bits_graph_replays_and_streams():
+    x, W, target, dloss = _make(2100, 12345, 128, "bf16", 8)
+    want = _run(x, W, target, dloss, "bf16")
+    again = _run(x, W, target, dloss, "bf16", fill=3.0)
+    for n in want:
+        assert torch.equal(want[n], again[n]), n
+    cfg = L.make_xent_cfg(2100, 12345, 128)
+    ws = torch.empty(max(L.moe_xent_workspace_bytes(cfg, b) for b in (False, True)), dtype=torch.uint8, device="cuda")
+    out = {n: torch.empty_like(v) for n, v in want.items()}
+
+    def step(stream=None):
+        L.moe_xent(cfg, x, W, target, out["loss"], out["lse"], ws, stream)
+        L.moe_xent_bwd(cfg, x, W, target, out["lse"], dloss, out["dx"], out["dW"], ws, stream)
+    step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    keep = x.clone()
+    for _ in range(3):
+        x.copy_(torch.randn_like(x))
+        step()
+        x.copy_(keep)
+        graph.replay()
+        torch.cuda.synchronize()
+        for n in want:
+            assert torch.equal(out[n], want[n]), n
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for v in out.values():
+        v.zero_()
+    torch.cuda.synchronize()
+    step(side)
+    side.synchronize()
+    for n in want:
+        assert torch.equal(out[n], want[n]), n

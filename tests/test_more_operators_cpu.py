@@ -187,3 +187,89 @@ def test_oracle_layout_is_the_header_s():
     for r, c in ((0, 0), (5, 33), (17, 2), (31, 63)):
         assert int(flat[((r // 16) * 2 + c // 32) * 512 + (r % 16) * 32 + c % 32]) == r * 64 + c
     assert torch.equal(O.unblocked(O.blocked(m)), m)
+
+
+def _xent(**kw):
+    base = dict(T=100, V=1000, d_model=128, dtype="bf16")
+    base.update(kw)
+    return L.make_xent_cfg(**base)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(T=-1), L.MOE_EINVAL), (dict(T=1 << 30), L.MOE_ESHAPE), (dict(T=1 << 22), L.MOE_ESHAPE), (dict(V=0), L.MOE_ESHAPE),
+    (dict(V=(1 << 30) + 1), L.MOE_ESHAPE), (dict(V=1 << 30, d_model=2048), L.MOE_ESHAPE), (dict(d_model=96), L.MOE_ESHAPE),
+    (dict(d_model=12, dtype="f32"), L.MOE_ESHAPE), (dict(d_model=1 << 21), L.MOE_ESHAPE), (dict(dtype=2), L.MOE_EDTYPE)])
+def test_xent_sizes_are_refused(kw, status):
+    c, p = _xent(**kw), _ptrs(8)
+    assert L._lib.moe_xent(c, *p[:6], 1 << 40, None) == status
+    assert L._lib.moe_xent_bwd(c, *p, 1 << 40, None) == status
+    for b in (0, 1):
+        assert L.moe_xent_workspace_bytes(c, b) == 0 and L.moe_last_error()
+
+
+def test_xent_pointers_are_refused():
+    c = _xent()
+    for n, fn, optional in ((6, L._lib.moe_xent, ()), (8, L._lib.moe_xent_bwd, (5, 6))):
+        for i in range(n - 1):
+            p = _ptrs(n)
+            p[i] += 4
+            assert fn(c, *p, 1 << 40, None) == L.MOE_EALIGN, i
+            p[i] = None
+            if i not in optional:
+                assert fn(c, *p, 1 << 40, None) == L.MOE_EINVAL, i
+        for o in ((3, 4, 5) if n == 6 else (5, 6, 7)):
+            for i in range(o):
+                p = _ptrs(n)
+                p[o] = p[i]
+                assert fn(c, *p, 1 << 40, None) == L.MOE_EINVAL, (o, i)
+        assert fn(c, *_ptrs(n), 1024, None) == L.MOE_EWORKSPACE
+        assert fn(c, *_ptrs(n - 1), None, 0, None) == L.MOE_EWORKSPACE
+        assert fn(None, *_ptrs(n), 1 << 40, None) == L.MOE_EINVAL
+    p = _ptrs(8)
+    p[5] = p[6] = None
+    assert L._lib.moe_xent_bwd(c, *p, 1 << 40, None) == L.MOE_EINVAL
+    if not torch.cuda.is_available():
+        for i in (5, 6):
+            p = _ptrs(8)
+            p[i] = None
+            assert L._lib.moe_xent_bwd(c, *p, 1 << 40, None) == L.MOE_EDEVICE
+    with pytest.raises(TypeError, match="moe_xent_cfg"):
+        L.moe_xent(_embed(), *[torch.zeros(1)] * 6)
+
+
+def test_xent_workspaces_stay_small():
+    """The forward keeps an eighth of a byte for each logit at most, and the backward
+    never holds the whole vocabulary's gradient of many tokens."""
+    c = _xent(T=16384, V=50257, d_model=2048)
+    assert L.moe_xent_workspace_bytes(c, 0) <= 16384 * (50257 / 8 + 100)
+    assert L.moe_xent_workspace_bytes(c, 1) <= (256 << 20) + 16384 * 2048 * 6 + 4096
+    assert L.moe_xent_workspace_bytes(_xent(T=0), 1) == 0
+
+
+@pytest.mark.parametrize("T,V,d", [(3, 5, 4), (6, 2, 3)])
+def test_oracle_xent_against_differences(T, V, d):
+    torch.manual_seed(0)
+    x, W, dloss = (torch.randn(*s, dtype=torch.float64) for s in ((T, d), (V, d), (T,)))
+    target = torch.randint(0, V, (T,))
+    target[0] = -1
+    got = O.xent(x, W, target, dloss)
+    assert torch.allclose(got["lse"][0], torch.logsumexp(x @ W.t(), 1)) and float(got["loss"][0][0]) == 0
+    f = lambda: float((dloss * O.xent(x, W, target)["loss"][0]).sum())   # noqa: E731
+    for m, key in ((x, "dx"), (W, "dW")):
+        for i in ((0, 0), (1, 2)):
+            was, h = float(m[i]), 1e-6
+            m[i] = was + h
+            up = f()
+            m[i] = was - h
+            slope = (up - f()) / (2 * h)
+            m[i] = was
+            assert abs(slope - float(got[key][0][i])) <= 1e-6 * (1 + abs(slope))
+
+
+def test_oracle_embed_by_hand():
+    ids = torch.tensor([2, -1, 0, 2, 3], dtype=torch.int32)
+    dy = torch.arange(10.0).view(5, 2)
+    dW, _ = O.embed_bwd(ids, dy, 3, 2.0)
+    assert dW.tolist() == [[8.0, 10.0], [0.0, 0.0], [12.0, 16.0]]
+    y, _ = O.embed(ids, torch.tensor([[1.0, 2.0], [3.0, 4.0], [5.0, 6.0]]), 0.5)
+    assert y.tolist() == [[2.5, 3.0], [0.0, 0.0], [0.5, 1.0], [2.5, 3.0], [0.0, 0.0]]
