@@ -216,10 +216,11 @@ __global__ __launch_bounds__(256) void gemm_f32_kernel(GemmParams p, int tm, int
     for (int i = 0; i < WT; ++i) {
       const XentRow r = xent_row(p.x, m0 + wm + 16 * i + (lane & 15), Mlim);
 #pragma unroll
-      for (int j = 0; j < WT; ++j)
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-          acc[i][j][u] = xent_dl(p.x, r, acc[i][j][u], n0 + wn + 16 * j + 4 * (lane >> 4) + u);
+      for (int j = 0; j < WT; ++j) {
+        float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+        xent_dl4(p.x, r, v, n0 + wn + 16 * j + 4 * (lane >> 4), true, false);
+        acc[i][j] = f32x4{v[0], v[1], v[2], v[3]};
+      }
     }
   }
   const int64_t cbase = (int64_t)g * p.sC + (RAGGED_K ? 0 : (int64_t)lo * p.ldc);
@@ -365,6 +366,7 @@ static TileK tile_k(const WideCall& w, int cus) {
   const int64_t slices = ((w.rows + 127) / 128 + (w.cols + 127) / 128) * w.groups;
   const double three = small > per ? 850. : slices <= 128 ? 780. : 1000.;
   const double c128 = 7000. + cost(small, per, three, 2000., rem <= cus ? 440. : rem <= 2 * cus ? 620. : three);
+  if (w.groups == 1) return c128 <= c256 ? kTileK128 : kTileK256;   // (one group is as long as it is)
   if (c128 <= c256 + 3000.) return kTileK128;
   return 2 * large <= 3 * cus || c256 >= 1e5 ? kTileKByRows : kTileK256;
 }
@@ -682,13 +684,30 @@ static WideCall xent_call(WideKind kind, int64_t T, int cols, const GemmParams& 
 constexpr int64_t kXentNarrow = 1024;
 int xent_run_columns(int dtype, int64_t T) { return dtype == MOE_BF16 ? (T <= kXentNarrow ? 32 : 64) : (T <= kXentNarrow ? 16 : 32); }
 
-int launch_xent_lse(int dtype, int64_t T, int d, const void* x, const void* W, const XentParams& xp, hipStream_t s) {
-  GemmParams p = xent_params(T, xp.cols, d, x, d, T * d, W, d, (int64_t)xp.cols * d, nullptr, 0);
+// Columns of a product of T rows that fill whole rounds of 256-tiles (a multiple of 256; all of them if there is no
+// whole round, or nothing is left past the last).  The columns left run as a product of their own on the tiles that
+// suit them, where that takes less: a last round of a few 256-tiles takes as long as a full one.  2048 tokens, width
+// 1024, 50257 classes: 1576 tiles, six rounds and 40 tiles.
+static int whole_rounds(const WideCall& w, int cus) {
+  const int64_t tm = (w.rows + 255) / 256, tn = (w.cols + 255) / 256;
+  const int64_t main = tm * tn / cus * cus / tm * 256;
+  if (main <= 0 || main >= w.cols) return w.cols;
+  WideCall a = w, b = w;
+  a.cols = (int)main;
+  b.cols = w.cols - (int)main;
+  const double apart = tile_cost(kTilesM[tile_m(a, cus)], a, cus) + tile_cost(kTilesM[tile_m(b, cus)], b, cus) + 3000.;
+  return apart < tile_cost(kTilesM[tile_m(w, cus)], w, cus) ? (int)main : w.cols;
+}
+
+static int launch_lse_part(int dtype, int form, int64_t T, int d, const void* x, const void* W, const XentParams& xp,
+                           hipStream_t s) {
+  GemmParams p = xent_params(T, xp.cols, d, x, d, form >= kXentX ? pad16(T) * d : T * d, W, d,
+                             (form == kXentBlocked ? pad16(xp.cols) : (int64_t)xp.cols) * d, nullptr, 0);
   p.x = xp;
-  WideCall w = xent_call(WK_LSE, T, xp.cols, p);
+  WideCall w = xent_call(form == kXentBlocked ? WK_LSE_BLK : form == kXentX ? WK_LSE_X : WK_LSE, T, xp.cols, p);
   if (dtype == MOE_BF16) {
-    w.p.eA = p.sA;
-    w.p.eB = p.sB;
+    w.p.eA = w.p.sA;
+    w.p.eB = w.p.sB;
     const TileCost& t = kTilesM[tile_m(w, num_cus(), T <= kXentNarrow ? kTileCount : kTileCount - 1)];
     t.run(w, s);
     return (xp.cols + t.bn - 1) / t.bn * (t.bn / t.wtn);
@@ -700,16 +719,51 @@ int launch_xent_lse(int dtype, int64_t T, int d, const void* x, const void* W, c
   launch_f32<2, true, false, EPI_LSE>(p, 1, T, xp.cols, s);
   return (xp.cols + 63) / 64 * 2;
 }
+// Returns the runs of columns written from xp.block0 on.
+int launch_xent_lse(int dtype, int form, int64_t T, int d, const void* x, const void* W, const XentParams& xp,
+                    hipStream_t s) {
+  if (dtype != MOE_BF16) return launch_lse_part(dtype, kXentRows, T, d, x, W, xp, s);
+  GemmParams p{};
+  p.K = d;
+  const int main = whole_rounds(xent_call(WK_LSE, T, xp.cols, p), num_cus());
+  XentParams a = xp, b = xp;
+  a.cols = main;
+  int n = launch_lse_part(dtype, form, T, d, x, W, a, s);
+  if (main < xp.cols) {   // (whole 16-row blocks of W come before the rest)
+    b.col0 += main;
+    b.cols -= main;
+    b.block0 += n;
+    n += launch_lse_part(dtype, form, T, d, x, (const uint16_t*)W + (int64_t)main * d, b, s);
+  }
+  return n;
+}
 
 // dl [T][ld] (bf16: blocked, pad16(T) rows), ld >= xp.cols a multiple of 64 (float: 8); x: bf16 blocked.
-void launch_xent_dl(int dtype, int64_t T, int d, const void* x, const void* W, const XentParams& xp, void* dl, int ld,
-                    hipStream_t s) {
-  GemmParams p = xent_params(T, ld, d, x, d, pad16(T) * d, W, d, (int64_t)xp.cols * d, dl, ld);
+void launch_xent_dl(int dtype, int form, int64_t T, int d, const void* x, const void* W, const XentParams& xp, void* dl,
+                    int ld, hipStream_t s) {
+  auto extent = [&](int cols) { return (form == kXentBlocked ? pad16(cols) : (int64_t)cols) * d; };
+  GemmParams p = xent_params(T, ld, d, x, d, pad16(T) * d, W, d, extent(xp.cols), dl, ld);
   p.x = xp;
-  const WideCall w = xent_call(WK_DL, T, ld, p);
-  if (dtype == MOE_BF16) return run_wide_any(w, s);
-  if (f32_tile(w, num_cus()) == 32) launch_f32<1, true, false, EPI_DL>(p, 1, T, ld, s);
-  else launch_f32<2, true, false, EPI_DL>(p, 1, T, ld, s);
+  WideCall w = xent_call(form == kXentBlocked ? WK_DL_BLK : WK_DL, T, ld, p);
+  if (dtype != MOE_BF16) {
+    if (f32_tile(w, num_cus()) == 32) launch_f32<1, true, false, EPI_DL>(p, 1, T, ld, s);
+    else launch_f32<2, true, false, EPI_DL>(p, 1, T, ld, s);
+    return;
+  }
+  const int main = whole_rounds(w, num_cus());
+  if (main < w.cols) {   // (the columns left, in a dl that begins further right: 32 columns are a block)
+    WideCall b = w;
+    b.cols = b.p.N = ld - main;
+    b.p.x.col0 += main;
+    b.p.x.cols -= main;
+    b.p.B = (const uint16_t*)W + (int64_t)main * d;
+    b.p.sB = extent(b.p.x.cols);
+    b.p.C = (uint16_t*)dl + (int64_t)main / 32 * 512;
+    run_wide_any(b, s);
+    w.cols = w.p.N = w.p.x.cols = main;
+    w.p.sB = extent(main);
+  }
+  run_wide_any(w, s);
 }
 
 // dx over one piece: acc_in (NULL = 0) + dl W -> acc_out (float), or rounded to dx (bf16).
@@ -744,14 +798,30 @@ void launch_xent_dx_whole(int64_t T, int d, int cols, const void* dl, int ld, co
   run_wide_any(w, s);
 }
 
-// dW [cols][d] = dl^T x; x as dl (bf16: blocked).
+// dW [cols][d] = dl^T x; x as dl (bf16: blocked).  Whole rounds of 256-tiles, and what is left past them on smaller
+// ones (as whole_rounds, with the rows in the columns' place).
 void launch_xent_dw(int dtype, int64_t T, int d, int cols, const void* dl, int ld, const void* x, void* dW, hipStream_t s) {
   GemmParams p{dl, ld, pad16(T) * ld, x, d, pad16(T) * d, dW, d, 0, nullptr, nullptr, nullptr, nullptr, cols, d, 0, 0, (int)T};
-  WideCall q = xent_call(WK_DW, cols, d, p);
-  q.expect = (double)T;
-  if (dtype == MOE_BF16) return run_wide_any(q, s);
-  if (f32_tile(q, num_cus()) == 32) launch_f32<1, false, true, EPI_STORE>(p, 1, cols, d, s);
-  else launch_f32<2, false, true, EPI_STORE>(p, 1, cols, d, s);
+  WideCall w = xent_call(WK_DW, cols, d, p);
+  w.expect = (double)T;
+  if (dtype != MOE_BF16) {
+    if (f32_tile(w, num_cus()) == 32) launch_f32<1, false, true, EPI_STORE>(p, 1, cols, d, s);
+    else launch_f32<2, false, true, EPI_STORE>(p, 1, cols, d, s);
+    return;
+  }
+  const int cus = num_cus();
+  const int64_t tn = (d + 255) / 256, tm = (cols + 255) / 256, main = tm * tn / cus * cus / tn * 256;
+  // (half a round or more left: it is as well spent on 256-tiles)
+  if (main > 0 && main < cols && 2 * (tm * tn % cus) < cus) {
+    WideCall b = w;
+    b.rows = b.p.M = cols - (int)main;
+    b.p.A = (const uint16_t*)dl + main / 32 * 512;
+    b.p.eA = p.sA - main / 32 * 512;
+    b.p.C = (uint16_t*)dW + main * d;
+    run_wide_any(b, s);
+    w.rows = w.p.M = (int)main;
+  }
+  run_wide_any(w, s);
 }
 
 // Sum of the S float partials of a K-split weight gradient, in group order,

@@ -69,65 +69,91 @@ __device__ __forceinline__ void group_rows(const GemmParams& p, int g, int& lo, 
   span = b - a;
 }
 
-constexpr float kLog2e = 1.44269504088896f;
+// Which of the cross entropy's bf16 operands are copied to blocks: none, x, or x and W.
+enum { kXentRows = 0, kXentX = 1, kXentBlocked = 2 };
+constexpr float kLog2e = 1.44269504088896f, kLn2 = 0.693147180559945f;
 // One wave's fragments of logits: acc[i][j] holds row row0 + 16 i + lane % 16, columns col0 + 16 j + 4 (lane / 16) .. + 3.
 // A row's columns lie in the four lanes that share lane % 16, which meet by two exchanges.  Rows: up to `rows`.
+//
+// Exponentials are of base 2, exp(v - m) = 2^(v c - m2) with c = log2(e) and m2 = m c as it is rounded and kept: one
+// multiply-add and one exponential a logit.  The target's logit and columns past the piece are looked for only where
+// a wave has them.
 template <int FM, int FN>
-__device__ __forceinline__ void xent_lse_rows(const XentParams& x, const f32x4 (&acc)[FM][FN], int row0, int col0, int rows,
+__device__ __forceinline__ void xent_lse_rows(const XentParams& x, f32x4 (&acc)[FM][FN], int row0, int col0, int rows,
                                               int block, int lane) {
   const int rl = lane & 15, c0 = col0 + 4 * (lane >> 4);
+  int t[FM];   // the target's column from c0 (of another piece or none: negative or past the run)
 #pragma unroll
   for (int i = 0; i < FM; ++i) {
     const int row = row0 + 16 * i + rl;
-    const bool live = row < rows;
-    const int id = live ? x.target[row] : -1;
-    const int t = id >= 0 && id < x.V ? id - x.col0 : -1;   // (of another piece: meets no column here)
-    float m = -INFINITY, tv = 0.f;
-    bool hit = false;
+    const int id = row < rows ? x.target[row] : -1;
+    t[i] = id >= 0 && id < x.V ? id - x.col0 - c0 : -1;
+  }
+  const bool full = col0 + 16 * FN <= x.cols;
+#pragma unroll
+  for (int i = 0; i < FM; ++i) {
+    const int row = row0 + 16 * i + rl;
+    f32x4 v[FN];
+#pragma unroll
+    for (int j = 0; j < FN; ++j) v[j] = acc[i][j];
+    if (!full) {
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[j][u] = c0 + 16 * j + u < x.cols ? v[j][u] : -INFINITY;
+    }
+    float m = -INFINITY;
 #pragma unroll
     for (int j = 0; j < FN; ++j)
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int c = c0 + 16 * j + u;
-        const float v = c < x.cols ? acc[i][j][u] : -INFINITY;
-        m = fmaxf(m, v);
-        const bool is = c == t && c < x.cols;
-        tv = is ? v : tv;
-        hit |= is;
-      }
+      for (int u = 0; u < 4; ++u) m = fmaxf(m, v[j][u]);
     m = fmaxf(m, __shfl_xor(m, 16, kWave));
     m = fmaxf(m, __shfl_xor(m, 32, kWave));
-    const float b = m > -INFINITY ? m : 0.f;   // (a run of -inf: a sum of 0)
+    const float m2 = m * kLog2e, b = m > -INFINITY ? m2 : 0.f;   // (a run of -inf: a sum of 0)
     float s = 0.f;
 #pragma unroll
     for (int j = 0; j < FN; ++j)
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int c = c0 + 16 * j + u;
-        const float v = c < x.cols ? acc[i][j][u] : -INFINITY;
-        s += __builtin_amdgcn_exp2f((v - b) * kLog2e);
-      }
+      for (int u = 0; u < 4; ++u) s += __builtin_amdgcn_exp2f(fmaf(v[j][u], kLog2e, -b));
     s += __shfl_xor(s, 16, kWave);
     s += __shfl_xor(s, 32, kWave);
-    if (live && lane < 16) x.part[(int64_t)block * x.stride + row] = make_float2(m, s);
-    if (live && hit) x.tl[row] = tv;
+    if (row < rows && lane < 16) x.part[(int64_t)block * x.stride + row] = make_float2(m2, s);
+    const bool hit = t[i] >= 0 && t[i] < 16 * FN && (t[i] & 12) == 0;
+    if (__ballot(hit)) {
+      float tv = 0.f;
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) tv = t[i] == 16 * j + u ? v[j][u] : tv;
+      if (hit && c0 + t[i] < x.cols) x.tl[row] = tv;
+    }
   }
 }
-// What a row's gradient needs, and the gradient at one logit of it.
+// What a row's gradient needs: lse in base 2, g, and the target's column in the piece.  A row whose target is no
+// class has g = 0, and its x is zeros (the backward's copy), so its gradient is 0 * 2^0 whatever the caller's x holds.
 struct XentRow {
-  float lse, g;
-  int t;      // the target's column in the piece
-  bool live;
+  float lse2, g;
+  int t;
 };
 __device__ __forceinline__ XentRow xent_row(const XentParams& x, int row, int rows) {
   const int r = min(row, rows - 1);
   const int t = x.target[r];
   const bool live = t >= 0 && t < x.V;
-  return XentRow{x.lse[r], x.g[r], live ? t - x.col0 : -1, live};
+  return XentRow{live ? x.lse[r] * kLog2e : 0.f, live ? x.g[r] : 0.f, live ? t - x.col0 : -1};
 }
-__device__ __forceinline__ float xent_dl(const XentParams& x, const XentRow& r, float v, int c) {
-  const float p = __builtin_amdgcn_exp2f((v - r.lse) * kLog2e) - (c == r.t ? 1.f : 0.f);
-  return r.live && c < x.cols ? r.g * p : 0.f;
+// The gradient at four logits of a row, columns c .. c + 3.  any: a lane of the wave has its row's target among the
+// fragment's columns; full: no column is past the piece.
+__device__ __forceinline__ void xent_dl4(const XentParams& x, const XentRow& r, float (&v)[4], int c, bool any, bool full) {
+#pragma unroll
+  for (int u = 0; u < 4; ++u) v[u] = r.g * __builtin_amdgcn_exp2f(fmaf(v[u], kLog2e, -r.lse2));
+  if (any) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] -= r.t == c + u ? r.g : 0.f;
+  }
+  if (!full) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] = c + u < x.cols ? v[u] : 0.f;
+  }
 }
 
 // ----------------------------------------------------------------- bf16 MFMA
@@ -660,9 +686,15 @@ __device__ __forceinline__ void wide_epilogue(const GemmParams& p, const WGeo& G
         }
     }
     XentRow xr[HR];
+    bool xany[HR], xfull = true;
     if constexpr (EPI == EPI_DL) {
+      const int w0 = G.n0 + wn * WTN;
+      xfull = w0 + WTN <= p.x.cols;
 #pragma unroll
-      for (int ii = 0; ii < HR; ++ii) xr[ii] = xent_row(p.x, row_of(HR * h + ii), G.Mlim);
+      for (int ii = 0; ii < HR; ++ii) {
+        xr[ii] = xent_row(p.x, row_of(HR * h + ii), G.Mlim);
+        xany[ii] = __ballot(xr[ii].t >= w0 && xr[ii].t < w0 + WTN) != 0;
+      }
     }
 #pragma unroll
     for (int ii = 0; ii < HR; ++ii) {
@@ -700,9 +732,7 @@ __device__ __forceinline__ void wide_epilogue(const GemmParams& p, const WGeo& G
         if constexpr (EPI == EPI_DL) {
 #pragma unroll
           for (int e = 0; e < 2; ++e)
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-              v[e][u] = xent_dl(p.x, xr[ii], v[e][u], G.n0 + wn * WTN + 16 * (2 * jp + e) + 4 * q + u);
+            xent_dl4(p.x, xr[ii], v[e], G.n0 + wn * WTN + 16 * (2 * jp + e) + 4 * q, xany[ii], xfull);
         }
         if constexpr (EPI == EPI_ADD) store(pack4_bf16(v[0]), pack4_bf16(v[1]), rC2, vo < 0 ? vo : vo / 2);
         else store(pack4_bf16(v[0]), pack4_bf16(v[1]), rC, vo);
@@ -1239,7 +1269,10 @@ enum WideKind {
   WK_DACT,      // B [K][N], dA * act'(H) epilogue, blocked output
   WK_KN,        // B [K][N], plain store, row-major output
   WK_LSE,       // x W^T of the cross entropy, x and W row-major: EPI_LSE
-  WK_DL,        // the same with x blocked: EPI_DL, blocked output
+  WK_LSE_X,     // the same with x blocked
+  WK_LSE_BLK,   // the same with x and W blocked
+  WK_DL,        // x blocked, W row-major: EPI_DL, blocked output
+  WK_DL_BLK,    // the same with x and W blocked
   WK_KN_RM,     // WK_KN with a row-major B
   WK_ADD,       // the same added over calls: EPI_ADD
   WK_DW,        // (this kind and the later ones) ragged-K, row-major output
@@ -1303,7 +1336,10 @@ static void run_wide_m(const WideCall& w, hipStream_t s) {
     case WK_DACT: return launch_wide_act<TC, false, EPI_DACT>(w, s);
     case WK_KN: return launch_wide<TC, false, false, EPI_STORE, ID, false>(w, s);
     case WK_LSE: return launch_wide<TC, true, false, EPI_LSE, ID, false, true, true>(w, s);
+    case WK_LSE_X: return launch_wide<TC, true, false, EPI_LSE, ID, false, false, true>(w, s);
     case WK_DL: return launch_wide<TC, true, false, EPI_DL, ID, true, false, true>(w, s);
+    case WK_LSE_BLK: return launch_wide<TC, true, false, EPI_LSE, ID, false>(w, s);
+    case WK_DL_BLK: return launch_wide<TC, true, false, EPI_DL, ID, true>(w, s);
     case WK_KN_RM: return launch_wide<TC, false, false, EPI_STORE, ID, false, false, true>(w, s);
     case WK_ADD: return launch_wide<TC, false, false, EPI_ADD, ID, false, false, true>(w, s);
     default: return;

@@ -17,9 +17,10 @@ namespace lmoe {
 
 // gemm.hip
 int xent_run_columns(int dtype, int64_t T);
-int launch_xent_lse(int dtype, int64_t T, int d, const void* x, const void* W, const XentParams& xp, hipStream_t s);
-void launch_xent_dl(int dtype, int64_t T, int d, const void* x, const void* W, const XentParams& xp, void* dl, int ld,
+int launch_xent_lse(int dtype, int form, int64_t T, int d, const void* x, const void* W, const XentParams& xp,
                     hipStream_t s);
+void launch_xent_dl(int dtype, int form, int64_t T, int d, const void* x, const void* W, const XentParams& xp, void* dl,
+                    int ld, hipStream_t s);
 void launch_xent_dx(int dtype, int64_t T, int d, int cols, const void* dl, int ld, const void* W, const float* acc_in,
                     float* acc_out, void* dx, hipStream_t s);
 void launch_xent_dx_whole(int64_t T, int d, int cols, const void* dl, int ld, const void* W, void* dx, void* part,
@@ -30,52 +31,77 @@ size_t xent_part_bytes();
 namespace {
 
 constexpr int64_t kDlBytes = (int64_t)256 << 20;
+constexpr int64_t kWBytes = (int64_t)128 << 20;  // of W in blocks, in the forward
+// From how many tokens on the forward copies x, and x and W, to blocks, and the backward W (x it always does).
+constexpr int64_t kFwdX = 512, kFwdBlocked = 4096, kBwdBlocked = 8192;
+constexpr int64_t kCus = 256;   // compute units (the sizes below are asked for on hosts without a device too)
 constexpr int64_t kOperand = (int64_t)1 << 31;   // the bf16 products' operands: 32-bit byte offsets
 
 int64_t esize(const moe_xent_cfg& c) { return c.dtype == MOE_BF16 ? 2 : 4; }
 
-// Columns of a piece: as many as `most`, in equal pieces of whole tiles.
-int piece_columns(const moe_xent_cfg& c, int64_t most) {
-  if (c.V <= most) return c.V;
-  const int64_t n = (c.V + most - 1) / most, even = (c.V + n - 1) / n;
-  return (int)std::min<int64_t>(most, (even + 255) / 256 * 256);
+int fwd_form(const moe_xent_cfg& c) {
+  if (c.dtype != MOE_BF16 || c.T < kFwdX) return kXentRows;
+  return c.T < kFwdBlocked ? kXentX : kXentBlocked;
 }
-int fwd_columns(const moe_xent_cfg& c) {
-  return piece_columns(c, (kOperand - 1) / (c.d_model * 2) / 256 * 256);
-}
-struct BwdPlan {
-  int cols, pieces, ld;   // columns of a piece, pieces, columns of dl's rows
-  size_t x, dl, acc, part, bytes;
+struct FwdPlan {
+  int form, cols;         // kXent*; columns of a piece
+  int64_t blocks;         // runs of columns, at most
+  size_t part, tl, x, W, bytes;
 };
-BwdPlan bwd_plan(const moe_xent_cfg& c) {
-  BwdPlan p{};
-  const int64_t e = esize(c), rows = pad16(c.T);
-  int64_t most = std::max<int64_t>(2048, kDlBytes / (rows * e) / 256 * 256);
-  most = std::min(most, (kOperand - 1) / (c.d_model * 2) / 256 * 256);
-  most = std::min(most, std::max<int64_t>(64, (kOperand - 1) / (rows * 2) / 64 * 64));
-  p.cols = piece_columns(c, most);
-  p.pieces = (c.V + p.cols - 1) / p.cols;
-  const int unit = c.dtype == MOE_BF16 ? 64 : 8;
-  p.ld = (p.cols + unit - 1) / unit * unit;
+FwdPlan fwd_plan(const moe_xent_cfg& c) {
+  FwdPlan p{};
+  p.form = fwd_form(c);
+  const int64_t room = p.form == kXentBlocked ? kWBytes : kOperand - 1;
+  p.cols = (int)std::min<int64_t>(c.V, std::max<int64_t>(256, room / (c.d_model * 2) / 256 * 256));
+  const int run = xent_run_columns(c.dtype, c.T);
+  const int64_t pieces = (c.V + p.cols - 1) / p.cols;
+  p.blocks = (c.V + run - 1) / run + (int64_t)(512 / run) * pieces;   // (a piece is two products at most)
   size_t at = 0;
   auto take = [&](size_t n) {
     const size_t o = at;
     at += (n + 255) / 256 * 256;
     return o;
   };
+  p.part = take((size_t)p.blocks * c.T * sizeof(float2));
+  p.tl = take((size_t)c.T * sizeof(float));
+  if (p.form >= kXentX) p.x = take(pad16(c.T) * c.d_model * 2);
+  if (p.form == kXentBlocked) p.W = take(pad16(p.cols) * c.d_model * 2);
+  p.bytes = at;
+  return p;
+}
+struct BwdPlan {
+  int cols, pieces, ld;   // columns of a piece, pieces, columns of dl's rows
+  size_t x, W, dl, acc, part, bytes;
+  int form;               // kXentX or kXentBlocked
+};
+BwdPlan bwd_plan(const moe_xent_cfg& c) {
+  BwdPlan p{};
+  const int64_t e = esize(c), rows = pad16(c.T);
+  int64_t most = std::max<int64_t>(2048, kDlBytes / (rows * e) / 256 * 256);
+  // Pieces that are whole rounds of the tiles of dW (and, with as many tokens, of the others).
+  const int64_t unit = kCus / std::min<int64_t>(kCus, (c.d_model + 255) / 256) * 256;
+  if (c.dtype == MOE_BF16 && most < c.V && most >= unit) most = most / unit * unit;
+  most = std::min(most, (kOperand - 1) / (c.d_model * 2) / 256 * 256);
+  most = std::min(most, std::max<int64_t>(64, (kOperand - 1) / (rows * 2) / 64 * 64));
+  p.cols = (int)std::min<int64_t>(c.V, most);
+  p.pieces = (c.V + p.cols - 1) / p.cols;
+  const int pad = c.dtype == MOE_BF16 ? 64 : 8;
+  p.ld = (p.cols + pad - 1) / pad * pad;
+  size_t at = 0;
+  auto take = [&](size_t n) {
+    const size_t o = at;
+    at += (n + 255) / 256 * 256;
+    return o;
+  };
+  p.form = c.dtype == MOE_BF16 && c.T >= kBwdBlocked ? kXentBlocked : kXentX;
   p.x = take(rows * c.d_model * e);
+  if (p.form == kXentBlocked) p.W = take(pad16(p.cols) * c.d_model * 2);
   p.dl = take(rows * p.ld * e);
   if (c.dtype == MOE_BF16 && p.pieces > 1) p.acc = take((size_t)c.T * c.d_model * 4);
   if (c.dtype == MOE_BF16 && p.pieces == 1) p.part = take(xent_part_bytes());
   p.bytes = at;
   return p;
 }
-// Forward: the runs' (largest, sum) of every row, then the targets' logits.
-int64_t fwd_blocks(const moe_xent_cfg& c) {
-  const int run = xent_run_columns(c.dtype, c.T), cols = fwd_columns(c);
-  return (c.V + run - 1) / run + (int64_t)(256 / run) * ((c.V + cols - 1) / cols);
-}
-
 // lse and loss of a row from its runs.  A block takes TX rows, TY slices of the runs each.
 __global__ __launch_bounds__(256) void xent_join_kernel(const float2* __restrict__ part, const float* __restrict__ tl,
                                                         const int32_t* __restrict__ target, int blocks, int64_t T, int V,
@@ -83,10 +109,10 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const float2* __restrict
   __shared__ float2 red[256];
   const int lx = threadIdx.x % tx, ly = threadIdx.x / tx, ny = 256 / tx;
   const int64_t t = (int64_t)blockIdx.x * tx + lx;
-  // Sums of exp(l - m) under the largest so far; a NaN logit is in its run's sum.
+  // Sums under the largest so far, in base 2; a NaN logit is in its run's sum.
   auto join = [](float2 a, float2 b) {
     const float m = fmaxf(a.x, b.x), at = m > -INFINITY ? m : 0.f;
-    return make_float2(m, a.y * __builtin_amdgcn_exp2f((a.x - at) * kLog2e) + b.y * __builtin_amdgcn_exp2f((b.x - at) * kLog2e));
+    return make_float2(m, a.y * __builtin_amdgcn_exp2f(a.x - at) + b.y * __builtin_amdgcn_exp2f(b.x - at));
   };
   float2 v = make_float2(-INFINITY, 0.f);
   if (t < T)
@@ -103,7 +129,7 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const float2* __restrict
     __syncthreads();
   }
   if (ly == 0 && t < T) {
-    const float z = red[threadIdx.x].x + logf(red[threadIdx.x].y);
+    const float z = (red[threadIdx.x].x + log2f(red[threadIdx.x].y)) * kLn2;
     const int id = target[t];
     lse[t] = z;
     loss[t] = id >= 0 && id < V ? z - tl[t] : 0.f;
@@ -112,6 +138,7 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const float2* __restrict
 
 // x for the backward's products: the rows whose target is no class as zeros, so that
 // whatever padding holds stays out of dW.  bf16: 16 x 32 blocks, a wave each.
+// target NULL: every row as it is.
 __global__ __launch_bounds__(256) void xent_pack_kernel(const uint16_t* __restrict__ x, const int32_t* __restrict__ target,
                                                         uint16_t* __restrict__ out, int64_t T, int V, int d) {
   const int64_t b = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 6;
@@ -121,7 +148,7 @@ __global__ __launch_bounds__(256) void xent_pack_kernel(const uint16_t* __restri
   const int64_t row = rb * 16 + (lane >> 2);
   const int col = (int)(b - rb * kb) * 32 + (lane & 3) * 8;
   u32x4 v = u32x4{0u, 0u, 0u, 0u};
-  if (row < T && target[row] >= 0 && target[row] < V) v = *reinterpret_cast<const u32x4*>(x + row * d + col);
+  if (row < T && (target == nullptr || (target[row] >= 0 && target[row] < V))) v = *reinterpret_cast<const u32x4*>(x + row * d + col);
   *reinterpret_cast<u32x4*>(out + b * 512 + lane * 8) = v;
 }
 __global__ __launch_bounds__(256) void xent_copy_kernel(const float* __restrict__ x, const int32_t* __restrict__ target,
@@ -136,31 +163,47 @@ __global__ __launch_bounds__(256) void xent_zero_kernel(u32x4* z, int64_t n) {
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) z[i] = u32x4{0u, 0u, 0u, 0u};
 }
 
+void launch_pack(const void* src, const int32_t* target, void* dst, int64_t rows, int V, int d, hipStream_t s) {
+  hipLaunchKernelGGL(xent_pack_kernel, dim3((unsigned)((pad16(rows) / 16 * (d / 32) * 64 + 255) / 256)), dim3(256), 0, s,
+                     (const uint16_t*)src, target, (uint16_t*)dst, rows, V, d);
+}
+
 }  // namespace
 
 size_t xent_ws_bytes(const moe_xent_cfg& c, bool backward) {
   if (c.T == 0) return 0;
   if (backward) return bwd_plan(c).bytes;
-  return (size_t)fwd_blocks(c) * c.T * sizeof(float2) + (size_t)c.T * sizeof(float);
+  return fwd_plan(c).bytes;
 }
 
 void launch_xent(const moe_xent_cfg& c, const void* x, const void* W, const int32_t* target, float* loss, float* lse,
                  void* ws, hipStream_t s) {
   if (c.T == 0) return;
-  const int cols = fwd_columns(c);
+  const FwdPlan p = fwd_plan(c);
+  char* w = (char*)ws;
   XentParams xp{};
   xp.target = target;
-  xp.part = (float2*)ws;
-  xp.tl = (float*)(xp.part + fwd_blocks(c) * c.T);
+  xp.part = (float2*)(w + p.part);
+  xp.tl = (float*)(w + p.tl);
   xp.stride = c.T;
   xp.V = c.V;
-  for (int v = 0; v < c.V; v += cols) {
-    xp.col0 = v;
-    xp.cols = std::min(cols, c.V - v);
-    xp.block0 += launch_xent_lse(c.dtype, c.T, c.d_model, x, (const char*)W + (int64_t)v * c.d_model * esize(c), xp, s);
+  if (p.form >= kXentX) {
+    launch_pack(x, nullptr, w + p.x, c.T, c.V, c.d_model, s);
+    x = w + p.x;
   }
+  for (int64_t v = 0; v < c.V; v += p.cols) {
+    xp.col0 = (int)v;
+    xp.cols = (int)std::min<int64_t>(p.cols, c.V - v);
+    const void* Wv = (const char*)W + v * c.d_model * esize(c);
+    if (p.form == kXentBlocked) {
+      launch_pack(Wv, nullptr, w + p.W, xp.cols, c.V, c.d_model, s);
+      Wv = w + p.W;
+    }
+    xp.block0 += launch_xent_lse(c.dtype, p.form, c.T, c.d_model, x, Wv, xp, s);
+  }
+  // Rows a block: enough blocks for every CU, 64 bytes of a run's rows at least where there are as many.
   int tx = 1;
-  while (tx < 64 && tx < c.T) tx *= 2;
+  while (tx < 64 && tx < c.T && (tx < 8 || c.T >= (int64_t)1024 * tx)) tx *= 2;
   hipLaunchKernelGGL(xent_join_kernel, dim3((unsigned)((c.T + tx - 1) / tx)), dim3(256), 0, s, xp.part, xp.tl, target,
                      xp.block0, c.T, c.V, tx, loss, lse);
 }
@@ -180,8 +223,7 @@ void launch_xent_bwd(const moe_xent_cfg& c, const void* x, const void* W, const 
   void *xp_ = w + p.x, *dl = w + p.dl;
   const bool bf = c.dtype == MOE_BF16;
   if (bf)
-    hipLaunchKernelGGL(xent_pack_kernel, dim3((unsigned)((pad16(c.T) / 16 * (d / 32) * 64 + 255) / 256)), dim3(256), 0, s,
-                       (const uint16_t*)x, target, (uint16_t*)xp_, c.T, c.V, (int)d);
+    launch_pack(x, target, xp_, c.T, c.V, (int)d, s);
   else
     hipLaunchKernelGGL(xent_copy_kernel, dim3((unsigned)((c.T * d / 4 + 255) / 256)), dim3(256), 0, s, (const float*)x,
                        target, (float*)xp_, c.T, c.V, (int)d);
@@ -192,19 +234,20 @@ void launch_xent_bwd(const moe_xent_cfg& c, const void* x, const void* W, const 
   xp.stride = c.T;
   xp.V = c.V;
   float* acc = bf ? (float*)(w + p.acc) : (float*)dx;
-  for (int v = 0; v < c.V; v += p.cols) {
-    xp.col0 = v;
-    xp.cols = std::min(p.cols, c.V - v);
+  for (int64_t v = 0; v < c.V; v += p.cols) {
+    xp.col0 = (int)v;
+    xp.cols = (int)std::min<int64_t>(p.cols, c.V - v);
     const int unit = bf ? 64 : 8, ld = (xp.cols + unit - 1) / unit * unit;
-    const void* Wv = (const char*)W + (int64_t)v * d * e;
-    launch_xent_dl(c.dtype, c.T, (int)d, xp_, Wv, xp, dl, ld, s);
+    const void* Wv = (const char*)W + v * d * e;
+    if (p.form == kXentBlocked) launch_pack(Wv, nullptr, w + p.W, xp.cols, c.V, (int)d, s);
+    launch_xent_dl(c.dtype, p.form, c.T, (int)d, xp_, p.form == kXentBlocked ? w + p.W : Wv, xp, dl, ld, s);
     if (dx && bf && p.pieces == 1) {
       launch_xent_dx_whole(c.T, (int)d, xp.cols, dl, ld, Wv, dx, w + p.part, s);
     } else if (dx) {
       const bool last = v + p.cols >= c.V;
       launch_xent_dx(c.dtype, c.T, (int)d, xp.cols, dl, ld, Wv, v > 0 ? acc : nullptr, acc, bf && last ? dx : nullptr, s);
     }
-    if (dW) launch_xent_dw(c.dtype, c.T, (int)d, xp.cols, dl, ld, xp_, (char*)dW + (int64_t)v * d * e, s);
+    if (dW) launch_xent_dw(c.dtype, c.T, (int)d, xp.cols, dl, ld, xp_, (char*)dW + v * d * e, s);
   }
 }
 
