@@ -535,8 +535,8 @@ size_t moe_embed_bwd_workspace_bytes(const moe_embed_cfg* cfg);
 
 /* dW[v] (accum: +)= scale * sum of dy[t] over the tokens with ids[t] = v: dy [T][d], dW
  * [V][d] dtype.  Summed in float in an order that depends on ids only, rounded once;
- * the same call gives the same bits.  dy of a token whose id is outside the table is
- * not read.  dW may alias no input.  Calls that overlap in time need separate
+ * the same call gives the same bits.  A token whose id is outside the table takes no
+ * part, whatever its dy holds.  dW may alias no input.  Calls that overlap in time need separate
  * workspaces. */
 moe_status moe_embed_bwd(const moe_embed_cfg* cfg, const int32_t* ids, const void* dy, void* dW, void* ws,
                          size_t ws_bytes, moe_stream_t stream);

@@ -42,11 +42,13 @@ void launch_embed(const moe_embed_cfg& c, const int32_t* ids, const void* W, voi
 // -------------------------------------------------------------------- gradient
 // dW[v] = scale * sum of dy[t] over the tokens with ids[t] = v, in token order: the
 // tokens are sorted by id (digits of at most nine bits, lowest first, each pass a
-// stable placement), then a thread owns 16 bytes of a run of kRun sorted tokens,
-// adds in float and stores where the id changes.  An id whose tokens cross a run's
-// border leaves partial sums (one at the run's head, one at its tail), which a last
-// launch adds in run order: the same bits every time, whatever the ids.
-constexpr int kRun = 32;
+// stable placement; up to one tile of tokens all passes in one launch), then a
+// thread owns 16 bytes of a run of kRun sorted tokens, has their rows in flight
+// together, adds in float and stores where the id changes.  An id whose tokens cross
+// a run's border leaves partial sums (one at the run's head, one at its tail), which
+// a last launch adds in run order: the same bits every time, whatever the ids.
+// Bound: bytes, the table's gradient written once and dy read once.
+constexpr int kRun = 16;
 
 struct EmbedPlan {
   int passes, bits;
@@ -61,7 +63,7 @@ static EmbedPlan embed_plan(const moe_embed_cfg& c) {
   p.tiles = std::max<int64_t>(1, sort_tiles(c.T));
   p.runs = (c.T + kRun - 1) / kRun;
   size_t at = 0;
-  auto take = [&](size_t n) {
+  auto take = [&](size_t n) {   // (whole runs of keys and tokens can be read)
     const size_t o = at;
     at += (n + 255) / 256 * 256;
     return o;
@@ -77,15 +79,16 @@ static EmbedPlan embed_plan(const moe_embed_cfg& c) {
 }
 size_t embed_bwd_ws_bytes(const moe_embed_cfg& c) { return c.T == 0 ? 0 : embed_plan(c).bytes; }
 
+// A token's id as a key; V for a token without one.
+__device__ __forceinline__ int id_key(const int32_t* ids, int64_t t, int V) {
+  const int id = ids[t];
+  return id >= 0 && id < V ? id : V;
+}
 struct Digit {   // the digit of sorted item i (pass 0: of token i)
   const int32_t* ids;   // pass 0
   const int32_t* keys;  // later passes
   int V, shift, mask;
-  __device__ __forceinline__ int key(int64_t i) const {
-    if (keys) return keys[i];
-    const int id = ids[i];
-    return id >= 0 && id < V ? id : V;
-  }
+  __device__ __forceinline__ int key(int64_t i) const { return keys ? keys[i] : id_key(ids, i, V); }
   __device__ __forceinline__ int operator()(int64_t i) const { return (key(i) >> shift) & mask; }
 };
 
@@ -116,6 +119,34 @@ __global__ __launch_bounds__(kSortThreads) void embed_place_kernel(Digit dg, con
   }, N, D, 1, counts, blockIdx.x, tiles, L);
 }
 
+// One tile of tokens: every pass, the order between passes in LDS.
+__global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const int32_t* __restrict__ ids, int N, int V, int passes,
+                                                                  int bits, int32_t* __restrict__ key_out,
+                                                                  int32_t* __restrict__ tok_out, u32x4* z, int64_t zb) {
+  __shared__ SortLds L;
+  __shared__ uint16_t order[2][kSortTile];
+  if (blockIdx.x > 0) return fill_zero(z, 0, zb, blockIdx.x - 1, gridDim.x - 1);
+  const int D = 1 << bits;
+  for (int p = 0; p < passes; ++p) {
+    const uint16_t* from = order[(p & 1) ^ 1];
+    uint16_t* to = order[p & 1];
+    auto tok = [&](int64_t i) { return p ? (int)from[i] : (int)i; };
+    const bool last = p == passes - 1;
+    sort_place([&](int64_t i) { return (id_key(ids, tok(i), V) >> (p * bits)) & (D - 1); },
+               [&](int64_t i, int at) {
+                 const int t = tok(i);
+                 if (last) {
+                   key_out[at] = id_key(ids, t, V);
+                   tok_out[at] = t;
+                 } else {
+                   to[at] = (uint16_t)t;
+                 }
+               },
+               N, D, 1, nullptr, 0, 1, L);
+    __syncthreads();
+  }
+}
+
 template <typename T>
 __device__ __forceinline__ void embed_row(T* dW, int64_t at, const float (&acc)[Vec<T>::N], float scale, bool accum) {
   constexpr int V = Vec<T>::N;
@@ -133,87 +164,117 @@ __global__ __launch_bounds__(256) void embed_runs_kernel(const int32_t* __restri
                                                          const T* __restrict__ dy, T* __restrict__ dW,
                                                          float* __restrict__ part, int64_t N, int64_t runs, int V_rows, int d,
                                                          float scale, int accum) {
-  constexpr int V = Vec<T>::N, U = 8;
+  constexpr int V = Vec<T>::N;
+  typedef int i32x4 __attribute__((ext_vector_type(4)));
   const int nc = d / V;
   const int64_t gid = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
   const int64_t run = gid / nc;
   if (run >= runs) return;
   const int c = (int)(gid - run * nc) * V;
-  const int64_t j0 = run * kRun, j1 = min(N, j0 + kRun);
-  int cur = key[j0];
-  bool head = j0 > 0 && key[j0 - 1] == cur;
+  const int64_t j0 = run * kRun;
+  const int n = (int)min((int64_t)kRun, N - j0);   // the run's tokens
+  int k[kRun + 1], t[kRun];
+#pragma unroll
+  for (int q = 0; q < kRun; q += 4) {
+    const i32x4 a = *reinterpret_cast<const i32x4*>(key + j0 + q), b = *reinterpret_cast<const i32x4*>(tok + j0 + q);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      k[q + u] = q + u < n ? a[u] : V_rows;
+      t[q + u] = q + u < n ? b[u] : 0;
+    }
+  }
+  const int prev = j0 > 0 ? key[j0 - 1] : -1;
+  k[kRun] = j0 + kRun < N ? key[j0 + kRun] : V_rows;
+  u32x4 v[kRun];
+#pragma unroll
+  for (int u = 0; u < kRun; ++u)   // (a token without an id has a row too; it is not added)
+    v[u] = *reinterpret_cast<const u32x4*>(dy + (int64_t)t[u] * d + c);
   float acc[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) acc[i] = 0.f;
-  auto partial = [&](int which) {
-    float* o = part + (run * 2 + which) * d + c;
+  bool head = prev == k[0];
 #pragma unroll
-    for (int i = 0; i < V; i += 4) *reinterpret_cast<f32x4*>(o + i) = f32x4{acc[i], acc[i + 1], acc[i + 2], acc[i + 3]};
-  };
-  for (int64_t j = j0; j < j1; j += U) {
-    u32x4 v[U];
-    int k[U];
+  for (int u = 0; u < kRun; ++u) {   // (ids go up: past the last id of the table come the tokens without one)
+    if (k[u] >= V_rows) break;
+    float f[V];
+    Vec<T>::load(&v[u], f);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      k[u] = j + u < j1 ? key[j + u] : V_rows;
-      if (k[u] < V_rows) v[u] = *reinterpret_cast<const u32x4*>(dy + (int64_t)tok[j + u] * d + c);
+    for (int i = 0; i < V; ++i) acc[i] += f[i];
+    if (k[u + 1] == k[u] && u + 1 < kRun) continue;
+    const bool tail = k[u + 1] == k[u];
+    if (head || tail) {
+      float* o = part + (run * 2 + (head ? 0 : 1)) * d + c;
+#pragma unroll
+      for (int i = 0; i < V; i += 4) *reinterpret_cast<f32x4*>(o + i) = f32x4{acc[i], acc[i + 1], acc[i + 2], acc[i + 3]};
+    } else {
+      embed_row(dW, (int64_t)k[u] * d + c, acc, scale, accum);
     }
+    head = false;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (j + u >= j1) break;
-      if (k[u] != cur) {   // (ids go up: past the last id of the table come the tokens without one)
-        if (head) partial(0);
-        else embed_row(dW, (int64_t)cur * d + c, acc, scale, accum);
-        head = false;
-        cur = k[u];
-#pragma unroll
-        for (int i = 0; i < V; ++i) acc[i] = 0.f;
-      }
-      if (cur < V_rows) {
-        float f[V];
-        Vec<T>::load(&v[u], f);
-#pragma unroll
-        for (int i = 0; i < V; ++i) acc[i] += f[i];
-      }
-    }
+    for (int i = 0; i < V; ++i) acc[i] = 0.f;
   }
-  if (cur >= V_rows) return;
-  if (head) partial(0);
-  else if (j1 < N && key[j1] == cur) partial(1);
-  else embed_row(dW, (int64_t)cur * d + c, acc, scale, accum);
 }
 
-// The ids that began in a run and went on past it: its tail, and the heads of the runs up to the last one that they reach.
+// The ids that began in a run and went on past it: its tail, and the heads of the
+// runs up to the last one that they reach.  A block is kJoinCols vectors of columns
+// by four equal shares of those runs, which meet in LDS in order (an id that most
+// tokens have is a long chain).
+constexpr int kJoinCols = 64;
 template <typename T>
-__global__ __launch_bounds__(256) void embed_join_kernel(const int32_t* __restrict__ key, T* __restrict__ dW,
-                                                         const float* __restrict__ part, int64_t N, int64_t runs, int V_rows,
-                                                         int d, float scale, int accum) {
+__global__ __launch_bounds__(4 * kJoinCols) void embed_join_kernel(const int32_t* __restrict__ key, T* __restrict__ dW,
+                                                                   const float* __restrict__ part, int64_t N, int64_t runs,
+                                                                   int V_rows, int d, int slabs, float scale, int accum) {
   constexpr int V = Vec<T>::N;
-  const int nc = d / V;
-  const int64_t gid = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-  const int64_t run = gid / nc;
-  if (run >= runs) return;
-  const int c = (int)(gid - run * nc) * V;
+  __shared__ f32x4 red[3][kJoinCols][V / 4];
+  const int64_t run = (int64_t)blockIdx.x / slabs;
   const int64_t j0 = run * kRun, j1 = j0 + kRun;
   if (j1 >= N) return;
   const int cur = key[j1 - 1];
   if (cur >= V_rows || key[j1] != cur || (j0 > 0 && key[j0 - 1] == cur)) return;
-  float acc[V];
-  auto add = [&](int64_t at, bool first) {
-    const float* o = part + at * d + c;
-#pragma unroll
-    for (int i = 0; i < V; i += 4) {
-      const f32x4 v = *reinterpret_cast<const f32x4*>(o + i);
-#pragma unroll
-      for (int u = 0; u < 4; ++u) acc[i + u] = first ? v[u] : acc[i + u] + v[u];
-    }
-  };
-  add(run * 2 + 1, true);
-  for (int64_t m = run + 1; m < runs; ++m) {
-    add(m * 2, false);
-    const int64_t end = (m + 1) * kRun;
-    if (end >= N || key[end] != cur) break;
+  // The last run that begins with this id: steps that double, then halve.
+  int64_t lo = run + 1, step = 1;
+  while (lo + step < runs && key[(lo + step) * kRun] == cur) {
+    lo += step;
+    step *= 2;
   }
+  for (; step > 0; step /= 2)
+    if (lo + step < runs && key[(lo + step) * kRun] == cur) lo += step;
+  const int64_t heads = lo - run;   // runs run + 1 .. lo
+  const int share = threadIdx.x / kJoinCols, lc = threadIdx.x % kJoinCols;
+  const int c = ((int)(blockIdx.x % slabs) * kJoinCols + lc) * V;
+  const bool on = c < d;
+  const int64_t a = run + 1 + heads * share / 4, b = run + 1 + heads * (share + 1) / 4;
+  float acc[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) acc[i] = 0.f;
+  if (on) {
+    if (share == 0)
+#pragma unroll
+      for (int q = 0; q < V / 4; ++q) Vec<float>::load(part + (run * 2 + 1) * d + c + 4 * q, acc + 4 * q);
+    constexpr int U = 8;
+    for (int64_t m = a; m < b; m += U) {
+      f32x4 p[U][V / 4];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int q = 0; q < V / 4; ++q)
+          p[u][q] = *reinterpret_cast<const f32x4*>(part + min(m + u, b - 1) * 2 * d + c + 4 * q);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (m + u < b)
+#pragma unroll
+          for (int i = 0; i < V; ++i) acc[i] += p[u][i / 4][i % 4];
+    }
+    if (share > 0)
+#pragma unroll
+      for (int q = 0; q < V / 4; ++q) red[share - 1][lc][q] = f32x4{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
+  }
+  __syncthreads();
+  if (share > 0 || !on) return;
+#pragma unroll
+  for (int s = 0; s < 3; ++s)
+#pragma unroll
+    for (int i = 0; i < V; ++i) acc[i] += red[s][lc][i / 4][i % 4];
   embed_row(dW, (int64_t)cur * d + c, acc, scale, accum);
 }
 
@@ -231,36 +292,34 @@ void launch_embed_bwd(const moe_embed_cfg& c, const int32_t* ids, const void* dy
   const EmbedPlan p = embed_plan(c);
   char* w = (char*)ws;
   int32_t* counts = (int32_t*)(w + p.counts);
-  const bool count = p.tiles > 1;
-  const int launches = p.passes * (count ? 2 : 1);
-  int done = 0;
-  auto za = [&](int i) { return zeros * i / launches; };
-  const unsigned grid = (unsigned)p.tiles + zblocks;
-  const int D = 1 << p.bits;
-  for (int q = 0; q < p.passes; ++q) {
-    const int32_t *kin = q ? (const int32_t*)(w + p.key[(q - 1) & 1]) : nullptr,
-                  *tin = q ? (const int32_t*)(w + p.tok[(q - 1) & 1]) : nullptr;
-    const Digit dg{ids, kin, c.V, q * p.bits, D - 1};
-    if (count) {
-      hipLaunchKernelGGL(embed_count_kernel, dim3(grid), dim3(kSortThreads), 0, s, dg, c.T, D, counts, p.tiles, z,
-                         za(done), za(done + 1));
-      ++done;
+  int32_t *key = (int32_t*)(w + p.key[0]), *tok = (int32_t*)(w + p.tok[0]);
+  if (p.tiles == 1) {
+    hipLaunchKernelGGL(embed_sort_kernel, dim3(1 + zblocks), dim3(kSortThreads), 0, s, ids, (int)c.T, c.V, p.passes, p.bits,
+                       key, tok, z, zeros);
+  } else {
+    const int launches = 2 * p.passes, D = 1 << p.bits;
+    const unsigned grid = (unsigned)p.tiles + zblocks;
+    auto za = [&](int i) { return zeros * i / launches; };
+    for (int q = 0; q < p.passes; ++q) {
+      const Digit dg{ids, q ? key : nullptr, c.V, q * p.bits, D - 1};
+      const int32_t* from = q ? tok : nullptr;
+      key = (int32_t*)(w + p.key[q & 1]);
+      tok = (int32_t*)(w + p.tok[q & 1]);
+      hipLaunchKernelGGL(embed_count_kernel, dim3(grid), dim3(kSortThreads), 0, s, dg, c.T, D, counts, p.tiles, z, za(2 * q),
+                         za(2 * q + 1));
+      hipLaunchKernelGGL(embed_place_kernel, dim3(grid), dim3(kSortThreads), 0, s, dg, from, c.T, D, counts, p.tiles, key, tok,
+                         z, za(2 * q + 1), za(2 * q + 2));
     }
-    hipLaunchKernelGGL(embed_place_kernel, dim3(grid), dim3(kSortThreads), 0, s, dg, tin, c.T, D, counts, p.tiles,
-                       (int32_t*)(w + p.key[q & 1]), (int32_t*)(w + p.tok[q & 1]), z, za(done), za(done + 1));
-    ++done;
   }
-  const int last = (p.passes - 1) & 1;
-  const int32_t *key = (const int32_t*)(w + p.key[last]), *tok = (const int32_t*)(w + p.tok[last]);
   auto go = [&](auto tag) {
     using T = decltype(tag);
-    const int64_t n = p.runs * (c.d_model / Vec<T>::N);
-    const unsigned blocks = (unsigned)((n + 255) / 256);
-    hipLaunchKernelGGL(embed_runs_kernel<T>, dim3(blocks), dim3(256), 0, s, key, tok, (const T*)dy, (T*)dW,
-                       (float*)(w + p.part), c.T, p.runs, c.V, c.d_model, c.scale, c.accum);
+    const int nc = c.d_model / Vec<T>::N, slabs = (nc + kJoinCols - 1) / kJoinCols;
+    const int64_t n = p.runs * nc;
+    hipLaunchKernelGGL(embed_runs_kernel<T>, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, key, tok, (const T*)dy,
+                       (T*)dW, (float*)(w + p.part), c.T, p.runs, c.V, c.d_model, c.scale, c.accum);
     if (p.runs > 1)
-      hipLaunchKernelGGL(embed_join_kernel<T>, dim3(blocks), dim3(256), 0, s, key, (T*)dW, (const float*)(w + p.part), c.T,
-                         p.runs, c.V, c.d_model, c.scale, c.accum);
+      hipLaunchKernelGGL(embed_join_kernel<T>, dim3((unsigned)((p.runs - 1) * slabs)), dim3(4 * kJoinCols), 0, s, key, (T*)dW,
+                         (const float*)(w + p.part), c.T, p.runs, c.V, c.d_model, slabs, c.scale, c.accum);
   };
   if (c.dtype == MOE_BF16) go(uint16_t{});
   else go(float{});

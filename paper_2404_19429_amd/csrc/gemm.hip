@@ -153,9 +153,12 @@ __global__ __launch_bounds__(256) void gemm_f32_kernel(GemmParams p, int tm, int
     lo = __builtin_amdgcn_readlane(P.lo, g);
     span = __builtin_amdgcn_readlane(P.span, g);
   }
-  const int Mlim = RAGGED_K ? p.M : span, Klim = RAGGED_K ? span : p.K;
-  // The cross entropy: the gradient at the logits has padding columns (zeros) that W has no rows for.
-  const int Alim = RAGGED_K ? (Mlim + 3) & ~3 : Mlim, Blim = EPI == EPI_DL ? p.x.cols : p.N, KlimB = EPI == EPI_ADD ? p.M : Klim;
+  // The cross entropy: the gradient at the logits has padding columns (zeros) that W has no rows for; its product
+  // with W may be in groups, each a slice of p.ksplit classes.
+  const int k0g = EPI == EPI_ADD ? g * p.ksplit : 0;
+  const int Mlim = RAGGED_K ? p.M : span, Klim = RAGGED_K ? span : EPI == EPI_ADD ? min(p.ksplit, p.K - k0g) : p.K;
+  const int Alim = RAGGED_K ? (Mlim + 3) & ~3 : Mlim, Blim = EPI == EPI_DL ? p.x.cols : p.N;
+  const int KlimB = EPI == EPI_ADD ? min(p.ksplit, p.M - k0g) : Klim;
   if (m0 >= Mlim) return;
   const float* Ab = (const float*)p.A + g * p.sA + (int64_t)lo * p.lda;
   const float* Bb = (const float*)p.B + g * p.sB + (RAGGED_K ? (int64_t)lo * p.ldb : 0);
@@ -767,16 +770,58 @@ void launch_xent_dl(int dtype, int form, int64_t T, int d, const void* x, const 
 }
 
 // dx over one piece: acc_in (NULL = 0) + dl W -> acc_out (float), or rounded to dx (bf16).
+//
+// float: few tiles with long sums are cut into slices of the classes (each a group of the launch, its sums in `part`),
+// enough of them for four blocks a CU, which a launch adds in order.  500 tokens, 10007 classes, width 512: 109 us in
+// one, the product of the same size that has tiles enough 63.
+static int xent_slices(int64_t T, int d, int cols) {
+  const int64_t tiles = (T + 63) / 64 * ((d + 63) / 64);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(16, 1024 / tiles), cols / 256));
+}
+size_t xent_slices_bytes(int64_t T, int d, int cols) {
+  const int n = xent_slices(T, d, cols);
+  return n > 1 ? (size_t)n * T * d * sizeof(float) : 0;
+}
+__global__ __launch_bounds__(256) void xent_slices_kernel(const float* __restrict__ part, int n, int64_t size,
+                                                          const float* __restrict__ in, float* __restrict__ out) {
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (i >= size) return;
+  f32x4 v[16];
+#pragma unroll
+  for (int q = 0; q < 16; ++q)
+    if (q < n) v[q] = *reinterpret_cast<const f32x4*>(part + q * size + i);
+  f32x4 a = v[0];
+#pragma unroll
+  for (int q = 1; q < 16; ++q)
+    if (q < n) a += v[q];
+  if (in) a += *reinterpret_cast<const f32x4*>(in + i);
+  *reinterpret_cast<f32x4*>(out + i) = a;
+}
+
 void launch_xent_dx(int dtype, int64_t T, int d, int cols, const void* dl, int ld, const void* W, const float* acc_in,
-                    float* acc_out, void* dx, hipStream_t s) {
+                    float* acc_out, void* dx, void* part, hipStream_t s) {
   GemmParams p = xent_params(T, d, ld, dl, ld, pad16(T) * ld, W, d, (int64_t)cols * d, acc_out, d);
   p.Aux = acc_in;
   p.C2 = dx;
   p.M = cols;
-  const WideCall w = xent_call(WK_ADD, T, d, p);
+  WideCall w = xent_call(WK_ADD, T, d, p);
   if (dtype == MOE_BF16) return run_wide_any(w, s);
-  if (f32_tile(w, num_cus()) == 32) launch_f32<1, false, false, EPI_ADD>(p, 1, T, d, s);
-  else launch_f32<2, false, false, EPI_ADD>(p, 1, T, d, s);
+  int n = xent_slices(T, d, cols);
+  p.ksplit = n > 1 ? ((cols + n - 1) / n + 15) / 16 * 16 : ld;
+  n = (cols + p.ksplit - 1) / p.ksplit;
+  p.sA = p.ksplit;
+  p.sB = (int64_t)p.ksplit * d;
+  if (n > 1) {
+    p.sC = T * d;
+    p.C = part;
+    p.Aux = nullptr;
+  }
+  w.groups = n;
+  if (n == 1 && f32_tile(w, num_cus()) == 32) launch_f32<1, false, false, EPI_ADD>(p, n, T, d, s);
+  else launch_f32<2, false, false, EPI_ADD>(p, n, T, d, s);
+  if (n > 1)
+    hipLaunchKernelGGL(xent_slices_kernel, dim3((unsigned)((T * d / 4 + 255) / 256)), dim3(256), 0, s, (const float*)part, n,
+                       T * d, acc_in, acc_out);
 }
 
 // dx where the vocabulary is one piece (bf16): no float sums to keep, and where the

@@ -8,7 +8,9 @@
 // with one ballot per key bit.  Up to one tile it is one launch; past that the
 // tiles' counts come from a launch before it, and every block sums those of the
 // tiles before its own (D numbers a tile, L2-resident).  Integers only, no
-// atomics on device memory: the same positions every time.
+// atomics on device memory: the same positions every time.  A block is a chain of
+// latencies (keys, the tiles' counts, three barriers), so what can be in flight
+// together is.
 #pragma once
 
 #include "internal.h"
@@ -98,18 +100,26 @@ __device__ __forceinline__ void sort_place(const Key& key, const Emit& emit, int
   const int e = threadIdx.x;
   if (e < D) {
     if (tiles > 1) {
+      constexpr int U = 8;   // tiles whose counts are read together
       const int32_t* c = counts + e;
-      for (int64_t t = 0; t < tiles; ++t) {
-        const int n = c[t * D];
-        if (t < tile) run += n;
-        total += n;
+      for (int64_t t = 0; t < tiles; t += U) {
+        int n[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) n[u] = t + u < tiles ? c[(t + u) * D] : 0;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          run += t + u < tile ? n[u] : 0;
+          total += n[u];
+        }
       }
     }
-    int sum = 0;
+    int n[kSortWaves], sum = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) n[w] = L.cnt[w][e];
+#pragma unroll
     for (int w = 0; w < kSortWaves; ++w) {
-      const int n = L.cnt[w][e];
       L.cnt[w][e] = run + sum;
-      sum += n;
+      sum += n[w];
     }
     if (tiles <= 1) total = sum;
   }
