@@ -6,7 +6,7 @@ namespace lmoe {
 
 // ---------------------------------------------------------------------- lookup
 // y[t] = scale W[ids[t]], 0 for an id outside the table.  A thread owns 16 bytes.
-template <typename T>
+template <typename T, bool S>
 __global__ __launch_bounds__(256) void embed_kernel(const int32_t* __restrict__ ids, const T* __restrict__ W,
                                                     T* __restrict__ y, int64_t T_tokens, int V_rows, int d, float scale) {
   constexpr int V = Vec<T>::N;
@@ -24,25 +24,29 @@ __global__ __launch_bounds__(256) void embed_kernel(const int32_t* __restrict__ 
 #pragma unroll
     for (int i = 0; i < V; ++i) f[i] *= scale;
   }
-  Vec<T>::store(y + t * d + c, f);
+  store16<S>(y + t * d + c, f);
 }
 
 void launch_embed(const moe_embed_cfg& c, const int32_t* ids, const void* W, void* y, hipStream_t s) {
   if (c.T == 0) return;
-  auto go = [&](auto tag) {
+  auto go = [&](auto tag, auto stream) {
     using T = decltype(tag);
     const int64_t n = c.T * (c.d_model / Vec<T>::N);
-    hipLaunchKernelGGL(embed_kernel<T>, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, ids, (const T*)W, (T*)y, c.T,
-                       c.V, c.d_model, c.scale);
+    hipLaunchKernelGGL((embed_kernel<T, decltype(stream)::value>), dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, ids,
+                       (const T*)W, (T*)y, c.T, c.V, c.d_model, c.scale);
   };
-  if (c.dtype == MOE_BF16) go(uint16_t{});
-  else go(float{});
+  auto type = [&](auto stream) {
+    if (c.dtype == MOE_BF16) go(uint16_t{}, stream);
+    else go(float{}, stream);
+  };
+  if (stream_bytes(c.T * c.d_model * (c.dtype == MOE_BF16 ? 2 : 4))) type(std::true_type{});
+  else type(std::false_type{});
 }
 
 // -------------------------------------------------------------------- gradient
 // dW[v] = scale * sum of dy[t] over the tokens with ids[t] = v, in token order: the
 // tokens are sorted by id (digits of at most nine bits, lowest first, each pass a
-// stable placement; up to one tile of tokens all passes in one launch), then a
+// stable placement; few tokens by comparing all pairs, in one launch), then a
 // thread owns 16 bytes of a run of kRun sorted tokens, has their rows in flight
 // together, adds in float and stores where the id changes.  An id whose tokens cross
 // a run's border leaves partial sums (one at the run's head, one at its tail), which
@@ -94,56 +98,73 @@ struct Digit {   // the digit of sorted item i (pass 0: of token i)
 
 // Zeros for the table's gradient, 16-byte vectors [a, b), from the blocks that a
 // launch has beside its sorting ones: the table is written while the few blocks
-// of the sort wait for one another.
+// of the sort wait for one another.  The table's gradient is the optimiser's next, far
+// behind: stored past the caches (16384 tokens, 50257 rows of 2048: 113 -> 103 us).
 __device__ __forceinline__ void fill_zero(u32x4* z, int64_t a, int64_t b, int64_t block, int64_t blocks) {
-  for (int64_t i = a + block * blockDim.x + threadIdx.x; i < b; i += blocks * blockDim.x) z[i] = u32x4{0u, 0u, 0u, 0u};
+  for (int64_t i = a + block * blockDim.x + threadIdx.x; i < b; i += blocks * blockDim.x) store16<true>((void*)(z + i), u32x4{0u, 0u, 0u, 0u});
 }
 
-__global__ __launch_bounds__(kSortThreads) void embed_count_kernel(Digit dg, int64_t N, int D, int32_t* __restrict__ counts,
-                                                                   int64_t tiles, u32x4* z, int64_t za, int64_t zb) {
+template <int NT>
+__global__ __launch_bounds__(NT) void embed_count_kernel(Digit dg, int64_t N, int D, int32_t* __restrict__ counts,
+                                                         int64_t tiles, u32x4* z, int64_t za, int64_t zb) {
   __shared__ int32_t hist[kSortMaxD];
   if (blockIdx.x >= tiles) return fill_zero(z, za, zb, blockIdx.x - tiles, gridDim.x - tiles);
-  sort_count(dg, N, D, counts, blockIdx.x, hist);
+  sort_count<NT>(dg, N, D, counts, blockIdx.x, hist);
 }
 
-__global__ __launch_bounds__(kSortThreads) void embed_place_kernel(Digit dg, const int32_t* __restrict__ toks, int64_t N,
-                                                                   int D, const int32_t* __restrict__ counts, int64_t tiles,
-                                                                   int32_t* __restrict__ key_out,
-                                                                   int32_t* __restrict__ tok_out, u32x4* z, int64_t za,
-                                                                   int64_t zb) {
-  __shared__ SortLds L;
+template <int NT>
+__global__ __launch_bounds__(NT) void embed_place_kernel(Digit dg, const int32_t* __restrict__ toks, int64_t N, int D,
+                                                         const int32_t* __restrict__ counts, int64_t tiles,
+                                                         int32_t* __restrict__ key_out, int32_t* __restrict__ tok_out, u32x4* z,
+                                                         int64_t za, int64_t zb) {
+  __shared__ SortLds<NT> L;
   if (blockIdx.x >= tiles) return fill_zero(z, za, zb, blockIdx.x - tiles, gridDim.x - tiles);
-  sort_place(dg, [&](int64_t i, int at) {
+  sort_place<NT>(dg, [&](int64_t i, int at) {
     key_out[at] = dg.key(i);
     tok_out[at] = toks ? toks[i] : (int32_t)i;
   }, N, D, 1, counts, blockIdx.x, tiles, L);
 }
 
-// One tile of tokens: every pass, the order between passes in LDS.
-__global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const int32_t* __restrict__ ids, int N, int V, int passes,
-                                                                  int bits, int32_t* __restrict__ key_out,
-                                                                  int32_t* __restrict__ tok_out, u32x4* z, int64_t zb) {
-  __shared__ SortLds L;
-  __shared__ uint16_t order[2][kSortTile];
-  if (blockIdx.x > 0) return fill_zero(z, 0, zb, blockIdx.x - 1, gridDim.x - 1);
-  const int D = 1 << bits;
-  for (int p = 0; p < passes; ++p) {
-    const uint16_t* from = order[(p & 1) ^ 1];
-    uint16_t* to = order[p & 1];
-    auto tok = [&](int64_t i) { return p ? (int)from[i] : (int)i; };
-    const bool last = p == passes - 1;
-    sort_place([&](int64_t i) { return (id_key(ids, tok(i), V) >> (p * bits)) & (D - 1); },
-               [&](int64_t i, int at) {
-                 const int t = tok(i);
-                 if (last) {
-                   key_out[at] = id_key(ids, t, V);
-                   tok_out[at] = t;
-                 } else {
-                   to[at] = (uint16_t)t;
-                 }
-               },
-               N, D, 1, nullptr, 0, 1, L);
-    __syncthreads();
+// Few tokens: a token's place is the number of tokens whose id is smaller, or the
+// same and earlier.  A block takes 64 tokens, each of its waves compares them with a
+// quarter of all ids (in LDS, four to a read): N^2 / 64 comparisons of a wave, over
+// many CUs, against the radix passes' chain of launches.
+constexpr int kPairs = 8192;
+__global__ __launch_bounds__(256) void embed_pairs_kernel(const int32_t* __restrict__ ids, int N, int V, int blocks,
+                                                          int32_t* __restrict__ key_out, int32_t* __restrict__ tok_out,
+                                                          u32x4* z, int64_t zb) {
+  typedef int i32x4 __attribute__((ext_vector_type(4)));
+  extern __shared__ __attribute__((aligned(16))) int flat[];   // the ids, padded to whole chunks for four waves
+  __shared__ int part[4][64];
+  const i32x4* keys = (const i32x4*)flat;
+  if (blockIdx.x >= blocks) return fill_zero(z, 0, zb, blockIdx.x - blocks, gridDim.x - blocks);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int padded = (N + 255) / 256 * 256;
+  for (int i = threadIdx.x; i < padded; i += 256) flat[i] = i < N ? id_key(ids, i, V) : 0x7fffffff;
+  __syncthreads();
+  const int t0 = blockIdx.x * 64, t = t0 + lane;
+  const int mine = flat[min(t, padded - 1)];
+  int n = 0;
+  const int quarter = padded / 4;   // a multiple of 64
+  for (int b = wave * quarter; b < (wave + 1) * quarter; b += 64) {
+    if (b != t0) {
+      const int limit = mine + (b < t0 ? 1 : 0);   // (ids are at most 2^30)
+#pragma unroll
+      for (int q = 0; q < 16; ++q) {
+        const i32x4 k = keys[b / 4 + q];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) n += k[u] < limit ? 1 : 0;
+      }
+    } else {
+      for (int j = 0; j < 64; ++j) n += flat[b + j] < mine + (j < lane ? 1 : 0) ? 1 : 0;
+    }
+  }
+  part[wave][lane] = n;
+  __syncthreads();
+  if (wave == 0 && t < N) {
+    const int at = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
+    key_out[at] = mine;
+    tok_out[at] = t;
   }
 }
 
@@ -156,7 +177,7 @@ __device__ __forceinline__ void embed_row(T* dW, int64_t at, const float (&acc)[
   if (accum) Vec<T>::load(dW + at, o);
 #pragma unroll
   for (int i = 0; i < V; ++i) o[i] = accum ? fmaf(scale, acc[i], o[i]) : scale * acc[i];
-  Vec<T>::store(dW + at, o);
+  store16<true>(dW + at, o);
 }
 
 template <typename T>
@@ -281,35 +302,43 @@ __global__ __launch_bounds__(4 * kJoinCols) void embed_join_kernel(const int32_t
 void launch_embed_bwd(const moe_embed_cfg& c, const int32_t* ids, const void* dy, void* dW, void* ws, hipStream_t s) {
   const int esz = c.dtype == MOE_BF16 ? 2 : 4;
   const int64_t zeros = c.accum ? 0 : (int64_t)c.V * c.d_model * esz / 16;
-  const unsigned zblocks = zeros ? (unsigned)std::min<int64_t>(1024, (zeros + 4 * kSortThreads - 1) / (4 * kSortThreads)) : 0;
+  const unsigned zblocks = zeros ? (unsigned)std::min<int64_t>(512, (zeros + 1023) / 1024) : 0;   // of 256 threads
   u32x4* z = (u32x4*)dW;
   if (c.T == 0) {
     if (zeros)
-      hipLaunchKernelGGL(embed_count_kernel, dim3(zblocks), dim3(kSortThreads), 0, s, Digit{}, (int64_t)0, 0, nullptr,
-                         (int64_t)0, z, (int64_t)0, zeros);
+      hipLaunchKernelGGL(embed_pairs_kernel, dim3(zblocks), dim3(256), 0, s, ids, 0, c.V, 0, nullptr, nullptr, z, zeros);
     return;
   }
   const EmbedPlan p = embed_plan(c);
   char* w = (char*)ws;
   int32_t* counts = (int32_t*)(w + p.counts);
   int32_t *key = (int32_t*)(w + p.key[0]), *tok = (int32_t*)(w + p.tok[0]);
-  if (p.tiles == 1) {
-    hipLaunchKernelGGL(embed_sort_kernel, dim3(1 + zblocks), dim3(kSortThreads), 0, s, ids, (int)c.T, c.V, p.passes, p.bits,
-                       key, tok, z, zeros);
-  } else {
+  auto radix = [&](auto nt) {
+    constexpr int NT = decltype(nt)::value;
     const int launches = 2 * p.passes, D = 1 << p.bits;
-    const unsigned grid = (unsigned)p.tiles + zblocks;
+    const unsigned grid = (unsigned)p.tiles + (zblocks * 256 + NT - 1) / NT;
     auto za = [&](int i) { return zeros * i / launches; };
     for (int q = 0; q < p.passes; ++q) {
       const Digit dg{ids, q ? key : nullptr, c.V, q * p.bits, D - 1};
       const int32_t* from = q ? tok : nullptr;
       key = (int32_t*)(w + p.key[q & 1]);
       tok = (int32_t*)(w + p.tok[q & 1]);
-      hipLaunchKernelGGL(embed_count_kernel, dim3(grid), dim3(kSortThreads), 0, s, dg, c.T, D, counts, p.tiles, z, za(2 * q),
+      hipLaunchKernelGGL(embed_count_kernel<NT>, dim3(grid), dim3(NT), 0, s, dg, c.T, D, counts, p.tiles, z, za(2 * q),
                          za(2 * q + 1));
-      hipLaunchKernelGGL(embed_place_kernel, dim3(grid), dim3(kSortThreads), 0, s, dg, from, c.T, D, counts, p.tiles, key, tok,
-                         z, za(2 * q + 1), za(2 * q + 2));
+      hipLaunchKernelGGL(embed_place_kernel<NT>, dim3(grid), dim3(NT), 0, s, dg, from, c.T, D, counts, p.tiles, key, tok, z,
+                         za(2 * q + 1), za(2 * q + 2));
     }
+  };
+  if (c.T <= kPairs) {
+    const int blocks = (int)((c.T + 63) / 64), lds = (int)((c.T + 255) / 256 * 256 * 4);
+    static std::atomic<uint64_t> lds_ok{0};
+    allow_dyn_lds((const void*)embed_pairs_kernel, kPairs * 4, lds_ok);
+    hipLaunchKernelGGL(embed_pairs_kernel, dim3(blocks + zblocks), dim3(256), lds, s, ids, (int)c.T, c.V, blocks, key, tok, z,
+                       zeros);
+  } else if (sort_threads(c.T) == kSortSmall) {
+    radix(std::integral_constant<int, kSortSmall>{});
+  } else {
+    radix(std::integral_constant<int, kSortLarge>{});
   }
   auto go = [&](auto tag) {
     using T = decltype(tag);

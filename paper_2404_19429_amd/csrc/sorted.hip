@@ -24,35 +24,43 @@ struct ExpertOf {   // the expert of choice i, -1: none
   }
 };
 
-__global__ __launch_bounds__(kSortThreads) void sorted_count_kernel(const int32_t* __restrict__ idx, int64_t N, int E,
-                                                                    int32_t* __restrict__ counts) {
+template <int NT>
+__global__ __launch_bounds__(NT) void sorted_count_kernel(const int32_t* __restrict__ idx, int64_t N, int E,
+                                                          int32_t* __restrict__ counts) {
   __shared__ int32_t hist[kSortMaxD];
-  sort_count(ExpertOf{idx, E}, N, E, counts, blockIdx.x, hist);
+  sort_count<NT>(ExpertOf{idx, E}, N, E, counts, blockIdx.x, hist);
 }
 
-// slot and src of a tile's choices; block 0 also writes the row ranges.  Rows
-// between an expert's last and the next one's first, and past the last, hold none.
-__global__ __launch_bounds__(kSortThreads) void sorted_place_kernel(const int32_t* __restrict__ idx, int64_t N, int E,
-                                                                    int align, int64_t R,
-                                                                    const int32_t* __restrict__ counts,
-                                                                    int32_t* __restrict__ row_begin,
-                                                                    int32_t* __restrict__ row_end,
-                                                                    int32_t* __restrict__ slot,
-                                                                    int32_t* __restrict__ src) {
-  __shared__ SortLds L;
-  sort_place(ExpertOf{idx, E}, [&](int64_t i, int at) {
+// The row ranges, and which rows hold no choice: those between an expert's last
+// and the next one's first, and those past the last (none(r) for each, shared by
+// the grid's threads).
+template <int NT, typename None>
+__device__ __forceinline__ void sorted_ranges(const SortLds<NT>& L, int E, int align, int64_t R, int32_t* row_begin,
+                                              int32_t* row_end, int64_t block, int64_t blocks, const None& none) {
+  for (int e = threadIdx.x; e < E; e += NT) {
+    const int b = L.first[e], n = L.total[e];
+    if (block == 0) {
+      row_begin[e] = b;
+      row_end[e] = b + n;
+    }
+    if (block == 0)
+      for (int r = b + n; r < b + (n + align - 1) / align * align; ++r) none(r);
+  }
+  for (int64_t r = L.used + block * NT + threadIdx.x; r < R; r += blocks * NT) none(r);
+}
+
+// slot and src of a tile's choices; block 0 also writes the row ranges.
+template <int NT>
+__global__ __launch_bounds__(NT) void sorted_place_kernel(const int32_t* __restrict__ idx, int64_t N, int E, int align,
+                                                          int64_t R, const int32_t* __restrict__ counts,
+                                                          int32_t* __restrict__ row_begin, int32_t* __restrict__ row_end,
+                                                          int32_t* __restrict__ slot, int32_t* __restrict__ src) {
+  __shared__ SortLds<NT> L;
+  sort_place<NT>(ExpertOf{idx, E}, [&](int64_t i, int at) {
     slot[i] = at;
     if (at >= 0) src[at] = (int32_t)i;
   }, N, E, align, counts, blockIdx.x, gridDim.x, L);
-  const int e = threadIdx.x;
-  if (blockIdx.x == 0 && e < E) {
-    const int b = L.first[e], n = L.total[e];
-    row_begin[e] = b;
-    row_end[e] = b + n;
-    for (int r = b + n; r < b + (n + align - 1) / align * align; ++r) src[r] = -1;
-  }
-  const int64_t step = (int64_t)gridDim.x * kSortThreads;
-  for (int64_t r = L.used + (int64_t)blockIdx.x * kSortThreads + threadIdx.x; r < R; r += step) src[r] = -1;
+  sorted_ranges<NT>(L, E, align, R, row_begin, row_end, blockIdx.x, gridDim.x, [&](int64_t r) { src[r] = -1; });
 }
 
 size_t sorted_dispatch_ws_bytes(const moe_sorted_cfg& c) {
@@ -61,46 +69,114 @@ size_t sorted_dispatch_ws_bytes(const moe_sorted_cfg& c) {
 }
 
 // ---------------------------------------------------------------------- gather
-// rows[r] = x[src[r] / k].  A wave moves sixteen rows by U * 4 vectors of columns:
-// four lanes a row, so that a bfloat16 block is written as one KiB.
-template <typename T, int U>
+// rows[r] = x[src[r] / k].  A wave moves sixteen rows by U * 8 vectors of columns:
+// eight lanes a row, so that a load and a store are whole cache lines (a bfloat16
+// block's half is 512 bytes in one run).  Bound: bytes; 16384 x 2 rows of 2048 in
+// bfloat16, 201 MB moved.
+template <typename T, int U, bool S>
+__device__ __forceinline__ void gather_rows(const T* __restrict__ x, T* __restrict__ rows, int64_t r0, const int (&i)[2], int d,
+                                            int k, int c0) {
+  constexpr int V = Vec<T>::N;
+  u32x4 v[2][U];
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    if (i[h] >= 0) {
+      const T* from = x + (int64_t)((uint32_t)i[h] / (uint32_t)k) * d;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (c0 + u * 8 * V < d) v[h][u] = *reinterpret_cast<const u32x4*>(from + c0 + u * 8 * V);
+    }
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    if (i[h] >= 0)
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (c0 + u * 8 * V < d) store16<S>((void*)(rows + ebuf_off<T>(r0 + 8 * h, c0 + u * 8 * V, d)), v[h][u]);
+}
+template <typename T, int U, bool S>
 __global__ __launch_bounds__(256) void sorted_gather_kernel(const T* __restrict__ x, const int32_t* __restrict__ src,
                                                             T* __restrict__ rows, int64_t R, int64_t N, int d, int k,
                                                             int cols) {
-  constexpr int V = Vec<T>::N;
   const int64_t w = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 6;
   const int lane = threadIdx.x & 63;
-  const int64_t r = w / cols * 16 + (lane >> 2);
-  if (r >= R) return;
-  const int i = src[r];
-  if (i < 0 || i >= N) return;
-  const T* from = x + (int64_t)((uint32_t)i / (uint32_t)k) * d;
-  const int c0 = ((int)(w % cols) * U * 4 + (lane & 3)) * V;
-  u32x4 v[U];
+  const int64_t r = w / cols * 16 + (lane >> 3);
+  int i[2];
 #pragma unroll
-  for (int u = 0; u < U; ++u)
-    if (c0 + u * 4 * V < d) v[u] = *reinterpret_cast<const u32x4*>(from + c0 + u * 4 * V);
-#pragma unroll
-  for (int u = 0; u < U; ++u)
-    if (c0 + u * 4 * V < d) *reinterpret_cast<u32x4*>(rows + ebuf_off<T>(r, c0 + u * 4 * V, d)) = v[u];
+  for (int h = 0; h < 2; ++h) {
+    i[h] = r + 8 * h < R ? src[r + 8 * h] : -1;
+    if (i[h] >= N) i[h] = -1;
+  }
+  gather_rows<T, U, S>(x, rows, r, i, d, k, ((int)(w % cols) * U * 8 + (lane & 7)) * Vec<T>::N);
+}
+
+// One tile of choices (a decode batch): every block places it for itself, a couple
+// of microseconds beside a launch and its wait, and moves its share of the rows;
+// block 0 writes what the caller keeps.
+template <typename T, int U>
+__global__ __launch_bounds__(kSortSmall) void sorted_small_kernel(const T* __restrict__ x, const int32_t* __restrict__ idx,
+                                                                  int N, int E, int align, int R, int32_t* row_begin,
+                                                                  int32_t* row_end, int32_t* slot, int32_t* src,
+                                                                  T* __restrict__ rows, int d, int k, int cols) {
+  constexpr int NT = kSortSmall;
+  __shared__ SortLds<NT> L;
+  __shared__ int16_t held[kSortRounds * NT + 15 * kSortMaxD + 16];   // the choice that a row holds
+  const bool first = blockIdx.x == 0;
+  sort_place<NT>(ExpertOf{idx, E}, [&](int64_t i, int at) {
+    if (first) slot[i] = at;
+    if (at >= 0) held[at] = (int16_t)i;
+  }, N, E, align, nullptr, 0, 1, L);
+  for (int e = threadIdx.x; e < E; e += NT) {
+    const int b = L.first[e], n = L.total[e];
+    if (first) {
+      row_begin[e] = b;
+      row_end[e] = b + n;
+    }
+    for (int r = b + n; r < b + (n + align - 1) / align * align; ++r) held[r] = -1;
+  }
+  __syncthreads();
+  const int used = L.used;
+  if (first)
+    for (int r = threadIdx.x; r < R; r += NT) src[r] = r < used ? held[r] : -1;
+  const int lane = threadIdx.x & 63;
+  for (int w = blockIdx.x * (NT / kWave) + (threadIdx.x >> 6); w / cols * 16 < used; w += gridDim.x * (NT / kWave)) {
+    const int r = w / cols * 16 + (lane >> 3);
+    const int i[2] = {r < used ? held[r] : -1, r + 8 < used ? held[r + 8] : -1};
+    gather_rows<T, U, false>(x, rows, r, i, d, k, (w % cols * U * 8 + (lane & 7)) * Vec<T>::N);
+  }
 }
 
 void launch_sorted_dispatch(const moe_sorted_cfg& c, const void* x, const int32_t* idx, int32_t* row_begin,
                             int32_t* row_end, int32_t* slot, int32_t* src, void* rows, void* ws, hipStream_t s) {
   const int64_t N = c.T * c.k, R = sorted_rows(c), tiles = std::max<int64_t>(1, sort_tiles(N));
+  const int align = c.dtype == MOE_BF16 ? 16 : 1;
   int32_t* counts = (int32_t*)ws;
-  if (tiles > 1)
-    hipLaunchKernelGGL(sorted_count_kernel, dim3((unsigned)tiles), dim3(kSortThreads), 0, s, idx, N, c.E, counts);
-  hipLaunchKernelGGL(sorted_place_kernel, dim3((unsigned)tiles), dim3(kSortThreads), 0, s, idx, N, c.E,
-                     c.dtype == MOE_BF16 ? 16 : 1, R, counts, row_begin, row_end, slot, src);
-  if (R == 0) return;
+  auto place = [&](auto nt) {
+    constexpr int NT = decltype(nt)::value;
+    if (tiles > 1)
+      hipLaunchKernelGGL(sorted_count_kernel<NT>, dim3((unsigned)tiles), dim3(NT), 0, s, idx, N, c.E, counts);
+    hipLaunchKernelGGL(sorted_place_kernel<NT>, dim3((unsigned)tiles), dim3(NT), 0, s, idx, N, c.E, align, R, counts, row_begin,
+                       row_end, slot, src);
+  };
   auto go = [&](auto tag) {
     using T = decltype(tag);
-    constexpr int U = 4;
-    const int cols = (c.d_model + U * 4 * Vec<T>::N - 1) / (U * 4 * Vec<T>::N);
+    constexpr int U = 1;
+    const int cols = (c.d_model + U * 8 * Vec<T>::N - 1) / (U * 8 * Vec<T>::N);
     const int64_t waves = (R + 15) / 16 * cols;
-    hipLaunchKernelGGL((sorted_gather_kernel<T, U>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, (const T*)x, src,
-                       (T*)rows, R, N, c.d_model, c.k, cols);
+    if (tiles == 1 && N > 0) {
+      const unsigned blocks = (unsigned)std::min<int64_t>(256, (waves + 3) / 4);
+      hipLaunchKernelGGL((sorted_small_kernel<T, U>), dim3(blocks), dim3(kSortSmall), 0, s, (const T*)x, idx, (int)N, c.E, align,
+                         (int)R, row_begin, row_end, slot, src, (T*)rows, c.d_model, c.k, cols);
+      return;
+    }
+    if (sort_threads(N) == kSortSmall) place(std::integral_constant<int, kSortSmall>{});
+    else place(std::integral_constant<int, kSortLarge>{});
+    auto gather = [&](auto stream) {
+      hipLaunchKernelGGL((sorted_gather_kernel<T, U, decltype(stream)::value>), dim3((unsigned)((waves + 3) / 4)), dim3(256),
+                         0, s, (const T*)x, src, (T*)rows, R, N, c.d_model, c.k, cols);
+    };
+    if (R == 0) return;
+    if (stream_bytes(R * c.d_model * (int64_t)sizeof(T))) gather(std::true_type{});
+    else gather(std::false_type{});
   };
   if (c.dtype == MOE_BF16) go(uint16_t{});
   else go(float{});
@@ -110,7 +186,7 @@ void launch_sorted_dispatch(const moe_sorted_cfg& c, const void* x, const int32_
 // W: y[t] = sum over r of w[t][r] rows[slot[t][r]] (combine).  Otherwise the sum
 // alone (the dispatch's gradient), G: plus sum over j of dlogits[t][j] Wg[j] (the
 // gate's).  Float sums in choice order; a thread owns 16 bytes of a token.
-template <typename T, bool W, bool G>
+template <typename T, bool W, bool G, bool S>
 __global__ __launch_bounds__(256) void sorted_back_kernel(const T* __restrict__ rows, const int32_t* __restrict__ slot,
                                                           const float* __restrict__ w, const T* __restrict__ Wg,
                                                           const float* __restrict__ dl, T* __restrict__ y,
@@ -159,25 +235,30 @@ __global__ __launch_bounds__(256) void sorted_back_kernel(const T* __restrict__ 
       for (int i = 0; i < V; ++i) acc[i] = fmaf(a, f[i], acc[i]);
     }
   }
-  Vec<T>::store(y + t * d + c, acc);
+  store16<S>(y + t * d + c, acc);
 }
 
 template <bool W>
 static void launch_back(const moe_sorted_cfg& c, const void* rows, const int32_t* slot, const float* w, const void* Wg,
                         const float* dl, void* y, hipStream_t s) {
   if (c.T == 0) return;
-  auto go = [&](auto tag, auto gate) {
+  auto go = [&](auto tag, auto gate, auto stream) {
     using T = decltype(tag);
     const int64_t n = c.T * (c.d_model / Vec<T>::N);
-    hipLaunchKernelGGL((sorted_back_kernel<T, W, decltype(gate)::value>), dim3((unsigned)((n + 255) / 256)), dim3(256), 0,
-                       s, (const T*)rows, slot, w, (const T*)Wg, dl, (T*)y, c.T, sorted_rows(c), c.d_model, c.k, c.E);
+    hipLaunchKernelGGL((sorted_back_kernel<T, W, decltype(gate)::value, decltype(stream)::value>),
+                       dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, (const T*)rows, slot, w, (const T*)Wg, dl, (T*)y,
+                       c.T, sorted_rows(c), c.d_model, c.k, c.E);
   };
-  auto type = [&](auto gate) {
-    if (c.dtype == MOE_BF16) go(uint16_t{}, gate);
-    else go(float{}, gate);
+  auto type = [&](auto gate, auto stream) {
+    if (c.dtype == MOE_BF16) go(uint16_t{}, gate, stream);
+    else go(float{}, gate, stream);
   };
-  if (Wg) type(std::true_type{});
-  else type(std::false_type{});
+  auto gated = [&](auto stream) {
+    if (Wg) type(std::true_type{}, stream);
+    else type(std::false_type{}, stream);
+  };
+  if (stream_bytes(c.T * c.d_model * (c.dtype == MOE_BF16 ? 2 : 4))) gated(std::true_type{});
+  else gated(std::false_type{});
 }
 
 void launch_sorted_combine(const moe_sorted_cfg& c, const void* O, const int32_t* slot, const float* w, void* y,
@@ -191,10 +272,10 @@ void launch_sorted_dispatch_bwd(const moe_sorted_cfg& c, const int32_t* slot, co
 
 // ------------------------------------------------------------ combine backward
 // dO[row] = w dy[t], dw = <dy[t], O[row]> for the choice that the row holds.  A
-// block takes sixteen rows, each wave a run of columns of all of them (four lanes
+// block takes sixteen rows, each wave a run of columns of all of them (eight lanes
 // a row, as in the gather); the waves' dot products meet in LDS, in wave order.
 // The blocks past the rows write the zeros of the choices that have none.
-template <typename T, int U>
+template <typename T, int U, bool S>
 __global__ __launch_bounds__(256) void sorted_combine_bwd_kernel(const T* __restrict__ O, const int32_t* __restrict__ slot,
                                                                  const int32_t* __restrict__ src,
                                                                  const float* __restrict__ w, const T* __restrict__ dy,
@@ -209,44 +290,57 @@ __global__ __launch_bounds__(256) void sorted_combine_bwd_kernel(const T* __rest
     return;
   }
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t r = (int64_t)blockIdx.x * 16 + (lane >> 2);
-  int i = r < R ? src[r] : -1;
-  if (i >= N) i = -1;
-  float dot = 0.f;
-  if (i >= 0) {
-    const float wr = w[i];
-    const T* g = dy + (int64_t)((uint32_t)i / (uint32_t)k) * d;
-    const T* o = O + r * d;
-    for (int c0 = (wave * U * 4 + (lane & 3)) * V; c0 < d; c0 += 4 * U * 4 * V) {
-      u32x4 a[U], b[U];
+  const int64_t r0 = (int64_t)blockIdx.x * 16 + (lane >> 3);
+  int i[2];
+  float wr[2], dot[2];
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (c0 + u * 4 * V < d) {
-          a[u] = *reinterpret_cast<const u32x4*>(g + c0 + u * 4 * V);
-          b[u] = *reinterpret_cast<const u32x4*>(o + c0 + u * 4 * V);
-        }
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (c0 + u * 4 * V < d) {
-          float p[V], q[V];
-          Vec<T>::load(&a[u], p);
-          Vec<T>::load(&b[u], q);
-#pragma unroll
-          for (int j = 0; j < V; ++j) {
-            dot = fmaf(p[j], q[j], dot);
-            p[j] *= wr;
-          }
-          Vec<T>::store(dO + ebuf_off<T>(r, c0 + u * 4 * V, d), p);
-        }
-    }
+  for (int h = 0; h < 2; ++h) {
+    i[h] = r0 + 8 * h < R ? src[r0 + 8 * h] : -1;
+    if (i[h] >= N) i[h] = -1;
+    wr[h] = i[h] >= 0 ? w[i[h]] : 0.f;
+    dot[h] = 0.f;
   }
-  dot += __shfl_xor(dot, 1, kWave);
-  dot += __shfl_xor(dot, 2, kWave);
-  if ((lane & 3) == 0) part[wave][lane >> 2] = dot;
+  for (int c0 = (wave * U * 8 + (lane & 7)) * V; c0 < d; c0 += 4 * U * 8 * V) {
+    u32x4 a[2][U], b[2][U];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      if (i[h] >= 0) {
+        const T *g = dy + (int64_t)((uint32_t)i[h] / (uint32_t)k) * d, *o = O + (r0 + 8 * h) * d;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (c0 + u * 8 * V < d) {
+            a[h][u] = *reinterpret_cast<const u32x4*>(g + c0 + u * 8 * V);
+            b[h][u] = *reinterpret_cast<const u32x4*>(o + c0 + u * 8 * V);
+          }
+      }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      if (i[h] >= 0)
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (c0 + u * 8 * V < d) {
+            float p[V], q[V];
+            Vec<T>::load(&a[h][u], p);
+            Vec<T>::load(&b[h][u], q);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+              dot[h] = fmaf(p[j], q[j], dot[h]);
+              p[j] *= wr[h];
+            }
+            store16<S>(dO + ebuf_off<T>(r0 + 8 * h, c0 + u * 8 * V, d), p);
+          }
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) dot[h] += __shfl_xor(dot[h], o, kWave);
+    if ((lane & 7) == 0) part[wave][8 * h + (lane >> 3)] = dot[h];
+  }
   __syncthreads();
-  if (wave == 0 && (lane & 3) == 0 && i >= 0) {
-    const int q = lane >> 2;
-    dw[i] = ((part[0][q] + part[1][q]) + part[2][q]) + part[3][q];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int q = 8 * h + (lane >> 3);
+    if (wave == 0 && (lane & 7) == 0 && i[h] >= 0) dw[i[h]] = ((part[0][q] + part[1][q]) + part[2][q]) + part[3][q];
   }
 }
 
@@ -254,13 +348,18 @@ void launch_sorted_combine_bwd(const moe_sorted_cfg& c, const void* O, const int
                                const float* w, const void* dy, void* dO, float* dw, hipStream_t s) {
   const int64_t N = c.T * c.k, R = sorted_rows(c);
   if (N == 0) return;
-  auto go = [&](auto tag) {
+  auto go = [&](auto tag, auto stream) {
     using T = decltype(tag);
-    hipLaunchKernelGGL((sorted_combine_bwd_kernel<T, 4>), dim3((unsigned)((R + 15) / 16 + (N + 255) / 256)), dim3(256), 0,
-                       s, (const T*)O, slot, src, w, (const T*)dy, (T*)dO, dw, R, N, c.d_model, c.k);
+    hipLaunchKernelGGL((sorted_combine_bwd_kernel<T, 2, decltype(stream)::value>),
+                       dim3((unsigned)((R + 15) / 16 + (N + 255) / 256)), dim3(256), 0, s, (const T*)O, slot, src, w,
+                       (const T*)dy, (T*)dO, dw, R, N, c.d_model, c.k);
   };
-  if (c.dtype == MOE_BF16) go(uint16_t{});
-  else go(float{});
+  auto type = [&](auto stream) {
+    if (c.dtype == MOE_BF16) go(uint16_t{}, stream);
+    else go(float{}, stream);
+  };
+  if (stream_bytes(R * c.d_model * (c.dtype == MOE_BF16 ? 2 : 4))) type(std::true_type{});
+  else type(std::false_type{});
 }
 
 }  // namespace lmoe

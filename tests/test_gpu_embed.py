@@ -34,7 +34,8 @@ def _ids(T, V, how, g):
 CASES = [(1, 1, 8, "plain"), (1, 50257, 64, "plain"), (3, 2, 24, "none"), (31, 7, 64, "same"), (32, 7, 64, "same"),
          (33, 7, 64, "same"), (15, 5, 64, "same"), (16, 5, 64, "same"), (17, 5, 64, "same"), (272, 1, 520, "same"),
          (2000, 3, 64, "plain"), (160, 10, 24, "runs"), (64, 511, 8, "plain"), (320, 10, 72, "runs"), (500, 512, 136, "zipf"), (1111, 10007, 640, "padded"),
-         (4096, 513, 64, "zipf"), (4097, 300000, 64, "plain"), (5000, 262144, 16, "zipf"), (20000, 3, 8, "plain"),
+         (4096, 513, 64, "zipf"), (4097, 300000, 64, "plain"), (8192, 5000, 32, "zipf"), (8193, 5000, 32, "zipf"), (16384, 50257, 16, "zipf"), (16385, 50257, 16, "padded"), (65536, 70000, 16, "plain"),
+         (65537, 511, 16, "zipf"), (5000, 262144, 16, "zipf"), (20000, 3, 8, "plain"),
          (9000, 40, 2048, "same"), (70000, 1000, 32, "zipf"), (12345, 131071, 264, "padded")]
 
 

@@ -43,7 +43,8 @@ def _ws(cfg, *calls):
 
 CASES = [(1, 64, 1, 1, "plain"), (1, 128, 16, 2, "plain"), (1, 64, 8, 2, "none"), (7, 64, 512, 16, "plain"),
          (48, 192, 16, 2, "plain"), (93, 64, 3, 16, "twice"), (257, 320, 64, 2, "dropped"), (300, 64, 5, 1, "one"),
-         (2048, 64, 8, 2, "plain"), (4097, 64, 512, 1, "plain"), (1366, 128, 160, 6, "dropped"),
+         (2048, 64, 8, 2, "plain"), (64, 64, 512, 16, "plain"), (65, 64, 512, 16, "twice"), (1023, 192, 7, 1, "dropped"),
+         (512, 256, 300, 2, "plain"), (70000, 64, 16, 1, "plain"), (4097, 64, 512, 1, "plain"), (1366, 128, 160, 6, "dropped"),
          (9000, 64, 33, 3, "one"), (6000, 64, 2, 2, "twice"), (3000, 64, 512, 8, "dropped")]
 
 

@@ -101,8 +101,8 @@ def test_rows_and_workspaces():
     assert L.moe_sorted_rows(_sorted(T=0)) == 0
     assert L.moe_sorted_rows(_sorted(T=1, E=512, k=1)) == 16
     assert L.moe_sorted_rows(_sorted(T=1000, dtype="f32")) == 2000
-    assert L.moe_sorted_workspace_bytes(_sorted(T=2048), L.MOE_CALL_DISPATCH) == 0
-    assert L.moe_sorted_workspace_bytes(_sorted(T=2049), L.MOE_CALL_DISPATCH) > 0
+    assert L.moe_sorted_workspace_bytes(_sorted(T=512), L.MOE_CALL_DISPATCH) == 0
+    assert L.moe_sorted_workspace_bytes(_sorted(T=513), L.MOE_CALL_DISPATCH) > 0
     assert L.moe_sorted_workspace_bytes(_sorted(), L.MOE_CALL_DISPATCH_BPR) == 0 and L.moe_last_error()
 
 
@@ -241,8 +241,8 @@ def test_xent_workspaces_stay_small():
     """Beside copies of x and of a piece of W, the forward keeps an eighth of a byte for each
     logit, and the backward never holds the whole vocabulary's gradient of many tokens."""
     c = _xent(T=16384, V=50257, d_model=2048)
-    assert L.moe_xent_workspace_bytes(c, 0) <= 16384 * (50257 / 8 + 100) + 16384 * 2048 * 2 + (128 << 20)
-    assert L.moe_xent_workspace_bytes(c, 1) <= (512 << 20) + 16384 * 2048 * (4 + 2 + 2) + 4096
+    assert L.moe_xent_workspace_bytes(c, 0) <= 16384 * (50257 / 8 + 2 * 128) + 16384 * 2048 * 2 + (128 << 20)
+    assert L.moe_xent_workspace_bytes(c, 1) <= (512 << 20) + 16384 * 2048 * (4 + 2 + 2) + 65536
     assert L.moe_xent_workspace_bytes(_xent(T=0), 1) == 0
 
 
