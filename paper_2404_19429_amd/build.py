@@ -21,7 +21,8 @@ LIB = os.path.join(PKG, "liblancet_moe.so")
 BIND = os.path.join(PKG, "_bind.so")   # the native argument marshalling (a Python extension module)
 SOURCES = ["api.cpp", "block.cpp", "plan.cpp", "gate.hip", "route.hip", "gemm.hip", "gemm_256x256.hip",
            "gemm_192x256.hip", "gemm_128x128.hip", "gemm_64x128.hip", "gemm_64x64.hip", "attn.hip", "norm.hip",
-           "router.hip", "experts_w4.hip", "ckpt.hip", "sorted.hip", "embed.hip", "xent.hip"]
+           "router.hip", "experts_w4.hip", "ckpt.hip", "sorted.hip", "embed.hip", "xent.hip", "gemm_rows_256x256.hip",
+           "gemm_rows_192x256.hip", "gemm_rows_128x128.hip", "gemm_rows_64x128.hip", "gemm_rows_64x64.hip"]
 ARCH = "gfx950"
 
 HIPCC_FLAGS = [
@@ -54,7 +55,8 @@ def _compile(src: str, verbose: bool) -> str:
 
 # kernels that read LDS through inline asm
 ASM_READ_SOURCES = ["gemm_256x256.hip", "gemm_192x256.hip", "gemm_128x128.hip", "gemm_64x128.hip", "gemm_64x64.hip",
-                    "attn.hip"]
+                    "gemm_rows_256x256.hip", "gemm_rows_192x256.hip", "gemm_rows_128x128.hip", "gemm_rows_64x128.hip",
+                    "gemm_rows_64x64.hip", "attn.hip"]
 
 
 def _check_isa(src: str, verbose: bool) -> None:

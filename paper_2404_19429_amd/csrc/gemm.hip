@@ -102,7 +102,7 @@ struct F32Tile {
 };
 
 template <int EPI>
-__device__ __forceinline__ void f32_store(const GemmParams& p, int64_t off, const f32x4& v) {
+__device__ __forceinline__ void f32_store(const KernParams<EPI>& p, int64_t off, const f32x4& v) {
   f32x4 o = v;
   if constexpr (EPI == EPI_DACT) {
     const f32x4 h = *reinterpret_cast<const f32x4*>((const float*)p.Aux + off);
@@ -126,7 +126,7 @@ __device__ __forceinline__ void f32_store(const GemmParams& p, int64_t off, cons
 // Ragged-K (tiles as long as their group): rows of tn tiles are dealt to the
 // XCDs in turn, so a few large experts still spread over the chip.
 template <int WT, bool B_K, bool RAGGED_K, int EPI>
-__global__ __launch_bounds__(256) void gemm_f32_kernel(GemmParams p, int tm, int tn, int groups) {
+__global__ __launch_bounds__(256) void gemm_f32_kernel(KernParams<EPI> p, int tm, int tn, int groups) {
   using TA = F32Tile<WT, !RAGGED_K>;
   using TB = F32Tile<WT, B_K && !RAGGED_K>;
   constexpr int BM = TA::ROWS, BK = TA::BK;
@@ -157,7 +157,9 @@ __global__ __launch_bounds__(256) void gemm_f32_kernel(GemmParams p, int tm, int
   // with W may be in groups, each a slice of p.ksplit classes.
   const int k0g = EPI == EPI_ADD ? g * p.ksplit : 0;
   const int Mlim = RAGGED_K ? p.M : span, Klim = RAGGED_K ? span : EPI == EPI_ADD ? min(p.ksplit, p.K - k0g) : p.K;
-  const int Alim = RAGGED_K ? (Mlim + 3) & ~3 : Mlim, Blim = EPI == EPI_DL ? p.x.cols : p.N;
+  const int Alim = RAGGED_K ? (Mlim + 3) & ~3 : Mlim;
+  int Blim = p.N;
+  if constexpr (EPI == EPI_DL) Blim = p.x.cols;
   const int KlimB = EPI == EPI_ADD ? min(p.ksplit, p.M - k0g) : Klim;
   if (m0 >= Mlim) return;
   const float* Ab = (const float*)p.A + g * p.sA + (int64_t)lo * p.lda;
@@ -241,7 +243,7 @@ __global__ __launch_bounds__(256) void gemm_f32_kernel(GemmParams p, int tm, int
 }
 
 template <int WT, bool B_K, bool RAGGED_K, int EPI>
-static void launch_f32(const GemmParams& p, int groups, int64_t rows, int cols, hipStream_t s, int64_t all_rows = 0) {
+static void launch_f32(const KernParams<EPI>& p, int groups, int64_t rows, int cols, hipStream_t s, int64_t all_rows = 0) {
   // (ragged-M: with up to 15 alignment rows, as wide_tile_prefix counts them; all_rows: the groups' rows together
   // are at most so many)
   const int tm = (int)((rows + (RAGGED_K ? 0 : 15) + 32 * WT - 1) / (32 * WT)), tn = (cols + 32 * WT - 1) / (32 * WT);
@@ -279,13 +281,14 @@ struct TileCost {
   int bm, bn, per_cu;   // per_cu: blocks of this shape on a CU, so a round is per_cu tiles per CU
   double full, part, store;
   void (*run)(const WideCall&, hipStream_t);
+  void (*run_rows)(const WideCall&, hipStream_t);
   int wtn;              // columns of a wave's tile
 };
-static const TileCost kTilesM[] = {{256, 256, 1, 650., 650., 8000., run_wide_256x256, 64},
-                                   {192, 256, 1, 560., 560., 7000., run_wide_192x256, 64},
-                                   {128, 128, 2, 520., 330., 4500., run_wide_128x128, 64},
-                                   {64, 128, 2, 390., 230., 3000., run_wide_64x128, 64},
-                                   {64, 64, 2, 300., 190., 2000., run_wide_64x64, 32}};
+static const TileCost kTilesM[] = {{256, 256, 1, 650., 650., 8000., run_wide_256x256, run_rows_256x256, 64},
+                                   {192, 256, 1, 560., 560., 7000., run_wide_192x256, run_rows_192x256, 64},
+                                   {128, 128, 2, 520., 330., 4500., run_wide_128x128, run_rows_128x128, 64},
+                                   {64, 128, 2, 390., 230., 3000., run_wide_64x128, run_rows_64x128, 64},
+                                   {64, 64, 2, 300., 190., 2000., run_wide_64x64, run_rows_64x64, 32}};
 constexpr int kTileCount = sizeof kTilesM / sizeof kTilesM[0];
 static double tile_cost(const TileCost& t, const WideCall& w, int cus) {
   // M-tiles of a group: a mean over the routed rows' spread.
@@ -375,15 +378,17 @@ static TileK tile_k(const WideCall& w, int cus) {
 }
 static void run_wide_any(const WideCall& w, hipStream_t s) {
   if (w.rows <= 0 || w.cols <= 0 || w.groups <= 0) return;
-  WideCall q = w;
-  if (q.p.eA == 0) q.p.eA = q.p.sA;
-  if (q.p.eB == 0) q.p.eB = q.p.sB;
-  if (w.kind < WK_DW) return kTilesM[tile_m(w, num_cus())].run(q, s);
+  const bool rows = w.shared || (w.kind >= WK_LSE && w.kind < WK_DW);
+  if (w.kind < WK_DW) {
+    const TileCost& t = kTilesM[tile_m(w, num_cus())];
+    return (rows ? t.run_rows : t.run)(w, s);
+  }
   const TileK t = tile_k(w, num_cus());
+  WideCall q = w;
   q.p.only = t == kTileKByRows ? 1 : 0;
-  if (t != kTileK128) run_wide_256x256(q, s);
+  if (t != kTileK128) (rows ? run_rows_256x256 : run_wide_256x256)(q, s);
   q.p.only = t == kTileKByRows ? 2 : 0;
-  if (t != kTileK256) run_wide_128x128(q, s);
+  if (t != kTileK256) (rows ? run_rows_128x128 : run_wide_128x128)(q, s);
 }
 
 // Rows a group is expected to hold, and their standard deviation: the call's
@@ -575,7 +580,7 @@ void launch_expert_bwd_dw(const moe_cfg& c, const void* X, const void* A, const 
 
 // ------------------------------------------------- experts over sorted rows
 // The same products over one buffer of rows that the experts share (moe_sorted_*):
-// groups without a stride, each on its range of rows, which in bf16 starts at a
+// groups without a stride (SharedRows), each on its range of rows, which in bf16 starts at a
 // 16-row block; up to kMaxE experts a launch.
 namespace {
 struct Part {   // experts [e0, e0 + n) of a call
@@ -598,7 +603,8 @@ void run_sorted(const moe_sorted_cfg& c, const Part& part, int prod, WideKind ki
   p.rb += part.e0;
   p.re += part.e0;
   const double expect = (double)c.T * c.k / c.E;
-  const WideCall w{kind, c.act, part.n, rows, cols, expect, std::sqrt(expect * (1. - (double)c.k / c.E)), p};
+  WideCall w{kind, c.act, part.n, rows, cols, expect, std::sqrt(expect * std::max(0., 1. - (double)c.k / c.E)), p};
+  w.shared = true;
   const bool tb = ptimer_begin(prod, s);
   if (c.dtype == MOE_BF16) {
     run_wide_any(w, s);
@@ -627,12 +633,10 @@ void launch_sorted_fwd(const moe_sorted_cfg& c, const void* X, const int32_t* rb
   if (R == 0) return;
   each_part(c, [&](const Part& q) {
     GemmParams p{X, d, 0, mat(c, W1, q.e0, f * d), d, f * d, H, f, 0, A, nullptr, rb, re, 0, (int)f, (int)d};
-    p.eA = R * d;
     run_sorted<true, false, EPI_FWD1>(c, q, kProdFwd1, WK_FWD1, p, R, (int)f, ws, s);
   });
   each_part(c, [&](const Part& q) {
     GemmParams p{A, f, 0, mat(c, W2, q.e0, d * f), f, d * f, O, d, 0, nullptr, nullptr, rb, re, 0, (int)d, (int)f};
-    p.eA = R * f;
     run_sorted<true, false, EPI_STORE>(c, q, kProdFwd2, WK_NK, p, R, (int)d, ws, s);
   });
 }
@@ -643,12 +647,10 @@ void launch_sorted_bwd_dx(const moe_sorted_cfg& c, const int32_t* rb, const int3
   if (R == 0) return;
   each_part(c, [&](const Part& q) {
     GemmParams p{dO, d, 0, mat(c, W2, q.e0, d * f), f, d * f, dH, f, 0, nullptr, H, rb, re, 0, (int)f, (int)d};
-    p.eA = R * d;
     run_sorted<false, false, EPI_DACT>(c, q, kProdDA, WK_DACT, p, R, (int)f, ws, s);
   });
   each_part(c, [&](const Part& q) {
     GemmParams p{dH, f, 0, mat(c, W1, q.e0, f * d), d, f * d, dXe, d, 0, nullptr, nullptr, rb, re, 0, (int)d, (int)f};
-    p.eA = R * f;
     run_sorted<false, false, EPI_STORE>(c, q, kProdDXe, WK_KN, p, R, (int)d, ws, s);
   });
 }
@@ -659,14 +661,10 @@ void launch_sorted_bwd_dw(const moe_sorted_cfg& c, const int32_t* rb, const int3
   const WideKind kind = c.wpacked && c.dtype == MOE_BF16 ? WK_DW_BLK : WK_DW;
   each_part(c, [&](const Part& q) {
     GemmParams p{dO, d, 0, A, f, 0, (void*)mat(c, dW2, q.e0, d * f), f, d * f, nullptr, nullptr, rb, re, (int)d, (int)f};
-    p.eA = R * d;
-    p.eB = R * f;
     run_sorted<false, true, EPI_STORE>(c, q, kProdDW2, kind, p, d, (int)f, nullptr, s);
   });
   each_part(c, [&](const Part& q) {
     GemmParams p{dH, f, 0, X, d, 0, (void*)mat(c, dW1, q.e0, f * d), d, f * d, nullptr, nullptr, rb, re, (int)f, (int)d};
-    p.eA = R * f;
-    p.eB = R * d;
     run_sorted<false, true, EPI_STORE>(c, q, kProdDW1, kind, p, f, (int)d, nullptr, s);
   });
 }
@@ -675,9 +673,9 @@ void launch_sorted_bwd_dw(const moe_sorted_cfg& c, const int32_t* rb, const int3
 // Logits over a piece of the vocabulary (see XentParams), and the products of the
 // gradient at them.  bf16: the wide kernel, W (and in the forward x) as the caller has
 // it, row-major, x in the backward and dl blocked; float: the float kernel, row-major.
-static GemmParams xent_params(int64_t T, int N, int K, const void* A, int64_t lda, int64_t eA, const void* B, int64_t ldb,
-                              int64_t eB, void* C, int64_t ldc) {
-  GemmParams p{A, lda, eA, B, ldb, eB, C, ldc, 0, nullptr, nullptr, nullptr, nullptr, 0, N, K, 0, (int)T};
+static GemmParams xent_params(int64_t T, int N, int K, const void* A, int64_t lda, int64_t sA, const void* B, int64_t ldb,
+                              int64_t sB, void* C, int64_t ldc) {
+  GemmParams p{A, lda, sA, B, ldb, sB, C, ldc, 0, nullptr, nullptr, nullptr, nullptr, 0, N, K, 0, (int)T};
   return p;
 }
 static WideCall xent_call(WideKind kind, int64_t T, int cols, const GemmParams& p) {
@@ -706,20 +704,18 @@ static int launch_lse_part(int dtype, int form, int64_t T, int d, const void* x,
                            hipStream_t s) {
   GemmParams p = xent_params(T, xp.cols, d, x, d, form >= kXentX ? pad16(T) * d : T * d, W, d,
                              (form == kXentBlocked ? pad16(xp.cols) : (int64_t)xp.cols) * d, nullptr, 0);
-  p.x = xp;
   WideCall w = xent_call(form == kXentBlocked ? WK_LSE_BLK : form == kXentX ? WK_LSE_X : WK_LSE, T, xp.cols, p);
+  w.x = xp;
   if (dtype == MOE_BF16) {
-    w.p.eA = w.p.sA;
-    w.p.eB = w.p.sB;
     const TileCost& t = kTilesM[tile_m(w, num_cus(), T <= kXentNarrow ? kTileCount : kTileCount - 1)];
-    t.run(w, s);
+    t.run_rows(w, s);
     return (xp.cols + t.bn - 1) / t.bn * (t.bn / t.wtn);
   }
   if (T <= kXentNarrow && f32_tile(w, num_cus()) == 32) {
-    launch_f32<1, true, false, EPI_LSE>(p, 1, T, xp.cols, s);
+    launch_f32<1, true, false, EPI_LSE>(XentGemmParams{p, xp}, 1, T, xp.cols, s);
     return (xp.cols + 31) / 32 * 2;
   }
-  launch_f32<2, true, false, EPI_LSE>(p, 1, T, xp.cols, s);
+  launch_f32<2, true, false, EPI_LSE>(XentGemmParams{p, xp}, 1, T, xp.cols, s);
   return (xp.cols + 63) / 64 * 2;
 }
 // Returns the runs of columns written from xp.block0 on.
@@ -746,24 +742,24 @@ void launch_xent_dl(int dtype, int form, int64_t T, int d, const void* x, const 
                     int ld, hipStream_t s) {
   auto extent = [&](int cols) { return (form == kXentBlocked ? pad16(cols) : (int64_t)cols) * d; };
   GemmParams p = xent_params(T, ld, d, x, d, pad16(T) * d, W, d, extent(xp.cols), dl, ld);
-  p.x = xp;
   WideCall w = xent_call(form == kXentBlocked ? WK_DL_BLK : WK_DL, T, ld, p);
+  w.x = xp;
   if (dtype != MOE_BF16) {
-    if (f32_tile(w, num_cus()) == 32) launch_f32<1, true, false, EPI_DL>(p, 1, T, ld, s);
-    else launch_f32<2, true, false, EPI_DL>(p, 1, T, ld, s);
+    if (f32_tile(w, num_cus()) == 32) launch_f32<1, true, false, EPI_DL>(XentGemmParams{p, xp}, 1, T, ld, s);
+    else launch_f32<2, true, false, EPI_DL>(XentGemmParams{p, xp}, 1, T, ld, s);
     return;
   }
   const int main = whole_rounds(w, num_cus());
   if (main < w.cols) {   // (the columns left, in a dl that begins further right: 32 columns are a block)
     WideCall b = w;
     b.cols = b.p.N = ld - main;
-    b.p.x.col0 += main;
-    b.p.x.cols -= main;
+    b.x.col0 += main;
+    b.x.cols -= main;
     b.p.B = (const uint16_t*)W + (int64_t)main * d;
-    b.p.sB = extent(b.p.x.cols);
+    b.p.sB = extent(b.x.cols);
     b.p.C = (uint16_t*)dl + (int64_t)main / 32 * 512;
     run_wide_any(b, s);
-    w.cols = w.p.N = w.p.x.cols = main;
+    w.cols = w.p.N = w.x.cols = main;
     w.p.sB = extent(main);
   }
   run_wide_any(w, s);
@@ -836,9 +832,7 @@ void launch_xent_dx_whole(int64_t T, int d, int cols, const void* dl, int ld, co
   WideCall w = xent_call(WK_KN_RM, T, d, p);
   if (4 * large <= num_cus()) {
     w.p.ksplit = 2;
-    w.p.eA = p.sA;
-    w.p.eB = p.sB;
-    return run_wide_256x256(w, s);
+    return run_rows_256x256(w, s);
   }
   run_wide_any(w, s);
 }
@@ -861,7 +855,7 @@ void launch_xent_dw(int dtype, int64_t T, int d, int cols, const void* dl, int l
     WideCall b = w;
     b.rows = b.p.M = cols - (int)main;
     b.p.A = (const uint16_t*)dl + main / 32 * 512;
-    b.p.eA = p.sA - main / 32 * 512;
+    b.p.sA = p.sA - main / 32 * 512;
     b.p.C = (uint16_t*)dW + main * d;
     run_wide_any(b, s);
     w.rows = w.p.M = (int)main;

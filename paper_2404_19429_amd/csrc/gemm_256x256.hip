@@ -3,7 +3,7 @@
 
 namespace lmoe {
 
-using Tile = Wide<256, 256, 8, 4, 1, 4, 5, 2, true>;
+using Tile = Tile256;
 
 void run_wide_256x256(const WideCall& w, hipStream_t s) {
   if (w.kind < WK_DW) run_wide_m<Tile>(w, s);

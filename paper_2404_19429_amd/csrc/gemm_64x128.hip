@@ -7,7 +7,7 @@ namespace lmoe {
 // latency, barrier and scalar work, so two K halves share one (expert_out of
 // 1531 tokens, d_model 768, 8 experts: 32 -> 26 us; a step of 32 K with more
 // stages or one barrier per two steps measured no faster).
-using Tile = Wide<64, 128, 4, 2, 2, 3, 3, 2, false>;
+using Tile = Tile64x128;
 
 void run_wide_64x128(const WideCall& w, hipStream_t s) { run_wide_m<Tile>(w, s); }
 

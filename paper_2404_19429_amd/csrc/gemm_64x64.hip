@@ -3,7 +3,7 @@
 
 namespace lmoe {
 
-using Tile = Wide<64, 64, 4, 2, 2, 4, 4, 2, false>;
+using Tile = Tile64;
 
 void run_wide_64x64(const WideCall& w, hipStream_t s) { run_wide_m<Tile>(w, s); }
 

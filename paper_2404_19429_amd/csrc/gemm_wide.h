@@ -54,10 +54,17 @@ struct GemmParams {
                     // one, on every CU (few tiles, a long K)
   int kchunk;       // rb == re == NULL and kchunk > 0: group g's rows are [g kchunk, (g + 1) kchunk)
   int only;         // ragged-K: 1 = run only if the groups are even, 2 = only if they are skewed, 0 = always
-  int64_t eA, eB;   // elements that a group's operand spans from its start (run_wide_any: sA, sB where 0; groups
-                    // that share one buffer have a stride of 0 and its extent)
+};
+struct XentGemmParams : GemmParams {
   XentParams x;
 };
+// (A kernel takes no more arguments than it reads: 80 bytes more cost the smallest products about 1 %.)
+template <int EPI> struct KernParamsOf { using type = GemmParams; };
+template <> struct KernParamsOf<EPI_LSE> { using type = XentGemmParams; };
+template <> struct KernParamsOf<EPI_DL> { using type = XentGemmParams; };
+// (A kernel's signature goes into its name, which host and device have to spell alike: no unnamed type, so no
+// expression of the enumerators above, may be in it.)
+template <int EPI> using KernParams = typename KernParamsOf<EPI>::type;
 
 // Row range of group g, clamped to the buffer so bad ranges cannot reach outside it.
 __device__ __forceinline__ void group_rows(const GemmParams& p, int g, int& lo, int& span) {
@@ -256,11 +263,20 @@ struct Wide {
   static constexpr int stages(bool b_k) { return b_k ? STB : STT; }
   static constexpr bool pair(bool b_k) { return stages(b_k) >= 5; }
   static constexpr bool KSPLIT = KSPLIT_;
+  static constexpr bool SHARED = false;
   static constexpr size_t lds_bytes(bool b_k) { return (size_t)stages(b_k) * STAGE * sizeof(uint16_t); }
   static constexpr int per_cu(bool b_k) {                 // blocks resident on a CU
     return (int)std::min<size_t>(4 * WPE / NW, (size_t)160 * 1024 / lds_bytes(b_k));
   }
 };
+
+// The tile for groups that share one buffer of rows (the row operands' group stride
+// is 0): its extent is not the stride, and the descriptors span all that an offset
+// reaches -- a lane's row is checked against the buffer's rows or its group's
+// anyway.  A kernel of its own: with the extent as one more argument the plain-store
+// products of 15 to 30 us took 2 % longer.
+template <class TC> struct SharedRows : TC { static constexpr bool SHARED = true; };
+constexpr int64_t kSharedExtent = (int64_t)1 << 30;
 
 // Immediate byte offset of fragment read r from its base (see read_base in the
 // kernel): K-contiguous fragment r sits r KB on; an MN-contiguous half r % 2
@@ -334,9 +350,9 @@ constexpr int kBufCfg = 0x00020000;   // buffer descriptor word 3: raw 32-bit da
 constexpr uint32_t kOob = 0x80000000u;
 // RM: the operand is row-major ([K][ld]; K-contiguous: [ROWS][ld]) instead of
 // blocked; a lane loads the same 16-byte chunk (row, 8 columns) that it would take
-// from the blocked layout, so the stage's LDS layout is the same.  A row-major
-// MN-contiguous operand may end before K does (a descriptor past its end is empty).
-template <bool KC, bool KCHK, int NW, int ROWS, bool RM = false>
+// from the blocked layout, so the stage's LDS layout is the same.  END: the operand
+// may end before K does (a descriptor past its end is empty).
+template <bool KC, bool KCHK, int NW, int ROWS, bool RM = false, bool END = false>
 struct WOp {
   static constexpr int kWNI = ROWS / 16 / NW;   // loads per wave per stage (1 KB blocks)
   const char* base;      // the group's operand (uniform)
@@ -383,7 +399,7 @@ struct WOp {
     }
   }
   // Bytes of the operand from `adv` on.
-  __device__ __forceinline__ int left(uint32_t adv) const { return RM && !KC && adv > bytes ? 0 : (int)(bytes - adv); }
+  __device__ __forceinline__ int left(uint32_t adv) const { return END && adv > bytes ? 0 : (int)(bytes - adv); }
   // Load i (0 .. kWNI-1) of K-step kk into its place in the stage.
   __device__ __forceinline__ void issue(int i, int kk, uint16_t* stage, int wid) const {
     const uint32_t adv = (uint32_t)kk * stride;
@@ -576,7 +592,7 @@ __device__ __forceinline__ WRange wide_range(const WPrefix& P, int xcd) {
 // acc[i][j] holds output row 16 i + l % 16, columns 16 j + 4 (l / 16) .. +3 of
 // the wave tile at (G.m0 + wm WTM, G.n0 + wn WTN).
 template <int FM, int FN, int WTM, int WTN, int BN, bool RAGGED_K, int EPI, int ACT, bool CBLK>
-__device__ __forceinline__ void wide_epilogue(const GemmParams& p, const WGeo& G, f32x4 (&acc)[FM][FN], int wm,
+__device__ __forceinline__ void wide_epilogue(const KernParams<EPI>& p, const WGeo& G, f32x4 (&acc)[FM][FN], int wm,
                                               int wn, int lane, int i_lo = 0, int i_hi = FM) {
   if constexpr (EPI == EPI_LSE) {
     constexpr int WGN = BN / WTN;
@@ -744,7 +760,7 @@ __device__ __forceinline__ void wide_epilogue(const GemmParams& p, const WGeo& G
 // ARM, BRM: a ragged-M product's A (K-contiguous), B operand is row-major.
 template <class TC, bool B_K, bool RAGGED_K, int EPI, int ACT, bool CBLK, bool ARM = false, bool BRM = false>
 __global__ __attribute__((amdgpu_flat_work_group_size(TC::NW * 64, TC::NW * 64), amdgpu_waves_per_eu(TC::WPE, TC::WPE))) void
-gemm_wide_kernel(GemmParams p, int tilesM, int tilesN, int groups) {
+gemm_wide_kernel(KernParams<EPI> p, int tilesM, int tilesN, int groups) {
   constexpr int BK = TC::BK, SUB = TC::SUB, HALF = TC::HALF;
   constexpr int BM = TC::BM, BN = TC::BN, BMT = TC::BMT, NW = TC::NW, WGN = TC::WGN;
   constexpr int WTM = TC::WTM, WTN = TC::WTN;   // wave tile
@@ -865,13 +881,14 @@ gemm_wide_kernel(GemmParams p, int tilesM, int tilesN, int groups) {
   static_assert(!RMO || RAGGED_K, "row-major operands: ragged-K products only");
   static_assert(!RAGGED_K || (!ARM && !BRM), "row-major operands of ragged-K products: EPI_WGF32");
   WOp<AK, RAGGED_K, NW, BM, RMO || ARM> opA;
-  WOp<BKK, RAGGED_K, NW, BN, RMO || BRM> opB;
+  WOp<BKK, RAGGED_K, NW, BN, RMO || BRM, BRM && !BKK> opB;
   int le = 0, lt = 0, lk = 0, lkend = 0, ls = 0;
   auto plan = [&](int t) __attribute__((always_inline)) {
     const WGeo G = geo(t);
     const uint16_t* Ab = (const uint16_t*)p.A + (RMO ? 0 : G.g * p.sA);
     const uint16_t* Bb = (const uint16_t*)p.B + (RMO ? 0 : G.g * p.sB);
-    const int64_t extA = RMO ? (int64_t)p.cap * p.lda : p.eA, extB = RMO ? (int64_t)p.cap * p.ldb : p.eB;
+    const int64_t extA = RMO ? (int64_t)p.cap * p.lda : TC::SHARED ? kSharedExtent : p.sA;
+    const int64_t extB = RMO ? (int64_t)p.cap * p.ldb : TC::SHARED && RAGGED_K ? kSharedExtent : p.sB;
     // (rows of the stage past the tile's BMT are not loaded: their places get zeros, which no wave reads)
     const int rlim = min(ARM ? p.cap : (int)pad16(p.cap), G.lo_al + G.m0 + BMT);
     if constexpr (AK) opA.plan(Ab, extA, p.lda, G.lo_al + G.m0, rlim, 0, 0, 0, wid, lane);
@@ -1211,7 +1228,7 @@ gemm_wide_kernel(GemmParams p, int tilesM, int tilesN, int groups) {
 // spread over FM blocks.  The schedule is recomputed exactly as the product
 // made it (nslot blocks per XCD).
 template <class TC, int EPI, int ACT, bool CBLK>
-__global__ __launch_bounds__(TC::NW * 64) void gemm_wide_fixup_kernel(GemmParams p, int tilesM, int tilesN, int groups,
+__global__ __launch_bounds__(TC::NW * 64) void gemm_wide_fixup_kernel(KernParams<EPI> p, int tilesM, int tilesN, int groups,
                                                                    int nslot) {
   constexpr int BM = TC::BMT, BN = TC::BN, WGN = TC::WGN, WTM = TC::WTM, WTN = TC::WTN, FM = TC::FM, FN = TC::FN;
   const int lane = threadIdx.x & 63;
@@ -1289,6 +1306,8 @@ struct WideCall {
   double spread;  // standard deviation (hints for the tile choice)
   GemmParams p;
   bool beside = false;   // ragged-K: other work runs beside it on another stream
+  bool shared = false;   // the groups share their rows
+  XentParams x{};        // WK_LSE .. WK_DL_BLK
 };
 
 constexpr int64_t kSkPartElems = (int64_t)256 * 256 * 256;   // floats of the K-split's partial tiles (one per block)
@@ -1297,7 +1316,9 @@ template <class TC, bool B_K, bool RAGGED_K, int EPI, int ACT, bool CBLK, bool A
 static void launch_wide(const WideCall& w, hipStream_t s) {
   constexpr size_t shmem = TC::lds_bytes(B_K);
   constexpr bool SPLIT = TC::KSPLIT && !RAGGED_K && EPI == EPI_STORE;
-  const GemmParams& p = w.p;
+  KernParams<EPI> p;
+  (GemmParams&)p = w.p;
+  if constexpr (std::is_same_v<KernParams<EPI>, XentGemmParams>) p.x = w.x;
   auto kern = gemm_wide_kernel<TC, B_K, RAGGED_K, EPI, ACT, CBLK, ARM, BRM>;
   static std::atomic<uint64_t> lds_ok{0};
   allow_dyn_lds((const void*)kern, (int)shmem, lds_ok);
@@ -1335,13 +1356,6 @@ static void run_wide_m(const WideCall& w, hipStream_t s) {
     case WK_NK_RES: return launch_wide<TC, true, false, EPI_RES, ID, false>(w, s);
     case WK_DACT: return launch_wide_act<TC, false, EPI_DACT>(w, s);
     case WK_KN: return launch_wide<TC, false, false, EPI_STORE, ID, false>(w, s);
-    case WK_LSE: return launch_wide<TC, true, false, EPI_LSE, ID, false, true, true>(w, s);
-    case WK_LSE_X: return launch_wide<TC, true, false, EPI_LSE, ID, false, false, true>(w, s);
-    case WK_DL: return launch_wide<TC, true, false, EPI_DL, ID, true, false, true>(w, s);
-    case WK_LSE_BLK: return launch_wide<TC, true, false, EPI_LSE, ID, false>(w, s);
-    case WK_DL_BLK: return launch_wide<TC, true, false, EPI_DL, ID, true>(w, s);
-    case WK_KN_RM: return launch_wide<TC, false, false, EPI_STORE, ID, false, false, true>(w, s);
-    case WK_ADD: return launch_wide<TC, false, false, EPI_ADD, ID, false, false, true>(w, s);
     default: return;
   }
 }
@@ -1356,11 +1370,61 @@ static void run_wide_k(const WideCall& w, hipStream_t s) {
   }
 }
 
-// One source file per tile shape (they compile in parallel).
+// The products of groups that share their rows.
+template <class T>
+static void run_rows_m(const WideCall& w, hipStream_t s) {
+  using TC = SharedRows<T>;
+  constexpr int ID = MOE_ACT_IDENTITY;
+  switch (w.kind) {
+    case WK_FWD1: return launch_wide_act<TC, true, EPI_FWD1>(w, s);
+    case WK_NK: return launch_wide<TC, true, false, EPI_STORE, ID, false>(w, s);
+    case WK_DACT: return launch_wide_act<TC, false, EPI_DACT>(w, s);
+    case WK_KN: return launch_wide<TC, false, false, EPI_STORE, ID, false>(w, s);
+    default: return;
+  }
+}
+template <class T>
+static void run_rows_k(const WideCall& w, hipStream_t s) {
+  using TC = SharedRows<T>;
+  constexpr int ID = MOE_ACT_IDENTITY;
+  if (w.kind == WK_DW) launch_wide<TC, false, true, EPI_STORE, ID, false>(w, s);
+  else launch_wide<TC, false, true, EPI_STORE, ID, true>(w, s);
+}
+// The cross entropy's.
+template <class TC>
+static void run_xent_m(const WideCall& w, hipStream_t s) {
+  constexpr int ID = MOE_ACT_IDENTITY;
+  switch (w.kind) {
+    case WK_LSE: return launch_wide<TC, true, false, EPI_LSE, ID, false, true, true>(w, s);
+    case WK_LSE_X: return launch_wide<TC, true, false, EPI_LSE, ID, false, false, true>(w, s);
+    case WK_LSE_BLK: return launch_wide<TC, true, false, EPI_LSE, ID, false>(w, s);
+    case WK_DL: return launch_wide<TC, true, false, EPI_DL, ID, true, false, true>(w, s);
+    case WK_DL_BLK: return launch_wide<TC, true, false, EPI_DL, ID, true>(w, s);
+    case WK_KN_RM: return launch_wide<TC, false, false, EPI_STORE, ID, false, false, true>(w, s);
+    case WK_ADD: return launch_wide<TC, false, false, EPI_ADD, ID, false, false, true>(w, s);
+    default: return;
+  }
+}
+
+// The tile shapes.  Ragged-M; ragged-K where it is another (see the source files).
+using Tile256 = Wide<256, 256, 8, 4, 1, 4, 5, 2, true>;
+using Tile192 = Wide<256, 256, 8, 4, 1, 4, 5, 2, false, 192>;
+using Tile128 = Wide<128, 128, 4, 2, 1, 4, 4, 2, false>;
+using Tile128K = Wide<128, 128, 4, 2, 1, 3, 3, 3, false>;
+using Tile64x128 = Wide<64, 128, 4, 2, 2, 3, 3, 2, false>;
+using Tile64 = Wide<64, 64, 4, 2, 2, 4, 4, 2, false>;
+
+// Two source files per tile shape (they compile in parallel).
 void run_wide_256x256(const WideCall& w, hipStream_t s);
 void run_wide_192x256(const WideCall& w, hipStream_t s);  // ragged-M products only
 void run_wide_128x128(const WideCall& w, hipStream_t s);
 void run_wide_64x128(const WideCall& w, hipStream_t s);   // ragged-M products only
 void run_wide_64x64(const WideCall& w, hipStream_t s);    // ragged-M products only
+// Rows that the groups share, and the cross entropy's products.
+void run_rows_256x256(const WideCall& w, hipStream_t s);
+void run_rows_192x256(const WideCall& w, hipStream_t s);
+void run_rows_128x128(const WideCall& w, hipStream_t s);
+void run_rows_64x128(const WideCall& w, hipStream_t s);
+void run_rows_64x64(const WideCall& w, hipStream_t s);
 
 }  // namespace lmoe
