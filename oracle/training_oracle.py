@@ -201,7 +201,7 @@ def xent(x, W, target, dloss=None):
     one = torch.zeros_like(p).scatter_(1, at, 1.0)
     dl = g * (p - one)
     t = g.abs() * (p * (tl + tz + (2 * (l - lse).abs() + 4) * U32) + 2 * U32 * (p - one).abs())
-    t = t + u * (dl.abs() + t) + (1 + g.abs()) * TINY
+    t = t + u * (dl.abs() + t) + (1 + g.abs().amax()) * TINY   # (bf16: dl is kept relative to the largest g)
     xz = torch.where(ok.unsqueeze(1), x, 0.0)
     for name, a, b, n in (("dx", (dl, t), W, V), ("dW", (dl.t(), t.t()), xz, T)):
         v = a[0] @ b

@@ -378,7 +378,7 @@ static TileK tile_k(const WideCall& w, int cus) {
 }
 static void run_wide_any(const WideCall& w, hipStream_t s) {
   if (w.rows <= 0 || w.cols <= 0 || w.groups <= 0) return;
-  const bool rows = w.shared || (w.kind >= WK_LSE && w.kind < WK_DW);
+  const bool rows = w.shared || (w.kind >= WK_LSE && w.kind < WK_DW) || w.kind == WK_DW_SCALED;
   if (w.kind < WK_DW) {
     const TileCost& t = kTilesM[tile_m(w, num_cus())];
     return (rows ? t.run_rows : t.run)(w, s);
@@ -765,7 +765,7 @@ void launch_xent_dl(int dtype, int form, int64_t T, int d, const void* x, const 
   run_wide_any(w, s);
 }
 
-// dx over one piece: acc_in (NULL = 0) + dl W -> acc_out (float), or rounded to dx (bf16).
+// dx over one piece: acc_in (NULL = 0) + dl W -> acc_out (float), or times *scale rounded to dx (bf16).
 //
 // float: few tiles with long sums are cut into slices of the classes (each a group of the launch, its sums in `part`),
 // enough of them for four blocks a CU, which a launch adds in order.  500 tokens, 10007 classes, width 512: 109 us in
@@ -795,9 +795,10 @@ __global__ __launch_bounds__(256) void xent_slices_kernel(const float* __restric
 }
 
 void launch_xent_dx(int dtype, int64_t T, int d, int cols, const void* dl, int ld, const void* W, const float* acc_in,
-                    float* acc_out, void* dx, void* part, hipStream_t s) {
+                    float* acc_out, void* dx, const float* scale, void* part, hipStream_t s) {
   GemmParams p = xent_params(T, d, ld, dl, ld, pad16(T) * ld, W, d, (int64_t)cols * d, acc_out, d);
   p.Aux = acc_in;
+  if (dtype == MOE_BF16) p.part = (float*)scale;
   p.C2 = dx;
   p.M = cols;
   WideCall w = xent_call(WK_ADD, T, d, p);
@@ -824,9 +825,10 @@ void launch_xent_dx(int dtype, int64_t T, int d, int cols, const void* dl, int l
 // result has few tiles, their long sums over the vocabulary are split over the CUs
 // (part: sorted_ffn_ws_bytes-sized).
 size_t xent_part_bytes() { return (size_t)kSkPartElems * sizeof(float); }
-void launch_xent_dx_whole(int64_t T, int d, int cols, const void* dl, int ld, const void* W, void* dx, void* part,
-                          hipStream_t s) {
+void launch_xent_dx_whole(int64_t T, int d, int cols, const void* dl, int ld, const void* W, void* dx, const float* scale,
+                          void* part, hipStream_t s) {
   GemmParams p = xent_params(T, d, ld, dl, ld, pad16(T) * ld, W, d, (int64_t)cols * d, dx, d);
+  p.Aux = scale;
   p.part = (float*)part;
   const int64_t large = (T + 255) / 256 * ((d + 255) / 256);
   WideCall w = xent_call(WK_KN_RM, T, d, p);
@@ -837,11 +839,13 @@ void launch_xent_dx_whole(int64_t T, int d, int cols, const void* dl, int ld, co
   run_wide_any(w, s);
 }
 
-// dW [cols][d] = dl^T x; x as dl (bf16: blocked).  Whole rounds of 256-tiles, and what is left past them on smaller
+// dW [cols][d] = dl^T x (bf16: times *scale); x as dl (bf16: blocked).  Whole rounds of 256-tiles, and what is left past them on smaller
 // ones (as whole_rounds, with the rows in the columns' place).
-void launch_xent_dw(int dtype, int64_t T, int d, int cols, const void* dl, int ld, const void* x, void* dW, hipStream_t s) {
+void launch_xent_dw(int dtype, int64_t T, int d, int cols, const void* dl, int ld, const void* x, void* dW,
+                    const float* scale, hipStream_t s) {
   GemmParams p{dl, ld, pad16(T) * ld, x, d, pad16(T) * d, dW, d, 0, nullptr, nullptr, nullptr, nullptr, cols, d, 0, 0, (int)T};
-  WideCall w = xent_call(WK_DW, cols, d, p);
+  p.Aux = scale;
+  WideCall w = xent_call(WK_DW_SCALED, cols, d, p);
   w.expect = (double)T;
   if (dtype != MOE_BF16) {
     if (f32_tile(w, num_cus()) == 32) launch_f32<1, false, true, EPI_STORE>(p, 1, cols, d, s);

@@ -16,21 +16,36 @@ namespace lmoe {
 // C + g sC; gemm_wgrad_reduce_kernel adds the partials in group order.
 // EPI_LSE, EPI_DL: logits that are not kept (see XentParams).  EPI_ADD: a float sum
 // over calls -- the product plus Aux (float, NULL = 0) goes to C (float) or, with
-// C2, rounded to C2.
-enum { EPI_STORE = 0, EPI_FWD1 = 1, EPI_DACT = 2, EPI_RES = 3, EPI_WGF32 = 4, EPI_LSE = 5, EPI_DL = 6, EPI_ADD = 7 };
+// C2, times the float at `part`, rounded to C2.  EPI_SCALED: the product times the
+// float at Aux.
+enum {
+  EPI_STORE = 0,
+  EPI_FWD1 = 1,
+  EPI_DACT = 2,
+  EPI_RES = 3,
+  EPI_WGF32 = 4,
+  EPI_LSE = 5,
+  EPI_DL = 6,
+  EPI_ADD = 7,
+  EPI_SCALED = 8
+};
 
 // The cross entropy's products x W^T over a piece of the vocabulary, columns
 // col0 .. col0 + cols - 1 of it.  EPI_LSE: of each row, and of each wave's run of
 // columns, the largest logit and the sum of exp(logit - largest), at
 // part[block * stride + row]; and the target's logit.  EPI_DL: the gradient at
 // the logits, g (exp(logit - lse) - [column = target]), 0 in the padding columns
-// and in the rows whose target is outside 0 .. V - 1.
+// and in the rows whose target is outside 0 .. V - 1.  In bf16 it is kept relative
+// to *scale, the largest |g|, which the products with it bring back in float: of a
+// mean, whose g are one 1 / n, every target's -1 would otherwise be rounded by the
+// same factor, up to 2^-8 of every gradient.
 struct XentParams {
   const int32_t* target;
   float2* part;
   float* tl;           // the target's logit (rows whose target is in the piece)
   const float* lse;
   const float* g;
+  const float* scale;  // NULL: 1
   int64_t stride;
   int V, col0, cols, block0;
 };
@@ -146,7 +161,8 @@ __device__ __forceinline__ XentRow xent_row(const XentParams& x, int row, int ro
   const int r = min(row, rows - 1);
   const int t = x.target[r];
   const bool live = t >= 0 && t < x.V;
-  return XentRow{live ? x.lse[r] * kLog2e : 0.f, live ? x.g[r] : 0.f, live ? t - x.col0 : -1};
+  const float g = live ? x.g[r] : 0.f;
+  return XentRow{live ? x.lse[r] * kLog2e : 0.f, x.scale ? g / *x.scale : g, live ? t - x.col0 : -1};
 }
 // The gradient at four logits of a row, columns c .. c + 3.  any: a lane of the wave has its row's target among the
 // fragment's columns; full: no column is past the piece.
@@ -668,6 +684,9 @@ __device__ __forceinline__ void wide_epilogue(const KernParams<EPI>& p, const WG
     }
     rC2 = __builtin_amdgcn_make_buffer_rsrc((uint16_t*)p.C2 + cofs, (short)0, 0x7fffffff, kBufCfg);
   }
+  float scale = 1.f;
+  if constexpr (EPI == EPI_ADD) scale = *p.part;
+  if constexpr (EPI == EPI_SCALED) scale = *(const float*)p.Aux;
   // bf16 outputs move as 16 bytes per lane: of a pair of fragments (32 columns)
   // a lane holds columns 4 q .. +3 of each 16; swapping the odd 16-lane groups of
   // the first with the even ones of the second leaves it columns cq .. cq + 7 of
@@ -750,6 +769,12 @@ __device__ __forceinline__ void wide_epilogue(const KernParams<EPI>& p, const WG
           for (int e = 0; e < 2; ++e)
             xent_dl4(p.x, xr[ii], v[e], G.n0 + wn * WTN + 16 * (2 * jp + e) + 4 * q, xany[ii], xfull);
         }
+        if constexpr (EPI == EPI_ADD || EPI == EPI_SCALED) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) v[e][u] *= scale;
+        }
         if constexpr (EPI == EPI_ADD) store(pack4_bf16(v[0]), pack4_bf16(v[1]), rC2, vo < 0 ? vo : vo / 2);
         else store(pack4_bf16(v[0]), pack4_bf16(v[1]), rC, vo);
       }
@@ -790,7 +815,7 @@ gemm_wide_kernel(KernParams<EPI> p, int tilesM, int tilesN, int groups) {
   // others keep the simpler whole-tile schedule and its register budget.
   // The K-split products place their short tiles last (SEP), so the split
   // round holds the short tiles, whose partial sums stop at the group's rows.
-  constexpr bool SPLIT = TC::KSPLIT && !RAGGED_K && EPI == EPI_STORE;
+  constexpr bool SPLIT = TC::KSPLIT && !RAGGED_K && (EPI == EPI_STORE || EPI == EPI_SCALED);
   if constexpr (RAGGED_K && EPI != EPI_WGF32) {
     // A product launched on two tile shapes: the row counts say which one runs
     // (skewed: the longest group has at least 1.5 times the mean of all).
@@ -1290,10 +1315,11 @@ enum WideKind {
   WK_LSE_BLK,   // the same with x and W blocked
   WK_DL,        // x blocked, W row-major: EPI_DL, blocked output
   WK_DL_BLK,    // the same with x and W blocked
-  WK_KN_RM,     // WK_KN with a row-major B
+  WK_KN_RM,     // B [K][N] row-major, EPI_SCALED, row-major output
   WK_ADD,       // the same added over calls: EPI_ADD
   WK_DW,        // (this kind and the later ones) ragged-K, row-major output
   WK_DW_BLK,    // ragged-K, blocked output
+  WK_DW_SCALED, // WK_DW with EPI_SCALED
   WK_WGF32      // ragged-K over row-major operands, float partials
 };
 struct WideCall {
@@ -1315,7 +1341,7 @@ constexpr int64_t kSkPartElems = (int64_t)256 * 256 * 256;   // floats of the K-
 template <class TC, bool B_K, bool RAGGED_K, int EPI, int ACT, bool CBLK, bool ARM = false, bool BRM = false>
 static void launch_wide(const WideCall& w, hipStream_t s) {
   constexpr size_t shmem = TC::lds_bytes(B_K);
-  constexpr bool SPLIT = TC::KSPLIT && !RAGGED_K && EPI == EPI_STORE;
+  constexpr bool SPLIT = TC::KSPLIT && !RAGGED_K && (EPI == EPI_STORE || EPI == EPI_SCALED);
   KernParams<EPI> p;
   (GemmParams&)p = w.p;
   if constexpr (std::is_same_v<KernParams<EPI>, XentGemmParams>) p.x = w.x;
@@ -1388,7 +1414,8 @@ static void run_rows_k(const WideCall& w, hipStream_t s) {
   using TC = SharedRows<T>;
   constexpr int ID = MOE_ACT_IDENTITY;
   if (w.kind == WK_DW) launch_wide<TC, false, true, EPI_STORE, ID, false>(w, s);
-  else launch_wide<TC, false, true, EPI_STORE, ID, true>(w, s);
+  else if (w.kind == WK_DW_BLK) launch_wide<TC, false, true, EPI_STORE, ID, true>(w, s);
+  else launch_wide<T, false, true, EPI_SCALED, ID, false>(w, s);
 }
 // The cross entropy's.
 template <class TC>
@@ -1400,7 +1427,7 @@ static void run_xent_m(const WideCall& w, hipStream_t s) {
     case WK_LSE_BLK: return launch_wide<TC, true, false, EPI_LSE, ID, false>(w, s);
     case WK_DL: return launch_wide<TC, true, false, EPI_DL, ID, true, false, true>(w, s);
     case WK_DL_BLK: return launch_wide<TC, true, false, EPI_DL, ID, true>(w, s);
-    case WK_KN_RM: return launch_wide<TC, false, false, EPI_STORE, ID, false, false, true>(w, s);
+    case WK_KN_RM: return launch_wide<TC, false, false, EPI_SCALED, ID, false, false, true>(w, s);
     case WK_ADD: return launch_wide<TC, false, false, EPI_ADD, ID, false, false, true>(w, s);
     default: return;
   }

@@ -7,7 +7,8 @@
 //     were 4 T V; one launch joins them.
 //   backward: dl = g (exp(l - lse) - [v = target]) in the type of x, computed again
 //     piece by piece (EPI_DL); dx += dl W in float over the pieces, dW = dl^T x.  dl's
-//     rounding to bfloat16 is half a step of each, as every operand of the products.
+//     rounding to bfloat16 (relative to the largest g) is half a step of each, as of
+//     every operand of the products.
 //
 // A piece's dl takes kDlBytes at most.  Every piece reads and writes dx's float sums, so
 // fewer are faster (16384 tokens, 50257 classes, width 2048, bfloat16, one step: 128 MiB
@@ -23,19 +24,23 @@ int launch_xent_lse(int dtype, int form, int64_t T, int d, const void* x, const 
 void launch_xent_dl(int dtype, int form, int64_t T, int d, const void* x, const void* W, const XentParams& xp, void* dl,
                     int ld, hipStream_t s);
 void launch_xent_dx(int dtype, int64_t T, int d, int cols, const void* dl, int ld, const void* W, const float* acc_in,
-                    float* acc_out, void* dx, void* part, hipStream_t s);
+                    float* acc_out, void* dx, const float* scale, void* part, hipStream_t s);
 size_t xent_slices_bytes(int64_t T, int d, int cols);
-void launch_xent_dx_whole(int64_t T, int d, int cols, const void* dl, int ld, const void* W, void* dx, void* part,
-                          hipStream_t s);
-void launch_xent_dw(int dtype, int64_t T, int d, int cols, const void* dl, int ld, const void* x, void* dW, hipStream_t s);
+void launch_xent_dx_whole(int64_t T, int d, int cols, const void* dl, int ld, const void* W, void* dx, const float* scale,
+                          void* part, hipStream_t s);
+void launch_xent_dw(int dtype, int64_t T, int d, int cols, const void* dl, int ld, const void* x, void* dW,
+                    const float* scale, hipStream_t s);
 size_t xent_part_bytes();
 
 namespace {
 
 constexpr int64_t kDlBytes = (int64_t)512 << 20;
 constexpr int64_t kWBytes = (int64_t)128 << 20;  // of W in blocks, in the forward
-// From how many tokens on the forward copies x, and x and W, to blocks, and the backward W (x it always does).
-constexpr int64_t kFwdX = 512, kFwdBlocked = 4096, kBwdBlocked = 8192;
+// From how many tokens on the forward copies x, and x and W, to blocks, and the backward W (x it always does).  Blocks
+// feed the products' loads whole cache lines, for a pass over the operand.  Forward, no copy / x / both, us (50257
+// classes): 64 tokens, width 1024 33.1 / 32.0 / 58.1; 2048 232.8 / 201.8 / 222.4; 4096, width 2048 834 / 715 / 721; 8192,
+// width 1024 863 / 761 / 739.  Backward, W as it is / copied: 4096 tokens 2497 / 2510, 8192 (32000 classes) 2697 / 2632.
+constexpr int64_t kFwdX = 64, kFwdBlocked = 8192, kBwdBlocked = 8192;
 constexpr int64_t kCus = 256;   // compute units (the sizes below are asked for on hosts without a device too)
 constexpr int64_t kOperand = (int64_t)1 << 31;   // the bf16 products' operands: 32-bit byte offsets
 
@@ -73,7 +78,7 @@ FwdPlan fwd_plan(const moe_xent_cfg& c) {
 }
 struct BwdPlan {
   int cols, pieces, ld;   // columns of a piece, pieces, columns of dl's rows
-  size_t x, W, dl, acc, part, bytes;
+  size_t scale, x, W, dl, acc, part, bytes;
   int form;               // kXentX or kXentBlocked
 };
 BwdPlan bwd_plan(const moe_xent_cfg& c) {
@@ -96,6 +101,7 @@ BwdPlan bwd_plan(const moe_xent_cfg& c) {
     return o;
   };
   p.form = c.dtype == MOE_BF16 && c.T >= kBwdBlocked ? kXentBlocked : kXentX;
+  p.scale = take(sizeof(float));
   p.x = take(rows * c.d_model * e);
   if (p.form == kXentBlocked) p.W = take(pad16(p.cols) * c.d_model * 2);
   p.dl = take(rows * p.ld * e);
@@ -140,12 +146,43 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const float2* __restrict
   }
 }
 
+// The largest |g| of the tokens that count (1 if there is none, or none that is finite): what bf16's dl is relative to.
+// One block's work.
+__device__ __forceinline__ void largest_g(const float* __restrict__ g, const int32_t* __restrict__ target, int64_t T, int V,
+                                          float* __restrict__ out) {
+  __shared__ float red[4];
+  float m = 0.f;
+  constexpr int U = 16;
+  for (int64_t t0 = threadIdx.x; t0 < T; t0 += U * 256) {
+    float v[U];
+    int id[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t t = t0 + u * 256;
+      v[u] = t < T ? fabsf(g[t]) : 0.f;
+      id[u] = t < T ? target[t] : -1;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) m = id[u] >= 0 && id[u] < V ? fmaxf(m, v[u]) : m;   // (NaN: left out)
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, kWave));
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    *out = m > 0.f && m < INFINITY ? m : 1.f;
+  }
+}
+
 // x for the backward's products: the rows whose target is no class as zeros, so that
 // whatever padding holds stays out of dW.  bf16: 16 x 32 blocks, a wave each.
-// target NULL: every row as it is.
+// target NULL: every row as it is.  scale (nullable): the first block finds largest_g.
 __global__ __launch_bounds__(256) void xent_pack_kernel(const uint16_t* __restrict__ x, const int32_t* __restrict__ target,
-                                                        uint16_t* __restrict__ out, int64_t T, int V, int d) {
-  const int64_t b = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 6;
+                                                        uint16_t* __restrict__ out, int64_t T, int V, int d,
+                                                        const float* __restrict__ g, float* __restrict__ scale) {
+  if (scale && blockIdx.x == 0) return largest_g(g, target, T, V, scale);
+  const int64_t b = ((int64_t)(blockIdx.x - (scale ? 1 : 0)) * blockDim.x + threadIdx.x) >> 6;
   const int lane = threadIdx.x & 63, kb = d >> 5;
   const int64_t rb = b / kb;
   if (rb * 16 >= pad16(T)) return;
@@ -167,9 +204,11 @@ __global__ __launch_bounds__(256) void xent_zero_kernel(u32x4* z, int64_t n) {
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) z[i] = u32x4{0u, 0u, 0u, 0u};
 }
 
-void launch_pack(const void* src, const int32_t* target, void* dst, int64_t rows, int V, int d, hipStream_t s) {
-  hipLaunchKernelGGL(xent_pack_kernel, dim3((unsigned)((pad16(rows) / 16 * (d / 32) * 64 + 255) / 256)), dim3(256), 0, s,
-                     (const uint16_t*)src, target, (uint16_t*)dst, rows, V, d);
+void launch_pack(const void* src, const int32_t* target, void* dst, int64_t rows, int V, int d, hipStream_t s,
+                 const float* g = nullptr, float* scale = nullptr) {
+  const int64_t blocks = (pad16(rows) / 16 * (d / 32) * 64 + 255) / 256 + (scale ? 1 : 0);
+  hipLaunchKernelGGL(xent_pack_kernel, dim3((unsigned)blocks), dim3(256), 0, s, (const uint16_t*)src, target,
+                     (uint16_t*)dst, rows, V, d, g, scale);
 }
 
 }  // namespace
@@ -227,7 +266,7 @@ void launch_xent_bwd(const moe_xent_cfg& c, const void* x, const void* W, const 
   void *xp_ = w + p.x, *dl = w + p.dl;
   const bool bf = c.dtype == MOE_BF16;
   if (bf)
-    launch_pack(x, target, xp_, c.T, c.V, (int)d, s);
+    launch_pack(x, target, xp_, c.T, c.V, (int)d, s, dloss, (float*)(w + p.scale));
   else
     hipLaunchKernelGGL(xent_copy_kernel, dim3((unsigned)((c.T * d / 4 + 255) / 256)), dim3(256), 0, s, (const float*)x,
                        target, (float*)xp_, c.T, c.V, (int)d);
@@ -235,6 +274,8 @@ void launch_xent_bwd(const moe_xent_cfg& c, const void* x, const void* W, const 
   xp.target = target;
   xp.lse = lse;
   xp.g = dloss;
+  const float* scale = bf ? (const float*)(w + p.scale) : nullptr;
+  xp.scale = scale;
   xp.stride = c.T;
   xp.V = c.V;
   float* acc = bf ? (float*)(w + p.acc) : (float*)dx;
@@ -246,13 +287,13 @@ void launch_xent_bwd(const moe_xent_cfg& c, const void* x, const void* W, const 
     if (p.form == kXentBlocked) launch_pack(Wv, nullptr, w + p.W, xp.cols, c.V, (int)d, s);
     launch_xent_dl(c.dtype, p.form, c.T, (int)d, xp_, p.form == kXentBlocked ? w + p.W : Wv, xp, dl, ld, s);
     if (dx && bf && p.pieces == 1) {
-      launch_xent_dx_whole(c.T, (int)d, xp.cols, dl, ld, Wv, dx, w + p.part, s);
+      launch_xent_dx_whole(c.T, (int)d, xp.cols, dl, ld, Wv, dx, scale, w + p.part, s);
     } else if (dx) {
       const bool last = v + p.cols >= c.V;
       launch_xent_dx(c.dtype, c.T, (int)d, xp.cols, dl, ld, Wv, v > 0 ? acc : nullptr, acc, bf && last ? dx : nullptr,
-                     w + p.part, s);
+                     scale, w + p.part, s);
     }
-    if (dW) launch_xent_dw(c.dtype, c.T, (int)d, xp.cols, dl, ld, xp_, (char*)dW + v * d * e, s);
+    if (dW) launch_xent_dw(c.dtype, c.T, (int)d, xp.cols, dl, ld, xp_, (char*)dW + v * d * e, scale, s);
   }
 }
 

@@ -768,3 +768,58 @@ def alloc_block(cfg: moe_block_cfg, n_chunks: int, device="cuda", names=None) ->
             out[n] = torch.empty(numel, dtype=dt, device=device)
     out["ws"] = torch.empty(max(16, moe_block_workspace_bytes(cfg, n_chunks)), dtype=torch.uint8, device=device)
     return out
+
+
+# ----------------------------------------------------- a model step around the block
+@dataclass
+class LmBuffers:
+    """What a step of token lookup, blocks and loss keeps beside the blocks' own buffers."""
+    embed: moe_embed_cfg
+    embed_add: moe_embed_cfg   # the lookup's gradient added to the loss's, for a tied table
+    xent: moe_xent_cfg
+    h: list                    # [T][d] the blocks' inputs, and the last one's output
+    loss: torch.Tensor
+    lse: torch.Tensor
+    dh: torch.Tensor           # gradients at the activations, in turn
+    dx: torch.Tensor
+    dWout: torch.Tensor        # [V][d]
+    dWin: Optional[torch.Tensor]   # [V][d]; None: tied to the output matrix
+    ws: torch.Tensor
+
+
+def alloc_lm(cfg: moe_block_cfg, V: int, n_blocks: int = 1, scale: float = 1.0, tied: bool = True,
+             device="cuda") -> LmBuffers:
+    m = cfg.moe
+    T, d, bf = m.T, m.d_model, torch.bfloat16
+    embed, xent = make_embed_cfg(T, V, d, "bf16", scale), make_xent_cfg(T, V, d, "bf16")
+    e = lambda *s, dtype=bf: torch.empty(*s, dtype=dtype, device=device)
+    need = max(moe_embed_bwd_workspace_bytes(embed), moe_xent_workspace_bytes(xent), moe_xent_workspace_bytes(xent, True))
+    return LmBuffers(embed=embed, embed_add=make_embed_cfg(T, V, d, "bf16", scale, accum=1), xent=xent,
+                     h=[e(T, d) for _ in range(n_blocks + 1)], loss=e(T, dtype=torch.float32),
+                     lse=e(T, dtype=torch.float32), dh=e(T, d), dx=e(T, d), dWout=e(V, d),
+                     dWin=None if tied else e(V, d), ws=e(max(16, need), dtype=torch.uint8))
+
+
+def lm_forward(b: LmBuffers, cfg: moe_block_cfg, ids, target, Win, Wout, weights: list, acts: list, n_chunks: int, streams):
+    """Token lookup -> blocks -> cross entropy of every token (b.loss).  weights, acts: of each block (block_shapes,
+    alloc_block); ids, target [T] int32.  streams as for moe_block_chunked; the rest runs on the first."""
+    moe_embed(b.embed, ids, Win, b.h[0], streams[0])
+    for i, (w, a) in enumerate(zip(weights, acts)):
+        moe_block_chunked(cfg, w, None, b.h[i], b.h[i + 1], None, None, a, MOE_BLOCK_FWD, n_chunks, streams, a["ws"])
+    moe_xent(b.xent, b.h[-1], Wout, target, b.loss, b.lse, b.ws, streams[0])
+
+
+def lm_backward(b: LmBuffers, cfg: moe_block_cfg, ids, target, Wout, weights: list, grads: list, acts: list, dloss,
+                n_chunks: int, streams):
+    """After lm_forward: dloss [T] float (1 / n for the mean of n tokens) -> b.dWout, every block's grads, and the
+    table's gradient in b.dWin, or added to b.dWout where the two are tied."""
+    moe_xent_bwd(b.xent, b.h[-1], Wout, target, b.lse, dloss, b.dh, b.dWout, b.ws, streams[0])
+    dy, dx = b.dh, b.dx
+    for i in reversed(range(len(weights))):
+        moe_block_chunked(cfg, weights[i], grads[i], b.h[i], b.h[i + 1], dy, dx, acts[i], MOE_BLOCK_BWD, n_chunks, streams,
+                          acts[i]["ws"])
+        dy, dx = dx, dy
+    if b.dWin is None:
+        moe_embed_bwd(b.embed_add, ids, dy, b.dWout, b.ws, streams[0])
+    else:
+        moe_embed_bwd(b.embed, ids, dy, b.dWin, b.ws, streams[0])

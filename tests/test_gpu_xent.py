@@ -91,6 +91,36 @@ def test_large_logits(dtype):
         assert O.off(got[n], want[n]) <= 1, n
 
 
+def test_gradients_of_a_mean_are_not_scaled():
+    """1 / n of a mean is no bfloat16: its rounding must not be a factor of every gradient.  A
+    target's -1 + p is off by p at most (p under half a step of 1), the sums' and the results'
+    roundings average out (a 2^-12 is ten times what they leave of 38400 values)."""
+    x, W, target, _ = _make(300, 5000, 128, "bf16", 11)
+    dloss = torch.full((300,), 1 / 300.5, device="cuda")       # 2^-8.2, off by 0.3 half steps as bfloat16
+    got, want = _run(x, W, target, dloss, "bf16"), O.xent(x, W, target, dloss)
+    p = float(torch.exp(-want["loss"][0]).max())
+    assert p <= 2 ** -9
+    for n in ("dx", "dW"):
+        v = want[n][0]
+        assert abs(float((got[n].double() * v).sum() / (v * v).sum()) - 1) <= p + 2 ** -12, n
+
+
+@pytest.mark.parametrize("g", [float("inf"), float("nan"), 3e38, 1e-37])
+def test_extreme_upstream_gradients_stay_with_their_rows(g):
+    x, W, target, dloss = _make(40, 300, 64, "bf16", 12)
+    clean = _run(x, W, target, dloss, "bf16")
+    dloss[7] = g
+    got = _run(x, W, target, dloss, "bf16")
+    keep = torch.arange(40, device="cuda") != 7
+    if g == g and abs(g) < 1:
+        assert O.off(got["dx"], O.xent(x, W, target, dloss)["dx"]) <= 1
+    elif g == g and abs(g) < float("inf"):                      # the others are as nothing beside it
+        assert bool(torch.isfinite(got["dx"][keep].float()).all())
+    else:
+        assert not bool(torch.isfinite(got["dx"][7].float()).any())
+        assert torch.equal(torch.isfinite(got["dx"][keep].float()), torch.isfinite(clean["dx"][keep].float()))
+
+
 def test_rows_do_not_mix():
     """A row with NaN has a NaN loss; the others keep their bits."""
     x, W, target, dloss = _make(300, 1000, 128, "bf16", 5)
