@@ -546,8 +546,8 @@ moe_status moe_embed_bwd(const moe_embed_cfg* cfg, const int32_t* ids, const voi
 /* The loss of a language model from its last activations x and its output matrix W,
  * in pieces of the vocabulary; the logits x W^T are never kept. */
 typedef struct {
-  int64_t T;       /* tokens; T * d_model < 2^29 */
-  int32_t V;       /* rows of W, 1..2^30; V * d_model <= 2^40 */
+  int64_t T;       /* tokens; (T + 15) * d_model < 2^29 */
+  int32_t V;       /* rows of W, 1..2^30; V * d_model <= 2^40, T * V <= 2^42 */
   int32_t d_model; /* MOE_BF16: a multiple of 64; MOE_F32: of 8; up to 2^20 */
   int32_t dtype;   /* moe_dtype of x, W, dx and dW */
 } moe_xent_cfg;

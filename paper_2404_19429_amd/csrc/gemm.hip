@@ -839,10 +839,33 @@ void launch_xent_dx_whole(int64_t T, int d, int cols, const void* dl, int ld, co
   run_wide_any(w, s);
 }
 
-// dW [cols][d] = dl^T x (bf16: times *scale); x as dl (bf16: blocked).  Whole rounds of 256-tiles, and what is left past them on smaller
-// ones (as whole_rounds, with the rows in the columns' place).
+// Sum of the token ranges' partials in range order, times *scale: 8 consecutive elements a thread.
+__global__ __launch_bounds__(256) void xent_ranges_kernel(const float* __restrict__ part, int n, int64_t size,
+                                                          const float* __restrict__ scale, uint16_t* __restrict__ out) {
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+  if (i >= size) return;
+  f32x4 a = *reinterpret_cast<const f32x4*>(part + i), b = *reinterpret_cast<const f32x4*>(part + i + 4);
+  for (int q = 1; q < n; ++q) {
+    a += *reinterpret_cast<const f32x4*>(part + q * size + i);
+    b += *reinterpret_cast<const f32x4*>(part + q * size + i + 4);
+  }
+  const float k = *scale, v[8] = {a[0] * k, a[1] * k, a[2] * k, a[3] * k, b[0] * k, b[1] * k, b[2] * k, b[3] * k};
+  Vec<uint16_t>::store(out + i, v);
+}
+
+// Token ranges of a dW product that has too few tiles for the chip: it is one 128-tile a CU at most, as long as the
+// batch, so its tokens are cut into ranges (float partials, joined in order) until there are three a CU.
+static int dw_ranges(int64_t T, int rows, int d, int cus) {
+  const int64_t tiles = (int64_t)((rows + 127) / 128) * ((d + 127) / 128);
+  if (tiles > cus) return 1;
+  const int64_t n = std::min<int64_t>(std::min<int64_t>(8, 3 * cus / tiles), T / 256);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(n, kSkPartElems / ((int64_t)rows * d)));
+}
+
+// dW [cols][d] = dl^T x (bf16: times *scale); x as dl (bf16: blocked).  Whole rounds of 256-tiles, and what is left
+// past them on smaller ones (as whole_rounds, with the rows in the columns' place).  part: xent_part_bytes.
 void launch_xent_dw(int dtype, int64_t T, int d, int cols, const void* dl, int ld, const void* x, void* dW,
-                    const float* scale, hipStream_t s) {
+                    const float* scale, void* part, hipStream_t s) {
   GemmParams p{dl, ld, pad16(T) * ld, x, d, pad16(T) * d, dW, d, 0, nullptr, nullptr, nullptr, nullptr, cols, d, 0, 0, (int)T};
   p.Aux = scale;
   WideCall w = xent_call(WK_DW_SCALED, cols, d, p);
@@ -853,6 +876,22 @@ void launch_xent_dw(int dtype, int64_t T, int d, int cols, const void* dl, int l
     return;
   }
   const int cus = num_cus();
+  auto run = [&](WideCall q) {
+    const int n = dw_ranges(T, q.p.M, d, cus);
+    if (n == 1) return run_wide_any(q, s);
+    const int64_t size = (int64_t)q.p.M * d;
+    uint16_t* const out = (uint16_t*)q.p.C;
+    q.kind = WK_DW_PART;
+    q.groups = n;
+    q.p.kchunk = (int)(((T + n - 1) / n + 31) / 32 * 32);
+    q.p.sA = q.p.sB = 0;
+    q.p.C = part;
+    q.p.sC = size;
+    q.p.Aux = nullptr;
+    run_rows_128x128(q, s);
+    hipLaunchKernelGGL(xent_ranges_kernel, dim3((unsigned)((size / 8 + 255) / 256)), dim3(256), 0, s, (const float*)part, n,
+                       size, scale, out);
+  };
   const int64_t tn = (d + 255) / 256, tm = (cols + 255) / 256, main = tm * tn / cus * cus / tn * 256;
   // (half a round or more left: it is as well spent on 256-tiles)
   if (main > 0 && main < cols && 2 * (tm * tn % cus) < cus) {
@@ -861,10 +900,10 @@ void launch_xent_dw(int dtype, int64_t T, int d, int cols, const void* dl, int l
     b.p.A = (const uint16_t*)dl + main / 32 * 512;
     b.p.sA = p.sA - main / 32 * 512;
     b.p.C = (uint16_t*)dW + main * d;
-    run_wide_any(b, s);
+    run(b);
     w.rows = w.p.M = (int)main;
   }
-  run_wide_any(w, s);
+  run(w);
 }
 
 // Sum of the S float partials of a K-split weight gradient, in group order,

@@ -838,12 +838,13 @@ gemm_wide_kernel(KernParams<EPI> p, int tilesM, int tilesN, int groups) {
     // Groups without rows have no tiles: their [M][N] outputs are zeroed here,
     // spread over the whole grid (16-byte stores; no tile writes them).
     uint64_t empty = __ballot(lane < groups && P.incl == P.excl);
-    const int64_t chunks = (int64_t)p.M * p.N / (EPI == EPI_WGF32 ? 4 : 8);
+    constexpr bool F32 = EPI == EPI_WGF32 || EPI == EPI_ADD;
+    const int64_t chunks = (int64_t)p.M * p.N / (F32 ? 4 : 8);
     const int64_t gtid = (int64_t)blockIdx.x * blockDim.x + threadIdx.x, gstride = (int64_t)gridDim.x * blockDim.x;
     while (empty) {
       const int g = __builtin_ctzll(empty);
       empty &= empty - 1;
-      u32x4* o = EPI == EPI_WGF32 ? reinterpret_cast<u32x4*>((float*)p.C + (int64_t)g * p.sC)
+      u32x4* o = F32 ? reinterpret_cast<u32x4*>((float*)p.C + (int64_t)g * p.sC)
                                   : reinterpret_cast<u32x4*>((uint16_t*)p.C + (int64_t)g * p.sC);
       for (int64_t i = gtid; i < chunks; i += gstride) o[i] = u32x4{0u, 0u, 0u, 0u};
     }
@@ -1320,6 +1321,7 @@ enum WideKind {
   WK_DW,        // (this kind and the later ones) ragged-K, row-major output
   WK_DW_BLK,    // ragged-K, blocked output
   WK_DW_SCALED, // WK_DW with EPI_SCALED
+  WK_DW_PART,   // WK_DW whose groups are K ranges of shared operands: float partials (EPI_ADD)
   WK_WGF32      // ragged-K over row-major operands, float partials
 };
 struct WideCall {
@@ -1415,7 +1417,8 @@ static void run_rows_k(const WideCall& w, hipStream_t s) {
   constexpr int ID = MOE_ACT_IDENTITY;
   if (w.kind == WK_DW) launch_wide<TC, false, true, EPI_STORE, ID, false>(w, s);
   else if (w.kind == WK_DW_BLK) launch_wide<TC, false, true, EPI_STORE, ID, true>(w, s);
-  else launch_wide<T, false, true, EPI_SCALED, ID, false>(w, s);
+  else if (w.kind == WK_DW_SCALED) launch_wide<T, false, true, EPI_SCALED, ID, false>(w, s);
+  else if constexpr (T::BM == 128) launch_wide<TC, false, true, EPI_ADD, ID, false>(w, s);
 }
 // The cross entropy's.
 template <class TC>

@@ -13,7 +13,8 @@
 // A block is a chain of latencies (keys, the tiles' counts, barriers, scattered
 // stores of a line a lane), so small tiles on many CUs are the faster ones until
 // the sums over the tiles are the longer part: 1024 items up to 64 tiles of them,
-// 4096 beyond.
+// 4096 beyond.  Counting and placing 12000 items of 160 keys in tiles of 4096: 2.6 +
+// 9.5 us, of 1024: 3.1 + 6.3.
 #pragma once
 
 #include "internal.h"

@@ -72,7 +72,8 @@ size_t sorted_dispatch_ws_bytes(const moe_sorted_cfg& c) {
 // rows[r] = x[src[r] / k].  A wave moves sixteen rows by U * 8 vectors of columns:
 // eight lanes a row, so that a load and a store are whole cache lines (a bfloat16
 // block's half is 512 bytes in one run).  Bound: bytes; 16384 x 2 rows of 2048 in
-// bfloat16, 201 MB moved.
+// bfloat16: 201 MB moved in 41 us (traced); four lanes a row, whose accesses were half
+// lines, 48.
 template <typename T, int U, bool S>
 __device__ __forceinline__ void gather_rows(const T* __restrict__ x, T* __restrict__ rows, int64_t r0, const int (&i)[2], int d,
                                             int k, int c0) {
@@ -185,7 +186,8 @@ void launch_sorted_dispatch(const moe_sorted_cfg& c, const void* x, const int32_
 // -------------------------------------------------- rows back to their tokens
 // W: y[t] = sum over r of w[t][r] rows[slot[t][r]] (combine).  Otherwise the sum
 // alone (the dispatch's gradient), G: plus sum over j of dlogits[t][j] Wg[j] (the
-// gate's).  Float sums in choice order; a thread owns 16 bytes of a token.
+// gate's).  Float sums in choice order; a thread owns 16 bytes of a token.  Bound:
+// bytes, 201 MB in 34 and 36 us (traced; 16384 tokens, two choices, 2048 in bfloat16).
 template <typename T, bool W, bool G, bool S>
 __global__ __launch_bounds__(256) void sorted_back_kernel(const T* __restrict__ rows, const int32_t* __restrict__ slot,
                                                           const float* __restrict__ w, const T* __restrict__ Wg,
@@ -274,7 +276,8 @@ void launch_sorted_dispatch_bwd(const moe_sorted_cfg& c, const int32_t* slot, co
 // dO[row] = w dy[t], dw = <dy[t], O[row]> for the choice that the row holds.  A
 // block takes sixteen rows, each wave a run of columns of all of them (eight lanes
 // a row, as in the gather); the waves' dot products meet in LDS, in wave order.
-// The blocks past the rows write the zeros of the choices that have none.
+// The blocks past the rows write the zeros of the choices that have none.  Bound:
+// bytes, 336 MB in 67 us (traced; as above).
 template <typename T, int U, bool S>
 __global__ __launch_bounds__(256) void sorted_combine_bwd_kernel(const T* __restrict__ O, const int32_t* __restrict__ slot,
                                                                  const int32_t* __restrict__ src,

@@ -29,7 +29,7 @@ size_t xent_slices_bytes(int64_t T, int d, int cols);
 void launch_xent_dx_whole(int64_t T, int d, int cols, const void* dl, int ld, const void* W, void* dx, const float* scale,
                           void* part, hipStream_t s);
 void launch_xent_dw(int dtype, int64_t T, int d, int cols, const void* dl, int ld, const void* x, void* dW,
-                    const float* scale, hipStream_t s);
+                    const float* scale, void* part, hipStream_t s);
 size_t xent_part_bytes();
 
 namespace {
@@ -106,7 +106,7 @@ BwdPlan bwd_plan(const moe_xent_cfg& c) {
   if (p.form == kXentBlocked) p.W = take(pad16(p.cols) * c.d_model * 2);
   p.dl = take(rows * p.ld * e);
   if (c.dtype == MOE_BF16 && p.pieces > 1) p.acc = take((size_t)c.T * c.d_model * 4);
-  if (c.dtype == MOE_BF16 && p.pieces == 1) p.part = take(xent_part_bytes());
+  if (c.dtype == MOE_BF16) p.part = take(xent_part_bytes());
   if (c.dtype == MOE_F32) p.part = take(xent_slices_bytes(c.T, c.d_model, p.cols));
   p.bytes = at;
   return p;
@@ -293,7 +293,7 @@ void launch_xent_bwd(const moe_xent_cfg& c, const void* x, const void* W, const 
       launch_xent_dx(c.dtype, c.T, (int)d, xp.cols, dl, ld, Wv, v > 0 ? acc : nullptr, acc, bf && last ? dx : nullptr,
                      scale, w + p.part, s);
     }
-    if (dW) launch_xent_dw(c.dtype, c.T, (int)d, xp.cols, dl, ld, xp_, (char*)dW + v * d * e, scale, s);
+    if (dW) launch_xent_dw(c.dtype, c.T, (int)d, xp.cols, dl, ld, xp_, (char*)dW + v * d * e, scale, w + p.part, s);
   }
 }
 

@@ -116,11 +116,14 @@ def test_no_tokens():
         dW1, dW2 = W.clone(), W.clone()
         L.moe_sorted_bwd_dw(cfg, rb, re, e(0, 64), e(0, 64), e(0, 64), e(0, 64), dW1, dW2)
         assert not dW1.any() and not dW2.any()
+        dWg, f0 = torch.full((5, 64), 3.0, device="cuda"), e(0, dtype=torch.float32)
+        L.moe_sorted_bwd_dw(cfg, rb, re, e(0, 64), e(0, 64), e(0, 64), e(0, 64), dW1, dW2, None, e(0, 64), f0, dWg)
+        assert not dWg.any()
 
 
 FFN = [(1, 64, 64, 1, 1, "relu", "plain"), (5, 64, 128, 96, 3, "gelu_tanh", "plain"), (48, 256, 512, 16, 2, "gelu_tanh", "plain"),
        (333, 128, 192, 7, 2, "gelu_erf", "dropped"), (700, 192, 64, 130, 4, "relu", "twice"),
-       (1025, 320, 576, 4, 1, "gelu_tanh", "one"), (2500, 512, 1024, 8, 2, "gelu_tanh", "plain"), (64, 64, 64, 3, 2, "identity", "none")]
+       (1025, 320, 576, 4, 1, "gelu_tanh", "one"), (2500, 512, 1024, 8, 2, "gelu_tanh", "plain"), (64, 64, 64, 3, 2, "identity", "none"), (50, 64, 64, 2, 5, "relu", "twice")]
 
 
 @pytest.mark.parametrize("dtype,wpacked", [("bf16", 0), ("bf16", 1), ("f32", 0)])

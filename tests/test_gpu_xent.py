@@ -34,7 +34,8 @@ def _run(x, W, target, dloss, dtype, want_dx=True, want_dW=True, fill=7.0):
 
 
 CASES = [(1, 1, 64), (1, 2, 128), (1, 50257, 64), (3, 63, 64), (17, 64, 320), (64, 65, 64), (65, 257, 192), (100, 20011, 128),
-         (257, 1000, 64), (1000, 5003, 128), (1025, 777, 64), (2100, 12345, 64), (4096, 512, 256), (300, 3, 1024)]
+         (257, 1000, 64), (1000, 5003, 128), (1025, 777, 64), (2100, 12345, 64), (4096, 512, 256), (300, 3, 1024), (9001, 100, 64),
+         (5000, 1281, 320), (2049, 33, 128)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
