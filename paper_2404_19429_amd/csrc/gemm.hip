@@ -833,7 +833,8 @@ void launch_xent_dx_whole(int64_t T, int d, int cols, const void* dl, int ld, co
   const int64_t large = (T + 255) / 256 * ((d + 255) / 256);
   WideCall w = xent_call(WK_KN_RM, T, d, p);
   // (the split: its share of a 256-tile's steps, and 30 us for 64 MB of partial tiles written, read and summed; with few
-  // classes smaller whole tiles take less)
+  // classes smaller whole tiles take less.  Whole backward, us, never split and always: 2000 classes of 1024 tokens of
+  // width 512 49 and 82, 5000 90 and 109, 10000 117 and 111; of 2048 of width 2048 362 and 322; 20000 of 64 157 and 74)
   const int cus = num_cus();
   const double split = ld / 32. * 650. * large / cus + 30000.;
   if (4 * large <= cus && split < tile_cost(kTilesM[tile_m(w, cus)], w, cus)) {
