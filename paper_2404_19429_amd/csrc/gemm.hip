@@ -29,9 +29,13 @@ namespace lmoe {
 
 // ------------------------------------------------------------------ f32 path
 // v_mfma_f32_16x16x4_f32 over LDS tiles, float in, float accumulation.  Bound:
-// the matrix cores' float rate (157 TFLOP/s nominal); an MFMA takes 32 cycles
-// for two 4-byte operands per lane, so plain loads (global -> registers -> LDS,
-// one stage ahead) and LDS reads hide under it.  Training step of 2000 tokens
+// the matrix cores' float rate (157 TFLOP/s nominal; 119 reached on 4096 x 16384
+// x 2048); an MFMA takes 32 cycles for two 4-byte operands per lane, so plain
+// loads (global -> registers -> LDS, one stage ahead) and LDS reads hide under
+// it where a wave's own MFMAs stand between them and their use: with reads, then
+// MFMAs, stage by stage, waves of a SIMD in turn had them busy 72 % of the time
+// (113 TFLOP/s).  Unpadded LDS rows for five blocks a CU in place of four need
+// more addresses than 96 registers hold (108).  Training step of 2000 tokens
 // (d 512, f 2048, 8 experts, one MI355X), against a 64 x 64 tile of vector
 // multiply-adds: H 191 -> 113 us, expert_out 358 -> 125, each dW 146 -> 104 (81
 // TFLOP/s); a 128-tile was slower on all but dW (its ragged rows and rounds).
@@ -74,11 +78,12 @@ struct F32Tile {
   }
   // To LDS, K at and past klim as zeros.  KC: within 16 of K, k = 4 s + q goes
   // to place 4 q + s, so that a lane's elements of four MFMAs are one 16-byte read.
+  template <bool WHOLE>
   __device__ static void store(const f32x4 (&v)[NLD], float* st, int k0, int klim) {
 #pragma unroll
     for (int i = 0; i < NLD; ++i) {
       const int c = threadIdx.x + 256 * i;
-      const f32x4 x = k0 + kofs(i) < klim ? v[i] : f32x4{0.f, 0.f, 0.f, 0.f};
+      const f32x4 x = WHOLE || k0 + kofs(i) < klim ? v[i] : f32x4{0.f, 0.f, 0.f, 0.f};
       if constexpr (KC) {
         float* o = st + c / W * LD + (c % W >> 2) * 16 + (c & 3);
 #pragma unroll
@@ -126,7 +131,7 @@ __device__ __forceinline__ void f32_store(const KernParams<EPI>& p, int64_t off,
 // Ragged-K (tiles as long as their group): rows of tn tiles are dealt to the
 // XCDs in turn, so a few large experts still spread over the chip.
 template <int WT, bool B_K, bool RAGGED_K, int EPI>
-__global__ __launch_bounds__(256) void gemm_f32_kernel(KernParams<EPI> p, int tm, int tn, int groups) {
+__global__ __launch_bounds__(256, 4) void gemm_f32_kernel(KernParams<EPI> p, int tm, int tn, int groups) {
   using TA = F32Tile<WT, !RAGGED_K>;
   using TB = F32Tile<WT, B_K && !RAGGED_K>;
   constexpr int BM = TA::ROWS, BK = TA::BK;
@@ -175,42 +180,65 @@ __global__ __launch_bounds__(256) void gemm_f32_kernel(KernParams<EPI> p, int tm
   TB tb;
   ta.plan(Ab, p.lda, m0, Alim);
   tb.plan(Bb, p.ldb, n0, Blim);
-  if (Klim > 0) {
-    ta.load(va, p.lda, 0, Klim);
-    tb.load(vb, p.ldb, 0, KlimB);
-  }
-  int buf = 0;
-  for (int k0 = 0; k0 < Klim; k0 += BK, buf ^= 1) {
-    TA::store(va, As[buf], k0, Klim);
-    TB::store(vb, Bs[buf], k0, KlimB);
-    __syncthreads();   // this stage is in LDS; every wave is past the stage before (the other buffer)
-    // The next stage's loads, in flight under this stage's MFMAs (past the last
-    // stage: one that is not stored).  The opaque start keeps the compiler from
-    // moving them to their use at the top of the loop.
-    int kn = k0 + BK;
-    asm volatile("" : "+s"(kn));
-    ta.load(va, p.lda, kn, Klim);
-    tb.load(vb, p.ldb, kn, KlimB);
+  auto load = [&](int k0) {
+    ta.load(va, p.lda, k0, Klim);
+    tb.load(vb, p.ldb, k0, KlimB);
+  };
+  auto store = [&](int k0, int buf) {
+    if (k0 + BK <= KlimB) {   // (not the last of either operand)
+      TA::template store<true>(va, As[buf], k0, Klim);
+      TB::template store<true>(vb, Bs[buf], k0, KlimB);
+    } else {
+      TA::template store<false>(va, As[buf], k0, Klim);
+      TB::template store<false>(vb, Bs[buf], k0, KlimB);
+    }
+  };
+  constexpr int KB = BK / 16;
+  f32x4 fa[2][WT], fb[2][WT];
+  auto frags = [&](int kb, int buf) {
+#pragma unroll
+    for (int i = 0; i < WT; ++i) fa[kb & 1][i] = TA::frag(As[buf], wm + 16 * i, kb, lane);
+#pragma unroll
+    for (int j = 0; j < WT; ++j) fb[kb & 1][j] = TB::frag(Bs[buf], wn + 16 * j, kb, lane);
+  };
+  auto half = [&](int kb, int h) {
+#pragma unroll
+    for (int s = 2 * h; s < 2 * h + 2; ++s)
+#pragma unroll
+      for (int i = 0; i < WT; ++i)
+#pragma unroll
+        for (int j = 0; j < WT; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fb[kb & 1][j][s], fa[kb & 1][i][s], acc[i][j], 0, 0, 0);
     __builtin_amdgcn_sched_barrier(0);
-    constexpr int KB = BK / 16;
-    f32x4 fa[KB][WT], fb[KB][WT];
+  };
+  if (Klim > 0) {
+    load(0);
+    store(0, 0);
+    load(BK);
+    __syncthreads();
+    frags(0, 0);
+  }
+  // Nothing is waited for next to what asks for it: under the MFMAs of 16 of K the fragments of the next 16 come from
+  // LDS, under the first the next stage goes there and the one after it is asked for (one past the last is not stored),
+  // and the barrier (the next stage is in LDS; every wave is past its reads of the stage before this) stands ahead of the
+  // last eight, with the next stage's first fragments.
+  for (int k0 = 0, buf = 0; k0 < Klim; k0 += BK, buf ^= 1) {
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
-#pragma unroll
-      for (int i = 0; i < WT; ++i) fa[kb][i] = TA::frag(As[buf], wm + 16 * i, kb, lane);
-#pragma unroll
-      for (int j = 0; j < WT; ++j) fb[kb][j] = TB::frag(Bs[buf], wn + 16 * j, kb, lane);
+      if (kb + 1 < KB) frags(kb + 1, buf);
+      __builtin_amdgcn_sched_barrier(0);
+      half(kb, 0);
+      if (kb == 0 && k0 + BK < Klim) {
+        store(k0 + BK, buf ^ 1);
+        load(k0 + 2 * BK);
+      }
+      if (kb == KB - 1 && k0 + BK < Klim) {
+        __syncthreads();
+        frags(0, buf ^ 1);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      half(kb, 1);
     }
-    __builtin_amdgcn_sched_barrier(0);   // the stage's reads together, ahead of its MFMAs
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-      for (int s = 0; s < 4; ++s)
-#pragma unroll
-        for (int i = 0; i < WT; ++i)
-#pragma unroll
-          for (int j = 0; j < WT; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fb[kb][j][s], fa[kb][i][s], acc[i][j], 0, 0, 0);
   }
   if constexpr (EPI == EPI_LSE) {
     xent_lse_rows<WT, WT>(p.x, acc, m0 + wm, n0 + wn, Mlim, p.x.block0 + n0 / BM * 2 + (wid & 1), lane);
