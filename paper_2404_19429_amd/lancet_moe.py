@@ -216,6 +216,23 @@ def _stream(stream) -> int:
     return int(stream)
 
 
+def _torch_stream(stream) -> torch.cuda.Stream:
+    """The torch stream of whatever an entry point takes as its stream (None: the current one)."""
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    if stream is None:
+        return torch.cuda.current_stream()
+    handle = int(stream)
+    return torch.cuda.ExternalStream(handle) if handle else torch.cuda.default_stream()
+
+
+def _wait_for(stream, earlier):
+    """What is called on `stream` from here on runs after what is on `earlier` so far."""
+    ev = torch.cuda.Event()
+    ev.record(_torch_stream(earlier))
+    _torch_stream(stream).wait_event(ev)
+
+
 def _check(st: int):
     if st != MOE_OK:
         raise MoeError(st, _lib.moe_last_error().decode())
@@ -587,9 +604,7 @@ def layer_backward(b: LayerBuffers, x, Wg, dy, stream=None, dw_stream=None, rout
         moe_bwd_dx(c, Wg, b.logits, b.idx, b.w, b.slot, b.carry, b.fill, b.H, b.O, b.W1p, b.W2p, dy, b.dO, b.dH, b.dXe,
                    b.dlogits, b.dx, b.ws_dx, stream)
     if dw_stream is not None:
-        ev = torch.cuda.Event()
-        ev.record(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.current_stream())
-        dw_stream.wait_event(ev)
+        _wait_for(dw_stream, stream)
     moe_bwd_dw(c, x, b.dlogits, b.carry, b.fill, b.send_buf, b.A, b.dO, b.dH, b.dW1, b.dW2, b.dWg, b.ws_dw,
                dw_stream if dw_stream is not None else stream)
 
@@ -670,9 +685,7 @@ def sorted_layer_backward(b: SortedBuffers, x, Wg, dy, stream=None, dw_stream=No
     moe_sorted_bwd_dx(c, b.row_begin, b.row_end, b.H, b.W1p, b.W2p, b.dO, b.dH, b.dXe, b.ws, stream)
     moe_sorted_dispatch_bwd(c, b.slot, b.dXe, b.dx, Wg, b.dlogits, stream)
     if dw_stream is not None:
-        ev = torch.cuda.Event()
-        ev.record(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.current_stream())
-        dw_stream.wait_event(ev)
+        _wait_for(dw_stream, stream)
     moe_sorted_bwd_dw(c, b.row_begin, b.row_end, b.rows, b.A, b.dO, b.dH, b.dW1, b.dW2, b.ws_dw, x, b.dlogits, b.dWg,
                       dw_stream if dw_stream is not None else stream)
 
