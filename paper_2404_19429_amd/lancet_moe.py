@@ -39,6 +39,8 @@ EXPORTS = ["moe_capacity", "moe_workspace_bytes", "moe_last_error", "moe_gate_to
            "moe_embed_bwd_workspace_bytes", "moe_embed_bwd", "moe_xent_workspace_bytes", "moe_xent", "moe_xent_bwd"]
 #: The expert products moe_product_times reports, in its order.
 PRODUCTS = ["fwd1", "fwd2", "dA", "dXe", "dW2", "dW1"]
+#: Experts and choices that the gate (moe_gate_topk) takes; moe_route and the moe_sorted_* calls take 512 and 16.
+GATE_MAX_E, GATE_MAX_K = 64, 8
 MOE_BLOCK_FWD, MOE_BLOCK_BWD, MOE_BLOCK_TIMED = 1, 2, 4
 #: The block backward's operations (moe_block_op): the chain 0..7, the weight-gradient groups 8..13.
 BLOCK_OPS = ["combine_bwd", "expert_dx", "dispatch_bwd", "ln2_bwd", "dattn", "attn_bwd", "da", "ln1_bwd",
@@ -643,10 +645,15 @@ class SortedBuffers:
 
 
 def alloc_sorted(cfg: moe_sorted_cfg, renorm=1, device="cuda") -> SortedBuffers:
-    """E <= 64 and k <= 8, as the gate takes them."""
+    """E <= GATE_MAX_E and k <= min(E, GATE_MAX_K), as the gate takes them (MoeError otherwise).  More experts or
+    choices: the moe_sorted_* calls themselves, with choices from elsewhere (moe_route)."""
     T, d, f, E, k, R = cfg.T, cfg.d_model, cfg.d_ff, cfg.E, cfg.k, moe_sorted_rows(cfg)
     if R < 0:
         raise MoeError(MOE_ESHAPE, moe_last_error())
+    if E > GATE_MAX_E:
+        raise MoeError(MOE_ESHAPE, f"alloc_sorted: the step's gate takes up to {GATE_MAX_E} experts, E={E}")
+    if k > min(E, GATE_MAX_K):
+        raise MoeError(MOE_EINVAL, f"alloc_sorted: the step's gate takes k up to min(E, {GATE_MAX_K}), k={k}")
     gate = make_cfg(T, d, f, E, k, 1, 1, cfg.dtype, cfg.act, renorm, cfg.wpacked)
     dt, f32, i32 = torch_dtype(gate), torch.float32, torch.int32
     e = lambda *s, dtype=dt: torch.empty(*s, dtype=dtype, device=device)
