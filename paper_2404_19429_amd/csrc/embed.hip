@@ -78,7 +78,7 @@ static EmbedPlan embed_plan(const moe_embed_cfg& c) {
     p.key[i] = take((size_t)c.T * 4);
     p.tok[i] = take((size_t)c.T * 4);
   }
-  p.counts = take((size_t)p.tiles * (1 << p.bits) * 4);
+  p.counts = take((size_t)sort_counts(p.tiles, 1 << p.bits) * 4);
   p.part = take((size_t)p.runs * 2 * c.d_model * 4);
   p.bytes = at;
   return p;
@@ -328,6 +328,7 @@ void launch_embed_bwd(const moe_embed_cfg& c, const int32_t* ids, const void* dy
       tok = (int32_t*)(w + p.tok[q & 1]);
       hipLaunchKernelGGL(embed_count_kernel<NT>, dim3(grid), dim3(NT), 0, s, dg, c.T, D, counts, p.tiles, z, za(2 * q),
                          za(2 * q + 1));
+      launch_sort_scan(counts, p.tiles, D, s);
       hipLaunchKernelGGL(embed_place_kernel<NT>, dim3(grid), dim3(NT), 0, s, dg, from, c.T, D, counts, p.tiles, key, tok, z,
                          za(2 * q + 1), za(2 * q + 2));
     }

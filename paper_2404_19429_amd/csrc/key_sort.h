@@ -7,8 +7,10 @@
 // 4 NT items, its waves 256 each, in order; a wave takes 64 at a time and finds
 // the lanes of the same key with one ballot per key bit.  One tile is one launch;
 // past that the tiles' counts come from a launch before it, and every block sums
-// those of the tiles before its own (D numbers a tile, L2-resident).  Integers
-// only, no atomics on device memory: the same positions every time.
+// those of the tiles before its own: D numbers a tile, tiles^2 D reads in all, out of
+// the L2s while they are few megabytes.  Past kSortSumTiles tiles a launch between
+// the two turns the counts into those sums (sort_scan), so that the work grows with
+// the items.  Integers only, no atomics on device memory: the same positions every time.
 //
 // A block is a chain of latencies (keys, the tiles' counts, barriers, scattered
 // stores of a line a lane), so small tiles on many CUs are the faster ones until
@@ -28,6 +30,11 @@ inline int64_t sort_tiles(int64_t n) {
   const int64_t tile = kSortRounds * sort_threads(n);
   return (n + tile - 1) / tile;
 }
+// Tiles up to which every block sums the others' counts.  Lookup gradient of 2^21 + 1 tokens (513 tiles), 500 ids of
+// width 8: 280 us summed, 213 scanned; of 2^26 43 ms and 7.3; the smaller batches are as they were.
+constexpr int64_t kSortSumTiles = 512;
+// Numbers of `counts`: D a tile, and where they are scanned the keys' totals behind them.
+inline int64_t sort_counts(int64_t tiles, int D) { return (tiles + (tiles > kSortSumTiles ? 1 : 0)) * D; }
 
 // Lanes whose item has the same key (of `bits` bits) as this lane's.
 __device__ __forceinline__ uint64_t same_key(int key, int bits) {
@@ -61,6 +68,47 @@ __device__ __forceinline__ void sort_count(const Key& key, int64_t N, int D, int
   for (int e = threadIdx.x; e < D; e += NT) counts[tile * D + e] = hist[e];
 }
 
+// counts[tile][key] -> the sums over the tiles before it, and the keys' totals behind
+// the last tile's.  A block takes kScanKeys keys by kScanParts shares of the tiles,
+// whose sums meet in LDS.
+constexpr int kScanKeys = 16, kScanParts = 64;
+static __global__ __launch_bounds__(kScanKeys * kScanParts) void sort_scan_kernel(int32_t* __restrict__ counts, int64_t tiles, int D) {
+  __shared__ int32_t sum[kScanParts][kScanKeys];
+  const int q = threadIdx.x % kScanKeys, part = threadIdx.x / kScanKeys;
+  const int e = blockIdx.x * kScanKeys + q;
+  const int64_t share = (tiles + kScanParts - 1) / kScanParts;
+  const int64_t a = min(tiles, part * share), b = e < D ? min(tiles, a + share) : a;
+  constexpr int U = 8;   // tiles in flight
+  int32_t n[U];
+  int32_t mine = 0;
+  for (int64_t t = a; t < b; t += U) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) n[u] = t + u < b ? counts[(t + u) * D + e] : 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) mine += n[u];
+  }
+  sum[part][q] = mine;
+  __syncthreads();
+  int32_t run = 0;
+  for (int p = 0; p < part; ++p) run += sum[p][q];
+  for (int64_t t = a; t < b; t += U) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) n[u] = t + u < b ? counts[(t + u) * D + e] : 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (t + u < b) counts[(t + u) * D + e] = run;
+      run += n[u];
+    }
+  }
+  if (part == kScanParts - 1 && e < D) counts[tiles * D + e] = run;
+}
+// The launch between counting and placing, if there is one.
+inline void launch_sort_scan(int32_t* counts, int64_t tiles, int D, hipStream_t s) {
+  if (tiles > kSortSumTiles)
+    hipLaunchKernelGGL(sort_scan_kernel, dim3((unsigned)((D + kScanKeys - 1) / kScanKeys)), dim3(kScanKeys * kScanParts), 0, s,
+                       counts, tiles, D);
+}
+
 template <int NT>
 struct SortLds {
   static constexpr int W = NT / kWave;
@@ -88,7 +136,14 @@ __device__ __forceinline__ void sort_place(const Key& key, const Emit& emit, int
 #pragma unroll
   for (int h = 0; h < KT; ++h) run[h] = total[h] = 0;
   const int e0 = threadIdx.x * KT;
-  if (tiles > 1 && e0 < D) {
+  if (tiles > kSortSumTiles) {   // (sums already)
+#pragma unroll
+    for (int h = 0; h < KT; ++h)
+      if (e0 + h < D) {
+        run[h] = counts[tile * D + e0 + h];
+        total[h] = counts[tiles * D + e0 + h];
+      }
+  } else if (tiles > 1 && e0 < D) {
     constexpr int U = 8;   // tiles whose counts are read together
     for (int64_t t = 0; t < tiles; t += U) {
       int n[U][KT];

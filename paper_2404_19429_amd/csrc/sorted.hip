@@ -65,7 +65,7 @@ __global__ __launch_bounds__(NT) void sorted_place_kernel(const int32_t* __restr
 
 size_t sorted_dispatch_ws_bytes(const moe_sorted_cfg& c) {
   const int64_t tiles = sort_tiles(c.T * c.k);
-  return tiles > 1 ? (size_t)tiles * c.E * sizeof(int32_t) : 0;
+  return tiles > 1 ? (size_t)sort_counts(tiles, c.E) * sizeof(int32_t) : 0;
 }
 
 // ---------------------------------------------------------------------- gather
@@ -155,6 +155,7 @@ void launch_sorted_dispatch(const moe_sorted_cfg& c, const void* x, const int32_
     constexpr int NT = decltype(nt)::value;
     if (tiles > 1)
       hipLaunchKernelGGL(sorted_count_kernel<NT>, dim3((unsigned)tiles), dim3(NT), 0, s, idx, N, c.E, counts);
+    launch_sort_scan(counts, tiles, c.E, s);
     hipLaunchKernelGGL(sorted_place_kernel<NT>, dim3((unsigned)tiles), dim3(NT), 0, s, idx, N, c.E, align, R, counts, row_begin,
                        row_end, slot, src);
   };
