@@ -31,9 +31,11 @@ void launch_embed(const moe_embed_cfg& c, const int32_t* ids, const void* W, voi
   if (c.T == 0) return;
   auto go = [&](auto tag, auto stream) {
     using T = decltype(tag);
-    const int64_t n = c.T * (c.d_model / Vec<T>::N);
-    hipLaunchKernelGGL((embed_kernel<T, decltype(stream)::value>), dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, ids,
-                       (const T*)W, (T*)y, c.T, c.V, c.d_model, c.scale);
+    const int64_t nc = c.d_model / Vec<T>::N;
+    each_launch(c.T, nc, [&](int64_t t0, int64_t n) {
+      hipLaunchKernelGGL((embed_kernel<T, decltype(stream)::value>), dim3((unsigned)((n * nc + 255) / 256)), dim3(256), 0, s,
+                         ids + t0, (const T*)W, (T*)y + t0 * c.d_model, n, c.V, c.d_model, c.scale);
+    });
   };
   auto type = [&](auto stream) {
     if (c.dtype == MOE_BF16) go(uint16_t{}, stream);
@@ -186,15 +188,15 @@ __device__ __forceinline__ void embed_row(T* dW, int64_t at, const float (&acc)[
 template <typename T>
 __global__ __launch_bounds__(256) void embed_runs_kernel(const int32_t* __restrict__ key, const int32_t* __restrict__ tok,
                                                          const T* __restrict__ dy, T* __restrict__ dW,
-                                                         float* __restrict__ part, int64_t N, int64_t runs, int V_rows, int d,
-                                                         float scale, int accum) {
+                                                         float* __restrict__ part, int64_t N, int64_t run0, int64_t runs,
+                                                         int V_rows, int d, float scale, int accum) {
   constexpr int V = Vec<T>::N;
   typedef int i32x4 __attribute__((ext_vector_type(4)));
   const int nc = d / V;
   const int64_t gid = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-  const int64_t run = gid / nc;
+  const int64_t local = gid / nc, run = run0 + local;   // of the launch's runs, run0 .. runs - 1
   if (run >= runs) return;
-  const int c = (int)(gid - run * nc) * V;
+  const int c = (int)(gid - local * nc) * V;
   const int64_t j0 = run * kRun;
   const int n = (int)min((int64_t)kRun, N - j0);   // the run's tokens
   int k[kRun + 1], t[kRun];
@@ -246,11 +248,11 @@ __global__ __launch_bounds__(256) void embed_runs_kernel(const int32_t* __restri
 constexpr int kJoinCols = 64;
 template <typename T>
 __global__ __launch_bounds__(4 * kJoinCols) void embed_join_kernel(const int32_t* __restrict__ key, T* __restrict__ dW,
-                                                                   const float* __restrict__ part, int64_t N, int64_t runs,
-                                                                   int V_rows, int d, int slabs, float scale, int accum) {
+                                                                   const float* __restrict__ part, int64_t N, int64_t run0,
+                                                                   int64_t runs, int V_rows, int d, int slabs, float scale, int accum) {
   constexpr int V = Vec<T>::N;
   __shared__ f32x4 red[3][kJoinCols][V / 4];
-  const int64_t run = (int64_t)blockIdx.x / slabs;
+  const int64_t run = run0 + (int64_t)blockIdx.x / slabs;
   const int64_t j0 = run * kRun, j1 = j0 + kRun;
   if (j1 >= N) return;
   const int cur = key[j1 - 1];
@@ -347,12 +349,14 @@ void launch_embed_bwd(const moe_embed_cfg& c, const int32_t* ids, const void* dy
   auto go = [&](auto tag) {
     using T = decltype(tag);
     const int nc = c.d_model / Vec<T>::N, slabs = (nc + kJoinCols - 1) / kJoinCols;
-    const int64_t n = p.runs * nc;
-    hipLaunchKernelGGL(embed_runs_kernel<T>, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, key, tok, (const T*)dy,
-                       (T*)dW, (float*)(w + p.part), c.T, p.runs, c.V, c.d_model, c.scale, c.accum);
-    if (p.runs > 1)
-      hipLaunchKernelGGL(embed_join_kernel<T>, dim3((unsigned)((p.runs - 1) * slabs)), dim3(4 * kJoinCols), 0, s, key, (T*)dW,
-                         (const float*)(w + p.part), c.T, p.runs, c.V, c.d_model, slabs, c.scale, c.accum);
+    each_launch(p.runs, nc, [&](int64_t r0, int64_t n) {
+      hipLaunchKernelGGL(embed_runs_kernel<T>, dim3((unsigned)((n * nc + 255) / 256)), dim3(256), 0, s, key, tok, (const T*)dy,
+                         (T*)dW, (float*)(w + p.part), c.T, r0, r0 + n, c.V, c.d_model, c.scale, c.accum);
+    });
+    each_launch(p.runs - 1, (int64_t)slabs * 4 * kJoinCols, [&](int64_t r0, int64_t n) {
+      hipLaunchKernelGGL(embed_join_kernel<T>, dim3((unsigned)(n * slabs)), dim3(4 * kJoinCols), 0, s, key, (T*)dW,
+                         (const float*)(w + p.part), c.T, r0, p.runs, c.V, c.d_model, slabs, c.scale, c.accum);
+    });
   };
   if (c.dtype == MOE_BF16) go(uint16_t{});
   else go(float{});

@@ -41,6 +41,15 @@ inline int num_cus() {
   return n;
 }
 
+// Threads of a launch at most: a dispatch counts them in 32 bits, and what is past 2^32 of them is left out without an
+// error.  What takes more goes in several launches.
+constexpr int64_t kMostThreads = (int64_t)1 << 31;
+// f(begin, count) for items 0 .. n - 1 of `threads` threads each, as many at a time as a launch takes.
+template <typename F> inline void each_launch(int64_t n, int64_t threads, F&& f) {
+  const int64_t most = std::max<int64_t>(1, kMostThreads / threads);
+  for (int64_t i = 0; i < n; i += most) f(i, std::min(most, n - i));
+}
+
 constexpr int kMaxK = 8;       // largest supported top-k
 constexpr int kMaxE = 64;      // largest supported expert count (one lane per expert in the gate)
 constexpr int kRouteChunk = 256;  // tokens per slot-assignment chunk
