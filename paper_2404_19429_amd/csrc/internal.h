@@ -41,8 +41,8 @@ inline int num_cus() {
   return n;
 }
 
-// Threads of a launch at most: a dispatch counts them in 32 bits, and what is past 2^32 of them is left out without an
-// error.  What takes more goes in several launches.
+// Threads of a launch at most.  A dispatch counts them in 32 bits: of 2^32 + n threads n run, without an error.  What
+// takes more goes in several launches.
 constexpr int64_t kMostThreads = (int64_t)1 << 31;
 // f(begin, count) for items 0 .. n - 1 of `threads` threads each, as many at a time as a launch takes.
 template <typename F> inline void each_launch(int64_t n, int64_t threads, F&& f) {

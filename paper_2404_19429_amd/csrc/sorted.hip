@@ -163,7 +163,7 @@ void launch_sorted_dispatch(const moe_sorted_cfg& c, const void* x, const int32_
     using T = decltype(tag);
     constexpr int U = 1;
     const int cols = (c.d_model + U * 8 * Vec<T>::N - 1) / (U * 8 * Vec<T>::N);
-    const int64_t waves = (R + 15) / 16 * cols;
+    const int64_t strips = (R + 15) / 16, waves = strips * cols;   // of sixteen rows
     if (tiles == 1 && N > 0) {
       const unsigned blocks = (unsigned)std::min<int64_t>(256, (waves + 3) / 4);
       hipLaunchKernelGGL((sorted_small_kernel<T, U>), dim3(blocks), dim3(kSortSmall), 0, s, (const T*)x, idx, (int)N, c.E, align,
@@ -173,8 +173,11 @@ void launch_sorted_dispatch(const moe_sorted_cfg& c, const void* x, const int32_
     if (sort_threads(N) == kSortSmall) place(std::integral_constant<int, kSortSmall>{});
     else place(std::integral_constant<int, kSortLarge>{});
     auto gather = [&](auto stream) {
-      hipLaunchKernelGGL((sorted_gather_kernel<T, U, decltype(stream)::value>), dim3((unsigned)((waves + 3) / 4)), dim3(256),
-                         0, s, (const T*)x, src, (T*)rows, R, N, c.d_model, c.k, cols);
+      each_launch(strips, (int64_t)cols * kWave, [&](int64_t b, int64_t n) {   // (rows of whole strips lie together)
+        hipLaunchKernelGGL((sorted_gather_kernel<T, U, decltype(stream)::value>), dim3((unsigned)((n * cols + 3) / 4)),
+                           dim3(256), 0, s, (const T*)x, src + 16 * b, (T*)rows + 16 * b * c.d_model,
+                           std::min(16 * n, R - 16 * b), N, c.d_model, c.k, cols);
+      });
     };
     if (R == 0) return;
     if (stream_bytes(R * c.d_model * (int64_t)sizeof(T))) gather(std::true_type{});
@@ -247,10 +250,13 @@ static void launch_back(const moe_sorted_cfg& c, const void* rows, const int32_t
   if (c.T == 0) return;
   auto go = [&](auto tag, auto gate, auto stream) {
     using T = decltype(tag);
-    const int64_t n = c.T * (c.d_model / Vec<T>::N);
-    hipLaunchKernelGGL((sorted_back_kernel<T, W, decltype(gate)::value, decltype(stream)::value>),
-                       dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, (const T*)rows, slot, w, (const T*)Wg, dl, (T*)y,
-                       c.T, sorted_rows(c), c.d_model, c.k, c.E);
+    const int64_t nc = c.d_model / Vec<T>::N;
+    each_launch(c.T, nc, [&](int64_t t0, int64_t n) {
+      hipLaunchKernelGGL((sorted_back_kernel<T, W, decltype(gate)::value, decltype(stream)::value>),
+                         dim3((unsigned)((n * nc + 255) / 256)), dim3(256), 0, s, (const T*)rows, slot + t0 * c.k,
+                         W ? w + t0 * c.k : nullptr, (const T*)Wg, dl ? dl + t0 * c.E : nullptr, (T*)y + t0 * c.d_model, n,
+                         sorted_rows(c), c.d_model, c.k, c.E);
+    });
   };
   auto type = [&](auto gate, auto stream) {
     if (c.dtype == MOE_BF16) go(uint16_t{}, gate, stream);
@@ -277,20 +283,20 @@ void launch_sorted_dispatch_bwd(const moe_sorted_cfg& c, const int32_t* slot, co
 // dO[row] = w dy[t], dw = <dy[t], O[row]> for the choice that the row holds.  A
 // block takes sixteen rows, each wave a run of columns of all of them (eight lanes
 // a row, as in the gather); the waves' dot products meet in LDS, in wave order.
-// The blocks past the rows write the zeros of the choices that have none.  Bound:
+// The blocks past the rows (of the first launch) write the zeros of the choices that have none.  Bound:
 // bytes, 336 MB in 67 us (traced; as above).
 template <typename T, int U, bool S>
 __global__ __launch_bounds__(256) void sorted_combine_bwd_kernel(const T* __restrict__ O, const int32_t* __restrict__ slot,
                                                                  const int32_t* __restrict__ src,
                                                                  const float* __restrict__ w, const T* __restrict__ dy,
                                                                  T* __restrict__ dO, float* __restrict__ dw, int64_t R,
-                                                                 int64_t N, int d, int k) {
+                                                                 int64_t all_rows, int64_t N, int d, int k) {
   constexpr int V = Vec<T>::N;
   __shared__ float part[4][16];
-  const int64_t rb = (R + 15) / 16;
+  const int64_t rb = (R + 15) / 16;   // R: the launch's rows, of all_rows
   if (blockIdx.x >= rb) {
     const int64_t i = ((int64_t)blockIdx.x - rb) * blockDim.x + threadIdx.x;
-    if (i < N && (slot[i] < 0 || slot[i] >= R)) dw[i] = 0.f;
+    if (i < N && (slot[i] < 0 || slot[i] >= all_rows)) dw[i] = 0.f;
     return;
   }
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -354,9 +360,12 @@ void launch_sorted_combine_bwd(const moe_sorted_cfg& c, const void* O, const int
   if (N == 0) return;
   auto go = [&](auto tag, auto stream) {
     using T = decltype(tag);
-    hipLaunchKernelGGL((sorted_combine_bwd_kernel<T, 2, decltype(stream)::value>),
-                       dim3((unsigned)((R + 15) / 16 + (N + 255) / 256)), dim3(256), 0, s, (const T*)O, slot, src, w,
-                       (const T*)dy, (T*)dO, dw, R, N, c.d_model, c.k);
+    each_launch((R + 15) / 16, 256, [&](int64_t b, int64_t n) {   // (beside N threads at most: together under 2^32)
+      const int64_t r0 = 16 * b, zeros = b == 0 ? (N + 255) / 256 : 0;
+      hipLaunchKernelGGL((sorted_combine_bwd_kernel<T, 2, decltype(stream)::value>), dim3((unsigned)(n + zeros)), dim3(256), 0, s,
+                         (const T*)O + r0 * c.d_model, slot, src + r0, w, (const T*)dy, (T*)dO + r0 * c.d_model, dw,
+                         std::min(16 * n, R - r0), R, N, c.d_model, c.k);
+    });
   };
   auto type = [&](auto stream) {
     if (c.dtype == MOE_BF16) go(uint16_t{}, stream);
