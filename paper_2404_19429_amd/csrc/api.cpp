@@ -844,7 +844,7 @@ moe_status check_xent(const moe_xent_cfg* c, const char* fn) {
   if (c->T > (int64_t)1 << 29 || (c->T + 15) * c->d_model >= (int64_t)1 << 29)
     return fail(MOE_ESHAPE, "%s: T * d_model must stay under 2^29", fn);
   if ((int64_t)c->V * c->d_model > (int64_t)1 << 40) return fail(MOE_ESHAPE, "%s: V * d_model above 2^40", fn);
-  if (c->T * c->V > (int64_t)1 << 42) return fail(MOE_ESHAPE, "%s: T * V above 2^42", fn);   // (2^30 tiles of 64 x 64)
+  if (c->T * c->V > (int64_t)1 << 42) return fail(MOE_ESHAPE, "%s: T * V above 2^42", fn);   // (tiles are counted in 32 bits)
   return MOE_OK;
 }
 

@@ -60,6 +60,10 @@ FwdPlan fwd_plan(const moe_xent_cfg& c) {
   p.form = fwd_form(c);
   const int64_t room = p.form == kXentBlocked ? kWBytes : kOperand - 1;
   p.cols = (int)std::min<int64_t>(c.V, std::max<int64_t>(256, room / (c.d_model * 2) / 256 * 256));
+  if (c.dtype == MOE_F32) {   // (the float product has a block of 256 threads for every 64 x 64 tile)
+    const int64_t tiles = kMostThreads / 256 / ((c.T + 15 + 63) / 64);
+    p.cols = (int)std::min<int64_t>(p.cols, std::max<int64_t>(1, tiles) * 64);
+  }
   const int run = xent_run_columns(c.dtype, c.T);
   const int64_t pieces = (c.V + p.cols - 1) / p.cols;
   p.blocks = (c.V + run - 1) / run + (int64_t)(512 / run) * pieces;   // (a piece is two products at most)
