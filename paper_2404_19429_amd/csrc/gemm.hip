@@ -806,8 +806,9 @@ size_t xent_slices_bytes(int64_t T, int d, int cols) {
   const int n = xent_slices(T, d, cols);
   return n > 1 ? (size_t)n * T * d * sizeof(float) : 0;
 }
+// (in may be out: a thread reads its four values of it before it writes them)
 __global__ __launch_bounds__(256) void xent_slices_kernel(const float* __restrict__ part, int n, int64_t size,
-                                                          const float* __restrict__ in, float* __restrict__ out) {
+                                                          const float* in, float* out) {
   const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
   if (i >= size) return;
   f32x4 v[16];
