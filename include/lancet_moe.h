@@ -553,8 +553,12 @@ typedef struct {
 } moe_xent_cfg;
 
 /* Bytes of device workspace moe_xent (backward = 0) or moe_xent_bwd (1) needs (host
- * only; 0 if none, 0 and a message on an invalid cfg).  Calls that overlap in time
- * need separate workspaces. */
+ * only; 0 if none, 0 and a message on an invalid cfg): forward 1/8 of a byte a logit for
+ * MOE_BF16 and 1/4 for MOE_F32, twice that up to 1024 tokens, and copies of x and of up to
+ * 128 MiB of W; backward up to 512 MiB (past 131072 bf16 or 65536 float tokens up to 2 or
+ * 4 GiB, past 2^23 tokens 64 columns of T) of the gradient at the logits, copies of x and,
+ * as many columns, of W, float sums of dx, and 64 MiB.  Calls that overlap in time need
+ * separate workspaces. */
 size_t moe_xent_workspace_bytes(const moe_xent_cfg* cfg, int32_t backward);
 
 /* x [T][d], W [V][d] dtype, target [T] int32 -> lse [T] float = log sum over v of

@@ -2,17 +2,21 @@
 // without keeping the logits, and its gradients.
 //
 //   forward: l = x W^T, lse = log sum exp l, loss = lse - l[target].  The product's
-//     epilogue leaves of each row and run of 32 or 64 columns the largest logit and
-//     the sum of exp(l - largest) (EPI_LSE), T V / 8 bytes at most where the logits
-//     were 4 T V; one launch joins them.
+//     epilogue leaves of each row and run of columns the largest logit and the sum of
+//     exp(l - largest) (EPI_LSE), 8 bytes; one launch joins them.  A run is what the
+//     narrowest tile allowed has in a wave: 64 columns in bfloat16, 32 in float, half of
+//     that up to 1024 tokens.  Where the logits were 4 T V bytes the runs are T V / 8
+//     (bfloat16), T V / 4 (float), twice that up to 1024 tokens.
 //   backward: dl = g (exp(l - lse) - [v = target]) in the type of x, computed again
 //     piece by piece (EPI_DL); dx += dl W in float over the pieces, dW = dl^T x.  dl's
 //     rounding to bfloat16 (relative to the largest g) is half a step of each, as of
 //     every operand of the products.
 //
-// A piece's dl takes kDlBytes at most.  Every piece reads and writes dx's float sums, so
-// fewer are faster (16384 tokens, 50257 classes, width 2048, bfloat16, one step: 128 MiB
-// 13.41 ms, 256 12.08, 512 11.77, 1024 11.53), and 512 MiB are a third of that dl.
+// A piece's dl takes kDlBytes, or 2048 columns where those are more (past 131072 tokens
+// of bfloat16, 65536 of float), but no more than the products address, 2 GiB (float: 4),
+// with 64 columns at the least.  Every piece reads and writes dx's float sums, so fewer are
+// faster (16384 tokens, 50257 classes, width 2048, bfloat16, one step: 128 MiB 13.41 ms, 256
+// 12.08, 512 11.77, 1024 11.53), and 512 MiB are a third of that dl.
 #include "gemm_wide.h"
 
 namespace lmoe {
