@@ -364,6 +364,11 @@ static int tile_m(const WideCall& w, int cus, int tiles = kTileCount) {
 // to one and a half rounds, and up to two where an idle launch (3 us) is little
 // against the product, both shapes are launched and the row counts pick the one that
 // runs.
+// A single group is as long as it is: no second launch.  Where the model has 256-tiles up
+// to 3 us ahead, they are for long groups, and 128-tiles stay for short ones, up to twice as
+// long where the operands are few slices.  128- against 256-tiles: 2048 rows (d 1280, f 6656) 54 and 60 us, (d 1536, f
+// 14080) 111 and 112; 3000 (d 768, f 12032) 79 and 78; 4096 (d 1792, f 5120) 94 and 101, (d 2816, f 3328) 97 and 102, (d 768,
+// f 12800) 106 and 102; 8192 (d 1024, f 10240) 210 and 192; 16384 (d 768, f 14080) 434 and 375.
 // The dense weight gradients' groups are token ranges of one length (w.expect): where
 // they are not short, 128-tiles take 3/4 of the time of a 256-tile round for the work
 // of 192 large tiles.  dW of 256 large tiles and 8192 rows each, 128- against
@@ -400,7 +405,7 @@ static TileK tile_k(const WideCall& w, int cus) {
   const int64_t slices = ((w.rows + 127) / 128 + (w.cols + 127) / 128) * w.groups;
   const double three = small > per ? 850. : slices <= 128 ? 780. : 1000.;
   const double c128 = 7000. + cost(small, per, three, 2000., rem <= cus ? 440. : rem <= 2 * cus ? 620. : three);
-  if (w.groups == 1) return c128 <= c256 ? kTileK128 : kTileK256;   // (one group is as long as it is)
+  if (w.groups == 1) return c128 <= c256 + (w.expect <= (slices <= 72 ? 4096. : 2048.) ? 3000. : 0.) ? kTileK128 : kTileK256;
   if (c128 <= c256 + 3000.) return kTileK128;
   return 2 * large <= 3 * cus || c256 >= 1e5 ? kTileKByRows : kTileK256;
 }
