@@ -67,7 +67,7 @@ typedef enum {
   MOE_EALIGN = -3,     /* a pointer not 16-byte aligned */
   MOE_EDTYPE = -4,     /* unknown dtype */
   MOE_EDEVICE = -5,    /* no HIP device, or the current device is not gfx950 */
-  MOE_ELAUNCH = -6,    /* the HIP runtime reported an error */
+  MOE_ELAUNCH = -6,    /* the HIP runtime reported an error, or the sizes need a launch of 2^32 threads or more */
   MOE_EWORKSPACE = -7  /* workspace missing or smaller than moe_workspace_bytes() */
 } moe_status;
 

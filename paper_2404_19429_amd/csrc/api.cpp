@@ -89,6 +89,7 @@ moe_status check_cfg(const moe_cfg* c, const char* fn, bool need_gemm_shape) {
 
 // One gfx950 check per device, then cached.
 moe_status check_device(const char* fn) {
+  lmoe::g_launch_refused = false;
   static thread_local int checked_dev = -1;
   int dev = -1;
   if (hipGetDevice(&dev) != hipSuccess) return fail(MOE_EDEVICE, "%s: no HIP device", fn);
@@ -102,6 +103,7 @@ moe_status check_device(const char* fn) {
 }
 
 moe_status check_launch(const char* fn) {
+  if (lmoe::g_launch_refused) return fail(MOE_ELAUNCH, "%s: these sizes need a launch of 2^32 threads or more", fn);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(MOE_ELAUNCH, "%s: %s", fn, hipGetErrorString(e));
   return ok();
@@ -956,7 +958,7 @@ moe_status moe_block_chunked(const moe_block_cfg* cfg, const moe_block_weights* 
   const hipStream_t st[3] = {(hipStream_t)streams[0], (hipStream_t)streams[1], (hipStream_t)streams[2]};
   const hipError_t e = lmoe::run_block(*cfg, *wts, grads, x, out, dy, dx, *acts, passes, n_chunks, st, ws);
   if (e != hipSuccess) return fail(MOE_ELAUNCH, "%s: %s", fn, hipGetErrorString(e));
-  return ok();
+  return check_launch(fn);
 }
 
 }  // extern "C"

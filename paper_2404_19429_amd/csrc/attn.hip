@@ -648,8 +648,8 @@ void launch_attn_fwd(const void* qkv, void* o, float* lse, int nseq, int S, int 
   const int nbh = nseq * H;
   const float c2 = kLog2e / sqrtf((float)kHD);
   auto go = [&](auto kern, int q) {
-    hipLaunchKernelGGL(kern, dim3((unsigned)((S + q - 1) / q * nbh)), dim3(256), 0, s, (const uint16_t*)qkv,
-                       (uint16_t*)o, (uint16_t*)o_blk, lse, S, attn_stat_stride(S), H, nbh, c2);
+    launch_kernel(kern, dim3((unsigned)((S + q - 1) / q * nbh)), dim3(256), 0, s, (const uint16_t*)qkv,
+                  (uint16_t*)o, (uint16_t*)o_blk, lse, S, attn_stat_stride(S), H, nbh, c2);
   };
   // 64 queries per block where 128 would not give every CU its two blocks: a
   // wave's chain per key tile is then half as long, on twice the CUs (500 tokens x 8
@@ -665,16 +665,16 @@ void launch_attn_bwd(const void* qkv, const void* o, const void* dout, const flo
   const int64_t T = (int64_t)nseq * S;
   const int64_t nthr = T * H * 16;
   const int Sp = attn_stat_stride(S);
-  hipLaunchKernelGGL(attn_delta_kernel, dim3((unsigned)((nthr + 255) / 256)), dim3(256), 0, s,
-                     (const uint16_t*)dout, (const uint16_t*)o, delta, T, S, Sp, H);
+  launch_kernel(attn_delta_kernel, dim3((unsigned)((nthr + 255) / 256)), dim3(256), 0, s,
+                (const uint16_t*)dout, (const uint16_t*)o, delta, T, S, Sp, H);
   const float scale = 1.f / sqrtf((float)kHD);
   const float c2 = kLog2e * scale;
   const int nq = (S + kDqQ - 1) / kDqQ;
-  hipLaunchKernelGGL(attn_dq_kernel, dim3((unsigned)(nq * nbh)), dim3(256), 0, s, (const uint16_t*)qkv,
-                     (const uint16_t*)dout, lse, delta, (uint16_t*)dqkv, (uint16_t*)dqkv_blk, S, Sp, H, nbh, c2, scale);
+  launch_kernel(attn_dq_kernel, dim3((unsigned)(nq * nbh)), dim3(256), 0, s, (const uint16_t*)qkv,
+                (const uint16_t*)dout, lse, delta, (uint16_t*)dqkv, (uint16_t*)dqkv_blk, S, Sp, H, nbh, c2, scale);
   const int nk = (S + kKvK - 1) / kKvK;
-  hipLaunchKernelGGL(attn_dkdv_kernel, dim3((unsigned)(nk * nbh)), dim3(256), 0, s, (const uint16_t*)qkv,
-                     (const uint16_t*)dout, lse, delta, (uint16_t*)dqkv, (uint16_t*)dqkv_blk, S, Sp, H, nbh, c2, scale);
+  launch_kernel(attn_dkdv_kernel, dim3((unsigned)(nk * nbh)), dim3(256), 0, s, (const uint16_t*)qkv,
+                (const uint16_t*)dout, lse, delta, (uint16_t*)dqkv, (uint16_t*)dqkv_blk, S, Sp, H, nbh, c2, scale);
 }
 
 }  // namespace lmoe

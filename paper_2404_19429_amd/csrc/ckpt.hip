@@ -270,14 +270,14 @@ static dim3 ckpt_grid(const CkptArgs& a) { return dim3((unsigned)std::min<int64_
 void launch_ckpt_save(const moe_cfg& c, const void* send, const void* H, const void* O, const int32_t* rb,
                       const int32_t* re, void* ckpt, hipStream_t s) {
   const CkptArgs a = ckpt_args(c, send, H, nullptr, O, rb, re, ckpt);
-  if (c.dtype == MOE_BF16) hipLaunchKernelGGL(ckpt_save_kernel<uint16_t>, ckpt_grid(a), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(ckpt_save_kernel<float>, ckpt_grid(a), dim3(256), 0, s, a);
+  if (c.dtype == MOE_BF16) launch_kernel(ckpt_save_kernel<uint16_t>, ckpt_grid(a), dim3(256), 0, s, a);
+  else launch_kernel(ckpt_save_kernel<float>, ckpt_grid(a), dim3(256), 0, s, a);
 }
 
 void launch_ckpt_load(const moe_cfg& c, const void* ckpt, const int32_t* rb, const int32_t* re, void* send, void* H,
                       void* A, void* O, hipStream_t s) {
   const CkptArgs a = ckpt_args(c, send, H, A, O, rb, re, ckpt);
-  auto go = [&](auto kern) { hipLaunchKernelGGL(kern, ckpt_grid(a), dim3(256), 0, s, a); };
+  auto go = [&](auto kern) { launch_kernel(kern, ckpt_grid(a), dim3(256), 0, s, a); };
   auto pick = [&](auto tag) {
     using T = decltype(tag);
     switch (c.act) {

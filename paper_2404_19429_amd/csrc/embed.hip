@@ -33,8 +33,8 @@ void launch_embed(const moe_embed_cfg& c, const int32_t* ids, const void* W, voi
     using T = decltype(tag);
     const int64_t nc = c.d_model / Vec<T>::N;
     each_launch(c.T, nc, [&](int64_t t0, int64_t n) {
-      hipLaunchKernelGGL((embed_kernel<T, decltype(stream)::value>), dim3((unsigned)((n * nc + 255) / 256)), dim3(256), 0, s,
-                         ids + t0, (const T*)W, (T*)y + t0 * c.d_model, n, c.V, c.d_model, c.scale);
+      launch_kernel((embed_kernel<T, decltype(stream)::value>), dim3((unsigned)((n * nc + 255) / 256)), dim3(256), 0, s,
+                    ids + t0, (const T*)W, (T*)y + t0 * c.d_model, n, c.V, c.d_model, c.scale);
     });
   };
   auto type = [&](auto stream) {
@@ -311,7 +311,7 @@ void launch_embed_bwd(const moe_embed_cfg& c, const int32_t* ids, const void* dy
   u32x4* z = (u32x4*)dW;
   if (c.T == 0) {
     if (zeros)
-      hipLaunchKernelGGL(embed_pairs_kernel, dim3(zblocks), dim3(256), 0, s, ids, 0, c.V, 0, nullptr, nullptr, z, zeros);
+      launch_kernel(embed_pairs_kernel, dim3(zblocks), dim3(256), 0, s, ids, 0, c.V, 0, nullptr, nullptr, z, zeros);
     return;
   }
   const EmbedPlan p = embed_plan(c);
@@ -328,19 +328,19 @@ void launch_embed_bwd(const moe_embed_cfg& c, const int32_t* ids, const void* dy
       const int32_t* from = q ? tok : nullptr;
       key = (int32_t*)(w + p.key[q & 1]);
       tok = (int32_t*)(w + p.tok[q & 1]);
-      hipLaunchKernelGGL(embed_count_kernel<NT>, dim3(grid), dim3(NT), 0, s, dg, c.T, D, counts, p.tiles, z, za(2 * q),
-                         za(2 * q + 1));
+      launch_kernel(embed_count_kernel<NT>, dim3(grid), dim3(NT), 0, s, dg, c.T, D, counts, p.tiles, z, za(2 * q),
+                    za(2 * q + 1));
       launch_sort_scan(counts, p.tiles, D, s);
-      hipLaunchKernelGGL(embed_place_kernel<NT>, dim3(grid), dim3(NT), 0, s, dg, from, c.T, D, counts, p.tiles, key, tok, z,
-                         za(2 * q + 1), za(2 * q + 2));
+      launch_kernel(embed_place_kernel<NT>, dim3(grid), dim3(NT), 0, s, dg, from, c.T, D, counts, p.tiles, key, tok, z,
+                    za(2 * q + 1), za(2 * q + 2));
     }
   };
   if (c.T <= kPairs) {
     const int blocks = (int)((c.T + 63) / 64), lds = (int)((c.T + 255) / 256 * 256 * 4);
     static std::atomic<uint64_t> lds_ok{0};
     allow_dyn_lds((const void*)embed_pairs_kernel, kPairs * 4, lds_ok);
-    hipLaunchKernelGGL(embed_pairs_kernel, dim3(blocks + zblocks), dim3(256), lds, s, ids, (int)c.T, c.V, blocks, key, tok, z,
-                       zeros);
+    launch_kernel(embed_pairs_kernel, dim3(blocks + zblocks), dim3(256), lds, s, ids, (int)c.T, c.V, blocks, key, tok, z,
+                  zeros);
   } else if (sort_threads(c.T) == kSortSmall) {
     radix(std::integral_constant<int, kSortSmall>{});
   } else {
@@ -350,12 +350,12 @@ void launch_embed_bwd(const moe_embed_cfg& c, const int32_t* ids, const void* dy
     using T = decltype(tag);
     const int nc = c.d_model / Vec<T>::N, slabs = (nc + kJoinCols - 1) / kJoinCols;
     each_launch(p.runs, nc, [&](int64_t r0, int64_t n) {
-      hipLaunchKernelGGL(embed_runs_kernel<T>, dim3((unsigned)((n * nc + 255) / 256)), dim3(256), 0, s, key, tok, (const T*)dy,
-                         (T*)dW, (float*)(w + p.part), c.T, r0, r0 + n, c.V, c.d_model, c.scale, c.accum);
+      launch_kernel(embed_runs_kernel<T>, dim3((unsigned)((n * nc + 255) / 256)), dim3(256), 0, s, key, tok, (const T*)dy,
+                    (T*)dW, (float*)(w + p.part), c.T, r0, r0 + n, c.V, c.d_model, c.scale, c.accum);
     });
     each_launch(p.runs - 1, (int64_t)slabs * 4 * kJoinCols, [&](int64_t r0, int64_t n) {
-      hipLaunchKernelGGL(embed_join_kernel<T>, dim3((unsigned)(n * slabs)), dim3(4 * kJoinCols), 0, s, key, (T*)dW,
-                         (const float*)(w + p.part), c.T, r0, p.runs, c.V, c.d_model, slabs, c.scale, c.accum);
+      launch_kernel(embed_join_kernel<T>, dim3((unsigned)(n * slabs)), dim3(4 * kJoinCols), 0, s, key, (T*)dW,
+                    (const float*)(w + p.part), c.T, r0, p.runs, c.V, c.d_model, slabs, c.scale, c.accum);
     });
   };
   if (c.dtype == MOE_BF16) go(uint16_t{});

@@ -601,7 +601,7 @@ template <typename T>
 static void launch_w4_combine(const moe_w4_cfg& c, const float* O, const int32_t* idx, const float* w, void* y, int splits,
                               hipStream_t s) {
   const dim3 grid((c.d_model + 1023) / 1024, (unsigned)std::min<int64_t>(c.T, 32768));
-  auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, O, idx, w, (T*)y, c.T, c.d_model, c.E, c.k); };
+  auto go = [&](auto kern) { launch_kernel(kern, grid, dim3(256), 0, s, O, idx, w, (T*)y, c.T, c.d_model, c.E, c.k); };
   auto choices = [&](auto sp) {
     constexpr int SP = decltype(sp)::value;
     if (c.k <= 2) go(w4_combine_kernel<T, SP, 2>);
@@ -967,8 +967,8 @@ static int launch_w4_rows(W4Args a, int gy, hipStream_t s) {
   if (2 * blocks * splits >= 3 * cus) {
     for (; a.tile0 < gy; a.tile0 += kMaxGridY)   // (only a list's tiles pass the grid's limit)
       how([&](auto h) {
-        hipLaunchKernelGGL((w4_rows_kernel<T, FIRST, NS, NO, FULL, decltype(h)::value>),
-                           dim3((a.N + 127) / 128, std::min(kMaxGridY, gy - a.tile0), splits), dim3(256), 0, s, a);
+        launch_kernel((w4_rows_kernel<T, FIRST, NS, NO, FULL, decltype(h)::value>),
+                      dim3((a.N + 127) / 128, std::min(kMaxGridY, gy - a.tile0), splits), dim3(256), 0, s, a);
       });
     return splits;
   }
@@ -985,7 +985,7 @@ static int launch_w4_rows(W4Args a, int gy, hipStream_t s) {
   how([&](auto h) {   // (gy is within a grid's limit: more tiles are blocks of 128 rows)
     constexpr int H = decltype(h)::value;
     auto go = [&](auto kern, size_t lds) {
-      hipLaunchKernelGGL(kern, dim3(a.N / (16 * rt), gy), dim3(64 * waves), waves * lds, s, a);
+      launch_kernel(kern, dim3(a.N / (16 * rt), gy), dim3(64 * waves), waves * lds, s, a);
     };
     if (rt == 2) go(w4_product_kernel<T, FIRST, NS, NO, 2, FULL, H>, sizeof(W4Lds<2>));
     else go(w4_product_kernel<T, FIRST, NS, NO, 1, FULL, H>, sizeof(W4Lds<1>));
@@ -1007,18 +1007,18 @@ static void launch_w4_gemm(const moe_w4_cfg& c, const void* x, const int32_t* id
   W4Group* tiles = (W4Group*)(base + L.tiles);
   int32_t* ntiles = (int32_t*)(base + L.ntiles);
   static_assert(sizeof(W4Group) == sizeof(W4Tile), "one table's room");
-  hipLaunchKernelGGL(w4_group_kernel, dim3(1), dim3(kW4ListThreads), 0, s, idx, n, c.E, choice_of, tiles, ntiles,
-                     (int)L.rows);
+  launch_kernel(w4_group_kernel, dim3(1), dim3(kW4ListThreads), 0, s, idx, n, c.E, choice_of, tiles, ntiles,
+                (int)L.rows);
   const int64_t pieces = L.rows * (w4_pad(d) / 8);
-  hipLaunchKernelGGL(w4_pack_kernel, dim3((unsigned)std::min<int64_t>((pieces + 255) / 256, 1 << 20)), dim3(256), 0, s,
-                     (const uint16_t*)x, (const int32_t*)choice_of, (uint16_t*)(base + L.x), d, c.k, pieces);
+  launch_kernel(w4_pack_kernel, dim3((unsigned)std::min<int64_t>((pieces + 255) / 256, 1 << 20)), dim3(256), 0, s,
+                (const uint16_t*)x, (const int32_t*)choice_of, (uint16_t*)(base + L.x), d, c.k, pieces);
   const int gy = std::min<int64_t>(n, c.E) + n / kGemmToks;
   const W4GemmArgs a{W1c, W1s, (const uint16_t*)(base + L.x), base + L.parts, choice_of, tiles, ntiles, f, d, n, c.act,
                      (d + kStep - 1) / kStep};
   const bool whole = d % kGemmRows == 0 && f % kGemmRows == 0;
   static_assert(kGemmRows == 128, "the padding of a layout's rows");
   auto go = [&](auto kern, int N, int splits, const W4GemmArgs& g) {
-    hipLaunchKernelGGL(kern, dim3(w4_pad(N) / kGemmRows, gy, splits), dim3(256), 0, s, g);
+    launch_kernel(kern, dim3(w4_pad(N) / kGemmRows, gy, splits), dim3(256), 0, s, g);
   };
   whole ? go(w4_gemm_kernel<true, true>, f, 1, a) : go(w4_gemm_kernel<true, false>, f, 1, a);
   // K is split where the blocks would not fill the CUs twice; whole steps, no split empty.
@@ -1044,7 +1044,7 @@ static void launch_w4_t(const moe_w4_cfg& c, const void* x, const int32_t* idx, 
   const bool scan = n <= kW4Scan;
   const int by_choice = scan && n < c.E;
   if (!scan)
-    hipLaunchKernelGGL(w4_list_kernel, dim3(1), dim3(kW4ListThreads), 0, s, idx, n, c.E, list, tiles, ntiles);
+    launch_kernel(w4_list_kernel, dim3(1), dim3(kW4ListThreads), 0, s, idx, n, c.E, list, tiles, ntiles);
   else
     tiles = nullptr;
   const int gy = !scan ? L.max_tiles : by_choice ? n : c.E;
@@ -1105,9 +1105,9 @@ void launch_w4_quantize(int64_t rows, int K, int dtype, const void* W, uint8_t* 
   if (groups == 0) return;
   const dim3 grid((unsigned)std::min<int64_t>((groups + 255) / 256, 1 << 16));
   if (dtype == MOE_BF16)
-    hipLaunchKernelGGL(w4_quantize_kernel<uint16_t>, grid, dim3(256), 0, s, (const uint16_t*)W, codes, scales, groups);
+    launch_kernel(w4_quantize_kernel<uint16_t>, grid, dim3(256), 0, s, (const uint16_t*)W, codes, scales, groups);
   else
-    hipLaunchKernelGGL(w4_quantize_kernel<float>, grid, dim3(256), 0, s, (const float*)W, codes, scales, groups);
+    launch_kernel(w4_quantize_kernel<float>, grid, dim3(256), 0, s, (const float*)W, codes, scales, groups);
 }
 
 }  // namespace lmoe

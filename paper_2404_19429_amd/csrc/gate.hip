@@ -214,8 +214,8 @@ template <typename T, int MT, int NT, int NWV, int KT>
 static void launch_gate_k(const moe_cfg& c, const void* x, const void* Wg, const float* bias, float* logits,
                           int32_t* idx, float* w, hipStream_t s) {
   const int64_t blocks = (c.T + 16 * MT - 1) / (16 * MT);
-  hipLaunchKernelGGL((gate_topk_kernel<T, MT, NT, NWV, KT>), dim3((unsigned)blocks), dim3(64 * NWV), 0, s,
-                     (const T*)x, (const T*)Wg, bias, logits, idx, w, c.T, c.d_model, c.E, c.k, c.renorm);
+  launch_kernel((gate_topk_kernel<T, MT, NT, NWV, KT>), dim3((unsigned)blocks), dim3(64 * NWV), 0, s,
+                (const T*)x, (const T*)Wg, bias, logits, idx, w, c.T, c.d_model, c.E, c.k, c.renorm);
 }
 // 32 tokens per block; 16 where that gives the CUs at most three blocks each (the
 // kernel is then latency: loads, a short MFMA chain, the sums, the selection).

@@ -277,8 +277,8 @@ static void launch_f32(const KernParams<EPI>& p, int groups, int64_t rows, int c
   const int tm = (int)((rows + (RAGGED_K ? 0 : 15) + 32 * WT - 1) / (32 * WT)), tn = (cols + 32 * WT - 1) / (32 * WT);
   const int64_t mt = all_rows > 0 ? (all_rows + 15 * groups) / (32 * WT) + groups : (int64_t)groups * tm;
   const int64_t blocks = RAGGED_K ? ((int64_t)groups * tm + 7) / 8 * 8 * tn : (mt * tn + 7) / 8 * 8;
-  hipLaunchKernelGGL((gemm_f32_kernel<WT, B_K, RAGGED_K, EPI>), dim3((unsigned)blocks), dim3(256), 0, s, p, tm, tn,
-                     groups);
+  launch_kernel((gemm_f32_kernel<WT, B_K, RAGGED_K, EPI>), dim3((unsigned)blocks), dim3(256), 0, s, p, tm, tn,
+                groups);
 }
 
 // --------------------------------------------------------------- launchers
@@ -851,8 +851,8 @@ void launch_xent_dx(int dtype, int64_t T, int d, int cols, const void* dl, int l
   if (n == 1 && f32_tile(w, num_cus()) == 32) launch_f32<1, false, false, EPI_ADD>(p, n, T, d, s);
   else launch_f32<2, false, false, EPI_ADD>(p, n, T, d, s);
   if (n > 1)
-    hipLaunchKernelGGL(xent_slices_kernel, dim3((unsigned)((T * d / 4 + 255) / 256)), dim3(256), 0, s, (const float*)part, n,
-                       T * d, acc_in, acc_out);
+    launch_kernel(xent_slices_kernel, dim3((unsigned)((T * d / 4 + 255) / 256)), dim3(256), 0, s, (const float*)part, n,
+                  T * d, acc_in, acc_out);
 }
 
 // dx where the vocabulary is one piece (bf16): no float sums to keep, and where the
@@ -930,8 +930,8 @@ void launch_xent_dw(int dtype, int64_t T, int d, int cols, const void* dl, int l
     q.p.sC = size;
     q.p.Aux = nullptr;
     run_rows_128x128(q, s);
-    hipLaunchKernelGGL(xent_ranges_kernel, dim3((unsigned)((size / 8 + 255) / 256)), dim3(256), 0, s, (const float*)part, n,
-                       size, scale, out);
+    launch_kernel(xent_ranges_kernel, dim3((unsigned)((size / 8 + 255) / 256)), dim3(256), 0, s, (const float*)part, n,
+                  size, scale, out);
   };
   const int64_t tn = (d + 255) / 256, tm = (cols + 255) / 256, main = tm * tn / cus * cus / tn * 256;
   // (half a round or more left: it is as well spent on 256-tiles)
@@ -983,8 +983,8 @@ void launch_dense_wgrad(int M, int N, int64_t K, const void* A, const void* B, v
   p.kchunk = (int)(((K + S - 1) / S + 31) / 32 * 32);
   run_wide_any(WideCall{WK_WGF32, MOE_ACT_IDENTITY, S, M, N, (double)std::min<int64_t>(K, p.kchunk), 0., p, beside},
                s);
-  hipLaunchKernelGGL(gemm_wgrad_reduce_kernel, dim3((unsigned)((MN / 8 + 255) / 256)), dim3(256), 0, s,
-                     (const float*)part, S, MN, (uint16_t*)C);
+  launch_kernel(gemm_wgrad_reduce_kernel, dim3((unsigned)((MN / 8 + 255) / 256)), dim3(256), 0, s,
+                (const float*)part, S, MN, (uint16_t*)C);
 }
 
 // Row-major [M][K] bf16 -> the blocked layout with pad16(M) rows (rows past M
@@ -1008,8 +1008,8 @@ __global__ __launch_bounds__(256) void pack_rows_kernel(const uint16_t* __restri
 void launch_pack_rows(const void* src, void* dst, int64_t M, int K, hipStream_t s) {
   if (M <= 0 || K <= 0) return;
   const int64_t blocks = pad16(M) / 16 * (K / 32);
-  hipLaunchKernelGGL(pack_rows_kernel, dim3((unsigned)((blocks * 64 + 255) / 256)), dim3(256), 0, s,
-                     (const uint16_t*)src, (uint16_t*)dst, M, K);
+  launch_kernel(pack_rows_kernel, dim3((unsigned)((blocks * 64 + 255) / 256)), dim3(256), 0, s,
+                (const uint16_t*)src, (uint16_t*)dst, M, K);
 }
 
 // Dense products on the wide MFMA kernel: one group of M rows, both operands

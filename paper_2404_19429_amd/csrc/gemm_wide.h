@@ -1366,12 +1366,12 @@ static void launch_wide(const WideCall& w, hipStream_t s) {
   if (SPLIT) blocks = std::min<int64_t>(blocks, kSkPartElems / (TC::BMT * TC::BN));   // partial tiles in the workspace
   if (!(SPLIT && p.ksplit == 2)) blocks = std::min(blocks, (int64_t)tm * tn * w.groups);
   blocks = (blocks + 7) / 8 * 8;
-  hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(TC::NW * 64), shmem, s, p, tm, tn, w.groups);
+  launch_kernel(kern, dim3((unsigned)blocks), dim3(TC::NW * 64), shmem, s, p, tm, tn, w.groups);
   if constexpr (SPLIT) {
     const int nslot = (int)blocks / 8;   // a K-split last round has at most nslot / 4 tiles per XCD
     if (nslot >= 4 && p.ksplit)
-      hipLaunchKernelGGL((gemm_wide_fixup_kernel<TC, EPI, ACT, CBLK>), dim3((unsigned)(8 * (nslot / 4) * TC::FM)),
-                         dim3(TC::NW * 64), 0, s, p, tm, tn, w.groups, nslot);
+      launch_kernel((gemm_wide_fixup_kernel<TC, EPI, ACT, CBLK>), dim3((unsigned)(8 * (nslot / 4) * TC::FM)),
+                    dim3(TC::NW * 64), 0, s, p, tm, tn, w.groups, nslot);
   }
 }
 

@@ -41,8 +41,17 @@ inline int num_cus() {
   return n;
 }
 
-// Threads of a launch at most.  A dispatch counts them in 32 bits: of 2^32 + n threads n run, without an error.  What
-// takes more goes in several launches.
+// A dispatch counts its threads in 32 bits: of 2^32 + n threads n run, without an error.  Such a launch is left out here,
+// and with it the later ones of the call, which returns MOE_ELAUNCH (check_launch in api.cpp).
+inline thread_local bool g_launch_refused = false;
+template <typename... P, typename... A>
+inline void launch_kernel(void (*kern)(P...), dim3 grid, dim3 block, size_t lds, hipStream_t s, A&&... args) {
+  auto fits = [](uint64_t blocks, uint64_t threads) { return blocks * threads < (uint64_t)1 << 32; };
+  if (!fits(grid.x, block.x) || !fits(grid.y, block.y) || !fits(grid.z, block.z)) g_launch_refused = true;
+  if (!g_launch_refused) hipLaunchKernelGGL(kern, grid, block, lds, s, static_cast<P>(args)...);
+}
+
+// Threads of a launch at most where work is split into several.
 constexpr int64_t kMostThreads = (int64_t)1 << 31;
 // f(begin, count) for items 0 .. n - 1 of `threads` threads each, as many at a time as a launch takes.
 template <typename F> inline void each_launch(int64_t n, int64_t threads, F&& f) {

@@ -105,8 +105,8 @@ static __global__ __launch_bounds__(kScanKeys * kScanParts) void sort_scan_kerne
 // The launch between counting and placing, if there is one.
 inline void launch_sort_scan(int32_t* counts, int64_t tiles, int D, hipStream_t s) {
   if (tiles > kSortSumTiles)
-    hipLaunchKernelGGL(sort_scan_kernel, dim3((unsigned)((D + kScanKeys - 1) / kScanKeys)), dim3(kScanKeys * kScanParts), 0, s,
-                       counts, tiles, D);
+    launch_kernel(sort_scan_kernel, dim3((unsigned)((D + kScanKeys - 1) / kScanKeys)), dim3(kScanKeys * kScanParts), 0, s,
+                  counts, tiles, D);
 }
 
 template <int NT>

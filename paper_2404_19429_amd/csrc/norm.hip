@@ -239,8 +239,8 @@ void launch_ln_fwd(const void* x, const void* g, const void* b, void* y, float* 
   const dim3 grid((unsigned)((T + 3) / 4));
   const int nc = ln_chunks(d);
 #define LMOE_LN_FWD(NC)                                                                                     \
-  hipLaunchKernelGGL(ln_fwd_kernel<NC>, grid, dim3(256), 0, s, (const uint16_t*)x, (const uint16_t*)g,      \
-                     (const uint16_t*)b, (uint16_t*)y, (uint16_t*)y_blk, mean, rstd, T, d, 1e-5)
+  launch_kernel(ln_fwd_kernel<NC>, grid, dim3(256), 0, s, (const uint16_t*)x, (const uint16_t*)g,           \
+                (const uint16_t*)b, (uint16_t*)y, (uint16_t*)y_blk, mean, rstd, T, d, 1e-5)
   if (nc == 1) LMOE_LN_FWD(1); else if (nc == 2) LMOE_LN_FWD(2); else if (nc == 4) LMOE_LN_FWD(4); else LMOE_LN_FWD(8);
 #undef LMOE_LN_FWD
 }
@@ -251,8 +251,8 @@ void launch_ln_bwd(const void* dyl, const void* x, const float* mean, const floa
   const dim3 grid((unsigned)ln_bwd_blocks(T));
   const int nc = ln_chunks(d);
 #define LMOE_LN_BWD(NC)                                                                                     \
-  hipLaunchKernelGGL(ln_bwd_kernel<NC>, grid, dim3(256), 0, s, (const uint16_t*)dyl, (const uint16_t*)x,    \
-                     mean, rstd, (const uint16_t*)g, (const uint16_t*)dres, (uint16_t*)dx, (uint16_t*)dx_blk, part, T, d, ln_bwd_rpw(T))
+  launch_kernel(ln_bwd_kernel<NC>, grid, dim3(256), 0, s, (const uint16_t*)dyl, (const uint16_t*)x,         \
+                mean, rstd, (const uint16_t*)g, (const uint16_t*)dres, (uint16_t*)dx, (uint16_t*)dx_blk, part, T, d, ln_bwd_rpw(T))
   if (nc == 1) LMOE_LN_BWD(1); else if (nc == 2) LMOE_LN_BWD(2); else if (nc == 4) LMOE_LN_BWD(4); else LMOE_LN_BWD(8);
 #undef LMOE_LN_BWD
 }
@@ -261,9 +261,9 @@ void launch_ln_gain_reduce(float* part, int64_t T, int d, float* dg, float* db, 
   const int nblk = T > 0 ? ln_bwd_blocks(T) : 0;
   const unsigned cols = (unsigned)((2 * d + 255) / 256);
   if (nblk > 0)
-    hipLaunchKernelGGL(ln_gain_run_kernel, dim3(cols, (unsigned)((nblk + kGainRun - 1) / kGainRun)), dim3(256), 0, s,
-                       part, nblk, d);
-  hipLaunchKernelGGL(ln_gain_reduce_kernel, dim3(cols), dim3(256), 0, s, (const float*)part, nblk, d, dg, db);
+    launch_kernel(ln_gain_run_kernel, dim3(cols, (unsigned)((nblk + kGainRun - 1) / kGainRun)), dim3(256), 0, s,
+                  part, nblk, d);
+  launch_kernel(ln_gain_reduce_kernel, dim3(cols), dim3(256), 0, s, (const float*)part, nblk, d, dg, db);
 }
 
 }  // namespace lmoe

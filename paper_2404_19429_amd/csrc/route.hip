@@ -305,7 +305,7 @@ static void row_launch(const moe_cfg& c, hipStream_t s, Args... args) {
   const int nc = c.d_model / Vec<T>::N;
   auto go = [&](auto kern, int U) {
     const int64_t n = (c.T + U - 1) / U * nc;
-    hipLaunchKernelGGL(kern, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, args...);
+    launch_kernel(kern, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, args...);
   };
   const bool uni = nc % kWave == 0 && c.T < ((int64_t)1 << 30);
   auto pick = [&](auto ucst) {
@@ -340,8 +340,8 @@ static void dispatch_walk(const moe_cfg& c, const void* x, const int32_t* idx, c
   if (nch == 1 && sb * c.k < (int64_t)16 * num_cus()) {
     auto go = [&](auto tag) {
       using T = decltype(tag);
-      hipLaunchKernelGGL(dispatch_small_kernel<T>, dim3((unsigned)sb), dim3(kRouteChunk), 0, s, (const T*)x, idx, perm,
-                         carry, fill, slot, (T*)send_buf, (int)c.T, c.d_model, c.E, c.k, c.C);
+      launch_kernel(dispatch_small_kernel<T>, dim3((unsigned)sb), dim3(kRouteChunk), 0, s, (const T*)x, idx, perm,
+                    carry, fill, slot, (T*)send_buf, (int)c.T, c.d_model, c.E, c.k, c.C);
     };
     if (c.dtype == MOE_BF16) go(uint16_t{});
     else go(float{});
@@ -363,11 +363,11 @@ static void dispatch_walk(const moe_cfg& c, const void* x, const int32_t* idx, c
   const bool fused = nch > 0 && (uni ? nch <= kWave : nch <= 8 && nch * c.k <= 24);
   const int nfused = fused ? (int)nch : 0;
   if (nch > 0)
-    hipLaunchKernelGGL(route_rank_kernel, dim3((unsigned)nch), dim3(kRouteChunk), 0, s, idx, perm, counts, rank, c.T,
-                       c.E, c.k);
+    launch_kernel(route_rank_kernel, dim3((unsigned)nch), dim3(kRouteChunk), 0, s, idx, perm, counts, rank, c.T,
+                  c.E, c.k);
   if (c.E > 0 && !fused)
-    hipLaunchKernelGGL(route_scan_kernel, dim3((unsigned)c.E), dim3(64), 0, s, counts, base, carry, fill, (int)nch, c.E,
-                       c.C);
+    launch_kernel(route_scan_kernel, dim3((unsigned)c.E), dim3(64), 0, s, counts, base, carry, fill, (int)nch, c.E,
+                  c.C);
   if (nch == 0) return;
   if (c.dtype == MOE_BF16)
     row_launch<DispatchCopy, uint16_t, 4, 2>(c, s, (const uint16_t*)x, idx, perm, rank, (const int32_t*)base, slot,
@@ -740,7 +740,7 @@ void launch_dispatch_bpr(const moe_cfg& c, const void* x, const float* logits, c
   uint64_t* spl = (uint64_t*)(w + 2 * eb + tb);
   if (c.T > 0) {
     auto keys = [&](auto kern) {
-      hipLaunchKernelGGL(kern, dim3((unsigned)((c.T + 3) / 4)), dim3(256), 0, s, logits, idx, e0, c.T, c.E, c.k);
+      launch_kernel(kern, dim3((unsigned)((c.T + 3) / 4)), dim3(256), 0, s, logits, idx, e0, c.T, c.E, c.k);
     };
     if (score == MOE_SCORE_SOFTMAX) keys(bpr_key_kernel<MOE_SCORE_SOFTMAX>);
     else keys(bpr_key_kernel<MOE_SCORE_SIGMOID>);
@@ -749,11 +749,11 @@ void launch_dispatch_bpr(const moe_cfg& c, const void* x, const float* logits, c
       static std::atomic<uint64_t> lds_ok{0};
       allow_dyn_lds((const void*)bpr_tile_sort_kernel<ST>, (int)ST::kLds, lds_ok);
       const int64_t ntiles = (c.T + ST::kTile - 1) / ST::kTile;
-      hipLaunchKernelGGL(bpr_tile_sort_kernel<ST>, dim3((unsigned)ntiles), dim3(ST::kThreads), ST::kLds, s, e0, e1, spl,
-                         ntiles == 1 ? perm : (int32_t*)nullptr, c.T);
+      launch_kernel(bpr_tile_sort_kernel<ST>, dim3((unsigned)ntiles), dim3(ST::kThreads), ST::kLds, s, e0, e1, spl,
+                    ntiles == 1 ? perm : (int32_t*)nullptr, c.T);
       if (ntiles > 1)
-        hipLaunchKernelGGL(bpr_merge_kernel<ST>, dim3((unsigned)((c.T + 255) / 256)), dim3(256), 0, s, e1, spl, perm,
-                           c.T);
+        launch_kernel(bpr_merge_kernel<ST>, dim3((unsigned)((c.T + 255) / 256)), dim3(256), 0, s, e1, spl, perm,
+                      c.T);
     };
     if (c.T <= SortSmall::kTile) sort(SortSmall{});
     else if (c.T <= SortMid::kTile || (c.T > SortLarge::kTile && c.T <= 4 * SortLarge::kTile)) sort(SortMid{});
@@ -944,8 +944,8 @@ void launch_combine_bwd(const moe_cfg& c, const float* logits, const int32_t* id
   const unsigned blocks = (unsigned)((c.T + 3) / 4);
   auto go = [&](auto kern, auto tag, float* out) {
     using T = decltype(tag);
-    hipLaunchKernelGGL(kern, dim3(blocks), dim3(256), 0, s, logits, idx, w, slot, (const T*)O, (const T*)dy,
-                       (T*)dO, out, c.T, c.d_model, c.E, c.k, c.C, c.renorm);
+    launch_kernel(kern, dim3(blocks), dim3(256), 0, s, logits, idx, w, slot, (const T*)O, (const T*)dy,
+                  (T*)dO, out, c.T, c.d_model, c.E, c.k, c.C, c.renorm);
   };
   auto pick = [&](auto kt) {
     constexpr int KT = decltype(kt)::value;
@@ -1261,11 +1261,11 @@ static void launch_dwg_eg(const moe_cfg& c, const void* x, const float* dl, floa
                           hipStream_t s) {
   dim3 grid((unsigned)q.slabs, (unsigned)q.nch, (unsigned)q.egroups);
   if (c.renorm)
-    hipLaunchKernelGGL((dwg_partial_kernel<T, EG, true>), grid, dim3(64 * kDwgWaves), 0, s, (const T*)x, dl, part,
-                       c.T, c.d_model, c.E, q.tch);
+    launch_kernel((dwg_partial_kernel<T, EG, true>), grid, dim3(64 * kDwgWaves), 0, s, (const T*)x, dl, part,
+                  c.T, c.d_model, c.E, q.tch);
   else
-    hipLaunchKernelGGL((dwg_partial_kernel<T, EG, false>), grid, dim3(64 * kDwgWaves), 0, s, (const T*)x, dl, part,
-                       c.T, c.d_model, c.E, q.tch);
+    launch_kernel((dwg_partial_kernel<T, EG, false>), grid, dim3(64 * kDwgWaves), 0, s, (const T*)x, dl, part,
+                  c.T, c.d_model, c.E, q.tch);
 }
 template <typename T>
 static void launch_dwg_t(const moe_cfg& c, const void* x, const float* dl, float* part, const DwgPlan& q,
@@ -1283,7 +1283,7 @@ void launch_dwg(const moe_cfg& c, const void* x, const float* dlogits, float* dW
     if (c.dtype == MOE_BF16) launch_dwg_t<uint16_t>(c, x, dlogits, part, q, s);
     else launch_dwg_t<float>(c, x, dlogits, part, q, s);
   }
-  if (q.nch != 1) hipLaunchKernelGGL(dwg_reduce_kernel, dim3((unsigned)((ed / 4 + 31) / 32)), dim3(32 * kDwgRuns), 0, s, part,
+  if (q.nch != 1) launch_kernel(dwg_reduce_kernel, dim3((unsigned)((ed / 4 + 31) / 32)), dim3(32 * kDwgRuns), 0, s, part,
                      dWg, (int)q.nch, ed);
 }
 
@@ -1340,8 +1340,8 @@ void launch_pack_weights(const moe_cfg& c, const void* W1, const void* W2, void*
   if (c.dtype == MOE_BF16) {
     const int64_t nb = E * f * d / 4096;
     auto go = [&](int64_t b1, int64_t b2) {
-      hipLaunchKernelGGL(pack_blocked_kernel, dim3((unsigned)(b1 + b2)), dim3(512), 0, s, (const uint16_t*)W1,
-                         (uint16_t*)W1p, (uint32_t)d, b1, (const uint16_t*)W2, (uint16_t*)W2p, (uint32_t)f);
+      launch_kernel(pack_blocked_kernel, dim3((unsigned)(b1 + b2)), dim3(512), 0, s, (const uint16_t*)W1,
+                    (uint16_t*)W1p, (uint32_t)d, b1, (const uint16_t*)W2, (uint16_t*)W2p, (uint32_t)f);
     };
     if (2 * nb <= 1 << 22 && !over) {
       go(nb, nb);
@@ -1354,8 +1354,8 @@ void launch_pack_weights(const moe_cfg& c, const void* W1, const void* W2, void*
     auto go = [&](bool one, bool two) {
       for (int64_t o = 0; o < n; o += most) {
         const int64_t m = std::min(n - o, most), b = (m + 255) / 256;
-        hipLaunchKernelGGL(copy_weights_kernel, dim3((unsigned)((one ? b : 0) + (two ? b : 0))), dim3(256), 0, s,
-                           (const u32x4*)W1 + o, (u32x4*)W1p + o, one ? b : 0, (const u32x4*)W2 + o, (u32x4*)W2p + o, m);
+        launch_kernel(copy_weights_kernel, dim3((unsigned)((one ? b : 0) + (two ? b : 0))), dim3(256), 0, s,
+                      (const u32x4*)W1 + o, (u32x4*)W1p + o, one ? b : 0, (const u32x4*)W2 + o, (u32x4*)W2p + o, m);
       }
     };
     go(true, !over);

@@ -561,7 +561,7 @@ static void launch_route_n(const RouteArgs& a, hipStream_t s) {
     RouteArgs b = a;
     for (b.first = 0; b.first < a.T; b.first += most) {
       const int64_t n = std::min(a.T - b.first, most);
-      hipLaunchKernelGGL(kern, dim3((unsigned)((n + tokens - 1) / tokens)), dim3(64 * kRouteWaves), 0, s, b);
+      launch_kernel(kern, dim3((unsigned)((n + tokens - 1) / tokens)), dim3(64 * kRouteWaves), 0, s, b);
     }
   };
   if (a.k <= 2) go(route_kernel<LPT, NCH, 2, GROUPS>);
@@ -579,7 +579,7 @@ void launch_route(const moe_route_cfg& c, const float* logits, const float* bias
   // 65536 71 where it takes 9.4.)
   if (c.E < 4 || (c.groups > 1 && (c.groups > kRouteGroupsFast || (c.E / c.groups) % 4 != 0))) {
     const unsigned blocks = (unsigned)std::min<int64_t>((c.T + 3) / 4, 8 * num_cus());
-    auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(blocks), dim3(256), 0, s, a); };
+    auto go = [&](auto kern) { launch_kernel(kern, dim3(blocks), dim3(256), 0, s, a); };
     if (c.E <= 64) go(route_exact_kernel<1>);
     else if (c.E <= 128) go(route_exact_kernel<2>);
     else if (c.E <= 256) go(route_exact_kernel<4>);
@@ -605,7 +605,7 @@ void launch_route(const moe_route_cfg& c, const float* logits, const float* bias
   if (load) {
     const int64_t n = c.T * c.k;
     const unsigned blocks = (unsigned)std::min<int64_t>((n + 4 * kLoadThreads - 1) / (4 * kLoadThreads), 64);
-    hipLaunchKernelGGL(route_load_kernel, dim3(blocks), dim3(kLoadThreads), 0, s, (const int32_t*)idx, n, c.E, load);
+    launch_kernel(route_load_kernel, dim3(blocks), dim3(kLoadThreads), 0, s, (const int32_t*)idx, n, c.E, load);
   }
 }
 
@@ -728,7 +728,7 @@ void launch_route_bwd(const moe_route_cfg& c, const float* logits, const int32_t
   };
   if (c.score == MOE_SCORE_SOFTMAX && !c.renorm) {
     auto go = [&](auto kern) {
-      slices(4, [&](const RouteBwdArgs& b, dim3 grid) { hipLaunchKernelGGL(kern, grid, dim3(64 * kBwdWaves), 0, s, b); });
+      slices(4, [&](const RouteBwdArgs& b, dim3 grid) { launch_kernel(kern, grid, dim3(64 * kBwdWaves), 0, s, b); });
     };
     if (c.E <= 16) go(route_bwd_softmax_kernel<1>);
     else if (c.E <= 64) go(route_bwd_softmax_kernel<4>);
@@ -743,7 +743,7 @@ void launch_route_bwd(const moe_route_cfg& c, const float* logits, const int32_t
   while (tokens * 2 * kp <= kWave && tokens * 2 * c.E <= kBwdLds) tokens *= 2;
   auto go = [&](auto kern) {
     slices(tokens, [&](const RouteBwdArgs& b, dim3 grid) {
-      hipLaunchKernelGGL(kern, grid, dim3(64 * kBwdWaves), 0, s, b, tokens);
+      launch_kernel(kern, grid, dim3(64 * kBwdWaves), 0, s, b, tokens);
     });
   };
   if (kp == 1) go(route_bwd_kernel<1>);

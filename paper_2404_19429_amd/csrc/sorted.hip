@@ -154,10 +154,10 @@ void launch_sorted_dispatch(const moe_sorted_cfg& c, const void* x, const int32_
   auto place = [&](auto nt) {
     constexpr int NT = decltype(nt)::value;
     if (tiles > 1)
-      hipLaunchKernelGGL(sorted_count_kernel<NT>, dim3((unsigned)tiles), dim3(NT), 0, s, idx, N, c.E, counts);
+      launch_kernel(sorted_count_kernel<NT>, dim3((unsigned)tiles), dim3(NT), 0, s, idx, N, c.E, counts);
     launch_sort_scan(counts, tiles, c.E, s);
-    hipLaunchKernelGGL(sorted_place_kernel<NT>, dim3((unsigned)tiles), dim3(NT), 0, s, idx, N, c.E, align, R, counts, row_begin,
-                       row_end, slot, src);
+    launch_kernel(sorted_place_kernel<NT>, dim3((unsigned)tiles), dim3(NT), 0, s, idx, N, c.E, align, R, counts, row_begin,
+                  row_end, slot, src);
   };
   auto go = [&](auto tag) {
     using T = decltype(tag);
@@ -166,17 +166,17 @@ void launch_sorted_dispatch(const moe_sorted_cfg& c, const void* x, const int32_
     const int64_t strips = (R + 15) / 16, waves = strips * cols;   // of sixteen rows
     if (tiles == 1 && N > 0) {
       const unsigned blocks = (unsigned)std::min<int64_t>(256, (waves + 3) / 4);
-      hipLaunchKernelGGL((sorted_small_kernel<T, U>), dim3(blocks), dim3(kSortSmall), 0, s, (const T*)x, idx, (int)N, c.E, align,
-                         (int)R, row_begin, row_end, slot, src, (T*)rows, c.d_model, c.k, cols);
+      launch_kernel((sorted_small_kernel<T, U>), dim3(blocks), dim3(kSortSmall), 0, s, (const T*)x, idx, (int)N, c.E, align,
+                    (int)R, row_begin, row_end, slot, src, (T*)rows, c.d_model, c.k, cols);
       return;
     }
     if (sort_threads(N) == kSortSmall) place(std::integral_constant<int, kSortSmall>{});
     else place(std::integral_constant<int, kSortLarge>{});
     auto gather = [&](auto stream) {
       each_launch(strips, (int64_t)cols * kWave, [&](int64_t b, int64_t n) {   // (rows of whole strips lie together)
-        hipLaunchKernelGGL((sorted_gather_kernel<T, U, decltype(stream)::value>), dim3((unsigned)((n * cols + 3) / 4)),
-                           dim3(256), 0, s, (const T*)x, src + 16 * b, (T*)rows + 16 * b * c.d_model,
-                           std::min(16 * n, R - 16 * b), N, c.d_model, c.k, cols);
+        launch_kernel((sorted_gather_kernel<T, U, decltype(stream)::value>), dim3((unsigned)((n * cols + 3) / 4)),
+                      dim3(256), 0, s, (const T*)x, src + 16 * b, (T*)rows + 16 * b * c.d_model,
+                      std::min(16 * n, R - 16 * b), N, c.d_model, c.k, cols);
       });
     };
     if (R == 0) return;
@@ -252,10 +252,10 @@ static void launch_back(const moe_sorted_cfg& c, const void* rows, const int32_t
     using T = decltype(tag);
     const int64_t nc = c.d_model / Vec<T>::N;
     each_launch(c.T, nc, [&](int64_t t0, int64_t n) {
-      hipLaunchKernelGGL((sorted_back_kernel<T, W, decltype(gate)::value, decltype(stream)::value>),
-                         dim3((unsigned)((n * nc + 255) / 256)), dim3(256), 0, s, (const T*)rows, slot + t0 * c.k,
-                         W ? w + t0 * c.k : nullptr, (const T*)Wg, dl ? dl + t0 * c.E : nullptr, (T*)y + t0 * c.d_model, n,
-                         sorted_rows(c), c.d_model, c.k, c.E);
+      launch_kernel((sorted_back_kernel<T, W, decltype(gate)::value, decltype(stream)::value>),
+                    dim3((unsigned)((n * nc + 255) / 256)), dim3(256), 0, s, (const T*)rows, slot + t0 * c.k,
+                    W ? w + t0 * c.k : nullptr, (const T*)Wg, dl ? dl + t0 * c.E : nullptr, (T*)y + t0 * c.d_model, n,
+                    sorted_rows(c), c.d_model, c.k, c.E);
     });
   };
   auto type = [&](auto gate, auto stream) {
@@ -362,9 +362,9 @@ void launch_sorted_combine_bwd(const moe_sorted_cfg& c, const void* O, const int
     using T = decltype(tag);
     each_launch((R + 15) / 16, 256, [&](int64_t b, int64_t n) {   // (beside N threads at most: together under 2^32)
       const int64_t r0 = 16 * b, zeros = b == 0 ? (N + 255) / 256 : 0;
-      hipLaunchKernelGGL((sorted_combine_bwd_kernel<T, 2, decltype(stream)::value>), dim3((unsigned)(n + zeros)), dim3(256), 0, s,
-                         (const T*)O + r0 * c.d_model, slot, src + r0, w, (const T*)dy, (T*)dO + r0 * c.d_model, dw,
-                         std::min(16 * n, R - r0), R, N, c.d_model, c.k);
+      launch_kernel((sorted_combine_bwd_kernel<T, 2, decltype(stream)::value>), dim3((unsigned)(n + zeros)), dim3(256), 0, s,
+                    (const T*)O + r0 * c.d_model, slot, src + r0, w, (const T*)dy, (T*)dO + r0 * c.d_model, dw,
+                    std::min(16 * n, R - r0), R, N, c.d_model, c.k);
     });
   };
   auto type = [&](auto stream) {

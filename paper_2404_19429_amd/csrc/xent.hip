@@ -215,8 +215,8 @@ __global__ __launch_bounds__(256) void xent_zero_kernel(u32x4* z, int64_t n) {
 void launch_pack(const void* src, const int32_t* target, void* dst, int64_t rows, int V, int d, hipStream_t s,
                  const float* g = nullptr, float* scale = nullptr) {
   const int64_t blocks = (pad16(rows) / 16 * (d / 32) * 64 + 255) / 256 + (scale ? 1 : 0);
-  hipLaunchKernelGGL(xent_pack_kernel, dim3((unsigned)blocks), dim3(256), 0, s, (const uint16_t*)src, target,
-                     (uint16_t*)dst, rows, V, d, g, scale);
+  launch_kernel(xent_pack_kernel, dim3((unsigned)blocks), dim3(256), 0, s, (const uint16_t*)src, target,
+                (uint16_t*)dst, rows, V, d, g, scale);
 }
 
 }  // namespace
@@ -255,8 +255,8 @@ void launch_xent(const moe_xent_cfg& c, const void* x, const void* W, const int3
   // Rows a block: enough blocks for every CU, 64 bytes of a run's rows at least where there are as many.
   int tx = 1;
   while (tx < 64 && tx < c.T && (tx < 8 || c.T >= (int64_t)1024 * tx)) tx *= 2;
-  hipLaunchKernelGGL(xent_join_kernel, dim3((unsigned)((c.T + tx - 1) / tx)), dim3(256), 0, s, xp.part, xp.tl, target,
-                     xp.block0, c.T, c.V, tx, loss, lse);
+  launch_kernel(xent_join_kernel, dim3((unsigned)((c.T + tx - 1) / tx)), dim3(256), 0, s, xp.part, xp.tl, target,
+                xp.block0, c.T, c.V, tx, loss, lse);
 }
 
 void launch_xent_bwd(const moe_xent_cfg& c, const void* x, const void* W, const int32_t* target, const float* lse,
@@ -265,8 +265,8 @@ void launch_xent_bwd(const moe_xent_cfg& c, const void* x, const void* W, const 
   if (c.T == 0) {
     const int64_t n = c.V * d * e / 16;
     if (dW)
-      hipLaunchKernelGGL(xent_zero_kernel, dim3((unsigned)std::min<int64_t>(4096, (n + 255) / 256)), dim3(256), 0, s,
-                         (u32x4*)dW, n);
+      launch_kernel(xent_zero_kernel, dim3((unsigned)std::min<int64_t>(4096, (n + 255) / 256)), dim3(256), 0, s,
+                    (u32x4*)dW, n);
     return;
   }
   const BwdPlan p = bwd_plan(c);
@@ -276,8 +276,8 @@ void launch_xent_bwd(const moe_xent_cfg& c, const void* x, const void* W, const 
   if (bf)
     launch_pack(x, target, xp_, c.T, c.V, (int)d, s, dloss, (float*)(w + p.scale));
   else
-    hipLaunchKernelGGL(xent_copy_kernel, dim3((unsigned)((c.T * d / 4 + 255) / 256)), dim3(256), 0, s, (const float*)x,
-                       target, (float*)xp_, c.T, c.V, (int)d);
+    launch_kernel(xent_copy_kernel, dim3((unsigned)((c.T * d / 4 + 255) / 256)), dim3(256), 0, s, (const float*)x,
+                  target, (float*)xp_, c.T, c.V, (int)d);
   XentParams xp{};
   xp.target = target;
   xp.lse = lse;
