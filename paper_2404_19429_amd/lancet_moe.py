@@ -813,7 +813,10 @@ def alloc_lm(cfg: moe_block_cfg, V: int, n_blocks: int = 1, scale: float = 1.0, 
     T, d, bf = m.T, m.d_model, torch.bfloat16
     embed, xent = make_embed_cfg(T, V, d, "bf16", scale), make_xent_cfg(T, V, d, "bf16")
     e = lambda *s, dtype=bf: torch.empty(*s, dtype=dtype, device=device)
-    need = max(moe_embed_bwd_workspace_bytes(embed), moe_xent_workspace_bytes(xent), moe_xent_workspace_bytes(xent, True))
+    sizes = [moe_embed_bwd_workspace_bytes(embed), moe_xent_workspace_bytes(xent), moe_xent_workspace_bytes(xent, True)]
+    if T > 0 and 0 in sizes:   # (tokens need some of each; the message is of the last one refused)
+        raise MoeError(MOE_ESHAPE, moe_last_error())
+    need = max(sizes)
     return LmBuffers(embed=embed, embed_add=make_embed_cfg(T, V, d, "bf16", scale, accum=1), xent=xent,
                      h=[e(T, d) for _ in range(n_blocks + 1)], loss=e(T, dtype=torch.float32),
                      lse=e(T, dtype=torch.float32), dh=e(T, d), dx=e(T, d), dWout=e(V, d),

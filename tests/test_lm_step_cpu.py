@@ -1,0 +1,22 @@
+"""What the step of lookup, blocks and loss refuses before anything runs."""
+import pytest
+import torch
+
+L = pytest.importorskip("paper_2404_19429_amd.lancet_moe", reason="library not built")
+
+
+def _cfg(B=2, S=16, heads=1):
+    return L.make_block_cfg(B, S, heads, 64, 2, 1, 64)
+
+
+@pytest.mark.parametrize("cfg,V,scale", [(_cfg(B=1 << 12, S=1 << 12, heads=8), 100, 1.0),     # 2^34 elements of x
+                                         (_cfg(), 0, 1.0), (_cfg(), 100, float("inf")), (_cfg(), (1 << 30) + 1, 1.0)])
+def test_sizes_that_the_calls_do_not_take(monkeypatch, cfg, V, scale):
+    monkeypatch.setattr(torch, "empty", lambda *a, **k: pytest.fail("allocated"))
+    with pytest.raises(L.MoeError):
+        L.alloc_lm(cfg, V, scale=scale, device="cpu")
+
+
+def test_no_tokens_are_allowed():
+    assert L.alloc_lm(_cfg(B=0), 100, device="cpu").ws.numel() == 16
+
