@@ -823,9 +823,15 @@ def alloc_lm(cfg: moe_block_cfg, V: int, n_blocks: int = 1, scale: float = 1.0, 
                      dWin=None if tied else e(V, d), ws=e(max(16, need), dtype=torch.uint8))
 
 
+def _lm_blocks(b: LmBuffers, *per_block):
+    if any(len(q) != len(b.h) - 1 for q in per_block):
+        raise ValueError(f"{len(b.h) - 1} blocks were allocated, got {[len(q) for q in per_block]}")
+
+
 def lm_forward(b: LmBuffers, cfg: moe_block_cfg, ids, target, Win, Wout, weights: list, acts: list, n_chunks: int, streams):
     """Token lookup -> blocks -> cross entropy of every token (b.loss).  weights, acts: of each block (block_shapes,
     alloc_block); ids, target [T] int32.  streams as for moe_block_chunked; the rest runs on the first."""
+    _lm_blocks(b, weights, acts)
     moe_embed(b.embed, ids, Win, b.h[0], streams[0])
     for i, (w, a) in enumerate(zip(weights, acts)):
         moe_block_chunked(cfg, w, None, b.h[i], b.h[i + 1], None, None, a, MOE_BLOCK_FWD, n_chunks, streams, a["ws"])
@@ -836,6 +842,7 @@ def lm_backward(b: LmBuffers, cfg: moe_block_cfg, ids, target, Wout, weights: li
                 n_chunks: int, streams):
     """After lm_forward: dloss [T] float (1 / n for the mean of n tokens) -> b.dWout, every block's grads, and the
     table's gradient in b.dWin, or added to b.dWout where the two are tied."""
+    _lm_blocks(b, weights, grads, acts)
     moe_xent_bwd(b.xent, b.h[-1], Wout, target, b.lse, dloss, b.dh, b.dWout, b.ws, streams[0])
     dy, dx = b.dh, b.dx
     for i in reversed(range(len(weights))):

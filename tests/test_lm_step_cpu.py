@@ -20,3 +20,14 @@ def test_sizes_that_the_calls_do_not_take(monkeypatch, cfg, V, scale):
 def test_no_tokens_are_allowed():
     assert L.alloc_lm(_cfg(B=0), 100, device="cpu").ws.numel() == 16
 
+
+@pytest.mark.parametrize("weights,acts", [(1, 2), (2, 1), (1, 1), (3, 3)])
+def test_other_numbers_of_blocks(monkeypatch, weights, acts):
+    b = L.alloc_lm(_cfg(), 100, n_blocks=2, device="cpu")
+    for n in ("moe_embed", "moe_xent", "moe_xent_bwd", "moe_block_chunked", "moe_embed_bwd"):
+        monkeypatch.setattr(L, n, lambda *a, **k: pytest.fail("called"))
+    w, a = [{}] * weights, [{"ws": None}] * acts
+    with pytest.raises(ValueError):
+        L.lm_forward(b, _cfg(), None, None, None, None, w, a, 1, [None] * 3)
+    with pytest.raises(ValueError):
+        L.lm_backward(b, _cfg(), None, None, None, w, w, a, None, 1, [None] * 3)
