@@ -41,7 +41,10 @@
  *     (expert_out, dXe) are row-major: (e, r, c) at (e*Cp + r)*X + c, so a
  *     row is one contiguous run.  For MOE_F32 every buffer is row-major.
  *   - A device other than gfx950 gives MOE_EDEVICE; a failed launch
- *     MOE_ELAUNCH.
+ *     MOE_ELAUNCH, and so do sizes that need a launch of 2^32 threads or more
+ *     (the layer's calls from 2^26 tokens on, at the earliest; the sorted
+ *     rows', lookup's and loss's split theirs): some of the call's launches
+ *     may have run then.
  *
  * Layouts (nn.Linear [out][in]): Wg [E][d], W1 [E][f][d], W2 [E][d][f]
  * (row-major; the expert GEMMs take copies made by moe_pack_weights).
@@ -564,7 +567,9 @@ size_t moe_xent_workspace_bytes(const moe_xent_cfg* cfg, int32_t backward);
 /* x [T][d], W [V][d] dtype, target [T] int32 -> lse [T] float = log sum over v of
  * exp(<x_t, W_v>) of every token, loss [T] float = lse[t] - <x_t, W_target>, 0 where the
  * target is outside 0..V-1 (padding, tokens that do not count).  Products and sums in
- * float, logits not rounded in between. */
+ * float, logits not rounded in between; their exponents are taken in base 2, so a row's
+ * largest logit has to be under 2^127 in size (past that lse may be NaN).  lse and loss are
+ * as exact as a float of the size of lse (a sure token's loss may be that much below 0). */
 moe_status moe_xent(const moe_xent_cfg* cfg, const void* x, const void* W, const int32_t* target, float* loss,
                     float* lse, void* ws, size_t ws_bytes, moe_stream_t stream);
 
@@ -572,8 +577,9 @@ moe_status moe_xent(const moe_xent_cfg* cfg, const void* x, const void* W, const
  *   dx [T][d] dtype = sum over v of dl[t][v] W_v, dW [V][d] dtype = sum over t of
  *   dl[t][v] x_t, dl[t][v] = dloss[t] (exp(<x_t, W_v> - lse[t]) - [v = target[t]]); the
  *   rows of tokens whose target is outside 0..V-1 are 0 in dx and take no part in dW,
- *   whatever their x, lse and dloss hold.  dx or dW may be NULL (not wanted).  dl is
- *   rounded to dtype, sums are float.  The same call gives the same bits. */
+ *   whatever their x, lse and dloss hold.  dx or dW may be NULL (not wanted); both are
+ *   written, not added to.  dl is rounded to dtype, sums are float.  The same call gives
+ *   the same bits. */
 moe_status moe_xent_bwd(const moe_xent_cfg* cfg, const void* x, const void* W, const int32_t* target,
                         const float* lse, const float* dloss, void* dx, void* dW, void* ws, size_t ws_bytes,
                         moe_stream_t stream);

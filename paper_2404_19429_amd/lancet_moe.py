@@ -790,7 +790,7 @@ def alloc_block(cfg: moe_block_cfg, n_chunks: int, device="cuda", names=None) ->
     return out
 
 
-# ----------------------------------------------------- a model step around the block
+# ----------------------------------------------------- lookup and loss around the block
 @dataclass
 class LmBuffers:
     """What a step of token lookup, blocks and loss keeps beside the blocks' own buffers."""
@@ -829,7 +829,8 @@ def _lm_blocks(b: LmBuffers, *per_block):
 
 
 def lm_forward(b: LmBuffers, cfg: moe_block_cfg, ids, target, Win, Wout, weights: list, acts: list, n_chunks: int, streams):
-    """Token lookup -> blocks -> cross entropy of every token (b.loss).  weights, acts: of each block (block_shapes,
+    """Token lookup -> blocks (with a capacity) -> cross entropy of every token (b.loss), which takes the last block's
+    output as it is: a norm in front of the output matrix is the caller's, with moe_xent called behind it.  weights, acts: of each block (block_shapes,
     alloc_block); ids, target [T] int32.  streams as for moe_block_chunked; the rest runs on the first."""
     _lm_blocks(b, weights, acts)
     moe_embed(b.embed, ids, Win, b.h[0], streams[0])
